@@ -46,7 +46,9 @@ typedef enum {
     FPDE_ERR_COEFF_COUNT = 7,  /* ncoeffs does not match the operator                        */
     FPDE_ERR_BC = 8,           /* boundary kinds not supported by the operator               */
     FPDE_ERR_WORKSPACE = 9,    /* workspace NULL, misaligned or smaller than required        */
-    FPDE_ERR_CUDA = 10         /* the CUDA runtime reported an error                         */
+    FPDE_ERR_CUDA = 10,        /* the CUDA runtime reported an error                         */
+    FPDE_ERR_DTYPE = 11,       /* element type not one of fpde_dtype                         */
+    FPDE_ERR_PARAM = 12        /* a setting (width, states, steps, ...) outside its range    */
 } fpde_status;
 
 /*
@@ -446,6 +448,152 @@ unsigned int fpde_diag_tma_timeouts(void);
  * on a 128-byte boundary.
  */
 int fpde_diag_ns_tma_geometry(const int64_t* shape, int tile_rows, int narrays, size_t smem_limit);
+
+/* ================================================================================================
+ * Operators of the network and the optimiser around the residual loss.
+ *
+ * A network that marches fields along one axis of the grid treats every other axis as its batch: a
+ * row of `length` nodes with `channels` features per node.  Its mixer is a short causal convolution
+ * followed by a selective state space scan; its weight matrices are updated with orthogonalised
+ * momentum.  (The paper leaves network and optimiser to PyTorch; nothing here has a counterpart in it.)
+ *
+ * Rules on top of the general ones above
+ *   - Activations are fp32, bf16 or fp16 (fpde_dtype); everything is computed in fp32 and rounded
+ *     once, when it is stored.  Parameters, states and their gradients are fp32.
+ *   - Activation inputs are (batch, length, channels) views: the channel axis is contiguous, the
+ *     batch and node strides are given in elements (any value, zero included).  Outputs, parameters
+ *     and states are dense.  Pointers need the alignment of their element type only; 16-byte
+ *     aligned rows are read in wide loads.
+ *   - Extents may be zero: an empty row leaves the state as it was.
+ *   - The results of a call do not depend on what else runs: no atomics, sums in a fixed order.
+ * ============================================================================================== */
+
+typedef enum { FPDE_F32 = 0, FPDE_BF16 = 1, FPDE_F16 = 2 } fpde_dtype;
+
+#define FPDE_CONV_MAX_WIDTH 4
+#define FPDE_SCAN_MAX_STATES 64
+
+/*
+ * Causal convolution along the row, one filter of `width` taps per channel:
+ *     pre[t] = bias + sum_j weight[j] x[t - width + 1 + j],   y = silu ? pre * sigmoid(pre) : pre
+ * where x before node 0 is `state`, the window of the last width-1 nodes of an earlier call (zeros
+ * if NULL).  `state_out` receives the window that the next call needs.
+ */
+typedef struct {
+    int32_t dtype, width, silu, reserved;
+    int64_t batch, length, channels;
+    const void* x;            /* (batch, length, channels) */
+    int64_t x_batch, x_node;  /* strides of x */
+    const float* weight;      /* (channels, width) */
+    const float* bias;        /* (channels), or NULL */
+    const void* state;        /* (batch, width-1, channels), or NULL */
+    void* y;                  /* fwd, step: (batch, length, channels) */
+    void* state_out;          /* fwd: (batch, width-1, channels), or NULL.  Must not be `state`. */
+    /* gradients (fpde_causal_conv_bwd) */
+    const void* gy;           /* (batch, length, channels) */
+    int64_t gy_batch, gy_node;
+    const void* gstate_out;   /* gradient of state_out, or NULL */
+    void* gx;                 /* (batch, length, channels), or NULL */
+    void* gstate;             /* (batch, width-1, channels), or NULL */
+    float* gweight;           /* (channels, width) */
+    float* gbias;             /* (channels), or NULL */
+    void* workspace;          /* bwd: at least fpde_causal_conv_workspace_bytes(), 16-byte aligned */
+    size_t workspace_bytes;
+} fpde_conv_args;
+
+size_t fpde_causal_conv_workspace_bytes(const fpde_conv_args* args);
+int fpde_causal_conv_fwd(const fpde_conv_args* args, void* stream);
+int fpde_causal_conv_bwd(const fpde_conv_args* args, void* stream);
+/* One node per row (length is taken as 1): reads x and `state`, writes y and moves the window in
+ * `state_out` on by one node; here `state_out` may be (and usually is) `state` itself. */
+int fpde_causal_conv_step(const fpde_conv_args* args, void* stream);
+
+/*
+ * Selective scan: for every row and channel, with `states` states,
+ *     dt = softplus ? log(1 + exp(delta + delta_bias)) : delta + delta_bias
+ *     h[t] = exp(dt A) h[t-1] + dt B[t] u[t]              (h[-1] = state, zeros if NULL)
+ *     y[t] = sum_n C[t,n] h[t,n] + D u[t],   out = z ? y * z * sigmoid(z) : y
+ * A is (channels, states); B and C are (batch, length, states), shared by all channels.
+ *
+ * Training: fpde_selective_scan_fwd with `kept` (fpde_selective_scan_kept_bytes() bytes) stores the
+ * states that fpde_selective_scan_bwd starts from; both calls take the same sizes.
+ * Rows are split along their length where batch and channels do not fill the GPU; the partial
+ * states are joined in a fixed order.
+ */
+typedef struct {
+    int32_t dtype, states, softplus, reserved;
+    int64_t batch, length, channels;
+    const void* u;     int64_t u_batch, u_node;          /* (batch, length, channels) */
+    const void* delta; int64_t delta_batch, delta_node;  /* (batch, length, channels) */
+    const void* z;     int64_t z_batch, z_node;          /* (batch, length, channels), or NULL */
+    const void* B;     int64_t B_batch, B_node;          /* (batch, length, states) */
+    const void* C;     int64_t C_batch, C_node;          /* (batch, length, states) */
+    const float* A;           /* (channels, states) */
+    const float* D;           /* (channels), or NULL */
+    const float* delta_bias;  /* (channels), or NULL */
+    const float* state;       /* (batch, channels, states), or NULL */
+    void* out;                /* fwd, step: (batch, length, channels) */
+    float* state_out;         /* (batch, channels, states), or NULL */
+    void* kept;               /* fwd: written if not NULL; bwd: read.  16-byte aligned */
+    size_t kept_bytes;
+    /* gradients (fpde_selective_scan_bwd) */
+    const void* gout;  int64_t gout_batch, gout_node;    /* (batch, length, channels) */
+    const float* gstate_out;  /* gradient of state_out, or NULL */
+    void* gu;                 /* (batch, length, channels) */
+    void* gdelta;             /* (batch, length, channels) */
+    void* gz;                 /* (batch, length, channels); NULL if z is */
+    void* gB;                 /* (batch, length, states) */
+    void* gC;                 /* (batch, length, states) */
+    float* gA;                /* (channels, states) */
+    float* gD;                /* (channels), or NULL */
+    float* gdelta_bias;       /* (channels), or NULL */
+    float* gstate;            /* (batch, channels, states), or NULL */
+    void* workspace;          /* at least fpde_selective_scan_workspace_bytes(), 16-byte aligned; NULL if that is 0 */
+    size_t workspace_bytes;
+} fpde_scan_args;
+
+size_t fpde_selective_scan_kept_bytes(const fpde_scan_args* args);
+size_t fpde_selective_scan_workspace_bytes(const fpde_scan_args* args, int backward);
+int fpde_selective_scan_fwd(const fpde_scan_args* args, void* stream);
+int fpde_selective_scan_bwd(const fpde_scan_args* args, void* stream);
+/* One node per row (length is taken as 1): `state_out` may be (and usually is) `state` itself. */
+int fpde_selective_scan_step(const fpde_scan_args* args, void* stream);
+
+/*
+ * Orthogonalised update of a stack of `count` matrices (count, rows, cols):
+ *     X = G / (|G|_F + eps);  `steps` times:  X <- a X + (b S + c S S) X,  S = X X^T
+ * with (a, b, c) = (3.4445, -4.775, 2.0315), on the shorter side: it drives the singular values of
+ * G towards one and leaves its singular vectors.
+ *
+ * fpde_orthogonalize writes that X to `out`.  fpde_muon_step is the optimiser's whole step:
+ *     momentum <- momentum_decay * momentum + grad
+ *     U = nesterov ? grad + momentum_decay * momentum : momentum
+ *     weight <- (1 - lr * weight_decay) * weight - lr * sqrt(max(1, rows / cols)) * X(U)
+ * in place on weight (dtype) and momentum (fp32).
+ *
+ * Precision: with fp32 arrays the products are formed from fp16 pairs that hold 22 bits of each
+ * factor and summed in fp32; with 16-bit arrays from single fp16 factors (11 bits), while the
+ * running X keeps 22 bits.
+ */
+typedef struct {
+    int32_t dtype, steps, nesterov, reserved;
+    int64_t count, rows, cols;
+    const void* grad;                   /* (count, rows, cols), cols contiguous */
+    int64_t grad_matrix, grad_row;      /* strides of grad */
+    void* out;                          /* orthogonalize: (count, rows, cols) dense */
+    void* weight;                       /* muon: (count, rows, cols) dense, updated */
+    float* momentum;                    /* muon: (count, rows, cols) dense, updated */
+    double eps, lr, momentum_decay, weight_decay;
+    void* workspace;                    /* at least fpde_orthogonalize_workspace_bytes(), 256-byte aligned */
+    size_t workspace_bytes;
+} fpde_ortho_args;
+
+size_t fpde_orthogonalize_workspace_bytes(const fpde_ortho_args* args);
+int fpde_orthogonalize(const fpde_ortho_args* args, void* stream);
+int fpde_muon_step(const fpde_ortho_args* args, void* stream);
+/* Bounded waits inside the orthogonalisation's products that gave up since the library was loaded
+ * (0 in a healthy run; see fpde_diag_tma_timeouts). */
+unsigned int fpde_diag_ortho_timeouts(void);
 
 #ifdef __cplusplus
 }

@@ -30,6 +30,41 @@ class FpdeError(RuntimeError):
         super().__init__("%s failed: status %d (%s)" % (where, status, strerror(status)))
 
 
+DTYPE_IDS = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}
+_vp, _i64c, _i32c = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32
+
+
+class ConvArgs(ctypes.Structure):
+    """fpde_conv_args of include/fpde.h."""
+    _fields_ = [("dtype", _i32c), ("width", _i32c), ("silu", _i32c), ("reserved", _i32c),
+                ("batch", _i64c), ("length", _i64c), ("channels", _i64c),
+                ("x", _vp), ("x_batch", _i64c), ("x_node", _i64c), ("weight", _vp), ("bias", _vp), ("state", _vp),
+                ("y", _vp), ("state_out", _vp),
+                ("gy", _vp), ("gy_batch", _i64c), ("gy_node", _i64c), ("gstate_out", _vp), ("gx", _vp), ("gstate", _vp),
+                ("gweight", _vp), ("gbias", _vp), ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class ScanArgs(ctypes.Structure):
+    """fpde_scan_args of include/fpde.h."""
+    _fields_ = [("dtype", _i32c), ("states", _i32c), ("softplus", _i32c), ("reserved", _i32c),
+                ("batch", _i64c), ("length", _i64c), ("channels", _i64c)] + \
+               [(n + k, t) for n in ("u", "delta", "z", "B", "C") for k, t in (("", _vp), ("_batch", _i64c), ("_node", _i64c))] + \
+               [("A", _vp), ("D", _vp), ("delta_bias", _vp), ("state", _vp), ("out", _vp), ("state_out", _vp),
+                ("kept", _vp), ("kept_bytes", ctypes.c_size_t),
+                ("gout", _vp), ("gout_batch", _i64c), ("gout_node", _i64c), ("gstate_out", _vp),
+                ("gu", _vp), ("gdelta", _vp), ("gz", _vp), ("gB", _vp), ("gC", _vp), ("gA", _vp), ("gD", _vp),
+                ("gdelta_bias", _vp), ("gstate", _vp), ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class OrthoArgs(ctypes.Structure):
+    """fpde_ortho_args of include/fpde.h."""
+    _fields_ = [("dtype", _i32c), ("steps", _i32c), ("nesterov", _i32c), ("reserved", _i32c),
+                ("count", _i64c), ("rows", _i64c), ("cols", _i64c),
+                ("grad", _vp), ("grad_matrix", _i64c), ("grad_row", _i64c), ("out", _vp), ("weight", _vp), ("momentum", _vp),
+                ("eps", ctypes.c_double), ("lr", ctypes.c_double), ("momentum_decay", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t)]
+
+
 class OpInfo(ctypes.Structure):
     _fields_ = [("ndim", ctypes.c_int), ("nfields", ctypes.c_int), ("nsources", ctypes.c_int),
                 ("nresiduals", ctypes.c_int), ("ncoeffs", ctypes.c_int), ("radius", ctypes.c_int),
@@ -115,6 +150,19 @@ def lib():
         L.fpde_diag_ns_tma_geometry.restype = ctypes.c_int
         L.fpde_diag_ns_tma_geometry.argtypes = [ctypes.POINTER(ctypes.c_int64), ctypes.c_int, ctypes.c_int,
                                                 ctypes.c_size_t]
+        for name, args, extra in (("fpde_causal_conv_workspace_bytes", ConvArgs, []),
+                                  ("fpde_selective_scan_kept_bytes", ScanArgs, []),
+                                  ("fpde_selective_scan_workspace_bytes", ScanArgs, [ctypes.c_int]),
+                                  ("fpde_orthogonalize_workspace_bytes", OrthoArgs, [])):
+            getattr(L, name).restype = ctypes.c_size_t
+            getattr(L, name).argtypes = [ctypes.POINTER(args)] + extra
+        for name, args in (("fpde_causal_conv_fwd", ConvArgs), ("fpde_causal_conv_bwd", ConvArgs), ("fpde_causal_conv_step", ConvArgs),
+                           ("fpde_selective_scan_fwd", ScanArgs), ("fpde_selective_scan_bwd", ScanArgs),
+                           ("fpde_selective_scan_step", ScanArgs), ("fpde_orthogonalize", OrthoArgs), ("fpde_muon_step", OrthoArgs)):
+            getattr(L, name).restype = ctypes.c_int
+            getattr(L, name).argtypes = [ctypes.POINTER(args), ctypes.c_void_p]
+        L.fpde_diag_ortho_timeouts.restype = ctypes.c_uint
+        L.fpde_diag_ortho_timeouts.argtypes = []
         _lib = L
     return _lib
 
@@ -543,3 +591,21 @@ def diag_ns_tma_geometry(shape, tile_rows: int, narrays: int, smem_limit: int) -
 def diag_tma_timeouts() -> int:
     """Bounded barrier waits that gave up on the current device (0 in a healthy run)."""
     return int(lib().fpde_diag_tma_timeouts())
+
+
+def diag_ortho_timeouts() -> int:
+    """Bounded waits of the orthogonalisation's products that gave up (0 in a healthy run)."""
+    return int(lib().fpde_diag_ortho_timeouts())
+
+
+def call_with(name: str, args, device):
+    """Queue entry point `name` with the argument block `args` on torch's current stream of `device`."""
+    import torch
+    fn = getattr(lib(), name)
+    if torch.cuda.current_device() == device.index:
+        st = fn(ctypes.byref(args), torch.cuda.current_stream().cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            st = fn(ctypes.byref(args), torch.cuda.current_stream().cuda_stream)
+    if st != FPDE_OK:
+        raise FpdeError(st, name)

@@ -19,6 +19,7 @@ NVCC_FLAGS = [
     "-O3", "-std=c++17", "-lineinfo",
     "-Xcompiler", "-fPIC", "-shared",
     "-cudart", "static",
+    "--threads", "0",            # one compiler job per core
 ]
 
 

@@ -214,6 +214,8 @@ const char* fpde_strerror(int status) {
     case FPDE_ERR_BC: return "boundary kinds not supported by the operator";
     case FPDE_ERR_WORKSPACE: return "workspace NULL, misaligned or too small";
     case FPDE_ERR_CUDA: return "CUDA runtime error";
+    case FPDE_ERR_DTYPE: return "element type not supported";
+    case FPDE_ERR_PARAM: return "a setting is outside its range";
     default: return "unknown status";
     }
 }

@@ -1,0 +1,67 @@
+// What the sequence operators (causal convolution, selective scan) and the orthogonalised update
+// share: element types, wide loads with a scalar form, the gate functions, launch helpers.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "../../include/fpde.h"
+#include "fpde_common.cuh"
+#include "fpde_internal.h"
+
+namespace fpde {
+
+template <typename T> __device__ __forceinline__ float to_f32(T v);
+template <> __device__ __forceinline__ float to_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ float to_f32<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <> __device__ __forceinline__ float to_f32<__half>(__half v) { return __half2float(v); }
+template <typename T> __device__ __forceinline__ T from_f32(float v);
+template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+
+// N elements of type T moved by one load or store of N * sizeof(T) bytes (at most 16).
+template <typename T, int N>
+struct alignas(sizeof(T) * N) Pack {
+    T v[N];
+};
+template <typename T, int N>
+__device__ __forceinline__ Pack<T, N> load_pack(const T* p) {
+    return *reinterpret_cast<const Pack<T, N>*>(p);
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_pack(T* p, const float (&v)[N]) {
+    Pack<T, N> k;
+#pragma unroll
+    for (int i = 0; i < N; ++i) k.v[i] = from_f32<T>(v[i]);
+    *reinterpret_cast<Pack<T, N>*>(p) = k;
+}
+
+// exp(-v) may overflow to infinity: the quotient is then 0, which is the limit.
+__device__ __forceinline__ float sigmoid_f32(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
+// The same to within an ulp or two.  A 16-bit result that another operator reads should round as the
+// exact one does: every fp32 error turns some of the roundings, and the reader sees those as 2^-8.
+__device__ __forceinline__ float sigmoid_exact_f32(float v) { return __fdiv_rn(1.f, 1.f + expf(-v)); }
+// log(1 + exp(v)); above 20 the two agree with v to fp32 precision.
+__device__ __forceinline__ float softplus_f32(float v) { return v > 20.f ? v : log1pf(__expf(v)); }
+__device__ __forceinline__ float exp2_f32(float v) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+constexpr float LOG2_E = 1.4426950408889634f;
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline bool aligned(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+inline size_t dtype_bytes(int dtype) { return dtype == FPDE_F32 ? 4 : 2; }
+inline bool dtype_ok(int dtype) { return dtype == FPDE_F32 || dtype == FPDE_BF16 || dtype == FPDE_F16; }
+
+// Can rows of this array be read in packs of n elements?
+inline bool packs(const void* p, int64_t batch_stride, int64_t node_stride, size_t elem, int n) {
+    return aligned(p, elem * n) && batch_stride % n == 0 && node_stride % n == 0;
+}
+
+}  // namespace fpde

@@ -1,0 +1,288 @@
+"""Sequence operators of a network that marches fields along one axis of the grid: a short causal
+convolution and a selective state space scan over rows of (batch, length, channels) tensors.
+
+    y = causal_conv(x, weight, bias)                              differentiable
+    y = selective_scan(u, delta, A, B, C, D, z, delta_bias)       differentiable
+
+with `state=` / `return_state=True` for a row that continues an earlier one, and for one node at a time
+
+    y = causal_conv_step(x, window, weight, bias)                 window moved on in place
+    y = selective_scan_step(state, u, delta, A, B, C, D, z, ...)  state moved on in place
+
+`*_fwd` / `*_bwd` are the same calls without autograd.  Activations are fp32, bf16 or fp16 CUDA tensors
+of one type whose channel axis is contiguous (slices of a wider projection are read in place);
+parameters and scan states are fp32.  Everything runs in libfpde.so on torch's current stream; torch
+allocates the outputs and the scratch memory.  There is no CPU path.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import NamedTuple, Optional
+
+import torch
+
+from . import binding as B_
+
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+class ConvGrads(NamedTuple):
+    x: torch.Tensor
+    weight: torch.Tensor
+    bias: Optional[torch.Tensor]
+    state: Optional[torch.Tensor]
+
+
+class ScanGrads(NamedTuple):
+    u: torch.Tensor
+    delta: torch.Tensor
+    A: torch.Tensor
+    B: torch.Tensor
+    C: torch.Tensor
+    D: Optional[torch.Tensor]
+    z: Optional[torch.Tensor]
+    delta_bias: Optional[torch.Tensor]
+    state: Optional[torch.Tensor]
+
+
+def _activation(name, t, shape, dtype, device):
+    """`t` with a contiguous last axis; checked against what the call expects."""
+    if t.shape != shape:
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+    if t.dtype != dtype:
+        raise ValueError("%s is %s, expected %s" % (name, t.dtype, dtype))
+    if t.device != device:
+        raise ValueError("%s is on %s, expected %s" % (name, t.device, device))
+    return t if t.stride(-1) == 1 or t.shape[-1] <= 1 else t.contiguous()
+
+
+def _dense(name, t, shape, dtype, device):
+    if t is None:
+        return None
+    _activation(name, t, shape, dtype, device)
+    return t.contiguous()
+
+
+def _first(name, t, dims):
+    if t.device.type != "cuda":
+        raise ValueError("%s is on %s, expected a CUDA tensor" % (name, t.device))
+    if t.dtype not in _TYPES:
+        raise ValueError("%s is %s, expected fp32, bf16 or fp16" % (name, t.dtype))
+    if t.dim() != dims:
+        raise ValueError("%s has %d axes, expected %d" % (name, t.dim(), dims))
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+# ------------------------------------------------------------------------------------- convolution
+def _conv_args(x, weight, bias, state, silu, step):
+    """The argument block of a convolution call, and the tensors that it points to."""
+    _first("x", x, 2 if step else 3)
+    dev, dt = x.device, x.dtype
+    batch, channels = x.shape[0], x.shape[-1]
+    if weight.dim() != 2:
+        raise ValueError("weight has %d axes, expected 2 (channels, width)" % weight.dim())
+    width = weight.shape[1]
+    x = _activation("x", x, x.shape, dt, dev)
+    weight = _dense("weight", weight, (channels, width), torch.float32, dev)
+    bias = _dense("bias", bias, (channels,), torch.float32, dev)
+    if not step:
+        state = _dense("state", state, (batch, width - 1, channels), dt, dev)
+    a = B_.ConvArgs(dtype=_TYPES[dt], width=width, silu=int(silu), batch=batch, length=1 if step else x.shape[1], channels=channels,
+                    x=x.data_ptr(), x_batch=x.stride(0), x_node=0 if step else x.stride(1),
+                    weight=weight.data_ptr(), bias=_ptr(bias), state=_ptr(state))
+    return a, (x, weight, bias, state)
+
+
+def causal_conv_fwd(x, weight, bias=None, state=None, silu=True):
+    """y[t] = act(bias + sum_j weight[:, j] x[t - width + 1 + j]) along axis 1 of x (batch, length, channels), and
+    the window (batch, width - 1, channels) that the next call continues from.  Before node 0 stands `state`,
+    such a window of an earlier call, or zeros.  weight: (channels, width), width 1 to 4; bias: (channels)."""
+    a, keep = _conv_args(x, weight, bias, state, silu, False)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    left = torch.empty((a.batch, a.width - 1, a.channels), dtype=x.dtype, device=x.device)
+    a.y, a.state_out = y.data_ptr(), left.data_ptr()
+    B_.call_with("fpde_causal_conv_fwd", a, x.device)
+    return y, left
+
+
+def causal_conv_bwd(gy, x, weight, bias=None, state=None, silu=True, gstate=None) -> ConvGrads:
+    """Gradients of causal_conv_fwd for upstream gradients gy of y and `gstate` of the window it left."""
+    a, keep = _conv_args(x, weight, bias, state, silu, False)
+    dev, dt = x.device, x.dtype
+    gy = _activation("gy", gy, x.shape, dt, dev)
+    gstate = _dense("gstate", gstate, (a.batch, a.width - 1, a.channels), dt, dev)
+    gx = torch.empty(x.shape, dtype=dt, device=dev)
+    gw = torch.empty((a.channels, a.width), dtype=torch.float32, device=dev)
+    gb = None if bias is None else torch.empty((a.channels,), dtype=torch.float32, device=dev)
+    gs = None if state is None else torch.empty((a.batch, a.width - 1, a.channels), dtype=dt, device=dev)
+    a.gy, a.gy_batch, a.gy_node, a.gstate_out = gy.data_ptr(), gy.stride(0), gy.stride(1), _ptr(gstate)
+    a.gx, a.gstate, a.gweight, a.gbias = gx.data_ptr(), _ptr(gs), gw.data_ptr(), _ptr(gb)
+    a.workspace_bytes = B_.lib().fpde_causal_conv_workspace_bytes(ctypes.byref(a))
+    ws = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=dev)
+    a.workspace = ws.data_ptr()
+    B_.call_with("fpde_causal_conv_bwd", a, dev)
+    return ConvGrads(gx, gw, gb, gs)
+
+
+def causal_conv_step(x, window, weight, bias=None, silu=True):
+    """One node per row: x (batch, channels) -> y; `window` (batch, width - 1, channels) is moved on in place."""
+    a, keep = _conv_args(x, weight, bias, None, silu, True)
+    _activation("window", window, (a.batch, a.width - 1, a.channels), x.dtype, x.device)
+    if not window.is_contiguous():
+        raise ValueError("window is updated in place and must be contiguous")
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    a.state = a.state_out = window.data_ptr()
+    a.y = y.data_ptr()
+    B_.call_with("fpde_causal_conv_step", a, x.device)
+    return y
+
+
+class _CausalConv(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, state, silu):
+        y, left = causal_conv_fwd(x, weight, bias, state, silu)
+        ctx.save_for_backward(x, weight, bias, state)
+        ctx.silu = silu
+        ctx.set_materialize_grads(False)
+        return y, left
+
+    @staticmethod
+    def backward(ctx, gy, gleft):
+        x, weight, bias, state = ctx.saved_tensors
+        if gy is None:
+            gy = torch.zeros_like(x)
+        g = causal_conv_bwd(gy, x, weight, bias, state, ctx.silu, gleft)
+        return g.x, g.weight, g.bias, g.state, None
+
+
+def causal_conv(x, weight, bias=None, state=None, silu=True, return_state=False):
+    """causal_conv_fwd, differentiable in x, weight, bias and state."""
+    y, left = _CausalConv.apply(x, weight, bias, state, silu)
+    return (y, left) if return_state else y
+
+
+# -------------------------------------------------------------------------------------------- scan
+def _scan_args(u, delta, A, B, C, D, z, delta_bias, delta_softplus, step):
+    _first("u", u, 2 if step else 3)
+    dev, dt, lead, channels = u.device, u.dtype, u.shape[:-1], u.shape[-1]
+    if A.dim() != 2:
+        raise ValueError("A has %d axes, expected 2 (channels, states)" % A.dim())
+    states = A.shape[1]
+    u = _activation("u", u, u.shape, dt, dev)
+    delta = _activation("delta", delta, u.shape, dt, dev)
+    z = None if z is None else _activation("z", z, u.shape, dt, dev)
+    B = _activation("B", B, lead + (states,), dt, dev)
+    C = _activation("C", C, lead + (states,), dt, dev)
+    A = _dense("A", A, (channels, states), torch.float32, dev)
+    D = _dense("D", D, (channels,), torch.float32, dev)
+    delta_bias = _dense("delta_bias", delta_bias, (channels,), torch.float32, dev)
+    a = B_.ScanArgs(dtype=_TYPES[dt], states=states, softplus=int(delta_softplus), batch=u.shape[0], length=1 if step else u.shape[1],
+                    channels=channels, A=A.data_ptr(), D=_ptr(D), delta_bias=_ptr(delta_bias))
+    a.u, a.u_batch, a.delta, a.delta_batch = u.data_ptr(), u.stride(0), delta.data_ptr(), delta.stride(0)
+    a.B, a.B_batch, a.C, a.C_batch = B.data_ptr(), B.stride(0), C.data_ptr(), C.stride(0)
+    if z is not None:
+        a.z, a.z_batch = z.data_ptr(), z.stride(0)
+    if not step:
+        a.u_node, a.delta_node, a.B_node, a.C_node = u.stride(1), delta.stride(1), B.stride(1), C.stride(1)
+        if z is not None:
+            a.z_node = z.stride(1)
+    return a, (u, delta, A, B, C, D, z, delta_bias)
+
+
+def selective_scan_fwd(u, delta, A, B, C, D=None, z=None, delta_bias=None, delta_softplus=True, state=None, keep=False):
+    """The scan of each row of u (batch, length, channels):
+
+        dt = softplus(delta + delta_bias);  h[t] = exp(dt A) h[t-1] + dt B[t] u[t];  out[t] = (C[t].h[t] + D u[t]) * silu(z[t])
+
+    with A (channels, states), B and C (batch, length, states), h[-1] = state (batch, channels, states) or zeros;
+    D, z, delta_bias and the softplus may be left out.  Returns (out, the last state, what selective_scan_bwd
+    needs of this pass if `keep`, else None).  1 to 64 states."""
+    a, hold = _scan_args(u, delta, A, B, C, D, z, delta_bias, delta_softplus, False)
+    dev = u.device
+    shape = (a.batch, a.channels, a.states)
+    state = _dense("state", state, shape, torch.float32, dev)
+    out = torch.empty(u.shape, dtype=u.dtype, device=dev)
+    last = torch.empty(shape, dtype=torch.float32, device=dev)
+    a.state, a.out, a.state_out = _ptr(state), out.data_ptr(), last.data_ptr()
+    kept = None
+    if keep:
+        a.kept_bytes = B_.lib().fpde_selective_scan_kept_bytes(ctypes.byref(a))
+        kept = torch.empty(a.kept_bytes, dtype=torch.uint8, device=dev)
+        a.kept = kept.data_ptr()
+    a.workspace_bytes = B_.lib().fpde_selective_scan_workspace_bytes(ctypes.byref(a), 0)
+    if a.workspace_bytes:
+        ws = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=dev)
+        a.workspace = ws.data_ptr()
+    B_.call_with("fpde_selective_scan_fwd", a, dev)
+    return out, last, kept
+
+
+def selective_scan_bwd(gout, u, delta, A, B, C, D=None, z=None, delta_bias=None, delta_softplus=True, state=None, kept=None,
+                       gstate=None) -> ScanGrads:
+    """Gradients of selective_scan_fwd (called with keep=True: pass its `kept`) for upstream gradients gout of
+    `out` and `gstate` of the last state."""
+    a, hold = _scan_args(u, delta, A, B, C, D, z, delta_bias, delta_softplus, False)
+    dev, dt, f = u.device, u.dtype, torch.float32
+    shape = (a.batch, a.channels, a.states)
+    gout = _activation("gout", gout, u.shape, dt, dev)
+    gstate = _dense("gstate", gstate, shape, f, dev)
+    if kept is None:
+        raise ValueError("selective_scan_bwd needs what selective_scan_fwd(..., keep=True) returned")
+    g = ScanGrads(torch.empty(u.shape, dtype=dt, device=dev), torch.empty(u.shape, dtype=dt, device=dev),
+                  torch.empty((a.channels, a.states), dtype=f, device=dev),
+                  torch.empty(B.shape, dtype=dt, device=dev), torch.empty(C.shape, dtype=dt, device=dev),
+                  None if D is None else torch.empty((a.channels,), dtype=f, device=dev),
+                  None if z is None else torch.empty(u.shape, dtype=dt, device=dev),
+                  None if delta_bias is None else torch.empty((a.channels,), dtype=f, device=dev),
+                  None if state is None else torch.empty(shape, dtype=f, device=dev))
+    a.gout, a.gout_batch, a.gout_node, a.gstate_out = gout.data_ptr(), gout.stride(0), gout.stride(1), _ptr(gstate)
+    a.gu, a.gdelta, a.gA, a.gB, a.gC = g.u.data_ptr(), g.delta.data_ptr(), g.A.data_ptr(), g.B.data_ptr(), g.C.data_ptr()
+    a.gD, a.gz, a.gdelta_bias, a.gstate = _ptr(g.D), _ptr(g.z), _ptr(g.delta_bias), _ptr(g.state)
+    a.kept, a.kept_bytes = kept.data_ptr(), kept.numel()
+    a.workspace_bytes = B_.lib().fpde_selective_scan_workspace_bytes(ctypes.byref(a), 1)
+    ws = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=dev)
+    a.workspace = ws.data_ptr()
+    B_.call_with("fpde_selective_scan_bwd", a, dev)
+    return g
+
+
+def selective_scan_step(state, u, delta, A, B, C, D=None, z=None, delta_bias=None, delta_softplus=True):
+    """One node per row: u, delta, z (batch, channels), B, C (batch, states) -> out (batch, channels); `state`
+    (batch, channels, states) is moved on in place."""
+    a, hold = _scan_args(u, delta, A, B, C, D, z, delta_bias, delta_softplus, True)
+    _activation("state", state, (a.batch, a.channels, a.states), torch.float32, u.device)
+    if not state.is_contiguous():
+        raise ValueError("state is updated in place and must be contiguous")
+    out = torch.empty(u.shape, dtype=u.dtype, device=u.device)
+    a.state = a.state_out = state.data_ptr()
+    a.out = out.data_ptr()
+    B_.call_with("fpde_selective_scan_step", a, u.device)
+    return out
+
+
+class _SelectiveScan(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, u, delta, A, B, C, D, z, delta_bias, delta_softplus, state):
+        out, last, kept = selective_scan_fwd(u, delta, A, B, C, D, z, delta_bias, delta_softplus, state,
+                                             keep=any(ctx.needs_input_grad))
+        ctx.save_for_backward(u, delta, A, B, C, D, z, delta_bias, state, kept)
+        ctx.delta_softplus = delta_softplus
+        ctx.set_materialize_grads(False)
+        return out, last
+
+    @staticmethod
+    def backward(ctx, gout, glast):
+        u, delta, A, B, C, D, z, delta_bias, state, kept = ctx.saved_tensors
+        if gout is None:
+            gout = torch.zeros_like(u)
+        g = selective_scan_bwd(gout, u, delta, A, B, C, D, z, delta_bias, ctx.delta_softplus, state, kept, glast)
+        return g.u, g.delta, g.A, g.B, g.C, g.D, g.z, g.delta_bias, None, g.state
+
+
+def selective_scan(u, delta, A, B, C, D=None, z=None, delta_bias=None, delta_softplus=True, state=None, return_state=False):
+    """selective_scan_fwd, differentiable in every tensor."""
+    out, last = _SelectiveScan.apply(u, delta, A, B, C, D, z, delta_bias, delta_softplus, state)
+    return (out, last) if return_state else out
