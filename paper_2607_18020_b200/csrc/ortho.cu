@@ -4,11 +4,13 @@
 //   X = U / (|U| + eps);  `steps` times:  S = X X^T,  P = b S + c S S,  X <- a X + P X
 // on the shorter side (taller matrices are turned on the way in and back on the way out).
 #include "seq_common.cuh"
+#include "tma_common.cuh"
 
 namespace fpde {
 namespace {
 
 constexpr float NS_A = 3.4445f, NS_B = -4.775f, NS_C = 2.0315f;
+constexpr float SCALE = 16384.f;    // 2^14: matrices are stored times this, see the products
 constexpr int SUM_BLOCKS = 64;      // blocks that sum the squares of one matrix
 
 // What the matrices are read from and written to.
@@ -17,7 +19,7 @@ struct OrthoIo {
     int64_t grad_matrix, grad_row;
     void* out;          // orthogonalize: result;  muon: weight
     float* momentum;    // muon only
-    int rows, cols, m, n;
+    int rows, cols, m, n, mp, np;   // m <= n: the sides of X; mp, np padded
     bool turned, nesterov;
     float decay, keep, rate;   // momentum decay, 1 - lr wd, lr sqrt(max(1, rows / cols))
     double eps;
@@ -66,74 +68,347 @@ __device__ __forceinline__ float inverse_norm(const double* sums, double eps) {
     return (float)(1.0 / (sqrt(v) + eps));
 }
 
-// X (m x n) of matrix k.
-template <typename T>
-__global__ void __launch_bounds__(256) ortho_start_kernel(OrthoIo io, const double* __restrict__ sums, float* __restrict__ x, int64_t all) {
-    pdl_wait_then_trigger();
-    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (e >= all) return;
-    const int64_t per = (int64_t)io.m * io.n, k = e / per, i = e % per / io.n, j = e % io.n;
-    x[e] = update_at<T>(io, k, io.turned ? j : i, io.turned ? i : j) * inverse_norm(sums + k * SUM_BLOCKS, io.eps);
+__device__ __forceinline__ void store_planes(__half* hi, __half* lo, float v) {     // v: already scaled
+    const __half h = __float2half_rn(v);
+    *hi = h;
+    *lo = __float2half_rn(v - __half2float(h));
 }
 
-// C = alpha L R + beta D for row-major L (m x k), R (k x n), or its transpose as stored when RT.
-template <bool RT>
-__global__ void __launch_bounds__(256) product_kernel(const float* __restrict__ l, const float* __restrict__ r, const float* __restrict__ d,
-                                                      float* __restrict__ c, int m, int n, int kk, float alpha, float beta) {
+// The first X (m x n, padded to mp x np) of every matrix, turned where the matrix is taller than wide.
+template <typename T>
+__global__ void __launch_bounds__(256) ortho_start_kernel(OrthoIo io, const double* __restrict__ sums, __half* __restrict__ x) {
     pdl_wait_then_trigger();
-    __shared__ float sl[16][65], sr[16][65];
-    const int64_t which = blockIdx.z;
-    l += which * m * kk; r += which * (int64_t)kk * n; d += which * (int64_t)m * n; c += which * (int64_t)m * n;
-    const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64, ty = threadIdx.x / 16, tx = threadIdx.x % 16;
-    float acc[4][4] = {};
-    for (int k0 = 0; k0 < kk; k0 += 16) {
-        for (int e = threadIdx.x; e < 1024; e += 256) {
-            const int a = e / 16, b = e % 16;
-            sl[b][a] = i0 + a < m && k0 + b < kk ? l[(int64_t)(i0 + a) * kk + k0 + b] : 0.f;
-            if (RT) sr[b][a] = j0 + a < n && k0 + b < kk ? r[(int64_t)(j0 + a) * kk + k0 + b] : 0.f;
-            else sr[e / 64][e % 64] = k0 + e / 64 < kk && j0 + e % 64 < n ? r[(int64_t)(k0 + e / 64) * n + j0 + e % 64] : 0.f;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < 16; ++k)
-#pragma unroll
-            for (int a = 0; a < 4; ++a)
-#pragma unroll
-                for (int b = 0; b < 4; ++b) acc[a][b] = fmaf(sl[k][ty * 4 + a], sr[k][tx * 4 + b], acc[a][b]);
-        __syncthreads();
+    __shared__ float tile[32][33];
+    __shared__ float scale;
+    const int across = io.np / 32, down = io.mp / 32;
+    const int64_t k = blockIdx.x / (across * down);
+    const int t = (int)(blockIdx.x % (across * down)), i0 = t / across * 32, j0 = t % across * 32;
+    if (threadIdx.x == 0) scale = inverse_norm(sums + k * SUM_BLOCKS, io.eps) * SCALE;
+    const int a = threadIdx.x / 32, b = threadIdx.x % 32;
+    for (int r = a; r < 32; r += 8) {
+        const int row = (io.turned ? j0 : i0) + r, col = (io.turned ? i0 : j0) + b;
+        tile[r][b] = row < io.rows && col < io.cols ? update_at<T>(io, k, row, col) : 0.f;
     }
-#pragma unroll
-    for (int a = 0; a < 4; ++a)
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const int i = i0 + ty * 4 + a, j = j0 + tx * 4 + b;
-            if (i < m && j < n) c[(int64_t)i * n + j] = alpha * acc[a][b] + (beta != 0.f ? beta * d[(int64_t)i * n + j] : 0.f);
-        }
+    __syncthreads();
+    const int64_t plane = (int64_t)io.mp * io.np;
+    for (int r = a; r < 32; r += 8) {
+        const bool there = i0 + r < io.m && j0 + b < io.n;       // padding stays zero, whatever the norm is
+        const float v = there ? (io.turned ? tile[b][r] : tile[r][b]) * scale : 0.f;
+        __half* p = x + 2 * k * plane + (int64_t)(i0 + r) * io.np + j0 + b;
+        store_planes(p, p + plane, v);
+    }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) ortho_finish_kernel(OrthoIo io, const float* __restrict__ x, int64_t all) {
+// ------------------------------------------------------------------------------------------ products
+// One product of the iteration over all matrices of the stack, on the tensor cores:
+//   GRAM    S  = X X^T              SQUARE  P = b S + c S S             APPLY  X' = a X + P X
+//
+// Every matrix is held as two fp16 planes, hi and lo, of the value times 2^14: hi is the value rounded to
+// 11 bits, lo the next 11 bits of what is left.  The entries are at most 1.25 (X, S) or 2.81 (P) in size,
+// so the scaled hi stays below 65504, and 2^14 keeps lo above fp16's smallest numbers for entries down to
+// 2^-16.  With PAIR three products (hi hi, hi lo, lo hi) go into one fp32 accumulator: 22-bit factors.
+// Without it only hi hi is formed, and lo serves the terms a X and b S that are added in the epilogue.
+//
+// S and P are symmetric: only tiles on and below the diagonal are computed, and stored twice.
+//
+// A block is persistent and has one warp that loads (TMA into a ring of 64-deep slices, 128-byte
+// swizzle), one that issues tcgen05.mma (128 x BN tiles, accumulators in TMEM) and four that turn the
+// accumulators into the next operand; two accumulators let a tile's epilogue run under the next tile's
+// products.  X enters APPLY as it is stored, rows along k: its slices are MN-major operands.
+// The planes are padded to multiples of 64 with zeros.
+enum Kind { GRAM, SQUARE, APPLY };
+
+constexpr int BM = 128, BK = 64;
+constexpr int PRODUCT_THREADS = 192;
+
+template <bool PAIR, int BN>
+struct Ring {
+    static constexpr int PLANES = PAIR ? 2 : 1;
+    static constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2;
+    static constexpr int STAGE = PLANES * (A_BYTES + B_BYTES);
+    static constexpr int STAGES = 196608 / STAGE;
+    static constexpr int BYTES = STAGES * STAGE + 1024 + 256;    // slack to start on 1024 bytes, barriers
+};
+
+struct ProductShape {
+    int mp, np;                 // padded extents of X; S and P are mp x mp
+    int depth;                  // np (GRAM) or mp
+    int tiles, per_matrix, across;   // tiles in all, of one matrix, of one row of tiles (APPLY)
+    int cols;                   // columns of the result: mp or np
+    float alpha, beta;          // stored = alpha acc + beta (hi + lo of the added term)
+};
+
+// 64-bit description of an operand slice in shared memory, 128-byte swizzle.  K-major: rows of 64 fp16,
+// 1024 bytes per 8 rows.  MN-major: blocks of 64 columns by 64 k-rows, 8192 bytes apart; 1024 bytes per 8 k-rows.
+__device__ __forceinline__ uint64_t slice_desc(uint32_t addr, bool mn_major) {
+    uint64_t d = (uint64_t)((addr & 0x3ffff) >> 4);
+    d |= (uint64_t)((mn_major ? 8192 : 16) >> 4) << 16;   // leading offset (K-major, swizzled: not used)
+    d |= (uint64_t)(1024 >> 4) << 32;                     // stride offset
+    d |= 1ull << 46;                                      // descriptor version of sm_100
+    d |= 2ull << 61;                                      // 128-byte swizzle
+    return d;
+}
+
+__device__ __forceinline__ void mma_f16(uint32_t tmem, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+        : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
+    uint32_t r[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
+        "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+__device__ unsigned int g_ortho_timeouts;
+
+// Tile number t of one matrix -> first row and column.
+template <int KIND, int BN>
+__device__ __forceinline__ void tile_at(int t, int across, int& i0, int& j0) {
+    if (KIND == APPLY) {
+        i0 = t / across * BM;
+        j0 = t % across * BN;
+    } else {                    // lower triangle, row by row
+        int i = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
+        while ((i + 1) * (i + 2) / 2 <= t) ++i;
+        while (i * (i + 1) / 2 > t) --i;
+        i0 = i * BM;
+        j0 = (t - i * (i + 1) / 2) * BN;
+    }
+}
+
+// left: K-major map of X (GRAM), S (SQUARE) or P (APPLY), also the right operand of GRAM and SQUARE;
+// right: map of X in 64 x 64 boxes (APPLY).  added: planes of the term in the epilogue (S or X).
+template <bool PAIR, int BN, int KIND>
+__global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __grid_constant__ CUtensorMap left, const __grid_constant__ CUtensorMap right,
+                                                                      const __half* __restrict__ added, __half* __restrict__ out, ProductShape s) {
+    using R = Ring<PAIR, BN>;
+    static_assert(KIND == APPLY || BN == BM, "mirrored tiles are square");
+    extern __shared__ uint8_t raw[];
+    uint8_t* ring = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(ring + R::STAGES * R::STAGE);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * R::STAGES + 4);
+    const uint32_t full = smem_u32(bars), empty = full + 8 * R::STAGES, done = empty + 8 * R::STAGES, freed = done + 16;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < R::STAGES; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(done + 8 * i, 1); mbar_init(freed + 8 * i, 128); }
+        mbar_fence_init();
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(2 * BN) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = *tmem_slot;
     pdl_wait_then_trigger();
-    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (e >= all) return;
-    const int64_t per = (int64_t)io.rows * io.cols, k = e / per, r = e % per / io.cols, c = e % io.cols;
-    const float v = x[k * per + (io.turned ? c * io.n + r : r * io.n + c)];
-    T* out = (T*)io.out + e;
-    *out = from_f32<T>(io.momentum == nullptr ? v : fmaf(-io.rate, v, io.keep * to_f32<T>(*out)));
+    const int steps = s.depth / BK;
+    bool gave_up = false;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int stage = 0, phase = 0;
+            for (int tile = blockIdx.x; tile < s.tiles; tile += gridDim.x) {
+                const int k = tile / s.per_matrix;
+                int i0, j0;
+                tile_at<KIND, BN>(tile % s.per_matrix, s.across, i0, j0);
+                for (int step = 0; step < steps; ++step) {
+                    mbar_wait(empty + 8 * stage, phase ^ 1, gave_up, &g_ortho_timeouts);
+                    mbar_expect_tx(full + 8 * stage, R::STAGE);
+                    const uint32_t base = smem_u32(ring + stage * R::STAGE), bar = full + 8 * stage;
+#pragma unroll
+                    for (int p = 0; p < R::PLANES; ++p) {
+                        tma_load_3d(base + p * R::A_BYTES, &left, step * BK, i0, 2 * k + p, bar);
+                        const uint32_t b = base + R::PLANES * R::A_BYTES + p * R::B_BYTES;
+                        if (KIND == APPLY) {
+#pragma unroll
+                            for (int q = 0; q < BN / 64; ++q) tma_load_3d(b + q * 8192, &right, j0 + 64 * q, step * BK, 2 * k + p, bar);
+                        } else {
+                            tma_load_3d(b, &left, step * BK, j0, 2 * k + p, bar);
+                        }
+                    }
+                    if (++stage == R::STAGES) { stage = 0; phase ^= 1; }
+                }
+            }
+            // the last copies have to land before the block may end: wait until they have been used
+            for (int i = 0; i < R::STAGES; ++i) {
+                mbar_wait(empty + 8 * stage, phase ^ 1, gave_up, &g_ortho_timeouts);
+                if (++stage == R::STAGES) { stage = 0; phase ^= 1; }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            constexpr uint32_t IDESC = (1u << 4) | (KIND == APPLY ? 1u << 16 : 0u) | ((uint32_t)(BN / 8) << 17) | ((uint32_t)(BM / 16) << 24);
+            constexpr int KB = KIND == APPLY ? 2048 : 32;      // bytes from one 16-deep piece of B to the next
+            int stage = 0, phase = 0, acc = 0, acc_phase = 0;
+            for (int tile = blockIdx.x; tile < s.tiles; tile += gridDim.x) {
+                mbar_wait(freed + 8 * acc, acc_phase ^ 1, gave_up, &g_ortho_timeouts);
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t d = tmem + acc * BN;
+                for (int step = 0; step < steps; ++step) {
+                    mbar_wait(full + 8 * stage, phase, gave_up, &g_ortho_timeouts);
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t a = smem_u32(ring + stage * R::STAGE), b = a + R::PLANES * R::A_BYTES;
+#pragma unroll
+                    for (int kk = 0; kk < BK / 16; ++kk) {
+                        const uint64_t ah = slice_desc(a + kk * 32, false), bh = slice_desc(b + kk * KB, KIND == APPLY);
+                        mma_f16(d, ah, bh, IDESC, step > 0 || kk > 0);
+                        if (PAIR) {
+                            mma_f16(d, ah, slice_desc(b + R::B_BYTES + kk * KB, KIND == APPLY), IDESC, true);
+                            mma_f16(d, slice_desc(a + R::A_BYTES + kk * 32, false), bh, IDESC, true);
+                        }
+                    }
+                    mma_commit(empty + 8 * stage);
+                    if (++stage == R::STAGES) { stage = 0; phase ^= 1; }
+                }
+                mma_commit(done + 8 * acc);
+                if (acc == 1) acc_phase ^= 1;
+                acc ^= 1;
+            }
+        }
+    } else {
+        const int quarter = warp % 4;                      // TMEM lanes this warp may read
+        int acc = 0, acc_phase = 0;
+        const int64_t out_plane = (int64_t)s.mp * s.cols;
+        for (int tile = blockIdx.x; tile < s.tiles; tile += gridDim.x) {
+            const int k = tile / s.per_matrix;
+            int i0, j0;
+            tile_at<KIND, BN>(tile % s.per_matrix, s.across, i0, j0);
+            const int row = i0 + quarter * 32 + lane;
+            mbar_wait(done + 8 * acc, acc_phase, gave_up, &g_ortho_timeouts);
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            __half* hi = out + 2 * k * out_plane;
+            __half* lo = hi + out_plane;
+            const __half* add = KIND == GRAM ? nullptr : added + 2 * k * out_plane + (int64_t)row * s.cols;
+#pragma unroll 1
+            for (int c = 0; c < BN; c += 32) {
+                float v[32];
+                tmem_load32(tmem + acc * BN + c + ((uint32_t)(quarter * 32) << 16), v);
+                const int col = j0 + c;
+                if (row >= s.mp || col >= s.cols) continue;      // a warp's lanes share col; rows past the end are whole warps (mp % 64 == 0)
+                __align__(16) __half h[32], l[32];
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    Pack<__half, 8> ph = {}, pl = {};
+                    if (KIND != GRAM) {
+                        ph = load_pack<__half, 8>(add + col + 8 * g);
+                        pl = load_pack<__half, 8>(add + out_plane + col + 8 * g);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        float w = s.alpha * v[8 * g + i];
+                        if (KIND != GRAM) w = fmaf(s.beta, __half2float(ph.v[i]) + __half2float(pl.v[i]), w);
+                        h[8 * g + i] = __float2half_rn(w);
+                        l[8 * g + i] = __float2half_rn(w - __half2float(h[8 * g + i]));
+                    }
+                }
+                const bool both = PAIR || KIND != SQUARE;        // P is only ever a factor
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    *reinterpret_cast<uint4*>(hi + (int64_t)row * s.cols + col + 8 * g) = *reinterpret_cast<const uint4*>(h + 8 * g);
+                    if (both) *reinterpret_cast<uint4*>(lo + (int64_t)row * s.cols + col + 8 * g) = *reinterpret_cast<const uint4*>(l + 8 * g);
+                }
+                if (KIND != APPLY && i0 != j0) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        hi[(int64_t)(col + i) * s.cols + row] = h[i];
+                        if (both) lo[(int64_t)(col + i) * s.cols + row] = l[i];
+                    }
+                }
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            mbar_arrive(freed + 8 * acc);
+            if (acc == 1) acc_phase ^= 1;
+            acc ^= 1;
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * BN) : "memory");
+}
+
+// Planes of a stack of r x c matrices as a 3-D tensor (columns, rows, 2 count) read in boxes of 64 columns
+// by `box_rows` rows; what lies outside reads as zero.
+bool encode_planes(CUtensorMap* m, const __half* p, int64_t count, int r, int c, int box_rows) {
+    EncodeTiledFn fn = tma_encode_fn();
+    if (fn == nullptr) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)c, (cuuint64_t)r, (cuuint64_t)(2 * count)};
+    const cuuint64_t strides[2] = {(cuuint64_t)c * 2u, (cuuint64_t)c * r * 2u};
+    const cuuint32_t box[3] = {64u, (cuuint32_t)box_rows, 1u}, one[3] = {1u, 1u, 1u};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<__half*>(p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool PAIR, int BN, int KIND>
+cudaError_t launch_product(const CUtensorMap& left, const CUtensorMap& right, const __half* added, __half* out, ProductShape s, int64_t count,
+                           int sms, cudaStream_t st) {
+    const int down = (int)ceil_div(s.mp, BM);
+    s.across = (int)ceil_div(s.cols, BN);
+    s.depth = KIND == GRAM ? s.np : s.mp;
+    const int64_t per = KIND == APPLY ? (int64_t)down * s.across : (int64_t)down * (down + 1) / 2;
+    if (per * count > 0x3fffffff) return cudaErrorInvalidConfiguration;
+    s.per_matrix = (int)per;
+    s.tiles = (int)(per * count);
+    constexpr int bytes = Ring<PAIR, BN>::BYTES;
+    const cudaError_t e = cudaFuncSetAttribute(product_kernel<PAIR, BN, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != cudaSuccess) return e;
+    return launch_kernel_smem(product_kernel<PAIR, BN, KIND>, dim3((unsigned)(s.tiles < sms ? s.tiles : sms)), dim3(PRODUCT_THREADS), bytes, st,
+                              left, right, added, out, s);
+}
+
+// X back in the shape of the matrices: written out, or applied to the weights.
+template <typename T>
+__global__ void __launch_bounds__(256) ortho_finish_kernel(OrthoIo io, const __half* __restrict__ x) {
+    pdl_wait_then_trigger();
+    __shared__ float tile[32][33];
+    const int across = (io.cols + 31) / 32, down = (io.rows + 31) / 32;
+    const int64_t k = blockIdx.x / (across * down), plane = (int64_t)io.mp * io.np;
+    const int t = (int)(blockIdx.x % (across * down)), r0 = t / across * 32, c0 = t % across * 32;
+    const int a = threadIdx.x / 32, b = threadIdx.x % 32;
+    const __half* p = x + 2 * k * plane;
+    for (int r = a; r < 32; r += 8) {
+        const int64_t at = (int64_t)((io.turned ? c0 : r0) + r) * io.np + (io.turned ? r0 : c0) + b;    // inside the padding
+        tile[r][b] = (__half2float(p[at]) + __half2float(p[at + plane])) * (1.f / SCALE);
+    }
+    __syncthreads();
+    for (int r = a; r < 32; r += 8) {
+        if (r0 + r >= io.rows || c0 + b >= io.cols) continue;
+        const float v = io.turned ? tile[b][r] : tile[r][b];
+        T* out = (T*)io.out + (k * io.rows + r0 + r) * io.cols + c0 + b;
+        *out = from_f32<T>(io.momentum == nullptr ? v : fmaf(-io.rate, v, io.keep * to_f32<T>(*out)));
+    }
 }
 
 struct OrthoSpace {
     size_t sums, x[2], s, p, total;
 };
+int64_t padded(int64_t n) { return ceil_div(n, 64) * 64; }
 OrthoSpace space(int64_t count, int64_t m, int64_t n) {
     OrthoSpace w;
+    const int64_t mp = padded(m), np = padded(n);
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
     w.sums = take(count * SUM_BLOCKS * 8);
-    w.x[0] = take(count * m * n * 4);
-    w.x[1] = take(count * m * n * 4);
-    w.s = take(count * m * m * 4);
-    w.p = take(count * m * m * 4);
+    w.x[0] = take(count * mp * np * 4);
+    w.x[1] = take(count * mp * np * 4);
+    w.s = take(count * mp * mp * 4);
+    w.p = take(count * mp * mp * 4);
     w.total = at;
     return w;
 }
@@ -166,26 +441,40 @@ cudaError_t run(const fpde_ortho_args* a, bool muon, cudaStream_t st) {
     io.keep = (float)(1.0 - a->lr * a->weight_decay);
     io.rate = (float)(a->lr * sqrt(io.rows > io.cols ? (double)io.rows / io.cols : 1.0));
     io.eps = a->eps;
+    io.mp = (int)padded(io.m); io.np = (int)padded(io.n);
     const OrthoSpace w = space(a->count, io.m, io.n);
     char* ws = (char*)a->workspace;
     double* sums = (double*)(ws + w.sums);
-    float* x[2] = {(float*)(ws + w.x[0]), (float*)(ws + w.x[1])};
-    float *s = (float*)(ws + w.s), *p = (float*)(ws + w.p);
-    const int64_t all = a->count * (int64_t)io.m * io.n;
-    const dim3 flat((unsigned)ceil_div(all, 256));
+    __half* x[2] = {(__half*)(ws + w.x[0]), (__half*)(ws + w.x[1])};
+    __half *s = (__half*)(ws + w.s), *p = (__half*)(ws + w.p);
+    const int64_t pieces = (int64_t)(io.mp / 32) * (io.np / 32) * a->count;
+    const int64_t back = ceil_div(io.rows, 32) * ceil_div(io.cols, 32) * a->count;
+    if (pieces > 0x7fffffff || a->count * SUM_BLOCKS > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    CUtensorMap xk[2], xn[2], sk, pk;
+    if (a->steps > 0) {
+        bool ok = encode_planes(&sk, s, a->count, io.mp, io.mp, BM) && encode_planes(&pk, p, a->count, io.mp, io.mp, BM);
+        for (int i = 0; i < 2; ++i)
+            ok = ok && encode_planes(&xk[i], x[i], a->count, io.mp, io.np, BM) && encode_planes(&xn[i], x[i], a->count, io.mp, io.np, BK);
+        if (!ok) return cudaErrorNotSupported;
+    }
     FPDE_TRY(launch_kernel(ortho_square_kernel<T>, dim3((unsigned)(a->count * SUM_BLOCKS)), dim3(256), st, io, sums));
-    FPDE_TRY(launch_kernel(ortho_start_kernel<T>, flat, dim3(256), st, io, (const double*)sums, x[0], all));
-    const unsigned mt = (unsigned)ceil_div(io.m, 64), nt = (unsigned)ceil_div(io.n, 64), k = (unsigned)a->count;
+    FPDE_TRY(launch_kernel(ortho_start_kernel<T>, dim3((unsigned)pieces), dim3(256), st, io, (const double*)sums, x[0]));
+    const int sms = sm_count_or_default();
     int at = 0;
     for (int i = 0; i < a->steps; ++i, at ^= 1) {
-        FPDE_TRY(launch_kernel(product_kernel<true>, dim3(mt, mt, k), dim3(256), st, (const float*)x[at], (const float*)x[at],
-                               (const float*)s, s, io.m, io.m, io.n, 1.f, 0.f));
-        FPDE_TRY(launch_kernel(product_kernel<true>, dim3(mt, mt, k), dim3(256), st, (const float*)s, (const float*)s, (const float*)s, p,
-                               io.m, io.m, io.m, NS_C, NS_B));
-        FPDE_TRY(launch_kernel(product_kernel<false>, dim3(nt, mt, k), dim3(256), st, (const float*)p, (const float*)x[at],
-                               (const float*)x[at], x[at ^ 1], io.m, io.n, io.m, 1.f, NS_A));
+        constexpr bool PAIR = sizeof(T) == 4;
+        ProductShape gram{io.mp, io.np, 0, 0, 0, 0, io.mp, 1.f / SCALE, 0.f};
+        ProductShape square{io.mp, io.np, 0, 0, 0, 0, io.mp, NS_C / SCALE, NS_B};
+        ProductShape apply{io.mp, io.np, 0, 0, 0, 0, io.np, 1.f / SCALE, NS_A};
+        FPDE_TRY((launch_product<PAIR, 128, GRAM>(xk[at], xk[at], s, s, gram, a->count, sms, st)));
+        FPDE_TRY((launch_product<PAIR, 128, SQUARE>(sk, sk, s, p, square, a->count, sms, st)));
+        // 256 columns halve the loads of P per product; 128 make enough tiles where 256 leave SMs idle
+        if (ceil_div(io.mp, BM) * ceil_div(io.np, 256) * a->count >= sms)
+            FPDE_TRY((launch_product<PAIR, 256, APPLY>(pk, xn[at], x[at], x[at ^ 1], apply, a->count, sms, st)));
+        else
+            FPDE_TRY((launch_product<PAIR, 128, APPLY>(pk, xn[at], x[at], x[at ^ 1], apply, a->count, sms, st)));
     }
-    return launch_kernel(ortho_finish_kernel<T>, flat, dim3(256), st, io, (const float*)x[at], all);
+    return launch_kernel(ortho_finish_kernel<T>, dim3((unsigned)back), dim3(256), st, io, (const __half*)x[at]);
 }
 
 int call(const fpde_ortho_args* a, bool muon, void* stream) {
@@ -217,6 +506,13 @@ size_t fpde_orthogonalize_workspace_bytes(const fpde_ortho_args* a) {
 
 int fpde_orthogonalize(const fpde_ortho_args* a, void* stream) { return call(a, false, stream); }
 int fpde_muon_step(const fpde_ortho_args* a, void* stream) { return call(a, true, stream); }
-unsigned int fpde_diag_ortho_timeouts(void) { return 0; }
+unsigned int fpde_diag_ortho_timeouts(void) {
+    unsigned int n = 0;
+    if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpyFromSymbol(&n, g_ortho_timeouts, sizeof n) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return ~0u;
+    }
+    return n;
+}
 
 }  // extern "C"
