@@ -39,21 +39,25 @@ __device__ __forceinline__ void store_pack(T* p, const float (&v)[N]) {
     *reinterpret_cast<Pack<T, N>*>(p) = k;
 }
 
-// exp(-v) may overflow to infinity: the quotient is then 0, which is the limit.
-__device__ __forceinline__ float sigmoid_f32(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
-// The same to within an ulp or two.  A 16-bit result that another operator reads should round as the
-// exact one does: every fp32 error turns some of the roundings, and the reader sees those as 2^-8.
-__device__ __forceinline__ float sigmoid_exact_f32(float v) { return __fdiv_rn(1.f, 1.f + expf(-v)); }
-// log(1 + exp(v)); above 20 the two agree with v to fp32 precision.
-__device__ __forceinline__ float softplus_f32(float v) { return v > 20.f ? v : log1pf(__expf(v)); }
 __device__ __forceinline__ float exp2_f32(float v) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
-
+__device__ __forceinline__ float reciprocal_f32(float v) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
 constexpr float LOG2_E = 1.4426950408889634f;
 
+// exp(-v) may overflow to infinity: the quotient is then 0, which is the limit.
+__device__ __forceinline__ float sigmoid_f32(float v) { return reciprocal_f32(1.f + exp2_f32(-LOG2_E * v)); }
+// The same to within an ulp or two.  A 16-bit result that another operator reads at once should round as
+// the exact one does: every fp32 error turns some of the roundings, and the reader sees those as 2^-8.
+__device__ __forceinline__ float sigmoid_exact_f32(float v) { return __fdiv_rn(1.f, 1.f + expf(-v)); }
+// log(1 + exp(v)); above 20 the two agree with v to fp32 precision.
+__device__ __forceinline__ float softplus_f32(float v) { return v > 20.f ? v : log1pf(__expf(v)); }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline bool aligned(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 inline size_t dtype_bytes(int dtype) { return dtype == FPDE_F32 ? 4 : 2; }

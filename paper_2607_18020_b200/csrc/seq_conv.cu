@@ -11,59 +11,130 @@
 // keeps the last W values of g and emits the gradient of the node W-1 behind.  The weights' gradient
 // needs sums over all rows and nodes: every block leaves one partial sum per channel and tap, and a
 // second kernel adds them in a fixed order.
+#include <type_traits>
+
 #include "seq_common.cuh"
 
 namespace fpde {
 namespace {
 
 constexpr int CONV_LANES = 32;    // channel packs of a block
-constexpr int CONV_ROWS = 8;      // pieces of a row marched by a block
-constexpr int CONV_NODES = 16;    // nodes of a piece
+constexpr int CONV_ROWS = 4;      // pieces of a row marched by a block
+constexpr int CONV_THREADS = CONV_LANES * CONV_ROWS;
+constexpr int GROUP = 4;          // nodes computed together
+constexpr int MOST_NODES = 256;  // of a piece
+constexpr int AHEAD = 2;          // groups on their way per thread and array (a power of two); four are no faster
 
 struct ConvShape {
     int64_t length, x_batch, x_node, gy_batch, gy_node;
     int channels, silu;
     int groups;     // blocks along the channels
     int spans;      // blocks along a row
+    int nodes;      // nodes of a piece (a multiple of GROUP)
 };
 
+// A thread's own nodes of one array, a few groups ahead of where it computes: 4- and 8-byte packs travel
+// by cp.async into shared memory that only this thread reads (no registers held, no barrier needed),
+// 2-byte ones, which cp.async does not have, through registers one group ahead.
 template <typename T, int VEC>
-__device__ __forceinline__ void load_node(float (&out)[VEC], const T* p, bool there) {
-    if (there) {
-        const Pack<T, VEC> k = load_pack<T, VEC>(p);
+struct Feed {
+    static constexpr int BYTES = sizeof(T) * VEC;
+    static constexpr bool ASYNC = BYTES >= 4;
+    static constexpr int SLOTS = ASYNC ? AHEAD * GROUP : 1;
+    using P = Pack<T, VEC>;
+    P (*ring)[CONV_THREADS];      // [SLOTS][threads]
+    P held[ASYNC ? 1 : GROUP];
+    const T* p;
+    int64_t node;
+    int left;                     // nodes from p on that exist
+    int tid;
+
+    __device__ __forceinline__ void request(int slot) {      // the next GROUP nodes
+        const T* q = p;
+        if (ASYNC) {
+            const uint32_t dst = static_cast<uint32_t>(__cvta_generic_to_shared(&ring[slot * GROUP][tid]));
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) out[i] = to_f32<T>(k.v[i]);
-    } else {
+            for (int k = 0; k < GROUP; ++k, q += node) {
+                if (k < left) asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst + k * (uint32_t)(CONV_THREADS * BYTES)), "l"(q), "n"(BYTES < 4 ? 4 : BYTES) : "memory");
+                else ring[slot * GROUP + k][tid] = P{};
+            }
+        } else {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) out[i] = 0.f;
+            for (int k = 0; k < GROUP; ++k, q += node) {
+                held[k] = P{};
+                if (k < left) held[k] = load_pack<T, VEC>(q);
+            }
+        }
+        p = q;
+        left -= GROUP;
     }
+    __device__ __forceinline__ P get(int slot, int k) const { return ASYNC ? ring[slot * GROUP + k][tid] : held[k]; }
+};
+__device__ __forceinline__ void feed_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void feed_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD - 1) : "memory"); }
+__device__ __forceinline__ int clamp_left(int64_t n) { return n < 0 ? 0 : n > (1 << 30) ? 1 << 30 : (int)n; }
+
+struct ConvWhere {
+    int c;              // first channel of the thread
+    int span;
+    int64_t b, t0;      // row; first node of the thread's piece
+};
+template <int VEC>
+__device__ __forceinline__ ConvWhere conv_where(const ConvShape& s) {
+    ConvWhere w;
+    int64_t blk = blockIdx.x;
+    w.c = ((int)(blk % s.groups) * CONV_LANES + threadIdx.x) * VEC;
+    blk /= s.groups;
+    w.span = (int)(blk % s.spans);
+    w.b = blk / s.spans;
+    w.t0 = ((int64_t)w.span * CONV_ROWS + threadIdx.y) * s.nodes;
+    return w;
+}
+
+template <typename T, int VEC>
+__device__ __forceinline__ Pack<T, VEC> pack_at(const T* p, bool there) {
+    Pack<T, VEC> k;
+    if (there) return load_pack<T, VEC>(p);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) k.v[i] = from_f32<T>(0.f);
+    return k;
 }
 
 // x at node t of the row; before node 0 the window of the call before, or zeros.
 template <typename T, int VEC, int W>
-__device__ __forceinline__ void load_x(float (&out)[VEC], const T* x, int64_t x_node, const T* window, int64_t t,
-                                       int64_t length, int channels) {
-    if (t >= 0) load_node<T, VEC>(out, x + t * x_node, t < length);
-    else load_node<T, VEC>(out, window + (t + W - 1) * channels, window != nullptr && t + W - 1 >= 0);
+__device__ __forceinline__ Pack<T, VEC> x_at(const T* x, int64_t x_node, const T* window, int64_t t, int64_t length, int channels) {
+    if (t >= 0) return pack_at<T, VEC>(x + t * x_node, t < length);
+    return pack_at<T, VEC>(window + (t + W - 1) * channels, window != nullptr && t + W - 1 >= 0);
+}
+
+template <typename T, int VEC>
+__device__ __forceinline__ void widen(float (&out)[VEC], const Pack<T, VEC>& k) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) out[i] = to_f32<T>(k.v[i]);
 }
 
 template <typename T, int VEC, int W>
-__global__ void __launch_bounds__(CONV_LANES* CONV_ROWS) conv_fwd_kernel(
+__global__ void __launch_bounds__(CONV_THREADS) conv_fwd_kernel(
     const T* __restrict__ x, const float* __restrict__ weight, const float* __restrict__ bias, const T* __restrict__ state,
     T* __restrict__ y, T* __restrict__ state_out, ConvShape s) {
     pdl_wait_then_trigger();
-    int64_t blk = blockIdx.x;
-    const int group = (int)(blk % s.groups);
-    blk /= s.groups;
-    const int span = (int)(blk % s.spans);
-    const int64_t b = blk / s.spans;
-    const int c = (group * CONV_LANES + threadIdx.x) * VEC;
+    using F = Feed<T, VEC>;
+    __shared__ Pack<T, VEC> ring[F::SLOTS][CONV_THREADS];
+    const ConvWhere at = conv_where<VEC>(s);
+    const int c = at.c;
     if (c >= s.channels) return;
-    const int64_t t0 = ((int64_t)span * CONV_ROWS + threadIdx.y) * CONV_NODES;
-    const T* xr = x + b * s.x_batch + c;
-    const T* win = state ? state + b * (W - 1) * (int64_t)s.channels + c : nullptr;
-    T* yr = y + b * s.length * s.channels + c;
-    if (t0 < s.length) {
+    const T* xr = x + at.b * s.x_batch + c;
+    const T* win = state ? state + at.b * (W - 1) * (int64_t)s.channels + c : nullptr;
+    if (at.t0 < s.length) {
+        const int total = (int)(s.length - at.t0 < s.nodes ? s.length - at.t0 : s.nodes);
+        F fx;
+        fx.ring = ring; fx.p = xr + at.t0 * s.x_node; fx.node = s.x_node; fx.left = total; fx.tid = threadIdx.y * CONV_LANES + threadIdx.x;
+        if (F::ASYNC) {
+#pragma unroll
+            for (int a = 0; a < AHEAD - 1; ++a) { fx.request(a); feed_commit(); }
+        } else {
+            fx.request(0);
+        }
         float w[VEC][W], bs[VEC];
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
@@ -71,56 +142,79 @@ __global__ void __launch_bounds__(CONV_LANES* CONV_ROWS) conv_fwd_kernel(
 #pragma unroll
             for (int j = 0; j < W; ++j) w[i][j] = weight[(int64_t)(c + i) * W + j];
         }
-        float xs[CONV_NODES + W - 1][VEC];
+        float xs[GROUP + W - 1][VEC];           // the W-1 nodes before the group, then the group
 #pragma unroll
-        for (int k = 0; k < CONV_NODES + W - 1; ++k)
-            load_x<T, VEC, W>(xs[k], xr, s.x_node, win, t0 + k - (W - 1), s.length, s.channels);
+        for (int j = 0; j < W - 1; ++j)
+            widen<T, VEC>(xs[GROUP + j], x_at<T, VEC, W>(xr, s.x_node, win, at.t0 + j - (W - 1), s.length, s.channels));
+        T* yp = y + (at.b * s.length + at.t0) * s.channels + c;
+        int slot = 0;
+        for (int t = 0; t < total; t += GROUP) {
 #pragma unroll
-        for (int k = 0; k < CONV_NODES; ++k) {
-            if (t0 + k >= s.length) break;
-            float v[VEC];
+            for (int j = 0; j < W - 1; ++j)
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                float pre = bs[i];
+                for (int i = 0; i < VEC; ++i) xs[j][i] = xs[GROUP + j][i];
+            if (F::ASYNC) { fx.request((slot + AHEAD - 1) % AHEAD); feed_commit(); feed_wait(); }
 #pragma unroll
-                for (int j = 0; j < W; ++j) pre = fmaf(w[i][j], xs[k + j][i], pre);
-                v[i] = s.silu ? pre * sigmoid_exact_f32(pre) : pre;
+            for (int k = 0; k < GROUP; ++k) widen<T, VEC>(xs[W - 1 + k], fx.get(slot, k));
+            if (F::ASYNC) slot = (slot + 1) % AHEAD;
+            else fx.request(0);
+#pragma unroll
+            for (int k = 0; k < GROUP; ++k) {
+                float v[VEC];
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    float pre = bs[i];
+#pragma unroll
+                    for (int j = 0; j < W; ++j) pre = fmaf(w[i][j], xs[k + j][i], pre);
+                    v[i] = s.silu ? pre * sigmoid_f32(pre) : pre;
+                }
+                if (t + k < total) store_pack<T, VEC>(yp + k * (int64_t)s.channels, v);
             }
-            store_pack<T, VEC>(yr + (t0 + k) * s.channels, v);
+            yp += GROUP * (int64_t)s.channels;
         }
     }
     // the window that is left: the last W-1 nodes of the row, or of window and row together
-    if (state_out != nullptr && span == 0 && threadIdx.y == 0) {
+    if (state_out != nullptr && at.span == 0 && threadIdx.y == 0) {
 #pragma unroll
-        for (int j = 0; j < W - 1; ++j) {
-            float v[VEC];
-            load_x<T, VEC, W>(v, xr, s.x_node, win, s.length - (W - 1) + j, s.length, s.channels);
-            store_pack<T, VEC>(state_out + (b * (W - 1) + j) * s.channels + c, v);
-        }
+        for (int j = 0; j < W - 1; ++j)
+            *reinterpret_cast<Pack<T, VEC>*>(state_out + (at.b * (W - 1) + j) * s.channels + c) =
+                x_at<T, VEC, W>(xr, s.x_node, win, s.length - (W - 1) + j, s.length, s.channels);
     }
 }
 
+// A thread emits the gradients of window-and-row positions t0 .. t0 + nodes - 1 (position f is node
+// f - (W-1)); the g of node f is formed at the same time, after a halo of W-1 nodes.
 // One block's sums go to partial[(b * spans + span)][channels][W + 1]: taps, then bias.
 template <typename T, int VEC, int W>
-__global__ void __launch_bounds__(CONV_LANES* CONV_ROWS) conv_bwd_kernel(
+__global__ void __launch_bounds__(CONV_THREADS) conv_bwd_kernel(
     const T* __restrict__ x, const float* __restrict__ weight, const float* __restrict__ bias, const T* __restrict__ state,
     const T* __restrict__ gy, const T* __restrict__ gstate_out, T* __restrict__ gx, T* __restrict__ gstate,
     float* __restrict__ partial, ConvShape s) {
     pdl_wait_then_trigger();
+    using F = Feed<T, VEC>;
+    __shared__ Pack<T, VEC> ring_x[F::SLOTS][CONV_THREADS], ring_g[F::SLOTS][CONV_THREADS];
     __shared__ float sums[CONV_ROWS][VEC * (W + 1)][CONV_LANES];
-    int64_t blk = blockIdx.x;
-    const int group = (int)(blk % s.groups);
-    blk /= s.groups;
-    const int span = (int)(blk % s.spans);
-    const int64_t b = blk / s.spans;
-    const int c = (group * CONV_LANES + threadIdx.x) * VEC;
+    const ConvWhere at = conv_where<VEC>(s);
+    const int c = at.c;
     float acc[VEC][W + 1] = {};
-    // this thread emits the gradients of window-and-row positions f0 .. f0 + NODES - 1 (position f is node f - (W-1))
-    const int64_t f0 = ((int64_t)span * CONV_ROWS + threadIdx.y) * CONV_NODES;
-    if (c < s.channels && f0 < s.length + W - 1) {
-        const T* xr = x + b * s.x_batch + c;
-        const T* gr = gy + b * s.gy_batch + c;
-        const T* win = state ? state + b * (W - 1) * (int64_t)s.channels + c : nullptr;
+    if (c < s.channels && at.t0 < s.length + W - 1) {
+        const int total = (int)(s.length + W - 1 - at.t0 < s.nodes ? s.length + W - 1 - at.t0 : s.nodes);   // positions
+        const int nodes = min(total, clamp_left(s.length - at.t0));                                          // of these, nodes that exist
+        const T* xr = x + at.b * s.x_batch + c;
+        const T* gr = gy + at.b * s.gy_batch + c;
+        const T* win = state ? state + at.b * (W - 1) * (int64_t)s.channels + c : nullptr;
+        F fx, fg;
+        fx.ring = ring_x; fx.p = xr + at.t0 * s.x_node; fx.node = s.x_node;
+        fg.ring = ring_g; fg.p = gr + at.t0 * s.gy_node; fg.node = s.gy_node;
+        fx.left = fg.left = nodes;
+        fx.tid = fg.tid = threadIdx.y * CONV_LANES + threadIdx.x;
+        if (F::ASYNC) {
+#pragma unroll
+            for (int a = 0; a < AHEAD - 1; ++a) { fx.request(a); fg.request(a); feed_commit(); }
+        } else {
+            fx.request(0);
+            fg.request(0);
+        }
         float w[VEC][W], bs[VEC];
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
@@ -128,64 +222,105 @@ __global__ void __launch_bounds__(CONV_LANES* CONV_ROWS) conv_bwd_kernel(
 #pragma unroll
             for (int j = 0; j < W; ++j) w[i][j] = weight[(int64_t)(c + i) * W + j];
         }
-        float xs[W][VEC], g[W][VEC];    // x[t-W+1 .. t] and g[t-W+1 .. t]
+        // g of one node from the W values of x that reach it
+        auto slope = [&](float gv, const float (&xv)[W], int i) {
+            if (!s.silu) return gv;
+            float pre = bs[i];
 #pragma unroll
-        for (int j = 0; j < W; ++j)
+            for (int j = 0; j < W; ++j) pre = fmaf(w[i][j], xv[j], pre);
+            const float q = sigmoid_f32(pre);
+            return gv * (q * fmaf(pre, 1.f - q, 1.f));
+        };
+        float xs[GROUP + W - 1][VEC], g[GROUP + W - 1][VEC];      // the W-1 nodes before the group, then the group
+        {
+            float h[2 * W - 2 + (W == 1)][VEC];                    // x from 2 (W-1) nodes before
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) g[j][i] = 0.f;
+            for (int j = 0; j < 2 * (W - 1); ++j)
+                widen<T, VEC>(h[j], x_at<T, VEC, W>(xr, s.x_node, win, at.t0 - 2 * (W - 1) + j, s.length, s.channels));
 #pragma unroll
-        for (int j = 1; j < W; ++j)
-            load_x<T, VEC, W>(xs[j], xr, s.x_node, win, f0 - (W - 1) + j - W, s.length, s.channels);
+            for (int k = 0; k < W - 1; ++k) {
+                const int64_t t = at.t0 - (W - 1) + k;
+                const bool inside = t >= 0 && t < s.length;
+                float gv[VEC];
+                widen<T, VEC>(gv, pack_at<T, VEC>(gr + t * s.gy_node, inside));
 #pragma unroll
-        for (int k = -(W - 1); k < CONV_NODES; ++k) {      // node whose g is formed; the first W-1 are the halo
-            const int64_t t = f0 + k;
-            if (k >= 0 && t >= s.length + W - 1) break;
+                for (int i = 0; i < VEC; ++i) {
+                    float xv[W];
+#pragma unroll
+                    for (int j = 0; j < W; ++j) xv[j] = h[k + j][i];
+                    g[GROUP + k][i] = inside ? slope(gv[i], xv, i) : 0.f;
+                    xs[GROUP + k][i] = h[W - 1 + k][i];
+                }
+            }
+        }
+        T* gxp = gx + (at.b * s.length + at.t0 - (W - 1)) * s.channels + c;      // of the thread's first position
+        int slot = 0;
+        for (int t = 0; t < total; t += GROUP) {
 #pragma unroll
             for (int j = 0; j < W - 1; ++j)
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) { xs[j][i] = xs[j + 1][i]; g[j][i] = g[j + 1][i]; }
-            load_x<T, VEC, W>(xs[W - 1], xr, s.x_node, win, t, s.length, s.channels);
-            const bool inside = t >= 0 && t < s.length;
-            float gv[VEC];
-            load_node<T, VEC>(gv, gr + t * s.gy_node, inside);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                float d = gv[i];
-                if (s.silu) {
-                    float pre = bs[i];
-#pragma unroll
-                    for (int j = 0; j < W; ++j) pre = fmaf(w[i][j], xs[j][i], pre);
-                    const float q = sigmoid_f32(pre);
-                    d *= q * fmaf(pre, 1.f - q, 1.f);
-                }
-                d = inside ? d : 0.f;
-                g[W - 1][i] = d;
-                if (k >= 0 && inside) {
-#pragma unroll
-                    for (int j = 0; j < W; ++j) acc[i][j] = fmaf(d, xs[j][i], acc[i][j]);
-                    acc[i][W] += d;
-                }
+                for (int i = 0; i < VEC; ++i) { xs[j][i] = xs[GROUP + j][i]; g[j][i] = g[GROUP + j][i]; }
+            if (F::ASYNC) {
+                fx.request((slot + AHEAD - 1) % AHEAD);
+                fg.request((slot + AHEAD - 1) % AHEAD);
+                feed_commit();
+                feed_wait();
             }
-            if (k >= 0) {
-                float v[VEC];
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    v[i] = 0.f;
-#pragma unroll
-                    for (int j = 0; j < W; ++j) v[i] = fmaf(w[i][j], g[W - 1 - j][i], v[i]);
-                }
-                if (gstate_out != nullptr && t >= s.length) {   // position t is entry t - length of the window that was left
-                    float e[VEC];
-                    load_node<T, VEC>(e, gstate_out + (b * (W - 1) + (t - s.length)) * s.channels + c, true);
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) v[i] += e[i];
-                }
-                if (t >= W - 1) {
-                    if (gx != nullptr) store_pack<T, VEC>(gx + (b * s.length + t - (W - 1)) * s.channels + c, v);
-                } else if (gstate != nullptr) {
-                    store_pack<T, VEC>(gstate + (b * (W - 1) + t) * s.channels + c, v);
-                }
+            for (int k = 0; k < GROUP; ++k) {
+                widen<T, VEC>(xs[W - 1 + k], fx.get(slot, k));
+                widen<T, VEC>(g[W - 1 + k], fg.get(slot, k));
             }
+            if (F::ASYNC) slot = (slot + 1) % AHEAD;
+            else { fx.request(0); fg.request(0); }
+            // INNER: every node of the group exists and none of its positions lies in a window
+            auto compute = [&](auto inner) {
+                constexpr bool INNER = decltype(inner)::value;
+#pragma unroll
+                for (int k = 0; k < GROUP; ++k) {
+                    const bool inside = INNER || t + k < nodes;
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) {
+                        float xv[W];
+#pragma unroll
+                        for (int j = 0; j < W; ++j) xv[j] = xs[k + j][i];
+                        const float d = inside ? slope(g[W - 1 + k][i], xv, i) : 0.f;   // not a product: x may hold NaN
+                        g[W - 1 + k][i] = d;
+                        if (inside) {
+#pragma unroll
+                            for (int j = 0; j < W; ++j) acc[i][j] = fmaf(d, xv[j], acc[i][j]);
+                            acc[i][W] += d;
+                        }
+                    }
+                    float v[VEC];
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) {
+                        v[i] = 0.f;
+#pragma unroll
+                        for (int j = 0; j < W; ++j) v[i] = fmaf(w[i][j], g[W - 1 + k - j][i], v[i]);
+                    }
+                    if (INNER) {
+                        store_pack<T, VEC>(gxp + k * (int64_t)s.channels, v);
+                        continue;
+                    }
+                    const int64_t f = at.t0 + t + k;
+                    if (t + k >= total) continue;
+                    if (f >= s.length && gstate_out != nullptr) {      // entry f - length of the window that was left
+                        float e[VEC];
+                        widen<T, VEC>(e, load_pack<T, VEC>(gstate_out + (at.b * (W - 1) + (f - s.length)) * s.channels + c));
+#pragma unroll
+                        for (int i = 0; i < VEC; ++i) v[i] += e[i];
+                    }
+                    if (f >= W - 1) {
+                        if (gx != nullptr) store_pack<T, VEC>(gxp + k * (int64_t)s.channels, v);
+                    } else if (gstate != nullptr) {
+                        store_pack<T, VEC>(gstate + (at.b * (W - 1) + f) * s.channels + c, v);
+                    }
+                }
+            };
+            if (t + GROUP <= nodes && at.t0 + t >= W - 1 && gx != nullptr) compute(std::true_type{});
+            else compute(std::false_type{});
+            gxp += GROUP * (int64_t)s.channels;
         }
     }
 #pragma unroll
@@ -193,10 +328,10 @@ __global__ void __launch_bounds__(CONV_LANES* CONV_ROWS) conv_bwd_kernel(
 #pragma unroll
         for (int j = 0; j <= W; ++j) sums[threadIdx.y][i * (W + 1) + j][threadIdx.x] = acc[i][j];
     __syncthreads();
-    const int c0 = group * CONV_LANES * VEC;
-    float* out = partial + (b * s.spans + span) * (int64_t)s.channels * (W + 1) + (int64_t)c0 * (W + 1);
+    const int c0 = c - threadIdx.x * VEC;
+    float* out = partial + (at.b * s.spans + at.span) * (int64_t)s.channels * (W + 1) + (int64_t)c0 * (W + 1);
     const int here = min(CONV_LANES * VEC, s.channels - c0) * (W + 1);
-    for (int e = threadIdx.y * CONV_LANES + threadIdx.x; e < here; e += CONV_LANES * CONV_ROWS) {
+    for (int e = threadIdx.y * CONV_LANES + threadIdx.x; e < here; e += CONV_THREADS) {
         const int lane = e / (VEC * (W + 1)), k = e % (VEC * (W + 1));
         float v = 0.f;
 #pragma unroll
@@ -266,8 +401,15 @@ int check_conv(const fpde_conv_args* a, bool step) {
     return FPDE_OK;
 }
 
-int conv_spans(const fpde_conv_args* a, int64_t positions) {
-    return (int)ceil_div(positions > 0 ? positions : 1, CONV_ROWS * CONV_NODES);
+// Nodes of a thread's piece: long pieces re-read fewer halo nodes, short ones give a small grid more
+// threads.  Doubled while there are still 1024 threads per SM.
+int conv_nodes(const fpde_conv_args* a, int64_t positions) {
+    int nodes = 2 * GROUP;
+    while (nodes < MOST_NODES && a->batch * ceil_div(a->channels, 2) * ceil_div(positions, 2 * nodes) >= 148 * 1024) nodes *= 2;
+    return nodes;
+}
+int64_t conv_spans(const fpde_conv_args* a, int64_t positions) {
+    return ceil_div(positions > 0 ? positions : 1, (int64_t)CONV_ROWS * conv_nodes(a, positions));
 }
 
 // Channels of one thread: 16 bytes of them where every row of every array starts on 16 bytes.
@@ -281,29 +423,33 @@ bool conv_wide(const fpde_conv_args* a, int vec, bool backward) {
     return ok && aligned(a->y, e * vec) && aligned(a->state_out, e * vec);
 }
 
-template <typename T, int VEC, int W>
-cudaError_t conv_launch(const fpde_conv_args* a, bool backward, cudaStream_t st) {
-    ConvShape s{a->length, a->x_batch, a->x_node, a->gy_batch, a->gy_node, (int)a->channels, a->silu, 0, 0};
+template <typename T, int VEC, int W, bool backward>
+cudaError_t conv_launch(const fpde_conv_args* a, cudaStream_t st) {
+    ConvShape s{a->length, a->x_batch, a->x_node, a->gy_batch, a->gy_node, (int)a->channels, a->silu, 0, 0, 0};
     s.groups = (int)ceil_div(a->channels, CONV_LANES * VEC);
-    s.spans = conv_spans(a, backward ? a->length + W - 1 : a->length);
-    const int64_t blocks = a->batch * s.groups * s.spans;
+    const int64_t positions = backward ? a->length + W - 1 : a->length, spans = conv_spans(a, positions);
+    s.spans = (int)spans;
+    s.nodes = conv_nodes(a, positions);
+    const int64_t blocks = a->batch * s.groups * spans;
     if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
     const dim3 grid((unsigned)blocks), block(CONV_LANES, CONV_ROWS);
-    if (!backward)
+    if constexpr (!backward)
         return launch_kernel(conv_fwd_kernel<T, VEC, W>, grid, block, st, (const T*)a->x, a->weight, a->bias, (const T*)a->state,
                              (T*)a->y, (T*)a->state_out, s);
-    float* partial = (float*)a->workspace;
-    cudaError_t e = launch_kernel(conv_bwd_kernel<T, VEC, W>, grid, block, st, (const T*)a->x, a->weight, a->bias,
-                                  (const T*)a->state, (const T*)a->gy, (const T*)a->gstate_out, (T*)a->gx, (T*)a->gstate, partial, s);
-    if (e != cudaSuccess) return e;
-    return launch_kernel(conv_sum_kernel, dim3((unsigned)ceil_div(a->channels * (W + 1), 32)), dim3(32, 8), st,
-                         (const float*)partial, a->batch * s.spans, (int)a->channels, W, a->gweight, a->gbias);
+    else {
+        float* partial = (float*)a->workspace;
+        cudaError_t e = launch_kernel(conv_bwd_kernel<T, VEC, W>, grid, block, st, (const T*)a->x, a->weight, a->bias,
+                                      (const T*)a->state, (const T*)a->gy, (const T*)a->gstate_out, (T*)a->gx, (T*)a->gstate, partial, s);
+        if (e != cudaSuccess) return e;
+        return launch_kernel(conv_sum_kernel, dim3((unsigned)ceil_div(a->channels * (W + 1), 32)), dim3(32, 8), st,
+                             (const float*)partial, a->batch * spans, (int)a->channels, W, a->gweight, a->gbias);
+    }
 }
 
 template <typename T, int W>
 cudaError_t conv_by_pack(const fpde_conv_args* a, bool backward, cudaStream_t st) {
-    if (conv_wide<T>(a, 4, backward)) return conv_launch<T, 4, W>(a, backward, st);
-    return conv_launch<T, 1, W>(a, backward, st);
+    if (backward) return conv_wide<T>(a, 2, true) ? conv_launch<T, 2, W, true>(a, st) : conv_launch<T, 1, W, true>(a, st);
+    return conv_wide<T>(a, 2, false) ? conv_launch<T, 2, W, false>(a, st) : conv_launch<T, 1, W, false>(a, st);
 }
 
 template <typename T>
