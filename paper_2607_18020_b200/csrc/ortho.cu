@@ -11,7 +11,7 @@ namespace {
 
 constexpr float NS_A = 3.4445f, NS_B = -4.775f, NS_C = 2.0315f;
 constexpr float SCALE = 16384.f;    // 2^14: matrices are stored times this, see the products
-constexpr int SUM_BLOCKS = 64;      // blocks that sum the squares of one matrix
+constexpr int MOST_SUMS = 256;      // blocks that sum the squares of one matrix, at most
 
 // What the matrices are read from and written to.
 struct OrthoIo {
@@ -35,25 +35,31 @@ __device__ __forceinline__ float update_at(const OrthoIo& io, int64_t k, int64_t
 }
 
 // Moves the momentum on (muon) and leaves each block's sum of squares of the update, in 64 bits: the
-// squares of gradients of any scale fit.
+// squares of gradients of any scale fit.  A warp takes whole rows, `blocks` blocks share a matrix.
 template <typename T>
-__global__ void __launch_bounds__(256) ortho_square_kernel(OrthoIo io, double* __restrict__ sums) {
+__global__ void __launch_bounds__(256) ortho_square_kernel(OrthoIo io, double* __restrict__ sums, int blocks) {
     pdl_wait_then_trigger();
     __shared__ double part[8];
-    const int64_t k = blockIdx.x / SUM_BLOCKS, all = (int64_t)io.rows * io.cols;
+    const int k = blockIdx.x / blocks, lane = threadIdx.x % 32;
+    const float decay = io.decay;
     double v = 0.0;
-    for (int64_t e = (int64_t)(blockIdx.x % SUM_BLOCKS) * 256 + threadIdx.x; e < all; e += SUM_BLOCKS * 256) {
-        const int64_t r = e / io.cols, c = e % io.cols;
-        if (io.momentum != nullptr) {
-            float* mom = io.momentum + k * all + e;
-            *mom = fmaf(io.decay, *mom, to_f32<T>(((const T*)io.grad)[k * io.grad_matrix + r * io.grad_row + c]));
+    for (int r = (blockIdx.x % blocks) * 8 + threadIdx.x / 32; r < io.rows; r += blocks * 8) {
+        const T* g = (const T*)io.grad + k * io.grad_matrix + r * io.grad_row;
+        float* mom = io.momentum ? io.momentum + ((int64_t)k * io.rows + r) * io.cols : nullptr;
+#pragma unroll 8
+        for (int c = lane; c < io.cols; c += 32) {
+            float u = to_f32<T>(g[c]);
+            if (mom != nullptr) {
+                const float next = fmaf(decay, mom[c], u);
+                mom[c] = next;
+                u = io.nesterov ? fmaf(decay, next, u) : next;
+            }
+            v += (double)u * u;
         }
-        const double u = update_at<T>(io, k, r, c);
-        v += u * u;
     }
 #pragma unroll
     for (int m = 16; m > 0; m /= 2) v += __shfl_xor_sync(~0u, v, m);
-    if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = v;
+    if (lane == 0) part[threadIdx.x / 32] = v;
     __syncthreads();
     if (threadIdx.x == 0) {
 #pragma unroll
@@ -62,40 +68,60 @@ __global__ void __launch_bounds__(256) ortho_square_kernel(OrthoIo io, double* _
     }
 }
 
-__device__ __forceinline__ float inverse_norm(const double* sums, double eps) {
-    double v = 0.0;
-    for (int i = 0; i < SUM_BLOCKS; ++i) v += sums[i];
+// 1 / (|U| + eps) from the blocks' sums (at most 256), added in the same order by every block that asks.
+__device__ __forceinline__ float inverse_norm(const double* sums, int blocks, double eps, double (&part)[8]) {
+    double v = threadIdx.x < blocks ? sums[threadIdx.x] : 0.0;
+#pragma unroll
+    for (int m = 16; m > 0; m /= 2) v += __shfl_xor_sync(~0u, v, m);
+    if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = v;
+    __syncthreads();
+    v = 0.0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v += part[i];
     return (float)(1.0 / (sqrt(v) + eps));
 }
 
-__device__ __forceinline__ void store_planes(__half* hi, __half* lo, float v) {     // v: already scaled
-    const __half h = __float2half_rn(v);
-    *hi = h;
-    *lo = __float2half_rn(v - __half2float(h));
+// Eight values of a row, already scaled, as hi and lo halves.
+__device__ __forceinline__ void split8(const float (&v)[8], Pack<__half, 8>& hi, Pack<__half, 8>& lo) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        hi.v[i] = __float2half_rn(v[i]);
+        lo.v[i] = __float2half_rn(v[i] - __half2float(hi.v[i]));
+    }
 }
 
 // The first X (m x n, padded to mp x np) of every matrix, turned where the matrix is taller than wide.
+// A block moves 64 x 64 elements through shared memory: read along the matrix's rows, written along X's.
 template <typename T>
-__global__ void __launch_bounds__(256) ortho_start_kernel(OrthoIo io, const double* __restrict__ sums, __half* __restrict__ x) {
+__global__ void __launch_bounds__(256) ortho_start_kernel(OrthoIo io, const double* __restrict__ sums, int blocks, __half* __restrict__ x) {
     pdl_wait_then_trigger();
-    __shared__ float tile[32][33];
-    __shared__ float scale;
-    const int across = io.np / 32, down = io.mp / 32;
-    const int64_t k = blockIdx.x / (across * down);
-    const int t = (int)(blockIdx.x % (across * down)), i0 = t / across * 32, j0 = t % across * 32;
-    if (threadIdx.x == 0) scale = inverse_norm(sums + k * SUM_BLOCKS, io.eps) * SCALE;
-    const int a = threadIdx.x / 32, b = threadIdx.x % 32;
-    for (int r = a; r < 32; r += 8) {
-        const int row = (io.turned ? j0 : i0) + r, col = (io.turned ? i0 : j0) + b;
-        tile[r][b] = row < io.rows && col < io.cols ? update_at<T>(io, k, row, col) : 0.f;
+    __shared__ float tile[64][65];
+    __shared__ double part[8];
+    const int across = io.np / 64, down = io.mp / 64;
+    const int k = blockIdx.x / (across * down), t = blockIdx.x % (across * down), i0 = t / across * 64, j0 = t % across * 64;
+    const float scale = inverse_norm(sums + (int64_t)k * blocks, blocks, io.eps, part) * SCALE;
+    const int r0 = io.turned ? j0 : i0, c0 = io.turned ? i0 : j0;
+#pragma unroll
+    for (int e = threadIdx.x; e < 64 * 64; e += 256) {
+        const int r = e / 64, c = e % 64;
+        tile[r][c] = r0 + r < io.rows && c0 + c < io.cols ? update_at<T>(io, k, r0 + r, c0 + c) : 0.f;
     }
     __syncthreads();
     const int64_t plane = (int64_t)io.mp * io.np;
-    for (int r = a; r < 32; r += 8) {
-        const bool there = i0 + r < io.m && j0 + b < io.n;       // padding stays zero, whatever the norm is
-        const float v = there ? (io.turned ? tile[b][r] : tile[r][b]) * scale : 0.f;
-        __half* p = x + 2 * k * plane + (int64_t)(i0 + r) * io.np + j0 + b;
-        store_planes(p, p + plane, v);
+#pragma unroll
+    for (int e = threadIdx.x; e < 64 * 8; e += 256) {
+        const int i = e / 8, j = e % 8 * 8;
+        float v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {       // padding stays zero, whatever the norm is
+            const bool there = i0 + i < io.m && j0 + j + q < io.n;
+            v[q] = there ? (io.turned ? tile[j + q][i] : tile[i][j + q]) * scale : 0.f;
+        }
+        Pack<__half, 8> hi, lo;
+        split8(v, hi, lo);
+        Pack<__half, 8>* p = reinterpret_cast<Pack<__half, 8>*>(x + 2 * k * plane + (int64_t)(i0 + i) * io.np + j0 + j);
+        p[0] = hi;
+        p[plane / 8] = lo;
     }
 }
 
@@ -404,7 +430,7 @@ OrthoSpace space(int64_t count, int64_t m, int64_t n) {
     const int64_t mp = padded(m), np = padded(n);
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
-    w.sums = take(count * SUM_BLOCKS * 8);
+    w.sums = take(count * MOST_SUMS * 8);
     w.x[0] = take(count * mp * np * 4);
     w.x[1] = take(count * mp * np * 4);
     w.s = take(count * mp * mp * 4);
@@ -447,9 +473,14 @@ cudaError_t run(const fpde_ortho_args* a, bool muon, cudaStream_t st) {
     double* sums = (double*)(ws + w.sums);
     __half* x[2] = {(__half*)(ws + w.x[0]), (__half*)(ws + w.x[1])};
     __half *s = (__half*)(ws + w.s), *p = (__half*)(ws + w.p);
-    const int64_t pieces = (int64_t)(io.mp / 32) * (io.np / 32) * a->count;
+    // enough blocks for two per SM over the stack, at least 8 rows (one per warp) each
+    const int sms = sm_count_or_default();
+    int64_t blocks = ceil_div(io.rows, 8);
+    if (blocks > ceil_div(4 * sms, a->count)) blocks = ceil_div(4 * sms, a->count);
+    if (blocks > MOST_SUMS) blocks = MOST_SUMS;
+    const int64_t pieces = (int64_t)(io.mp / 64) * (io.np / 64) * a->count;
     const int64_t back = ceil_div(io.rows, 32) * ceil_div(io.cols, 32) * a->count;
-    if (pieces > 0x7fffffff || a->count * SUM_BLOCKS > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    if (pieces > 0x7fffffff || back > 0x7fffffff || a->count * blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
     CUtensorMap xk[2], xn[2], sk, pk;
     if (a->steps > 0) {
         bool ok = encode_planes(&sk, s, a->count, io.mp, io.mp, BM) && encode_planes(&pk, p, a->count, io.mp, io.mp, BM);
@@ -457,9 +488,8 @@ cudaError_t run(const fpde_ortho_args* a, bool muon, cudaStream_t st) {
             ok = ok && encode_planes(&xk[i], x[i], a->count, io.mp, io.np, BM) && encode_planes(&xn[i], x[i], a->count, io.mp, io.np, BK);
         if (!ok) return cudaErrorNotSupported;
     }
-    FPDE_TRY(launch_kernel(ortho_square_kernel<T>, dim3((unsigned)(a->count * SUM_BLOCKS)), dim3(256), st, io, sums));
-    FPDE_TRY(launch_kernel(ortho_start_kernel<T>, dim3((unsigned)pieces), dim3(256), st, io, (const double*)sums, x[0]));
-    const int sms = sm_count_or_default();
+    FPDE_TRY(launch_kernel(ortho_square_kernel<T>, dim3((unsigned)(a->count * blocks)), dim3(256), st, io, sums, (int)blocks));
+    FPDE_TRY(launch_kernel(ortho_start_kernel<T>, dim3((unsigned)pieces), dim3(256), st, io, (const double*)sums, (int)blocks, x[0]));
     int at = 0;
     for (int i = 0; i < a->steps; ++i, at ^= 1) {
         constexpr bool PAIR = sizeof(T) == 4;
