@@ -56,8 +56,49 @@ __device__ __forceinline__ float sigmoid_f32(float v) { return reciprocal_f32(1.
 // The same to within an ulp or two.  A 16-bit result that another operator reads at once should round as
 // the exact one does: every fp32 error turns some of the roundings, and the reader sees those as 2^-8.
 __device__ __forceinline__ float sigmoid_exact_f32(float v) { return __fdiv_rn(1.f, 1.f + expf(-v)); }
-// log(1 + exp(v)); above 20 the two agree with v to fp32 precision.
-__device__ __forceinline__ float softplus_f32(float v) { return v > 20.f ? v : log1pf(__expf(v)); }
+// log(1 + exp(v)) = max(v, 0) + log(1 + e), e = exp(-|v|) in (0, 1]; log(1 + e) / e is a polynomial of
+// degree 8 fitted to the relative error on [0, 1] (3e-8), so small results keep their digits.  The product
+// with log2(e) is carried in two parts: its rounding alone would cost |v| 2^-24 of the result.
+__device__ __forceinline__ float softplus_f32(float v) {
+    const float a = fmaxf(-fabsf(v), -150.f), hi = a * LOG2_E;      // exp(-150) is 0
+    const float lo = fmaf(a, 1.925963033e-8f, fmaf(a, LOG2_E, -hi));
+    float e = exp2_f32(hi);
+    e = fmaf(e, lo * 0.6931471806f, e);
+    float p = 0.00523267686f;
+    p = fmaf(p, e, -0.029505169f);
+    p = fmaf(p, e, 0.0782258362f);
+    p = fmaf(p, e, -0.136632353f);
+    p = fmaf(p, e, 0.191060022f);
+    p = fmaf(p, e, -0.248429805f);
+    p = fmaf(p, e, 0.333190978f);
+    p = fmaf(p, e, -0.499994934f);
+    p = fmaf(p, e, 0.99999994f);
+    return fmaf(e, p, v < 0.f ? 0.f : v);      // a NaN stays
+}
+
+// Pairs of fp32 values in one 64-bit register: one instruction for two multiplications or fused adds.
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t p, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p)); }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ float sum2(uint64_t p) {
+    float lo, hi;
+    unpair(p, lo, hi);
+    return lo + hi;
+}
+
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline bool aligned(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 inline size_t dtype_bytes(int dtype) { return dtype == FPDE_F32 ? 4 : 2; }

@@ -9,7 +9,7 @@
 //
 // Layout.  A thread keeps four states of one channel; S = 2, 4, 8 or 16 neighbouring lanes share a
 // channel, so a warp covers 32/S channels and the sums over states are shuffles among S lanes.  A
-// block of 128 threads marches CT = 128/S channels through tiles of nodes; the tile's dt, dt u, B and
+// block marches its threads / S channels through tiles of nodes; the tile's dt, dt u, B and
 // C are brought to shared memory once, in fp32, by loads that run along the channels.
 //
 // Long rows.  Where batch x channels gives too few blocks, a row is cut into chunks: one kernel forms
@@ -27,8 +27,9 @@
 namespace fpde {
 namespace {
 
-constexpr int THREADS = 128;
-constexpr int WARPS = THREADS / 32;
+constexpr int THREADS = 128;      // of the forward kernels
+constexpr int BACK_THREADS = 256; // of the backward kernel: halves the partial sums of gB and gC
+constexpr int FWD_BLOCKS = 4, BACK_BLOCKS = 1;     // resident blocks that the registers are budgeted for
 constexpr int TILE = 32;          // nodes of a forward tile
 constexpr int KEEP = 16;          // nodes between stored states = nodes of a backward tile
 constexpr int NS = 4;             // states of a thread
@@ -65,6 +66,28 @@ __device__ __forceinline__ Where where(const ScanShape& s) {
 
 __device__ __forceinline__ float step_of(float raw, int softplus) { return softplus ? softplus_f32(raw) : raw; }
 
+// One tile of an activation on its way: the thread's pack column and rows r0, r0 + RP, ...  The loads of a
+// tile are issued while the tile before it is computed.
+template <typename T, int VEC, int NODES, int RP>
+struct Rows {
+    static constexpr int PER = (NODES + RP - 1) / RP;
+    Pack<T, VEC> v[PER];
+    const T* p;                   // of row r0 of the tile to load next
+    int64_t node;
+    __device__ __forceinline__ void start(const T* base, int64_t node_stride, int64_t first) {
+        node = node_stride;
+        p = base + first * node_stride;
+    }
+    __device__ __forceinline__ void load(int r0, int here, bool column, int64_t advance) {   // then on by `advance` nodes
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            v[k] = Pack<T, VEC>{};
+            if (column && r0 + k * RP < here) v[k] = load_pack<T, VEC>(p + (int64_t)(k * RP) * node);
+        }
+        p += advance * node;
+    }
+};
+
 // Sum over the S lanes of a channel of four values, one per node: lane q (of S) returns the sum of
 // value q & 3 for S >= 4; S = 2: v[0], v[1] become the sums of values 2 (q & 1) and 2 (q & 1) + 1.
 template <int S>
@@ -96,83 +119,172 @@ __device__ __forceinline__ void put_sums(float (*dst)[CT], const float (&v)[4], 
     }
 }
 
-// ------------------------------------------------------------------------------------- chunk states
-// BACK = false: local[b][chunk][channel][state] = state at the chunk's end when it starts from zero,
-// sums[b][chunk][channel] = sum of dt.  BACK = true: local = what the adjoint state hands to the node
-// before the chunk when nothing comes from behind it.
-template <typename T, int S, bool BACK>
-__global__ void __launch_bounds__(THREADS) scan_local_kernel(ScanIn<T> in, float* __restrict__ local, float* __restrict__ sums,
-                                                             ScanShape s) {
+__device__ __forceinline__ uint64_t exp2_pair(uint64_t v) {
+    float a, b;
+    unpair(v, a, b);
+    return pair(exp2_f32(a), exp2_f32(b));
+}
+
+struct alignas(16) Quad {            // four floats as two pairs
+    uint64_t lo, hi;
+};
+__device__ __forceinline__ Quad quad_at(const float* p) { return *reinterpret_cast<const Quad*>(p); }
+__device__ __forceinline__ Quad quad_of(const float (&v)[NS]) { return {pair(v[0], v[1]), pair(v[2], v[3])}; }
+__device__ __forceinline__ void quad_to(float (&v)[NS], const Quad& q) { unpair(q.lo, v[0], v[1]); unpair(q.hi, v[2], v[3]); }
+
+// Four states from memory, or what stands in for those that do not exist.
+__device__ __forceinline__ Quad load_states(const float* p, int n, int states, float scale) {
+    float v[NS];
+#pragma unroll
+    for (int i = 0; i < NS; ++i) v[i] = p != nullptr && n + i < states ? p[n + i] * scale : 0.f;
+    return quad_of(v);
+}
+__device__ __forceinline__ bool states_packed(int states) { return states % NS == 0; }
+__device__ __forceinline__ void store_states(float* p, int n, int states, const Quad& q) {
+    if (states_packed(states)) {     // rows of states start on 16 bytes
+        if (n < states) *reinterpret_cast<Quad*>(p + n) = q;
+        return;
+    }
+    float v[NS];
+    quad_to(v, q);
+#pragma unroll
+    for (int i = 0; i < NS; ++i)
+        if (n + i < states) p[n + i] = v[i];
+}
+
+// ------------------------------------------------------------------------------------------ forward
+// ENDS = false: the march.  ENDS = true, for rows cut into chunks: only what the join needs,
+// local[b][chunk][channel][state] = state at the chunk's end when it starts from zero and
+// sums[b][chunk][channel] = sum of dt.
+template <typename T, int S, int VEC, bool ENDS>
+__global__ void __launch_bounds__(THREADS, FWD_BLOCKS) scan_fwd_kernel(ScanIn<T> in, const float* __restrict__ state, const float* __restrict__ enter,
+                                                           T* __restrict__ out, float* __restrict__ state_out, float* __restrict__ kept,
+                                                           float* __restrict__ local, float* __restrict__ sums, ScanShape s) {
     pdl_wait_then_trigger();
     constexpr int CT = THREADS / S, NP = S * NS;
-    __shared__ float2 sd[TILE][CT];       // dt, dt u  (BACK: dt, gy)
-    __shared__ float sb[TILE][NP];        // B (BACK: C)
+    constexpr int CP = CT / VEC, RP = THREADS / CP, RN = THREADS / NP;      // packs of a row; rows at a time
+    using Act = Rows<T, VEC, TILE, RP>;
+    using Bc = Rows<T, 1, TILE, RN>;
+    __shared__ float4 sd[TILE][CT];              // dt, dt, dt u, dt u
+    __shared__ __align__(16) float sb[TILE][NP], sc[TILE][NP];
+    __shared__ float sy[TILE][CT];               // ENDS: not used
     const Where w = where(s);
     const int tid = threadIdx.x, q = tid % S, cl = tid / S;
     const int c0 = w.tile * CT, c = c0 + cl;
     const int64_t first = (int64_t)w.chunk * s.chunk;
     const int64_t end = first + s.chunk < s.length ? first + s.chunk : s.length;
-    float a2[NS], h[NS];
+    const int64_t per = (int64_t)s.channels * s.states;
+    const int64_t at = w.b * s.chunks + w.chunk;
+    const bool mine = c < s.channels;
+    const Quad a2 = load_states(mine ? in.A + (int64_t)c * s.states : nullptr, q * NS, s.states, LOG2_E);
+    Quad h = load_states(ENDS || !mine ? nullptr : enter ? enter + at * per + (int64_t)c * s.states : state ? state + w.b * per + (int64_t)c * s.states : nullptr,
+                         q * NS, s.states, 1.f);
+    // what this thread brings in: pack column `col` of rows r0, r0 + RP, ... and state n of rows rn, rn + RN, ...
+    const int col = tid % CP * VEC, r0 = tid / CP, n = tid % NP, rn = tid / NP;
+    const bool column = c0 + col < s.channels, row_n = n < s.states;
+    float bias[VEC], dd[VEC];
 #pragma unroll
-    for (int i = 0; i < NS; ++i) {
-        const int n = q * NS + i;
-        a2[i] = c < s.channels && n < s.states ? in.A[(int64_t)c * s.states + n] * LOG2_E : 0.f;
-        h[i] = 0.f;
+    for (int i = 0; i < VEC; ++i) {
+        bias[i] = in.bias && column ? in.bias[c0 + col + i] : 0.f;
+        dd[i] = in.D && column ? in.D[c0 + col + i] : 0.f;
     }
+    Act u, dl, z;
+    Bc bt, ct;
+    u.start(in.u + w.b * s.u_batch + c0 + col, s.u_node, first + r0);
+    dl.start(in.delta + w.b * s.delta_batch + c0 + col, s.delta_node, first + r0);
+    z.start(in.z + w.b * s.z_batch + c0 + col, s.z_node, first + r0);
+    bt.start(in.B + w.b * s.B_batch + n, s.B_node, first + rn);
+    ct.start(in.C + w.b * s.C_batch + n, s.C_node, first + rn);
+    auto fetch = [&](int here) {
+        u.load(r0, here, column, TILE);
+        dl.load(r0, here, column, TILE);
+        if (!ENDS && in.z) z.load(r0, here, column, TILE);
+        bt.load(rn, here, row_n, TILE);
+        if (!ENDS) ct.load(rn, here, row_n, TILE);
+    };
+    T* op = out + (w.b * s.length + first + r0) * s.channels + c0 + col;
     float total = 0.f;
-    const int ntiles = (int)((end - first + TILE - 1) / TILE);
-    for (int k = 0; k < ntiles; ++k) {
-        const int64_t t0 = first + (int64_t)(BACK ? ntiles - 1 - k : k) * TILE;
-        const int here = (int)(end - t0 < TILE ? end - t0 : TILE);
+    int left = (int)(end - first);               // nodes of the chunk from this tile on
+    fetch(left);
+    for (int64_t t0 = first; left > 0; t0 += TILE, left -= TILE) {
+        Act ku, kz;
+#pragma unroll
+        for (int k = 0; k < Act::PER; ++k) {
+            ku.v[k] = u.v[k];
+            kz.v[k] = z.v[k];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {      // nodes past the end get dt = 0: the state stays
+                const float dt = r0 + k * RP < left && column ? step_of(to_f32<T>(dl.v[k].v[i]) + bias[i], s.softplus) : 0.f;
+                const float du = r0 + k * RP < left ? dt * to_f32<T>(u.v[k].v[i]) : 0.f;
+                sd[r0 + k * RP][col + i] = make_float4(dt, dt, du, du);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < Bc::PER; ++k) {
+            sb[rn + k * RN][n] = to_f32<T>(bt.v[k].v[0]);
+            if (!ENDS) sc[rn + k * RN][n] = to_f32<T>(ct.v[k].v[0]);
+        }
         __syncthreads();
-        for (int e = tid; e < TILE * CT; e += THREADS) {
-            const int r = e / CT, lc = e % CT, ch = c0 + lc;
-            float2 v = make_float2(0.f, 0.f);
-            if (r < here && ch < s.channels) {
-                const int64_t t = t0 + r;
-                const float raw = to_f32<T>(in.delta[w.b * s.delta_batch + t * s.delta_node + ch]) + (in.bias ? in.bias[ch] : 0.f);
-                v.x = step_of(raw, s.softplus);
-                if (BACK) {
-                    float g = to_f32<T>(in.gout[w.b * s.g_batch + t * s.g_node + ch]);
-                    if (in.z) {
-                        const float z = to_f32<T>(in.z[w.b * s.z_batch + t * s.z_node + ch]);
-                        g *= z * sigmoid_f32(z);
-                    }
-                    v.y = g;
+        if (left > TILE) fetch(left - TILE);
+        const int here = left < TILE ? left : TILE;
+        for (int k0 = 0; k0 < TILE; k0 += 4) {
+            if (k0 >= here) break;
+            if (!ENDS && kept != nullptr && k0 % KEEP == 0 && mine)
+                store_states(kept + ((w.b * s.kept_nodes + (t0 + k0) / KEEP) * s.channels + c) * s.states, q * NS, s.states, h);
+            float y[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const Quad d = quad_at(&sd[k0 + k][cl].x);
+                const Quad b4 = quad_at(&sb[k0 + k][q * NS]);
+                h.lo = fma2(exp2_pair(mul2(d.lo, a2.lo)), h.lo, mul2(d.hi, b4.lo));
+                h.hi = fma2(exp2_pair(mul2(d.lo, a2.hi)), h.hi, mul2(d.hi, b4.hi));
+                if (ENDS) {
+                    float dt, same;
+                    unpair(d.lo, dt, same);
+                    total += dt;
                 } else {
-                    v.y = v.x * to_f32<T>(in.u[w.b * s.u_batch + t * s.u_node + ch]);
+                    const Quad c4 = quad_at(&sc[k0 + k][q * NS]);
+                    y[k] = sum2(fma2(c4.lo, h.lo, mul2(c4.hi, h.hi)));
                 }
             }
-            sd[r][lc] = v;
-        }
-        for (int e = tid; e < TILE * NP; e += THREADS) {
-            const int r = e / NP, n = e % NP;
-            const bool there = r < here && n < s.states;
-            sb[r][n] = !there ? 0.f
-                     : BACK   ? to_f32<T>(in.C[w.b * s.C_batch + (t0 + r) * s.C_node + n])
-                              : to_f32<T>(in.B[w.b * s.B_batch + (t0 + r) * s.B_node + n]);
-        }
-        __syncthreads();
-#pragma unroll 4
-        for (int k2 = 0; k2 < TILE; ++k2) {
-            const int r = BACK ? TILE - 1 - k2 : k2;     // nodes past the end have dt = 0 and add nothing
-            const float2 d = sd[r][cl];
-            const float4 b4 = *reinterpret_cast<const float4*>(&sb[r][q * NS]);
-            const float bb[NS] = {b4.x, b4.y, b4.z, b4.w};
-            total += d.x;
-#pragma unroll
-            for (int i = 0; i < NS; ++i) {
-                const float a = exp2_f32(d.x * a2[i]);
-                h[i] = BACK ? a * fmaf(d.y, bb[i], h[i]) : fmaf(a, h[i], d.y * bb[i]);
+            if (!ENDS) {
+                sum_lanes<S>(y, q);
+                put_sums<S, CT>(sy, y, k0, cl, q);
             }
         }
+        __syncthreads();
+        if (!ENDS) {
+#pragma unroll
+            for (int k = 0; k < Act::PER; ++k) {
+                const int r = r0 + k * RP;
+                if (r >= here || !column) continue;
+                float y[VEC];
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    y[i] = sy[r][col + i];
+                    if (in.D) y[i] = fmaf(dd[i], to_f32<T>(ku.v[k].v[i]), y[i]);
+                    if (in.z) {
+                        const float g = to_f32<T>(kz.v[k].v[i]);
+                        y[i] *= g * sigmoid_f32(g);
+                    }
+                }
+                store_pack<T, VEC>(op + (int64_t)(k * RP) * s.channels, y);
+            }
+            op += (int64_t)TILE * s.channels;
+        }
+        // no barrier: the next tile writes sy only after its own first barrier, and sd, sb, sc were
+        // last read before the barrier above
     }
-    if (c < s.channels) {
-        const int64_t at = (w.b * s.chunks + w.chunk) * s.channels + c;
+    if (!mine) return;
+    if (ENDS) {
+        store_states(local + (at * s.channels + c) * s.states, q * NS, s.states, h);
+        if (q == 0) sums[at * s.channels + c] = total;
+    } else if (state_out != nullptr && w.chunk == s.chunks - 1) {
+        float v[NS];
+        quad_to(v, h);
 #pragma unroll
         for (int i = 0; i < NS; ++i)
-            if (q * NS + i < s.states) local[at * s.states + q * NS + i] = h[i];
-        if (q == 0) sums[at] = total;
+            if (q * NS + i < s.states) state_out[w.b * per + (int64_t)c * s.states + q * NS + i] = v[i];
     }
 }
 
@@ -189,207 +301,167 @@ __global__ void __launch_bounds__(256) scan_join_kernel(float* __restrict__ loca
     const int64_t b = e / per, cn = e % per, c = cn / s.states;
     const float a2 = A[cn] * LOG2_E;
     float carry = start ? start[e] : 0.f;
-    for (int k = 0; k < s.chunks; ++k) {
-        const int64_t at = b * s.chunks + (BACK ? s.chunks - 1 - k : k);
-        const float own = local[at * per + cn];
-        const float keep = exp2_f32(a2 * sums[at * s.channels + c]);
-        local[at * per + cn] = carry;
-        carry = fmaf(keep, carry, own);
-    }
-}
-
-// ------------------------------------------------------------------------------------------ forward
-template <typename T, int S>
-__global__ void __launch_bounds__(THREADS) scan_fwd_kernel(ScanIn<T> in, const float* __restrict__ state, const float* __restrict__ enter,
-                                                           T* __restrict__ out, float* __restrict__ state_out, float* __restrict__ kept,
-                                                           ScanShape s) {
-    pdl_wait_then_trigger();
-    constexpr int CT = THREADS / S, NP = S * NS, PER = TILE * CT / THREADS;
-    __shared__ float2 sd[TILE][CT];
-    __shared__ float sb[TILE][NP], sc[TILE][NP];
-    __shared__ float sy[TILE][CT];
-    const Where w = where(s);
-    const int tid = threadIdx.x, q = tid % S, cl = tid / S;
-    const int c0 = w.tile * CT, c = c0 + cl;
-    const int64_t first = (int64_t)w.chunk * s.chunk;
-    const int64_t end = first + s.chunk < s.length ? first + s.chunk : s.length;
-    const int64_t per = (int64_t)s.channels * s.states;
-    float a2[NS], h[NS];
+    constexpr int AHEAD = 8;      // chunks whose values are loaded together: the chain itself is one fused add each
+    for (int k0 = 0; k0 < s.chunks; k0 += AHEAD) {
+        float own[AHEAD], keep[AHEAD];
 #pragma unroll
-    for (int i = 0; i < NS; ++i) {
-        const int n = q * NS + i;
-        const bool there = c < s.channels && n < s.states;
-        a2[i] = there ? in.A[(int64_t)c * s.states + n] * LOG2_E : 0.f;
-        h[i] = !there  ? 0.f
-               : enter ? enter[(w.b * s.chunks + w.chunk) * per + (int64_t)c * s.states + n]
-               : state ? state[w.b * per + (int64_t)c * s.states + n]
-                       : 0.f;
-    }
-    for (int64_t t0 = first; t0 < end; t0 += TILE) {
-        const int here = (int)(end - t0 < TILE ? end - t0 : TILE);
-        float u[PER], z[PER];
-#pragma unroll
-        for (int k = 0; k < PER; ++k) {
-            const int e = tid + k * THREADS, r = e / CT, lc = e % CT, ch = c0 + lc;
-            float2 v = make_float2(0.f, 0.f);
-            u[k] = z[k] = 0.f;
-            if (r < here && ch < s.channels) {
-                const int64_t t = t0 + r;
-                const float raw = to_f32<T>(in.delta[w.b * s.delta_batch + t * s.delta_node + ch]) + (in.bias ? in.bias[ch] : 0.f);
-                u[k] = to_f32<T>(in.u[w.b * s.u_batch + t * s.u_node + ch]);
-                if (in.z) z[k] = to_f32<T>(in.z[w.b * s.z_batch + t * s.z_node + ch]);
-                v.x = step_of(raw, s.softplus);
-                v.y = v.x * u[k];
-            }
-            sd[r][lc] = v;
+        for (int k = 0; k < AHEAD; ++k) {
+            const bool there = k0 + k < s.chunks;
+            const int64_t at = b * s.chunks + (BACK ? s.chunks - 1 - (k0 + k) : k0 + k);
+            own[k] = there ? local[at * per + cn] : 0.f;
+            keep[k] = there ? exp2_f32(a2 * sums[at * s.channels + c]) : 0.f;
         }
-        for (int e = tid; e < TILE * NP; e += THREADS) {
-            const int r = e / NP, n = e % NP;
-            const bool there = r < here && n < s.states;
-            sb[r][n] = there ? to_f32<T>(in.B[w.b * s.B_batch + (t0 + r) * s.B_node + n]) : 0.f;
-            sc[r][n] = there ? to_f32<T>(in.C[w.b * s.C_batch + (t0 + r) * s.C_node + n]) : 0.f;
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            if (k0 + k >= s.chunks) break;
+            const int64_t at = b * s.chunks + (BACK ? s.chunks - 1 - (k0 + k) : k0 + k);
+            local[at * per + cn] = carry;
+            carry = fmaf(keep[k], carry, own[k]);
         }
-        __syncthreads();
-        for (int k0 = 0; k0 < TILE; k0 += 4) {       // nodes past the end have dt = 0: the state stays
-            if (kept != nullptr && k0 % KEEP == 0 && k0 < here && c < s.channels) {
-                float* dst = kept + ((w.b * s.kept_nodes + (t0 + k0) / KEEP) * s.channels + c) * s.states + q * NS;
-#pragma unroll
-                for (int i = 0; i < NS; ++i)
-                    if (q * NS + i < s.states) dst[i] = h[i];
-            }
-            float y[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float2 d = sd[k0 + k][cl];
-                const float4 b4 = *reinterpret_cast<const float4*>(&sb[k0 + k][q * NS]);
-                const float4 c4 = *reinterpret_cast<const float4*>(&sc[k0 + k][q * NS]);
-                const float bb[NS] = {b4.x, b4.y, b4.z, b4.w}, cc[NS] = {c4.x, c4.y, c4.z, c4.w};
-                y[k] = 0.f;
-#pragma unroll
-                for (int i = 0; i < NS; ++i) {
-                    h[i] = fmaf(exp2_f32(d.x * a2[i]), h[i], d.y * bb[i]);
-                    y[k] = fmaf(cc[i], h[i], y[k]);
-                }
-            }
-            sum_lanes<S>(y, q);
-            put_sums<S, CT>(sy, y, k0, cl, q);
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < PER; ++k) {
-            const int e = tid + k * THREADS, r = e / CT, lc = e % CT, ch = c0 + lc;
-            if (r < here && ch < s.channels) {
-                float y = sy[r][lc];
-                if (in.D) y = fmaf(in.D[ch], u[k], y);
-                if (in.z) y *= z[k] * sigmoid_f32(z[k]);
-                out[(w.b * s.length + t0 + r) * s.channels + ch] = from_f32<T>(y);
-            }
-        }
-        // no barrier: the next tile writes sy only after its own first barrier, and sd, sb, sc were
-        // last read before the barrier above
-    }
-    if (state_out != nullptr && w.chunk == s.chunks - 1 && c < s.channels) {
-#pragma unroll
-        for (int i = 0; i < NS; ++i)
-            if (q * NS + i < s.states) state_out[w.b * per + (int64_t)c * s.states + q * NS + i] = h[i];
     }
 }
 
 // ----------------------------------------------------------------------------------------- backward
+// What one block keeps in shared memory.
+template <int S>
+struct BackSpace {
+    static constexpr int CT = BACK_THREADS / S, NP = S * NS, WARPS = BACK_THREADS / 32;
+    float4 sd[KEEP][CT];                                    // dt, dt, dt u, dt u
+    float2 sg[KEEP][CT];                                    // gy, gy
+    __align__(16) float sb[KEEP][NP], sc[KEEP][NP];
+    float sy[KEEP][CT], st[KEEP][CT], sq[KEEP][CT];         // C.h, p.B, sum p a h A
+    float red[WARPS][KEEP][2 * NP];                         // the warps' sums over channels: gB, gC
+};
+
 // part_bc[tile][b][t][2 NP]: this block's share of gB and gC; part_a[b][chunk][channel][states + 2]:
 // this chunk's share of gA, gD and gdelta_bias.
-template <typename T, int S>
-__global__ void __launch_bounds__(THREADS) scan_bwd_kernel(ScanIn<T> in, const float* __restrict__ kept, const float* __restrict__ enter,
-                                                           const float* __restrict__ gstate_out, T* __restrict__ gu, T* __restrict__ gdelta,
-                                                           T* __restrict__ gz, float* __restrict__ gstate, float* __restrict__ part_bc,
-                                                           float* __restrict__ part_a, int64_t rows, ScanShape s) {
+// ENDS = true, for rows cut into chunks: only local = what the adjoint state hands to the node before the
+// chunk when nothing comes from behind it, and the sums of dt.
+template <typename T, int S, int VEC, bool ENDS>
+__global__ void __launch_bounds__(BACK_THREADS, BACK_BLOCKS) scan_bwd_kernel(ScanIn<T> in, const float* __restrict__ kept, const float* __restrict__ enter,
+                                                                const float* __restrict__ gstate_out, T* __restrict__ gu,
+                                                                T* __restrict__ gdelta, T* __restrict__ gz, float* __restrict__ gstate,
+                                                                float* __restrict__ part_bc, float* __restrict__ part_a,
+                                                                float* __restrict__ local, float* __restrict__ sums, int64_t rows, ScanShape s) {
     pdl_wait_then_trigger();
-    constexpr int CT = THREADS / S, NP = S * NS, PER = KEEP * CT / THREADS;
-    constexpr int CW = 32 / S;                     // channels of a warp
-    __shared__ float2 sd[KEEP][CT];                // dt, dt u
-    __shared__ float sg[KEEP][CT];                 // gy
-    __shared__ float sb[KEEP][NP], sc[KEEP][NP];
-    __shared__ float sy[KEEP][CT], st[KEEP][CT], sq[KEEP][CT];   // C.h, p.B, sum p a h A
-    __shared__ float red[WARPS][KEEP][2 * NP];
+    using Space = BackSpace<S>;
+    constexpr int CT = Space::CT, NP = Space::NP;
+    constexpr int CP = CT / VEC, RP = BACK_THREADS / CP, RN = BACK_THREADS / NP;
+    using Act = Rows<T, VEC, KEEP, RP>;
+    using Bc = Rows<T, 1, KEEP, RN>;
+    extern __shared__ __align__(16) uint8_t raw_space[];
+    Space& m = *reinterpret_cast<Space*>(raw_space);
     const Where w = where(s);
     const int tid = threadIdx.x, q = tid % S, cl = tid / S, warp = tid / 32, lane = tid % 32;
     const int c0 = w.tile * CT, c = c0 + cl;
     const int64_t first = (int64_t)w.chunk * s.chunk;
     const int64_t end = first + s.chunk < s.length ? first + s.chunk : s.length;
     const int64_t per = (int64_t)s.channels * s.states;
-    float a2[NS], p[NS], ga[NS];                   // p: what the adjoint state brings from behind
+    const int64_t at = w.b * s.chunks + w.chunk;
+    const bool mine = c < s.channels;
+    const Quad a2 = load_states(mine ? in.A + (int64_t)c * s.states : nullptr, q * NS, s.states, LOG2_E);
+    Quad p = load_states(ENDS || !mine ? nullptr                                     // the adjoint state, from behind
+                         : enter       ? enter + at * per + (int64_t)c * s.states
+                         : gstate_out  ? gstate_out + w.b * per + (int64_t)c * s.states
+                                       : nullptr,
+                         q * NS, s.states, 1.f);
+    Quad ga = {0, 0};
+    const int col = tid % CP * VEC, r0 = tid / CP, n = tid % NP, rn = tid / NP;
+    const bool column = c0 + col < s.channels, row_n = n < s.states;
+    float bias[VEC], dd[VEC], gd[VEC] = {}, gbias[VEC] = {};
 #pragma unroll
-    for (int i = 0; i < NS; ++i) {
-        const int n = q * NS + i;
-        const bool there = c < s.channels && n < s.states;
-        a2[i] = there ? in.A[(int64_t)c * s.states + n] * LOG2_E : 0.f;
-        ga[i] = 0.f;
-        p[i] = !there       ? 0.f
-               : enter      ? enter[(w.b * s.chunks + w.chunk) * per + (int64_t)c * s.states + n]
-               : gstate_out ? gstate_out[w.b * per + (int64_t)c * s.states + n]
-                            : 0.f;
+    for (int i = 0; i < VEC; ++i) {
+        bias[i] = in.bias && column ? in.bias[c0 + col + i] : 0.f;
+        dd[i] = in.D && column ? in.D[c0 + col + i] : 0.f;
     }
-    float gd = 0.f, gbias = 0.f;                   // of channel c0 + tid % CT
     const int ntiles = (int)((end - first + KEEP - 1) / KEEP);
-    for (int k = ntiles - 1; k >= 0; --k) {
-        const int64_t t0 = first + (int64_t)k * KEEP;
+    const int64_t last = first + (int64_t)(ntiles - 1) * KEEP;
+    Act u, dl, z, go;
+    Bc bt, ct;
+    u.start(in.u + w.b * s.u_batch + c0 + col, s.u_node, last + r0);
+    dl.start(in.delta + w.b * s.delta_batch + c0 + col, s.delta_node, last + r0);
+    z.start(in.z + w.b * s.z_batch + c0 + col, s.z_node, last + r0);
+    go.start(in.gout + w.b * s.g_batch + c0 + col, s.g_node, last + r0);
+    bt.start(in.B + w.b * s.B_batch + n, s.B_node, last + rn);
+    ct.start(in.C + w.b * s.C_batch + n, s.C_node, last + rn);
+    Quad h0 = {0, 0};
+    const float* hp = mine && !ENDS ? kept + ((w.b * s.kept_nodes + last / KEEP) * s.channels + c) * s.states : nullptr;
+    auto fetch = [&](int here) {
+        if (!ENDS) u.load(r0, here, column, -KEEP);
+        dl.load(r0, here, column, -KEEP);
+        if (in.z) z.load(r0, here, column, -KEEP);
+        go.load(r0, here, column, -KEEP);
+        if (!ENDS) bt.load(rn, here, row_n, -KEEP);
+        ct.load(rn, here, row_n, -KEEP);
+        if (!ENDS) {
+            if (states_packed(s.states)) { if (mine && q * NS < s.states) h0 = quad_at(hp + q * NS); }
+            else if (mine) h0 = load_states(hp, q * NS, s.states, 1.f);
+            hp -= mine ? per : 0;
+        }
+    };
+    float total = 0.f;
+    if (ntiles > 0) fetch((int)(end - last));
+    for (int64_t t0 = last; t0 >= first && ntiles > 0; t0 -= KEEP) {
         const int here = (int)(end - t0 < KEEP ? end - t0 : KEEP);
-        float u[PER], z[PER], go[PER], raw[PER];
+        Act ku, kz, kg, kd;
 #pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            const int e = tid + j * THREADS, r = e / CT, lc = e % CT, ch = c0 + lc;
-            float2 v = make_float2(0.f, 0.f);
-            float g = 0.f;
-            u[j] = z[j] = go[j] = raw[j] = 0.f;
-            if (r < here && ch < s.channels) {
-                const int64_t t = t0 + r;
-                raw[j] = to_f32<T>(in.delta[w.b * s.delta_batch + t * s.delta_node + ch]) + (in.bias ? in.bias[ch] : 0.f);
-                u[j] = to_f32<T>(in.u[w.b * s.u_batch + t * s.u_node + ch]);
-                go[j] = to_f32<T>(in.gout[w.b * s.g_batch + t * s.g_node + ch]);
-                g = go[j];
+        for (int k = 0; k < Act::PER; ++k) {
+            const int r = r0 + k * RP;
+            if (KEEP % RP != 0 && r >= KEEP) break;
+            ku.v[k] = u.v[k]; kz.v[k] = z.v[k]; kg.v[k] = go.v[k]; kd.v[k] = dl.v[k];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const bool there = r < here && column;
+                const float dt = there ? step_of(to_f32<T>(dl.v[k].v[i]) + bias[i], s.softplus) : 0.f;
+                const float du = ENDS || !there ? 0.f : dt * to_f32<T>(u.v[k].v[i]);
+                float g = to_f32<T>(go.v[k].v[i]);
                 if (in.z) {
-                    z[j] = to_f32<T>(in.z[w.b * s.z_batch + t * s.z_node + ch]);
-                    g *= z[j] * sigmoid_f32(z[j]);
+                    const float zv = to_f32<T>(z.v[k].v[i]);
+                    g *= zv * sigmoid_f32(zv);
                 }
-                v.x = step_of(raw[j], s.softplus);
-                v.y = v.x * u[j];
+                if (!there) g = 0.f;
+                m.sd[r][col + i] = make_float4(dt, dt, du, du);
+                m.sg[r][col + i] = make_float2(g, g);
             }
-            sd[r][lc] = v;
-            sg[r][lc] = g;
         }
-        for (int e = tid; e < KEEP * NP; e += THREADS) {
-            const int r = e / NP, n = e % NP;
-            const bool there = r < here && n < s.states;
-            sb[r][n] = there ? to_f32<T>(in.B[w.b * s.B_batch + (t0 + r) * s.B_node + n]) : 0.f;
-            sc[r][n] = there ? to_f32<T>(in.C[w.b * s.C_batch + (t0 + r) * s.C_node + n]) : 0.f;
-        }
-        __syncthreads();
-        // forward through the tile: hs[r] is the state BEFORE node r
-        float hs[KEEP + 1][NS];
 #pragma unroll
-        for (int i = 0; i < NS; ++i)
-            hs[0][i] = c < s.channels && q * NS + i < s.states
-                           ? kept[((w.b * s.kept_nodes + t0 / KEEP) * s.channels + c) * s.states + q * NS + i]
-                           : 0.f;
+        for (int k = 0; k < Bc::PER; ++k) {
+            if (KEEP % RN != 0 && rn + k * RN >= KEEP) break;
+            if (!ENDS) m.sb[rn + k * RN][n] = to_f32<T>(bt.v[k].v[0]);
+            m.sc[rn + k * RN][n] = to_f32<T>(ct.v[k].v[0]);
+        }
+        Quad hs[KEEP + 1];                         // hs[r]: the state BEFORE node r
+        hs[0] = h0;
+        __syncthreads();
+        if (t0 > first) fetch(KEEP);
+        if constexpr (ENDS) {
+#pragma unroll
+            for (int r = KEEP - 1; r >= 0; --r) {
+                const Quad d = quad_at(&m.sd[r][cl].x), c4 = quad_at(&m.sc[r][q * NS]);
+                const uint64_t g = *reinterpret_cast<const uint64_t*>(&m.sg[r][cl]);
+                float dt, same;
+                unpair(d.lo, dt, same);
+                total += dt;
+                p.lo = mul2(fma2(c4.lo, g, p.lo), exp2_pair(mul2(d.lo, a2.lo)));
+                p.hi = mul2(fma2(c4.hi, g, p.hi), exp2_pair(mul2(d.lo, a2.hi)));
+            }
+            __syncthreads();
+        } else {
+        // forward through the tile
 #pragma unroll
         for (int k0 = 0; k0 < KEEP; k0 += 4) {
+            asm volatile("" ::: "memory");
             float y[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int r = k0 + j;
-                const float2 d = sd[r][cl];
-                const float4 b4 = *reinterpret_cast<const float4*>(&sb[r][q * NS]);
-                const float4 c4 = *reinterpret_cast<const float4*>(&sc[r][q * NS]);
-                const float bb[NS] = {b4.x, b4.y, b4.z, b4.w}, cc[NS] = {c4.x, c4.y, c4.z, c4.w};
-                y[j] = 0.f;
-#pragma unroll
-                for (int i = 0; i < NS; ++i) {
-                    hs[r + 1][i] = fmaf(exp2_f32(d.x * a2[i]), hs[r][i], d.y * bb[i]);
-                    y[j] = fmaf(cc[i], hs[r + 1][i], y[j]);
-                }
+                const Quad d = quad_at(&m.sd[r][cl].x), b4 = quad_at(&m.sb[r][q * NS]), c4 = quad_at(&m.sc[r][q * NS]);
+                hs[r + 1].lo = fma2(exp2_pair(mul2(d.lo, a2.lo)), hs[r].lo, mul2(d.hi, b4.lo));
+                hs[r + 1].hi = fma2(exp2_pair(mul2(d.lo, a2.hi)), hs[r].hi, mul2(d.hi, b4.hi));
+                y[j] = sum2(fma2(c4.lo, hs[r + 1].lo, mul2(c4.hi, hs[r + 1].hi)));
             }
             sum_lanes<S>(y, q);
-            put_sums<S, CT>(sy, y, k0, cl, q);
+            put_sums<S, CT>(m.sy, y, k0, cl, q);
         }
         // and backwards
 #pragma unroll
@@ -398,104 +470,123 @@ __global__ void __launch_bounds__(THREADS) scan_bwd_kernel(ScanIn<T> in, const f
 #pragma unroll
             for (int j = 3; j >= 0; --j) {
                 const int r = k0 + j;
-                const float2 d = sd[r][cl];
-                const float g = sg[r][cl];
-                const float4 b4 = *reinterpret_cast<const float4*>(&sb[r][q * NS]);
-                const float4 c4 = *reinterpret_cast<const float4*>(&sc[r][q * NS]);
-                const float bb[NS] = {b4.x, b4.y, b4.z, b4.w}, cc[NS] = {c4.x, c4.y, c4.z, c4.w};
+                asm volatile("" ::: "memory");     // the loads of a node stay with it: hoisted ones would spill the states
+                const Quad d = quad_at(&m.sd[r][cl].x), b4 = quad_at(&m.sb[r][q * NS]), c4 = quad_at(&m.sc[r][q * NS]);
+                const uint64_t g = *reinterpret_cast<const uint64_t*>(&m.sg[r][cl]);
                 float v[2 * NS];                   // shares of gB and gC of this node
-                tb[j] = ta[j] = 0.f;
-#pragma unroll
-                for (int i = 0; i < NS; ++i) {
-                    p[i] = fmaf(cc[i], g, p[i]);
-                    v[i] = p[i] * d.y;
-                    v[NS + i] = hs[r + 1][i] * g;
-                    tb[j] = fmaf(p[i], bb[i], tb[j]);
-                    p[i] *= exp2_f32(d.x * a2[i]);
-                    const float ph = p[i] * hs[r][i];
-                    ta[j] = fmaf(ph, a2[i], ta[j]);
-                    ga[i] = fmaf(ph, d.x, ga[i]);
-                }
+                p.lo = fma2(c4.lo, g, p.lo);
+                p.hi = fma2(c4.hi, g, p.hi);
+                unpair(mul2(p.lo, d.hi), v[0], v[1]);
+                unpair(mul2(p.hi, d.hi), v[2], v[3]);
+                unpair(mul2(hs[r + 1].lo, g), v[4], v[5]);
+                unpair(mul2(hs[r + 1].hi, g), v[6], v[7]);
+                tb[j] = sum2(fma2(p.lo, b4.lo, mul2(p.hi, b4.hi)));
+                p.lo = mul2(p.lo, exp2_pair(mul2(d.lo, a2.lo)));
+                p.hi = mul2(p.hi, exp2_pair(mul2(d.lo, a2.hi)));
+                const uint64_t ph_lo = mul2(p.lo, hs[r].lo), ph_hi = mul2(p.hi, hs[r].hi);
+                ta[j] = sum2(fma2(ph_lo, a2.lo, mul2(ph_hi, a2.hi)));
+                ga.lo = fma2(ph_lo, d.lo, ga.lo);
+                ga.hi = fma2(ph_hi, d.lo, ga.hi);
                 // sum over the warp's channels: halve the values while halving the lanes, then add
-                constexpr int TOP = 16;
-                int at = 0;                        // first value this lane still holds
+                int from = 0;                      // first value this lane still holds
 #pragma unroll
-                for (int m = TOP, n = 2 * NS; m >= S; m /= 2) {
-                    if (n > 1) {
-                        n /= 2;
-                        const bool up = lane & m;
+                for (int k = 16, left = 2 * NS; k >= S; k /= 2) {
+                    if (left > 1) {
+                        left /= 2;
+                        const bool up = lane & k;
 #pragma unroll
-                        for (int i = 0; i < n; ++i) {
-                            const float send = up ? v[i] : v[n + i];
-                            v[i] = (up ? v[n + i] : v[i]) + __shfl_xor_sync(~0u, send, m);
+                        for (int i = 0; i < left; ++i) {
+                            const float send = up ? v[i] : v[left + i];
+                            v[i] = (up ? v[left + i] : v[i]) + __shfl_xor_sync(~0u, send, k);
                         }
-                        at += up ? n : 0;
+                        from += up ? left : 0;
                     } else {
-                        v[0] += __shfl_xor_sync(~0u, v[0], m);
+                        v[0] += __shfl_xor_sync(~0u, v[0], k);
                     }
                 }
-                constexpr int LEFT = CW >= 2 * NS ? 1 : 2 * NS / CW;   // values left in a lane
+                constexpr int CW = 32 / S, LEFT = CW >= 2 * NS ? 1 : 2 * NS / CW;   // values left in a lane
 #pragma unroll
                 for (int i = 0; i < LEFT; ++i) {
-                    const int n = at + i;
-                    red[warp][r][(n / NS) * NP + q * NS + n % NS] = v[i];
+                    const int k = from + i;
+                    m.red[warp][r][(k / NS) * NP + q * NS + k % NS] = v[i];
                 }
             }
             sum_lanes<S>(tb, q);
-            put_sums<S, CT>(st, tb, k0, cl, q);
+            put_sums<S, CT>(m.st, tb, k0, cl, q);
             sum_lanes<S>(ta, q);
-            put_sums<S, CT>(sq, ta, k0, cl, q);
+            put_sums<S, CT>(m.sq, ta, k0, cl, q);
         }
         __syncthreads();
 #pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            const int e = tid + j * THREADS, r = e / CT, lc = e % CT, ch = c0 + lc;
-            if (r < here && ch < s.channels) {
-                const float dt = sd[r][lc].x, gy = sg[r][lc], through = st[r][lc];
-                const float dd = in.D ? in.D[ch] : 0.f;
-                const int64_t at = (w.b * s.length + t0 + r) * s.channels + ch;
-                gu[at] = from_f32<T>(fmaf(dt, through, dd * gy));
-                float gr = fmaf(u[j], through, sq[r][lc] * (1.f / LOG2_E));
-                if (s.softplus) gr *= sigmoid_f32(raw[j]);
-                gdelta[at] = from_f32<T>(gr);
+        for (int k = 0; k < Act::PER; ++k) {
+            const int r = r0 + k * RP;
+            if (r >= here || !column) continue;
+            float ou[VEC], od[VEC], oz[VEC];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float dt = m.sd[r][col + i].x, gy = m.sg[r][col + i].x, through = m.st[r][col + i];
+                const float uv = to_f32<T>(ku.v[k].v[i]);
+                ou[i] = fmaf(dt, through, dd[i] * gy);
+                float gr = fmaf(uv, through, m.sq[r][col + i] * (1.f / LOG2_E));
+                if (s.softplus) gr *= sigmoid_f32(to_f32<T>(kd.v[k].v[i]) + bias[i]);
+                od[i] = gr;
                 if (in.z) {
-                    const float y = fmaf(dd, u[j], sy[r][lc]), sig = sigmoid_f32(z[j]);
-                    gz[at] = from_f32<T>(go[j] * y * sig * fmaf(z[j], 1.f - sig, 1.f));
+                    const float zv = to_f32<T>(kz.v[k].v[i]), sig = sigmoid_f32(zv);
+                    oz[i] = to_f32<T>(kg.v[k].v[i]) * fmaf(dd[i], uv, m.sy[r][col + i]) * sig * fmaf(zv, 1.f - sig, 1.f);
                 }
-                gd = fmaf(gy, u[j], gd);
-                gbias += gr;
+                gd[i] = fmaf(gy, uv, gd[i]);
+                gbias[i] += gr;
             }
+            const int64_t o = (w.b * s.length + t0 + r) * s.channels + c0 + col;
+            store_pack<T, VEC>(gu + o, ou);
+            store_pack<T, VEC>(gdelta + o, od);
+            if (in.z) store_pack<T, VEC>(gz + o, oz);
         }
-        for (int e = tid; e < here * 2 * NP; e += THREADS) {
-            const int r = e / (2 * NP), n = e % (2 * NP);
+        for (int e = tid; e < here * 2 * NP; e += BACK_THREADS) {
+            const int r = e / (2 * NP), k = e % (2 * NP);
             float v = 0.f;
 #pragma unroll
-            for (int k2 = 0; k2 < WARPS; ++k2) v += red[k2][r][n];
-            part_bc[(((int64_t)w.tile * rows + w.b) * s.length + t0 + r) * (2 * NP) + n] = v;
+            for (int i = 0; i < Space::WARPS; ++i) v += m.red[i][r][k];
+            part_bc[(((int64_t)w.tile * rows + w.b) * s.length + t0 + r) * (2 * NP) + k] = v;
         }
         __syncthreads();
+        }
     }
+    if constexpr (ENDS) {
+        if (mine) {
+            store_states(local + (at * s.channels + c) * s.states, q * NS, s.states, p);
+            if (q == 0) sums[at * s.channels + c] = total;
+        }
+    } else {
     // this chunk's share of the parameters' gradients
-    float* pa = part_a + ((w.b * s.chunks + w.chunk) * s.channels) * (int64_t)(s.states + 2);
-    if (c < s.channels) {
+    float* pa = part_a + (at * s.channels) * (int64_t)(s.states + 2);
+    if (mine) {
+        float v[NS], e[NS];
+        quad_to(v, ga);
+        quad_to(e, p);
 #pragma unroll
         for (int i = 0; i < NS; ++i)
             if (q * NS + i < s.states) {
-                pa[(int64_t)c * (s.states + 2) + q * NS + i] = ga[i];
-                if (gstate != nullptr && w.chunk == 0) gstate[w.b * per + (int64_t)c * s.states + q * NS + i] = p[i];
+                pa[(int64_t)c * (s.states + 2) + q * NS + i] = v[i];
+                if (gstate != nullptr && w.chunk == 0) gstate[w.b * per + (int64_t)c * s.states + q * NS + i] = e[i];
             }
     }
-    // threads tid, tid + CT, ... hold the same channel's sums
-    static_assert(KEEP * CT >= THREADS, "room for two sums of every thread");
-    float* fin = &sd[0][0].x;
-    fin[tid] = gd;
-    fin[THREADS + tid] = gbias;
+    // threads tid, tid + CP, ... hold sums of the same channels
+    float(*fin)[BACK_THREADS] = reinterpret_cast<float(*)[BACK_THREADS]>(raw_space);     // 2 VEC rows
+    static_assert(sizeof(m.sd) >= 2 * VEC * BACK_THREADS * sizeof(float), "room for the sums of every thread");
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        fin[i][tid] = gd[i];
+        fin[VEC + i][tid] = gbias[i];
+    }
     __syncthreads();
     if (tid < CT && c0 + tid < s.channels) {
         float v0 = 0.f, v1 = 0.f;
-        for (int e = tid; e < THREADS; e += CT) { v0 += fin[e]; v1 += fin[THREADS + e]; }
+        for (int e = tid / VEC; e < BACK_THREADS; e += CP) { v0 += fin[tid % VEC][e]; v1 += fin[VEC + tid % VEC][e]; }
         pa[(int64_t)(c0 + tid) * (s.states + 2) + s.states] = v0;
         pa[(int64_t)(c0 + tid) * (s.states + 2) + s.states + 1] = v1;
+    }
     }
 }
 
@@ -588,6 +679,7 @@ int lanes_of(int states) {
 
 // The plan depends on sizes only, so that the forward and the backward call agree on it.
 ScanShape plan(const fpde_scan_args* a, bool backward) {
+    const int threads = backward ? BACK_THREADS : THREADS;
     ScanShape s = {};
     s.length = a->length;
     s.u_batch = a->u_batch; s.u_node = a->u_node;
@@ -599,7 +691,7 @@ ScanShape plan(const fpde_scan_args* a, bool backward) {
     s.channels = (int)a->channels;
     s.states = a->states;
     s.softplus = a->softplus;
-    s.tiles = (int)ceil_div(a->channels, THREADS / lanes_of(a->states));
+    s.tiles = (int)ceil_div(a->channels, threads / lanes_of(a->states));
     s.kept_nodes = ceil_div(a->length, KEEP);
     // Splitting a row costs a second pass over its exponentials: done while it still fills idle SMs.
     const int64_t blocks = a->batch * s.tiles;
@@ -667,43 +759,62 @@ ScanIn<T> inputs(const fpde_scan_args* a) {
         if (e_ != cudaSuccess) return e_;     \
     } while (0)
 
-template <typename T, int S>
+// Two channels per load where every row of every activation starts on two elements.
+template <typename T>
+bool scan_pairs(const fpde_scan_args* a, bool backward) {
+    const size_t e = sizeof(T);
+    bool ok = a->channels % 2 == 0 && packs(a->u, a->u_batch, a->u_node, e, 2) && packs(a->delta, a->delta_batch, a->delta_node, e, 2) &&
+              (a->z == nullptr || packs(a->z, a->z_batch, a->z_node, e, 2));
+    if (!backward) return ok && aligned(a->out, 2 * e);
+    return ok && packs(a->gout, a->gout_batch, a->gout_node, e, 2) && aligned(a->gu, 2 * e) && aligned(a->gdelta, 2 * e) && aligned(a->gz, 2 * e);
+}
+
+template <typename T, int S, int VEC>
 cudaError_t run_fwd(const fpde_scan_args* a, cudaStream_t st) {
     const ScanShape s = plan(a, false);
     const ScanSpace w = space(a, s, false);
     const ScanIn<T> in = inputs<T>(a);
     const int64_t blocks = a->batch * s.tiles * s.chunks;
     if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    const dim3 grid((unsigned)blocks);
     float* local = nullptr;
     if (s.chunks > 1) {
         local = (float*)((char*)a->workspace + w.local);
         float* sums = (float*)((char*)a->workspace + w.sums);
-        FPDE_TRY(launch_kernel(scan_local_kernel<T, S, false>, dim3((unsigned)blocks), dim3(THREADS), st, in, local, sums, s));
+        FPDE_TRY(launch_kernel(scan_fwd_kernel<T, S, VEC, true>, grid, dim3(THREADS), st, in, (const float*)nullptr, (const float*)nullptr,
+                               (T*)nullptr, (float*)nullptr, (float*)nullptr, local, sums, s));
         FPDE_TRY(launch_kernel(scan_join_kernel<false>, dim3((unsigned)ceil_div(a->batch * s.channels * s.states, 256)), dim3(256), st,
                                local, (const float*)sums, a->A, a->state, a->batch, s));
     }
-    return launch_kernel(scan_fwd_kernel<T, S>, dim3((unsigned)blocks), dim3(THREADS), st, in, a->state, (const float*)local, (T*)a->out,
-                         a->state_out, (float*)a->kept, s);
+    return launch_kernel(scan_fwd_kernel<T, S, VEC, false>, grid, dim3(THREADS), st, in, a->state, (const float*)local, (T*)a->out,
+                         a->state_out, (float*)a->kept, (float*)nullptr, (float*)nullptr, s);
 }
 
-template <typename T, int S>
+template <typename T, int S, int VEC>
 cudaError_t run_bwd(const fpde_scan_args* a, cudaStream_t st) {
     const ScanShape s = plan(a, true);
     const ScanSpace w = space(a, s, true);
     const ScanIn<T> in = inputs<T>(a);
     const int64_t blocks = a->batch * s.tiles * s.chunks;
     if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    const dim3 grid((unsigned)blocks);
+    constexpr size_t bytes = sizeof(BackSpace<S>);
     char* ws = (char*)a->workspace;
     float *local = nullptr, *part_bc = (float*)(ws + w.part_bc), *part_a = (float*)(ws + w.part_a);
     if (s.chunks > 1) {
         local = (float*)(ws + w.local);
         float* sums = (float*)(ws + w.sums);
-        FPDE_TRY(launch_kernel(scan_local_kernel<T, S, true>, dim3((unsigned)blocks), dim3(THREADS), st, in, local, sums, s));
+        FPDE_TRY(cudaFuncSetAttribute(scan_bwd_kernel<T, S, VEC, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+        FPDE_TRY(launch_kernel_smem(scan_bwd_kernel<T, S, VEC, true>, grid, dim3(BACK_THREADS), bytes, st, in, (const float*)nullptr,
+                                    (const float*)nullptr, (const float*)nullptr, (T*)nullptr, (T*)nullptr, (T*)nullptr, (float*)nullptr,
+                                    (float*)nullptr, (float*)nullptr, local, sums, a->batch, s));
         FPDE_TRY(launch_kernel(scan_join_kernel<true>, dim3((unsigned)ceil_div(a->batch * s.channels * s.states, 256)), dim3(256), st,
                                local, (const float*)sums, a->A, a->gstate_out, a->batch, s));
     }
-    FPDE_TRY(launch_kernel(scan_bwd_kernel<T, S>, dim3((unsigned)blocks), dim3(THREADS), st, in, (const float*)a->kept, (const float*)local,
-                           a->gstate_out, (T*)a->gu, (T*)a->gdelta, (T*)a->gz, a->gstate, part_bc, part_a, a->batch, s));
+    FPDE_TRY(cudaFuncSetAttribute(scan_bwd_kernel<T, S, VEC, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    FPDE_TRY(launch_kernel_smem(scan_bwd_kernel<T, S, VEC, false>, grid, dim3(BACK_THREADS), bytes, st, in, (const float*)a->kept,
+                                (const float*)local, a->gstate_out, (T*)a->gu, (T*)a->gdelta, (T*)a->gz, a->gstate, part_bc, part_a,
+                                (float*)nullptr, (float*)nullptr, a->batch, s));
     if (a->batch * a->length > 0)
         FPDE_TRY(launch_kernel(scan_sum_bc_kernel<T>, dim3((unsigned)ceil_div(a->batch * a->length * 2 * S * NS, 256)), dim3(256), st,
                                (const float*)part_bc, s.tiles, a->batch * a->length, S * NS, s.states, (T*)a->gB, (T*)a->gC));
@@ -724,8 +835,8 @@ enum Call { CALL_FWD, CALL_BWD, CALL_STEP };
 
 template <typename T, int S>
 cudaError_t run(const fpde_scan_args* a, Call call, cudaStream_t st) {
-    if (call == CALL_FWD) return run_fwd<T, S>(a, st);
-    if (call == CALL_BWD) return run_bwd<T, S>(a, st);
+    if (call == CALL_FWD) return scan_pairs<T>(a, false) ? run_fwd<T, S, 2>(a, st) : run_fwd<T, S, 1>(a, st);
+    if (call == CALL_BWD) return scan_pairs<T>(a, true) ? run_bwd<T, S, 2>(a, st) : run_bwd<T, S, 1>(a, st);
     return run_step<T, S>(a, st);
 }
 
