@@ -29,9 +29,10 @@ namespace {
 
 constexpr int THREADS = 128;      // of the forward kernels
 constexpr int BACK_THREADS = 256; // of the backward kernel: halves the partial sums of gB and gC
-constexpr int FWD_BLOCKS = 4, BACK_BLOCKS = 1;     // resident blocks that the registers are budgeted for
-constexpr int TILE = 32;          // nodes of a forward tile
+constexpr int FWD_BLOCKS = 6, BACK_BLOCKS = 2;     // resident blocks that the registers are budgeted for
+constexpr int TILE = 16;          // nodes of a forward tile
 constexpr int KEEP = 16;          // nodes between stored states = nodes of a backward tile
+static_assert(TILE == KEEP, "the forward march stores the state before each of its tiles");
 constexpr int NS = 4;             // states of a thread
 
 struct ScanShape {
@@ -66,25 +67,64 @@ __device__ __forceinline__ Where where(const ScanShape& s) {
 
 __device__ __forceinline__ float step_of(float raw, int softplus) { return softplus ? softplus_f32(raw) : raw; }
 
-// One tile of an activation on its way: the thread's pack column and rows r0, r0 + RP, ...  The loads of a
-// tile are issued while the tile before it is computed.
-template <typename T, int VEC, int NODES, int RP>
-struct Rows {
-    static constexpr int PER = (NODES + RP - 1) / RP;
-    Pack<T, VEC> v[PER];
-    const T* p;                   // of row r0 of the tile to load next
-    int64_t node;
-    __device__ __forceinline__ void start(const T* base, int64_t node_stride, int64_t first) {
-        node = node_stride;
-        p = base + first * node_stride;
-    }
-    __device__ __forceinline__ void load(int r0, int here, bool column, int64_t advance) {   // then on by `advance` nodes
+// A thread's own share of the tiles of ARRAYS activations: pack column `col` of rows r0, r0 + RP, ...  The
+// next tile travels while this one is computed, by cp.async into shared memory that only this thread reads
+// (no registers held, no barrier); 2-byte packs, which cp.async does not have, wait in registers.
+template <typename T, int VEC, int NODES, int RP, int ARRAYS, int THREADS_>
+struct Feed {
+    static constexpr int PER = (NODES + RP - 1) / RP, BYTES = sizeof(T) * VEC;
+    static constexpr bool ASYNC = BYTES >= 4;
+    using P = Pack<T, VEC>;
+    struct Space { P v[ASYNC ? 2 : 1][ARRAYS][PER][THREADS_]; };
+    Space& space;
+    int now = 0;                                  // half that holds the current tile
+    P held[ASYNC ? 1 : ARRAYS][PER];
+    __device__ __forceinline__ Feed(Space& where_) : space(where_) {}
+
+    // row0: the array's first row of the tile (block-uniform); rows from `here` on read as zero
+    __device__ __forceinline__ void request(int array, const T* row0, int64_t node, int r0, int col, int here, bool column) {
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
-            v[k] = Pack<T, VEC>{};
-            if (column && r0 + k * RP < here) v[k] = load_pack<T, VEC>(p + (int64_t)(k * RP) * node);
+            const int r = r0 + k * RP;
+            const bool there = column && r < here;
+            const T* src = row0 + r * node + col;
+            if (ASYNC) {
+                P* dst = &space.v[now ^ 1][array][k][threadIdx.x];
+                if (there)
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(dst))), "l"(src),
+                                 "n"(BYTES < 4 ? 4 : BYTES) : "memory");
+                else *dst = P{};
+            } else {
+                held[array][k] = P{};
+                if (there) held[array][k] = load_pack<T, VEC>(src);
+            }
         }
-        p += advance * node;
+    }
+    __device__ __forceinline__ void arrive() {    // what was requested becomes the current tile
+        if (ASYNC) {
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            now ^= 1;
+        } else {
+#pragma unroll
+            for (int a = 0; a < ARRAYS; ++a)
+#pragma unroll
+                for (int k = 0; k < PER; ++k) space.v[0][a][k][threadIdx.x] = held[a][k];
+        }
+    }
+    __device__ __forceinline__ P get(int array, int k) const { return space.v[ASYNC ? now : 0][array][k][threadIdx.x]; }
+};
+
+// The same for B and C, one state each of rows rn, rn + RN, ...: few, kept in registers.
+template <typename T, int NODES, int RN>
+struct States {
+    static constexpr int PER = (NODES + RN - 1) / RN;
+    T v[PER];
+    __device__ __forceinline__ void load(const T* row0, int64_t node, int rn, int n, int here, bool there) {
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            v[k] = from_f32<T>(0.f);
+            if (there && rn + k * RN < here) v[k] = row0[(rn + k * RN) * node + n];
+        }
     }
 };
 
@@ -163,11 +203,13 @@ __global__ void __launch_bounds__(THREADS, FWD_BLOCKS) scan_fwd_kernel(ScanIn<T>
     pdl_wait_then_trigger();
     constexpr int CT = THREADS / S, NP = S * NS;
     constexpr int CP = CT / VEC, RP = THREADS / CP, RN = THREADS / NP;      // packs of a row; rows at a time
-    using Act = Rows<T, VEC, TILE, RP>;
-    using Bc = Rows<T, 1, TILE, RN>;
+    enum { U, DELTA, Z };
+    using Act = Feed<T, VEC, TILE, RP, ENDS ? 2 : 3, THREADS>;
+    using Bc = States<T, TILE, RN>;
+    __shared__ typename Act::Space room;
     __shared__ float4 sd[TILE][CT];              // dt, dt, dt u, dt u
-    __shared__ __align__(16) float sb[TILE][NP], sc[TILE][NP];
-    __shared__ float sy[TILE][CT];               // ENDS: not used
+    __shared__ __align__(16) float sb[TILE][NP], sc[ENDS ? 1 : TILE][NP];
+    __shared__ float sy[ENDS ? 1 : TILE][CT];
     const Where w = where(s);
     const int tid = threadIdx.x, q = tid % S, cl = tid / S;
     const int c0 = w.tile * CT, c = c0 + cl;
@@ -182,55 +224,48 @@ __global__ void __launch_bounds__(THREADS, FWD_BLOCKS) scan_fwd_kernel(ScanIn<T>
     // what this thread brings in: pack column `col` of rows r0, r0 + RP, ... and state n of rows rn, rn + RN, ...
     const int col = tid % CP * VEC, r0 = tid / CP, n = tid % NP, rn = tid / NP;
     const bool column = c0 + col < s.channels, row_n = n < s.states;
-    float bias[VEC], dd[VEC];
+    float bias[VEC];
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-        bias[i] = in.bias && column ? in.bias[c0 + col + i] : 0.f;
-        dd[i] = in.D && column ? in.D[c0 + col + i] : 0.f;
-    }
-    Act u, dl, z;
+    for (int i = 0; i < VEC; ++i) bias[i] = in.bias && column ? in.bias[c0 + col + i] : 0.f;
+    Act act(room);
     Bc bt, ct;
-    u.start(in.u + w.b * s.u_batch + c0 + col, s.u_node, first + r0);
-    dl.start(in.delta + w.b * s.delta_batch + c0 + col, s.delta_node, first + r0);
-    z.start(in.z + w.b * s.z_batch + c0 + col, s.z_node, first + r0);
-    bt.start(in.B + w.b * s.B_batch + n, s.B_node, first + rn);
-    ct.start(in.C + w.b * s.C_batch + n, s.C_node, first + rn);
-    auto fetch = [&](int here) {
-        u.load(r0, here, column, TILE);
-        dl.load(r0, here, column, TILE);
-        if (!ENDS && in.z) z.load(r0, here, column, TILE);
-        bt.load(rn, here, row_n, TILE);
-        if (!ENDS) ct.load(rn, here, row_n, TILE);
+    auto fetch = [&](int64_t t, int here) {
+        act.request(U, in.u + w.b * s.u_batch + t * s.u_node + c0, s.u_node, r0, col, here, column);
+        act.request(DELTA, in.delta + w.b * s.delta_batch + t * s.delta_node + c0, s.delta_node, r0, col, here, column);
+        if (!ENDS && in.z) act.request(Z, in.z + w.b * s.z_batch + t * s.z_node + c0, s.z_node, r0, col, here, column);
+        bt.load(in.B + w.b * s.B_batch + t * s.B_node, s.B_node, rn, n, here, row_n);
+        if (!ENDS) ct.load(in.C + w.b * s.C_batch + t * s.C_node, s.C_node, rn, n, here, row_n);
     };
-    T* op = out + (w.b * s.length + first + r0) * s.channels + c0 + col;
     float total = 0.f;
     int left = (int)(end - first);               // nodes of the chunk from this tile on
-    fetch(left);
+    fetch(first, left);
     for (int64_t t0 = first; left > 0; t0 += TILE, left -= TILE) {
-        Act ku, kz;
+        act.arrive();
 #pragma unroll
         for (int k = 0; k < Act::PER; ++k) {
-            ku.v[k] = u.v[k];
-            kz.v[k] = z.v[k];
+            if (TILE % RP != 0 && r0 + k * RP >= TILE) break;
+            const Pack<T, VEC> u = act.get(U, k), dl = act.get(DELTA, k);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {      // nodes past the end get dt = 0: the state stays
-                const float dt = r0 + k * RP < left && column ? step_of(to_f32<T>(dl.v[k].v[i]) + bias[i], s.softplus) : 0.f;
-                const float du = r0 + k * RP < left ? dt * to_f32<T>(u.v[k].v[i]) : 0.f;
+                const bool there = r0 + k * RP < left && column;
+                const float dt = there ? step_of(to_f32<T>(dl.v[i]) + bias[i], s.softplus) : 0.f;
+                const float du = there ? dt * to_f32<T>(u.v[i]) : 0.f;
                 sd[r0 + k * RP][col + i] = make_float4(dt, dt, du, du);
             }
         }
 #pragma unroll
         for (int k = 0; k < Bc::PER; ++k) {
-            sb[rn + k * RN][n] = to_f32<T>(bt.v[k].v[0]);
-            if (!ENDS) sc[rn + k * RN][n] = to_f32<T>(ct.v[k].v[0]);
+            if (TILE % RN != 0 && rn + k * RN >= TILE) break;
+            sb[rn + k * RN][n] = to_f32<T>(bt.v[k]);
+            if constexpr (!ENDS) sc[rn + k * RN][n] = to_f32<T>(ct.v[k]);
         }
         __syncthreads();
-        if (left > TILE) fetch(left - TILE);
+        if (left > TILE) fetch(t0 + TILE, left - TILE);
         const int here = left < TILE ? left : TILE;
+        if (!ENDS && kept != nullptr && mine)
+            store_states(kept + ((w.b * s.kept_nodes + t0 / KEEP) * s.channels + c) * s.states, q * NS, s.states, h);
+#pragma unroll 2
         for (int k0 = 0; k0 < TILE; k0 += 4) {
-            if (k0 >= here) break;
-            if (!ENDS && kept != nullptr && k0 % KEEP == 0 && mine)
-                store_states(kept + ((w.b * s.kept_nodes + (t0 + k0) / KEEP) * s.channels + c) * s.states, q * NS, s.states, h);
             float y[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -238,7 +273,7 @@ __global__ void __launch_bounds__(THREADS, FWD_BLOCKS) scan_fwd_kernel(ScanIn<T>
                 const Quad b4 = quad_at(&sb[k0 + k][q * NS]);
                 h.lo = fma2(exp2_pair(mul2(d.lo, a2.lo)), h.lo, mul2(d.hi, b4.lo));
                 h.hi = fma2(exp2_pair(mul2(d.lo, a2.hi)), h.hi, mul2(d.hi, b4.hi));
-                if (ENDS) {
+                if constexpr (ENDS) {
                     float dt, same;
                     unpair(d.lo, dt, same);
                     total += dt;
@@ -247,30 +282,32 @@ __global__ void __launch_bounds__(THREADS, FWD_BLOCKS) scan_fwd_kernel(ScanIn<T>
                     y[k] = sum2(fma2(c4.lo, h.lo, mul2(c4.hi, h.hi)));
                 }
             }
-            if (!ENDS) {
+            if constexpr (!ENDS) {
                 sum_lanes<S>(y, q);
                 put_sums<S, CT>(sy, y, k0, cl, q);
             }
         }
         __syncthreads();
-        if (!ENDS) {
+        if constexpr (!ENDS) {
+            T* op = out + (w.b * s.length + t0) * s.channels + c0;
 #pragma unroll
             for (int k = 0; k < Act::PER; ++k) {
                 const int r = r0 + k * RP;
                 if (r >= here || !column) continue;
+                // the fetch of the next tile went to the other half (2-byte packs: it is still in registers)
+                const Pack<T, VEC> u = act.get(U, k), z = act.get(Z, k);
                 float y[VEC];
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
                     y[i] = sy[r][col + i];
-                    if (in.D) y[i] = fmaf(dd[i], to_f32<T>(ku.v[k].v[i]), y[i]);
+                    if (in.D) y[i] = fmaf(in.D[c0 + col + i], to_f32<T>(u.v[i]), y[i]);
                     if (in.z) {
-                        const float g = to_f32<T>(kz.v[k].v[i]);
+                        const float g = to_f32<T>(z.v[i]);
                         y[i] *= g * sigmoid_f32(g);
                     }
                 }
-                store_pack<T, VEC>(op + (int64_t)(k * RP) * s.channels, y);
+                store_pack<T, VEC>(op + (int64_t)r * s.channels + col, y);
             }
-            op += (int64_t)TILE * s.channels;
         }
         // no barrier: the next tile writes sy only after its own first barrier, and sd, sb, sc were
         // last read before the barrier above
@@ -323,7 +360,7 @@ __global__ void __launch_bounds__(256) scan_join_kernel(float* __restrict__ loca
 
 // ----------------------------------------------------------------------------------------- backward
 // What one block keeps in shared memory.
-template <int S>
+template <typename T, int S, int VEC>
 struct BackSpace {
     static constexpr int CT = BACK_THREADS / S, NP = S * NS, WARPS = BACK_THREADS / 32;
     float4 sd[KEEP][CT];                                    // dt, dt, dt u, dt u
@@ -331,6 +368,9 @@ struct BackSpace {
     __align__(16) float sb[KEEP][NP], sc[KEEP][NP];
     float sy[KEEP][CT], st[KEEP][CT], sq[KEEP][CT];         // C.h, p.B, sum p a h A
     float red[WARPS][KEEP][2 * NP];                         // the warps' sums over channels: gB, gC
+    static constexpr int RP = BACK_THREADS / (CT / VEC), RN = BACK_THREADS / NP;
+    using Act = Feed<T, VEC, KEEP, RP, 4, BACK_THREADS>;
+    typename Act::Space room;
 };
 
 // part_bc[tile][b][t][2 NP]: this block's share of gB and gC; part_a[b][chunk][channel][states + 2]:
@@ -344,11 +384,11 @@ __global__ void __launch_bounds__(BACK_THREADS, BACK_BLOCKS) scan_bwd_kernel(Sca
                                                                 float* __restrict__ part_bc, float* __restrict__ part_a,
                                                                 float* __restrict__ local, float* __restrict__ sums, int64_t rows, ScanShape s) {
     pdl_wait_then_trigger();
-    using Space = BackSpace<S>;
-    constexpr int CT = Space::CT, NP = Space::NP;
-    constexpr int CP = CT / VEC, RP = BACK_THREADS / CP, RN = BACK_THREADS / NP;
-    using Act = Rows<T, VEC, KEEP, RP>;
-    using Bc = Rows<T, 1, KEEP, RN>;
+    using Space = BackSpace<T, S, VEC>;
+    using Act = typename Space::Act;
+    constexpr int CT = Space::CT, NP = Space::NP, CP = CT / VEC, RP = Space::RP, RN = Space::RN;
+    enum { DELTA, Z, GOUT, U };
+    using Bc = States<T, KEEP, RN>;
     extern __shared__ __align__(16) uint8_t raw_space[];
     Space& m = *reinterpret_cast<Space*>(raw_space);
     const Where w = where(s);
@@ -368,55 +408,47 @@ __global__ void __launch_bounds__(BACK_THREADS, BACK_BLOCKS) scan_bwd_kernel(Sca
     Quad ga = {0, 0};
     const int col = tid % CP * VEC, r0 = tid / CP, n = tid % NP, rn = tid / NP;
     const bool column = c0 + col < s.channels, row_n = n < s.states;
-    float bias[VEC], dd[VEC], gd[VEC] = {}, gbias[VEC] = {};
+    float bias[VEC], gd[VEC] = {}, gbias[VEC] = {};
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-        bias[i] = in.bias && column ? in.bias[c0 + col + i] : 0.f;
-        dd[i] = in.D && column ? in.D[c0 + col + i] : 0.f;
-    }
+    for (int i = 0; i < VEC; ++i) bias[i] = in.bias && column ? in.bias[c0 + col + i] : 0.f;
     const int ntiles = (int)((end - first + KEEP - 1) / KEEP);
     const int64_t last = first + (int64_t)(ntiles - 1) * KEEP;
-    Act u, dl, z, go;
+    Act act(m.room);
     Bc bt, ct;
-    u.start(in.u + w.b * s.u_batch + c0 + col, s.u_node, last + r0);
-    dl.start(in.delta + w.b * s.delta_batch + c0 + col, s.delta_node, last + r0);
-    z.start(in.z + w.b * s.z_batch + c0 + col, s.z_node, last + r0);
-    go.start(in.gout + w.b * s.g_batch + c0 + col, s.g_node, last + r0);
-    bt.start(in.B + w.b * s.B_batch + n, s.B_node, last + rn);
-    ct.start(in.C + w.b * s.C_batch + n, s.C_node, last + rn);
     Quad h0 = {0, 0};
-    const float* hp = mine && !ENDS ? kept + ((w.b * s.kept_nodes + last / KEEP) * s.channels + c) * s.states : nullptr;
-    auto fetch = [&](int here) {
-        if (!ENDS) u.load(r0, here, column, -KEEP);
-        dl.load(r0, here, column, -KEEP);
-        if (in.z) z.load(r0, here, column, -KEEP);
-        go.load(r0, here, column, -KEEP);
-        if (!ENDS) bt.load(rn, here, row_n, -KEEP);
-        ct.load(rn, here, row_n, -KEEP);
-        if (!ENDS) {
-            if (states_packed(s.states)) { if (mine && q * NS < s.states) h0 = quad_at(hp + q * NS); }
-            else if (mine) h0 = load_states(hp, q * NS, s.states, 1.f);
-            hp -= mine ? per : 0;
+    auto fetch = [&](int64_t t, int here) {
+        act.request(DELTA, in.delta + w.b * s.delta_batch + t * s.delta_node + c0, s.delta_node, r0, col, here, column);
+        if (in.z) act.request(Z, in.z + w.b * s.z_batch + t * s.z_node + c0, s.z_node, r0, col, here, column);
+        act.request(GOUT, in.gout + w.b * s.g_batch + t * s.g_node + c0, s.g_node, r0, col, here, column);
+        ct.load(in.C + w.b * s.C_batch + t * s.C_node, s.C_node, rn, n, here, row_n);
+        if constexpr (!ENDS) {
+            act.request(U, in.u + w.b * s.u_batch + t * s.u_node + c0, s.u_node, r0, col, here, column);
+            bt.load(in.B + w.b * s.B_batch + t * s.B_node, s.B_node, rn, n, here, row_n);
+            if (mine) {
+                const float* hp = kept + ((w.b * s.kept_nodes + t / KEEP) * s.channels + c) * s.states;
+                if (!states_packed(s.states)) h0 = load_states(hp, q * NS, s.states, 1.f);
+                else if (q * NS < s.states) h0 = quad_at(hp + q * NS);
+            }
         }
     };
     float total = 0.f;
-    if (ntiles > 0) fetch((int)(end - last));
+    if (ntiles > 0) fetch(last, (int)(end - last));
     for (int64_t t0 = last; t0 >= first && ntiles > 0; t0 -= KEEP) {
         const int here = (int)(end - t0 < KEEP ? end - t0 : KEEP);
-        Act ku, kz, kg, kd;
+        act.arrive();
 #pragma unroll
         for (int k = 0; k < Act::PER; ++k) {
             const int r = r0 + k * RP;
             if (KEEP % RP != 0 && r >= KEEP) break;
-            ku.v[k] = u.v[k]; kz.v[k] = z.v[k]; kg.v[k] = go.v[k]; kd.v[k] = dl.v[k];
+            const Pack<T, VEC> dl = act.get(DELTA, k), z = act.get(Z, k), go = act.get(GOUT, k), u = act.get(U, k);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
                 const bool there = r < here && column;
-                const float dt = there ? step_of(to_f32<T>(dl.v[k].v[i]) + bias[i], s.softplus) : 0.f;
-                const float du = ENDS || !there ? 0.f : dt * to_f32<T>(u.v[k].v[i]);
-                float g = to_f32<T>(go.v[k].v[i]);
+                const float dt = there ? step_of(to_f32<T>(dl.v[i]) + bias[i], s.softplus) : 0.f;
+                const float du = ENDS || !there ? 0.f : dt * to_f32<T>(u.v[i]);
+                float g = to_f32<T>(go.v[i]);
                 if (in.z) {
-                    const float zv = to_f32<T>(z.v[k].v[i]);
+                    const float zv = to_f32<T>(z.v[i]);
                     g *= zv * sigmoid_f32(zv);
                 }
                 if (!there) g = 0.f;
@@ -427,13 +459,13 @@ __global__ void __launch_bounds__(BACK_THREADS, BACK_BLOCKS) scan_bwd_kernel(Sca
 #pragma unroll
         for (int k = 0; k < Bc::PER; ++k) {
             if (KEEP % RN != 0 && rn + k * RN >= KEEP) break;
-            if (!ENDS) m.sb[rn + k * RN][n] = to_f32<T>(bt.v[k].v[0]);
-            m.sc[rn + k * RN][n] = to_f32<T>(ct.v[k].v[0]);
+            if constexpr (!ENDS) m.sb[rn + k * RN][n] = to_f32<T>(bt.v[k]);
+            m.sc[rn + k * RN][n] = to_f32<T>(ct.v[k]);
         }
         Quad hs[KEEP + 1];                         // hs[r]: the state BEFORE node r
         hs[0] = h0;
         __syncthreads();
-        if (t0 > first) fetch(KEEP);
+        if (t0 > first) fetch(t0 - KEEP, KEEP);
         if constexpr (ENDS) {
 #pragma unroll
             for (int r = KEEP - 1; r >= 0; --r) {
@@ -521,18 +553,20 @@ __global__ void __launch_bounds__(BACK_THREADS, BACK_BLOCKS) scan_bwd_kernel(Sca
         for (int k = 0; k < Act::PER; ++k) {
             const int r = r0 + k * RP;
             if (r >= here || !column) continue;
+            const Pack<T, VEC> dl = act.get(DELTA, k), z = act.get(Z, k), go = act.get(GOUT, k), u = act.get(U, k);
             float ou[VEC], od[VEC], oz[VEC];
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
                 const float dt = m.sd[r][col + i].x, gy = m.sg[r][col + i].x, through = m.st[r][col + i];
-                const float uv = to_f32<T>(ku.v[k].v[i]);
-                ou[i] = fmaf(dt, through, dd[i] * gy);
+                const float uv = to_f32<T>(u.v[i]);
+                const float dd = in.D ? in.D[c0 + col + i] : 0.f;
+                ou[i] = fmaf(dt, through, dd * gy);
                 float gr = fmaf(uv, through, m.sq[r][col + i] * (1.f / LOG2_E));
-                if (s.softplus) gr *= sigmoid_f32(to_f32<T>(kd.v[k].v[i]) + bias[i]);
+                if (s.softplus) gr *= sigmoid_f32(to_f32<T>(dl.v[i]) + bias[i]);
                 od[i] = gr;
                 if (in.z) {
-                    const float zv = to_f32<T>(kz.v[k].v[i]), sig = sigmoid_f32(zv);
-                    oz[i] = to_f32<T>(kg.v[k].v[i]) * fmaf(dd[i], uv, m.sy[r][col + i]) * sig * fmaf(zv, 1.f - sig, 1.f);
+                    const float zv = to_f32<T>(z.v[i]), sig = sigmoid_f32(zv);
+                    oz[i] = to_f32<T>(go.v[i]) * fmaf(dd, uv, m.sy[r][col + i]) * sig * fmaf(zv, 1.f - sig, 1.f);
                 }
                 gd[i] = fmaf(gy, uv, gd[i]);
                 gbias[i] += gr;
@@ -693,13 +727,23 @@ ScanShape plan(const fpde_scan_args* a, bool backward) {
     s.softplus = a->softplus;
     s.tiles = (int)ceil_div(a->channels, threads / lanes_of(a->states));
     s.kept_nodes = ceil_div(a->length, KEEP);
-    // Splitting a row costs a second pass over its exponentials: done while it still fills idle SMs.
-    const int64_t blocks = a->batch * s.tiles;
-    const int64_t want = 148 * (backward ? 3 : 6);
-    int64_t chunks = 1;
-    if (blocks * 2 <= want) chunks = want / (blocks > 0 ? blocks : 1);
-    int64_t chunk = ceil_div(ceil_div(a->length > 0 ? a->length : 1, chunks), TILE) * TILE;
-    if (chunk < 2 * TILE) chunk = 2 * TILE;
+    // Chunks.  A march takes its nodes times the blocks that an SM has to run, over the number that run at
+    // full speed together (FULL: beyond it they share the special function units or the issue slots).
+    // Splitting adds the pass that forms the chunks' ends, a share ENDS_COST of the march, and two launches,
+    // worth about 80 nodes.  The cheapest number of chunks wins; the fewest of equals.
+    const int64_t length = a->length > 0 ? a->length : 1, blocks = a->batch * s.tiles;
+    const double full = backward ? 2 : 4, ends_cost = backward ? 0.3 : 0.5;
+    const int64_t most = ceil_div(length, 2 * TILE) < 1024 ? ceil_div(length, 2 * TILE) : 1024;
+    int64_t chunk = length;
+    double best = 0;
+    for (int64_t k = 1; k <= most; ++k) {
+        const int64_t nodes = k == 1 ? length : ceil_div(ceil_div(length, k), TILE) * TILE;
+        const double busy = (double)ceil_div(blocks * ceil_div(length, nodes), 148) / full;
+        const double cost = (double)nodes * (busy > 1 ? busy : 1) * (k == 1 ? 1 : 1 + ends_cost) + (k == 1 ? 0 : 80);
+        if (k == 1 || cost < best) { best = cost; chunk = nodes; }
+        if (busy > 2) break;
+    }
+    chunk = ceil_div(chunk, TILE) * TILE;
     if (chunk > (1 << 30)) chunk = 1 << 30;
     s.chunk = (int)chunk;
     s.chunks = (int)ceil_div(a->length > 0 ? a->length : 1, chunk);
@@ -798,7 +842,7 @@ cudaError_t run_bwd(const fpde_scan_args* a, cudaStream_t st) {
     const int64_t blocks = a->batch * s.tiles * s.chunks;
     if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
     const dim3 grid((unsigned)blocks);
-    constexpr size_t bytes = sizeof(BackSpace<S>);
+    constexpr size_t bytes = sizeof(BackSpace<T, S, VEC>);
     char* ws = (char*)a->workspace;
     float *local = nullptr, *part_bc = (float*)(ws + w.part_bc), *part_a = (float*)(ws + w.part_a);
     if (s.chunks > 1) {
