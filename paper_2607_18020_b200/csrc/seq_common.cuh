@@ -93,10 +93,66 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t both(float v) { return pair(v, v); }
 __device__ __forceinline__ float sum2(uint64_t p) {
     float lo, hi;
     unpair(p, lo, hi);
     return lo + hi;
+}
+
+__device__ __forceinline__ float max_nan(float a, float b) {      // NaN if either is
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+// softplus_f32 and sigmoid_f32 of two values.
+__device__ __forceinline__ uint64_t softplus_pair(uint64_t v) {
+    float x, y, nx, ny;
+    unpair(v, x, y);
+    const uint64_t a = pair(fmaxf(-fabsf(x), -150.f), fmaxf(-fabsf(y), -150.f));
+    const uint64_t neg = mul2(a, both(-LOG2_E));
+    const uint64_t lo = fma2(a, both(1.925963033e-8f), fma2(a, both(LOG2_E), neg));
+    unpair(neg, nx, ny);
+    uint64_t e = pair(exp2_f32(-nx), exp2_f32(-ny));
+    e = fma2(e, mul2(lo, both(0.6931471806f)), e);
+    uint64_t p = both(0.00523267686f);
+    p = fma2(p, e, both(-0.029505169f));
+    p = fma2(p, e, both(0.0782258362f));
+    p = fma2(p, e, both(-0.136632353f));
+    p = fma2(p, e, both(0.191060022f));
+    p = fma2(p, e, both(-0.248429805f));
+    p = fma2(p, e, both(0.333190978f));
+    p = fma2(p, e, both(-0.499994934f));
+    p = fma2(p, e, both(0.99999994f));
+    return fma2(e, p, pair(max_nan(x, 0.f), max_nan(y, 0.f)));
+}
+__device__ __forceinline__ uint64_t sigmoid_pair(uint64_t v) {
+    float x, y;
+    unpair(mul2(v, both(-LOG2_E)), x, y);
+    unpair(add2(pair(exp2_f32(x), exp2_f32(y)), both(1.f)), x, y);
+    return pair(reciprocal_f32(x), reciprocal_f32(y));
+}
+
+// The same for the one or two channels of a thread.
+template <int N>
+__device__ __forceinline__ void softplus_of(float (&v)[N]) {
+    if constexpr (N == 2) unpair(softplus_pair(pair(v[0], v[1])), v[0], v[1]);
+    else v[0] = softplus_f32(v[0]);
+}
+template <int N>
+__device__ __forceinline__ void sigmoid_of(float (&out)[N], const float (&v)[N]) {
+    if constexpr (N == 2) unpair(sigmoid_pair(pair(v[0], v[1])), out[0], out[1]);
+    else out[0] = sigmoid_f32(v[0]);
+}
+template <typename T, int N>
+__device__ __forceinline__ void widen(float (&out)[N], const Pack<T, N>& k) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) out[i] = to_f32<T>(k.v[i]);
 }
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }

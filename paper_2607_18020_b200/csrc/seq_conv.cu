@@ -107,12 +107,6 @@ __device__ __forceinline__ Pack<T, VEC> x_at(const T* x, int64_t x_node, const T
     return pack_at<T, VEC>(window + (t + W - 1) * channels, window != nullptr && t + W - 1 >= 0);
 }
 
-template <typename T, int VEC>
-__device__ __forceinline__ void widen(float (&out)[VEC], const Pack<T, VEC>& k) {
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) out[i] = to_f32<T>(k.v[i]);
-}
-
 template <typename T, int VEC, int W>
 __global__ void __launch_bounds__(CONV_THREADS) conv_fwd_kernel(
     const T* __restrict__ x, const float* __restrict__ weight, const float* __restrict__ bias, const T* __restrict__ state,

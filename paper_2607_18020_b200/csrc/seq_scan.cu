@@ -27,13 +27,12 @@
 namespace fpde {
 namespace {
 
-constexpr int THREADS = 128;      // of the forward kernels
-constexpr int BACK_THREADS = 256; // of the backward kernel: halves the partial sums of gB and gC
-constexpr int FWD_BLOCKS = 6, BACK_BLOCKS = 2;     // resident blocks that the registers are budgeted for
-constexpr int TILE = 16;          // nodes of a forward tile
-constexpr int KEEP = 16;          // nodes between stored states = nodes of a backward tile
-static_assert(TILE == KEEP, "the forward march stores the state before each of its tiles");
-constexpr int NS = 4;             // states of a thread
+constexpr int FWD_THREADS = 128, BACK_THREADS = 128, STEP_THREADS = 128;
+constexpr int FWD_UNROLL = 2;
+constexpr int TILE = 16;          // nodes brought to shared memory together
+constexpr int KEEP = 8;           // nodes between stored states: what the backward march holds in registers
+constexpr int NS = 4, NC = 2;     // states and channels of a thread
+constexpr int FWD_BLOCKS = 5, BACK_BLOCKS = 2;     // resident blocks that the registers are budgeted for
 
 struct ScanShape {
     int64_t length;
@@ -70,35 +69,51 @@ __device__ __forceinline__ float step_of(float raw, int softplus) { return softp
 // A thread's own share of the tiles of ARRAYS activations: pack column `col` of rows r0, r0 + RP, ...  The
 // next tile travels while this one is computed, by cp.async into shared memory that only this thread reads
 // (no registers held, no barrier); 2-byte packs, which cp.async does not have, wait in registers.
-template <typename T, int VEC, int NODES, int RP, int ARRAYS, int THREADS_>
+template <typename T, int VEC, int NODES, int RP, int ARRAYS, int THREADS>
 struct Feed {
     static constexpr int PER = (NODES + RP - 1) / RP, BYTES = sizeof(T) * VEC;
     static constexpr bool ASYNC = BYTES >= 4;
     using P = Pack<T, VEC>;
-    struct Space { P v[ASYNC ? 2 : 1][ARRAYS][PER][THREADS_]; };
+    struct Space { P v[ASYNC ? 2 : 1][ARRAYS][PER][THREADS]; };
     Space& space;
+    const T* p[ARRAYS];                           // of row r0 of the tile to request next
     int now = 0;                                  // half that holds the current tile
+    int r0;
+    bool column;                                  // the thread's channels exist (zeros where not)
     P held[ASYNC ? 1 : ARRAYS][PER];
-    __device__ __forceinline__ Feed(Space& where_) : space(where_) {}
-
-    // row0: the array's first row of the tile (block-uniform); rows from `here` on read as zero
-    __device__ __forceinline__ void request(int array, const T* row0, int64_t node, int r0, int col, int here, bool column) {
+    __device__ __forceinline__ Feed(Space& where_, int r0_, bool column_) : space(where_), r0(r0_), column(column_) {
 #pragma unroll
-        for (int k = 0; k < PER; ++k) {
-            const int r = r0 + k * RP;
-            const bool there = column && r < here;
-            const T* src = row0 + r * node + col;
-            if (ASYNC) {
-                P* dst = &space.v[now ^ 1][array][k][threadIdx.x];
-                if (there)
-                    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(dst))), "l"(src),
-                                 "n"(BYTES < 4 ? 4 : BYTES) : "memory");
-                else *dst = P{};
+        for (int h = 0; h < (ASYNC ? 2 : 1); ++h)
+#pragma unroll
+            for (int a = 0; a < ARRAYS; ++a)
+#pragma unroll
+                for (int k = 0; k < PER; ++k) {
+                    if (!column) space.v[h][a][k][threadIdx.x] = P{};
+                    if (!ASYNC) held[a][k] = P{};
+                }
+    }
+    __device__ __forceinline__ void start(int array, const T* row0, int64_t node, int col) { p[array] = row0 + r0 * node + col; }
+    __device__ __forceinline__ void one(int array, int k, const T* src) {
+        if (ASYNC)
+            asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(&space.v[now ^ 1][array][k][threadIdx.x]))),
+                         "l"(src), "n"(BYTES < 4 ? 4 : BYTES) : "memory");
+        else held[array][k] = load_pack<T, VEC>(src);
+    }
+    // Asks for the tile at p, of which `here` rows exist, and moves on by `advance` nodes.  Rows that do not
+    // exist keep what an earlier tile left: they are masked where they are used.
+    __device__ __forceinline__ void request(int array, int64_t node, int here, int advance) {
+        const T* src = p[array];
+        if (column) {
+            if (here >= NODES && NODES % RP == 0) {
+#pragma unroll
+                for (int k = 0; k < PER; ++k) one(array, k, src + (int64_t)(k * RP) * node);
             } else {
-                held[array][k] = P{};
-                if (there) held[array][k] = load_pack<T, VEC>(src);
+#pragma unroll
+                for (int k = 0; k < PER; ++k)
+                    if (r0 + k * RP < here) one(array, k, src + (int64_t)(k * RP) * node);
             }
         }
+        p[array] = src + advance * node;
     }
     __device__ __forceinline__ void arrive() {    // what was requested becomes the current tile
         if (ASYNC) {
@@ -111,7 +126,9 @@ struct Feed {
                 for (int k = 0; k < PER; ++k) space.v[0][a][k][threadIdx.x] = held[a][k];
         }
     }
-    __device__ __forceinline__ P get(int array, int k) const { return space.v[ASYNC ? now : 0][array][k][threadIdx.x]; }
+    __device__ __forceinline__ void get(float (&out)[VEC], int array, int k) const {
+        widen<T, VEC>(out, space.v[ASYNC ? now : 0][array][k][threadIdx.x]);
+    }
 };
 
 // The same for B and C, one state each of rows rn, rn + RN, ...: few, kept in registers.
@@ -119,43 +136,59 @@ template <typename T, int NODES, int RN>
 struct States {
     static constexpr int PER = (NODES + RN - 1) / RN;
     T v[PER];
-    __device__ __forceinline__ void load(const T* row0, int64_t node, int rn, int n, int here, bool there) {
+    const T* p;
+    __device__ __forceinline__ void load(int64_t node, int rn, int here, bool there, int advance) {
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
             v[k] = from_f32<T>(0.f);
-            if (there && rn + k * RN < here) v[k] = row0[(rn + k * RN) * node + n];
+            if (there && rn + k * RN < here) v[k] = p[(int64_t)(k * RN) * node];
         }
+        p += advance * node;
     }
 };
 
-// Sum over the S lanes of a channel of four values, one per node: lane q (of S) returns the sum of
-// value q & 3 for S >= 4; S = 2: v[0], v[1] become the sums of values 2 (q & 1) and 2 (q & 1) + 1.
-template <int S>
-__device__ __forceinline__ void sum_lanes(float (&v)[4], int q) {
-    if (S == 2) {
-        const bool up = q & 1;
-        const float s0 = up ? v[0] : v[2], s1 = up ? v[1] : v[3];
-        v[0] = (up ? v[2] : v[0]) + __shfl_xor_sync(~0u, s0, 1);
-        v[1] = (up ? v[3] : v[1]) + __shfl_xor_sync(~0u, s1, 1);
-        return;
-    }
-    const bool hi = q & 2, up = q & 1;
-    const float s0 = hi ? v[0] : v[2], s1 = hi ? v[1] : v[3];
-    const float a = (hi ? v[2] : v[0]) + __shfl_xor_sync(~0u, s0, 2);
-    const float b = (hi ? v[3] : v[1]) + __shfl_xor_sync(~0u, s1, 2);
-    v[0] = (up ? b : a) + __shfl_xor_sync(~0u, up ? a : b, 1);
+// Sums of N values over the lanes that differ in the bits HI .. LO of the lane number: while a lane holds
+// more than one value it gives half of them away and takes its partner's share of the others.  Afterwards
+// v[0 .. left) are the sums of values from .. from + left - 1 (`from` is returned).
+template <int N, int HI, int LO>
+__host__ __device__ constexpr int sums_left() {
+    int left = N;
+    for (int m = HI; m >= LO; m /= 2) left = left > 1 ? left / 2 : 1;
+    return left;
+}
+template <int N, int HI, int LO>
+__device__ __forceinline__ int sum_lanes(float (&v)[N], int lane) {
+    int from = 0;
 #pragma unroll
-    for (int m = 4; m < S; m *= 2) v[0] += __shfl_xor_sync(~0u, v[0], m);
+    for (int m = HI, left = N; m >= LO; m /= 2) {
+        if (left > 1) {
+            left /= 2;
+            const bool up = lane & m;
+#pragma unroll
+            for (int i = 0; i < left; ++i) {
+                const float send = up ? v[i] : v[left + i];
+                v[i] = (up ? v[left + i] : v[i]) + __shfl_xor_sync(~0u, send, m);
+            }
+            from += up ? left : 0;
+        } else {
+            v[0] += __shfl_xor_sync(~0u, v[0], m);
+        }
+    }
+    return from;
 }
 
-// Writes the sums that sum_lanes left for nodes k0 .. k0+3 of channel c.
+// Sums over the states of four nodes k0 .. k0+3 of the thread's two channels (value 2 * node + channel)
+// to dst[node][channel].
 template <int S, int CT>
-__device__ __forceinline__ void put_sums(float (*dst)[CT], const float (&v)[4], int k0, int c, int q) {
-    if (S == 2) {
-        dst[k0 + 2 * (q & 1)][c] = v[0];
-        dst[k0 + 2 * (q & 1) + 1][c] = v[1];
-    } else if (S == 4 || q < 4) {
-        dst[k0 + (q & 3)][c] = v[0];
+__device__ __forceinline__ void put_sums(float (*dst)[CT], float (&v)[4 * NC], int k0, int c, int q) {
+    const int from = sum_lanes<4 * NC, S / 2, 1>(v, q);
+    constexpr int LEFT = sums_left<4 * NC, S / 2, 1>();
+    float* at = &dst[k0 + from / NC][c];
+    if constexpr (LEFT >= NC) {
+#pragma unroll
+        for (int i = 0; i < LEFT / NC; ++i) *reinterpret_cast<float2*>(at + i * CT) = make_float2(v[NC * i], v[NC * i + 1]);
+    } else if (S <= 8 || q % 2 == 0) {
+        at[from % NC] = v[0];
     }
 }
 
@@ -193,135 +226,172 @@ __device__ __forceinline__ void store_states(float* p, int n, int states, const 
 }
 
 // ------------------------------------------------------------------------------------------ forward
+template <typename T, int S, int VEC, bool ENDS>
+struct FwdSpace {
+    static constexpr int CT = FWD_THREADS / S * NC, NP = S * NS;
+    static constexpr int RP = FWD_THREADS / (CT / VEC), RN = FWD_THREADS / NP;      // rows at a time
+    using Act = Feed<T, VEC, TILE, RP, ENDS ? 2 : 3, FWD_THREADS>;
+    float4 sd[TILE][CT];              // dt, dt, dt u, dt u
+    __align__(16) float sb[TILE][NP], sc[ENDS ? 1 : TILE][NP];
+    __align__(8) float sy[ENDS ? 1 : TILE][CT];
+    typename Act::Space room;
+};
+
 // ENDS = false: the march.  ENDS = true, for rows cut into chunks: only what the join needs,
 // local[b][chunk][channel][state] = state at the chunk's end when it starts from zero and
 // sums[b][chunk][channel] = sum of dt.
 template <typename T, int S, int VEC, bool ENDS>
-__global__ void __launch_bounds__(THREADS, FWD_BLOCKS) scan_fwd_kernel(ScanIn<T> in, const float* __restrict__ state, const float* __restrict__ enter,
+__global__ void __launch_bounds__(FWD_THREADS, FWD_BLOCKS) scan_fwd_kernel(ScanIn<T> in, const float* __restrict__ state, const float* __restrict__ enter,
                                                            T* __restrict__ out, float* __restrict__ state_out, float* __restrict__ kept,
                                                            float* __restrict__ local, float* __restrict__ sums, ScanShape s) {
     pdl_wait_then_trigger();
-    constexpr int CT = THREADS / S, NP = S * NS;
-    constexpr int CP = CT / VEC, RP = THREADS / CP, RN = THREADS / NP;      // packs of a row; rows at a time
+    using Space = FwdSpace<T, S, VEC, ENDS>;
+    using Act = typename Space::Act;
+    constexpr int CT = Space::CT, NP = Space::NP, CP = CT / VEC, RP = Space::RP, RN = Space::RN;
     enum { U, DELTA, Z };
-    using Act = Feed<T, VEC, TILE, RP, ENDS ? 2 : 3, THREADS>;
     using Bc = States<T, TILE, RN>;
-    __shared__ typename Act::Space room;
-    __shared__ float4 sd[TILE][CT];              // dt, dt, dt u, dt u
-    __shared__ __align__(16) float sb[TILE][NP], sc[ENDS ? 1 : TILE][NP];
-    __shared__ float sy[ENDS ? 1 : TILE][CT];
+    extern __shared__ __align__(16) uint8_t raw_space[];
+    Space& m = *reinterpret_cast<Space*>(raw_space);
     const Where w = where(s);
-    const int tid = threadIdx.x, q = tid % S, cl = tid / S;
+    const int tid = threadIdx.x, q = tid % S, cl = tid / S * NC;
     const int c0 = w.tile * CT, c = c0 + cl;
     const int64_t first = (int64_t)w.chunk * s.chunk;
     const int64_t end = first + s.chunk < s.length ? first + s.chunk : s.length;
     const int64_t per = (int64_t)s.channels * s.states;
     const int64_t at = w.b * s.chunks + w.chunk;
-    const bool mine = c < s.channels;
-    const Quad a2 = load_states(mine ? in.A + (int64_t)c * s.states : nullptr, q * NS, s.states, LOG2_E);
-    Quad h = load_states(ENDS || !mine ? nullptr : enter ? enter + at * per + (int64_t)c * s.states : state ? state + w.b * per + (int64_t)c * s.states : nullptr,
-                         q * NS, s.states, 1.f);
+    Quad a2[NC], h[NC];
+#pragma unroll
+    for (int k = 0; k < NC; ++k) {
+        const int64_t cn = (int64_t)(c + k) * s.states;
+        const bool mine = c + k < s.channels;
+        a2[k] = load_states(mine ? in.A + cn : nullptr, q * NS, s.states, LOG2_E);
+        h[k] = load_states(ENDS || !mine ? nullptr : enter ? enter + at * per + cn : state ? state + w.b * per + cn : nullptr, q * NS, s.states, 1.f);
+    }
     // what this thread brings in: pack column `col` of rows r0, r0 + RP, ... and state n of rows rn, rn + RN, ...
     const int col = tid % CP * VEC, r0 = tid / CP, n = tid % NP, rn = tid / NP;
     const bool column = c0 + col < s.channels, row_n = n < s.states;
-    float bias[VEC];
+    float bias[VEC], dd[VEC];
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) bias[i] = in.bias && column ? in.bias[c0 + col + i] : 0.f;
-    Act act(room);
+    for (int i = 0; i < VEC; ++i) {
+        bias[i] = in.bias && column ? in.bias[c0 + col + i] : 0.f;
+        dd[i] = in.D && column ? in.D[c0 + col + i] : 0.f;
+    }
+    Act act(m.room, r0, column);
     Bc bt, ct;
-    auto fetch = [&](int64_t t, int here) {
-        act.request(U, in.u + w.b * s.u_batch + t * s.u_node + c0, s.u_node, r0, col, here, column);
-        act.request(DELTA, in.delta + w.b * s.delta_batch + t * s.delta_node + c0, s.delta_node, r0, col, here, column);
-        if (!ENDS && in.z) act.request(Z, in.z + w.b * s.z_batch + t * s.z_node + c0, s.z_node, r0, col, here, column);
-        bt.load(in.B + w.b * s.B_batch + t * s.B_node, s.B_node, rn, n, here, row_n);
-        if (!ENDS) ct.load(in.C + w.b * s.C_batch + t * s.C_node, s.C_node, rn, n, here, row_n);
+    act.start(U, in.u + w.b * s.u_batch + first * s.u_node + c0, s.u_node, col);
+    act.start(DELTA, in.delta + w.b * s.delta_batch + first * s.delta_node + c0, s.delta_node, col);
+    if constexpr (!ENDS) act.start(Z, in.z + w.b * s.z_batch + first * s.z_node + c0, s.z_node, col);
+    bt.p = in.B + w.b * s.B_batch + (first + rn) * s.B_node + n;
+    ct.p = in.C + w.b * s.C_batch + (first + rn) * s.C_node + n;
+    auto fetch = [&](int here) {
+        act.request(U, s.u_node, here, TILE);
+        act.request(DELTA, s.delta_node, here, TILE);
+        bt.load(s.B_node, rn, here, row_n, TILE);
+        if constexpr (!ENDS) {
+            if (in.z) act.request(Z, s.z_node, here, TILE);
+            ct.load(s.C_node, rn, here, row_n, TILE);
+        }
     };
-    float total = 0.f;
+    float total[NC] = {};
     int left = (int)(end - first);               // nodes of the chunk from this tile on
-    fetch(first, left);
+    fetch(left);
     for (int64_t t0 = first; left > 0; t0 += TILE, left -= TILE) {
         act.arrive();
 #pragma unroll
         for (int k = 0; k < Act::PER; ++k) {
-            if (TILE % RP != 0 && r0 + k * RP >= TILE) break;
-            const Pack<T, VEC> u = act.get(U, k), dl = act.get(DELTA, k);
+            const int r = r0 + k * RP;
+            if (TILE % RP != 0 && r >= TILE) break;
+            float dt[VEC], u[VEC];
+            act.get(u, U, k);
+            act.get(dt, DELTA, k);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {      // nodes past the end get dt = 0: the state stays
-                const bool there = r0 + k * RP < left && column;
-                const float dt = there ? step_of(to_f32<T>(dl.v[i]) + bias[i], s.softplus) : 0.f;
-                const float du = there ? dt * to_f32<T>(u.v[i]) : 0.f;
-                sd[r0 + k * RP][col + i] = make_float4(dt, dt, du, du);
+            for (int i = 0; i < VEC; ++i) dt[i] += bias[i];
+            if (s.softplus) softplus_of<VEC>(dt);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                u[i] *= dt[i];
+                if (left < TILE && r >= left) dt[i] = u[i] = 0.f;      // past the end: the state stays
+                m.sd[r][col + i] = make_float4(dt[i], dt[i], u[i], u[i]);
             }
         }
 #pragma unroll
         for (int k = 0; k < Bc::PER; ++k) {
             if (TILE % RN != 0 && rn + k * RN >= TILE) break;
-            sb[rn + k * RN][n] = to_f32<T>(bt.v[k]);
-            if constexpr (!ENDS) sc[rn + k * RN][n] = to_f32<T>(ct.v[k]);
+            m.sb[rn + k * RN][n] = to_f32<T>(bt.v[k]);
+            if constexpr (!ENDS) m.sc[rn + k * RN][n] = to_f32<T>(ct.v[k]);
         }
         __syncthreads();
-        if (left > TILE) fetch(t0 + TILE, left - TILE);
+        if (left > TILE) fetch(left - TILE);
         const int here = left < TILE ? left : TILE;
-        if (!ENDS && kept != nullptr && mine)
-            store_states(kept + ((w.b * s.kept_nodes + t0 / KEEP) * s.channels + c) * s.states, q * NS, s.states, h);
-#pragma unroll 2
+#pragma unroll FWD_UNROLL
         for (int k0 = 0; k0 < TILE; k0 += 4) {
-            float y[4];
+            if (!ENDS && kept != nullptr && k0 % KEEP == 0 && k0 < here) {
+                float* dst = kept + ((w.b * s.kept_nodes + (t0 + k0) / KEEP) * s.channels + c) * s.states;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const Quad d = quad_at(&sd[k0 + k][cl].x);
-                const Quad b4 = quad_at(&sb[k0 + k][q * NS]);
-                h.lo = fma2(exp2_pair(mul2(d.lo, a2.lo)), h.lo, mul2(d.hi, b4.lo));
-                h.hi = fma2(exp2_pair(mul2(d.lo, a2.hi)), h.hi, mul2(d.hi, b4.hi));
-                if constexpr (ENDS) {
-                    float dt, same;
-                    unpair(d.lo, dt, same);
-                    total += dt;
-                } else {
-                    const Quad c4 = quad_at(&sc[k0 + k][q * NS]);
-                    y[k] = sum2(fma2(c4.lo, h.lo, mul2(c4.hi, h.hi)));
+                for (int k = 0; k < NC; ++k)
+                    if (c + k < s.channels) store_states(dst + k * s.states, q * NS, s.states, h[k]);
+            }
+            float y[4 * NC];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const Quad b4 = quad_at(&m.sb[k0 + r][q * NS]);
+                Quad c4;
+                if constexpr (!ENDS) c4 = quad_at(&m.sc[k0 + r][q * NS]);
+#pragma unroll
+                for (int k = 0; k < NC; ++k) {
+                    const Quad d = quad_at(&m.sd[k0 + r][cl + k].x);
+                    h[k].lo = fma2(exp2_pair(mul2(d.lo, a2[k].lo)), h[k].lo, mul2(d.hi, b4.lo));
+                    h[k].hi = fma2(exp2_pair(mul2(d.lo, a2[k].hi)), h[k].hi, mul2(d.hi, b4.hi));
+                    if constexpr (ENDS) {
+                        float dt, same;
+                        unpair(d.lo, dt, same);
+                        total[k] += dt;
+                    } else {
+                        y[NC * r + k] = sum2(fma2(c4.lo, h[k].lo, mul2(c4.hi, h[k].hi)));
+                    }
                 }
             }
-            if constexpr (!ENDS) {
-                sum_lanes<S>(y, q);
-                put_sums<S, CT>(sy, y, k0, cl, q);
-            }
+            if constexpr (!ENDS) put_sums<S, CT>(m.sy, y, k0, cl, q);
         }
         __syncthreads();
         if constexpr (!ENDS) {
-            T* op = out + (w.b * s.length + t0) * s.channels + c0;
+            T* op = out + (w.b * s.length + t0 + r0) * s.channels + c0 + col;
 #pragma unroll
             for (int k = 0; k < Act::PER; ++k) {
                 const int r = r0 + k * RP;
                 if (r >= here || !column) continue;
                 // the fetch of the next tile went to the other half (2-byte packs: it is still in registers)
-                const Pack<T, VEC> u = act.get(U, k), z = act.get(Z, k);
-                float y[VEC];
+                float y[VEC], u[VEC], z[VEC], g[VEC];
+                act.get(u, U, k);
+                if (in.z) {
+                    act.get(z, Z, k);
+                    sigmoid_of<VEC>(g, z);
+                }
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
-                    y[i] = sy[r][col + i];
-                    if (in.D) y[i] = fmaf(in.D[c0 + col + i], to_f32<T>(u.v[i]), y[i]);
-                    if (in.z) {
-                        const float g = to_f32<T>(z.v[i]);
-                        y[i] *= g * sigmoid_f32(g);
-                    }
+                    y[i] = m.sy[r][col + i];
+                    if (in.D) y[i] = fmaf(dd[i], u[i], y[i]);
+                    if (in.z) y[i] *= z[i] * g[i];
                 }
-                store_pack<T, VEC>(op + (int64_t)r * s.channels + col, y);
+                store_pack<T, VEC>(op + (int64_t)(k * RP) * s.channels, y);
             }
         }
         // no barrier: the next tile writes sy only after its own first barrier, and sd, sb, sc were
         // last read before the barrier above
     }
-    if (!mine) return;
-    if (ENDS) {
-        store_states(local + (at * s.channels + c) * s.states, q * NS, s.states, h);
-        if (q == 0) sums[at * s.channels + c] = total;
-    } else if (state_out != nullptr && w.chunk == s.chunks - 1) {
-        float v[NS];
-        quad_to(v, h);
 #pragma unroll
-        for (int i = 0; i < NS; ++i)
-            if (q * NS + i < s.states) state_out[w.b * per + (int64_t)c * s.states + q * NS + i] = v[i];
+    for (int k = 0; k < NC; ++k) {
+        if (c + k >= s.channels) continue;
+        if (ENDS) {
+            store_states(local + (at * s.channels + c + k) * s.states, q * NS, s.states, h[k]);
+            if (q == 0) sums[at * s.channels + c + k] = total[k];
+        } else if (state_out != nullptr && w.chunk == s.chunks - 1) {
+            float v[NS];
+            quad_to(v, h[k]);
+#pragma unroll
+            for (int i = 0; i < NS; ++i)
+                if (q * NS + i < s.states) state_out[w.b * per + (int64_t)(c + k) * s.states + q * NS + i] = v[i];
+        }
     }
 }
 
@@ -362,14 +432,14 @@ __global__ void __launch_bounds__(256) scan_join_kernel(float* __restrict__ loca
 // What one block keeps in shared memory.
 template <typename T, int S, int VEC>
 struct BackSpace {
-    static constexpr int CT = BACK_THREADS / S, NP = S * NS, WARPS = BACK_THREADS / 32;
-    float4 sd[KEEP][CT];                                    // dt, dt, dt u, dt u
-    float2 sg[KEEP][CT];                                    // gy, gy
-    __align__(16) float sb[KEEP][NP], sc[KEEP][NP];
-    float sy[KEEP][CT], st[KEEP][CT], sq[KEEP][CT];         // C.h, p.B, sum p a h A
-    float red[WARPS][KEEP][2 * NP];                         // the warps' sums over channels: gB, gC
+    static constexpr int CT = BACK_THREADS / S * NC, NP = S * NS, WARPS = BACK_THREADS / 32;
+    float4 sd[TILE][CT];                                    // dt, dt, dt u, dt u
+    float2 sg[TILE][CT];                                    // gy, gy
+    __align__(16) float sb[TILE][NP], sc[TILE][NP];
+    __align__(8) float sy[TILE][CT], st[TILE][CT], sq[TILE][CT];         // C.h, p.B, sum p a h A
+    float red[WARPS][TILE][2 * NP];                         // the warps' sums over channels: gB, gC
     static constexpr int RP = BACK_THREADS / (CT / VEC), RN = BACK_THREADS / NP;
-    using Act = Feed<T, VEC, KEEP, RP, 4, BACK_THREADS>;
+    using Act = Feed<T, VEC, TILE, RP, 4, BACK_THREADS>;
     typename Act::Space room;
 };
 
@@ -388,239 +458,272 @@ __global__ void __launch_bounds__(BACK_THREADS, BACK_BLOCKS) scan_bwd_kernel(Sca
     using Act = typename Space::Act;
     constexpr int CT = Space::CT, NP = Space::NP, CP = CT / VEC, RP = Space::RP, RN = Space::RN;
     enum { DELTA, Z, GOUT, U };
-    using Bc = States<T, KEEP, RN>;
+    using Bc = States<T, TILE, RN>;
     extern __shared__ __align__(16) uint8_t raw_space[];
     Space& m = *reinterpret_cast<Space*>(raw_space);
     const Where w = where(s);
-    const int tid = threadIdx.x, q = tid % S, cl = tid / S, warp = tid / 32, lane = tid % 32;
+    const int tid = threadIdx.x, q = tid % S, cl = tid / S * NC, warp = tid / 32, lane = tid % 32;
     const int c0 = w.tile * CT, c = c0 + cl;
     const int64_t first = (int64_t)w.chunk * s.chunk;
     const int64_t end = first + s.chunk < s.length ? first + s.chunk : s.length;
     const int64_t per = (int64_t)s.channels * s.states;
     const int64_t at = w.b * s.chunks + w.chunk;
-    const bool mine = c < s.channels;
-    const Quad a2 = load_states(mine ? in.A + (int64_t)c * s.states : nullptr, q * NS, s.states, LOG2_E);
-    Quad p = load_states(ENDS || !mine ? nullptr                                     // the adjoint state, from behind
-                         : enter       ? enter + at * per + (int64_t)c * s.states
-                         : gstate_out  ? gstate_out + w.b * per + (int64_t)c * s.states
-                                       : nullptr,
-                         q * NS, s.states, 1.f);
-    Quad ga = {0, 0};
+    Quad a2[NC], p[NC], ga[NC];                  // p: the adjoint state, from behind
+#pragma unroll
+    for (int k = 0; k < NC; ++k) {
+        const int64_t cn = (int64_t)(c + k) * s.states;
+        const bool mine = c + k < s.channels;
+        a2[k] = load_states(mine ? in.A + cn : nullptr, q * NS, s.states, LOG2_E);
+        p[k] = load_states(ENDS || !mine ? nullptr : enter ? enter + at * per + cn : gstate_out ? gstate_out + w.b * per + cn : nullptr, q * NS,
+                           s.states, 1.f);
+        ga[k] = {0, 0};
+    }
     const int col = tid % CP * VEC, r0 = tid / CP, n = tid % NP, rn = tid / NP;
     const bool column = c0 + col < s.channels, row_n = n < s.states;
-    float bias[VEC], gd[VEC] = {}, gbias[VEC] = {};
+    float bias[VEC], dd[VEC], gd[VEC] = {}, gbias[VEC] = {};
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) bias[i] = in.bias && column ? in.bias[c0 + col + i] : 0.f;
-    const int ntiles = (int)((end - first + KEEP - 1) / KEEP);
-    const int64_t last = first + (int64_t)(ntiles - 1) * KEEP;
-    Act act(m.room);
+    for (int i = 0; i < VEC; ++i) {
+        bias[i] = in.bias && column ? in.bias[c0 + col + i] : 0.f;
+        dd[i] = in.D && column ? in.D[c0 + col + i] : 0.f;
+    }
+    const int ntiles = (int)((end - first + TILE - 1) / TILE);
+    const int64_t last = first + (int64_t)(ntiles - 1) * TILE;
+    Act act(m.room, r0, column);
     Bc bt, ct;
-    Quad h0 = {0, 0};
-    auto fetch = [&](int64_t t, int here) {
-        act.request(DELTA, in.delta + w.b * s.delta_batch + t * s.delta_node + c0, s.delta_node, r0, col, here, column);
-        if (in.z) act.request(Z, in.z + w.b * s.z_batch + t * s.z_node + c0, s.z_node, r0, col, here, column);
-        act.request(GOUT, in.gout + w.b * s.g_batch + t * s.g_node + c0, s.g_node, r0, col, here, column);
-        ct.load(in.C + w.b * s.C_batch + t * s.C_node, s.C_node, rn, n, here, row_n);
+    act.start(DELTA, in.delta + w.b * s.delta_batch + last * s.delta_node + c0, s.delta_node, col);
+    act.start(Z, in.z + w.b * s.z_batch + last * s.z_node + c0, s.z_node, col);
+    act.start(GOUT, in.gout + w.b * s.g_batch + last * s.g_node + c0, s.g_node, col);
+    act.start(U, in.u + w.b * s.u_batch + last * s.u_node + c0, s.u_node, col);
+    bt.p = in.B + w.b * s.B_batch + (last + rn) * s.B_node + n;
+    ct.p = in.C + w.b * s.C_batch + (last + rn) * s.C_node + n;
+    auto fetch = [&](int here) {
+        act.request(DELTA, s.delta_node, here, -TILE);
+        if (in.z) act.request(Z, s.z_node, here, -TILE);
+        act.request(GOUT, s.g_node, here, -TILE);
+        ct.load(s.C_node, rn, here, row_n, -TILE);
         if constexpr (!ENDS) {
-            act.request(U, in.u + w.b * s.u_batch + t * s.u_node + c0, s.u_node, r0, col, here, column);
-            bt.load(in.B + w.b * s.B_batch + t * s.B_node, s.B_node, rn, n, here, row_n);
-            if (mine) {
-                const float* hp = kept + ((w.b * s.kept_nodes + t / KEEP) * s.channels + c) * s.states;
-                if (!states_packed(s.states)) h0 = load_states(hp, q * NS, s.states, 1.f);
-                else if (q * NS < s.states) h0 = quad_at(hp + q * NS);
+            act.request(U, s.u_node, here, -TILE);
+            bt.load(s.B_node, rn, here, row_n, -TILE);
+        }
+    };
+    // the stored state before node t
+    auto stored = [&](Quad (&h)[NC], int64_t t) {
+        const float* hp = kept + ((w.b * s.kept_nodes + t / KEEP) * s.channels + c) * s.states;
+#pragma unroll
+        for (int k = 0; k < NC; ++k) {
+            h[k] = {0, 0};
+            if (c + k < s.channels) {
+                if (!states_packed(s.states)) h[k] = load_states(hp + k * s.states, q * NS, s.states, 1.f);
+                else if (q * NS < s.states) h[k] = quad_at(hp + k * s.states + q * NS);
             }
         }
     };
-    float total = 0.f;
-    if (ntiles > 0) fetch(last, (int)(end - last));
-    for (int64_t t0 = last; t0 >= first && ntiles > 0; t0 -= KEEP) {
-        const int here = (int)(end - t0 < KEEP ? end - t0 : KEEP);
+    float total[NC] = {};
+    if (ntiles > 0) fetch((int)(end - last));
+    for (int64_t t0 = last; t0 >= first && ntiles > 0; t0 -= TILE) {
+        const int here = (int)(end - t0 < TILE ? end - t0 : TILE);
+        const int top = (here - 1) / KEEP * KEEP;      // first node of the last piece that has nodes
+        Quad next[NC];                                 // the state before the piece to come
+        if constexpr (!ENDS) stored(next, t0 + top);
         act.arrive();
 #pragma unroll
         for (int k = 0; k < Act::PER; ++k) {
             const int r = r0 + k * RP;
-            if (KEEP % RP != 0 && r >= KEEP) break;
-            const Pack<T, VEC> dl = act.get(DELTA, k), z = act.get(Z, k), go = act.get(GOUT, k), u = act.get(U, k);
+            if (TILE % RP != 0 && r >= TILE) break;
+            float dt[VEC], u[VEC], z[VEC], g[VEC], gate[VEC];
+            act.get(dt, DELTA, k);
+            act.get(g, GOUT, k);
+            if constexpr (!ENDS) act.get(u, U, k);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) dt[i] += bias[i];
+            if (s.softplus) softplus_of<VEC>(dt);
+            if (in.z) {
+                act.get(z, Z, k);
+                sigmoid_of<VEC>(gate, z);
+            }
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                const bool there = r < here && column;
-                const float dt = there ? step_of(to_f32<T>(dl.v[i]) + bias[i], s.softplus) : 0.f;
-                const float du = ENDS || !there ? 0.f : dt * to_f32<T>(u.v[i]);
-                float g = to_f32<T>(go.v[i]);
-                if (in.z) {
-                    const float zv = to_f32<T>(z.v[i]);
-                    g *= zv * sigmoid_f32(zv);
-                }
-                if (!there) g = 0.f;
-                m.sd[r][col + i] = make_float4(dt, dt, du, du);
-                m.sg[r][col + i] = make_float2(g, g);
+                if (in.z) g[i] *= z[i] * gate[i];
+                float du = ENDS ? 0.f : dt[i] * u[i];
+                if (here < TILE && r >= here) dt[i] = du = g[i] = 0.f;      // past the end: nothing changes
+                m.sd[r][col + i] = make_float4(dt[i], dt[i], du, du);
+                m.sg[r][col + i] = make_float2(g[i], g[i]);
             }
         }
 #pragma unroll
         for (int k = 0; k < Bc::PER; ++k) {
-            if (KEEP % RN != 0 && rn + k * RN >= KEEP) break;
+            if (TILE % RN != 0 && rn + k * RN >= TILE) break;
             if constexpr (!ENDS) m.sb[rn + k * RN][n] = to_f32<T>(bt.v[k]);
             m.sc[rn + k * RN][n] = to_f32<T>(ct.v[k]);
         }
-        Quad hs[KEEP + 1];                         // hs[r]: the state BEFORE node r
-        hs[0] = h0;
         __syncthreads();
-        if (t0 > first) fetch(t0 - KEEP, KEEP);
+        if (t0 > first) fetch(TILE);
         if constexpr (ENDS) {
+#pragma unroll 4
+            for (int r = TILE - 1; r >= 0; --r) {
+                const Quad c4 = quad_at(&m.sc[r][q * NS]);
 #pragma unroll
-            for (int r = KEEP - 1; r >= 0; --r) {
-                const Quad d = quad_at(&m.sd[r][cl].x), c4 = quad_at(&m.sc[r][q * NS]);
-                const uint64_t g = *reinterpret_cast<const uint64_t*>(&m.sg[r][cl]);
-                float dt, same;
-                unpair(d.lo, dt, same);
-                total += dt;
-                p.lo = mul2(fma2(c4.lo, g, p.lo), exp2_pair(mul2(d.lo, a2.lo)));
-                p.hi = mul2(fma2(c4.hi, g, p.hi), exp2_pair(mul2(d.lo, a2.hi)));
+                for (int k = 0; k < NC; ++k) {
+                    const Quad d = quad_at(&m.sd[r][cl + k].x);
+                    const uint64_t g = *reinterpret_cast<const uint64_t*>(&m.sg[r][cl + k]);
+                    float dt, same;
+                    unpair(d.lo, dt, same);
+                    total[k] += dt;
+                    p[k].lo = mul2(fma2(c4.lo, g, p[k].lo), exp2_pair(mul2(d.lo, a2[k].lo)));
+                    p[k].hi = mul2(fma2(c4.hi, g, p[k].hi), exp2_pair(mul2(d.lo, a2[k].hi)));
+                }
             }
             __syncthreads();
         } else {
-        // forward through the tile
+#pragma unroll 1
+            for (int base = top; base >= 0; base -= KEEP) {
+                Quad hs[KEEP + 1][NC];                 // hs[r]: the state BEFORE node base + r
 #pragma unroll
-        for (int k0 = 0; k0 < KEEP; k0 += 4) {
-            asm volatile("" ::: "memory");
-            float y[4];
+                for (int k = 0; k < NC; ++k) hs[0][k] = next[k];
+                if (base > 0) stored(next, t0 + base - KEEP);
+                // forward through the piece
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int r = k0 + j;
-                const Quad d = quad_at(&m.sd[r][cl].x), b4 = quad_at(&m.sb[r][q * NS]), c4 = quad_at(&m.sc[r][q * NS]);
-                hs[r + 1].lo = fma2(exp2_pair(mul2(d.lo, a2.lo)), hs[r].lo, mul2(d.hi, b4.lo));
-                hs[r + 1].hi = fma2(exp2_pair(mul2(d.lo, a2.hi)), hs[r].hi, mul2(d.hi, b4.hi));
-                y[j] = sum2(fma2(c4.lo, hs[r + 1].lo, mul2(c4.hi, hs[r + 1].hi)));
-            }
-            sum_lanes<S>(y, q);
-            put_sums<S, CT>(m.sy, y, k0, cl, q);
-        }
-        // and backwards
+                for (int k0 = 0; k0 < KEEP; k0 += 4) {
+                    asm volatile("" ::: "memory");     // the loads of a group stay with it: hoisted ones would spill the states
+                    float y[4 * NC];
 #pragma unroll
-        for (int k0 = KEEP - 4; k0 >= 0; k0 -= 4) {
-            float tb[4], ta[4];
+                    for (int j = 0; j < 4; ++j) {
+                        const int r = k0 + j;
+                        const Quad b4 = quad_at(&m.sb[base + r][q * NS]), c4 = quad_at(&m.sc[base + r][q * NS]);
 #pragma unroll
-            for (int j = 3; j >= 0; --j) {
-                const int r = k0 + j;
-                asm volatile("" ::: "memory");     // the loads of a node stay with it: hoisted ones would spill the states
-                const Quad d = quad_at(&m.sd[r][cl].x), b4 = quad_at(&m.sb[r][q * NS]), c4 = quad_at(&m.sc[r][q * NS]);
-                const uint64_t g = *reinterpret_cast<const uint64_t*>(&m.sg[r][cl]);
-                float v[2 * NS];                   // shares of gB and gC of this node
-                p.lo = fma2(c4.lo, g, p.lo);
-                p.hi = fma2(c4.hi, g, p.hi);
-                unpair(mul2(p.lo, d.hi), v[0], v[1]);
-                unpair(mul2(p.hi, d.hi), v[2], v[3]);
-                unpair(mul2(hs[r + 1].lo, g), v[4], v[5]);
-                unpair(mul2(hs[r + 1].hi, g), v[6], v[7]);
-                tb[j] = sum2(fma2(p.lo, b4.lo, mul2(p.hi, b4.hi)));
-                p.lo = mul2(p.lo, exp2_pair(mul2(d.lo, a2.lo)));
-                p.hi = mul2(p.hi, exp2_pair(mul2(d.lo, a2.hi)));
-                const uint64_t ph_lo = mul2(p.lo, hs[r].lo), ph_hi = mul2(p.hi, hs[r].hi);
-                ta[j] = sum2(fma2(ph_lo, a2.lo, mul2(ph_hi, a2.hi)));
-                ga.lo = fma2(ph_lo, d.lo, ga.lo);
-                ga.hi = fma2(ph_hi, d.lo, ga.hi);
-                // sum over the warp's channels: halve the values while halving the lanes, then add
-                int from = 0;                      // first value this lane still holds
-#pragma unroll
-                for (int k = 16, left = 2 * NS; k >= S; k /= 2) {
-                    if (left > 1) {
-                        left /= 2;
-                        const bool up = lane & k;
-#pragma unroll
-                        for (int i = 0; i < left; ++i) {
-                            const float send = up ? v[i] : v[left + i];
-                            v[i] = (up ? v[left + i] : v[i]) + __shfl_xor_sync(~0u, send, k);
+                        for (int k = 0; k < NC; ++k) {
+                            const Quad d = quad_at(&m.sd[base + r][cl + k].x);
+                            hs[r + 1][k].lo = fma2(exp2_pair(mul2(d.lo, a2[k].lo)), hs[r][k].lo, mul2(d.hi, b4.lo));
+                            hs[r + 1][k].hi = fma2(exp2_pair(mul2(d.lo, a2[k].hi)), hs[r][k].hi, mul2(d.hi, b4.hi));
+                            y[NC * j + k] = sum2(fma2(c4.lo, hs[r + 1][k].lo, mul2(c4.hi, hs[r + 1][k].hi)));
                         }
-                        from += up ? left : 0;
-                    } else {
-                        v[0] += __shfl_xor_sync(~0u, v[0], k);
                     }
+                    put_sums<S, CT>(m.sy, y, base + k0, cl, q);
                 }
-                constexpr int CW = 32 / S, LEFT = CW >= 2 * NS ? 1 : 2 * NS / CW;   // values left in a lane
+                // and backwards
 #pragma unroll
-                for (int i = 0; i < LEFT; ++i) {
-                    const int k = from + i;
-                    m.red[warp][r][(k / NS) * NP + q * NS + k % NS] = v[i];
+                for (int k0 = KEEP - 4; k0 >= 0; k0 -= 4) {
+                    float tb[4 * NC], ta[4 * NC];
+#pragma unroll
+                    for (int j = 3; j >= 0; --j) {
+                        const int r = k0 + j;
+                        asm volatile("" ::: "memory");
+                        const Quad b4 = quad_at(&m.sb[base + r][q * NS]), c4 = quad_at(&m.sc[base + r][q * NS]);
+                        Quad vb, vc;                   // shares of gB and gC of this node, summed over the thread's channels
+#pragma unroll
+                        for (int k = 0; k < NC; ++k) {
+                            const Quad d = quad_at(&m.sd[base + r][cl + k].x);
+                            const uint64_t g = *reinterpret_cast<const uint64_t*>(&m.sg[base + r][cl + k]);
+                            p[k].lo = fma2(c4.lo, g, p[k].lo);
+                            p[k].hi = fma2(c4.hi, g, p[k].hi);
+                            vb.lo = k == 0 ? mul2(p[k].lo, d.hi) : fma2(p[k].lo, d.hi, vb.lo);
+                            vb.hi = k == 0 ? mul2(p[k].hi, d.hi) : fma2(p[k].hi, d.hi, vb.hi);
+                            vc.lo = k == 0 ? mul2(hs[r + 1][k].lo, g) : fma2(hs[r + 1][k].lo, g, vc.lo);
+                            vc.hi = k == 0 ? mul2(hs[r + 1][k].hi, g) : fma2(hs[r + 1][k].hi, g, vc.hi);
+                            tb[NC * j + k] = sum2(fma2(p[k].lo, b4.lo, mul2(p[k].hi, b4.hi)));
+                            p[k].lo = mul2(p[k].lo, exp2_pair(mul2(d.lo, a2[k].lo)));
+                            p[k].hi = mul2(p[k].hi, exp2_pair(mul2(d.lo, a2[k].hi)));
+                            const uint64_t ph_lo = mul2(p[k].lo, hs[r][k].lo), ph_hi = mul2(p[k].hi, hs[r][k].hi);
+                            ta[NC * j + k] = sum2(fma2(ph_lo, a2[k].lo, mul2(ph_hi, a2[k].hi)));
+                            ga[k].lo = fma2(ph_lo, d.lo, ga[k].lo);
+                            ga[k].hi = fma2(ph_hi, d.lo, ga[k].hi);
+                        }
+                        float v[2 * NS];
+                        unpair(vb.lo, v[0], v[1]);
+                        unpair(vb.hi, v[2], v[3]);
+                        unpair(vc.lo, v[4], v[5]);
+                        unpair(vc.hi, v[6], v[7]);
+                        const int from = sum_lanes<2 * NS, 16, S>(v, lane);
+#pragma unroll
+                        for (int i = 0; i < sums_left<2 * NS, 16, S>(); ++i)
+                            m.red[warp][base + r][((from + i) / NS) * NP + q * NS + (from + i) % NS] = v[i];
+                    }
+                    put_sums<S, CT>(m.st, tb, base + k0, cl, q);
+                    put_sums<S, CT>(m.sq, ta, base + k0, cl, q);
                 }
             }
-            sum_lanes<S>(tb, q);
-            put_sums<S, CT>(m.st, tb, k0, cl, q);
-            sum_lanes<S>(ta, q);
-            put_sums<S, CT>(m.sq, ta, k0, cl, q);
-        }
-        __syncthreads();
+            __syncthreads();
 #pragma unroll
-        for (int k = 0; k < Act::PER; ++k) {
-            const int r = r0 + k * RP;
-            if (r >= here || !column) continue;
-            const Pack<T, VEC> dl = act.get(DELTA, k), z = act.get(Z, k), go = act.get(GOUT, k), u = act.get(U, k);
-            float ou[VEC], od[VEC], oz[VEC];
+            for (int k = 0; k < Act::PER; ++k) {
+                const int r = r0 + k * RP;
+                if (r >= here || !column) continue;
+                float ou[VEC], od[VEC], oz[VEC], raw[VEC], slope[VEC], z[VEC], gate[VEC], go[VEC], u[VEC];
+                act.get(u, U, k);
+                if (s.softplus) {
+                    act.get(raw, DELTA, k);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const float dt = m.sd[r][col + i].x, gy = m.sg[r][col + i].x, through = m.st[r][col + i];
-                const float uv = to_f32<T>(u.v[i]);
-                const float dd = in.D ? in.D[c0 + col + i] : 0.f;
-                ou[i] = fmaf(dt, through, dd * gy);
-                float gr = fmaf(uv, through, m.sq[r][col + i] * (1.f / LOG2_E));
-                if (s.softplus) gr *= sigmoid_f32(to_f32<T>(dl.v[i]) + bias[i]);
-                od[i] = gr;
+                    for (int i = 0; i < VEC; ++i) raw[i] += bias[i];
+                    sigmoid_of<VEC>(slope, raw);
+                }
                 if (in.z) {
-                    const float zv = to_f32<T>(z.v[i]), sig = sigmoid_f32(zv);
-                    oz[i] = to_f32<T>(go.v[i]) * fmaf(dd, uv, m.sy[r][col + i]) * sig * fmaf(zv, 1.f - sig, 1.f);
+                    act.get(z, Z, k);
+                    act.get(go, GOUT, k);
+                    sigmoid_of<VEC>(gate, z);
                 }
-                gd[i] = fmaf(gy, uv, gd[i]);
-                gbias[i] += gr;
-            }
-            const int64_t o = (w.b * s.length + t0 + r) * s.channels + c0 + col;
-            store_pack<T, VEC>(gu + o, ou);
-            store_pack<T, VEC>(gdelta + o, od);
-            if (in.z) store_pack<T, VEC>(gz + o, oz);
-        }
-        for (int e = tid; e < here * 2 * NP; e += BACK_THREADS) {
-            const int r = e / (2 * NP), k = e % (2 * NP);
-            float v = 0.f;
 #pragma unroll
-            for (int i = 0; i < Space::WARPS; ++i) v += m.red[i][r][k];
-            part_bc[(((int64_t)w.tile * rows + w.b) * s.length + t0 + r) * (2 * NP) + k] = v;
-        }
-        __syncthreads();
+                for (int i = 0; i < VEC; ++i) {
+                    const float dt = m.sd[r][col + i].x, gy = m.sg[r][col + i].x, through = m.st[r][col + i];
+                    ou[i] = fmaf(dt, through, dd[i] * gy);
+                    od[i] = fmaf(u[i], through, m.sq[r][col + i] * (1.f / LOG2_E));
+                    if (s.softplus) od[i] *= slope[i];
+                    if (in.z) oz[i] = go[i] * fmaf(dd[i], u[i], m.sy[r][col + i]) * (gate[i] * fmaf(z[i], 1.f - gate[i], 1.f));
+                    gd[i] = fmaf(gy, u[i], gd[i]);
+                    gbias[i] += od[i];
+                }
+                const int64_t o = (w.b * s.length + t0 + r) * s.channels + c0 + col;
+                store_pack<T, VEC>(gu + o, ou);
+                store_pack<T, VEC>(gdelta + o, od);
+                if (in.z) store_pack<T, VEC>(gz + o, oz);
+            }
+            for (int e = tid; e < here * 2 * NP; e += BACK_THREADS) {
+                const int r = e / (2 * NP), k = e % (2 * NP);
+                float v = 0.f;
+#pragma unroll
+                for (int i = 0; i < Space::WARPS; ++i) v += m.red[i][r][k];
+                part_bc[(((int64_t)w.tile * rows + w.b) * s.length + t0 + r) * (2 * NP) + k] = v;
+            }
+            __syncthreads();
         }
     }
     if constexpr (ENDS) {
-        if (mine) {
-            store_states(local + (at * s.channels + c) * s.states, q * NS, s.states, p);
-            if (q == 0) sums[at * s.channels + c] = total;
+#pragma unroll
+        for (int k = 0; k < NC; ++k) {
+            if (c + k >= s.channels) continue;
+            store_states(local + (at * s.channels + c + k) * s.states, q * NS, s.states, p[k]);
+            if (q == 0) sums[at * s.channels + c + k] = total[k];
         }
     } else {
-    // this chunk's share of the parameters' gradients
-    float* pa = part_a + (at * s.channels) * (int64_t)(s.states + 2);
-    if (mine) {
-        float v[NS], e[NS];
-        quad_to(v, ga);
-        quad_to(e, p);
+        // this chunk's share of the parameters' gradients
+        float* pa = part_a + (at * s.channels) * (int64_t)(s.states + 2);
 #pragma unroll
-        for (int i = 0; i < NS; ++i)
-            if (q * NS + i < s.states) {
-                pa[(int64_t)c * (s.states + 2) + q * NS + i] = v[i];
-                if (gstate != nullptr && w.chunk == 0) gstate[w.b * per + (int64_t)c * s.states + q * NS + i] = e[i];
-            }
-    }
-    // threads tid, tid + CP, ... hold sums of the same channels
-    float(*fin)[BACK_THREADS] = reinterpret_cast<float(*)[BACK_THREADS]>(raw_space);     // 2 VEC rows
-    static_assert(sizeof(m.sd) >= 2 * VEC * BACK_THREADS * sizeof(float), "room for the sums of every thread");
-    __syncthreads();
+        for (int k = 0; k < NC; ++k) {
+            if (c + k >= s.channels) continue;
+            float v[NS], e[NS];
+            quad_to(v, ga[k]);
+            quad_to(e, p[k]);
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-        fin[i][tid] = gd[i];
-        fin[VEC + i][tid] = gbias[i];
-    }
-    __syncthreads();
-    if (tid < CT && c0 + tid < s.channels) {
-        float v0 = 0.f, v1 = 0.f;
-        for (int e = tid / VEC; e < BACK_THREADS; e += CP) { v0 += fin[tid % VEC][e]; v1 += fin[VEC + tid % VEC][e]; }
-        pa[(int64_t)(c0 + tid) * (s.states + 2) + s.states] = v0;
-        pa[(int64_t)(c0 + tid) * (s.states + 2) + s.states + 1] = v1;
-    }
+            for (int i = 0; i < NS; ++i)
+                if (q * NS + i < s.states) {
+                    pa[(int64_t)(c + k) * (s.states + 2) + q * NS + i] = v[i];
+                    if (gstate != nullptr && w.chunk == 0) gstate[w.b * per + (int64_t)(c + k) * s.states + q * NS + i] = e[i];
+                }
+        }
+        // threads tid, tid + CP, ... hold sums of the same channels
+        float(*fin)[BACK_THREADS] = reinterpret_cast<float(*)[BACK_THREADS]>(raw_space);     // 2 VEC rows
+        static_assert(sizeof(m.sd) >= 2 * VEC * BACK_THREADS * sizeof(float), "room for the sums of every thread");
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            fin[i][tid] = gd[i];
+            fin[VEC + i][tid] = gbias[i];
+        }
+        __syncthreads();
+        if (tid < CT && c0 + tid < s.channels) {
+            float v0 = 0.f, v1 = 0.f;
+            for (int e = tid / VEC; e < BACK_THREADS; e += CP) { v0 += fin[tid % VEC][e]; v1 += fin[VEC + tid % VEC][e]; }
+            pa[(int64_t)(c0 + tid) * (s.states + 2) + s.states] = v0;
+            pa[(int64_t)(c0 + tid) * (s.states + 2) + s.states + 1] = v1;
+        }
     }
 }
 
@@ -668,10 +771,10 @@ __global__ void __launch_bounds__(256) scan_sum_a_kernel(const float* __restrict
 // ---------------------------------------------------------------------------------------- one node
 // S lanes share a channel, four states each; state_out may be state.
 template <typename T, int S>
-__global__ void __launch_bounds__(THREADS) scan_step_kernel(ScanIn<T> in, const float* state, T* __restrict__ out, float* state_out,
+__global__ void __launch_bounds__(STEP_THREADS) scan_step_kernel(ScanIn<T> in, const float* state, T* __restrict__ out, float* state_out,
                                                             int64_t rows, ScanShape s) {
     pdl_wait_then_trigger();
-    const int64_t e = ((int64_t)blockIdx.x * THREADS + threadIdx.x) / S;
+    const int64_t e = ((int64_t)blockIdx.x * STEP_THREADS + threadIdx.x) / S;
     const int q = threadIdx.x % S;
     const bool there = e < rows * s.channels;
     const int64_t b = there ? e / s.channels : 0;
@@ -713,7 +816,7 @@ int lanes_of(int states) {
 
 // The plan depends on sizes only, so that the forward and the backward call agree on it.
 ScanShape plan(const fpde_scan_args* a, bool backward) {
-    const int threads = backward ? BACK_THREADS : THREADS;
+
     ScanShape s = {};
     s.length = a->length;
     s.u_batch = a->u_batch; s.u_node = a->u_node;
@@ -725,14 +828,14 @@ ScanShape plan(const fpde_scan_args* a, bool backward) {
     s.channels = (int)a->channels;
     s.states = a->states;
     s.softplus = a->softplus;
-    s.tiles = (int)ceil_div(a->channels, threads / lanes_of(a->states));
+    s.tiles = (int)ceil_div(a->channels, (backward ? BACK_THREADS : FWD_THREADS) / lanes_of(a->states) * NC);
     s.kept_nodes = ceil_div(a->length, KEEP);
     // Chunks.  A march takes its nodes times the blocks that an SM has to run, over the number that run at
     // full speed together (FULL: beyond it they share the special function units or the issue slots).
     // Splitting adds the pass that forms the chunks' ends, a share ENDS_COST of the march, and two launches,
     // worth about 80 nodes.  The cheapest number of chunks wins; the fewest of equals.
     const int64_t length = a->length > 0 ? a->length : 1, blocks = a->batch * s.tiles;
-    const double full = backward ? 2 : 4, ends_cost = backward ? 0.3 : 0.5;
+    const double full = backward ? 3 : 3, ends_cost = backward ? 0.3 : 0.5;
     const int64_t most = ceil_div(length, 2 * TILE) < 1024 ? ceil_div(length, 2 * TILE) : 1024;
     int64_t chunk = length;
     double best = 0;
@@ -825,12 +928,16 @@ cudaError_t run_fwd(const fpde_scan_args* a, cudaStream_t st) {
     if (s.chunks > 1) {
         local = (float*)((char*)a->workspace + w.local);
         float* sums = (float*)((char*)a->workspace + w.sums);
-        FPDE_TRY(launch_kernel(scan_fwd_kernel<T, S, VEC, true>, grid, dim3(THREADS), st, in, (const float*)nullptr, (const float*)nullptr,
+        constexpr size_t bytes = sizeof(FwdSpace<T, S, VEC, true>);
+        FPDE_TRY(cudaFuncSetAttribute(scan_fwd_kernel<T, S, VEC, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+        FPDE_TRY(launch_kernel_smem(scan_fwd_kernel<T, S, VEC, true>, grid, dim3(FWD_THREADS), bytes, st, in, (const float*)nullptr, (const float*)nullptr,
                                (T*)nullptr, (float*)nullptr, (float*)nullptr, local, sums, s));
         FPDE_TRY(launch_kernel(scan_join_kernel<false>, dim3((unsigned)ceil_div(a->batch * s.channels * s.states, 256)), dim3(256), st,
                                local, (const float*)sums, a->A, a->state, a->batch, s));
     }
-    return launch_kernel(scan_fwd_kernel<T, S, VEC, false>, grid, dim3(THREADS), st, in, a->state, (const float*)local, (T*)a->out,
+    constexpr size_t bytes = sizeof(FwdSpace<T, S, VEC, false>);
+    FPDE_TRY(cudaFuncSetAttribute(scan_fwd_kernel<T, S, VEC, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    return launch_kernel_smem(scan_fwd_kernel<T, S, VEC, false>, grid, dim3(FWD_THREADS), bytes, st, in, a->state, (const float*)local, (T*)a->out,
                          a->state_out, (float*)a->kept, (float*)nullptr, (float*)nullptr, s);
 }
 
@@ -869,9 +976,9 @@ cudaError_t run_bwd(const fpde_scan_args* a, cudaStream_t st) {
 template <typename T, int S>
 cudaError_t run_step(const fpde_scan_args* a, cudaStream_t st) {
     const ScanShape s = plan(a, false);
-    const int64_t blocks = ceil_div(a->batch * s.channels * S, THREADS);
+    const int64_t blocks = ceil_div(a->batch * s.channels * S, STEP_THREADS);
     if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
-    return launch_kernel(scan_step_kernel<T, S>, dim3((unsigned)blocks), dim3(THREADS), st, inputs<T>(a), a->state, (T*)a->out, a->state_out,
+    return launch_kernel(scan_step_kernel<T, S>, dim3((unsigned)blocks), dim3(STEP_THREADS), st, inputs<T>(a), a->state, (T*)a->out, a->state_out,
                          a->batch, s);
 }
 
