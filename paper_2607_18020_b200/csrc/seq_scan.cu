@@ -27,12 +27,13 @@
 namespace fpde {
 namespace {
 
-constexpr int FWD_THREADS = 128, BACK_THREADS = 128, STEP_THREADS = 128;
-constexpr int FWD_UNROLL = 2;
+constexpr int FWD_THREADS = 64, BACK_THREADS = 128, STEP_THREADS = 128;
+constexpr int FWD_UNROLL = 4;
+constexpr double FWD_FULL = 8, BACK_FULL = 3;    // blocks of an SM that run at full speed together
 constexpr int TILE = 16;          // nodes brought to shared memory together
 constexpr int KEEP = 8;           // nodes between stored states: what the backward march holds in registers
 constexpr int NS = 4, NC = 2;     // states and channels of a thread
-constexpr int FWD_BLOCKS = 5, BACK_BLOCKS = 2;     // resident blocks that the registers are budgeted for
+constexpr int FWD_BLOCKS = 7, BACK_BLOCKS = 2;     // resident blocks that the registers are budgeted for
 
 struct ScanShape {
     int64_t length;
@@ -205,6 +206,21 @@ __device__ __forceinline__ Quad quad_at(const float* p) { return *reinterpret_ca
 __device__ __forceinline__ Quad quad_of(const float (&v)[NS]) { return {pair(v[0], v[1]), pair(v[2], v[3])}; }
 __device__ __forceinline__ void quad_to(float (&v)[NS], const Quad& q) { unpair(q.lo, v[0], v[1]); unpair(q.hi, v[2], v[3]); }
 
+// v[i], v[i] side by side for each channel of the thread.
+template <int N>
+__device__ __forceinline__ void put_twice(float2* at, const float (&v)[N]) {
+    if constexpr (N == 2) *reinterpret_cast<float4*>(at) = make_float4(v[0], v[0], v[1], v[1]);
+    else *at = make_float2(v[0], v[0]);
+}
+
+// The pairs of the thread's channels.
+__device__ __forceinline__ void get_channels(uint64_t (&v)[NC], const float2* at) {
+    static_assert(NC == 2, "read as one quad");
+    const Quad q = quad_at(&at->x);
+    v[0] = q.lo;
+    v[1] = q.hi;
+}
+
 // Four states from memory, or what stands in for those that do not exist.
 __device__ __forceinline__ Quad load_states(const float* p, int n, int states, float scale) {
     float v[NS];
@@ -231,7 +247,7 @@ struct FwdSpace {
     static constexpr int CT = FWD_THREADS / S * NC, NP = S * NS;
     static constexpr int RP = FWD_THREADS / (CT / VEC), RN = FWD_THREADS / NP;      // rows at a time
     using Act = Feed<T, VEC, TILE, RP, ENDS ? 2 : 3, FWD_THREADS>;
-    float4 sd[TILE][CT];              // dt, dt, dt u, dt u
+    __align__(16) float2 sdt[TILE][CT], sdu[TILE][CT];      // dt, dt;  dt u, dt u: pairs as the arithmetic wants them
     __align__(16) float sb[TILE][NP], sc[ENDS ? 1 : TILE][NP];
     __align__(8) float sy[ENDS ? 1 : TILE][CT];
     typename Act::Space room;
@@ -311,8 +327,9 @@ __global__ void __launch_bounds__(FWD_THREADS, FWD_BLOCKS) scan_fwd_kernel(ScanI
             for (int i = 0; i < VEC; ++i) {
                 u[i] *= dt[i];
                 if (left < TILE && r >= left) dt[i] = u[i] = 0.f;      // past the end: the state stays
-                m.sd[r][col + i] = make_float4(dt[i], dt[i], u[i], u[i]);
             }
+            put_twice<VEC>(&m.sdt[r][col], dt);
+            put_twice<VEC>(&m.sdu[r][col], u);
         }
 #pragma unroll
         for (int k = 0; k < Bc::PER; ++k) {
@@ -337,14 +354,16 @@ __global__ void __launch_bounds__(FWD_THREADS, FWD_BLOCKS) scan_fwd_kernel(ScanI
                 const Quad b4 = quad_at(&m.sb[k0 + r][q * NS]);
                 Quad c4;
                 if constexpr (!ENDS) c4 = quad_at(&m.sc[k0 + r][q * NS]);
+                uint64_t dt2[NC], du2[NC];
+                get_channels(dt2, &m.sdt[k0 + r][cl]);
+                get_channels(du2, &m.sdu[k0 + r][cl]);
 #pragma unroll
                 for (int k = 0; k < NC; ++k) {
-                    const Quad d = quad_at(&m.sd[k0 + r][cl + k].x);
-                    h[k].lo = fma2(exp2_pair(mul2(d.lo, a2[k].lo)), h[k].lo, mul2(d.hi, b4.lo));
-                    h[k].hi = fma2(exp2_pair(mul2(d.lo, a2[k].hi)), h[k].hi, mul2(d.hi, b4.hi));
+                    h[k].lo = fma2(exp2_pair(mul2(dt2[k], a2[k].lo)), h[k].lo, mul2(du2[k], b4.lo));
+                    h[k].hi = fma2(exp2_pair(mul2(dt2[k], a2[k].hi)), h[k].hi, mul2(du2[k], b4.hi));
                     if constexpr (ENDS) {
                         float dt, same;
-                        unpair(d.lo, dt, same);
+                        unpair(dt2[k], dt, same);
                         total[k] += dt;
                     } else {
                         y[NC * r + k] = sum2(fma2(c4.lo, h[k].lo, mul2(c4.hi, h[k].hi)));
@@ -433,8 +452,7 @@ __global__ void __launch_bounds__(256) scan_join_kernel(float* __restrict__ loca
 template <typename T, int S, int VEC>
 struct BackSpace {
     static constexpr int CT = BACK_THREADS / S * NC, NP = S * NS, WARPS = BACK_THREADS / 32;
-    float4 sd[TILE][CT];                                    // dt, dt, dt u, dt u
-    float2 sg[TILE][CT];                                    // gy, gy
+    __align__(16) float2 sdt[TILE][CT], sdu[TILE][CT], sg[TILE][CT];     // dt, dt;  dt u, dt u;  gy, gy
     __align__(16) float sb[TILE][NP], sc[TILE][NP];
     __align__(8) float sy[TILE][CT], st[TILE][CT], sq[TILE][CT];         // C.h, p.B, sum p a h A
     float red[WARPS][TILE][2 * NP];                         // the warps' sums over channels: gB, gC
@@ -544,11 +562,12 @@ __global__ void __launch_bounds__(BACK_THREADS, BACK_BLOCKS) scan_bwd_kernel(Sca
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
                 if (in.z) g[i] *= z[i] * gate[i];
-                float du = ENDS ? 0.f : dt[i] * u[i];
-                if (here < TILE && r >= here) dt[i] = du = g[i] = 0.f;      // past the end: nothing changes
-                m.sd[r][col + i] = make_float4(dt[i], dt[i], du, du);
-                m.sg[r][col + i] = make_float2(g[i], g[i]);
+                u[i] = ENDS ? 0.f : dt[i] * u[i];
+                if (here < TILE && r >= here) dt[i] = u[i] = g[i] = 0.f;      // past the end: nothing changes
             }
+            put_twice<VEC>(&m.sdt[r][col], dt);
+            put_twice<VEC>(&m.sg[r][col], g);
+            if constexpr (!ENDS) put_twice<VEC>(&m.sdu[r][col], u);
         }
 #pragma unroll
         for (int k = 0; k < Bc::PER; ++k) {
@@ -562,15 +581,16 @@ __global__ void __launch_bounds__(BACK_THREADS, BACK_BLOCKS) scan_bwd_kernel(Sca
 #pragma unroll 4
             for (int r = TILE - 1; r >= 0; --r) {
                 const Quad c4 = quad_at(&m.sc[r][q * NS]);
+                uint64_t dt2[NC], g2[NC];
+                get_channels(dt2, &m.sdt[r][cl]);
+                get_channels(g2, &m.sg[r][cl]);
 #pragma unroll
                 for (int k = 0; k < NC; ++k) {
-                    const Quad d = quad_at(&m.sd[r][cl + k].x);
-                    const uint64_t g = *reinterpret_cast<const uint64_t*>(&m.sg[r][cl + k]);
                     float dt, same;
-                    unpair(d.lo, dt, same);
+                    unpair(dt2[k], dt, same);
                     total[k] += dt;
-                    p[k].lo = mul2(fma2(c4.lo, g, p[k].lo), exp2_pair(mul2(d.lo, a2[k].lo)));
-                    p[k].hi = mul2(fma2(c4.hi, g, p[k].hi), exp2_pair(mul2(d.lo, a2[k].hi)));
+                    p[k].lo = mul2(fma2(c4.lo, g2[k], p[k].lo), exp2_pair(mul2(dt2[k], a2[k].lo)));
+                    p[k].hi = mul2(fma2(c4.hi, g2[k], p[k].hi), exp2_pair(mul2(dt2[k], a2[k].hi)));
                 }
             }
             __syncthreads();
@@ -590,11 +610,13 @@ __global__ void __launch_bounds__(BACK_THREADS, BACK_BLOCKS) scan_bwd_kernel(Sca
                     for (int j = 0; j < 4; ++j) {
                         const int r = k0 + j;
                         const Quad b4 = quad_at(&m.sb[base + r][q * NS]), c4 = quad_at(&m.sc[base + r][q * NS]);
+                        uint64_t dt2[NC], du2[NC];
+                        get_channels(dt2, &m.sdt[base + r][cl]);
+                        get_channels(du2, &m.sdu[base + r][cl]);
 #pragma unroll
                         for (int k = 0; k < NC; ++k) {
-                            const Quad d = quad_at(&m.sd[base + r][cl + k].x);
-                            hs[r + 1][k].lo = fma2(exp2_pair(mul2(d.lo, a2[k].lo)), hs[r][k].lo, mul2(d.hi, b4.lo));
-                            hs[r + 1][k].hi = fma2(exp2_pair(mul2(d.lo, a2[k].hi)), hs[r][k].hi, mul2(d.hi, b4.hi));
+                            hs[r + 1][k].lo = fma2(exp2_pair(mul2(dt2[k], a2[k].lo)), hs[r][k].lo, mul2(du2[k], b4.lo));
+                            hs[r + 1][k].hi = fma2(exp2_pair(mul2(dt2[k], a2[k].hi)), hs[r][k].hi, mul2(du2[k], b4.hi));
                             y[NC * j + k] = sum2(fma2(c4.lo, hs[r + 1][k].lo, mul2(c4.hi, hs[r + 1][k].hi)));
                         }
                     }
@@ -609,24 +631,27 @@ __global__ void __launch_bounds__(BACK_THREADS, BACK_BLOCKS) scan_bwd_kernel(Sca
                         const int r = k0 + j;
                         asm volatile("" ::: "memory");
                         const Quad b4 = quad_at(&m.sb[base + r][q * NS]), c4 = quad_at(&m.sc[base + r][q * NS]);
+                        uint64_t dt2[NC], du2[NC], g2[NC];
+                        get_channels(dt2, &m.sdt[base + r][cl]);
+                        get_channels(du2, &m.sdu[base + r][cl]);
+                        get_channels(g2, &m.sg[base + r][cl]);
                         Quad vb, vc;                   // shares of gB and gC of this node, summed over the thread's channels
 #pragma unroll
                         for (int k = 0; k < NC; ++k) {
-                            const Quad d = quad_at(&m.sd[base + r][cl + k].x);
-                            const uint64_t g = *reinterpret_cast<const uint64_t*>(&m.sg[base + r][cl + k]);
+                            const uint64_t g = g2[k], dt = dt2[k], du = du2[k];
                             p[k].lo = fma2(c4.lo, g, p[k].lo);
                             p[k].hi = fma2(c4.hi, g, p[k].hi);
-                            vb.lo = k == 0 ? mul2(p[k].lo, d.hi) : fma2(p[k].lo, d.hi, vb.lo);
-                            vb.hi = k == 0 ? mul2(p[k].hi, d.hi) : fma2(p[k].hi, d.hi, vb.hi);
+                            vb.lo = k == 0 ? mul2(p[k].lo, du) : fma2(p[k].lo, du, vb.lo);
+                            vb.hi = k == 0 ? mul2(p[k].hi, du) : fma2(p[k].hi, du, vb.hi);
                             vc.lo = k == 0 ? mul2(hs[r + 1][k].lo, g) : fma2(hs[r + 1][k].lo, g, vc.lo);
                             vc.hi = k == 0 ? mul2(hs[r + 1][k].hi, g) : fma2(hs[r + 1][k].hi, g, vc.hi);
                             tb[NC * j + k] = sum2(fma2(p[k].lo, b4.lo, mul2(p[k].hi, b4.hi)));
-                            p[k].lo = mul2(p[k].lo, exp2_pair(mul2(d.lo, a2[k].lo)));
-                            p[k].hi = mul2(p[k].hi, exp2_pair(mul2(d.lo, a2[k].hi)));
+                            p[k].lo = mul2(p[k].lo, exp2_pair(mul2(dt, a2[k].lo)));
+                            p[k].hi = mul2(p[k].hi, exp2_pair(mul2(dt, a2[k].hi)));
                             const uint64_t ph_lo = mul2(p[k].lo, hs[r][k].lo), ph_hi = mul2(p[k].hi, hs[r][k].hi);
                             ta[NC * j + k] = sum2(fma2(ph_lo, a2[k].lo, mul2(ph_hi, a2[k].hi)));
-                            ga[k].lo = fma2(ph_lo, d.lo, ga[k].lo);
-                            ga[k].hi = fma2(ph_hi, d.lo, ga[k].hi);
+                            ga[k].lo = fma2(ph_lo, dt, ga[k].lo);
+                            ga[k].hi = fma2(ph_hi, dt, ga[k].hi);
                         }
                         float v[2 * NS];
                         unpair(vb.lo, v[0], v[1]);
@@ -662,7 +687,7 @@ __global__ void __launch_bounds__(BACK_THREADS, BACK_BLOCKS) scan_bwd_kernel(Sca
                 }
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
-                    const float dt = m.sd[r][col + i].x, gy = m.sg[r][col + i].x, through = m.st[r][col + i];
+                    const float dt = m.sdt[r][col + i].x, gy = m.sg[r][col + i].x, through = m.st[r][col + i];
                     ou[i] = fmaf(dt, through, dd[i] * gy);
                     od[i] = fmaf(u[i], through, m.sq[r][col + i] * (1.f / LOG2_E));
                     if (s.softplus) od[i] *= slope[i];
@@ -710,7 +735,7 @@ __global__ void __launch_bounds__(BACK_THREADS, BACK_BLOCKS) scan_bwd_kernel(Sca
         }
         // threads tid, tid + CP, ... hold sums of the same channels
         float(*fin)[BACK_THREADS] = reinterpret_cast<float(*)[BACK_THREADS]>(raw_space);     // 2 VEC rows
-        static_assert(sizeof(m.sd) >= 2 * VEC * BACK_THREADS * sizeof(float), "room for the sums of every thread");
+        static_assert(2 * sizeof(m.sdt) >= 2 * VEC * BACK_THREADS * sizeof(float), "room for the sums of every thread");
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
@@ -835,7 +860,7 @@ ScanShape plan(const fpde_scan_args* a, bool backward) {
     // Splitting adds the pass that forms the chunks' ends, a share ENDS_COST of the march, and two launches,
     // worth about 80 nodes.  The cheapest number of chunks wins; the fewest of equals.
     const int64_t length = a->length > 0 ? a->length : 1, blocks = a->batch * s.tiles;
-    const double full = backward ? 3 : 3, ends_cost = backward ? 0.3 : 0.5;
+    const double full = backward ? BACK_FULL : FWD_FULL, ends_cost = backward ? 0.3 : 0.5;
     const int64_t most = ceil_div(length, 2 * TILE) < 1024 ? ceil_div(length, 2 * TILE) : 1024;
     int64_t chunk = length;
     double best = 0;
