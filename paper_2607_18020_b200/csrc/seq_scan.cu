@@ -29,11 +29,10 @@ namespace {
 
 constexpr int FWD_THREADS = 64, BACK_THREADS = 128, STEP_THREADS = 128;
 constexpr int FWD_UNROLL = 4;
-constexpr double FWD_FULL = 8, BACK_FULL = 3;    // blocks of an SM that run at full speed together
 constexpr int TILE = 16;          // nodes brought to shared memory together
 constexpr int KEEP = 8;           // nodes between stored states: what the backward march holds in registers
 constexpr int NS = 4, NC = 2;     // states and channels of a thread
-constexpr int FWD_BLOCKS = 7, BACK_BLOCKS = 2;     // resident blocks that the registers are budgeted for
+constexpr int FWD_BLOCKS = 7, BACK_BLOCKS = 3;     // resident blocks that the registers are budgeted for
 
 struct ScanShape {
     int64_t length;
@@ -855,21 +854,22 @@ ScanShape plan(const fpde_scan_args* a, bool backward) {
     s.softplus = a->softplus;
     s.tiles = (int)ceil_div(a->channels, (backward ? BACK_THREADS : FWD_THREADS) / lanes_of(a->states) * NC);
     s.kept_nodes = ceil_div(a->length, KEEP);
-    // Chunks.  A march takes its nodes times the blocks that an SM has to run, over the number that run at
-    // full speed together (FULL: beyond it they share the special function units or the issue slots).
-    // Splitting adds the pass that forms the chunks' ends, a share ENDS_COST of the march, and two launches,
-    // worth about 80 nodes.  The cheapest number of chunks wins; the fewest of equals.
+    // Chunks.  The blocks run in waves of `resident` per SM, and a wave takes as long as its nodes: the marches
+    // are bound by latency, so fewer blocks on an SM are hardly faster.  Splitting adds the pass that forms
+    // the chunks' ends, a share `ends_cost` of the march, and two launches, worth about 80 nodes.  The
+    // cheapest number of chunks wins, the fewest of equals.
     const int64_t length = a->length > 0 ? a->length : 1, blocks = a->batch * s.tiles;
-    const double full = backward ? BACK_FULL : FWD_FULL, ends_cost = backward ? 0.3 : 0.5;
+    const int64_t resident = 148 * (backward ? BACK_BLOCKS : FWD_BLOCKS);
+    const double ends_cost = backward ? 0.3 : 0.5;
     const int64_t most = ceil_div(length, 2 * TILE) < 1024 ? ceil_div(length, 2 * TILE) : 1024;
     int64_t chunk = length;
     double best = 0;
     for (int64_t k = 1; k <= most; ++k) {
         const int64_t nodes = k == 1 ? length : ceil_div(ceil_div(length, k), TILE) * TILE;
-        const double busy = (double)ceil_div(blocks * ceil_div(length, nodes), 148) / full;
-        const double cost = (double)nodes * (busy > 1 ? busy : 1) * (k == 1 ? 1 : 1 + ends_cost) + (k == 1 ? 0 : 80);
+        const int64_t waves = ceil_div(blocks * ceil_div(length, nodes), resident);
+        const double cost = (double)(nodes * waves) * (k == 1 ? 1 : 1 + ends_cost) + (k == 1 ? 0 : 80);
         if (k == 1 || cost < best) { best = cost; chunk = nodes; }
-        if (busy > 2) break;
+        if (waves > 4) break;
     }
     chunk = ceil_div(chunk, TILE) * TILE;
     if (chunk > (1 << 30)) chunk = 1 << 30;
