@@ -465,6 +465,7 @@ int fpde_diag_ns_tma_geometry(const int64_t* shape, int tile_rows, int narrays, 
  *     and states are dense.  Pointers need the alignment of their element type only; 16-byte
  *     aligned rows are read in wide loads.
  *   - Extents may be zero: an empty row leaves the state as it was.
+ *   - The *_bytes queries look at the type, the settings and the sizes only (0 if they are refused).
  *   - The results of a call do not depend on what else runs: no atomics, sums in a fixed order.
  * ============================================================================================== */
 

@@ -598,14 +598,42 @@ def diag_ortho_timeouts() -> int:
     return int(lib().fpde_diag_ortho_timeouts())
 
 
-def call_with(name: str, args, device):
-    """Queue entry point `name` with the argument block `args` on torch's current stream of `device`."""
+@functools.lru_cache(maxsize=None)
+def _entry(name: str):
     import torch
-    fn = getattr(lib(), name)
-    if torch.cuda.current_device() == device.index:
-        st = fn(ctypes.byref(args), torch.cuda.current_stream().cuda_stream)
+    return getattr(lib(), name), torch.cuda.current_device, torch._C._cuda_getCurrentRawStream, torch.cuda.device
+
+
+def call_with(name: str, args, device: int):
+    """Queue entry point `name` with the argument block `args` on torch's current stream of CUDA device number
+    `device`."""
+    fn, current, stream, on = _entry(name)
+    if current() == device:
+        st = fn(ctypes.byref(args), stream(device))
     else:
-        with torch.cuda.device(device):
-            st = fn(ctypes.byref(args), torch.cuda.current_stream().cuda_stream)
+        with on(device):
+            st = fn(ctypes.byref(args), stream(device))
     if st != FPDE_OK:
         raise FpdeError(st, name)
+
+
+class ArgPlans:
+    """Argument blocks without their pointers, by the sizes, strides and types of a call's tensors: checking
+    and marshalling a call costs several times what its kernels take on small tensors, and a program
+    makes the same few kinds of call over and over.  Nothing about a tensor but its layout is kept."""
+
+    def __init__(self, most=512):
+        self._most, self._plans = most, {}
+
+    @staticmethod
+    def layout(t):
+        return None if t is None else (t.dtype, t.get_device(), t.shape, t.stride())
+
+    def get(self, key):
+        plan = self._plans.get(key)
+        return None if plan is None else plan[0].from_buffer_copy(plan[1])
+
+    def keep(self, key, args):
+        if len(self._plans) >= self._most:
+            self._plans.clear()
+        self._plans[key] = (type(args), bytes(args))

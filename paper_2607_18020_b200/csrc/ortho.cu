@@ -392,7 +392,8 @@ cudaError_t launch_product(const CUtensorMap& left, const CUtensorMap& right, co
     s.per_matrix = (int)per;
     s.tiles = (int)(per * count);
     constexpr int bytes = Ring<PAIR, BN>::BYTES;
-    const cudaError_t e = cudaFuncSetAttribute(product_kernel<PAIR, BN, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    static std::atomic<uint64_t> allowed{0};
+    const cudaError_t e = allow_smem(product_kernel<PAIR, BN, KIND>, bytes, allowed);
     if (e != cudaSuccess) return e;
     return launch_kernel_smem(product_kernel<PAIR, BN, KIND>, dim3((unsigned)(s.tiles < sms ? s.tiles : sms)), dim3(PRODUCT_THREADS), bytes, st,
                               left, right, added, out, s);

@@ -7,6 +7,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/fpde.h"
 #include "fpde_common.cuh"
 #include "fpde_internal.h"
@@ -159,6 +161,19 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline bool aligned(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 inline size_t dtype_bytes(int dtype) { return dtype == FPDE_F32 ? 4 : 2; }
 inline bool dtype_ok(int dtype) { return dtype == FPDE_F32 || dtype == FPDE_BF16 || dtype == FPDE_F16; }
+
+// Allows a kernel its dynamic shared memory, once per device: `done` is the kernel's own mask of devices.
+template <typename K>
+inline cudaError_t allow_smem(K* kernel, size_t bytes, std::atomic<uint64_t>& done) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (dev < 64 && (done.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == cudaSuccess && dev < 64) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
 
 // Can rows of this array be read in packs of n elements?
 inline bool packs(const void* p, int64_t batch_stride, int64_t node_stride, size_t elem, int n) {

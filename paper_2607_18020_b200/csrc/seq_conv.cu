@@ -380,12 +380,18 @@ __global__ void __launch_bounds__(256) conv_step_kernel(const T* __restrict__ x,
     }
 }
 
-int check_conv(const fpde_conv_args* a, bool step) {
+int check_conv_sizes(const fpde_conv_args* a) {
     if (a == nullptr) return FPDE_ERR_NULL;
     if (!dtype_ok(a->dtype)) return FPDE_ERR_DTYPE;
     if (a->width < 1 || a->width > FPDE_CONV_MAX_WIDTH) return FPDE_ERR_PARAM;
     if (a->batch < 0 || a->channels < 0 || a->length < 0 || a->channels > (1 << 24) || a->length > (1ll << 40) || a->batch > (1ll << 40))
         return FPDE_ERR_SHAPE;
+    return FPDE_OK;
+}
+
+int check_conv(const fpde_conv_args* a, bool step) {
+    const int st = check_conv_sizes(a);
+    if (st != FPDE_OK) return st;
     if (a->batch * a->channels > 0) {
         const size_t e = dtype_bytes(a->dtype);
         if (a->weight == nullptr || (a->x == nullptr && (step || a->length > 0))) return FPDE_ERR_NULL;
@@ -490,7 +496,7 @@ using namespace fpde;
 extern "C" {
 
 size_t fpde_causal_conv_workspace_bytes(const fpde_conv_args* a) {
-    if (check_conv(a, false) != FPDE_OK) return 0;
+    if (check_conv_sizes(a) != FPDE_OK) return 0;
     const int64_t parts = a->batch * conv_spans(a, a->length + a->width - 1);
     return (size_t)(parts * a->channels * (a->width + 1)) * sizeof(float);
 }

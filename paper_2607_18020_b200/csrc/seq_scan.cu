@@ -878,12 +878,18 @@ ScanShape plan(const fpde_scan_args* a, bool backward) {
     return s;
 }
 
-int check_scan(const fpde_scan_args* a, bool step) {
+int check_scan_sizes(const fpde_scan_args* a) {
     if (a == nullptr) return FPDE_ERR_NULL;
     if (!dtype_ok(a->dtype)) return FPDE_ERR_DTYPE;
     if (a->states < 1 || a->states > FPDE_SCAN_MAX_STATES) return FPDE_ERR_PARAM;
     if (a->batch < 0 || a->channels < 0 || a->length < 0 || a->channels > (1 << 24) || a->length > (1ll << 36) || a->batch > (1ll << 36))
         return FPDE_ERR_SHAPE;
+    return FPDE_OK;
+}
+
+int check_scan(const fpde_scan_args* a, bool step) {
+    const int st = check_scan_sizes(a);
+    if (st != FPDE_OK) return st;
     if (a->batch * a->channels > 0) {
         if (a->A == nullptr) return FPDE_ERR_NULL;
         if ((step || a->length > 0) && (a->u == nullptr || a->delta == nullptr || a->B == nullptr || a->C == nullptr)) return FPDE_ERR_NULL;
@@ -954,14 +960,20 @@ cudaError_t run_fwd(const fpde_scan_args* a, cudaStream_t st) {
         local = (float*)((char*)a->workspace + w.local);
         float* sums = (float*)((char*)a->workspace + w.sums);
         constexpr size_t bytes = sizeof(FwdSpace<T, S, VEC, true>);
-        FPDE_TRY(cudaFuncSetAttribute(scan_fwd_kernel<T, S, VEC, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+        {
+    static std::atomic<uint64_t> allowed{0};
+    FPDE_TRY(allow_smem(scan_fwd_kernel<T, S, VEC, true>, bytes, allowed));
+    }
         FPDE_TRY(launch_kernel_smem(scan_fwd_kernel<T, S, VEC, true>, grid, dim3(FWD_THREADS), bytes, st, in, (const float*)nullptr, (const float*)nullptr,
                                (T*)nullptr, (float*)nullptr, (float*)nullptr, local, sums, s));
         FPDE_TRY(launch_kernel(scan_join_kernel<false>, dim3((unsigned)ceil_div(a->batch * s.channels * s.states, 256)), dim3(256), st,
                                local, (const float*)sums, a->A, a->state, a->batch, s));
     }
     constexpr size_t bytes = sizeof(FwdSpace<T, S, VEC, false>);
-    FPDE_TRY(cudaFuncSetAttribute(scan_fwd_kernel<T, S, VEC, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    {
+    static std::atomic<uint64_t> allowed{0};
+    FPDE_TRY(allow_smem(scan_fwd_kernel<T, S, VEC, false>, bytes, allowed));
+    }
     return launch_kernel_smem(scan_fwd_kernel<T, S, VEC, false>, grid, dim3(FWD_THREADS), bytes, st, in, a->state, (const float*)local, (T*)a->out,
                          a->state_out, (float*)a->kept, (float*)nullptr, (float*)nullptr, s);
 }
@@ -980,14 +992,20 @@ cudaError_t run_bwd(const fpde_scan_args* a, cudaStream_t st) {
     if (s.chunks > 1) {
         local = (float*)(ws + w.local);
         float* sums = (float*)(ws + w.sums);
-        FPDE_TRY(cudaFuncSetAttribute(scan_bwd_kernel<T, S, VEC, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+        {
+    static std::atomic<uint64_t> allowed{0};
+    FPDE_TRY(allow_smem(scan_bwd_kernel<T, S, VEC, true>, bytes, allowed));
+    }
         FPDE_TRY(launch_kernel_smem(scan_bwd_kernel<T, S, VEC, true>, grid, dim3(BACK_THREADS), bytes, st, in, (const float*)nullptr,
                                     (const float*)nullptr, (const float*)nullptr, (T*)nullptr, (T*)nullptr, (T*)nullptr, (float*)nullptr,
                                     (float*)nullptr, (float*)nullptr, local, sums, a->batch, s));
         FPDE_TRY(launch_kernel(scan_join_kernel<true>, dim3((unsigned)ceil_div(a->batch * s.channels * s.states, 256)), dim3(256), st,
                                local, (const float*)sums, a->A, a->gstate_out, a->batch, s));
     }
-    FPDE_TRY(cudaFuncSetAttribute(scan_bwd_kernel<T, S, VEC, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    {
+    static std::atomic<uint64_t> allowed{0};
+    FPDE_TRY(allow_smem(scan_bwd_kernel<T, S, VEC, false>, bytes, allowed));
+    }
     FPDE_TRY(launch_kernel_smem(scan_bwd_kernel<T, S, VEC, false>, grid, dim3(BACK_THREADS), bytes, st, in, (const float*)a->kept,
                                 (const float*)local, a->gstate_out, (T*)a->gu, (T*)a->gdelta, (T*)a->gz, a->gstate, part_bc, part_a,
                                 (float*)nullptr, (float*)nullptr, a->batch, s));
@@ -1047,12 +1065,12 @@ using namespace fpde;
 extern "C" {
 
 size_t fpde_selective_scan_kept_bytes(const fpde_scan_args* a) {
-    if (check_scan(a, false) != FPDE_OK) return 0;
+    if (check_scan_sizes(a) != FPDE_OK) return 0;
     return (size_t)(a->batch * ceil_div(a->length, KEEP) * a->channels * a->states) * 4;
 }
 
 size_t fpde_selective_scan_workspace_bytes(const fpde_scan_args* a, int backward) {
-    if (check_scan(a, false) != FPDE_OK) return 0;
+    if (check_scan_sizes(a) != FPDE_OK) return 0;
     return space(a, plan(a, backward != 0), backward != 0).total;
 }
 

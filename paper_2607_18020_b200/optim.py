@@ -28,26 +28,41 @@ def _matrices(name, t):
     return t.unsqueeze(0) if t.dim() == 2 else t
 
 
+_plans = B_.ArgPlans()
+_lay = _plans.layout
+
+
 def _args(grad, steps, eps):
+    """The argument block of a call without its pointers, and grad with contiguous columns."""
     g = _matrices("grad", grad)
     if g.stride(2) != 1 and g.shape[2] > 1:
         g = g.contiguous()
-    a = B_.OrthoArgs(dtype=_TYPES[g.dtype], steps=steps, count=g.shape[0], rows=g.shape[1], cols=g.shape[2], grad=g.data_ptr(),
-                     grad_matrix=g.stride(0), grad_row=g.stride(1), eps=eps)
+    a = B_.OrthoArgs(dtype=_TYPES[g.dtype], steps=steps, count=g.shape[0], rows=g.shape[1], cols=g.shape[2], grad_matrix=g.stride(0),
+                     grad_row=g.stride(1), eps=eps)
     a.workspace_bytes = B_.lib().fpde_orthogonalize_workspace_bytes(ctypes.byref(a))
-    ws = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=g.device)
-    a.workspace = ws.data_ptr()
-    return a, (g, ws)
+    return a, g
+
+
+def _plan(key, grad, steps, eps):
+    a = _plans.get(key)
+    if a is None:
+        a, g = _args(grad, steps, eps)
+        if g.data_ptr() == grad.data_ptr():     # a view at most
+            _plans.keep(key, a)
+        return a, g
+    return a, grad
 
 
 def orthogonalize(grad, steps=5, eps=1e-7):
     """grad (rows, cols), or a stack (count, rows, cols) treated matrix by matrix, with its singular values driven
     towards one: X = grad / (|grad| + eps), then `steps` times X <- a X + (b S + c S S) X with S = X X^T and
     (a, b, c) = (3.4445, -4.775, 2.0315), on the shorter side.  Returns a dense tensor of grad's type."""
-    a, keep = _args(grad, steps, eps)
-    out = torch.empty(grad.shape, dtype=grad.dtype, device=grad.device)
-    a.out = out.data_ptr()
-    B_.call_with("fpde_orthogonalize", a, grad.device)
+    a, g = _plan(("ortho", steps, eps, _lay(grad)), grad, steps, eps)
+    dev = grad.device
+    out = torch.empty(grad.shape, dtype=grad.dtype, device=dev)
+    ws = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=dev)
+    a.grad, a.out, a.workspace = g.data_ptr(), out.data_ptr(), ws.data_ptr()
+    B_.call_with("fpde_orthogonalize", a, dev.index)
     return out
 
 
@@ -59,7 +74,6 @@ def muon_step(weight, grad, momentum, lr, momentum_decay=0.95, weight_decay=0.0,
 
     where update is grad + momentum_decay * momentum (nesterov) or momentum.  weight and grad have one type,
     momentum is fp32."""
-    _matrices("weight", weight)
     if grad.shape != weight.shape or momentum.shape != weight.shape:
         raise ValueError("weight %s, grad %s and momentum %s differ in shape" % (tuple(weight.shape), tuple(grad.shape), tuple(momentum.shape)))
     if grad.dtype != weight.dtype or momentum.dtype != torch.float32:
@@ -68,11 +82,13 @@ def muon_step(weight, grad, momentum, lr, momentum_decay=0.95, weight_decay=0.0,
         raise ValueError("weight, grad and momentum live on different devices")
     if not (weight.is_contiguous() and momentum.is_contiguous()):
         raise ValueError("weight and momentum are updated in place and must be contiguous")
-    a, keep = _args(grad, steps, eps)
+    a, g = _plan(("muon", steps, eps, _lay(grad)), grad, steps, eps)
+    dev = weight.device
+    ws = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=dev)
     a.nesterov = int(nesterov)
-    a.weight, a.momentum = weight.data_ptr(), momentum.data_ptr()
+    a.grad, a.weight, a.momentum, a.workspace = g.data_ptr(), weight.data_ptr(), momentum.data_ptr(), ws.data_ptr()
     a.lr, a.momentum_decay, a.weight_decay = lr, momentum_decay, weight_decay
-    B_.call_with("fpde_muon_step", a, weight.device)
+    B_.call_with("fpde_muon_step", a, dev.index)
     torch.autograd.graph.increment_version((weight, momentum))    # they changed behind autograd's back
 
 

@@ -63,6 +63,10 @@ def _dense(name, t, shape, dtype, device):
     return t.contiguous()
 
 
+def _same(given, taken):
+    return all(a is b for a, b in zip(given, taken))
+
+
 def _first(name, t, dims):
     if t.device.type != "cuda":
         raise ValueError("%s is on %s, expected a CUDA tensor" % (name, t.device))
@@ -76,67 +80,97 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+_plans = B_.ArgPlans()
+_lay = _plans.layout
+
+
 # ------------------------------------------------------------------------------------- convolution
-def _conv_args(x, weight, bias, state, silu, step):
-    """The argument block of a convolution call, and the tensors that it points to."""
+def _conv_args(x, weight, bias, state, silu, step, gy=None, gstate=None, workspace=False):
+    """The argument block of a convolution call without its pointers, and the tensors as the call takes them:
+    checked, with contiguous channels, parameters and states dense."""
     _first("x", x, 2 if step else 3)
     dev, dt = x.device, x.dtype
     batch, channels = x.shape[0], x.shape[-1]
     if weight.dim() != 2:
         raise ValueError("weight has %d axes, expected 2 (channels, width)" % weight.dim())
     width = weight.shape[1]
+    window = (batch, width - 1, channels)
     x = _activation("x", x, x.shape, dt, dev)
     weight = _dense("weight", weight, (channels, width), torch.float32, dev)
     bias = _dense("bias", bias, (channels,), torch.float32, dev)
-    if not step:
-        state = _dense("state", state, (batch, width - 1, channels), dt, dev)
+    if step:
+        _activation("window", state, window, dt, dev)
+        if not state.is_contiguous():
+            raise ValueError("window is updated in place and must be contiguous")
+    else:
+        state = _dense("state", state, window, dt, dev)
     a = B_.ConvArgs(dtype=_TYPES[dt], width=width, silu=int(silu), batch=batch, length=1 if step else x.shape[1], channels=channels,
-                    x=x.data_ptr(), x_batch=x.stride(0), x_node=0 if step else x.stride(1),
-                    weight=weight.data_ptr(), bias=_ptr(bias), state=_ptr(state))
-    return a, (x, weight, bias, state)
+                    x_batch=x.stride(0), x_node=0 if step else x.stride(1))
+    if gy is not None:
+        gy = _activation("gy", gy, x.shape, dt, dev)
+        a.gy_batch, a.gy_node = gy.stride(0), gy.stride(1)
+    gstate = _dense("gstate", gstate, window, dt, dev)
+    if workspace:
+        a.workspace_bytes = B_.lib().fpde_causal_conv_workspace_bytes(ctypes.byref(a))
+    return a, (x, weight, bias, state, gy, gstate)
 
 
 def causal_conv_fwd(x, weight, bias=None, state=None, silu=True):
     """y[t] = act(bias + sum_j weight[:, j] x[t - width + 1 + j]) along axis 1 of x (batch, length, channels), and
     the window (batch, width - 1, channels) that the next call continues from.  Before node 0 stands `state`,
     such a window of an earlier call, or zeros.  weight: (channels, width), width 1 to 4; bias: (channels)."""
-    a, keep = _conv_args(x, weight, bias, state, silu, False)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    left = torch.empty((a.batch, a.width - 1, a.channels), dtype=x.dtype, device=x.device)
+    key = ("conv fwd", bool(silu), _lay(x), _lay(weight), _lay(bias), _lay(state))
+    a = _plans.get(key)
+    if a is None:
+        given = (x, weight, bias, state)
+        a, (x, weight, bias, state, _, _) = _conv_args(x, weight, bias, state, silu, False)
+        if _same(given, (x, weight, bias, state)):
+            _plans.keep(key, a)
+    dev = x.device
+    y = torch.empty(x.shape, dtype=x.dtype, device=dev)
+    left = torch.empty((a.batch, a.width - 1, a.channels), dtype=x.dtype, device=dev)
+    a.x, a.weight, a.bias, a.state = x.data_ptr(), weight.data_ptr(), _ptr(bias), _ptr(state)
     a.y, a.state_out = y.data_ptr(), left.data_ptr()
-    B_.call_with("fpde_causal_conv_fwd", a, x.device)
+    B_.call_with("fpde_causal_conv_fwd", a, dev.index)
     return y, left
 
 
 def causal_conv_bwd(gy, x, weight, bias=None, state=None, silu=True, gstate=None) -> ConvGrads:
     """Gradients of causal_conv_fwd for upstream gradients gy of y and `gstate` of the window it left."""
-    a, keep = _conv_args(x, weight, bias, state, silu, False)
-    dev, dt = x.device, x.dtype
-    gy = _activation("gy", gy, x.shape, dt, dev)
-    gstate = _dense("gstate", gstate, (a.batch, a.width - 1, a.channels), dt, dev)
+    key = ("conv bwd", bool(silu), _lay(gy), _lay(x), _lay(weight), _lay(bias), _lay(state), _lay(gstate))
+    a = _plans.get(key)
+    if a is None:
+        given = (x, weight, bias, state, gy, gstate)
+        a, taken = _conv_args(x, weight, bias, state, silu, False, gy, gstate, True)
+        if _same(given, taken):
+            _plans.keep(key, a)
+        x, weight, bias, state, gy, gstate = taken
+    dev, dt, f = x.device, x.dtype, torch.float32
     gx = torch.empty(x.shape, dtype=dt, device=dev)
-    gw = torch.empty((a.channels, a.width), dtype=torch.float32, device=dev)
-    gb = None if bias is None else torch.empty((a.channels,), dtype=torch.float32, device=dev)
+    gw = torch.empty((a.channels, a.width), dtype=f, device=dev)
+    gb = None if bias is None else torch.empty((a.channels,), dtype=f, device=dev)
     gs = None if state is None else torch.empty((a.batch, a.width - 1, a.channels), dtype=dt, device=dev)
-    a.gy, a.gy_batch, a.gy_node, a.gstate_out = gy.data_ptr(), gy.stride(0), gy.stride(1), _ptr(gstate)
-    a.gx, a.gstate, a.gweight, a.gbias = gx.data_ptr(), _ptr(gs), gw.data_ptr(), _ptr(gb)
-    a.workspace_bytes = B_.lib().fpde_causal_conv_workspace_bytes(ctypes.byref(a))
     ws = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=dev)
-    a.workspace = ws.data_ptr()
-    B_.call_with("fpde_causal_conv_bwd", a, dev)
+    a.x, a.weight, a.bias, a.state = x.data_ptr(), weight.data_ptr(), _ptr(bias), _ptr(state)
+    a.gy, a.gstate_out, a.gx, a.gstate = gy.data_ptr(), _ptr(gstate), gx.data_ptr(), _ptr(gs)
+    a.gweight, a.gbias, a.workspace = gw.data_ptr(), _ptr(gb), ws.data_ptr()
+    B_.call_with("fpde_causal_conv_bwd", a, dev.index)
     return ConvGrads(gx, gw, gb, gs)
 
 
 def causal_conv_step(x, window, weight, bias=None, silu=True):
     """One node per row: x (batch, channels) -> y; `window` (batch, width - 1, channels) is moved on in place."""
-    a, keep = _conv_args(x, weight, bias, None, silu, True)
-    _activation("window", window, (a.batch, a.width - 1, a.channels), x.dtype, x.device)
-    if not window.is_contiguous():
-        raise ValueError("window is updated in place and must be contiguous")
+    key = ("conv step", bool(silu), _lay(x), _lay(window), _lay(weight), _lay(bias))
+    a = _plans.get(key)
+    if a is None:
+        given = (x, weight, bias)
+        a, (x, weight, bias, _, _, _) = _conv_args(x, weight, bias, window, silu, True)
+        if _same(given, (x, weight, bias)):
+            _plans.keep(key, a)
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    a.x, a.weight, a.bias, a.y = x.data_ptr(), weight.data_ptr(), _ptr(bias), y.data_ptr()
     a.state = a.state_out = window.data_ptr()
-    a.y = y.data_ptr()
-    B_.call_with("fpde_causal_conv_step", a, x.device)
+    B_.call_with("fpde_causal_conv_step", a, x.device.index)
     return y
 
 
@@ -165,12 +199,14 @@ def causal_conv(x, weight, bias=None, state=None, silu=True, return_state=False)
 
 
 # -------------------------------------------------------------------------------------------- scan
-def _scan_args(u, delta, A, B, C, D, z, delta_bias, delta_softplus, step):
+def _scan_args(u, delta, A, B, C, D, z, delta_bias, delta_softplus, state, step, gout=None, gstate=None, keep=False, backward=False):
+    """As _conv_args, for a scan call."""
     _first("u", u, 2 if step else 3)
     dev, dt, lead, channels = u.device, u.dtype, u.shape[:-1], u.shape[-1]
     if A.dim() != 2:
         raise ValueError("A has %d axes, expected 2 (channels, states)" % A.dim())
     states = A.shape[1]
+    rest = (u.shape[0], channels, states)
     u = _activation("u", u, u.shape, dt, dev)
     delta = _activation("delta", delta, u.shape, dt, dev)
     z = None if z is None else _activation("z", z, u.shape, dt, dev)
@@ -179,17 +215,33 @@ def _scan_args(u, delta, A, B, C, D, z, delta_bias, delta_softplus, step):
     A = _dense("A", A, (channels, states), torch.float32, dev)
     D = _dense("D", D, (channels,), torch.float32, dev)
     delta_bias = _dense("delta_bias", delta_bias, (channels,), torch.float32, dev)
+    if step:
+        _activation("state", state, rest, torch.float32, dev)
+        if not state.is_contiguous():
+            raise ValueError("state is updated in place and must be contiguous")
+    else:
+        state = _dense("state", state, rest, torch.float32, dev)
     a = B_.ScanArgs(dtype=_TYPES[dt], states=states, softplus=int(delta_softplus), batch=u.shape[0], length=1 if step else u.shape[1],
-                    channels=channels, A=A.data_ptr(), D=_ptr(D), delta_bias=_ptr(delta_bias))
-    a.u, a.u_batch, a.delta, a.delta_batch = u.data_ptr(), u.stride(0), delta.data_ptr(), delta.stride(0)
-    a.B, a.B_batch, a.C, a.C_batch = B.data_ptr(), B.stride(0), C.data_ptr(), C.stride(0)
+                    channels=channels, u_batch=u.stride(0), delta_batch=delta.stride(0), B_batch=B.stride(0), C_batch=C.stride(0))
     if z is not None:
-        a.z, a.z_batch = z.data_ptr(), z.stride(0)
+        a.z_batch = z.stride(0)
     if not step:
         a.u_node, a.delta_node, a.B_node, a.C_node = u.stride(1), delta.stride(1), B.stride(1), C.stride(1)
         if z is not None:
             a.z_node = z.stride(1)
-    return a, (u, delta, A, B, C, D, z, delta_bias)
+        if gout is not None:
+            gout = _activation("gout", gout, u.shape, dt, dev)
+            a.gout_batch, a.gout_node = gout.stride(0), gout.stride(1)
+        gstate = _dense("gstate", gstate, rest, torch.float32, dev)
+        if keep:
+            a.kept_bytes = B_.lib().fpde_selective_scan_kept_bytes(ctypes.byref(a))
+        a.workspace_bytes = B_.lib().fpde_selective_scan_workspace_bytes(ctypes.byref(a), int(backward))
+    return a, (u, delta, A, B, C, D, z, delta_bias, state, gout, gstate)
+
+
+def _scan_pointers(a, u, delta, A, B, C, D, z, delta_bias, state):
+    a.u, a.delta, a.A, a.B, a.C = u.data_ptr(), delta.data_ptr(), A.data_ptr(), B.data_ptr(), C.data_ptr()
+    a.D, a.z, a.delta_bias, a.state = _ptr(D), _ptr(z), _ptr(delta_bias), _ptr(state)
 
 
 def selective_scan_fwd(u, delta, A, B, C, D=None, z=None, delta_bias=None, delta_softplus=True, state=None, keep=False):
@@ -200,23 +252,28 @@ def selective_scan_fwd(u, delta, A, B, C, D=None, z=None, delta_bias=None, delta
     with A (channels, states), B and C (batch, length, states), h[-1] = state (batch, channels, states) or zeros;
     D, z, delta_bias and the softplus may be left out.  Returns (out, the last state, what selective_scan_bwd
     needs of this pass if `keep`, else None).  1 to 64 states."""
-    a, hold = _scan_args(u, delta, A, B, C, D, z, delta_bias, delta_softplus, False)
-    dev = u.device
-    shape = (a.batch, a.channels, a.states)
-    state = _dense("state", state, shape, torch.float32, dev)
+    t = (u, delta, A, B, C, D, z, delta_bias, state)
+    key = ("scan fwd", bool(delta_softplus), bool(keep), _lay(u), _lay(delta), _lay(A), _lay(B), _lay(C), _lay(D), _lay(z), _lay(delta_bias),
+           _lay(state))
+    a = _plans.get(key)
+    if a is None:
+        a, taken = _scan_args(*t[:8], delta_softplus, state, False, keep=keep)
+        if _same(t, taken):
+            _plans.keep(key, a)
+        t = taken[:9]
+    dev, f = t[0].device, torch.float32
     out = torch.empty(u.shape, dtype=u.dtype, device=dev)
-    last = torch.empty(shape, dtype=torch.float32, device=dev)
-    a.state, a.out, a.state_out = _ptr(state), out.data_ptr(), last.data_ptr()
+    last = torch.empty((a.batch, a.channels, a.states), dtype=f, device=dev)
+    _scan_pointers(a, *t)
+    a.out, a.state_out = out.data_ptr(), last.data_ptr()
     kept = None
     if keep:
-        a.kept_bytes = B_.lib().fpde_selective_scan_kept_bytes(ctypes.byref(a))
         kept = torch.empty(a.kept_bytes, dtype=torch.uint8, device=dev)
         a.kept = kept.data_ptr()
-    a.workspace_bytes = B_.lib().fpde_selective_scan_workspace_bytes(ctypes.byref(a), 0)
     if a.workspace_bytes:
         ws = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=dev)
         a.workspace = ws.data_ptr()
-    B_.call_with("fpde_selective_scan_fwd", a, dev)
+    B_.call_with("fpde_selective_scan_fwd", a, dev.index)
     return out, last, kept
 
 
@@ -224,42 +281,50 @@ def selective_scan_bwd(gout, u, delta, A, B, C, D=None, z=None, delta_bias=None,
                        gstate=None) -> ScanGrads:
     """Gradients of selective_scan_fwd (called with keep=True: pass its `kept`) for upstream gradients gout of
     `out` and `gstate` of the last state."""
-    a, hold = _scan_args(u, delta, A, B, C, D, z, delta_bias, delta_softplus, False)
-    dev, dt, f = u.device, u.dtype, torch.float32
-    shape = (a.batch, a.channels, a.states)
-    gout = _activation("gout", gout, u.shape, dt, dev)
-    gstate = _dense("gstate", gstate, shape, f, dev)
     if kept is None:
         raise ValueError("selective_scan_bwd needs what selective_scan_fwd(..., keep=True) returned")
-    g = ScanGrads(torch.empty(u.shape, dtype=dt, device=dev), torch.empty(u.shape, dtype=dt, device=dev),
-                  torch.empty((a.channels, a.states), dtype=f, device=dev),
-                  torch.empty(B.shape, dtype=dt, device=dev), torch.empty(C.shape, dtype=dt, device=dev),
-                  None if D is None else torch.empty((a.channels,), dtype=f, device=dev),
-                  None if z is None else torch.empty(u.shape, dtype=dt, device=dev),
-                  None if delta_bias is None else torch.empty((a.channels,), dtype=f, device=dev),
-                  None if state is None else torch.empty(shape, dtype=f, device=dev))
-    a.gout, a.gout_batch, a.gout_node, a.gstate_out = gout.data_ptr(), gout.stride(0), gout.stride(1), _ptr(gstate)
+    t = (u, delta, A, B, C, D, z, delta_bias, state, gout, gstate)
+    key = ("scan bwd", bool(delta_softplus), _lay(u), _lay(delta), _lay(A), _lay(B), _lay(C), _lay(D), _lay(z), _lay(delta_bias), _lay(state),
+           _lay(gout), _lay(gstate))
+    a = _plans.get(key)
+    if a is None:
+        a, taken = _scan_args(*t[:8], delta_softplus, state, False, gout, gstate, backward=True)
+        if _same(t, taken):
+            _plans.keep(key, a)
+        t = taken
+    dev, dt, f = u.device, u.dtype, torch.float32
+    if kept.device != dev:
+        raise ValueError("kept is on %s, expected %s" % (kept.device, dev))
+
+    def new(like, dtype):
+        return None if like is None else torch.empty(like.shape, dtype=dtype, device=dev)
+    g = ScanGrads(new(u, dt), new(u, dt), new(A, f), new(B, dt), new(C, dt), new(D, f), new(z, dt), new(delta_bias, f), new(state, f))
+    _scan_pointers(a, *t[:9])
+    a.gout, a.gstate_out = t[9].data_ptr(), _ptr(t[10])
     a.gu, a.gdelta, a.gA, a.gB, a.gC = g.u.data_ptr(), g.delta.data_ptr(), g.A.data_ptr(), g.B.data_ptr(), g.C.data_ptr()
     a.gD, a.gz, a.gdelta_bias, a.gstate = _ptr(g.D), _ptr(g.z), _ptr(g.delta_bias), _ptr(g.state)
-    a.kept, a.kept_bytes = kept.data_ptr(), kept.numel()
-    a.workspace_bytes = B_.lib().fpde_selective_scan_workspace_bytes(ctypes.byref(a), 1)
+    a.kept, a.kept_bytes = kept.data_ptr(), kept.numel() * kept.element_size()
     ws = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=dev)
     a.workspace = ws.data_ptr()
-    B_.call_with("fpde_selective_scan_bwd", a, dev)
+    B_.call_with("fpde_selective_scan_bwd", a, dev.index)
     return g
 
 
 def selective_scan_step(state, u, delta, A, B, C, D=None, z=None, delta_bias=None, delta_softplus=True):
     """One node per row: u, delta, z (batch, channels), B, C (batch, states) -> out (batch, channels); `state`
     (batch, channels, states) is moved on in place."""
-    a, hold = _scan_args(u, delta, A, B, C, D, z, delta_bias, delta_softplus, True)
-    _activation("state", state, (a.batch, a.channels, a.states), torch.float32, u.device)
-    if not state.is_contiguous():
-        raise ValueError("state is updated in place and must be contiguous")
+    t = (u, delta, A, B, C, D, z, delta_bias, state)
+    key = ("scan step", bool(delta_softplus), _lay(u), _lay(delta), _lay(A), _lay(B), _lay(C), _lay(D), _lay(z), _lay(delta_bias), _lay(state))
+    a = _plans.get(key)
+    if a is None:
+        a, taken = _scan_args(*t[:8], delta_softplus, state, True)
+        if _same(t, taken):
+            _plans.keep(key, a)
+        t = taken[:9]
     out = torch.empty(u.shape, dtype=u.dtype, device=u.device)
-    a.state = a.state_out = state.data_ptr()
-    a.out = out.data_ptr()
-    B_.call_with("fpde_selective_scan_step", a, u.device)
+    _scan_pointers(a, *t)
+    a.state_out, a.out = state.data_ptr(), out.data_ptr()
+    B_.call_with("fpde_selective_scan_step", a, u.device.index)
     return out
 
 
