@@ -165,10 +165,11 @@ struct ProductShape {
 };
 
 // 64-bit description of an operand slice in shared memory, 128-byte swizzle.  K-major: rows of 64 fp16,
-// 1024 bytes per 8 rows.  MN-major: blocks of 64 columns by 64 k-rows, 8192 bytes apart; 1024 bytes per 8 k-rows.
-__device__ __forceinline__ uint64_t slice_desc(uint32_t addr, bool mn_major) {
+// 1024 bytes per 8 rows.  MN-major: blocks of 64 columns, `block` bytes apart (64 k-rows: 8192); 1024 bytes
+// per 8 k-rows.
+__device__ __forceinline__ uint64_t slice_desc(uint32_t addr, bool mn_major, uint32_t block = 8192) {
     uint64_t d = (uint64_t)((addr & 0x3ffff) >> 4);
-    d |= (uint64_t)((mn_major ? 8192 : 16) >> 4) << 16;   // leading offset (K-major, swizzled: not used)
+    d |= (uint64_t)((mn_major ? block : 16) >> 4) << 16;  // leading offset (K-major, swizzled: not used)
     d |= (uint64_t)(1024 >> 4) << 32;                     // stride offset
     d |= 1ull << 46;                                      // descriptor version of sm_100
     d |= 2ull << 61;                                      // 128-byte swizzle
@@ -317,6 +318,7 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
             tile_at<KIND, BN>(tile % s.per_matrix, s.across, i0, j0);
             const int row = i0 + quarter * 32 + lane;
             mbar_wait(done + 8 * acc, acc_phase, gave_up, &g_ortho_timeouts);
+            __syncwarp();                                  // the reads of TMEM are the whole warp's
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             __half* hi = out + 2 * k * out_plane;
             __half* lo = hi + out_plane;
@@ -399,6 +401,209 @@ cudaError_t launch_product(const CUtensorMap& left, const CUtensorMap& right, co
                               left, right, added, out, s);
 }
 
+// --------------------------------------------------------------------------------- small matrices
+// A matrix whose shorter side is at most 128 and whose longer side is at most 256 stays on one SM for the
+// whole call: X and S (then P) as swizzled hi and lo planes in shared memory, the products' sums in TMEM
+// (S in columns 0-127, S S in 128-255, P X from 256 on).  One launch instead of three per step and three
+// around them; what bounds it is the chain of 3 x steps products, each of which waits for the one before.
+// The planes of X, rows of 64-column blocks, serve as K-major factor of S and as MN-major factor of P X.
+constexpr int SMALL_M = 128, SMALL_N = 256, SMALL_THREADS = 256;
+constexpr int SMALL_BLOCK = SMALL_M * 128;              // bytes of a 64-column block of a plane
+constexpr int SMALL_S = 4 * SMALL_BLOCK;                // S: two blocks, hi and lo
+inline size_t small_bytes(int np) { return 2 * (size_t)(np / 64) * SMALL_BLOCK + SMALL_S + 1024; }
+
+// The 16 bytes of row r that hold columns c .. c+7 (c % 8 == 0), in a plane of swizzled blocks.
+__device__ __forceinline__ uint8_t* chunk_at(uint8_t* plane, int r, int c) {
+    return plane + (c / 64) * SMALL_BLOCK + r * 128 + (((c % 64 / 8) ^ (r & 7)) * 16);
+}
+__device__ __forceinline__ void put8(uint8_t* hi_plane, uint8_t* lo_plane, int r, int c, const float (&v)[8]) {
+    Pack<__half, 8> hi, lo;
+    split8(v, hi, lo);
+    *reinterpret_cast<Pack<__half, 8>*>(chunk_at(hi_plane, r, c)) = hi;
+    *reinterpret_cast<Pack<__half, 8>*>(chunk_at(lo_plane, r, c)) = lo;
+}
+__device__ __forceinline__ float value_at(uint8_t* hi_plane, uint8_t* lo_plane, int r, int c) {
+    return __half2float(*reinterpret_cast<const __half*>(chunk_at(hi_plane, r, c & ~7) + 2 * (c & 7))) +
+           __half2float(*reinterpret_cast<const __half*>(chunk_at(lo_plane, r, c & ~7) + 2 * (c & 7)));
+}
+
+template <typename T>
+__global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo io, int steps) {
+    constexpr bool PAIR = sizeof(T) == 4;
+    extern __shared__ uint8_t raw[];
+    __shared__ __align__(8) uint64_t bar;
+    __shared__ uint32_t tmem_slot;
+    __shared__ double part[8];
+    uint8_t* base = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
+    const int xplane = io.np / 64 * SMALL_BLOCK;
+    uint8_t *xh = base, *xl = base + xplane, *sh = base + 2 * xplane, *sl = sh + 2 * SMALL_BLOCK;
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    if (tid == 0) {
+        mbar_init(smem_u32(&bar), 1);
+        mbar_fence_init();
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_slot)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    pdl_wait_then_trigger();
+    const int64_t k = blockIdx.x;
+    // the update's norm (muon: after moving the momentum on), rows along the warps
+    const T* g = (const T*)io.grad + k * io.grad_matrix;
+    float* mom = io.momentum ? io.momentum + k * io.rows * io.cols : nullptr;
+    double sum = 0.0;
+    for (int r = warp; r < io.rows; r += SMALL_THREADS / 32)
+        for (int c = lane; c < io.cols; c += 32) {
+            float u = to_f32<T>(g[r * io.grad_row + c]);
+            if (mom != nullptr) {
+                const float next = fmaf(io.decay, mom[r * io.cols + c], u);
+                mom[r * io.cols + c] = next;
+                u = io.nesterov ? fmaf(io.decay, next, u) : next;
+            }
+            sum += (double)u * u;
+        }
+#pragma unroll
+    for (int m = 16; m > 0; m /= 2) sum += __shfl_xor_sync(~0u, sum, m);
+    if (lane == 0) part[warp] = sum;
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = tmem_slot;
+    sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += part[i];
+    const float scale = (float)(1.0 / (sqrt(sum) + io.eps)) * SCALE;
+    // the first X, zeros around it
+    {
+        const int i = tid % SMALL_M;
+        for (int c = tid / SMALL_M * 8; c < io.np; c += SMALL_THREADS / SMALL_M * 8) {
+            float v[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const int row = io.turned ? c + q : i, col = io.turned ? i : c + q;
+                v[q] = i < io.m && c + q < io.n ? update_at<T>(io, k, row, col) * scale : 0.f;
+            }
+            put8(xh, xl, i, c, v);
+        }
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();
+
+    const uint32_t axh = smem_u32(xh), axl = smem_u32(xl), ash = smem_u32(sh), asl = smem_u32(sl);
+    const int deep_m = (io.m + 15) / 16, deep_n = (io.n + 15) / 16;      // 16-deep pieces that are not all zeros
+    const int quarter = warp % 4, half = warp / 4, row = quarter * 32 + lane;
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    uint32_t phase = 0;
+    bool gave_up = false;
+    // D = L R^T over `deep` pieces, K-major factors as hi and lo planes
+    auto k_major = [](uint32_t plane, int piece) { return slice_desc(plane + piece / 4 * SMALL_BLOCK + piece % 4 * 32, false); };
+    auto finish = [&]() {               // the products are done, and every thread may read their sums
+        mbar_wait(smem_u32(&bar), phase, gave_up, &g_ortho_timeouts);
+        phase ^= 1;
+        __syncwarp();                   // the reads of TMEM are the whole warp's
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    };
+    auto written = [&]() {              // planes are written and sums are read: the next products may start
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncthreads();
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    };
+    constexpr uint32_t IDESC = (1u << 4) | ((uint32_t)(SMALL_M / 16) << 24);
+    for (int step = 0; step < steps; ++step) {
+        if (tid == 0) {                                                   // S = X X^T
+            for (int p = 0; p < deep_n; ++p) {
+                const uint64_t h = k_major(axh, p);
+                mma_f16(tmem, h, h, IDESC | (uint32_t)(128 / 8) << 17, p > 0);
+                if (PAIR) {
+                    const uint64_t l = k_major(axl, p);
+                    mma_f16(tmem, h, l, IDESC | (uint32_t)(128 / 8) << 17, true);
+                    mma_f16(tmem, l, h, IDESC | (uint32_t)(128 / 8) << 17, true);
+                }
+            }
+            mma_commit(smem_u32(&bar));
+        }
+        finish();
+#pragma unroll 1
+        for (int c = half * 64; c < half * 64 + 64; c += 32) {
+            float v[32];
+            tmem_load32(tmem + lanes + c, v);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                float w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = v[8 * q + i] * (1.f / SCALE);
+                put8(sh, sl, row, c + 8 * q, w);
+            }
+        }
+        written();
+        if (tid == 0) {                                                   // S S
+            for (int p = 0; p < deep_m; ++p) {
+                const uint64_t h = k_major(ash, p);
+                mma_f16(tmem + 128, h, h, IDESC | (uint32_t)(128 / 8) << 17, p > 0);
+                if (PAIR) {
+                    const uint64_t l = k_major(asl, p);
+                    mma_f16(tmem + 128, h, l, IDESC | (uint32_t)(128 / 8) << 17, true);
+                    mma_f16(tmem + 128, l, h, IDESC | (uint32_t)(128 / 8) << 17, true);
+                }
+            }
+            mma_commit(smem_u32(&bar));
+        }
+        finish();
+#pragma unroll 1
+        for (int c = half * 64; c < half * 64 + 64; c += 32) {            // P over S, which has been read
+            float v[32], w2[32];
+            tmem_load32(tmem + lanes + c, v);
+            tmem_load32(tmem + lanes + 128 + c, w2);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                float w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = fmaf(NS_C / SCALE, w2[8 * q + i], NS_B * (v[8 * q + i] * (1.f / SCALE)));
+                put8(sh, sl, row, c + 8 * q, w);
+            }
+        }
+        written();
+        if (tid == 0) {                                                   // P X
+            const uint32_t idesc = IDESC | 1u << 16 | (uint32_t)(io.np / 8) << 17;
+            for (int p = 0; p < deep_m; ++p) {
+                const uint64_t h = k_major(ash, p), r = slice_desc(axh + p * 2048, true, SMALL_BLOCK);
+                mma_f16(tmem + 256, h, r, idesc, p > 0);
+                if (PAIR) {
+                    mma_f16(tmem + 256, h, slice_desc(axl + p * 2048, true, SMALL_BLOCK), idesc, true);
+                    mma_f16(tmem + 256, k_major(asl, p), r, idesc, true);
+                }
+            }
+            mma_commit(smem_u32(&bar));
+        }
+        finish();
+#pragma unroll 1
+        for (int c = half * 32; c < io.np; c += 64) {
+            float v[32];
+            tmem_load32(tmem + lanes + 256 + c, v);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const Pack<__half, 8> h = *reinterpret_cast<const Pack<__half, 8>*>(chunk_at(xh, row, c + 8 * q));
+                const Pack<__half, 8> l = *reinterpret_cast<const Pack<__half, 8>*>(chunk_at(xl, row, c + 8 * q));
+                float w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = fmaf(NS_A, __half2float(h.v[i]) + __half2float(l.v[i]), v[8 * q + i] * (1.f / SCALE));
+                put8(xh, xl, row, c + 8 * q, w);
+            }
+        }
+        written();
+    }
+    // out, along the matrix's rows
+    T* out = (T*)io.out + k * io.rows * io.cols;
+    for (int r = warp; r < io.rows; r += SMALL_THREADS / 32)
+        for (int c = lane; c < io.cols; c += 32) {
+            const float v = (io.turned ? value_at(xh, xl, c, r) : value_at(xh, xl, r, c)) * (1.f / SCALE);
+            T* o = out + r * io.cols + c;
+            *o = from_f32<T>(mom == nullptr ? v : fmaf(-io.rate, v, io.keep * to_f32<T>(*o)));
+        }
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+
 // X back in the shape of the matrices: written out, or applied to the weights.
 template <typename T>
 __global__ void __launch_bounds__(256) ortho_finish_kernel(OrthoIo io, const __half* __restrict__ x) {
@@ -426,8 +631,10 @@ struct OrthoSpace {
     size_t sums, x[2], s, p, total;
 };
 int64_t padded(int64_t n) { return ceil_div(n, 64) * 64; }
+bool is_small(int64_t m, int64_t n) { return m <= SMALL_M && n <= SMALL_N; }
 OrthoSpace space(int64_t count, int64_t m, int64_t n) {
-    OrthoSpace w;
+    OrthoSpace w = {};
+    if (is_small(m, n)) return w;
     const int64_t mp = padded(m), np = padded(n);
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
@@ -469,6 +676,11 @@ cudaError_t run(const fpde_ortho_args* a, bool muon, cudaStream_t st) {
     io.rate = (float)(a->lr * sqrt(io.rows > io.cols ? (double)io.rows / io.cols : 1.0));
     io.eps = a->eps;
     io.mp = (int)padded(io.m); io.np = (int)padded(io.n);
+    if (is_small(io.m, io.n)) {
+        static std::atomic<uint64_t> allowed{0};
+        FPDE_TRY(allow_smem(ortho_small_kernel<T>, small_bytes(SMALL_N), allowed));
+        return launch_kernel_smem(ortho_small_kernel<T>, dim3((unsigned)a->count), dim3(SMALL_THREADS), small_bytes(io.np), st, io, a->steps);
+    }
     const OrthoSpace w = space(a->count, io.m, io.n);
     char* ws = (char*)a->workspace;
     double* sums = (double*)(ws + w.sums);
@@ -515,7 +727,8 @@ int call(const fpde_ortho_args* a, bool muon, void* stream) {
     const size_t e = dtype_bytes(a->dtype);
     if (a->grad == nullptr || (muon ? a->weight == nullptr || a->momentum == nullptr : a->out == nullptr)) return FPDE_ERR_NULL;
     if (!aligned(a->grad, e) || !aligned(a->out, e) || !aligned(a->weight, e) || !aligned(a->momentum, 4)) return FPDE_ERR_ALIGN;
-    if (a->workspace == nullptr || !aligned(a->workspace, 256) || a->workspace_bytes < fpde_orthogonalize_workspace_bytes(a))
+    const size_t need = fpde_orthogonalize_workspace_bytes(a);
+    if (need > 0 && (a->workspace == nullptr || !aligned(a->workspace, 256) || a->workspace_bytes < need))
         return FPDE_ERR_WORKSPACE;
     const cudaStream_t s = (cudaStream_t)stream;
     const cudaError_t err = a->dtype == FPDE_F32 ? run<float>(a, muon, s) : a->dtype == FPDE_BF16 ? run<__nv_bfloat16>(a, muon, s) : run<__half>(a, muon, s);
