@@ -135,31 +135,43 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(OrthoIo io, const doub
 // 2^-16.  With PAIR three products (hi hi, hi lo, lo hi) go into one fp32 accumulator: 22-bit factors.
 // Without it only hi hi is formed, and lo serves the terms a X and b S that are added in the epilogue.
 //
-// S and P are symmetric: only tiles on and below the diagonal are computed, and stored twice.
+// The cross products have an accumulator of their own: every product rounds the running sum towards zero,
+// and the large sum then sees a third of the roundings.
+//
+// S and P are symmetric: where their tiles fill the GPU, only those on and below the diagonal are
+// computed, and stored twice; where they do not, computing all of them is faster than storing twice.
 //
 // A block is persistent and has one warp that loads (TMA into a ring of 64-deep slices, 128-byte
-// swizzle), one that issues tcgen05.mma (128 x BN tiles, accumulators in TMEM) and four that turn the
-// accumulators into the next operand; two accumulators let a tile's epilogue run under the next tile's
-// products.  X enters APPLY as it is stored, rows along k: its slices are MN-major operands.
-// The planes are padded to multiples of 64 with zeros.
+// swizzle), one that issues tcgen05.mma (accumulators in TMEM, two sets, so that a tile's epilogue runs
+// under the next tile's products) and eight that turn the sums into the next operand.  X enters APPLY as
+// it is stored, rows along k: its slices are MN-major operands.  The planes are padded to multiples of
+// 64 with zeros.
+//
+// Large products run on pairs of SMs (CG = 2, cta_group::2): a tile has 256 rows, each block of the pair
+// loads its 128 rows of the left factor and half of the right one, and the first block issues for both.
+// What a block has to load per product is what bounds the one-block form (an SM takes 64 bytes a clock
+// from L2; 128 x 256 tiles need 96).
 enum Kind { GRAM, SQUARE, APPLY };
 
 constexpr int BM = 128, BK = 64;
-constexpr int PRODUCT_THREADS = 192;
+constexpr int EPILOGUE_WARPS = 8;
+constexpr int PRODUCT_THREADS = 64 + 32 * EPILOGUE_WARPS;
 
-template <bool PAIR, int BN>
+template <bool PAIR, int CG, int BN>
 struct Ring {
     static constexpr int PLANES = PAIR ? 2 : 1;
-    static constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2;
+    static constexpr int A_BYTES = BM * BK * 2, B_COLS = BN / CG, B_BYTES = B_COLS * BK * 2;    // of one block and plane
     static constexpr int STAGE = PLANES * (A_BYTES + B_BYTES);
-    static constexpr int STAGES = 196608 / STAGE;
+    static constexpr int STAGES = 196608 / STAGE > 6 ? 6 : 196608 / STAGE;
     static constexpr int BYTES = STAGES * STAGE + 1024 + 256;    // slack to start on 1024 bytes, barriers
+    static constexpr int SET = PLANES * BN;                      // TMEM columns of one set of accumulators
+    static_assert(2 * SET <= 512 && STAGES >= 2, "accumulators fit TMEM, the ring shared memory");
 };
 
 struct ProductShape {
     int mp, np;                 // padded extents of X; S and P are mp x mp
     int depth;                  // np (GRAM) or mp
-    int tiles, per_matrix, across;   // tiles in all, of one matrix, of one row of tiles (APPLY)
+    int tiles, per_matrix, across;   // tiles in all, of one matrix, of one row of tiles
     int cols;                   // columns of the result: mp or np
     float alpha, beta;          // stored = alpha acc + beta (hi + lo of the added term)
 };
@@ -176,14 +188,51 @@ __device__ __forceinline__ uint64_t slice_desc(uint32_t addr, bool mn_major, uin
     return d;
 }
 
+template <int CG = 1>
 __device__ __forceinline__ void mma_f16(uint32_t tmem, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
-        : "memory");
+    if constexpr (CG == 1)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+            : "memory");
 }
+// Arrives on the barrier when the products issued so far are done; CG = 2: on that of both blocks.
+template <int CG = 1>
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    if constexpr (CG == 1)
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+                     "h"((uint16_t)3)
+                     : "memory");
+}
+// A 64-column slice to this block's shared memory; CG = 2: its bytes count on the first block's barrier.
+template <int CG>
+__device__ __forceinline__ void load_slice(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar) {
+    if constexpr (CG == 1)
+        tma_load_3d(dst, map, c0, c1, c2, bar);
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+            "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+            : "memory");
+}
+__device__ __forceinline__ uint32_t in_first_block(uint32_t addr) {      // the same place in the pair's first block
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+    return r;
+}
+__device__ __forceinline__ void arrive_cluster(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
     uint32_t r[32];
@@ -202,45 +251,55 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
 
 __device__ unsigned int g_ortho_timeouts;
 
-// Tile number t of one matrix -> first row and column.
-template <int KIND, int BN>
+// Tile number t of one matrix -> first row and column of the tile (CG * 128 rows, BN columns).
+template <bool LOWER, int CG, int BN>
 __device__ __forceinline__ void tile_at(int t, int across, int& i0, int& j0) {
-    if (KIND == APPLY) {
-        i0 = t / across * BM;
+    if (!LOWER) {
+        i0 = t / across * (CG * BM);
         j0 = t % across * BN;
-    } else {                    // lower triangle, row by row
-        int i = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
-        while ((i + 1) * (i + 2) / 2 <= t) ++i;
-        while (i * (i + 1) / 2 > t) --i;
-        i0 = i * BM;
-        j0 = (t - i * (i + 1) / 2) * BN;
+    } else {                    // the tiles that touch the lower triangle, row by row: R (i + 1) in row i
+        constexpr int R = CG * BM / BN;
+        const int u = t / R;
+        int i = (int)((sqrtf(8.f * u + 1.f) - 1.f) * 0.5f);
+        while ((i + 1) * (i + 2) / 2 <= u) ++i;
+        while (i * (i + 1) / 2 > u) --i;
+        i0 = i * (CG * BM);
+        j0 = (t - R * (i * (i + 1) / 2)) * BN;
     }
 }
 
 // left: K-major map of X (GRAM), S (SQUARE) or P (APPLY), also the right operand of GRAM and SQUARE;
 // right: map of X in 64 x 64 boxes (APPLY).  added: planes of the term in the epilogue (S or X).
-template <bool PAIR, int BN, int KIND>
+template <bool PAIR, int CG, int BN, int KIND, bool LOWER>
 __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __grid_constant__ CUtensorMap left, const __grid_constant__ CUtensorMap right,
                                                                       const __half* __restrict__ added, __half* __restrict__ out, ProductShape s) {
-    using R = Ring<PAIR, BN>;
-    static_assert(KIND == APPLY || BN == BM, "mirrored tiles are square");
+    using R = Ring<PAIR, CG, BN>;
+    static_assert(!LOWER || CG * BM % BN == 0, "columns of tiles end where rows do");
     extern __shared__ uint8_t raw[];
     uint8_t* ring = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
     uint64_t* bars = reinterpret_cast<uint64_t*>(ring + R::STAGES * R::STAGE);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * R::STAGES + 4);
     const uint32_t full = smem_u32(bars), empty = full + 8 * R::STAGES, done = empty + 8 * R::STAGES, freed = done + 16;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int rank = CG == 2 ? (int)(blockIdx.x & 1) : 0, workers = gridDim.x / CG, worker = blockIdx.x / CG;
     if (threadIdx.x == 0) {
         for (int i = 0; i < R::STAGES; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(done + 8 * i, 1); mbar_init(freed + 8 * i, 128); }
+        for (int i = 0; i < 2; ++i) { mbar_init(done + 8 * i, 1); mbar_init(freed + 8 * i, CG * EPILOGUE_WARPS); }
         mbar_fence_init();
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(2 * BN) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        if constexpr (CG == 1) {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "n"(2 * R::SET) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "n"(2 * R::SET) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        }
     }
+    __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
+    if constexpr (CG == 2) cluster_sync();       // the other block's barriers are there
+    else __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = *tmem_slot;
     pdl_wait_then_trigger();
@@ -250,23 +309,26 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
     if (warp == 0) {
         if (lane == 0) {
             int stage = 0, phase = 0;
-            for (int tile = blockIdx.x; tile < s.tiles; tile += gridDim.x) {
+            for (int tile = worker; tile < s.tiles; tile += workers) {
                 const int k = tile / s.per_matrix;
                 int i0, j0;
-                tile_at<KIND, BN>(tile % s.per_matrix, s.across, i0, j0);
+                tile_at<LOWER, CG, BN>(tile % s.per_matrix, s.across, i0, j0);
+                i0 += rank * BM;
+                j0 += rank * R::B_COLS;
                 for (int step = 0; step < steps; ++step) {
                     mbar_wait(empty + 8 * stage, phase ^ 1, gave_up, &g_ortho_timeouts);
-                    mbar_expect_tx(full + 8 * stage, R::STAGE);
-                    const uint32_t base = smem_u32(ring + stage * R::STAGE), bar = full + 8 * stage;
+                    if (rank == 0) mbar_expect_tx(full + 8 * stage, CG * R::STAGE);
+                    const uint32_t base = smem_u32(ring + stage * R::STAGE);
+                    const uint32_t bar = CG == 2 ? in_first_block(full + 8 * stage) : full + 8 * stage;
 #pragma unroll
                     for (int p = 0; p < R::PLANES; ++p) {
-                        tma_load_3d(base + p * R::A_BYTES, &left, step * BK, i0, 2 * k + p, bar);
+                        load_slice<CG>(base + p * R::A_BYTES, &left, step * BK, i0, 2 * k + p, bar);
                         const uint32_t b = base + R::PLANES * R::A_BYTES + p * R::B_BYTES;
                         if (KIND == APPLY) {
 #pragma unroll
-                            for (int q = 0; q < BN / 64; ++q) tma_load_3d(b + q * 8192, &right, j0 + 64 * q, step * BK, 2 * k + p, bar);
+                            for (int q = 0; q < R::B_COLS / 64; ++q) load_slice<CG>(b + q * 8192, &right, j0 + 64 * q, step * BK, 2 * k + p, bar);
                         } else {
-                            tma_load_3d(b, &left, step * BK, j0, 2 * k + p, bar);
+                            load_slice<CG>(b, &right, step * BK, j0, 2 * k + p, bar);
                         }
                     }
                     if (++stage == R::STAGES) { stage = 0; phase ^= 1; }
@@ -279,14 +341,14 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
             }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            constexpr uint32_t IDESC = (1u << 4) | (KIND == APPLY ? 1u << 16 : 0u) | ((uint32_t)(BN / 8) << 17) | ((uint32_t)(BM / 16) << 24);
+        if (lane == 0 && rank == 0) {
+            constexpr uint32_t IDESC = (1u << 4) | (KIND == APPLY ? 1u << 16 : 0u) | ((uint32_t)(BN / 8) << 17) | ((uint32_t)(CG * BM / 16) << 24);
             constexpr int KB = KIND == APPLY ? 2048 : 32;      // bytes from one 16-deep piece of B to the next
             int stage = 0, phase = 0, acc = 0, acc_phase = 0;
-            for (int tile = blockIdx.x; tile < s.tiles; tile += gridDim.x) {
+            for (int tile = worker; tile < s.tiles; tile += workers) {
                 mbar_wait(freed + 8 * acc, acc_phase ^ 1, gave_up, &g_ortho_timeouts);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t d = tmem + acc * BN;
+                const uint32_t d = tmem + acc * R::SET;
                 for (int step = 0; step < steps; ++step) {
                     mbar_wait(full + 8 * stage, phase, gave_up, &g_ortho_timeouts);
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -294,81 +356,100 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
 #pragma unroll
                     for (int kk = 0; kk < BK / 16; ++kk) {
                         const uint64_t ah = slice_desc(a + kk * 32, false), bh = slice_desc(b + kk * KB, KIND == APPLY);
-                        mma_f16(d, ah, bh, IDESC, step > 0 || kk > 0);
+                        const bool add = step > 0 || kk > 0;
+                        mma_f16<CG>(d, ah, bh, IDESC, add);
                         if (PAIR) {
-                            mma_f16(d, ah, slice_desc(b + R::B_BYTES + kk * KB, KIND == APPLY), IDESC, true);
-                            mma_f16(d, slice_desc(a + R::A_BYTES + kk * 32, false), bh, IDESC, true);
+                            mma_f16<CG>(d + BN, ah, slice_desc(b + R::B_BYTES + kk * KB, KIND == APPLY), IDESC, add);
+                            mma_f16<CG>(d + BN, slice_desc(a + R::A_BYTES + kk * 32, false), bh, IDESC, true);
                         }
                     }
-                    mma_commit(empty + 8 * stage);
+                    mma_commit<CG>(empty + 8 * stage);
                     if (++stage == R::STAGES) { stage = 0; phase ^= 1; }
                 }
-                mma_commit(done + 8 * acc);
+                mma_commit<CG>(done + 8 * acc);
                 if (acc == 1) acc_phase ^= 1;
                 acc ^= 1;
             }
         }
     } else {
-        const int quarter = warp % 4;                      // TMEM lanes this warp may read
+        const int quarter = warp % 4, half = (warp - 2) / 4;          // TMEM lanes this warp may read; its half of the columns
+        const uint32_t freed_first = CG == 2 ? in_first_block(freed) : freed;
         int acc = 0, acc_phase = 0;
         const int64_t out_plane = (int64_t)s.mp * s.cols;
-        for (int tile = blockIdx.x; tile < s.tiles; tile += gridDim.x) {
+        for (int tile = worker; tile < s.tiles; tile += workers) {
             const int k = tile / s.per_matrix;
             int i0, j0;
-            tile_at<KIND, BN>(tile % s.per_matrix, s.across, i0, j0);
-            const int row = i0 + quarter * 32 + lane;
-            mbar_wait(done + 8 * acc, acc_phase, gave_up, &g_ortho_timeouts);
-            __syncwarp();                                  // the reads of TMEM are the whole warp's
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            tile_at<LOWER, CG, BN>(tile % s.per_matrix, s.across, i0, j0);
+            const bool mirror = LOWER && j0 < i0;      // tiles of the diagonal block hold both halves
+            const int row = i0 + rank * BM + quarter * 32 + lane;
             __half* hi = out + 2 * k * out_plane;
             __half* lo = hi + out_plane;
             const __half* add = KIND == GRAM ? nullptr : added + 2 * k * out_plane + (int64_t)row * s.cols;
+            mbar_wait(done + 8 * acc, acc_phase, gave_up, &g_ortho_timeouts);
+            __syncwarp();                                  // the reads of TMEM are the whole warp's
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
-            for (int c = 0; c < BN; c += 32) {
-                float v[32];
-                tmem_load32(tmem + acc * BN + c + ((uint32_t)(quarter * 32) << 16), v);
+            for (int c = half * 32; c < BN; c += 64) {
                 const int col = j0 + c;
-                if (row >= s.mp || col >= s.cols) continue;      // a warp's lanes share col; rows past the end are whole warps (mp % 64 == 0)
-                __align__(16) __half h[32], l[32];
+                const bool there = row < s.mp && col < s.cols;       // the same for the whole warp: extents are multiples of 64
+                Pack<__half, 8> ph[4] = {}, pl[4] = {};
+                if (KIND != GRAM && there) {
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    Pack<__half, 8> ph = {}, pl = {};
-                    if (KIND != GRAM) {
-                        ph = load_pack<__half, 8>(add + col + 8 * g);
-                        pl = load_pack<__half, 8>(add + out_plane + col + 8 * g);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        float w = s.alpha * v[8 * g + i];
-                        if (KIND != GRAM) w = fmaf(s.beta, __half2float(ph.v[i]) + __half2float(pl.v[i]), w);
-                        h[8 * g + i] = __float2half_rn(w);
-                        l[8 * g + i] = __float2half_rn(w - __half2float(h[8 * g + i]));
+                    for (int g = 0; g < 4; ++g) {
+                        ph[g] = load_pack<__half, 8>(add + col + 8 * g);
+                        pl[g] = load_pack<__half, 8>(add + out_plane + col + 8 * g);
                     }
                 }
+                float v[32];
+                const uint32_t at = tmem + acc * R::SET + c + ((uint32_t)(quarter * 32) << 16);
+                tmem_load32(at, v);
+                if (PAIR) {
+                    float x[32];
+                    tmem_load32(at + BN, x);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] += x[i];
+                }
+                if (!there) continue;
                 const bool both = PAIR || KIND != SQUARE;        // P is only ever a factor
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    *reinterpret_cast<uint4*>(hi + (int64_t)row * s.cols + col + 8 * g) = *reinterpret_cast<const uint4*>(h + 8 * g);
-                    if (both) *reinterpret_cast<uint4*>(lo + (int64_t)row * s.cols + col + 8 * g) = *reinterpret_cast<const uint4*>(l + 8 * g);
+                    float w[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        w[i] = s.alpha * v[8 * g + i];
+                        if (KIND != GRAM) w[i] = fmaf(s.beta, __half2float(ph[g].v[i]) + __half2float(pl[g].v[i]), w[i]);
+                    }
+                    split8(w, ph[g], pl[g]);
+                    *reinterpret_cast<Pack<__half, 8>*>(hi + (int64_t)row * s.cols + col + 8 * g) = ph[g];
+                    if (both) *reinterpret_cast<Pack<__half, 8>*>(lo + (int64_t)row * s.cols + col + 8 * g) = pl[g];
                 }
-                if (KIND != APPLY && i0 != j0) {
+                if (mirror) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
-                        hi[(int64_t)(col + i) * s.cols + row] = h[i];
-                        if (both) lo[(int64_t)(col + i) * s.cols + row] = l[i];
+                        hi[(int64_t)(col + i) * s.cols + row] = ph[i / 8].v[i % 8];
+                        if (both) lo[(int64_t)(col + i) * s.cols + row] = pl[i / 8].v[i % 8];
                     }
                 }
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            mbar_arrive(freed + 8 * acc);
+            __syncwarp();
+            if (lane == 0) {
+                if constexpr (CG == 2) arrive_cluster(freed_first + 8 * acc);
+                else mbar_arrive(freed + 8 * acc);
+            }
             if (acc == 1) acc_phase ^= 1;
             acc ^= 1;
         }
     }
+    __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
+    if constexpr (CG == 2) cluster_sync();       // nobody's barriers are needed any more
+    else __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * BN) : "memory");
+    if (warp == 1) {
+        if constexpr (CG == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(2 * R::SET) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(2 * R::SET) : "memory");
+    }
 }
 
 // Planes of a stack of r x c matrices as a 3-D tensor (columns, rows, 2 count) read in boxes of 64 columns
@@ -383,22 +464,65 @@ bool encode_planes(CUtensorMap* m, const __half* p, int64_t count, int r, int c,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool PAIR, int BN, int KIND>
-cudaError_t launch_product(const CUtensorMap& left, const CUtensorMap& right, const __half* added, __half* out, ProductShape s, int64_t count,
-                           int sms, cudaStream_t st) {
-    const int down = (int)ceil_div(s.mp, BM);
+// The maps of one operand: boxes of 128 rows, of 64 rows, and of 64 rows for MN-major slices (the same).
+struct Maps {
+    CUtensorMap tall, low;
+    bool encode(const __half* p, int64_t count, int r, int c) {
+        return encode_planes(&tall, p, count, r, c, BM) && encode_planes(&low, p, count, r, c, 64);
+    }
+};
+
+template <bool PAIR, int CG, int BN, int KIND, bool LOWER>
+cudaError_t launch_product(const Maps& left, const Maps& right, const __half* added, __half* out, ProductShape s, int64_t count, int sms,
+                           cudaStream_t st) {
+    using R = Ring<PAIR, CG, BN>;
+    const int64_t down = ceil_div(s.mp, CG * BM);
     s.across = (int)ceil_div(s.cols, BN);
     s.depth = KIND == GRAM ? s.np : s.mp;
-    const int64_t per = KIND == APPLY ? (int64_t)down * s.across : (int64_t)down * (down + 1) / 2;
+    const int64_t per = LOWER ? down * (down + 1) / 2 * (CG * BM / BN) : down * s.across;
     if (per * count > 0x3fffffff) return cudaErrorInvalidConfiguration;
     s.per_matrix = (int)per;
     s.tiles = (int)(per * count);
-    constexpr int bytes = Ring<PAIR, BN>::BYTES;
+    auto kernel = product_kernel<PAIR, CG, BN, KIND, LOWER>;
     static std::atomic<uint64_t> allowed{0};
-    const cudaError_t e = allow_smem(product_kernel<PAIR, BN, KIND>, bytes, allowed);
+    const cudaError_t e = allow_smem(kernel, R::BYTES, allowed);
     if (e != cudaSuccess) return e;
-    return launch_kernel_smem(product_kernel<PAIR, BN, KIND>, dim3((unsigned)(s.tiles < sms ? s.tiles : sms)), dim3(PRODUCT_THREADS), bytes, st,
-                              left, right, added, out, s);
+    const int workers = s.tiles < sms / CG ? s.tiles : sms / CG;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(workers * CG));
+    cfg.blockDim = dim3(PRODUCT_THREADS);
+    cfg.dynamicSmemBytes = R::BYTES;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    int n = 0;
+    if (CG == 2) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = 2;
+        attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    if (pdl_enabled()) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
+    cfg.attrs = attr;
+    cfg.numAttrs = n;
+    const bool boxes64 = KIND == APPLY || R::B_COLS == 64;
+    return cudaLaunchKernelEx(&cfg, kernel, left.tall, boxes64 ? right.low : right.tall, added, out, s);
+}
+
+// Which form a product takes: pairs of SMs where their tiles give every pair work; else 128 columns, where
+// that gives every SM work; else 64.
+template <bool PAIR, int KIND>
+cudaError_t run_product(const Maps& left, const Maps& right, const __half* added, __half* out, ProductShape s, int64_t count, int sms, cudaStream_t st) {
+    constexpr int WIDE = PAIR ? 128 : 256;      // PAIR: two accumulators a set
+    constexpr bool LOWER = KIND != APPLY;
+    const int64_t m = ceil_div(s.mp, 256), n = ceil_div(s.cols, WIDE), m1 = ceil_div(s.mp, 128), n1 = ceil_div(s.cols, 128);
+    if ((LOWER ? m * (m + 1) / 2 * (256 / WIDE) : m * n) * count >= sms / 2)
+        return launch_product<PAIR, 2, WIDE, KIND, LOWER>(left, right, added, out, s, count, sms, st);
+    if ((LOWER ? m1 * (m1 + 1) / 2 : m1 * n1) * count >= sms) return launch_product<PAIR, 1, 128, KIND, LOWER>(left, right, added, out, s, count, sms, st);
+    return launch_product<PAIR, 1, 64, KIND, false>(left, right, added, out, s, count, sms, st);
 }
 
 // --------------------------------------------------------------------------------- small matrices
@@ -694,13 +818,10 @@ cudaError_t run(const fpde_ortho_args* a, bool muon, cudaStream_t st) {
     const int64_t pieces = (int64_t)(io.mp / 64) * (io.np / 64) * a->count;
     const int64_t back = ceil_div(io.rows, 32) * ceil_div(io.cols, 32) * a->count;
     if (pieces > 0x7fffffff || back > 0x7fffffff || a->count * blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
-    CUtensorMap xk[2], xn[2], sk, pk;
-    if (a->steps > 0) {
-        bool ok = encode_planes(&sk, s, a->count, io.mp, io.mp, BM) && encode_planes(&pk, p, a->count, io.mp, io.mp, BM);
-        for (int i = 0; i < 2; ++i)
-            ok = ok && encode_planes(&xk[i], x[i], a->count, io.mp, io.np, BM) && encode_planes(&xn[i], x[i], a->count, io.mp, io.np, BK);
-        if (!ok) return cudaErrorNotSupported;
-    }
+    Maps xm[2], sm, pm;
+    if (a->steps > 0 && !(sm.encode(s, a->count, io.mp, io.mp) && pm.encode(p, a->count, io.mp, io.mp) && xm[0].encode(x[0], a->count, io.mp, io.np) &&
+                          xm[1].encode(x[1], a->count, io.mp, io.np)))
+        return cudaErrorNotSupported;
     FPDE_TRY(launch_kernel(ortho_square_kernel<T>, dim3((unsigned)(a->count * blocks)), dim3(256), st, io, sums, (int)blocks));
     FPDE_TRY(launch_kernel(ortho_start_kernel<T>, dim3((unsigned)pieces), dim3(256), st, io, (const double*)sums, (int)blocks, x[0]));
     int at = 0;
@@ -709,13 +830,9 @@ cudaError_t run(const fpde_ortho_args* a, bool muon, cudaStream_t st) {
         ProductShape gram{io.mp, io.np, 0, 0, 0, 0, io.mp, 1.f / SCALE, 0.f};
         ProductShape square{io.mp, io.np, 0, 0, 0, 0, io.mp, NS_C / SCALE, NS_B};
         ProductShape apply{io.mp, io.np, 0, 0, 0, 0, io.np, 1.f / SCALE, NS_A};
-        FPDE_TRY((launch_product<PAIR, 128, GRAM>(xk[at], xk[at], s, s, gram, a->count, sms, st)));
-        FPDE_TRY((launch_product<PAIR, 128, SQUARE>(sk, sk, s, p, square, a->count, sms, st)));
-        // 256 columns halve the loads of P per product; 128 make enough tiles where 256 leave SMs idle
-        if (ceil_div(io.mp, BM) * ceil_div(io.np, 256) * a->count >= sms)
-            FPDE_TRY((launch_product<PAIR, 256, APPLY>(pk, xn[at], x[at], x[at ^ 1], apply, a->count, sms, st)));
-        else
-            FPDE_TRY((launch_product<PAIR, 128, APPLY>(pk, xn[at], x[at], x[at ^ 1], apply, a->count, sms, st)));
+        FPDE_TRY((run_product<PAIR, GRAM>(xm[at], xm[at], s, s, gram, a->count, sms, st)));
+        FPDE_TRY((run_product<PAIR, SQUARE>(sm, sm, s, p, square, a->count, sms, st)));
+        FPDE_TRY((run_product<PAIR, APPLY>(pm, xm[at], x[at], x[at ^ 1], apply, a->count, sms, st)));
     }
     return launch_kernel(ortho_finish_kernel<T>, dim3((unsigned)back), dim3(256), st, io, (const __half*)x[at]);
 }

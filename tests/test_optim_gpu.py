@@ -51,6 +51,17 @@ def test_orthogonalize(size, dtype, guard):
     assert binding.diag_ortho_timeouts() == 0
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("size", [(8, 1000, 1030), (3, 1500, 700), (1, 2300, 2100), (20, 257, 513)])
+def test_orthogonalize_large(size, dtype, guard):
+    """Sizes that fill the GPU; the 64-bit form runs on it too."""
+    from paper_2607_18020_b200 import binding, optim
+    g = matrices(*size, dtype)
+    x = optim.orthogonalize(g)
+    assert rel(x, ortho_ref(g.double(), 5, 1e-7)) <= limit(dtype)
+    assert binding.diag_ortho_timeouts() == 0
+
+
 @pytest.mark.parametrize("steps", [0, 1, 2, 7])
 def test_number_of_steps(steps):
     from paper_2607_18020_b200 import optim
