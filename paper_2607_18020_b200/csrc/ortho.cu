@@ -101,7 +101,7 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(OrthoIo io, const doub
     const int k = blockIdx.x / (across * down), t = blockIdx.x % (across * down), i0 = t / across * 64, j0 = t % across * 64;
     const float scale = inverse_norm(sums + (int64_t)k * blocks, blocks, io.eps, part) * SCALE;
     const int r0 = io.turned ? j0 : i0, c0 = io.turned ? i0 : j0;
-#pragma unroll
+#pragma unroll 8
     for (int e = threadIdx.x; e < 64 * 64; e += 256) {
         const int r = e / 64, c = e % 64;
         tile[r][c] = r0 + r < io.rows && c0 + c < io.cols ? update_at<T>(io, k, r0 + r, c0 + c) : 0.f;
@@ -162,7 +162,7 @@ struct Ring {
     static constexpr int PLANES = PAIR ? 2 : 1;
     static constexpr int A_BYTES = BM * BK * 2, B_COLS = BN / CG, B_BYTES = B_COLS * BK * 2;    // of one block and plane
     static constexpr int STAGE = PLANES * (A_BYTES + B_BYTES);
-    static constexpr int STAGES = 196608 / STAGE > 6 ? 6 : 196608 / STAGE;
+    static constexpr int STAGES = 196608 / STAGE > 6 ? 6 : 196608 / STAGE;      // 229376 and 7 measured the same
     static constexpr int BYTES = STAGES * STAGE + 1024 + 256;    // slack to start on 1024 bytes, barriers
     static constexpr int SET = PLANES * BN;                      // TMEM columns of one set of accumulators
     static_assert(2 * SET <= 512 && STAGES >= 2, "accumulators fit TMEM, the ring shared memory");
@@ -512,16 +512,30 @@ cudaError_t launch_product(const Maps& left, const Maps& right, const __half* ad
     return cudaLaunchKernelEx(&cfg, kernel, left.tall, boxes64 ? right.low : right.tall, added, out, s);
 }
 
-// Which form a product takes: pairs of SMs where their tiles give every pair work; else 128 columns, where
-// that gives every SM work; else 64.
+// Seconds that a form of a product takes, for comparing the forms.  A block brings `STAGE` bytes per 64 of
+// depth; all of them together get some 9e12 bytes a second out of L2 (8.4 to 8.7e12 in products of
+// 4096 x 4096 and 2048 x 8192), one alone some 115e9, and its tensor core needs its time; the last tile's
+// epilogue is not hidden.
+template <bool PAIR, int CG, int BN, int KIND, bool LOWER>
+double product_seconds(const ProductShape& s, int64_t count, int sms) {
+    using R = Ring<PAIR, CG, BN>;
+    const int64_t down = ceil_div(s.mp, CG * BM), across = ceil_div(s.cols, BN), workers = sms / CG;
+    const int64_t tiles = count * (LOWER ? down * (down + 1) / 2 * (CG * BM / BN) : down * across);
+    const int64_t waves = ceil_div(tiles, workers), blocks = (tiles < workers ? tiles : workers) * CG;
+    const double shared = R::STAGE * (double)blocks / 9e12, alone = R::STAGE / 115e9, math = (PAIR ? 3 : 1) * 2.0 * BM * BN * BK * 1.0 / 14e12;
+    const double step = shared > alone ? (shared > math ? shared : math) : (alone > math ? alone : math);
+    return waves * ((KIND == GRAM ? s.np : s.mp) / BK) * step + 3e-6 * BN / 128 + (LOWER ? 2e-6 : 0);
+}
+
+// Pairs of SMs, or single blocks with tiles of 128 or 64 columns: whichever is reckoned fastest.
 template <bool PAIR, int KIND>
 cudaError_t run_product(const Maps& left, const Maps& right, const __half* added, __half* out, ProductShape s, int64_t count, int sms, cudaStream_t st) {
     constexpr int WIDE = PAIR ? 128 : 256;      // PAIR: two accumulators a set
     constexpr bool LOWER = KIND != APPLY;
-    const int64_t m = ceil_div(s.mp, 256), n = ceil_div(s.cols, WIDE), m1 = ceil_div(s.mp, 128), n1 = ceil_div(s.cols, 128);
-    if ((LOWER ? m * (m + 1) / 2 * (256 / WIDE) : m * n) * count >= sms / 2)
-        return launch_product<PAIR, 2, WIDE, KIND, LOWER>(left, right, added, out, s, count, sms, st);
-    if ((LOWER ? m1 * (m1 + 1) / 2 : m1 * n1) * count >= sms) return launch_product<PAIR, 1, 128, KIND, LOWER>(left, right, added, out, s, count, sms, st);
+    const double pairs = product_seconds<PAIR, 2, WIDE, KIND, LOWER>(s, count, sms), wide = product_seconds<PAIR, 1, 128, KIND, LOWER>(s, count, sms),
+                 narrow = product_seconds<PAIR, 1, 64, KIND, false>(s, count, sms);
+    if (pairs <= wide && pairs <= narrow) return launch_product<PAIR, 2, WIDE, KIND, LOWER>(left, right, added, out, s, count, sms, st);
+    if (wide <= narrow) return launch_product<PAIR, 1, 128, KIND, LOWER>(left, right, added, out, s, count, sms, st);
     return launch_product<PAIR, 1, 64, KIND, false>(left, right, added, out, s, count, sms, st);
 }
 
@@ -728,26 +742,34 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
     if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
-// X back in the shape of the matrices: written out, or applied to the weights.
+// X back in the shape of the matrices: written out, or applied to the weights.  64 x 64 elements a block:
+// read in 16-byte packs along X's rows, written along the matrix's rows, through shared memory where those
+// are not the same.
 template <typename T>
 __global__ void __launch_bounds__(256) ortho_finish_kernel(OrthoIo io, const __half* __restrict__ x) {
     pdl_wait_then_trigger();
-    __shared__ float tile[32][33];
-    const int across = (io.cols + 31) / 32, down = (io.rows + 31) / 32;
-    const int64_t k = blockIdx.x / (across * down), plane = (int64_t)io.mp * io.np;
-    const int t = (int)(blockIdx.x % (across * down)), r0 = t / across * 32, c0 = t % across * 32;
-    const int a = threadIdx.x / 32, b = threadIdx.x % 32;
-    const __half* p = x + 2 * k * plane;
-    for (int r = a; r < 32; r += 8) {
-        const int64_t at = (int64_t)((io.turned ? c0 : r0) + r) * io.np + (io.turned ? r0 : c0) + b;    // inside the padding
-        tile[r][b] = (__half2float(p[at]) + __half2float(p[at + plane])) * (1.f / SCALE);
+    __shared__ float tile[64][65];
+    const int across = io.np / 64, down = io.mp / 64;
+    const int k = blockIdx.x / (across * down), t = blockIdx.x % (across * down), i0 = t / across * 64, j0 = t % across * 64;
+    const int64_t plane = (int64_t)io.mp * io.np;
+#pragma unroll
+    for (int e = threadIdx.x; e < 64 * 8; e += 256) {
+        const int i = e / 8, j = e % 8 * 8;
+        const Pack<__half, 8>* p = reinterpret_cast<const Pack<__half, 8>*>(x + 2 * k * plane + (int64_t)(i0 + i) * io.np + j0 + j);
+        const Pack<__half, 8> hi = p[0], lo = p[plane / 8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) tile[i][j + q] = (__half2float(hi.v[q]) + __half2float(lo.v[q])) * (1.f / SCALE);
     }
     __syncthreads();
-    for (int r = a; r < 32; r += 8) {
-        if (r0 + r >= io.rows || c0 + b >= io.cols) continue;
-        const float v = io.turned ? tile[b][r] : tile[r][b];
-        T* out = (T*)io.out + (k * io.rows + r0 + r) * io.cols + c0 + b;
-        *out = from_f32<T>(io.momentum == nullptr ? v : fmaf(-io.rate, v, io.keep * to_f32<T>(*out)));
+    const int r0 = io.turned ? j0 : i0, c0 = io.turned ? i0 : j0;
+    T* out = (T*)io.out + ((int64_t)k * io.rows + r0) * io.cols + c0;
+#pragma unroll 4
+    for (int e = threadIdx.x; e < 64 * 64; e += 256) {
+        const int r = e / 64, c = e % 64;
+        if (r0 + r >= io.rows || c0 + c >= io.cols) continue;
+        const float v = io.turned ? tile[c][r] : tile[r][c];
+        T* o = out + (int64_t)r * io.cols + c;
+        *o = from_f32<T>(io.momentum == nullptr ? v : fmaf(-io.rate, v, io.keep * to_f32<T>(*o)));
     }
 }
 
@@ -816,8 +838,7 @@ cudaError_t run(const fpde_ortho_args* a, bool muon, cudaStream_t st) {
     if (blocks > ceil_div(4 * sms, a->count)) blocks = ceil_div(4 * sms, a->count);
     if (blocks > MOST_SUMS) blocks = MOST_SUMS;
     const int64_t pieces = (int64_t)(io.mp / 64) * (io.np / 64) * a->count;
-    const int64_t back = ceil_div(io.rows, 32) * ceil_div(io.cols, 32) * a->count;
-    if (pieces > 0x7fffffff || back > 0x7fffffff || a->count * blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    if (pieces > 0x7fffffff || a->count * blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
     Maps xm[2], sm, pm;
     if (a->steps > 0 && !(sm.encode(s, a->count, io.mp, io.mp) && pm.encode(p, a->count, io.mp, io.mp) && xm[0].encode(x[0], a->count, io.mp, io.np) &&
                           xm[1].encode(x[1], a->count, io.mp, io.np)))
@@ -834,7 +855,7 @@ cudaError_t run(const fpde_ortho_args* a, bool muon, cudaStream_t st) {
         FPDE_TRY((run_product<PAIR, SQUARE>(sm, sm, s, p, square, a->count, sms, st)));
         FPDE_TRY((run_product<PAIR, APPLY>(pm, xm[at], x[at], x[at ^ 1], apply, a->count, sms, st)));
     }
-    return launch_kernel(ortho_finish_kernel<T>, dim3((unsigned)back), dim3(256), st, io, (const __half*)x[at]);
+    return launch_kernel(ortho_finish_kernel<T>, dim3((unsigned)pieces), dim3(256), st, io, (const __half*)x[at]);
 }
 
 int call(const fpde_ortho_args* a, bool muon, void* stream) {
