@@ -356,27 +356,32 @@ __global__ void __launch_bounds__(256) conv_sum_kernel(const float* __restrict__
     }
 }
 
-// One node: a thread per channel and row.  `state_out` may be `state`: a thread reads its window first.
-template <typename T, int W>
-__global__ void __launch_bounds__(256) conv_step_kernel(const T* __restrict__ x, int64_t x_batch, const float* __restrict__ weight,
-                                                        const float* __restrict__ bias, const T* state, T* __restrict__ y,
-                                                        T* state_out, int64_t rows, int channels, int silu) {
+// One node: a thread takes VEC neighbouring channels of one row.  `state_out` may be `state`: a thread reads
+// its window first.
+template <typename T, int W, int VEC>
+__global__ void __launch_bounds__(128) conv_step_kernel(const T* __restrict__ x, int64_t x_batch, const float* __restrict__ weight,
+                                                        const float* __restrict__ bias, const T* state, T* __restrict__ y, T* state_out,
+                                                        int across, int channels, int silu) {
     pdl_wait_then_trigger();
-    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (e >= rows * channels) return;
-    const int64_t b = e / channels;
-    const int c = (int)(e % channels);
-    T v[W];
+    const int64_t b = blockIdx.x / across;
+    const int c = ((int)(blockIdx.x % across) * 128 + (int)threadIdx.x) * VEC;
+    if (c >= channels) return;
+    Pack<T, VEC> v[W];
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) v[j] = state ? state[(b * (W - 1) + j) * channels + c] : from_f32<T>(0.f);
-    v[W - 1] = x[b * x_batch + c];
-    float pre = bias ? bias[c] : 0.f;
+    for (int j = 0; j < W - 1; ++j) v[j] = pack_at<T, VEC>(state + (b * (W - 1) + j) * channels + c, state != nullptr);
+    v[W - 1] = load_pack<T, VEC>(x + b * x_batch + c);
+    float pre[VEC];
 #pragma unroll
-    for (int j = 0; j < W; ++j) pre = fmaf(weight[(int64_t)c * W + j], to_f32<T>(v[j]), pre);
-    y[e] = from_f32<T>(silu ? pre * sigmoid_exact_f32(pre) : pre);
+    for (int i = 0; i < VEC; ++i) {
+        pre[i] = bias ? bias[c + i] : 0.f;
+#pragma unroll
+        for (int j = 0; j < W; ++j) pre[i] = fmaf(weight[(int64_t)(c + i) * W + j], to_f32<T>(v[j].v[i]), pre[i]);
+        if (silu) pre[i] *= sigmoid_exact_f32(pre[i]);
+    }
+    store_pack<T, VEC>(y + b * channels + c, pre);
     if (state_out != nullptr) {
 #pragma unroll
-        for (int j = 0; j < W - 1; ++j) state_out[(b * (W - 1) + j) * channels + c] = v[j + 1];
+        for (int j = 0; j < W - 1; ++j) *reinterpret_cast<Pack<T, VEC>*>(state_out + (b * (W - 1) + j) * channels + c) = v[j + 1];
     }
 }
 
@@ -468,12 +473,19 @@ cudaError_t conv_by_type(const fpde_conv_args* a, bool backward, cudaStream_t st
     return conv_by_width<__half>(a, backward, st);
 }
 
+template <typename T, int W, int VEC>
+cudaError_t conv_step_run(const fpde_conv_args* a, cudaStream_t st) {
+    const int64_t across = ceil_div(a->channels, 128 * VEC), blocks = a->batch * across;
+    if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    return launch_kernel(conv_step_kernel<T, W, VEC>, dim3((unsigned)blocks), dim3(128), st, (const T*)a->x, a->x_batch, a->weight, a->bias,
+                         (const T*)a->state, (T*)a->y, (T*)a->state_out, (int)across, (int)a->channels, a->silu);
+}
+
 template <typename T, int W>
 cudaError_t conv_step_launch(const fpde_conv_args* a, cudaStream_t st) {
-    const int64_t blocks = ceil_div(a->batch * a->channels, 256);
-    if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
-    return launch_kernel(conv_step_kernel<T, W>, dim3((unsigned)blocks), dim3(256), st, (const T*)a->x, a->x_batch, a->weight,
-                         a->bias, (const T*)a->state, (T*)a->y, (T*)a->state_out, a->batch, (int)a->channels, a->silu);
+    const bool pairs = a->channels % 2 == 0 && packs(a->x, a->x_batch, 0, sizeof(T), 2) && aligned(a->y, 2 * sizeof(T)) &&
+                       aligned(a->state, 2 * sizeof(T)) && aligned(a->state_out, 2 * sizeof(T));
+    return pairs ? conv_step_run<T, W, 2>(a, st) : conv_step_run<T, W, 1>(a, st);
 }
 
 template <typename T>

@@ -27,7 +27,7 @@
 namespace fpde {
 namespace {
 
-constexpr int FWD_THREADS = 64, BACK_THREADS = 128, STEP_THREADS = 128;
+constexpr int FWD_THREADS = 64, BACK_THREADS = 128, STEP_THREADS = 128, STEP_CHANNELS = 4;
 constexpr int FWD_UNROLL = 4;
 constexpr int TILE = 16;          // nodes brought to shared memory together
 constexpr int KEEP = 8;           // nodes between stored states: what the backward march holds in registers
@@ -228,8 +228,8 @@ __device__ __forceinline__ Quad load_states(const float* p, int n, int states, f
     return quad_of(v);
 }
 __device__ __forceinline__ bool states_packed(int states) { return states % NS == 0; }
-__device__ __forceinline__ void store_states(float* p, int n, int states, const Quad& q) {
-    if (states_packed(states)) {     // rows of states start on 16 bytes
+__device__ __forceinline__ void store_states(float* p, int n, int states, bool packed, const Quad& q) {
+    if (packed) {     // rows of states start on 16 bytes
         if (n < states) *reinterpret_cast<Quad*>(p + n) = q;
         return;
     }
@@ -345,7 +345,7 @@ __global__ void __launch_bounds__(FWD_THREADS, FWD_BLOCKS) scan_fwd_kernel(ScanI
                 float* dst = kept + ((w.b * s.kept_nodes + (t0 + k0) / KEEP) * s.channels + c) * s.states;
 #pragma unroll
                 for (int k = 0; k < NC; ++k)
-                    if (c + k < s.channels) store_states(dst + k * s.states, q * NS, s.states, h[k]);
+                    if (c + k < s.channels) store_states(dst + k * s.states, q * NS, s.states, states_packed(s.states), h[k]);
             }
             float y[4 * NC];
 #pragma unroll
@@ -401,7 +401,7 @@ __global__ void __launch_bounds__(FWD_THREADS, FWD_BLOCKS) scan_fwd_kernel(ScanI
     for (int k = 0; k < NC; ++k) {
         if (c + k >= s.channels) continue;
         if (ENDS) {
-            store_states(local + (at * s.channels + c + k) * s.states, q * NS, s.states, h[k]);
+            store_states(local + (at * s.channels + c + k) * s.states, q * NS, s.states, states_packed(s.states), h[k]);
             if (q == 0) sums[at * s.channels + c + k] = total[k];
         } else if (state_out != nullptr && w.chunk == s.chunks - 1) {
             float v[NS];
@@ -713,7 +713,7 @@ __global__ void __launch_bounds__(BACK_THREADS, BACK_BLOCKS) scan_bwd_kernel(Sca
 #pragma unroll
         for (int k = 0; k < NC; ++k) {
             if (c + k >= s.channels) continue;
-            store_states(local + (at * s.channels + c + k) * s.states, q * NS, s.states, p[k]);
+            store_states(local + (at * s.channels + c + k) * s.states, q * NS, s.states, states_packed(s.states), p[k]);
             if (q == 0) sums[at * s.channels + c + k] = total[k];
         }
     } else {
@@ -793,41 +793,62 @@ __global__ void __launch_bounds__(256) scan_sum_a_kernel(const float* __restrict
 }
 
 // ---------------------------------------------------------------------------------------- one node
-// S lanes share a channel, four states each; state_out may be state.
+// Bound by the states' traffic, 8 bytes each.  S lanes share a channel, four states each, and a thread takes
+// STEP_CHANNELS channels of one row at once, so that their loads are on their way together; B and C of the
+// row are loaded once per thread.  state_out may be state: a thread reads what it writes.
 template <typename T, int S>
 __global__ void __launch_bounds__(STEP_THREADS) scan_step_kernel(ScanIn<T> in, const float* state, T* __restrict__ out, float* state_out,
-                                                            int64_t rows, ScanShape s) {
+                                                                 int across, bool packed, ScanShape s) {
     pdl_wait_then_trigger();
-    const int64_t e = ((int64_t)blockIdx.x * STEP_THREADS + threadIdx.x) / S;
-    const int q = threadIdx.x % S;
-    const bool there = e < rows * s.channels;
-    const int64_t b = there ? e / s.channels : 0;
-    const int c = there ? (int)(e % s.channels) : 0;
-    float y = 0.f, u = 0.f;
-    if (there) {
-        const float dt = step_of(to_f32<T>(in.delta[b * s.delta_batch + c]) + (in.bias ? in.bias[c] : 0.f), s.softplus);
-        u = to_f32<T>(in.u[b * s.u_batch + c]);
+    constexpr int CT = STEP_THREADS / S;           // channels next to one another
+    const int64_t b = blockIdx.x / across;
+    const int q = threadIdx.x % S, n0 = q * NS, c0 = (int)(blockIdx.x % across) * (CT * STEP_CHANNELS) + threadIdx.x / S;
+    const bool mine = n0 < s.states;
+    Quad h[STEP_CHANNELS], a2[STEP_CHANNELS];
+    float dt[STEP_CHANNELS], u[STEP_CHANNELS], z[STEP_CHANNELS];
 #pragma unroll
-        for (int i = 0; i < NS; ++i) {
-            const int n = q * NS + i;
-            if (n < s.states) {
-                const float h0 = state ? state[e * s.states + n] : 0.f;
-                const float h = fmaf(exp2_f32(dt * (in.A[(int64_t)c * s.states + n] * LOG2_E)), h0,
-                                     dt * u * to_f32<T>(in.B[b * s.B_batch + n]));
-                y = fmaf(to_f32<T>(in.C[b * s.C_batch + n]), h, y);
-                if (state_out != nullptr) state_out[e * s.states + n] = h;
-            }
+    for (int k = 0; k < STEP_CHANNELS; ++k) {
+        const int c = c0 + k * CT;
+        const bool there = c < s.channels;
+        const int64_t at = (b * s.channels + c) * s.states;
+        h[k] = a2[k] = {0, 0};
+        dt[k] = u[k] = z[k] = 0.f;
+        if (!there) continue;
+        if (packed) {
+            if (mine && state) h[k] = quad_at(state + at + n0);
+            if (mine) a2[k] = quad_at(in.A + (int64_t)c * s.states + n0);
+        } else {
+            h[k] = load_states(state ? state + at : nullptr, n0, s.states, 1.f);
+            a2[k] = load_states(in.A + (int64_t)c * s.states, n0, s.states, 1.f);
         }
+        dt[k] = to_f32<T>(in.delta[b * s.delta_batch + c]) + (in.bias ? in.bias[c] : 0.f);
+        u[k] = to_f32<T>(in.u[b * s.u_batch + c]);
+        if (in.z) z[k] = to_f32<T>(in.z[b * s.z_batch + c]);
     }
+    float bv[NS], cv[NS];
 #pragma unroll
-    for (int m = 1; m < S; m *= 2) y += __shfl_xor_sync(~0u, y, m);
-    if (there && q == 0) {
-        if (in.D) y = fmaf(in.D[c], u, y);
-        if (in.z) {
-            const float z = to_f32<T>(in.z[b * s.z_batch + c]);
-            y *= z * sigmoid_f32(z);
+    for (int i = 0; i < NS; ++i) {
+        bv[i] = n0 + i < s.states ? to_f32<T>(in.B[b * s.B_batch + n0 + i]) : 0.f;
+        cv[i] = n0 + i < s.states ? to_f32<T>(in.C[b * s.C_batch + n0 + i]) : 0.f;
+    }
+    const Quad b4 = quad_of(bv), c4 = quad_of(cv);
+#pragma unroll
+    for (int k = 0; k < STEP_CHANNELS; ++k) {
+        const int c = c0 + k * CT;
+        const float step = step_of(dt[k], s.softplus);
+        const uint64_t d = both(step * LOG2_E), du = both(step * u[k]);
+        h[k].lo = fma2(exp2_pair(mul2(d, a2[k].lo)), h[k].lo, mul2(du, b4.lo));
+        h[k].hi = fma2(exp2_pair(mul2(d, a2[k].hi)), h[k].hi, mul2(du, b4.hi));
+        float y = sum2(fma2(c4.lo, h[k].lo, mul2(c4.hi, h[k].hi)));
+#pragma unroll
+        for (int m = 1; m < S; m *= 2) y += __shfl_xor_sync(~0u, y, m);
+        if (c >= s.channels) continue;
+        if (state_out != nullptr) store_states(state_out + (b * s.channels + c) * s.states, n0, s.states, packed, h[k]);
+        if (q == 0) {
+            if (in.D) y = fmaf(in.D[c], u[k], y);
+            if (in.z) y *= z[k] * sigmoid_f32(z[k]);
+            out[b * s.channels + c] = from_f32<T>(y);
         }
-        out[e] = from_f32<T>(y);
     }
 }
 
@@ -838,9 +859,7 @@ int lanes_of(int states) {
     return s;
 }
 
-// The plan depends on sizes only, so that the forward and the backward call agree on it.
-ScanShape plan(const fpde_scan_args* a, bool backward) {
-
+ScanShape shape_of(const fpde_scan_args* a) {
     ScanShape s = {};
     s.length = a->length;
     s.u_batch = a->u_batch; s.u_node = a->u_node;
@@ -852,6 +871,12 @@ ScanShape plan(const fpde_scan_args* a, bool backward) {
     s.channels = (int)a->channels;
     s.states = a->states;
     s.softplus = a->softplus;
+    return s;
+}
+
+// The plan depends on sizes only, so that the forward and the backward call agree on it.
+ScanShape plan(const fpde_scan_args* a, bool backward) {
+    ScanShape s = shape_of(a);
     s.tiles = (int)ceil_div(a->channels, (backward ? BACK_THREADS : FWD_THREADS) / lanes_of(a->states) * NC);
     s.kept_nodes = ceil_div(a->length, KEEP);
     // Chunks.  The blocks run in waves of `resident` per SM, and a wave takes as long as its nodes: the marches
@@ -1018,11 +1043,12 @@ cudaError_t run_bwd(const fpde_scan_args* a, cudaStream_t st) {
 
 template <typename T, int S>
 cudaError_t run_step(const fpde_scan_args* a, cudaStream_t st) {
-    const ScanShape s = plan(a, false);
-    const int64_t blocks = ceil_div(a->batch * s.channels * S, STEP_THREADS);
+    const ScanShape s = shape_of(a);
+    const int64_t across = ceil_div(s.channels, STEP_THREADS / S * STEP_CHANNELS), blocks = a->batch * across;
     if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    const bool packed = s.states % NS == 0 && aligned(a->state, 16) && aligned(a->state_out, 16) && aligned(a->A, 16);
     return launch_kernel(scan_step_kernel<T, S>, dim3((unsigned)blocks), dim3(STEP_THREADS), st, inputs<T>(a), a->state, (T*)a->out, a->state_out,
-                         a->batch, s);
+                         (int)across, packed, s);
 }
 
 enum Call { CALL_FWD, CALL_BWD, CALL_STEP };
