@@ -793,37 +793,45 @@ __global__ void __launch_bounds__(256) scan_sum_a_kernel(const float* __restrict
 }
 
 // ---------------------------------------------------------------------------------------- one node
-// Bound by the states' traffic, 8 bytes each.  S lanes share a channel, four states each, and a thread takes
-// STEP_CHANNELS channels of one row at once, so that their loads are on their way together; B and C of the
-// row are loaded once per thread.  state_out may be state: a thread reads what it writes.
+// Bound by the states' traffic, 8 bytes each.  S lanes share a channel, four states each, and take four
+// channels of one row at once, so that their loads are on their way together.  What is per channel (dt,
+// the gate) is computed by one lane for each: the lane to which the sum over the states comes.  B and C
+// of the row are loaded once per thread.  state_out may be state: a thread reads what it writes.
 template <typename T, int S>
 __global__ void __launch_bounds__(STEP_THREADS) scan_step_kernel(ScanIn<T> in, const float* state, T* __restrict__ out, float* state_out,
                                                                  int across, bool packed, ScanShape s) {
     pdl_wait_then_trigger();
-    constexpr int CT = STEP_THREADS / S;           // channels next to one another
+    constexpr int CT = STEP_THREADS / S, K = STEP_CHANNELS;           // channels next to one another
+    constexpr int OWN = sums_left<K, S / 2, 1>(), SHARE = S > K ? S / K : 1;      // channels of a lane, lanes of a channel
     const int64_t b = blockIdx.x / across;
-    const int q = threadIdx.x % S, n0 = q * NS, c0 = (int)(blockIdx.x % across) * (CT * STEP_CHANNELS) + threadIdx.x / S;
+    const int lane = threadIdx.x % 32, q = threadIdx.x % S, n0 = q * NS, c0 = (int)(blockIdx.x % across) * (CT * K) + threadIdx.x / S;
+    const int first = q * K / S;                                      // its first channel
     const bool mine = n0 < s.states;
-    Quad h[STEP_CHANNELS], a2[STEP_CHANNELS];
-    float dt[STEP_CHANNELS], u[STEP_CHANNELS], z[STEP_CHANNELS];
+    Quad h[K], a2[K];
 #pragma unroll
-    for (int k = 0; k < STEP_CHANNELS; ++k) {
+    for (int k = 0; k < K; ++k) {
         const int c = c0 + k * CT;
-        const bool there = c < s.channels;
-        const int64_t at = (b * s.channels + c) * s.states;
+        const int64_t cn = (int64_t)c * s.states;
         h[k] = a2[k] = {0, 0};
-        dt[k] = u[k] = z[k] = 0.f;
-        if (!there) continue;
+        if (c >= s.channels) continue;
         if (packed) {
-            if (mine && state) h[k] = quad_at(state + at + n0);
-            if (mine) a2[k] = quad_at(in.A + (int64_t)c * s.states + n0);
+            if (mine && state) h[k] = quad_at(state + b * s.channels * s.states + cn + n0);
+            if (mine) a2[k] = quad_at(in.A + cn + n0);
         } else {
-            h[k] = load_states(state ? state + at : nullptr, n0, s.states, 1.f);
-            a2[k] = load_states(in.A + (int64_t)c * s.states, n0, s.states, 1.f);
+            h[k] = load_states(state ? state + b * s.channels * s.states + cn : nullptr, n0, s.states, 1.f);
+            a2[k] = load_states(in.A + cn, n0, s.states, 1.f);
         }
-        dt[k] = to_f32<T>(in.delta[b * s.delta_batch + c]) + (in.bias ? in.bias[c] : 0.f);
-        u[k] = to_f32<T>(in.u[b * s.u_batch + c]);
-        if (in.z) z[k] = to_f32<T>(in.z[b * s.z_batch + c]);
+    }
+    float dt[OWN], u[OWN], z[OWN];
+#pragma unroll
+    for (int k = 0; k < OWN; ++k) {
+        const int c = c0 + (first + k) * CT;
+        dt[k] = u[k] = z[k] = 0.f;
+        if (c < s.channels) {
+            dt[k] = to_f32<T>(in.delta[b * s.delta_batch + c]) + (in.bias ? in.bias[c] : 0.f);
+            u[k] = to_f32<T>(in.u[b * s.u_batch + c]);
+            if (in.z) z[k] = to_f32<T>(in.z[b * s.z_batch + c]);
+        }
     }
     float bv[NS], cv[NS];
 #pragma unroll
@@ -833,22 +841,27 @@ __global__ void __launch_bounds__(STEP_THREADS) scan_step_kernel(ScanIn<T> in, c
     }
     const Quad b4 = quad_of(bv), c4 = quad_of(cv);
 #pragma unroll
-    for (int k = 0; k < STEP_CHANNELS; ++k) {
-        const int c = c0 + k * CT;
-        const float step = step_of(dt[k], s.softplus);
-        const uint64_t d = both(step * LOG2_E), du = both(step * u[k]);
-        h[k].lo = fma2(exp2_pair(mul2(d, a2[k].lo)), h[k].lo, mul2(du, b4.lo));
-        h[k].hi = fma2(exp2_pair(mul2(d, a2[k].hi)), h[k].hi, mul2(du, b4.hi));
-        float y = sum2(fma2(c4.lo, h[k].lo, mul2(c4.hi, h[k].hi)));
+    for (int k = 0; k < OWN; ++k) dt[k] = step_of(dt[k], s.softplus);
+    float y[K];
 #pragma unroll
-        for (int m = 1; m < S; m *= 2) y += __shfl_xor_sync(~0u, y, m);
+    for (int k = 0; k < K; ++k) {
+        const int c = c0 + k * CT, owner = (lane & ~(S - 1)) + (S >= K ? k * (S / K) : k / OWN);
+        const float step = __shfl_sync(~0u, dt[k % OWN], owner), du = __shfl_sync(~0u, dt[k % OWN] * u[k % OWN], owner);
+        const uint64_t d = both(step * LOG2_E), w = both(du);
+        h[k].lo = fma2(exp2_pair(mul2(d, a2[k].lo)), h[k].lo, mul2(w, b4.lo));
+        h[k].hi = fma2(exp2_pair(mul2(d, a2[k].hi)), h[k].hi, mul2(w, b4.hi));
+        y[k] = sum2(fma2(c4.lo, h[k].lo, mul2(c4.hi, h[k].hi)));
+        if (c < s.channels && state_out != nullptr) store_states(state_out + (b * s.channels + c) * s.states, n0, s.states, packed, h[k]);
+    }
+    sum_lanes<K, S / 2, 1>(y, q);
+    if (q % SHARE != 0) return;
+#pragma unroll
+    for (int k = 0; k < OWN; ++k) {
+        const int c = c0 + (first + k) * CT;
         if (c >= s.channels) continue;
-        if (state_out != nullptr) store_states(state_out + (b * s.channels + c) * s.states, n0, s.states, packed, h[k]);
-        if (q == 0) {
-            if (in.D) y = fmaf(in.D[c], u[k], y);
-            if (in.z) y *= z[k] * sigmoid_f32(z[k]);
-            out[b * s.channels + c] = from_f32<T>(y);
-        }
+        if (in.D) y[k] = fmaf(in.D[c], u[k], y[k]);
+        if (in.z) y[k] *= z[k] * sigmoid_f32(z[k]);
+        out[b * s.channels + c] = from_f32<T>(y[k]);
     }
 }
 
