@@ -356,32 +356,42 @@ __global__ void __launch_bounds__(256) conv_sum_kernel(const float* __restrict__
     }
 }
 
-// One node: a thread takes VEC neighbouring channels of one row.  `state_out` may be `state`: a thread reads
-// its window first.
+// One node: a thread takes VEC neighbouring channels of `rows` rows, one after the other, and keeps their
+// filter in registers.  `state_out` may be `state`: a thread reads its window first.
 template <typename T, int W, int VEC>
 __global__ void __launch_bounds__(128) conv_step_kernel(const T* __restrict__ x, int64_t x_batch, const float* __restrict__ weight,
                                                         const float* __restrict__ bias, const T* state, T* __restrict__ y, T* state_out,
-                                                        int across, int channels, int silu) {
+                                                        int64_t batch, int across, int rows, int channels, int silu) {
     pdl_wait_then_trigger();
-    const int64_t b = blockIdx.x / across;
     const int c = ((int)(blockIdx.x % across) * 128 + (int)threadIdx.x) * VEC;
     if (c >= channels) return;
-    Pack<T, VEC> v[W];
-#pragma unroll
-    for (int j = 0; j < W - 1; ++j) v[j] = pack_at<T, VEC>(state + (b * (W - 1) + j) * channels + c, state != nullptr);
-    v[W - 1] = load_pack<T, VEC>(x + b * x_batch + c);
-    float pre[VEC];
+    float w[VEC][W], bs[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
-        pre[i] = bias ? bias[c + i] : 0.f;
+        bs[i] = bias ? bias[c + i] : 0.f;
 #pragma unroll
-        for (int j = 0; j < W; ++j) pre[i] = fmaf(weight[(int64_t)(c + i) * W + j], to_f32<T>(v[j].v[i]), pre[i]);
-        if (silu) pre[i] *= sigmoid_exact_f32(pre[i]);
+        for (int j = 0; j < W; ++j) w[i][j] = weight[(int64_t)(c + i) * W + j];
     }
-    store_pack<T, VEC>(y + b * channels + c, pre);
-    if (state_out != nullptr) {
+    const int64_t b0 = (int64_t)(blockIdx.x / across) * rows, b1 = b0 + rows < batch ? b0 + rows : batch;
+#pragma unroll 2
+    for (int64_t b = b0; b < b1; ++b) {
+        Pack<T, VEC> v[W];
 #pragma unroll
-        for (int j = 0; j < W - 1; ++j) *reinterpret_cast<Pack<T, VEC>*>(state_out + (b * (W - 1) + j) * channels + c) = v[j + 1];
+        for (int j = 0; j < W - 1; ++j) v[j] = pack_at<T, VEC>(state + (b * (W - 1) + j) * channels + c, state != nullptr);
+        v[W - 1] = load_pack<T, VEC>(x + b * x_batch + c);
+        float pre[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            pre[i] = bs[i];
+#pragma unroll
+            for (int j = 0; j < W; ++j) pre[i] = fmaf(w[i][j], to_f32<T>(v[j].v[i]), pre[i]);
+            if (silu) pre[i] *= sigmoid_exact_f32(pre[i]);
+        }
+        store_pack<T, VEC>(y + b * channels + c, pre);
+        if (state_out != nullptr) {
+#pragma unroll
+            for (int j = 0; j < W - 1; ++j) *reinterpret_cast<Pack<T, VEC>*>(state_out + (b * (W - 1) + j) * channels + c) = v[j + 1];
+        }
     }
 }
 
@@ -475,10 +485,12 @@ cudaError_t conv_by_type(const fpde_conv_args* a, bool backward, cudaStream_t st
 
 template <typename T, int W, int VEC>
 cudaError_t conv_step_run(const fpde_conv_args* a, cudaStream_t st) {
-    const int64_t across = ceil_div(a->channels, 128 * VEC), blocks = a->batch * across;
+    const int64_t across = ceil_div(a->channels, 128 * VEC);
+    const int rows = a->batch * across >= 148 * 16 ? 4 : 1;      // one row a thread while the GPU is not full: latency
+    const int64_t blocks = ceil_div(a->batch, rows) * across;
     if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
     return launch_kernel(conv_step_kernel<T, W, VEC>, dim3((unsigned)blocks), dim3(128), st, (const T*)a->x, a->x_batch, a->weight, a->bias,
-                         (const T*)a->state, (T*)a->y, (T*)a->state_out, (int)across, (int)a->channels, a->silu);
+                         (const T*)a->state, (T*)a->y, (T*)a->state_out, a->batch, (int)across, rows, (int)a->channels, a->silu);
 }
 
 template <typename T, int W>
