@@ -140,6 +140,26 @@ __device__ __forceinline__ uint64_t sigmoid_pair(uint64_t v) {
     return pair(reciprocal_f32(x), reciprocal_f32(y));
 }
 
+// One value, or a pair of them, in the same code.
+template <int N> struct Lanes;
+template <> struct Lanes<1> { using V = float; };
+template <> struct Lanes<2> { using V = uint64_t; };
+__device__ __forceinline__ float fma_v(float a, float b, float c) { return fmaf(a, b, c); }
+__device__ __forceinline__ uint64_t fma_v(uint64_t a, uint64_t b, uint64_t c) { return fma2(a, b, c); }
+__device__ __forceinline__ float mul_v(float a, float b) { return a * b; }
+__device__ __forceinline__ uint64_t mul_v(uint64_t a, uint64_t b) { return mul2(a, b); }
+__device__ __forceinline__ float add_v(float a, float b) { return a + b; }
+__device__ __forceinline__ uint64_t add_v(uint64_t a, uint64_t b) { return add2(a, b); }
+__device__ __forceinline__ float sigmoid_v(float v) { return sigmoid_f32(v); }
+__device__ __forceinline__ uint64_t sigmoid_v(uint64_t v) { return sigmoid_pair(v); }
+template <typename V> __device__ __forceinline__ V all_v(float v);
+template <> __device__ __forceinline__ float all_v<float>(float v) { return v; }
+template <> __device__ __forceinline__ uint64_t all_v<uint64_t>(float v) { return both(v); }
+__device__ __forceinline__ float of_array(const float (&v)[1]) { return v[0]; }
+__device__ __forceinline__ uint64_t of_array(const float (&v)[2]) { return pair(v[0], v[1]); }
+__device__ __forceinline__ void to_array(float (&v)[1], float a) { v[0] = a; }
+__device__ __forceinline__ void to_array(float (&v)[2], uint64_t a) { unpair(a, v[0], v[1]); }
+
 // The same for the one or two channels of a thread.
 template <int N>
 __device__ __forceinline__ void softplus_of(float (&v)[N]) {
@@ -155,6 +175,19 @@ template <typename T, int N>
 __device__ __forceinline__ void widen(float (&out)[N], const Pack<T, N>& k) {
 #pragma unroll
     for (int i = 0; i < N; ++i) out[i] = to_f32<T>(k.v[i]);
+}
+
+template <typename T, int N>
+__device__ __forceinline__ typename Lanes<N>::V widen_v(const Pack<T, N>& k) {
+    float v[N];
+    widen<T, N>(v, k);
+    return of_array(v);
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_v(T* p, typename Lanes<N>::V a) {
+    float v[N];
+    to_array(v, a);
+    store_pack<T, N>(p, v);
 }
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }

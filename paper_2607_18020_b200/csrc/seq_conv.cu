@@ -107,12 +107,28 @@ __device__ __forceinline__ Pack<T, VEC> x_at(const T* x, int64_t x_node, const T
     return pack_at<T, VEC>(window + (t + W - 1) * channels, window != nullptr && t + W - 1 >= 0);
 }
 
+// The filters of the thread's channels, tap by tap, and their biases.
+template <int VEC, int W>
+__device__ __forceinline__ void load_filter(typename Lanes<VEC>::V (&w)[W], typename Lanes<VEC>::V& bs, const float* weight, const float* bias, int c) {
+    float v[VEC];
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = weight[(int64_t)(c + i) * W + j];
+        w[j] = of_array(v);
+    }
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) v[i] = bias ? bias[c + i] : 0.f;
+    bs = of_array(v);
+}
+
 template <typename T, int VEC, int W>
 __global__ void __launch_bounds__(CONV_THREADS) conv_fwd_kernel(
     const T* __restrict__ x, const float* __restrict__ weight, const float* __restrict__ bias, const T* __restrict__ state,
     T* __restrict__ y, T* __restrict__ state_out, ConvShape s) {
     pdl_wait_then_trigger();
     using F = Feed<T, VEC>;
+    using V = typename Lanes<VEC>::V;
     __shared__ Pack<T, VEC> ring[F::SLOTS][CONV_THREADS];
     const ConvWhere at = conv_where<VEC>(s);
     const int c = at.c;
@@ -129,40 +145,29 @@ __global__ void __launch_bounds__(CONV_THREADS) conv_fwd_kernel(
         } else {
             fx.request(0);
         }
-        float w[VEC][W], bs[VEC];
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            bs[i] = bias ? bias[c + i] : 0.f;
-#pragma unroll
-            for (int j = 0; j < W; ++j) w[i][j] = weight[(int64_t)(c + i) * W + j];
-        }
-        float xs[GROUP + W - 1][VEC];           // the W-1 nodes before the group, then the group
+        V w[W], bs;
+        load_filter<VEC, W>(w, bs, weight, bias, c);
+        V xs[GROUP + W - 1];                    // the W-1 nodes before the group, then the group
 #pragma unroll
         for (int j = 0; j < W - 1; ++j)
-            widen<T, VEC>(xs[GROUP + j], x_at<T, VEC, W>(xr, s.x_node, win, at.t0 + j - (W - 1), s.length, s.channels));
+            xs[GROUP + j] = widen_v<T, VEC>(x_at<T, VEC, W>(xr, s.x_node, win, at.t0 + j - (W - 1), s.length, s.channels));
         T* yp = y + (at.b * s.length + at.t0) * s.channels + c;
         int slot = 0;
         for (int t = 0; t < total; t += GROUP) {
 #pragma unroll
-            for (int j = 0; j < W - 1; ++j)
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) xs[j][i] = xs[GROUP + j][i];
+            for (int j = 0; j < W - 1; ++j) xs[j] = xs[GROUP + j];
             if (F::ASYNC) { fx.request((slot + AHEAD - 1) % AHEAD); feed_commit(); feed_wait(); }
 #pragma unroll
-            for (int k = 0; k < GROUP; ++k) widen<T, VEC>(xs[W - 1 + k], fx.get(slot, k));
+            for (int k = 0; k < GROUP; ++k) xs[W - 1 + k] = widen_v<T, VEC>(fx.get(slot, k));
             if (F::ASYNC) slot = (slot + 1) % AHEAD;
             else fx.request(0);
 #pragma unroll
             for (int k = 0; k < GROUP; ++k) {
-                float v[VEC];
+                V pre = bs;
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    float pre = bs[i];
-#pragma unroll
-                    for (int j = 0; j < W; ++j) pre = fmaf(w[i][j], xs[k + j][i], pre);
-                    v[i] = s.silu ? pre * sigmoid_f32(pre) : pre;
-                }
-                if (t + k < total) store_pack<T, VEC>(yp + k * (int64_t)s.channels, v);
+                for (int j = 0; j < W; ++j) pre = fma_v(w[j], xs[k + j], pre);
+                if (s.silu) pre = mul_v(pre, sigmoid_v(pre));
+                if (t + k < total) store_v<T, VEC>(yp + k * (int64_t)s.channels, pre);
             }
             yp += GROUP * (int64_t)s.channels;
         }
@@ -186,11 +191,15 @@ __global__ void __launch_bounds__(CONV_THREADS) conv_bwd_kernel(
     float* __restrict__ partial, ConvShape s) {
     pdl_wait_then_trigger();
     using F = Feed<T, VEC>;
+    using V = typename Lanes<VEC>::V;
     __shared__ Pack<T, VEC> ring_x[F::SLOTS][CONV_THREADS], ring_g[F::SLOTS][CONV_THREADS];
     __shared__ float sums[CONV_ROWS][VEC * (W + 1)][CONV_LANES];
     const ConvWhere at = conv_where<VEC>(s);
     const int c = at.c;
-    float acc[VEC][W + 1] = {};
+    const V zero = all_v<V>(0.f), one = all_v<V>(1.f);
+    V acc[W + 1];                                  // gradients of the taps and the bias
+#pragma unroll
+    for (int j = 0; j <= W; ++j) acc[j] = zero;
     if (c < s.channels && at.t0 < s.length + W - 1) {
         const int total = (int)(s.length + W - 1 - at.t0 < s.nodes ? s.length + W - 1 - at.t0 : s.nodes);   // positions
         const int nodes = min(total, clamp_left(s.length - at.t0));                                          // of these, nodes that exist
@@ -209,51 +218,37 @@ __global__ void __launch_bounds__(CONV_THREADS) conv_bwd_kernel(
             fx.request(0);
             fg.request(0);
         }
-        float w[VEC][W], bs[VEC];
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            bs[i] = bias ? bias[c + i] : 0.f;
-#pragma unroll
-            for (int j = 0; j < W; ++j) w[i][j] = weight[(int64_t)(c + i) * W + j];
-        }
-        // g of one node from the W values of x that reach it
-        auto slope = [&](float gv, const float (&xv)[W], int i) {
+        V w[W], bs;
+        load_filter<VEC, W>(w, bs, weight, bias, c);
+        // g of one node from the W values of x that reach it: gy q (1 + pre (1 - q)), q the sigmoid
+        auto slope = [&](V gv, const V* xv) {
             if (!s.silu) return gv;
-            float pre = bs[i];
+            V pre = bs;
 #pragma unroll
-            for (int j = 0; j < W; ++j) pre = fmaf(w[i][j], xv[j], pre);
-            const float q = sigmoid_f32(pre);
-            return gv * (q * fmaf(pre, 1.f - q, 1.f));
+            for (int j = 0; j < W; ++j) pre = fma_v(w[j], xv[j], pre);
+            const V q = sigmoid_v(pre), rest = fma_v(q, all_v<V>(-1.f), one);
+            return mul_v(gv, mul_v(q, fma_v(pre, rest, one)));
         };
-        float xs[GROUP + W - 1][VEC], g[GROUP + W - 1][VEC];      // the W-1 nodes before the group, then the group
+        V xs[GROUP + W - 1], g[GROUP + W - 1];                     // the W-1 nodes before the group, then the group
         {
-            float h[2 * W - 2 + (W == 1)][VEC];                    // x from 2 (W-1) nodes before
+            V h[2 * W - 2 + (W == 1)];                             // x from 2 (W-1) nodes before
 #pragma unroll
             for (int j = 0; j < 2 * (W - 1); ++j)
-                widen<T, VEC>(h[j], x_at<T, VEC, W>(xr, s.x_node, win, at.t0 - 2 * (W - 1) + j, s.length, s.channels));
+                h[j] = widen_v<T, VEC>(x_at<T, VEC, W>(xr, s.x_node, win, at.t0 - 2 * (W - 1) + j, s.length, s.channels));
 #pragma unroll
             for (int k = 0; k < W - 1; ++k) {
                 const int64_t t = at.t0 - (W - 1) + k;
                 const bool inside = t >= 0 && t < s.length;
-                float gv[VEC];
-                widen<T, VEC>(gv, pack_at<T, VEC>(gr + t * s.gy_node, inside));
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    float xv[W];
-#pragma unroll
-                    for (int j = 0; j < W; ++j) xv[j] = h[k + j][i];
-                    g[GROUP + k][i] = inside ? slope(gv[i], xv, i) : 0.f;
-                    xs[GROUP + k][i] = h[W - 1 + k][i];
-                }
+                const V gv = widen_v<T, VEC>(pack_at<T, VEC>(gr + t * s.gy_node, inside));
+                g[GROUP + k] = inside ? slope(gv, h + k) : zero;
+                xs[GROUP + k] = h[W - 1 + k];
             }
         }
         T* gxp = gx + (at.b * s.length + at.t0 - (W - 1)) * s.channels + c;      // of the thread's first position
         int slot = 0;
         for (int t = 0; t < total; t += GROUP) {
 #pragma unroll
-            for (int j = 0; j < W - 1; ++j)
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) { xs[j][i] = xs[GROUP + j][i]; g[j][i] = g[GROUP + j][i]; }
+            for (int j = 0; j < W - 1; ++j) { xs[j] = xs[GROUP + j]; g[j] = g[GROUP + j]; }
             if (F::ASYNC) {
                 fx.request((slot + AHEAD - 1) % AHEAD);
                 fg.request((slot + AHEAD - 1) % AHEAD);
@@ -262,8 +257,8 @@ __global__ void __launch_bounds__(CONV_THREADS) conv_bwd_kernel(
             }
 #pragma unroll
             for (int k = 0; k < GROUP; ++k) {
-                widen<T, VEC>(xs[W - 1 + k], fx.get(slot, k));
-                widen<T, VEC>(g[W - 1 + k], fg.get(slot, k));
+                xs[W - 1 + k] = widen_v<T, VEC>(fx.get(slot, k));
+                g[W - 1 + k] = widen_v<T, VEC>(fg.get(slot, k));
             }
             if (F::ASYNC) slot = (slot + 1) % AHEAD;
             else { fx.request(0); fg.request(0); }
@@ -273,42 +268,28 @@ __global__ void __launch_bounds__(CONV_THREADS) conv_bwd_kernel(
 #pragma unroll
                 for (int k = 0; k < GROUP; ++k) {
                     const bool inside = INNER || t + k < nodes;
+                    const V d = inside ? slope(g[W - 1 + k], xs + k) : zero;   // not a product: x may hold NaN
+                    g[W - 1 + k] = d;
+                    if (inside) {
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i) {
-                        float xv[W];
-#pragma unroll
-                        for (int j = 0; j < W; ++j) xv[j] = xs[k + j][i];
-                        const float d = inside ? slope(g[W - 1 + k][i], xv, i) : 0.f;   // not a product: x may hold NaN
-                        g[W - 1 + k][i] = d;
-                        if (inside) {
-#pragma unroll
-                            for (int j = 0; j < W; ++j) acc[i][j] = fmaf(d, xv[j], acc[i][j]);
-                            acc[i][W] += d;
-                        }
+                        for (int j = 0; j < W; ++j) acc[j] = fma_v(d, xs[k + j], acc[j]);
+                        acc[W] = add_v(acc[W], d);
                     }
-                    float v[VEC];
+                    V v = mul_v(w[0], g[W - 1 + k]);
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i) {
-                        v[i] = 0.f;
-#pragma unroll
-                        for (int j = 0; j < W; ++j) v[i] = fmaf(w[i][j], g[W - 1 + k - j][i], v[i]);
-                    }
+                    for (int j = 1; j < W; ++j) v = fma_v(w[j], g[W - 1 + k - j], v);
                     if (INNER) {
-                        store_pack<T, VEC>(gxp + k * (int64_t)s.channels, v);
+                        store_v<T, VEC>(gxp + k * (int64_t)s.channels, v);
                         continue;
                     }
                     const int64_t f = at.t0 + t + k;
                     if (t + k >= total) continue;
-                    if (f >= s.length && gstate_out != nullptr) {      // entry f - length of the window that was left
-                        float e[VEC];
-                        widen<T, VEC>(e, load_pack<T, VEC>(gstate_out + (at.b * (W - 1) + (f - s.length)) * s.channels + c));
-#pragma unroll
-                        for (int i = 0; i < VEC; ++i) v[i] += e[i];
-                    }
+                    if (f >= s.length && gstate_out != nullptr)        // entry f - length of the window that was left
+                        v = add_v(v, widen_v<T, VEC>(load_pack<T, VEC>(gstate_out + (at.b * (W - 1) + (f - s.length)) * s.channels + c)));
                     if (f >= W - 1) {
-                        if (gx != nullptr) store_pack<T, VEC>(gxp + k * (int64_t)s.channels, v);
+                        if (gx != nullptr) store_v<T, VEC>(gxp + k * (int64_t)s.channels, v);
                     } else if (gstate != nullptr) {
-                        store_pack<T, VEC>(gstate + (at.b * (W - 1) + f) * s.channels + c, v);
+                        store_v<T, VEC>(gstate + (at.b * (W - 1) + f) * s.channels + c, v);
                     }
                 }
             };
@@ -318,9 +299,12 @@ __global__ void __launch_bounds__(CONV_THREADS) conv_bwd_kernel(
         }
     }
 #pragma unroll
-    for (int i = 0; i < VEC; ++i)
+    for (int j = 0; j <= W; ++j) {
+        float v[VEC];
+        to_array(v, acc[j]);
 #pragma unroll
-        for (int j = 0; j <= W; ++j) sums[threadIdx.y][i * (W + 1) + j][threadIdx.x] = acc[i][j];
+        for (int i = 0; i < VEC; ++i) sums[threadIdx.y][i * (W + 1) + j][threadIdx.x] = v[i];
+    }
     __syncthreads();
     const int c0 = c - threadIdx.x * VEC;
     float* out = partial + (at.b * s.spans + at.span) * (int64_t)s.channels * (W + 1) + (int64_t)c0 * (W + 1);
