@@ -59,9 +59,11 @@ def orthogonalize(grad, steps=5, eps=1e-7):
     (a, b, c) = (3.4445, -4.775, 2.0315), on the shorter side.  Returns a dense tensor of grad's type."""
     a, g = _plan(("ortho", steps, eps, _lay(grad)), grad, steps, eps)
     dev = grad.device
-    out = torch.empty(grad.shape, dtype=grad.dtype, device=dev)
-    ws = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=dev)
-    a.grad, a.out, a.workspace = g.data_ptr(), out.data_ptr(), ws.data_ptr()
+    out = torch.empty_like(grad) if grad.is_contiguous() else torch.empty(grad.shape, dtype=grad.dtype, device=dev)
+    a.grad, a.out = g.data_ptr(), out.data_ptr()
+    if a.workspace_bytes:
+        ws = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=dev)
+        a.workspace = ws.data_ptr()
     B_.call_with("fpde_orthogonalize", a, dev.index)
     return out
 
@@ -84,9 +86,11 @@ def muon_step(weight, grad, momentum, lr, momentum_decay=0.95, weight_decay=0.0,
         raise ValueError("weight and momentum are updated in place and must be contiguous")
     a, g = _plan(("muon", steps, eps, _lay(grad)), grad, steps, eps)
     dev = weight.device
-    ws = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=dev)
     a.nesterov = int(nesterov)
-    a.grad, a.weight, a.momentum, a.workspace = g.data_ptr(), weight.data_ptr(), momentum.data_ptr(), ws.data_ptr()
+    a.grad, a.weight, a.momentum = g.data_ptr(), weight.data_ptr(), momentum.data_ptr()
+    if a.workspace_bytes:
+        ws = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=dev)
+        a.workspace = ws.data_ptr()
     a.lr, a.momentum_decay, a.weight_decay = lr, momentum_decay, weight_decay
     B_.call_with("fpde_muon_step", a, dev.index)
     torch.autograd.graph.increment_version((weight, momentum))    # they changed behind autograd's back

@@ -80,6 +80,15 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _new(like, shape=None):
+    """A dense tensor of `like`'s type, shape (or `shape`) and device."""
+    if like is None:
+        return None
+    if shape is None and like.is_contiguous():
+        return torch.empty_like(like)            # a third of empty()'s host time
+    return torch.empty(like.shape if shape is None else shape, dtype=like.dtype, device=like.device)
+
+
 _plans = B_.ArgPlans()
 _lay = _plans.layout
 
@@ -127,8 +136,8 @@ def causal_conv_fwd(x, weight, bias=None, state=None, silu=True):
         if _same(given, (x, weight, bias, state)):
             _plans.keep(key, a)
     dev = x.device
-    y = torch.empty(x.shape, dtype=x.dtype, device=dev)
-    left = torch.empty((a.batch, a.width - 1, a.channels), dtype=x.dtype, device=dev)
+    y = _new(x)
+    left = _new(x, (a.batch, a.width - 1, a.channels)) if state is None else _new(state)
     a.x, a.weight, a.bias, a.state = x.data_ptr(), weight.data_ptr(), _ptr(bias), _ptr(state)
     a.y, a.state_out = y.data_ptr(), left.data_ptr()
     B_.call_with("fpde_causal_conv_fwd", a, dev.index)
@@ -145,11 +154,8 @@ def causal_conv_bwd(gy, x, weight, bias=None, state=None, silu=True, gstate=None
         if _same(given, taken):
             _plans.keep(key, a)
         x, weight, bias, state, gy, gstate = taken
-    dev, dt, f = x.device, x.dtype, torch.float32
-    gx = torch.empty(x.shape, dtype=dt, device=dev)
-    gw = torch.empty((a.channels, a.width), dtype=f, device=dev)
-    gb = None if bias is None else torch.empty((a.channels,), dtype=f, device=dev)
-    gs = None if state is None else torch.empty((a.batch, a.width - 1, a.channels), dtype=dt, device=dev)
+    dev = x.device
+    gx, gw, gb, gs = _new(x), _new(weight), _new(bias), _new(state)
     ws = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=dev)
     a.x, a.weight, a.bias, a.state = x.data_ptr(), weight.data_ptr(), _ptr(bias), _ptr(state)
     a.gy, a.gstate_out, a.gx, a.gstate = gy.data_ptr(), _ptr(gstate), gx.data_ptr(), _ptr(gs)
@@ -167,7 +173,7 @@ def causal_conv_step(x, window, weight, bias=None, silu=True):
         a, (x, weight, bias, _, _, _) = _conv_args(x, weight, bias, window, silu, True)
         if _same(given, (x, weight, bias)):
             _plans.keep(key, a)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    y = _new(x)
     a.x, a.weight, a.bias, a.y = x.data_ptr(), weight.data_ptr(), _ptr(bias), y.data_ptr()
     a.state = a.state_out = window.data_ptr()
     B_.call_with("fpde_causal_conv_step", a, x.device.index)
@@ -261,9 +267,9 @@ def selective_scan_fwd(u, delta, A, B, C, D=None, z=None, delta_bias=None, delta
         if _same(t, taken):
             _plans.keep(key, a)
         t = taken[:9]
-    dev, f = t[0].device, torch.float32
-    out = torch.empty(u.shape, dtype=u.dtype, device=dev)
-    last = torch.empty((a.batch, a.channels, a.states), dtype=f, device=dev)
+    dev = u.device
+    out = _new(u)
+    last = _new(A, (a.batch, a.channels, a.states)) if state is None else _new(state)
     _scan_pointers(a, *t)
     a.out, a.state_out = out.data_ptr(), last.data_ptr()
     kept = None
@@ -292,13 +298,10 @@ def selective_scan_bwd(gout, u, delta, A, B, C, D=None, z=None, delta_bias=None,
         if _same(t, taken):
             _plans.keep(key, a)
         t = taken
-    dev, dt, f = u.device, u.dtype, torch.float32
+    dev = u.device
     if kept.device != dev:
         raise ValueError("kept is on %s, expected %s" % (kept.device, dev))
-
-    def new(like, dtype):
-        return None if like is None else torch.empty(like.shape, dtype=dtype, device=dev)
-    g = ScanGrads(new(u, dt), new(u, dt), new(A, f), new(B, dt), new(C, dt), new(D, f), new(z, dt), new(delta_bias, f), new(state, f))
+    g = ScanGrads(_new(u), _new(delta), _new(A), _new(B), _new(C), _new(D), _new(z), _new(delta_bias), _new(state))
     _scan_pointers(a, *t[:9])
     a.gout, a.gstate_out = t[9].data_ptr(), _ptr(t[10])
     a.gu, a.gdelta, a.gA, a.gB, a.gC = g.u.data_ptr(), g.delta.data_ptr(), g.A.data_ptr(), g.B.data_ptr(), g.C.data_ptr()
@@ -321,7 +324,7 @@ def selective_scan_step(state, u, delta, A, B, C, D=None, z=None, delta_bias=Non
         if _same(t, taken):
             _plans.keep(key, a)
         t = taken[:9]
-    out = torch.empty(u.shape, dtype=u.dtype, device=u.device)
+    out = _new(u)
     _scan_pointers(a, *t)
     a.state_out, a.out = state.data_ptr(), out.data_ptr()
     B_.call_with("fpde_selective_scan_step", a, u.device.index)

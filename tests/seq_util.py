@@ -75,7 +75,7 @@ def ortho_ref(g, steps, eps):
 
 
 class GuardedTorch:
-    """Stands in for `torch` in a module under test: every tensor it gets from `empty` has canaries on both
+    """Stands in for `torch` in a module under test: every tensor it gets from `empty` or `empty_like` has canaries on both
     sides and starts as NaN (so that what is not written shows)."""
 
     def __init__(self):
@@ -96,6 +96,9 @@ class GuardedTorch:
         body.fill_(0xFF)                 # NaN in every floating type
         self.all.append((raw, lead, n * e))
         return body.view(dtype).view(*[int(k) for k in shape]) if n else torch.empty(*shape, dtype=dtype, device=device)
+
+    def empty_like(self, t):
+        return self.empty(t.shape, dtype=t.dtype, device=t.device)
 
     def check(self):
         for raw, lead, n in self.all:
