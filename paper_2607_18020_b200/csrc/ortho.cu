@@ -286,6 +286,8 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
         for (int i = 0; i < R::STAGES; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(done + 8 * i, 1); mbar_init(freed + 8 * i, CG * EPILOGUE_WARPS); }
         mbar_fence_init();
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&left) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&right) : "memory");
     }
     if (warp == 1) {
         if constexpr (CG == 1) {
@@ -385,6 +387,19 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
             __half* hi = out + 2 * k * out_plane;
             __half* lo = hi + out_plane;
             const __half* add = KIND == GRAM ? nullptr : added + 2 * k * out_plane + (int64_t)row * s.cols;
+            Pack<__half, 8> ph[4] = {}, pl[4] = {};
+            auto fetch = [&](int c) {                      // the added term of 32 columns: on its way while the sums are formed
+                if constexpr (KIND != GRAM) {
+                    const int col = j0 + c;
+                    if (row >= s.mp || col >= s.cols) return;
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        ph[g] = load_pack<__half, 8>(add + col + 8 * g);
+                        pl[g] = load_pack<__half, 8>(add + out_plane + col + 8 * g);
+                    }
+                }
+            };
+            fetch(half * 32);
             mbar_wait(done + 8 * acc, acc_phase, gave_up, &g_ortho_timeouts);
             __syncwarp();                                  // the reads of TMEM are the whole warp's
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -392,14 +407,7 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
             for (int c = half * 32; c < BN; c += 64) {
                 const int col = j0 + c;
                 const bool there = row < s.mp && col < s.cols;       // the same for the whole warp: extents are multiples of 64
-                Pack<__half, 8> ph[4] = {}, pl[4] = {};
-                if (KIND != GRAM && there) {
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        ph[g] = load_pack<__half, 8>(add + col + 8 * g);
-                        pl[g] = load_pack<__half, 8>(add + out_plane + col + 8 * g);
-                    }
-                }
+                if (c != half * 32) fetch(c);
                 float v[32];
                 const uint32_t at = tmem + acc * R::SET + c + ((uint32_t)(quarter * 32) << 16);
                 tmem_load32(at, v);
@@ -545,7 +553,7 @@ cudaError_t run_product(const Maps& left, const Maps& right, const __half* added
 // (S in columns 0-127, S S in 128-255, P X from 256 on).  One launch instead of three per step and three
 // around them; what bounds it is the chain of 3 x steps products, each of which waits for the one before.
 // The planes of X, rows of 64-column blocks, serve as K-major factor of S and as MN-major factor of P X.
-constexpr int SMALL_M = 128, SMALL_N = 256, SMALL_THREADS = 256;
+constexpr int SMALL_M = 128, SMALL_N = 256, SMALL_THREADS = 512;
 constexpr int SMALL_BLOCK = SMALL_M * 128;              // bytes of a 64-column block of a plane
 constexpr int SMALL_S = 4 * SMALL_BLOCK;                // S: two blocks, hi and lo
 inline size_t small_bytes(int np) { return 2 * (size_t)(np / 64) * SMALL_BLOCK + SMALL_S + 1024; }
@@ -571,7 +579,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bar;
     __shared__ uint32_t tmem_slot;
-    __shared__ double part[8];
+    __shared__ double part[SMALL_THREADS / 32];
     uint8_t* base = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
     const int xplane = io.np / 64 * SMALL_BLOCK;
     uint8_t *xh = base, *xl = base + xplane, *sh = base + 2 * xplane, *sl = sh + 2 * SMALL_BLOCK;
@@ -590,7 +598,9 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
     const T* g = (const T*)io.grad + k * io.grad_matrix;
     float* mom = io.momentum ? io.momentum + k * io.rows * io.cols : nullptr;
     double sum = 0.0;
+#pragma unroll 2
     for (int r = warp; r < io.rows; r += SMALL_THREADS / 32)
+#pragma unroll 4
         for (int c = lane; c < io.cols; c += 32) {
             float u = to_f32<T>(g[r * io.grad_row + c]);
             if (mom != nullptr) {
@@ -609,7 +619,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
     const uint32_t tmem = tmem_slot;
     sum = 0.0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum += part[i];
+    for (int i = 0; i < SMALL_THREADS / 32; ++i) sum += part[i];
     const float scale = (float)(1.0 / (sqrt(sum) + io.eps)) * SCALE;
     // the first X, zeros around it
     {
@@ -629,7 +639,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
 
     const uint32_t axh = smem_u32(xh), axl = smem_u32(xl), ash = smem_u32(sh), asl = smem_u32(sl);
     const int deep_m = (io.m + 15) / 16, deep_n = (io.n + 15) / 16;      // 16-deep pieces that are not all zeros
-    const int quarter = warp % 4, half = warp / 4, row = quarter * 32 + lane;
+    const int quarter = warp % 4, part_of = warp / 4, row = quarter * 32 + lane;      // TMEM lanes; which columns
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     uint32_t phase = 0;
     bool gave_up = false;
@@ -662,8 +672,8 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
             mma_commit(smem_u32(&bar));
         }
         finish();
-#pragma unroll 1
-        for (int c = half * 64; c < half * 64 + 64; c += 32) {
+        {
+            const int c = part_of * 32;
             float v[32];
             tmem_load32(tmem + lanes + c, v);
 #pragma unroll
@@ -688,8 +698,8 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
             mma_commit(smem_u32(&bar));
         }
         finish();
-#pragma unroll 1
-        for (int c = half * 64; c < half * 64 + 64; c += 32) {            // P over S, which has been read
+        {                                                                 // P over S, which has been read
+            const int c = part_of * 32;
             float v[32], w2[32];
             tmem_load32(tmem + lanes + c, v);
             tmem_load32(tmem + lanes + 128 + c, w2);
@@ -716,7 +726,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
         }
         finish();
 #pragma unroll 1
-        for (int c = half * 32; c < io.np; c += 64) {
+        for (int c = part_of * 32; c < io.np; c += 128) {
             float v[32];
             tmem_load32(tmem + lanes + 256 + c, v);
 #pragma unroll

@@ -27,12 +27,17 @@
 namespace fpde {
 namespace {
 
-constexpr int FWD_THREADS = 64, BACK_THREADS = 128, STEP_THREADS = 128, STEP_CHANNELS = 4;
+constexpr int STEP_THREADS = 128, STEP_CHANNELS = 4;
+constexpr int FWD_LANES = 32, BACK_LANES = 64;     // channels of a block with 4 lanes a channel: threads = that x 4 / NC
 constexpr int FWD_UNROLL = 4;
 constexpr int TILE = 16;          // nodes brought to shared memory together
 constexpr int KEEP = 8;           // nodes between stored states: what the backward march holds in registers
-constexpr int NS = 4, NC = 2;     // states and channels of a thread
-constexpr int FWD_BLOCKS = 7, BACK_BLOCKS = 3;     // resident blocks that the registers are budgeted for
+constexpr int NS = 4;             // states of a thread; it has NC = 1 or 2 channels
+// resident blocks that the registers are budgeted for
+__host__ __device__ constexpr int fwd_blocks(int nc) { return nc == 2 ? 7 : 5; }
+__host__ __device__ constexpr int back_blocks(int nc) { return nc == 2 ? 3 : 2; }
+__host__ __device__ constexpr int fwd_threads(int nc) { return FWD_LANES * 4 / nc; }
+__host__ __device__ constexpr int back_threads(int nc) { return BACK_LANES * 4 / nc; }
 
 struct ScanShape {
     int64_t length;
@@ -177,18 +182,19 @@ __device__ __forceinline__ int sum_lanes(float (&v)[N], int lane) {
     return from;
 }
 
-// Sums over the states of four nodes k0 .. k0+3 of the thread's two channels (value 2 * node + channel)
-// to dst[node][channel].
-template <int S, int CT>
+// Sums over the states of four nodes k0 .. k0+3 of the thread's channels (value NC * node + channel) to
+// dst[node][channel].
+template <int S, int NC, int CT>
 __device__ __forceinline__ void put_sums(float (*dst)[CT], float (&v)[4 * NC], int k0, int c, int q) {
     const int from = sum_lanes<4 * NC, S / 2, 1>(v, q);
-    constexpr int LEFT = sums_left<4 * NC, S / 2, 1>();
+    constexpr int LEFT = sums_left<4 * NC, S / 2, 1>(), SHARE = S > 4 * NC ? S / (4 * NC) : 1;      // lanes with the same sum
     float* at = &dst[k0 + from / NC][c];
-    if constexpr (LEFT >= NC) {
+    if constexpr (LEFT >= NC && NC == 2) {
 #pragma unroll
-        for (int i = 0; i < LEFT / NC; ++i) *reinterpret_cast<float2*>(at + i * CT) = make_float2(v[NC * i], v[NC * i + 1]);
-    } else if (S <= 8 || q % 2 == 0) {
-        at[from % NC] = v[0];
+        for (int i = 0; i < LEFT / 2; ++i) *reinterpret_cast<float2*>(at + i * CT) = make_float2(v[2 * i], v[2 * i + 1]);
+    } else if (SHARE == 1 || q % SHARE == 0) {
+#pragma unroll
+        for (int i = 0; i < LEFT; ++i) at[i * CT + from % NC] = v[i];
     }
 }
 
@@ -213,12 +219,12 @@ __device__ __forceinline__ void put_twice(float2* at, const float (&v)[N]) {
 }
 
 // The pairs of the thread's channels.
-__device__ __forceinline__ void get_channels(uint64_t (&v)[NC], const float2* at) {
-    static_assert(NC == 2, "read as one quad");
+__device__ __forceinline__ void get_channels(uint64_t (&v)[2], const float2* at) {
     const Quad q = quad_at(&at->x);
     v[0] = q.lo;
     v[1] = q.hi;
 }
+__device__ __forceinline__ void get_channels(uint64_t (&v)[1], const float2* at) { v[0] = *reinterpret_cast<const uint64_t*>(at); }
 
 // Four states from memory, or what stands in for those that do not exist.
 __device__ __forceinline__ Quad load_states(const float* p, int n, int states, float scale) {
@@ -241,11 +247,11 @@ __device__ __forceinline__ void store_states(float* p, int n, int states, bool p
 }
 
 // ------------------------------------------------------------------------------------------ forward
-template <typename T, int S, int VEC, bool ENDS>
+template <typename T, int S, int NC, int VEC, bool ENDS>
 struct FwdSpace {
-    static constexpr int CT = FWD_THREADS / S * NC, NP = S * NS;
-    static constexpr int RP = FWD_THREADS / (CT / VEC), RN = FWD_THREADS / NP;      // rows at a time
-    using Act = Feed<T, VEC, TILE, RP, ENDS ? 2 : 3, FWD_THREADS>;
+    static constexpr int THREADS = fwd_threads(NC), CT = THREADS / S * NC, NP = S * NS;
+    static constexpr int RP = THREADS / (CT / VEC), RN = THREADS / NP;      // rows at a time
+    using Act = Feed<T, VEC, TILE, RP, ENDS ? 2 : 3, THREADS>;
     __align__(16) float2 sdt[TILE][CT], sdu[TILE][CT];      // dt, dt;  dt u, dt u: pairs as the arithmetic wants them
     __align__(16) float sb[TILE][NP], sc[ENDS ? 1 : TILE][NP];
     __align__(8) float sy[ENDS ? 1 : TILE][CT];
@@ -255,12 +261,12 @@ struct FwdSpace {
 // ENDS = false: the march.  ENDS = true, for rows cut into chunks: only what the join needs,
 // local[b][chunk][channel][state] = state at the chunk's end when it starts from zero and
 // sums[b][chunk][channel] = sum of dt.
-template <typename T, int S, int VEC, bool ENDS>
-__global__ void __launch_bounds__(FWD_THREADS, FWD_BLOCKS) scan_fwd_kernel(ScanIn<T> in, const float* __restrict__ state, const float* __restrict__ enter,
+template <typename T, int S, int NC, int VEC, bool ENDS>
+__global__ void __launch_bounds__(fwd_threads(NC), fwd_blocks(NC)) scan_fwd_kernel(ScanIn<T> in, const float* __restrict__ state, const float* __restrict__ enter,
                                                            T* __restrict__ out, float* __restrict__ state_out, float* __restrict__ kept,
                                                            float* __restrict__ local, float* __restrict__ sums, ScanShape s) {
     pdl_wait_then_trigger();
-    using Space = FwdSpace<T, S, VEC, ENDS>;
+    using Space = FwdSpace<T, S, NC, VEC, ENDS>;
     using Act = typename Space::Act;
     constexpr int CT = Space::CT, NP = Space::NP, CP = CT / VEC, RP = Space::RP, RN = Space::RN;
     enum { U, DELTA, Z };
@@ -369,7 +375,7 @@ __global__ void __launch_bounds__(FWD_THREADS, FWD_BLOCKS) scan_fwd_kernel(ScanI
                     }
                 }
             }
-            if constexpr (!ENDS) put_sums<S, CT>(m.sy, y, k0, cl, q);
+            if constexpr (!ENDS) put_sums<S, NC, CT>(m.sy, y, k0, cl, q);
         }
         __syncthreads();
         if constexpr (!ENDS) {
@@ -448,15 +454,15 @@ __global__ void __launch_bounds__(256) scan_join_kernel(float* __restrict__ loca
 
 // ----------------------------------------------------------------------------------------- backward
 // What one block keeps in shared memory.
-template <typename T, int S, int VEC>
+template <typename T, int S, int NC, int VEC>
 struct BackSpace {
-    static constexpr int CT = BACK_THREADS / S * NC, NP = S * NS, WARPS = BACK_THREADS / 32;
+    static constexpr int THREADS = back_threads(NC), CT = THREADS / S * NC, NP = S * NS, WARPS = THREADS / 32;
     __align__(16) float2 sdt[TILE][CT], sdu[TILE][CT], sg[TILE][CT];     // dt, dt;  dt u, dt u;  gy, gy
     __align__(16) float sb[TILE][NP], sc[TILE][NP];
     __align__(8) float sy[TILE][CT], st[TILE][CT], sq[TILE][CT];         // C.h, p.B, sum p a h A
     float red[WARPS][TILE][2 * NP];                         // the warps' sums over channels: gB, gC
-    static constexpr int RP = BACK_THREADS / (CT / VEC), RN = BACK_THREADS / NP;
-    using Act = Feed<T, VEC, TILE, RP, 4, BACK_THREADS>;
+    static constexpr int RP = THREADS / (CT / VEC), RN = THREADS / NP;
+    using Act = Feed<T, VEC, TILE, RP, 4, THREADS>;
     typename Act::Space room;
 };
 
@@ -464,16 +470,16 @@ struct BackSpace {
 // this chunk's share of gA, gD and gdelta_bias.
 // ENDS = true, for rows cut into chunks: only local = what the adjoint state hands to the node before the
 // chunk when nothing comes from behind it, and the sums of dt.
-template <typename T, int S, int VEC, bool ENDS>
-__global__ void __launch_bounds__(BACK_THREADS, BACK_BLOCKS) scan_bwd_kernel(ScanIn<T> in, const float* __restrict__ kept, const float* __restrict__ enter,
+template <typename T, int S, int NC, int VEC, bool ENDS>
+__global__ void __launch_bounds__(back_threads(NC), back_blocks(NC)) scan_bwd_kernel(ScanIn<T> in, const float* __restrict__ kept, const float* __restrict__ enter,
                                                                 const float* __restrict__ gstate_out, T* __restrict__ gu,
                                                                 T* __restrict__ gdelta, T* __restrict__ gz, float* __restrict__ gstate,
                                                                 float* __restrict__ part_bc, float* __restrict__ part_a,
                                                                 float* __restrict__ local, float* __restrict__ sums, int64_t rows, ScanShape s) {
     pdl_wait_then_trigger();
-    using Space = BackSpace<T, S, VEC>;
+    using Space = BackSpace<T, S, NC, VEC>;
     using Act = typename Space::Act;
-    constexpr int CT = Space::CT, NP = Space::NP, CP = CT / VEC, RP = Space::RP, RN = Space::RN;
+    constexpr int THREADS = Space::THREADS, CT = Space::CT, NP = Space::NP, CP = CT / VEC, RP = Space::RP, RN = Space::RN;
     enum { DELTA, Z, GOUT, U };
     using Bc = States<T, TILE, RN>;
     extern __shared__ __align__(16) uint8_t raw_space[];
@@ -619,7 +625,7 @@ __global__ void __launch_bounds__(BACK_THREADS, BACK_BLOCKS) scan_bwd_kernel(Sca
                             y[NC * j + k] = sum2(fma2(c4.lo, hs[r + 1][k].lo, mul2(c4.hi, hs[r + 1][k].hi)));
                         }
                     }
-                    put_sums<S, CT>(m.sy, y, base + k0, cl, q);
+                    put_sums<S, NC, CT>(m.sy, y, base + k0, cl, q);
                 }
                 // and backwards
 #pragma unroll
@@ -662,8 +668,8 @@ __global__ void __launch_bounds__(BACK_THREADS, BACK_BLOCKS) scan_bwd_kernel(Sca
                         for (int i = 0; i < sums_left<2 * NS, 16, S>(); ++i)
                             m.red[warp][base + r][((from + i) / NS) * NP + q * NS + (from + i) % NS] = v[i];
                     }
-                    put_sums<S, CT>(m.st, tb, base + k0, cl, q);
-                    put_sums<S, CT>(m.sq, ta, base + k0, cl, q);
+                    put_sums<S, NC, CT>(m.st, tb, base + k0, cl, q);
+                    put_sums<S, NC, CT>(m.sq, ta, base + k0, cl, q);
                 }
             }
             __syncthreads();
@@ -699,7 +705,7 @@ __global__ void __launch_bounds__(BACK_THREADS, BACK_BLOCKS) scan_bwd_kernel(Sca
                 store_pack<T, VEC>(gdelta + o, od);
                 if (in.z) store_pack<T, VEC>(gz + o, oz);
             }
-            for (int e = tid; e < here * 2 * NP; e += BACK_THREADS) {
+            for (int e = tid; e < here * 2 * NP; e += THREADS) {
                 const int r = e / (2 * NP), k = e % (2 * NP);
                 float v = 0.f;
 #pragma unroll
@@ -733,8 +739,8 @@ __global__ void __launch_bounds__(BACK_THREADS, BACK_BLOCKS) scan_bwd_kernel(Sca
                 }
         }
         // threads tid, tid + CP, ... hold sums of the same channels
-        float(*fin)[BACK_THREADS] = reinterpret_cast<float(*)[BACK_THREADS]>(raw_space);     // 2 VEC rows
-        static_assert(2 * sizeof(m.sdt) >= 2 * VEC * BACK_THREADS * sizeof(float), "room for the sums of every thread");
+        float(*fin)[THREADS] = reinterpret_cast<float(*)[THREADS]>(raw_space);     // 2 VEC rows
+        static_assert(2 * sizeof(m.sdt) >= 2 * VEC * THREADS * sizeof(float), "room for the sums of every thread");
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
@@ -744,7 +750,7 @@ __global__ void __launch_bounds__(BACK_THREADS, BACK_BLOCKS) scan_bwd_kernel(Sca
         __syncthreads();
         if (tid < CT && c0 + tid < s.channels) {
             float v0 = 0.f, v1 = 0.f;
-            for (int e = tid / VEC; e < BACK_THREADS; e += CP) { v0 += fin[tid % VEC][e]; v1 += fin[VEC + tid % VEC][e]; }
+            for (int e = tid / VEC; e < THREADS; e += CP) { v0 += fin[tid % VEC][e]; v1 += fin[VEC + tid % VEC][e]; }
             pa[(int64_t)(c0 + tid) * (s.states + 2) + s.states] = v0;
             pa[(int64_t)(c0 + tid) * (s.states + 2) + s.states + 1] = v1;
         }
@@ -890,14 +896,14 @@ ScanShape shape_of(const fpde_scan_args* a) {
 // The plan depends on sizes only, so that the forward and the backward call agree on it.
 ScanShape plan(const fpde_scan_args* a, bool backward) {
     ScanShape s = shape_of(a);
-    s.tiles = (int)ceil_div(a->channels, (backward ? BACK_THREADS : FWD_THREADS) / lanes_of(a->states) * NC);
+    s.tiles = (int)ceil_div(a->channels, (backward ? BACK_LANES : FWD_LANES) * 4 / lanes_of(a->states));
     s.kept_nodes = ceil_div(a->length, KEEP);
     // Chunks.  The blocks run in waves of `resident` per SM, and a wave takes as long as its nodes: the marches
     // are bound by latency, so fewer blocks on an SM are hardly faster.  Splitting adds the pass that forms
     // the chunks' ends, a share `ends_cost` of the march, and two launches, worth about 80 nodes.  The
     // cheapest number of chunks wins, the fewest of equals.
     const int64_t length = a->length > 0 ? a->length : 1, blocks = a->batch * s.tiles;
-    const int64_t resident = 148 * (backward ? BACK_BLOCKS : FWD_BLOCKS);
+    const int64_t resident = 148 * (backward ? back_blocks(2) : fwd_blocks(2));
     const double ends_cost = backward ? 0.3 : 0.5;
     const int64_t most = ceil_div(length, 2 * TILE) < 1024 ? ceil_div(length, 2 * TILE) : 1024;
     int64_t chunk = length;
@@ -985,9 +991,8 @@ bool scan_pairs(const fpde_scan_args* a, bool backward) {
     return ok && packs(a->gout, a->gout_batch, a->gout_node, e, 2) && aligned(a->gu, 2 * e) && aligned(a->gdelta, 2 * e) && aligned(a->gz, 2 * e);
 }
 
-template <typename T, int S, int VEC>
-cudaError_t run_fwd(const fpde_scan_args* a, cudaStream_t st) {
-    const ScanShape s = plan(a, false);
+template <typename T, int S, int NC, int VEC>
+cudaError_t run_fwd(const fpde_scan_args* a, const ScanShape& s, cudaStream_t st) {
     const ScanSpace w = space(a, s, false);
     const ScanIn<T> in = inputs<T>(a);
     const int64_t blocks = a->batch * s.tiles * s.chunks;
@@ -997,54 +1002,46 @@ cudaError_t run_fwd(const fpde_scan_args* a, cudaStream_t st) {
     if (s.chunks > 1) {
         local = (float*)((char*)a->workspace + w.local);
         float* sums = (float*)((char*)a->workspace + w.sums);
-        constexpr size_t bytes = sizeof(FwdSpace<T, S, VEC, true>);
-        {
-    static std::atomic<uint64_t> allowed{0};
-    FPDE_TRY(allow_smem(scan_fwd_kernel<T, S, VEC, true>, bytes, allowed));
-    }
-        FPDE_TRY(launch_kernel_smem(scan_fwd_kernel<T, S, VEC, true>, grid, dim3(FWD_THREADS), bytes, st, in, (const float*)nullptr, (const float*)nullptr,
+        constexpr size_t bytes = sizeof(FwdSpace<T, S, 1, VEC, true>);
+        static std::atomic<uint64_t> allowed{0};
+        FPDE_TRY(allow_smem(scan_fwd_kernel<T, S, 1, VEC, true>, bytes, allowed));
+        FPDE_TRY(launch_kernel_smem(scan_fwd_kernel<T, S, 1, VEC, true>, grid, dim3(fwd_threads(1)), bytes, st, in, (const float*)nullptr, (const float*)nullptr,
                                (T*)nullptr, (float*)nullptr, (float*)nullptr, local, sums, s));
         FPDE_TRY(launch_kernel(scan_join_kernel<false>, dim3((unsigned)ceil_div(a->batch * s.channels * s.states, 256)), dim3(256), st,
                                local, (const float*)sums, a->A, a->state, a->batch, s));
     }
-    constexpr size_t bytes = sizeof(FwdSpace<T, S, VEC, false>);
-    {
+    constexpr size_t bytes = sizeof(FwdSpace<T, S, NC, VEC, false>);
     static std::atomic<uint64_t> allowed{0};
-    FPDE_TRY(allow_smem(scan_fwd_kernel<T, S, VEC, false>, bytes, allowed));
-    }
-    return launch_kernel_smem(scan_fwd_kernel<T, S, VEC, false>, grid, dim3(FWD_THREADS), bytes, st, in, a->state, (const float*)local, (T*)a->out,
+    FPDE_TRY(allow_smem(scan_fwd_kernel<T, S, NC, VEC, false>, bytes, allowed));
+    return launch_kernel_smem(scan_fwd_kernel<T, S, NC, VEC, false>, grid, dim3(fwd_threads(NC)), bytes, st, in, a->state, (const float*)local, (T*)a->out,
                          a->state_out, (float*)a->kept, (float*)nullptr, (float*)nullptr, s);
 }
 
-template <typename T, int S, int VEC>
-cudaError_t run_bwd(const fpde_scan_args* a, cudaStream_t st) {
-    const ScanShape s = plan(a, true);
+template <typename T, int S, int NC, int VEC>
+cudaError_t run_bwd(const fpde_scan_args* a, const ScanShape& s, cudaStream_t st) {
     const ScanSpace w = space(a, s, true);
     const ScanIn<T> in = inputs<T>(a);
     const int64_t blocks = a->batch * s.tiles * s.chunks;
     if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
     const dim3 grid((unsigned)blocks);
-    constexpr size_t bytes = sizeof(BackSpace<T, S, VEC>);
+    constexpr size_t bytes = sizeof(BackSpace<T, S, NC, VEC>);
     char* ws = (char*)a->workspace;
     float *local = nullptr, *part_bc = (float*)(ws + w.part_bc), *part_a = (float*)(ws + w.part_a);
     if (s.chunks > 1) {
+        constexpr size_t ends = sizeof(BackSpace<T, S, 1, VEC>);
         local = (float*)(ws + w.local);
         float* sums = (float*)(ws + w.sums);
-        {
-    static std::atomic<uint64_t> allowed{0};
-    FPDE_TRY(allow_smem(scan_bwd_kernel<T, S, VEC, true>, bytes, allowed));
-    }
-        FPDE_TRY(launch_kernel_smem(scan_bwd_kernel<T, S, VEC, true>, grid, dim3(BACK_THREADS), bytes, st, in, (const float*)nullptr,
+        static std::atomic<uint64_t> allowed{0};
+        FPDE_TRY(allow_smem(scan_bwd_kernel<T, S, 1, VEC, true>, ends, allowed));
+        FPDE_TRY(launch_kernel_smem(scan_bwd_kernel<T, S, 1, VEC, true>, grid, dim3(back_threads(1)), ends, st, in, (const float*)nullptr,
                                     (const float*)nullptr, (const float*)nullptr, (T*)nullptr, (T*)nullptr, (T*)nullptr, (float*)nullptr,
                                     (float*)nullptr, (float*)nullptr, local, sums, a->batch, s));
         FPDE_TRY(launch_kernel(scan_join_kernel<true>, dim3((unsigned)ceil_div(a->batch * s.channels * s.states, 256)), dim3(256), st,
                                local, (const float*)sums, a->A, a->gstate_out, a->batch, s));
     }
-    {
     static std::atomic<uint64_t> allowed{0};
-    FPDE_TRY(allow_smem(scan_bwd_kernel<T, S, VEC, false>, bytes, allowed));
-    }
-    FPDE_TRY(launch_kernel_smem(scan_bwd_kernel<T, S, VEC, false>, grid, dim3(BACK_THREADS), bytes, st, in, (const float*)a->kept,
+    FPDE_TRY(allow_smem(scan_bwd_kernel<T, S, NC, VEC, false>, bytes, allowed));
+    FPDE_TRY(launch_kernel_smem(scan_bwd_kernel<T, S, NC, VEC, false>, grid, dim3(back_threads(NC)), bytes, st, in, (const float*)a->kept,
                                 (const float*)local, a->gstate_out, (T*)a->gu, (T*)a->gdelta, (T*)a->gz, a->gstate, part_bc, part_a,
                                 (float*)nullptr, (float*)nullptr, a->batch, s));
     if (a->batch * a->length > 0)
@@ -1064,12 +1061,28 @@ cudaError_t run_step(const fpde_scan_args* a, cudaStream_t st) {
                          (int)across, packed, s);
 }
 
+// Up to so many blocks a march gives its threads one channel instead of two: a block then has twice the
+// threads with half the work, which pays while SMs have warps to spare (us, one channel against two:
+// forward 4 blocks 11.6 / 16.3, 512 blocks 25.8 / 29.8, 1024 blocks 313 / 287; backward 256 blocks 70 / 75,
+// 384 blocks 961 / 855).  The pass that only forms the chunks' ends always does (169 / 189, 216 / 213).
+constexpr int64_t FWD_ONE = 148 * 4, BACK_ONE = 148 * 2;
+
 enum Call { CALL_FWD, CALL_BWD, CALL_STEP };
 
 template <typename T, int S>
 cudaError_t run(const fpde_scan_args* a, Call call, cudaStream_t st) {
-    if (call == CALL_FWD) return scan_pairs<T>(a, false) ? run_fwd<T, S, 2>(a, st) : run_fwd<T, S, 1>(a, st);
-    if (call == CALL_BWD) return scan_pairs<T>(a, true) ? run_bwd<T, S, 2>(a, st) : run_bwd<T, S, 1>(a, st);
+    if (call == CALL_FWD) {
+        const ScanShape s = plan(a, false);
+        const bool pairs = scan_pairs<T>(a, false);
+        if (a->batch * s.tiles * s.chunks <= FWD_ONE) return pairs ? run_fwd<T, S, 1, 2>(a, s, st) : run_fwd<T, S, 1, 1>(a, s, st);
+        return pairs ? run_fwd<T, S, 2, 2>(a, s, st) : run_fwd<T, S, 2, 1>(a, s, st);
+    }
+    if (call == CALL_BWD) {
+        const ScanShape s = plan(a, true);
+        const bool pairs = scan_pairs<T>(a, true);
+        if (a->batch * s.tiles * s.chunks <= BACK_ONE) return pairs ? run_bwd<T, S, 1, 2>(a, s, st) : run_bwd<T, S, 1, 1>(a, s, st);
+        return pairs ? run_bwd<T, S, 2, 2>(a, s, st) : run_bwd<T, S, 2, 1>(a, s, st);
+    }
     return run_step<T, S>(a, st);
 }
 
