@@ -249,6 +249,18 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
+// The same, with the cross products' sums `cross` columns further on added.
+template <bool CROSS>
+__device__ __forceinline__ void load_sums(float (&v)[32], uint32_t addr, int cross) {
+    tmem_load32(addr, v);
+    if (CROSS) {
+        float x[32];
+        tmem_load32(addr + cross, x);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] += x[i];
+    }
+}
+
 __device__ unsigned int g_ortho_timeouts;
 
 // Tile number t of one matrix -> first row and column of the tile (CG * 128 rows, BN columns).
@@ -409,14 +421,7 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
                 const bool there = row < s.mp && col < s.cols;       // the same for the whole warp: extents are multiples of 64
                 if (c != half * 32) fetch(c);
                 float v[32];
-                const uint32_t at = tmem + acc * R::SET + c + ((uint32_t)(quarter * 32) << 16);
-                tmem_load32(at, v);
-                if (PAIR) {
-                    float x[32];
-                    tmem_load32(at + BN, x);
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] += x[i];
-                }
+                load_sums<PAIR>(v, tmem + acc * R::SET + c + ((uint32_t)(quarter * 32) << 16), BN);
                 if (!there) continue;
                 const bool both = PAIR || KIND != SQUARE;        // P is only ever a factor
 #pragma unroll
@@ -549,8 +554,10 @@ cudaError_t run_product(const Maps& left, const Maps& right, const __half* added
 
 // --------------------------------------------------------------------------------- small matrices
 // A matrix whose shorter side is at most 128 and whose longer side is at most 256 stays on one SM for the
-// whole call: X and S (then P) as swizzled hi and lo planes in shared memory, the products' sums in TMEM
-// (S in columns 0-127, S S in 128-255, P X from 256 on).  One launch instead of three per step and three
+// whole call: X and S (then P) as swizzled hi and lo planes in shared memory, the products' sums in TMEM,
+// cross products apart.  S S is formed from pairs whatever the type: in matrices this small its factors'
+// rounding is the largest part of the 16-bit types' error (64 x 200: 2.1e-3 of 2.1e-3, 1.2e-3 without it,
+// next to 1.7e-3 from rounding the result to bf16).  One launch instead of three per step and three
 // around them; what bounds it is the chain of 3 x steps products, each of which waits for the one before.
 // The planes of X, rows of 64-column blocks, serve as K-major factor of S and as MN-major factor of P X.
 constexpr int SMALL_M = 128, SMALL_N = 256, SMALL_THREADS = 512;
@@ -657,68 +664,64 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
         __syncthreads();
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     };
-    constexpr uint32_t IDESC = (1u << 4) | ((uint32_t)(SMALL_M / 16) << 24);
+    constexpr uint32_t IDESC = (1u << 4) | ((uint32_t)(SMALL_M / 16) << 24), SQUARE_IDESC = IDESC | (uint32_t)(128 / 8) << 17;
     for (int step = 0; step < steps; ++step) {
-        if (tid == 0) {                                                   // S = X X^T
+        if (tid == 0) {                                                   // S = X X^T: columns 0-127, cross products 128-255
             for (int p = 0; p < deep_n; ++p) {
                 const uint64_t h = k_major(axh, p);
-                mma_f16(tmem, h, h, IDESC | (uint32_t)(128 / 8) << 17, p > 0);
+                mma_f16(tmem, h, h, SQUARE_IDESC, p > 0);
                 if (PAIR) {
                     const uint64_t l = k_major(axl, p);
-                    mma_f16(tmem, h, l, IDESC | (uint32_t)(128 / 8) << 17, true);
-                    mma_f16(tmem, l, h, IDESC | (uint32_t)(128 / 8) << 17, true);
+                    mma_f16(tmem + 128, h, l, SQUARE_IDESC, p > 0);
+                    mma_f16(tmem + 128, l, h, SQUARE_IDESC, true);
                 }
             }
             mma_commit(smem_u32(&bar));
         }
         finish();
+        float kept[32];                                                   // this thread's part of S, times 2^14
         {
             const int c = part_of * 32;
-            float v[32];
-            tmem_load32(tmem + lanes + c, v);
+            load_sums<PAIR>(kept, tmem + lanes + c, 128);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 float w[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) w[i] = v[8 * q + i] * (1.f / SCALE);
+                for (int i = 0; i < 8; ++i) w[i] = kept[8 * q + i] *= 1.f / SCALE;
                 put8(sh, sl, row, c + 8 * q, w);
             }
         }
         written();
-        if (tid == 0) {                                                   // S S
+        if (tid == 0) {                                                   // S S: columns 256-383, cross products 384-511
             for (int p = 0; p < deep_m; ++p) {
-                const uint64_t h = k_major(ash, p);
-                mma_f16(tmem + 128, h, h, IDESC | (uint32_t)(128 / 8) << 17, p > 0);
-                if (PAIR) {
-                    const uint64_t l = k_major(asl, p);
-                    mma_f16(tmem + 128, h, l, IDESC | (uint32_t)(128 / 8) << 17, true);
-                    mma_f16(tmem + 128, l, h, IDESC | (uint32_t)(128 / 8) << 17, true);
-                }
+                const uint64_t h = k_major(ash, p), l = k_major(asl, p);
+                mma_f16(tmem + 256, h, h, SQUARE_IDESC, p > 0);
+                mma_f16(tmem + 384, h, l, SQUARE_IDESC, p > 0);
+                mma_f16(tmem + 384, l, h, SQUARE_IDESC, true);
             }
             mma_commit(smem_u32(&bar));
         }
         finish();
         {                                                                 // P over S, which has been read
             const int c = part_of * 32;
-            float v[32], w2[32];
-            tmem_load32(tmem + lanes + c, v);
-            tmem_load32(tmem + lanes + 128 + c, w2);
+            float v[32];
+            load_sums<true>(v, tmem + lanes + 256 + c, 128);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 float w[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) w[i] = fmaf(NS_C / SCALE, w2[8 * q + i], NS_B * (v[8 * q + i] * (1.f / SCALE)));
+                for (int i = 0; i < 8; ++i) w[i] = fmaf(NS_C / SCALE, v[8 * q + i], NS_B * kept[8 * q + i]);
                 put8(sh, sl, row, c + 8 * q, w);
             }
         }
         written();
-        if (tid == 0) {                                                   // P X
+        if (tid == 0) {                                                   // P X: columns 0-255, cross products 256-511
             const uint32_t idesc = IDESC | 1u << 16 | (uint32_t)(io.np / 8) << 17;
             for (int p = 0; p < deep_m; ++p) {
                 const uint64_t h = k_major(ash, p), r = slice_desc(axh + p * 2048, true, SMALL_BLOCK);
-                mma_f16(tmem + 256, h, r, idesc, p > 0);
+                mma_f16(tmem, h, r, idesc, p > 0);
                 if (PAIR) {
-                    mma_f16(tmem + 256, h, slice_desc(axl + p * 2048, true, SMALL_BLOCK), idesc, true);
+                    mma_f16(tmem + 256, h, slice_desc(axl + p * 2048, true, SMALL_BLOCK), idesc, p > 0);
                     mma_f16(tmem + 256, k_major(asl, p), r, idesc, true);
                 }
             }
@@ -728,7 +731,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
 #pragma unroll 1
         for (int c = part_of * 32; c < io.np; c += 128) {
             float v[32];
-            tmem_load32(tmem + lanes + 256 + c, v);
+            load_sums<PAIR>(v, tmem + lanes + c, 256);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const Pack<__half, 8> h = *reinterpret_cast<const Pack<__half, 8>*>(chunk_at(xh, row, c + 8 * q));

@@ -55,9 +55,6 @@ constexpr float LOG2_E = 1.4426950408889634f;
 
 // exp(-v) may overflow to infinity: the quotient is then 0, which is the limit.
 __device__ __forceinline__ float sigmoid_f32(float v) { return reciprocal_f32(1.f + exp2_f32(-LOG2_E * v)); }
-// The same to within an ulp or two.  A 16-bit result that another operator reads at once should round as
-// the exact one does: every fp32 error turns some of the roundings, and the reader sees those as 2^-8.
-__device__ __forceinline__ float sigmoid_exact_f32(float v) { return __fdiv_rn(1.f, 1.f + expf(-v)); }
 // log(1 + exp(v)) = max(v, 0) + log(1 + e), e = exp(-|v|) in (0, 1]; log(1 + e) / e is a polynomial of
 // degree 8 fitted to the relative error on [0, 1] (3e-8), so small results keep their digits.  The product
 // with log2(e) is carried in two parts: its rounding alone would cost |v| 2^-24 of the result.

@@ -366,10 +366,13 @@ __global__ void __launch_bounds__(128) conv_step_kernel(const T* __restrict__ x,
         float pre[VEC];
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-            pre[i] = bs[i];
+            // Rounded as the formula reads, products, sum, bias, quotient, without contraction: the scan reads
+            // a 16-bit y at once, and every fp32 difference turns some of its roundings.
+            pre[i] = __fmul_rn(w[i][0], to_f32<T>(v[0].v[i]));
 #pragma unroll
-            for (int j = 0; j < W; ++j) pre[i] = fmaf(w[i][j], to_f32<T>(v[j].v[i]), pre[i]);
-            if (silu) pre[i] *= sigmoid_exact_f32(pre[i]);
+            for (int j = 1; j < W; ++j) pre[i] = __fadd_rn(pre[i], __fmul_rn(w[i][j], to_f32<T>(v[j].v[i])));
+            pre[i] = __fadd_rn(pre[i], bs[i]);
+            if (silu) pre[i] = __fdiv_rn(pre[i], 1.f + expf(-pre[i]));
         }
         store_pack<T, VEC>(y + b * channels + c, pre);
         if (state_out != nullptr) {
