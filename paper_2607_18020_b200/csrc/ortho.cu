@@ -136,7 +136,9 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(OrthoIo io, const doub
 // Without it only hi hi is formed, and lo serves the terms a X and b S that are added in the epilogue.
 //
 // The cross products have an accumulator of their own: every product rounds the running sum towards zero,
-// and the large sum then sees a third of the roundings.
+// and the large sum then sees a third of the roundings; with 64-column tiles, where TMEM has the room, it
+// is split in two as well (40 x 900 fp32, S over 57 products: error 6.3e-6 before, 2.7e-6 after; plain fp32
+// 2.7e-6).
 //
 // S and P are symmetric: where their tiles fill the GPU, only those on and below the diagonal are
 // computed, and stored twice; where they do not, computing all of them is faster than storing twice.
@@ -164,8 +166,9 @@ struct Ring {
     static constexpr int STAGE = PLANES * (A_BYTES + B_BYTES);
     static constexpr int STAGES = 196608 / STAGE > 6 ? 6 : 196608 / STAGE;      // 229376 and 7 measured the same
     static constexpr int BYTES = STAGES * STAGE + 1024 + 256;    // slack to start on 1024 bytes, barriers
-    static constexpr int SET = PLANES * BN;                      // TMEM columns of one set of accumulators
-    static_assert(2 * SET <= 512 && STAGES >= 2, "accumulators fit TMEM, the ring shared memory");
+    static constexpr int MAINS = PAIR && BN == 64 ? 2 : 1;       // accumulators of the products of hi parts
+    static constexpr int SET = (MAINS + PLANES - 1) * BN <= 64 ? 64 : (MAINS + PLANES - 1) * BN <= 128 ? 128 : 256;     // TMEM columns of one set
+    static_assert((MAINS + PLANES - 1) * BN <= SET && 2 * SET <= 512 && STAGES >= 2, "accumulators fit TMEM, the ring shared memory");
 };
 
 struct ProductShape {
@@ -249,13 +252,14 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
-// The same, with the cross products' sums `cross` columns further on added.
-template <bool CROSS>
-__device__ __forceinline__ void load_sums(float (&v)[32], uint32_t addr, int cross) {
+// The same summed over `SETS` accumulators, `apart` columns from one another.
+template <int SETS>
+__device__ __forceinline__ void load_sums(float (&v)[32], uint32_t addr, int apart) {
     tmem_load32(addr, v);
-    if (CROSS) {
+#pragma unroll
+    for (int s = 1; s < SETS; ++s) {
         float x[32];
-        tmem_load32(addr + cross, x);
+        tmem_load32(addr + s * apart, x);
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] += x[i];
     }
@@ -370,11 +374,11 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
 #pragma unroll
                     for (int kk = 0; kk < BK / 16; ++kk) {
                         const uint64_t ah = slice_desc(a + kk * 32, false), bh = slice_desc(b + kk * KB, KIND == APPLY);
-                        const bool add = step > 0 || kk > 0;
-                        mma_f16<CG>(d, ah, bh, IDESC, add);
+                        mma_f16<CG>(d + kk % R::MAINS * BN, ah, bh, IDESC, step > 0 || kk >= R::MAINS);
                         if (PAIR) {
-                            mma_f16<CG>(d + BN, ah, slice_desc(b + R::B_BYTES + kk * KB, KIND == APPLY), IDESC, add);
-                            mma_f16<CG>(d + BN, slice_desc(a + R::A_BYTES + kk * 32, false), bh, IDESC, true);
+                            constexpr int CROSS = R::MAINS * BN;
+                            mma_f16<CG>(d + CROSS, ah, slice_desc(b + R::B_BYTES + kk * KB, KIND == APPLY), IDESC, step > 0 || kk > 0);
+                            mma_f16<CG>(d + CROSS, slice_desc(a + R::A_BYTES + kk * 32, false), bh, IDESC, true);
                         }
                     }
                     mma_commit<CG>(empty + 8 * stage);
@@ -421,7 +425,7 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
                 const bool there = row < s.mp && col < s.cols;       // the same for the whole warp: extents are multiples of 64
                 if (c != half * 32) fetch(c);
                 float v[32];
-                load_sums<PAIR>(v, tmem + acc * R::SET + c + ((uint32_t)(quarter * 32) << 16), BN);
+                load_sums<R::MAINS + R::PLANES - 1>(v, tmem + acc * R::SET + c + ((uint32_t)(quarter * 32) << 16), BN);
                 if (!there) continue;
                 const bool both = PAIR || KIND != SQUARE;        // P is only ever a factor
 #pragma unroll
@@ -682,7 +686,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
         float kept[32];                                                   // this thread's part of S, times 2^14
         {
             const int c = part_of * 32;
-            load_sums<PAIR>(kept, tmem + lanes + c, 128);
+            load_sums<PAIR ? 2 : 1>(kept, tmem + lanes + c, 128);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 float w[8];
@@ -705,7 +709,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
         {                                                                 // P over S, which has been read
             const int c = part_of * 32;
             float v[32];
-            load_sums<true>(v, tmem + lanes + 256 + c, 128);
+            load_sums<2>(v, tmem + lanes + 256 + c, 128);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 float w[8];
@@ -731,7 +735,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
 #pragma unroll 1
         for (int c = part_of * 32; c < io.np; c += 128) {
             float v[32];
-            load_sums<PAIR>(v, tmem + lanes + c, 256);
+            load_sums<PAIR ? 2 : 1>(v, tmem + lanes + c, 256);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const Pack<__half, 8> h = *reinterpret_cast<const Pack<__half, 8>*>(chunk_at(xh, row, c + 8 * q));
@@ -865,7 +869,10 @@ cudaError_t run(const fpde_ortho_args* a, bool muon, cudaStream_t st) {
         ProductShape square{io.mp, io.np, 0, 0, 0, 0, io.mp, NS_C / SCALE, NS_B};
         ProductShape apply{io.mp, io.np, 0, 0, 0, 0, io.np, 1.f / SCALE, NS_A};
         FPDE_TRY((run_product<PAIR, GRAM>(xm[at], xm[at], s, s, gram, a->count, sms, st)));
-        FPDE_TRY((run_product<PAIR, SQUARE>(sm, sm, s, p, square, a->count, sms, st)));
+        // while S is small its square is bound by latency: pairs cost nothing, and its factors' rounding is the
+        // largest part of the 16-bit types' error on matrices much wider than tall (40 x 900: 2.2e-3 of it)
+        if (PAIR || io.mp <= 512) FPDE_TRY((run_product<true, SQUARE>(sm, sm, s, p, square, a->count, sms, st)));
+        else FPDE_TRY((run_product<false, SQUARE>(sm, sm, s, p, square, a->count, sms, st)));
         FPDE_TRY((run_product<PAIR, APPLY>(pm, xm[at], x[at], x[at ^ 1], apply, a->count, sms, st)));
     }
     return launch_kernel(ortho_finish_kernel<T>, dim3((unsigned)pieces), dim3(256), st, io, (const __half*)x[at]);
