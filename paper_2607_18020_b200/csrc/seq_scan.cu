@@ -30,6 +30,7 @@ namespace {
 constexpr int STEP_THREADS = 128, STEP_CHANNELS = 4;
 constexpr int FWD_LANES = 32, BACK_LANES = 64;     // channels of a block with 4 lanes a channel: threads = that x 4 / NC
 constexpr int FWD_UNROLL = 4;
+constexpr double FWD_ENDS = 0.5, BACK_ENDS = 0.3;      // what forming the chunks' ends costs, as a share of the march
 constexpr int TILE = 16;          // nodes brought to shared memory together
 constexpr int KEEP = 8;           // nodes between stored states: what the backward march holds in registers
 constexpr int NS = 4;             // states of a thread; it has NC = 1 or 2 channels
@@ -904,7 +905,7 @@ ScanShape plan(const fpde_scan_args* a, bool backward) {
     // cheapest number of chunks wins, the fewest of equals.
     const int64_t length = a->length > 0 ? a->length : 1, blocks = a->batch * s.tiles;
     const int64_t resident = 148 * (backward ? back_blocks(2) : fwd_blocks(2));
-    const double ends_cost = backward ? 0.3 : 0.5;
+    const double ends_cost = backward ? BACK_ENDS : FWD_ENDS;
     const int64_t most = ceil_div(length, 2 * TILE) < 1024 ? ceil_div(length, 2 * TILE) : 1024;
     int64_t chunk = length;
     double best = 0;
