@@ -286,18 +286,20 @@ __device__ __forceinline__ void tile_at(int t, int across, int& i0, int& j0) {
 
 // left: K-major map of X (GRAM), S (SQUARE) or P (APPLY), also the right operand of GRAM and SQUARE;
 // right: map of X in 64 x 64 boxes (APPLY).  added: planes of the term in the epilogue (S or X).
-template <bool PAIR, int CG, int BN, int KIND, bool LOWER>
+template <bool PAIR, int CG, int BN, int KIND, bool LOWER, int KS>
 __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __grid_constant__ CUtensorMap left, const __grid_constant__ CUtensorMap right,
                                                                       const __half* __restrict__ added, __half* __restrict__ out, ProductShape s) {
     using R = Ring<PAIR, CG, BN>;
     static_assert(!LOWER || CG * BM % BN == 0, "columns of tiles end where rows do");
+    static_assert(KS == 1 || (CG == 1 && BN == 64 && !LOWER), "the depth is split where tiles are few and narrow");
     extern __shared__ uint8_t raw[];
     uint8_t* ring = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
     uint64_t* bars = reinterpret_cast<uint64_t*>(ring + R::STAGES * R::STAGE);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * R::STAGES + 4);
     const uint32_t full = smem_u32(bars), empty = full + 8 * R::STAGES, done = empty + 8 * R::STAGES, freed = done + 16;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int rank = CG == 2 ? (int)(blockIdx.x & 1) : 0, workers = gridDim.x / CG, worker = blockIdx.x / CG;
+    const int rank = CG == 2 ? (int)(blockIdx.x & 1) : 0, workers = gridDim.x / (CG * KS), worker = blockIdx.x / (CG * KS);
+    const int slice = KS > 1 ? (int)(blockIdx.x % KS) : 0;      // which part of the depth
     if (threadIdx.x == 0) {
         for (int i = 0; i < R::STAGES; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(done + 8 * i, 1); mbar_init(freed + 8 * i, CG * EPILOGUE_WARPS); }
@@ -321,7 +323,7 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = *tmem_slot;
     pdl_wait_then_trigger();
-    const int steps = s.depth / BK;
+    const int steps = s.depth / BK, step0 = steps * slice / KS, step1 = steps * (slice + 1) / KS;
     bool gave_up = false;
 
     if (warp == 0) {
@@ -333,7 +335,7 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
                 tile_at<LOWER, CG, BN>(tile % s.per_matrix, s.across, i0, j0);
                 i0 += rank * BM;
                 j0 += rank * R::B_COLS;
-                for (int step = 0; step < steps; ++step) {
+                for (int step = step0; step < step1; ++step) {
                     mbar_wait(empty + 8 * stage, phase ^ 1, gave_up, &g_ortho_timeouts);
                     if (rank == 0) mbar_expect_tx(full + 8 * stage, CG * R::STAGE);
                     const uint32_t base = smem_u32(ring + stage * R::STAGE);
@@ -367,17 +369,17 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
                 mbar_wait(freed + 8 * acc, acc_phase ^ 1, gave_up, &g_ortho_timeouts);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t d = tmem + acc * R::SET;
-                for (int step = 0; step < steps; ++step) {
+                for (int step = step0; step < step1; ++step) {
                     mbar_wait(full + 8 * stage, phase, gave_up, &g_ortho_timeouts);
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint32_t a = smem_u32(ring + stage * R::STAGE), b = a + R::PLANES * R::A_BYTES;
 #pragma unroll
                     for (int kk = 0; kk < BK / 16; ++kk) {
                         const uint64_t ah = slice_desc(a + kk * 32, false), bh = slice_desc(b + kk * KB, KIND == APPLY);
-                        mma_f16<CG>(d + kk % R::MAINS * BN, ah, bh, IDESC, step > 0 || kk >= R::MAINS);
+                        mma_f16<CG>(d + kk % R::MAINS * BN, ah, bh, IDESC, step > step0 || kk >= R::MAINS);
                         if (PAIR) {
                             constexpr int CROSS = R::MAINS * BN;
-                            mma_f16<CG>(d + CROSS, ah, slice_desc(b + R::B_BYTES + kk * KB, KIND == APPLY), IDESC, step > 0 || kk > 0);
+                            mma_f16<CG>(d + CROSS, ah, slice_desc(b + R::B_BYTES + kk * KB, KIND == APPLY), IDESC, step > step0 || kk > 0);
                             mma_f16<CG>(d + CROSS, slice_desc(a + R::A_BYTES + kk * 32, false), bh, IDESC, true);
                         }
                     }
@@ -389,7 +391,7 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
                 acc ^= 1;
             }
         }
-    } else {
+    } else if constexpr (KS == 1) {
         const int quarter = warp % 4, half = (warp - 2) / 4;          // TMEM lanes this warp may read; its half of the columns
         const uint32_t freed_first = CG == 2 ? in_first_block(freed) : freed;
         int acc = 0, acc_phase = 0;
@@ -458,9 +460,65 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
             acc ^= 1;
         }
     }
+    if constexpr (KS > 1) {
+        // Every block of the cluster has its part of the depth: it leaves its sums in shared memory (the ring is
+        // free by now), and then each adds up BN / KS of the tile's columns, in the same order everywhere.
+        const int quarter = warp % 4, half = (warp - 2) / 4;
+        float* mine = reinterpret_cast<float*>(ring);                 // [BN][128]
+        if (warp >= 2) {
+            mbar_wait(done, 0, gave_up, &g_ortho_timeouts);
+            __syncwarp();
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            float v[32];
+            load_sums<R::MAINS + R::PLANES - 1>(v, tmem + half * 32 + ((uint32_t)(quarter * 32) << 16), BN);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) mine[(half * 32 + i) * BM + quarter * 32 + lane] = v[i];
+        }
+        __syncwarp();
+        cluster_sync();
+        if (warp >= 2) {
+            constexpr int COLS = BN / KS / 2;                         // of a warp
+            int i0, j0;
+            tile_at<LOWER, CG, BN>(worker % s.per_matrix, s.across, i0, j0);
+            const int k = worker / s.per_matrix, row = i0 + quarter * 32 + lane, c = slice * (BN / KS) + half * COLS, col = j0 + c;
+            const int64_t out_plane = (int64_t)s.mp * s.cols;
+            if (row < s.mp && col < s.cols) {
+                __half* hi = out + 2 * k * out_plane + (int64_t)row * s.cols + col;
+                const __half* add = KIND == GRAM ? nullptr : added + 2 * k * out_plane + (int64_t)row * s.cols + col;
+                const uint32_t here = smem_u32(mine) + (uint32_t)(c * BM + quarter * 32 + lane) * 4;
+                uint32_t from[KS];
+#pragma unroll
+                for (int r = 0; r < KS; ++r) asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(from[r]) : "r"(here), "r"(r));
+#pragma unroll
+                for (int g = 0; g < COLS; g += 8) {
+                    Pack<__half, 8> ph = {}, pl = {};
+                    if constexpr (KIND != GRAM) {
+                        ph = load_pack<__half, 8>(add + g);
+                        pl = load_pack<__half, 8>(add + out_plane + g);
+                    }
+                    float w[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        float v = 0.f;
+#pragma unroll
+                        for (int r = 0; r < KS; ++r) {
+                            float x;
+                            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(from[r] + (uint32_t)((g + i) * BM * 4)) : "memory");
+                            v += x;
+                        }
+                        w[i] = s.alpha * v;
+                        if (KIND != GRAM) w[i] = fmaf(s.beta, __half2float(ph.v[i]) + __half2float(pl.v[i]), w[i]);
+                    }
+                    split8(w, ph, pl);
+                    *reinterpret_cast<Pack<__half, 8>*>(hi + g) = ph;
+                    if (PAIR || KIND != SQUARE) *reinterpret_cast<Pack<__half, 8>*>(hi + out_plane + g) = pl;
+                }
+            }
+        }
+    }
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    if constexpr (CG == 2) cluster_sync();       // nobody's barriers are needed any more
+    if constexpr (CG == 2 || KS > 1) cluster_sync();       // nobody's barriers or sums are needed any more
     else __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     if (warp == 1) {
@@ -489,7 +547,7 @@ struct Maps {
     }
 };
 
-template <bool PAIR, int CG, int BN, int KIND, bool LOWER>
+template <bool PAIR, int CG, int BN, int KIND, bool LOWER, int KS = 1>
 cudaError_t launch_product(const Maps& left, const Maps& right, const __half* added, __half* out, ProductShape s, int64_t count, int sms,
                            cudaStream_t st) {
     using R = Ring<PAIR, CG, BN>;
@@ -500,21 +558,21 @@ cudaError_t launch_product(const Maps& left, const Maps& right, const __half* ad
     if (per * count > 0x3fffffff) return cudaErrorInvalidConfiguration;
     s.per_matrix = (int)per;
     s.tiles = (int)(per * count);
-    auto kernel = product_kernel<PAIR, CG, BN, KIND, LOWER>;
+    auto kernel = product_kernel<PAIR, CG, BN, KIND, LOWER, KS>;
     static std::atomic<uint64_t> allowed{0};
     const cudaError_t e = allow_smem(kernel, R::BYTES, allowed);
     if (e != cudaSuccess) return e;
-    const int workers = s.tiles < sms / CG ? s.tiles : sms / CG;
+    const int workers = KS > 1 || s.tiles < sms / CG ? s.tiles : sms / CG;      // KS > 1: one tile each
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(workers * CG));
+    cfg.gridDim = dim3((unsigned)(workers * CG * KS));
     cfg.blockDim = dim3(PRODUCT_THREADS);
     cfg.dynamicSmemBytes = R::BYTES;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     int n = 0;
-    if (CG == 2) {
+    if (CG * KS > 1) {
         attr[n].id = cudaLaunchAttributeClusterDimension;
-        attr[n].val.clusterDim.x = 2;
+        attr[n].val.clusterDim.x = CG * KS;
         attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
         ++n;
     }
@@ -531,29 +589,39 @@ cudaError_t launch_product(const Maps& left, const Maps& right, const __half* ad
 
 // Seconds that a form of a product takes, for comparing the forms.  A block brings `STAGE` bytes per 64 of
 // depth; all of them together get some 9e12 bytes a second out of L2 (8.4 to 8.7e12 in products of
-// 4096 x 4096 and 2048 x 8192), one alone some 115e9, and its tensor core needs its time; the last tile's
-// epilogue is not hidden.
-template <bool PAIR, int CG, int BN, int KIND, bool LOWER>
+// 4096 x 4096 and 2048 x 8192), one alone some 76e9 (0.63 us for 48 KB), and its tensor core needs its time;
+// the last tile's epilogue is not hidden, and joining a split depth takes two barriers of the cluster.
+template <bool PAIR, int CG, int BN, int KIND, bool LOWER, int KS = 1>
 double product_seconds(const ProductShape& s, int64_t count, int sms) {
     using R = Ring<PAIR, CG, BN>;
-    const int64_t down = ceil_div(s.mp, CG * BM), across = ceil_div(s.cols, BN), workers = sms / CG;
-    const int64_t tiles = count * (LOWER ? down * (down + 1) / 2 * (CG * BM / BN) : down * across);
-    const int64_t waves = ceil_div(tiles, workers), blocks = (tiles < workers ? tiles : workers) * CG;
-    const double shared = R::STAGE * (double)blocks / 9e12, alone = R::STAGE / 115e9, math = (PAIR ? 3 : 1) * 2.0 * BM * BN * BK * 1.0 / 14e12;
+    const int64_t down = ceil_div(s.mp, CG * BM), across = ceil_div(s.cols, BN), workers = sms / (CG * KS);
+    const int64_t tiles = count * (LOWER ? down * (down + 1) / 2 * (CG * BM / BN) : down * across), steps = (KIND == GRAM ? s.np : s.mp) / BK;
+    if (KS > 1 && (tiles > workers || steps < KS)) return 1e9;      // one tile a cluster, all of them at once
+    const int64_t waves = ceil_div(tiles, workers), blocks = (tiles < workers ? tiles : workers) * CG * KS;
+    const double shared = R::STAGE * (double)blocks / 9e12, alone = R::STAGE / 76e9, math = (PAIR ? 3 : 1) * 2.0 * BM * BN * BK * 1.0 / 14e12;
     const double step = shared > alone ? (shared > math ? shared : math) : (alone > math ? alone : math);
-    return waves * ((KIND == GRAM ? s.np : s.mp) / BK) * step + 3e-6 * BN / 128 + (LOWER ? 2e-6 : 0);
+    return waves * ceil_div(steps, KS) * step + 3e-6 * BN / 128 + (LOWER ? 2e-6 : 0) + (KS > 1 ? 1.5e-6 : 0);
 }
 
-// Pairs of SMs, or single blocks with tiles of 128 or 64 columns: whichever is reckoned fastest.
+// Pairs of SMs, or single blocks with tiles of 128 or 64 columns, the latter with the depth split over 2 or 4
+// blocks where there are few: whichever is reckoned fastest.
 template <bool PAIR, int KIND>
 cudaError_t run_product(const Maps& left, const Maps& right, const __half* added, __half* out, ProductShape s, int64_t count, int sms, cudaStream_t st) {
     constexpr int WIDE = PAIR ? 128 : 256;      // PAIR: two accumulators a set
     constexpr bool LOWER = KIND != APPLY;
-    const double pairs = product_seconds<PAIR, 2, WIDE, KIND, LOWER>(s, count, sms), wide = product_seconds<PAIR, 1, 128, KIND, LOWER>(s, count, sms),
-                 narrow = product_seconds<PAIR, 1, 64, KIND, false>(s, count, sms);
-    if (pairs <= wide && pairs <= narrow) return launch_product<PAIR, 2, WIDE, KIND, LOWER>(left, right, added, out, s, count, sms, st);
-    if (wide <= narrow) return launch_product<PAIR, 1, 128, KIND, LOWER>(left, right, added, out, s, count, sms, st);
-    return launch_product<PAIR, 1, 64, KIND, false>(left, right, added, out, s, count, sms, st);
+    const double t[5] = {product_seconds<PAIR, 2, WIDE, KIND, LOWER>(s, count, sms), product_seconds<PAIR, 1, 128, KIND, LOWER>(s, count, sms),
+                         product_seconds<PAIR, 1, 64, KIND, false>(s, count, sms), product_seconds<PAIR, 1, 64, KIND, false, 2>(s, count, sms),
+                         product_seconds<PAIR, 1, 64, KIND, false, 4>(s, count, sms)};
+    int best = 0;
+    for (int i = 1; i < 5; ++i)
+        if (t[i] < t[best]) best = i;
+    switch (best) {
+    case 0: return launch_product<PAIR, 2, WIDE, KIND, LOWER>(left, right, added, out, s, count, sms, st);
+    case 1: return launch_product<PAIR, 1, 128, KIND, LOWER>(left, right, added, out, s, count, sms, st);
+    case 2: return launch_product<PAIR, 1, 64, KIND, false>(left, right, added, out, s, count, sms, st);
+    case 3: return launch_product<PAIR, 1, 64, KIND, false, 2>(left, right, added, out, s, count, sms, st);
+    default: return launch_product<PAIR, 1, 64, KIND, false, 4>(left, right, added, out, s, count, sms, st);
+    }
 }
 
 // --------------------------------------------------------------------------------- small matrices
