@@ -99,13 +99,16 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(OrthoIo io, const doub
     __shared__ double part[8];
     const int across = io.np / 64, down = io.mp / 64;
     const int k = blockIdx.x / (across * down), t = blockIdx.x % (across * down), i0 = t / across * 64, j0 = t % across * 64;
-    const float scale = inverse_norm(sums + (int64_t)k * blocks, blocks, io.eps, part) * SCALE;
     const int r0 = io.turned ? j0 : i0, c0 = io.turned ? i0 : j0;
-#pragma unroll 8
-    for (int e = threadIdx.x; e < 64 * 64; e += 256) {
-        const int r = e / 64, c = e % 64;
-        tile[r][c] = r0 + r < io.rows && c0 + c < io.cols ? update_at<T>(io, k, r0 + r, c0 + c) : 0.f;
+    float in[16];                        // on its way while the norm is added up
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+        const int r = threadIdx.x / 64 + q * 4, c = threadIdx.x % 64;
+        in[q] = r0 + r < io.rows && c0 + c < io.cols ? update_at<T>(io, k, r0 + r, c0 + c) : 0.f;
     }
+    const float scale = inverse_norm(sums + (int64_t)k * blocks, blocks, io.eps, part) * SCALE;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) tile[threadIdx.x / 64 + q * 4][threadIdx.x % 64] = in[q];
     __syncthreads();
     const int64_t plane = (int64_t)io.mp * io.np;
 #pragma unroll
@@ -837,6 +840,14 @@ __global__ void __launch_bounds__(256) ortho_finish_kernel(OrthoIo io, const __h
     const int across = io.np / 64, down = io.mp / 64;
     const int k = blockIdx.x / (across * down), t = blockIdx.x % (across * down), i0 = t / across * 64, j0 = t % across * 64;
     const int64_t plane = (int64_t)io.mp * io.np;
+    const int r0 = io.turned ? j0 : i0, c0 = io.turned ? i0 : j0, a = threadIdx.x / 64, b = threadIdx.x % 64;
+    T* out = (T*)io.out + ((int64_t)k * io.rows + r0 + a) * io.cols + c0 + b;
+    float w[16];                         // the weights, on their way while X is turned
+    if (io.momentum != nullptr) {
+#pragma unroll
+        for (int q = 0; q < 16; ++q)
+            w[q] = r0 + a + q * 4 < io.rows && c0 + b < io.cols ? to_f32<T>(out[(int64_t)q * 4 * io.cols]) : 0.f;
+    }
 #pragma unroll
     for (int e = threadIdx.x; e < 64 * 8; e += 256) {
         const int i = e / 8, j = e % 8 * 8;
@@ -846,15 +857,12 @@ __global__ void __launch_bounds__(256) ortho_finish_kernel(OrthoIo io, const __h
         for (int q = 0; q < 8; ++q) tile[i][j + q] = (__half2float(hi.v[q]) + __half2float(lo.v[q])) * (1.f / SCALE);
     }
     __syncthreads();
-    const int r0 = io.turned ? j0 : i0, c0 = io.turned ? i0 : j0;
-    T* out = (T*)io.out + ((int64_t)k * io.rows + r0) * io.cols + c0;
-#pragma unroll 4
-    for (int e = threadIdx.x; e < 64 * 64; e += 256) {
-        const int r = e / 64, c = e % 64;
-        if (r0 + r >= io.rows || c0 + c >= io.cols) continue;
-        const float v = io.turned ? tile[c][r] : tile[r][c];
-        T* o = out + (int64_t)r * io.cols + c;
-        *o = from_f32<T>(io.momentum == nullptr ? v : fmaf(-io.rate, v, io.keep * to_f32<T>(*o)));
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+        const int r = a + q * 4;
+        if (r0 + r >= io.rows || c0 + b >= io.cols) continue;
+        const float v = io.turned ? tile[b][r] : tile[r][b];
+        out[(int64_t)q * 4 * io.cols] = from_f32<T>(io.momentum == nullptr ? v : fmaf(-io.rate, v, io.keep * w[q]));
     }
 }
 
