@@ -20,7 +20,7 @@ struct OrthoIo {
     void* out;          // orthogonalize: result;  muon: weight
     float* momentum;    // muon only
     int rows, cols, m, n, mp, np;   // m <= n: the sides of X; mp, np padded
-    bool turned, nesterov;
+    bool turned, nesterov, wide;   // wide: eight neighbours of a row can be moved together
     float decay, keep, rate;   // momentum decay, 1 - lr wd, lr sqrt(max(1, rows / cols))
     double eps;
 };
@@ -32,6 +32,38 @@ __device__ __forceinline__ float update_at(const OrthoIo& io, int64_t k, int64_t
     if (io.momentum == nullptr) return g;
     const float mom = io.momentum[(k * io.rows + r) * io.cols + c];
     return io.nesterov ? fmaf(io.decay, mom, g) : mom;
+}
+
+template <typename T>
+__device__ __forceinline__ void load8(float (&v)[8], const T* p) {
+    constexpr int N = 16 / sizeof(T);
+#pragma unroll
+    for (int i = 0; i < 8; i += N) {
+        const Pack<T, N> k = load_pack<T, N>(p + i);
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[i + j] = to_f32<T>(k.v[j]);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
+    constexpr int N = 16 / sizeof(T);
+#pragma unroll
+    for (int i = 0; i < 8; i += N) {
+        Pack<T, N> k;
+#pragma unroll
+        for (int j = 0; j < N; ++j) k.v[j] = from_f32<T>(v[i + j]);
+        *reinterpret_cast<Pack<T, N>*>(p + i) = k;
+    }
+}
+// Eight neighbours of update_at (io.wide).
+template <typename T>
+__device__ __forceinline__ void update8(float (&v)[8], const OrthoIo& io, int64_t k, int64_t r, int64_t c) {
+    load8<T>(v, (const T*)io.grad + k * io.grad_matrix + r * io.grad_row + c);
+    if (io.momentum == nullptr) return;
+    float m[8];
+    load8<float>(m, io.momentum + (k * io.rows + r) * io.cols + c);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = io.nesterov ? fmaf(io.decay, m[i], v[i]) : m[i];
 }
 
 // Moves the momentum on (muon) and leaves each block's sum of squares of the update, in 64 bits: the
@@ -46,6 +78,26 @@ __global__ void __launch_bounds__(256) ortho_square_kernel(OrthoIo io, double* _
     for (int r = (blockIdx.x % blocks) * 8 + threadIdx.x / 32; r < io.rows; r += blocks * 8) {
         const T* g = (const T*)io.grad + k * io.grad_matrix + r * io.grad_row;
         float* mom = io.momentum ? io.momentum + ((int64_t)k * io.rows + r) * io.cols : nullptr;
+        if (io.wide) {
+#pragma unroll 2
+            for (int c = lane * 8; c < io.cols; c += 256) {
+                float u[8];
+                load8<T>(u, g + c);
+                if (mom != nullptr) {
+                    float next[8];
+                    load8<float>(next, mom + c);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        next[i] = fmaf(decay, next[i], u[i]);
+                        u[i] = io.nesterov ? fmaf(decay, next[i], u[i]) : next[i];
+                    }
+                    store8<float>(mom + c, next);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v += (double)u[i] * u[i];
+            }
+            continue;
+        }
 #pragma unroll 8
         for (int c = lane; c < io.cols; c += 32) {
             float u = to_f32<T>(g[c]);
@@ -100,15 +152,33 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(OrthoIo io, const doub
     const int across = io.np / 64, down = io.mp / 64;
     const int k = blockIdx.x / (across * down), t = blockIdx.x % (across * down), i0 = t / across * 64, j0 = t % across * 64;
     const int r0 = io.turned ? j0 : i0, c0 = io.turned ? i0 : j0;
-    float in[16];                        // on its way while the norm is added up
+    // the elements are on their way while the norm is added up
+    float scale;
+    if (io.wide) {
+        float in[2][8];
 #pragma unroll
-    for (int q = 0; q < 16; ++q) {
-        const int r = threadIdx.x / 64 + q * 4, c = threadIdx.x % 64;
-        in[q] = r0 + r < io.rows && c0 + c < io.cols ? update_at<T>(io, k, r0 + r, c0 + c) : 0.f;
+        for (int q = 0; q < 2; ++q) {
+            const int r = threadIdx.x / 8 + q * 32, c = threadIdx.x % 8 * 8;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) in[q][i] = 0.f;
+            if (r0 + r < io.rows && c0 + c < io.cols) update8<T>(in[q], io, k, r0 + r, c0 + c);
+        }
+        scale = inverse_norm(sums + (int64_t)k * blocks, blocks, io.eps, part) * SCALE;
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) tile[threadIdx.x / 8 + q * 32][threadIdx.x % 8 * 8 + i] = in[q][i];
+    } else {
+        float in[16];
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+            const int r = threadIdx.x / 64 + q * 4, c = threadIdx.x % 64;
+            in[q] = r0 + r < io.rows && c0 + c < io.cols ? update_at<T>(io, k, r0 + r, c0 + c) : 0.f;
+        }
+        scale = inverse_norm(sums + (int64_t)k * blocks, blocks, io.eps, part) * SCALE;
+#pragma unroll
+        for (int q = 0; q < 16; ++q) tile[threadIdx.x / 64 + q * 4][threadIdx.x % 64] = in[q];
     }
-    const float scale = inverse_norm(sums + (int64_t)k * blocks, blocks, io.eps, part) * SCALE;
-#pragma unroll
-    for (int q = 0; q < 16; ++q) tile[threadIdx.x / 64 + q * 4][threadIdx.x % 64] = in[q];
     __syncthreads();
     const int64_t plane = (int64_t)io.mp * io.np;
 #pragma unroll
@@ -843,7 +913,7 @@ __global__ void __launch_bounds__(256) ortho_finish_kernel(OrthoIo io, const __h
     const int r0 = io.turned ? j0 : i0, c0 = io.turned ? i0 : j0, a = threadIdx.x / 64, b = threadIdx.x % 64;
     T* out = (T*)io.out + ((int64_t)k * io.rows + r0 + a) * io.cols + c0 + b;
     float w[16];                         // the weights, on their way while X is turned
-    if (io.momentum != nullptr) {
+    if (io.momentum != nullptr && !io.wide) {
 #pragma unroll
         for (int q = 0; q < 16; ++q)
             w[q] = r0 + a + q * 4 < io.rows && c0 + b < io.cols ? to_f32<T>(out[(int64_t)q * 4 * io.cols]) : 0.f;
@@ -857,6 +927,23 @@ __global__ void __launch_bounds__(256) ortho_finish_kernel(OrthoIo io, const __h
         for (int q = 0; q < 8; ++q) tile[i][j + q] = (__half2float(hi.v[q]) + __half2float(lo.v[q])) * (1.f / SCALE);
     }
     __syncthreads();
+    if (io.wide) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int r = threadIdx.x / 8 + q * 32, c = threadIdx.x % 8 * 8;
+            if (r0 + r >= io.rows || c0 + c >= io.cols) continue;
+            T* o = (T*)io.out + ((int64_t)k * io.rows + r0 + r) * io.cols + c0 + c;
+            float v[8], old[8];
+            if (io.momentum != nullptr) load8<T>(old, o);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[i] = io.turned ? tile[c + i][r] : tile[r][c + i];
+                if (io.momentum != nullptr) v[i] = fmaf(-io.rate, v[i], io.keep * old[i]);
+            }
+            store8<T>(o, v);
+        }
+        return;
+    }
 #pragma unroll
     for (int q = 0; q < 16; ++q) {
         const int r = a + q * 4;
@@ -915,6 +1002,7 @@ cudaError_t run(const fpde_ortho_args* a, bool muon, cudaStream_t st) {
     io.rate = (float)(a->lr * sqrt(io.rows > io.cols ? (double)io.rows / io.cols : 1.0));
     io.eps = a->eps;
     io.mp = (int)padded(io.m); io.np = (int)padded(io.n);
+    io.wide = io.cols % 8 == 0 && packs(io.grad, io.grad_matrix, io.grad_row, sizeof(T), 16 / sizeof(T)) && aligned(io.out, 16) && aligned(io.momentum, 16);
     if (is_small(io.m, io.n)) {
         static std::atomic<uint64_t> allowed{0};
         FPDE_TRY(allow_smem(ortho_small_kernel<T>, small_bytes(SMALL_N), allowed));
