@@ -3,6 +3,12 @@
 //
 //   X = U / (|U| + eps);  `steps` times:  S = X X^T,  P = b S + c S S,  X <- a X + P X
 // on the shorter side (taller matrices are turned on the way in and back on the way out).
+//
+// Per step 2 m^2 (m + n) multiplications and additions are needed with the symmetry of S and S S, m <= n.
+// 4096^2 bf16, 5 steps: 1.37e12, 831 us at the measured bf16 rate, measured 1.39 ms (products 70, 70 and
+// 124 us a step, 83 % of the library product's rate for the one that has no symmetry; the passes around
+// them 68 us).  Four fp32 1000 x 333 steps of the optimiser: 184 us, small products that are bound by
+// latency.
 #include "seq_common.cuh"
 #include "tma_common.cuh"
 

@@ -5,29 +5,36 @@
 //
 // Each (node, channel, state) costs one exponential and four multiplications or fused adds, against
 // 16 bytes or less per (node, channel): with 16 states the special function unit (16 exponentials a
-// clock and SM) bounds the forward pass, not memory.
+// clock and SM) bounds the forward pass, not memory.  8 x 2048 x 4096 x 16 bf16: 239 us of exponentials,
+// 83 us of bytes, measured 531 us with that unit busy 55 to 63 % of the time; the rest is the latency of a
+// march of dependent nodes at 14 warps an SM.
 //
-// Layout.  A thread keeps four states of one channel; S = 2, 4, 8 or 16 neighbouring lanes share a
-// channel, so a warp covers 32/S channels and the sums over states are shuffles among S lanes.  A
-// block marches its threads / S channels through tiles of nodes; the tile's dt, dt u, B and
-// C are brought to shared memory once, in fp32, by loads that run along the channels.
+// Layout.  A thread keeps four states of one or two channels, as pairs for the packed fp32 instructions;
+// S = 2, 4, 8 or 16 neighbouring lanes share their channels and the sums over states are shuffles among
+// them.  Two channels a thread read B and C half as often (with one, shared memory's data pipe was 86 %
+// busy) and halve the shuffles that sum gB and gC; one channel a thread gives small grids more warps.  A
+// block marches through tiles of nodes: the tile's dt, dt u, B and C are brought to shared memory once, in
+// fp32, by loads that run along the channels and travel one tile ahead.
 //
-// Long rows.  Where batch x channels gives too few blocks, a row is cut into chunks: one kernel forms
-// each chunk's state from zero and its sum of dt (the chunk's decay is exp(A sum dt)), a second joins
+// Long rows.  Where batch x channels gives too few blocks, a row is cut into chunks: one pass forms
+// each chunk's state from zero and its sum of dt (the chunk's decay is exp(A sum dt)), a second kernel joins
 // them along the row, and the march starts every chunk from its joined state.  The gradient does the
-// same backwards with the adjoint state.
+// same backwards with the adjoint state.  1 x 16384 x 1536 x 16 bf16: 309 us (one block per SM or fewer
+// without chunks: 1442 us).
 //
 // Gradients.  With gy = gout silu(z) the adjoint state is p[t] = C gy + exp(dt[t+1] A) p[t+1]; then
 //   gC = sum_c h gy, gB = sum_c p dt u, gu = dt (p.B) + D gy, gdt = sum_n p exp(dt A) h[t-1] A + u (p.B),
 //   gA = sum_t p exp(dt A) h[t-1] dt.
 // The forward pass stores the state before every KEEP-th node; the backward march recomputes the
-// states inside such a piece in registers and walks it backwards.
+// states inside such a piece in registers and walks it backwards.  It is bound by instructions: about 105
+// per warp, node and four states, a fifth of them the sums over lanes; 4 x 4096 x 2048 x 16 bf16: 825 us,
+// and 216 us for the chunks' ends.
 #include "seq_common.cuh"
 
 namespace fpde {
 namespace {
 
-constexpr int STEP_THREADS = 128, STEP_CHANNELS = 4;
+constexpr int STEP_THREADS = 128, STEP_CHANNELS = 4;      // one node: 28 us for 256 x 4096 x 16 bf16, 134 MB of states
 constexpr int FWD_LANES = 32, BACK_LANES = 64;     // channels of a block with 4 lanes a channel: threads = that x 4 / NC
 constexpr int FWD_UNROLL = 4;
 constexpr double FWD_ENDS = 0.5, BACK_ENDS = 0.3;      // what forming the chunks' ends costs, as a share of the march
@@ -465,6 +472,7 @@ struct BackSpace {
     static constexpr int RP = THREADS / (CT / VEC), RN = THREADS / NP;
     using Act = Feed<T, VEC, TILE, RP, 4, THREADS>;
     typename Act::Space room;
+    Quad hold[TILE / KEEP][NC][THREADS];                    // the thread's stored states of the tile, on their way a tile ahead
 };
 
 // part_bc[tile][b][t][2 NP]: this block's share of gB and gC; part_a[b][chunk][channel][states + 2]:
@@ -530,26 +538,36 @@ __global__ void __launch_bounds__(back_threads(NC), back_blocks(NC)) scan_bwd_ke
             bt.load(s.B_node, rn, here, row_n, -TILE);
         }
     };
-    // the stored state before node t
-    auto stored = [&](Quad (&h)[NC], int64_t t) {
-        const float* hp = kept + ((w.b * s.kept_nodes + t / KEEP) * s.channels + c) * s.states;
+    // the stored states before the pieces of the tile at node t; lanes without states or channel keep zeros
+    auto fetch_states = [&](int64_t t) {
 #pragma unroll
-        for (int k = 0; k < NC; ++k) {
-            h[k] = {0, 0};
-            if (c + k < s.channels) {
-                if (!states_packed(s.states)) h[k] = load_states(hp + k * s.states, q * NS, s.states, 1.f);
-                else if (q * NS < s.states) h[k] = quad_at(hp + k * s.states + q * NS);
+        for (int piece = 0; piece < TILE / KEEP; ++piece) {
+            const float* hp = kept + ((w.b * s.kept_nodes + t / KEEP + piece) * s.channels + c) * s.states;
+#pragma unroll
+            for (int k = 0; k < NC; ++k) {
+                if (t + piece * KEEP >= end || c + k >= s.channels || q * NS >= s.states) continue;
+                Quad* dst = &m.hold[piece][k][tid];
+                if (states_packed(s.states))
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(dst))),
+                                 "l"(hp + k * s.states + q * NS) : "memory");
+                else *dst = load_states(hp + k * s.states, q * NS, s.states, 1.f);
             }
         }
     };
+    if constexpr (!ENDS) {
+#pragma unroll
+        for (int piece = 0; piece < TILE / KEEP; ++piece)
+#pragma unroll
+            for (int k = 0; k < NC; ++k) m.hold[piece][k][tid] = {0, 0};
+        if (ntiles > 0) fetch_states(last);
+    }
     float total[NC] = {};
     if (ntiles > 0) fetch((int)(end - last));
     for (int64_t t0 = last; t0 >= first && ntiles > 0; t0 -= TILE) {
         const int here = (int)(end - t0 < TILE ? end - t0 : TILE);
         const int top = (here - 1) / KEEP * KEEP;      // first node of the last piece that has nodes
-        Quad next[NC];                                 // the state before the piece to come
-        if constexpr (!ENDS) stored(next, t0 + top);
         act.arrive();
+        if constexpr (!ENDS && !Act::ASYNC) asm volatile("cp.async.wait_all;" ::: "memory");      // the stored states
 #pragma unroll
         for (int k = 0; k < Act::PER; ++k) {
             const int r = r0 + k * RP;
@@ -605,8 +623,8 @@ __global__ void __launch_bounds__(back_threads(NC), back_blocks(NC)) scan_bwd_ke
             for (int base = top; base >= 0; base -= KEEP) {
                 Quad hs[KEEP + 1][NC];                 // hs[r]: the state BEFORE node base + r
 #pragma unroll
-                for (int k = 0; k < NC; ++k) hs[0][k] = next[k];
-                if (base > 0) stored(next, t0 + base - KEEP);
+                for (int k = 0; k < NC; ++k) hs[0][k] = m.hold[base / KEEP][k][tid];
+                if (base == 0 && t0 > first) fetch_states(t0 - TILE);
                 // forward through the piece
 #pragma unroll
                 for (int k0 = 0; k0 < KEEP; k0 += 4) {
