@@ -6,7 +6,7 @@
 // A thread owns a pair of neighbouring channels (one where rows start on odd elements) and marches along
 // its piece of a row with the last W-1 nodes in registers, so every value is loaded once per piece plus
 // a halo of W-1 nodes; the nodes ahead are on their way to shared memory meanwhile.  A block has 4 pieces
-// of 32 channel packs.  8 x 8192 x 2048 bf16, W = 4: forward 118 us (floor 82), gradients 208 us (floor 123,
+// of 32 channel packs.  8 x 8192 x 2048 bf16, W = 4: forward 115 us (floor 82), gradients 208 us (floor 123,
 // issue slots 74 % busy: some 40 instructions an element for the filter, its gate, their gradients and the
 // weights').  Registers one group ahead instead of shared memory left too few bytes on their way: 328 and
 // 587 us.
@@ -25,7 +25,7 @@ namespace {
 constexpr int CONV_LANES = 32;    // channel packs of a block
 constexpr int CONV_ROWS = 4;      // pieces of a row marched by a block
 constexpr int CONV_THREADS = CONV_LANES * CONV_ROWS;
-constexpr int GROUP = 4;          // nodes computed together
+constexpr int GROUP = 8;          // nodes computed together
 constexpr int MOST_NODES = 256;  // of a piece
 constexpr int AHEAD = 2;          // groups on their way per thread and array (a power of two); four are no faster
 
@@ -156,15 +156,18 @@ __global__ void __launch_bounds__(CONV_THREADS) conv_fwd_kernel(
         for (int j = 0; j < W - 1; ++j)
             xs[GROUP + j] = widen_v<T, VEC>(x_at<T, VEC, W>(xr, s.x_node, win, at.t0 + j - (W - 1), s.length, s.channels));
         T* yp = y + (at.b * s.length + at.t0) * s.channels + c;
-        int slot = 0;
-        for (int t = 0; t < total; t += GROUP) {
+        // AHEAD groups a turn: the slots are then known when this is compiled, and the window moves by renaming
+        for (int turn = 0; turn < total; turn += AHEAD * GROUP)
+#pragma unroll
+        for (int slot = 0; slot < AHEAD; ++slot) {
+            const int t = turn + slot * GROUP;
+            if (t >= total) break;
 #pragma unroll
             for (int j = 0; j < W - 1; ++j) xs[j] = xs[GROUP + j];
             if (F::ASYNC) { fx.request((slot + AHEAD - 1) % AHEAD); feed_commit(); feed_wait(); }
 #pragma unroll
             for (int k = 0; k < GROUP; ++k) xs[W - 1 + k] = widen_v<T, VEC>(fx.get(slot, k));
-            if (F::ASYNC) slot = (slot + 1) % AHEAD;
-            else fx.request(0);
+            if (!F::ASYNC) fx.request(0);
 #pragma unroll
             for (int k = 0; k < GROUP; ++k) {
                 V pre = bs;
@@ -249,8 +252,11 @@ __global__ void __launch_bounds__(CONV_THREADS) conv_bwd_kernel(
             }
         }
         T* gxp = gx + (at.b * s.length + at.t0 - (W - 1)) * s.channels + c;      // of the thread's first position
-        int slot = 0;
-        for (int t = 0; t < total; t += GROUP) {
+        for (int turn = 0; turn < total; turn += AHEAD * GROUP)
+#pragma unroll
+        for (int slot = 0; slot < AHEAD; ++slot) {
+            const int t = turn + slot * GROUP;
+            if (t >= total) break;
 #pragma unroll
             for (int j = 0; j < W - 1; ++j) { xs[j] = xs[GROUP + j]; g[j] = g[GROUP + j]; }
             if (F::ASYNC) {
@@ -264,8 +270,7 @@ __global__ void __launch_bounds__(CONV_THREADS) conv_bwd_kernel(
                 xs[W - 1 + k] = widen_v<T, VEC>(fx.get(slot, k));
                 g[W - 1 + k] = widen_v<T, VEC>(fg.get(slot, k));
             }
-            if (F::ASYNC) slot = (slot + 1) % AHEAD;
-            else { fx.request(0); fg.request(0); }
+            if (!F::ASYNC) { fx.request(0); fg.request(0); }
             // INNER: every node of the group exists and none of its positions lies in a window
             auto compute = [&](auto inner) {
                 constexpr bool INNER = decltype(inner)::value;
@@ -410,7 +415,7 @@ int check_conv(const fpde_conv_args* a, bool step) {
 // Nodes of a thread's piece: long pieces re-read fewer halo nodes, short ones give a small grid more
 // threads.  Doubled while there are still 1024 threads per SM.
 int conv_nodes(const fpde_conv_args* a, int64_t positions) {
-    int nodes = 2 * GROUP;
+    int nodes = AHEAD * GROUP;
     while (nodes < MOST_NODES && a->batch * ceil_div(a->channels, 2) * ceil_div(positions, 2 * nodes) >= 148 * 1024) nodes *= 2;
     return nodes;
 }
