@@ -217,7 +217,8 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(OrthoIo io, const doub
 // The cross products have an accumulator of their own: every product rounds the running sum towards zero,
 // and the large sum then sees a third of the roundings; with 64-column tiles, where TMEM has the room, it
 // is split in two as well (40 x 900 fp32, S over 57 products: error 6.3e-6 before, 2.7e-6 after; plain fp32
-// 2.7e-6).
+// 2.7e-6).  And with PAIR the sums leave the accumulators every SEGMENT slices, to be added up in fp32 with
+// ordinary rounding: 33 x 70001 fp32 was 1.2e-4 off in one run of products.
 //
 // S and P are symmetric: where their tiles fill the GPU, only those on and below the diagonal are
 // computed, and stored twice; where they do not, computing all of them is faster than storing twice.
@@ -233,6 +234,11 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(OrthoIo io, const doub
 // What a block has to load per product is what bounds the one-block form (an SM takes 64 bytes a clock
 // from L2; 128 x 256 tiles need 96).
 enum Kind { GRAM, SQUARE, APPLY };
+
+// Tries of a wait before it gives up.  An epilogue waits for all the products of its tile: 2^20 columns are
+// 16384 slices, some 9 ms; a try takes 20 ns at the very least.
+constexpr int WAIT_TRIES = 1 << 20;
+constexpr int SEGMENT = 16;                 // slices of 64: 1024 of depth
 
 constexpr int BM = 128, BK = 64;
 constexpr int EPILOGUE_WARPS = 8;
@@ -415,7 +421,7 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
                 i0 += rank * BM;
                 j0 += rank * R::B_COLS;
                 for (int step = step0; step < step1; ++step) {
-                    mbar_wait(empty + 8 * stage, phase ^ 1, gave_up, &g_ortho_timeouts);
+                    mbar_wait<WAIT_TRIES>(empty + 8 * stage, phase ^ 1, gave_up, &g_ortho_timeouts);
                     if (rank == 0) mbar_expect_tx(full + 8 * stage, CG * R::STAGE);
                     const uint32_t base = smem_u32(ring + stage * R::STAGE);
                     const uint32_t bar = CG == 2 ? in_first_block(full + 8 * stage) : full + 8 * stage;
@@ -435,7 +441,7 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
             }
             // the last copies have to land before the block may end: wait until they have been used
             for (int i = 0; i < R::STAGES; ++i) {
-                mbar_wait(empty + 8 * stage, phase ^ 1, gave_up, &g_ortho_timeouts);
+                mbar_wait<WAIT_TRIES>(empty + 8 * stage, phase ^ 1, gave_up, &g_ortho_timeouts);
                 if (++stage == R::STAGES) { stage = 0; phase ^= 1; }
             }
         }
@@ -445,29 +451,33 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
             constexpr int KB = KIND == APPLY ? 2048 : 32;      // bytes from one 16-deep piece of B to the next
             int stage = 0, phase = 0, acc = 0, acc_phase = 0;
             for (int tile = worker; tile < s.tiles; tile += workers) {
-                mbar_wait(freed + 8 * acc, acc_phase ^ 1, gave_up, &g_ortho_timeouts);
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t d = tmem + acc * R::SET;
-                for (int step = step0; step < step1; ++step) {
-                    mbar_wait(full + 8 * stage, phase, gave_up, &g_ortho_timeouts);
+                for (int begin = step0; begin < step1;) {
+                    const int stop = PAIR && begin + SEGMENT < step1 ? begin + SEGMENT : step1;
+                    mbar_wait<WAIT_TRIES>(freed + 8 * acc, acc_phase ^ 1, gave_up, &g_ortho_timeouts);
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t a = smem_u32(ring + stage * R::STAGE), b = a + R::PLANES * R::A_BYTES;
+                    const uint32_t d = tmem + acc * R::SET;
+                    for (int step = begin; step < stop; ++step) {
+                        mbar_wait<WAIT_TRIES>(full + 8 * stage, phase, gave_up, &g_ortho_timeouts);
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        const uint32_t a = smem_u32(ring + stage * R::STAGE), b = a + R::PLANES * R::A_BYTES;
 #pragma unroll
-                    for (int kk = 0; kk < BK / 16; ++kk) {
-                        const uint64_t ah = slice_desc(a + kk * 32, false), bh = slice_desc(b + kk * KB, KIND == APPLY);
-                        mma_f16<CG>(d + kk % R::MAINS * BN, ah, bh, IDESC, step > step0 || kk >= R::MAINS);
-                        if (PAIR) {
-                            constexpr int CROSS = R::MAINS * BN;
-                            mma_f16<CG>(d + CROSS, ah, slice_desc(b + R::B_BYTES + kk * KB, KIND == APPLY), IDESC, step > step0 || kk > 0);
-                            mma_f16<CG>(d + CROSS, slice_desc(a + R::A_BYTES + kk * 32, false), bh, IDESC, true);
+                        for (int kk = 0; kk < BK / 16; ++kk) {
+                            const uint64_t ah = slice_desc(a + kk * 32, false), bh = slice_desc(b + kk * KB, KIND == APPLY);
+                            mma_f16<CG>(d + kk % R::MAINS * BN, ah, bh, IDESC, step > begin || kk >= R::MAINS);
+                            if (PAIR) {
+                                constexpr int CROSS = R::MAINS * BN;
+                                mma_f16<CG>(d + CROSS, ah, slice_desc(b + R::B_BYTES + kk * KB, KIND == APPLY), IDESC, step > begin || kk > 0);
+                                mma_f16<CG>(d + CROSS, slice_desc(a + R::A_BYTES + kk * 32, false), bh, IDESC, true);
+                            }
                         }
+                        mma_commit<CG>(empty + 8 * stage);
+                        if (++stage == R::STAGES) { stage = 0; phase ^= 1; }
                     }
-                    mma_commit<CG>(empty + 8 * stage);
-                    if (++stage == R::STAGES) { stage = 0; phase ^= 1; }
+                    mma_commit<CG>(done + 8 * acc);
+                    if (acc == 1) acc_phase ^= 1;
+                    acc ^= 1;
+                    begin = stop;
                 }
-                mma_commit<CG>(done + 8 * acc);
-                if (acc == 1) acc_phase ^= 1;
-                acc ^= 1;
             }
         }
     } else if constexpr (KS == 1) {
@@ -497,16 +507,51 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
                 }
             };
             fetch(half * 32);
-            mbar_wait(done + 8 * acc, acc_phase, gave_up, &g_ortho_timeouts);
-            __syncwarp();                                  // the reads of TMEM are the whole warp's
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-#pragma unroll 1
-            for (int c = half * 32; c < BN; c += 64) {
-                const int col = j0 + c;
+            auto wait_done = [&]() {
+                mbar_wait<WAIT_TRIES>(done + 8 * acc, acc_phase, gave_up, &g_ortho_timeouts);
+                __syncwarp();                              // the reads of TMEM are the whole warp's
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            };
+            auto release = [&]() {
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) {
+                    if constexpr (CG == 2) arrive_cluster(freed_first + 8 * acc);
+                    else mbar_arrive(freed + 8 * acc);
+                }
+                if (acc == 1) acc_phase ^= 1;
+                acc ^= 1;
+            };
+            float run[PAIR ? BN / 64 : 1][32];             // the segments before the last
+            if constexpr (PAIR) {
+#pragma unroll
+                for (int g = 0; g < BN / 64; ++g)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) run[g][i] = 0.f;
+                for (int begin = step0 + SEGMENT; begin < step1; begin += SEGMENT) {
+                    wait_done();
+#pragma unroll
+                    for (int g = 0; g < BN / 64; ++g) {
+                        float v[32];
+                        load_sums<R::MAINS + R::PLANES - 1>(v, tmem + acc * R::SET + half * 32 + 64 * g + ((uint32_t)(quarter * 32) << 16), BN);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) run[g][i] += v[i];
+                    }
+                    release();
+                }
+            }
+            wait_done();
+#pragma unroll(PAIR ? BN / 64 : 1)
+            for (int part = 0; part < BN / 64; ++part) {
+                const int c = half * 32 + 64 * part, col = j0 + c;
                 const bool there = row < s.mp && col < s.cols;       // the same for the whole warp: extents are multiples of 64
-                if (c != half * 32) fetch(c);
+                if (part > 0) fetch(c);
                 float v[32];
                 load_sums<R::MAINS + R::PLANES - 1>(v, tmem + acc * R::SET + c + ((uint32_t)(quarter * 32) << 16), BN);
+                if constexpr (PAIR) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] += run[part][i];
+                }
                 if (!there) continue;
                 const bool both = PAIR || KIND != SQUARE;        // P is only ever a factor
 #pragma unroll
@@ -529,14 +574,7 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
                     }
                 }
             }
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) {
-                if constexpr (CG == 2) arrive_cluster(freed_first + 8 * acc);
-                else mbar_arrive(freed + 8 * acc);
-            }
-            if (acc == 1) acc_phase ^= 1;
-            acc ^= 1;
+            release();
         }
     }
     if constexpr (KS > 1) {
@@ -545,13 +583,24 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
         const int quarter = warp % 4, half = (warp - 2) / 4;
         float* mine = reinterpret_cast<float*>(ring);                 // [BN][128]
         if (warp >= 2) {
-            mbar_wait(done, 0, gave_up, &g_ortho_timeouts);
-            __syncwarp();
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            float v[32];
-            load_sums<R::MAINS + R::PLANES - 1>(v, tmem + half * 32 + ((uint32_t)(quarter * 32) << 16), BN);
+            float run[32] = {};
+            int acc = 0, acc_phase = 0;
+            for (int begin = step0; begin < step1; begin = PAIR ? begin + SEGMENT : step1) {
+                mbar_wait<WAIT_TRIES>(done + 8 * acc, acc_phase, gave_up, &g_ortho_timeouts);
+                __syncwarp();
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                float v[32];
+                load_sums<R::MAINS + R::PLANES - 1>(v, tmem + acc * R::SET + half * 32 + ((uint32_t)(quarter * 32) << 16), BN);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) mine[(half * 32 + i) * BM + quarter * 32 + lane] = v[i];
+                for (int i = 0; i < 32; ++i) run[i] += v[i];
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(freed + 8 * acc);
+                if (acc == 1) acc_phase ^= 1;
+                acc ^= 1;
+            }
+#pragma unroll
+            for (int i = 0; i < 32; ++i) mine[(half * 32 + i) * BM + quarter * 32 + lane] = run[i];
         }
         __syncwarp();
         cluster_sync();
@@ -804,7 +853,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
     // D = L R^T over `deep` pieces, K-major factors as hi and lo planes
     auto k_major = [](uint32_t plane, int piece) { return slice_desc(plane + piece / 4 * SMALL_BLOCK + piece % 4 * 32, false); };
     auto finish = [&]() {               // the products are done, and every thread may read their sums
-        mbar_wait(smem_u32(&bar), phase, gave_up, &g_ortho_timeouts);
+        mbar_wait<WAIT_TRIES>(smem_u32(&bar), phase, gave_up, &g_ortho_timeouts);
         phase ^= 1;
         __syncwarp();                   // the reads of TMEM are the whole warp's
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");

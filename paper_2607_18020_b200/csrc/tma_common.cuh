@@ -35,9 +35,10 @@ __device__ __forceinline__ void mbar_fence_init() {
 // Bounded wait for the phase with the given parity to complete.  A thread that has given up once
 // (`gave_up`) does not wait again, so a broken pipeline costs one bounded wait per thread, not one
 // per step.  `timeouts` is the translation unit's counter.
+template <int LIMIT = (1 << 16)>
 __device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, bool& gave_up, unsigned int* timeouts) {
     if (gave_up) return;
-    for (int it = 0; it < (1 << 16); ++it) {
+    for (int it = 0; it < LIMIT; ++it) {
         uint32_t done;
         asm volatile(
             "{\n\t.reg .pred p;\n\t"

@@ -20,6 +20,7 @@ import ctypes
 from typing import NamedTuple, Optional
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as B_
 
@@ -190,6 +191,7 @@ class _CausalConv(torch.autograd.Function):
         return y, left
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, gy, gleft):
         x, weight, bias, state = ctx.saved_tensors
         if gy is None:
@@ -342,6 +344,7 @@ class _SelectiveScan(torch.autograd.Function):
         return out, last
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, gout, glast):
         u, delta, A, B, C, D, z, delta_bias, state, kept = ctx.saved_tensors
         if gout is None:

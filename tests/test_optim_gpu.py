@@ -52,7 +52,8 @@ def test_orthogonalize(size, dtype, guard):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("size", [(8, 1000, 1030), (3, 1500, 700), (1, 2300, 2100), (20, 257, 513)])
+@pytest.mark.parametrize("size", [(8, 1000, 1030), (3, 1500, 700), (1, 2300, 2100), (20, 257, 513), (1, 33, 70001),
+                                  (1, 30000, 200)])
 def test_orthogonalize_large(size, dtype, guard):
     """Sizes that fill the GPU; the 64-bit form runs on it too."""
     from paper_2607_18020_b200 import binding, optim

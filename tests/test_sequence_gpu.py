@@ -246,6 +246,42 @@ def test_scan_nan_stays_in_its_channel_and_behind_its_node():
     assert torch.equal(got, last)
 
 
+def test_offsets_past_32_bits():
+    """Two rows 2^31 elements apart."""
+    from paper_2607_18020_b200 import sequence as Q
+    far, channels, length, n = 2 ** 31, 40, 37, 16
+    base = torch.empty(far + length * channels, dtype=torch.bfloat16, device="cuda")
+    r = gen(21)
+
+    def spread(t):
+        v = base.as_strided(t.shape, (far, t.shape[2], 1))
+        v.copy_(t)
+        return v
+    x, w, b = r(2, length, channels).to(torch.bfloat16), 0.5 * r(channels, 4), r(channels)
+    gy = r(2, length, channels).to(torch.bfloat16)
+    want = Q.causal_conv_fwd(x, w, b)[0]
+    gwant = Q.causal_conv_bwd(gy, x, w, b)
+    xs = spread(x)
+    assert torch.equal(Q.causal_conv_fwd(xs, w, b)[0], want)
+    for a, e in zip(Q.causal_conv_bwd(gy, xs, w, b)[:3], gwant[:3]):
+        assert torch.equal(a, e)
+    t, _, s, go, gl = scan_inputs((2, length, channels, n, False, True, True, True), torch.bfloat16, seed=22)
+    out, last, kept = Q.selective_scan_fwd(*t, state=s, keep=True)
+    g = Q.selective_scan_bwd(go, *t, state=s, kept=kept, gstate=gl)
+    for k in (0, 1, 3, 4, 6):                      # u, delta, B, C, z, one after the other
+        far_t = t[:k] + (spread(t[k]),) + t[k + 1:]
+        o2, l2, k2 = Q.selective_scan_fwd(*far_t, state=s, keep=True)
+        assert torch.equal(o2, out) and torch.equal(l2, last)
+        for a, e in zip(Q.selective_scan_bwd(go, *far_t, state=s, kept=k2, gstate=gl), g):
+            assert torch.equal(a, e)
+    g3 = Q.selective_scan_bwd(spread(go), *t, state=s, kept=kept, gstate=gl)
+    assert all(torch.equal(a, e) for a, e in zip(g3, g))
+    u1 = spread(t[0])[:, 5]
+    s1, s2 = s.clone(), s.clone()
+    rest = (t[1][:, 5], t[2], t[3][:, 5], t[4][:, 5])
+    assert torch.equal(Q.selective_scan_step(s1, u1, *rest), Q.selective_scan_step(s2, t[0][:, 5], *rest)) and torch.equal(s1, s2)
+
+
 def test_scan_extreme_steps():
     """delta far below and above: dt underflows to 0 (the state stays) or is large (the state is replaced)."""
     from paper_2607_18020_b200 import sequence as Q
