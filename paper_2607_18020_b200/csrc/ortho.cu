@@ -9,6 +9,8 @@
 // 124 us a step, 83 % of the library product's rate for the one that has no symmetry; the passes around
 // them 68 us).  Four fp32 1000 x 333 steps of the optimiser: 184 us, small products that are bound by
 // latency.
+#include <type_traits>
+
 #include "seq_common.cuh"
 #include "tma_common.cuh"
 
@@ -801,22 +803,37 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
     }
     pdl_wait_then_trigger();
     const int64_t k = blockIdx.x;
-    // the update's norm (muon: after moving the momentum on), rows along the warps
+    // The update (muon: after moving the momentum on), read once: a thread holds its elements, 32 columns
+    // apart in the rows of its warp, until the norm is known.
     const T* g = (const T*)io.grad + k * io.grad_matrix;
     float* mom = io.momentum ? io.momentum + k * io.rows * io.cols : nullptr;
+    constexpr int WARPS = SMALL_THREADS / 32, MOST = SMALL_M * SMALL_N / SMALL_THREADS;
+    const int shift = io.cols > 128 ? 3 : io.cols > 64 ? 2 : io.cols > 32 ? 1 : 0;      // 2^shift segments a row
+    const int held = ((io.rows + WARPS - 1) / WARPS) << shift;                          // elements a thread has, at most
+    float u[MOST];
     double sum = 0.0;
-#pragma unroll 2
-    for (int r = warp; r < io.rows; r += SMALL_THREADS / 32)
-#pragma unroll 4
-        for (int c = lane; c < io.cols; c += 32) {
-            float u = to_f32<T>(g[r * io.grad_row + c]);
-            if (mom != nullptr) {
-                const float next = fmaf(io.decay, mom[r * io.cols + c], u);
-                mom[r * io.cols + c] = next;
-                u = io.nesterov ? fmaf(io.decay, next, u) : next;
+    auto read = [&](auto most) {
+#pragma unroll
+        for (int e = 0; e < decltype(most)::value; ++e) {
+            const int r = warp + WARPS * (e >> shift), c = lane + 32 * (e & ((1 << shift) - 1));
+            u[e] = 0.f;
+            if (r < io.rows && c < io.cols) {
+                u[e] = to_f32<T>(g[r * io.grad_row + c]);
+                if (mom != nullptr) {
+                    const float next = fmaf(io.decay, mom[r * io.cols + c], u[e]);
+                    mom[r * io.cols + c] = next;
+                    u[e] = io.nesterov ? fmaf(io.decay, next, u[e]) : next;
+                }
             }
-            sum += (double)u * u;
         }
+#pragma unroll
+        for (int e = 0; e < decltype(most)::value; ++e) sum += (double)u[e] * u[e];
+    };
+    if (held <= MOST / 4) read(std::integral_constant<int, MOST / 4>{});
+    else if (held <= MOST / 2) read(std::integral_constant<int, MOST / 2>{});
+    else read(std::integral_constant<int, MOST>{});
+    if (io.m < SMALL_M || io.n < io.np)                    // zeros around X
+        for (int i = tid; i < 2 * xplane / 16; i += SMALL_THREADS) reinterpret_cast<uint4*>(xh)[i] = make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int m = 16; m > 0; m /= 2) sum += __shfl_xor_sync(~0u, sum, m);
     if (lane == 0) part[warp] = sum;
@@ -826,21 +843,23 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
     const uint32_t tmem = tmem_slot;
     sum = 0.0;
 #pragma unroll
-    for (int i = 0; i < SMALL_THREADS / 32; ++i) sum += part[i];
+    for (int i = 0; i < WARPS; ++i) sum += part[i];
     const float scale = (float)(1.0 / (sqrt(sum) + io.eps)) * SCALE;
-    // the first X, zeros around it
-    {
-        const int i = tid % SMALL_M;
-        for (int c = tid / SMALL_M * 8; c < io.np; c += SMALL_THREADS / SMALL_M * 8) {
-            float v[8];
+    auto place = [&](auto most) {                          // the first X
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                const int row = io.turned ? c + q : i, col = io.turned ? i : c + q;
-                v[q] = i < io.m && c + q < io.n ? update_at<T>(io, k, row, col) * scale : 0.f;
-            }
-            put8(xh, xl, i, c, v);
+        for (int e = 0; e < decltype(most)::value; ++e) {
+            const int r = warp + WARPS * (e >> shift), c = lane + 32 * (e & ((1 << shift) - 1));
+            if (r >= io.rows || c >= io.cols) continue;
+            const int i = io.turned ? c : r, j = io.turned ? r : c;
+            const float v = u[e] * scale;
+            const __half h = __float2half_rn(v);
+            *reinterpret_cast<__half*>(chunk_at(xh, i, j & ~7) + 2 * (j & 7)) = h;
+            *reinterpret_cast<__half*>(chunk_at(xl, i, j & ~7) + 2 * (j & 7)) = __float2half_rn(v - __half2float(h));
         }
-    }
+    };
+    if (held <= MOST / 4) place(std::integral_constant<int, MOST / 4>{});
+    else if (held <= MOST / 2) place(std::integral_constant<int, MOST / 2>{});
+    else place(std::integral_constant<int, MOST>{});
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();
 
@@ -946,7 +965,9 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
     }
     // out, along the matrix's rows
     T* out = (T*)io.out + k * io.rows * io.cols;
+#pragma unroll 2
     for (int r = warp; r < io.rows; r += SMALL_THREADS / 32)
+#pragma unroll 4
         for (int c = lane; c < io.cols; c += 32) {
             const float v = (io.turned ? value_at(xh, xl, c, r) : value_at(xh, xl, r, c)) * (1.f / SCALE);
             T* o = out + r * io.cols + c;
