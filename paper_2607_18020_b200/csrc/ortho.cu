@@ -278,6 +278,11 @@ __device__ __forceinline__ uint64_t slice_desc(uint32_t addr, bool mn_major, uin
     return d;
 }
 
+// The description of a slice `bytes` further on: the address field is the lowest, and no slice lies past its end.
+__device__ __forceinline__ uint64_t desc_at(uint64_t d, uint32_t bytes) {
+    return (d & 0xffffffff00000000ull) | (uint32_t)((uint32_t)d + (bytes >> 4));
+}
+
 template <int CG = 1>
 __device__ __forceinline__ void mma_f16(uint32_t tmem, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
     if constexpr (CG == 1)
@@ -415,6 +420,7 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
 
     if (warp == 0) {
         if (lane == 0) {
+            const uint32_t full_first = CG == 2 ? in_first_block(full) : full;
             int stage = 0, phase = 0;
             for (int tile = worker; tile < s.tiles; tile += workers) {
                 const int k = tile / s.per_matrix;
@@ -426,7 +432,7 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
                     mbar_wait<WAIT_TRIES>(empty + 8 * stage, phase ^ 1, gave_up, &g_ortho_timeouts);
                     if (rank == 0) mbar_expect_tx(full + 8 * stage, CG * R::STAGE);
                     const uint32_t base = smem_u32(ring + stage * R::STAGE);
-                    const uint32_t bar = CG == 2 ? in_first_block(full + 8 * stage) : full + 8 * stage;
+                    const uint32_t bar = full_first + 8 * stage;
 #pragma unroll
                     for (int p = 0; p < R::PLANES; ++p) {
                         load_slice<CG>(base + p * R::A_BYTES, &left, step * BK, i0, 2 * k + p, bar);
@@ -451,6 +457,8 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
         if (lane == 0 && rank == 0) {
             constexpr uint32_t IDESC = (1u << 4) | (KIND == APPLY ? 1u << 16 : 0u) | ((uint32_t)(BN / 8) << 17) | ((uint32_t)(CG * BM / 16) << 24);
             constexpr int KB = KIND == APPLY ? 2048 : 32;      // bytes from one 16-deep piece of B to the next
+            // one thread issues everything: what it computes per product has to stay short
+            const uint64_t a0 = slice_desc(smem_u32(ring), false), b0 = slice_desc(smem_u32(ring) + R::PLANES * R::A_BYTES, KIND == APPLY);
             int stage = 0, phase = 0, acc = 0, acc_phase = 0;
             for (int tile = worker; tile < s.tiles; tile += workers) {
                 for (int begin = step0; begin < step1;) {
@@ -461,15 +469,15 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
                     for (int step = begin; step < stop; ++step) {
                         mbar_wait<WAIT_TRIES>(full + 8 * stage, phase, gave_up, &g_ortho_timeouts);
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        const uint32_t a = smem_u32(ring + stage * R::STAGE), b = a + R::PLANES * R::A_BYTES;
+                        const uint64_t a = desc_at(a0, stage * R::STAGE), b = desc_at(b0, stage * R::STAGE);
 #pragma unroll
                         for (int kk = 0; kk < BK / 16; ++kk) {
-                            const uint64_t ah = slice_desc(a + kk * 32, false), bh = slice_desc(b + kk * KB, KIND == APPLY);
+                            const uint64_t ah = desc_at(a, kk * 32), bh = desc_at(b, kk * KB);
                             mma_f16<CG>(d + kk % R::MAINS * BN, ah, bh, IDESC, step > begin || kk >= R::MAINS);
                             if (PAIR) {
                                 constexpr int CROSS = R::MAINS * BN;
-                                mma_f16<CG>(d + CROSS, ah, slice_desc(b + R::B_BYTES + kk * KB, KIND == APPLY), IDESC, step > begin || kk > 0);
-                                mma_f16<CG>(d + CROSS, slice_desc(a + R::A_BYTES + kk * 32, false), bh, IDESC, true);
+                                mma_f16<CG>(d + CROSS, ah, desc_at(b, R::B_BYTES + kk * KB), IDESC, step > begin || kk > 0);
+                                mma_f16<CG>(d + CROSS, desc_at(a, R::A_BYTES + kk * 32), bh, IDESC, true);
                             }
                         }
                         mma_commit<CG>(empty + 8 * stage);
@@ -788,7 +796,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bar;
     __shared__ uint32_t tmem_slot;
-    __shared__ double part[SMALL_THREADS / 32];
+    __shared__ float part[SMALL_THREADS / 32];
     uint8_t* base = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
     const int xplane = io.np / 64 * SMALL_BLOCK;
     uint8_t *xh = base, *xl = base + xplane, *sh = base + 2 * xplane, *sl = sh + 2 * SMALL_BLOCK;
@@ -808,58 +816,85 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
     const T* g = (const T*)io.grad + k * io.grad_matrix;
     float* mom = io.momentum ? io.momentum + k * io.rows * io.cols : nullptr;
     constexpr int WARPS = SMALL_THREADS / 32, MOST = SMALL_M * SMALL_N / SMALL_THREADS;
-    const int shift = io.cols > 128 ? 3 : io.cols > 64 ? 2 : io.cols > 32 ? 1 : 0;      // 2^shift segments a row
-    const int held = ((io.rows + WARPS - 1) / WARPS) << shift;                          // elements a thread has, at most
-    float u[MOST];
-    double sum = 0.0;
-    auto read = [&](auto most) {
+    float u[MOST], top = 0.f;
+    auto read = [&](auto segments) {            // 32-column segments of a row
+        constexpr int SEG = decltype(segments)::value, ROWS = 16 * SEG <= MOST ? 16 : MOST / SEG;
+        const T* gr = g + warp * io.grad_row + lane;
+        float* mr = mom ? mom + warp * io.cols + lane : nullptr;
 #pragma unroll
-        for (int e = 0; e < decltype(most)::value; ++e) {
-            const int r = warp + WARPS * (e >> shift), c = lane + 32 * (e & ((1 << shift) - 1));
-            u[e] = 0.f;
-            if (r < io.rows && c < io.cols) {
-                u[e] = to_f32<T>(g[r * io.grad_row + c]);
+        for (int e = 0; e < MOST; ++e) u[e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            if (warp + WARPS * i >= io.rows) break;
+#pragma unroll
+            for (int q = 0; q < SEG; ++q) {
+                if (lane + 32 * q >= io.cols) continue;
+                float v = to_f32<T>(gr[32 * q]);
                 if (mom != nullptr) {
-                    const float next = fmaf(io.decay, mom[r * io.cols + c], u[e]);
-                    mom[r * io.cols + c] = next;
-                    u[e] = io.nesterov ? fmaf(io.decay, next, u[e]) : next;
+                    const float next = fmaf(io.decay, mr[32 * q], v);
+                    mr[32 * q] = next;
+                    v = io.nesterov ? fmaf(io.decay, next, v) : next;
                 }
+                u[i * SEG + q] = v;
             }
+            gr += WARPS * io.grad_row;
+            if (mom != nullptr) mr += WARPS * io.cols;
         }
 #pragma unroll
-        for (int e = 0; e < decltype(most)::value; ++e) sum += (double)u[e] * u[e];
+        for (int e = 0; e < ROWS * SEG; ++e) top = max_nan(top, fabsf(u[e]));
     };
-    if (held <= MOST / 4) read(std::integral_constant<int, MOST / 4>{});
-    else if (held <= MOST / 2) read(std::integral_constant<int, MOST / 2>{});
-    else read(std::integral_constant<int, MOST>{});
+    if (io.cols > 128) read(std::integral_constant<int, 8>{});
+    else if (io.cols > 64) read(std::integral_constant<int, 4>{});
+    else if (io.cols > 32) read(std::integral_constant<int, 2>{});
+    else read(std::integral_constant<int, 1>{});
     if (io.m < SMALL_M || io.n < io.np)                    // zeros around X
         for (int i = tid; i < 2 * xplane / 16; i += SMALL_THREADS) reinterpret_cast<uint4*>(xh)[i] = make_uint4(0, 0, 0, 0);
+    // the largest element first: squares of u 2^-e of a matrix of any scale fit in 32 bits
 #pragma unroll
-    for (int m = 16; m > 0; m /= 2) sum += __shfl_xor_sync(~0u, sum, m);
-    if (lane == 0) part[warp] = sum;
+    for (int m = 16; m > 0; m /= 2) top = max_nan(top, __shfl_xor_sync(~0u, top, m));
+    if (lane == 0) part[warp] = top;
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = tmem_slot;
-    sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < WARPS; ++i) top = max_nan(top, part[i]);
+    const int e2 = top > 0.f && top < INFINITY ? max(ilogbf(top), -100) : 0;
+    const float fit = ldexpf(1.f, -e2);
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < MOST; ++e) sum = fmaf(u[e] * fit, u[e] * fit, sum);
+#pragma unroll
+    for (int m = 16; m > 0; m /= 2) sum += __shfl_xor_sync(~0u, sum, m);
+    __syncthreads();
+    if (lane == 0) part[warp] = sum;
+    __syncthreads();
+    sum = 0.f;
 #pragma unroll
     for (int i = 0; i < WARPS; ++i) sum += part[i];
-    const float scale = (float)(1.0 / (sqrt(sum) + io.eps)) * SCALE;
-    auto place = [&](auto most) {                          // the first X
+    const float scale = (float)(1.0 / (ldexp((double)sqrtf(sum), e2) + io.eps)) * SCALE;
+    auto place = [&](auto segments) {                      // the first X
+        constexpr int SEG = decltype(segments)::value, ROWS = 16 * SEG <= MOST ? 16 : MOST / SEG;
 #pragma unroll
-        for (int e = 0; e < decltype(most)::value; ++e) {
-            const int r = warp + WARPS * (e >> shift), c = lane + 32 * (e & ((1 << shift) - 1));
-            if (r >= io.rows || c >= io.cols) continue;
-            const int i = io.turned ? c : r, j = io.turned ? r : c;
-            const float v = u[e] * scale;
-            const __half h = __float2half_rn(v);
-            *reinterpret_cast<__half*>(chunk_at(xh, i, j & ~7) + 2 * (j & 7)) = h;
-            *reinterpret_cast<__half*>(chunk_at(xl, i, j & ~7) + 2 * (j & 7)) = __float2half_rn(v - __half2float(h));
+        for (int n = 0; n < ROWS; ++n) {
+            const int r = warp + WARPS * n;
+            if (r >= io.rows) break;
+#pragma unroll
+            for (int q = 0; q < SEG; ++q) {
+                const int c = lane + 32 * q, i = io.turned ? c : r, j = io.turned ? r : c;
+                if (c >= io.cols) continue;
+                const float v = u[n * SEG + q] * scale;
+                const __half h = __float2half_rn(v);
+                const uint32_t at = (uint32_t)(chunk_at(xh, i, j & ~7) - xh) + 2 * (j & 7);
+                *reinterpret_cast<__half*>(xh + at) = h;
+                *reinterpret_cast<__half*>(xl + at) = __float2half_rn(v - __half2float(h));
+            }
         }
     };
-    if (held <= MOST / 4) place(std::integral_constant<int, MOST / 4>{});
-    else if (held <= MOST / 2) place(std::integral_constant<int, MOST / 2>{});
-    else place(std::integral_constant<int, MOST>{});
+    if (io.cols > 128) place(std::integral_constant<int, 8>{});
+    else if (io.cols > 64) place(std::integral_constant<int, 4>{});
+    else if (io.cols > 32) place(std::integral_constant<int, 2>{});
+    else place(std::integral_constant<int, 1>{});
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();
 
@@ -870,7 +905,9 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
     uint32_t phase = 0;
     bool gave_up = false;
     // D = L R^T over `deep` pieces, K-major factors as hi and lo planes
-    auto k_major = [](uint32_t plane, int piece) { return slice_desc(plane + piece / 4 * SMALL_BLOCK + piece % 4 * 32, false); };
+    auto k_major = [](uint64_t plane, int piece) { return desc_at(plane, piece / 4 * SMALL_BLOCK + piece % 4 * 32); };
+    const uint64_t dxh = slice_desc(axh, false), dxl = slice_desc(axl, false), dsh = slice_desc(ash, false), dsl = slice_desc(asl, false);
+    const uint64_t rxh = slice_desc(axh, true, SMALL_BLOCK), rxl = slice_desc(axl, true, SMALL_BLOCK);
     auto finish = [&]() {               // the products are done, and every thread may read their sums
         mbar_wait<WAIT_TRIES>(smem_u32(&bar), phase, gave_up, &g_ortho_timeouts);
         phase ^= 1;
@@ -886,11 +923,13 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
     constexpr uint32_t IDESC = (1u << 4) | ((uint32_t)(SMALL_M / 16) << 24), SQUARE_IDESC = IDESC | (uint32_t)(128 / 8) << 17;
     for (int step = 0; step < steps; ++step) {
         if (tid == 0) {                                                   // S = X X^T: columns 0-127, cross products 128-255
-            for (int p = 0; p < deep_n; ++p) {
-                const uint64_t h = k_major(axh, p);
+#pragma unroll
+            for (int p = 0; p < SMALL_N / 16; ++p) {
+                if (p >= deep_n) break;
+                const uint64_t h = k_major(dxh, p);
                 mma_f16(tmem, h, h, SQUARE_IDESC, p > 0);
                 if (PAIR) {
-                    const uint64_t l = k_major(axl, p);
+                    const uint64_t l = k_major(dxl, p);
                     mma_f16(tmem + 128, h, l, SQUARE_IDESC, p > 0);
                     mma_f16(tmem + 128, l, h, SQUARE_IDESC, true);
                 }
@@ -912,8 +951,10 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
         }
         written();
         if (tid == 0) {                                                   // S S: columns 256-383, cross products 384-511
-            for (int p = 0; p < deep_m; ++p) {
-                const uint64_t h = k_major(ash, p), l = k_major(asl, p);
+#pragma unroll
+            for (int p = 0; p < SMALL_M / 16; ++p) {
+                if (p >= deep_m) break;
+                const uint64_t h = k_major(dsh, p), l = k_major(dsl, p);
                 mma_f16(tmem + 256, h, h, SQUARE_IDESC, p > 0);
                 mma_f16(tmem + 384, h, l, SQUARE_IDESC, p > 0);
                 mma_f16(tmem + 384, l, h, SQUARE_IDESC, true);
@@ -936,12 +977,14 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
         written();
         if (tid == 0) {                                                   // P X: columns 0-255, cross products 256-511
             const uint32_t idesc = IDESC | 1u << 16 | (uint32_t)(io.np / 8) << 17;
-            for (int p = 0; p < deep_m; ++p) {
-                const uint64_t h = k_major(ash, p), r = slice_desc(axh + p * 2048, true, SMALL_BLOCK);
+#pragma unroll
+            for (int p = 0; p < SMALL_M / 16; ++p) {
+                if (p >= deep_m) break;
+                const uint64_t h = k_major(dsh, p), r = desc_at(rxh, p * 2048);
                 mma_f16(tmem, h, r, idesc, p > 0);
                 if (PAIR) {
-                    mma_f16(tmem + 256, h, slice_desc(axl + p * 2048, true, SMALL_BLOCK), idesc, p > 0);
-                    mma_f16(tmem + 256, k_major(asl, p), r, idesc, true);
+                    mma_f16(tmem + 256, h, desc_at(rxl, p * 2048), idesc, p > 0);
+                    mma_f16(tmem + 256, k_major(dsl, p), r, idesc, true);
                 }
             }
             mma_commit(smem_u32(&bar));
