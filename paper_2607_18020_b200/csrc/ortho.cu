@@ -5,10 +5,10 @@
 // on the shorter side (taller matrices are turned on the way in and back on the way out).
 //
 // Per step 2 m^2 (m + n) multiplications and additions are needed with the symmetry of S and S S, m <= n.
-// 4096^2 bf16, 5 steps: 1.37e12, 831 us at the measured bf16 rate, measured 1.39 ms (products 70, 70 and
-// 124 us a step, 83 % of the library product's rate for the one that has no symmetry; the passes around
-// them 68 us).  Four fp32 1000 x 333 steps of the optimiser: 184 us, small products that are bound by
-// latency.
+// 4096^2 bf16, 5 steps: 1.37e12, 831 us at the measured bf16 rate, measured 1.35 ms (products 69, 69 and
+// 124 us a step, 80 % of the library product's rate for the one that has no symmetry; the passes around
+// them 64 us).  Four fp32 1000 x 333 steps of the optimiser: 187 us, small products that are bound by
+// latency.  Eight fp32 128 x 128 matrices: 36 us, 9 around the steps and 5.5 a step.
 #include <type_traits>
 
 #include "seq_common.cuh"
@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(256) ortho_square_kernel(OrthoIo io, double* _
         const T* g = (const T*)io.grad + k * io.grad_matrix + r * io.grad_row;
         float* mom = io.momentum ? io.momentum + ((int64_t)k * io.rows + r) * io.cols : nullptr;
         if (io.wide) {
-#pragma unroll 2
+#pragma unroll 4
             for (int c = lane * 8; c < io.cols; c += 256) {
                 float u[8];
                 load8<T>(u, g + c);
