@@ -7,7 +7,7 @@
 // Per step 2 m^2 (m + n) multiplications and additions are needed with the symmetry of S and S S, m <= n.
 // 4096^2 bf16, 5 steps: 1.37e12, 831 us at the measured bf16 rate, measured 1.35 ms (products 69, 69 and
 // 124 us a step, 80 % of the library product's rate for the one that has no symmetry; the passes around
-// them 64 us).  Four fp32 1000 x 333 steps of the optimiser: 187 us, small products that are bound by
+// them 64 us).  Four fp32 1000 x 333 steps of the optimiser: 183 us, small products that are bound by
 // latency.  Eight fp32 128 x 128 matrices: 36 us, 9 around the steps and 5.5 a step.
 #include <type_traits>
 
@@ -240,6 +240,7 @@ enum Kind { GRAM, SQUARE, APPLY };
 // Tries of a wait before it gives up.  An epilogue waits for all the products of its tile: 2^20 columns are
 // 16384 slices, some 9 ms; a try takes 20 ns at the very least.
 constexpr int WAIT_TRIES = 1 << 20;
+constexpr double PAIRS_START = 2e-6;        // seconds that a pair of blocks takes longer to start (four 333 x 1000: 14.4 us, 13.1 without pairs)
 constexpr int SEGMENT = 16;                 // slices of 64: 1024 of depth
 
 constexpr int BM = 128, BK = 64;
@@ -738,7 +739,7 @@ double product_seconds(const ProductShape& s, int64_t count, int sms) {
     const int64_t waves = ceil_div(tiles, workers), blocks = (tiles < workers ? tiles : workers) * CG * KS;
     const double shared = R::STAGE * (double)blocks / 9e12, alone = R::STAGE / 76e9, math = (PAIR ? 3 : 1) * 2.0 * BM * BN * BK * 1.0 / 14e12;
     const double step = shared > alone ? (shared > math ? shared : math) : (alone > math ? alone : math);
-    return waves * ceil_div(steps, KS) * step + 3e-6 * BN / 128 + (LOWER ? 2e-6 : 0) + (KS > 1 ? 1.5e-6 : 0);
+    return waves * ceil_div(steps, KS) * step + 3e-6 * BN / 128 + (LOWER ? 2e-6 : 0) + (KS > 1 ? 1.5e-6 : 0) + (CG > 1 ? PAIRS_START : 0);
 }
 
 // Pairs of SMs, or single blocks with tiles of 128 or 64 columns, the latter with the depth split over 2 or 4
