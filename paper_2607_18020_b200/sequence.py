@@ -9,7 +9,8 @@ with `state=` / `return_state=True` for a row that continues an earlier one, and
     y = causal_conv_step(x, window, weight, bias)                 window moved on in place
     y = selective_scan_step(state, u, delta, A, B, C, D, z, ...)  state moved on in place
 
-`*_fwd` / `*_bwd` are the same calls without autograd.  Activations are fp32, bf16 or fp16 CUDA tensors
+`*_fwd` / `*_bwd` are the same calls without autograd.  The single-node forms are not differentiable either:
+they compute values, and a backward pass that reaches their result raises.  Activations are fp32, bf16 or fp16 CUDA tensors
 of one type whose channel axis is contiguous (slices of a wider projection are read in place);
 parameters and scan states are fp32.  Everything runs in libfpde.so on torch's current stream; torch
 allocates the outputs and the scratch memory.  There is no CPU path.
@@ -90,6 +91,30 @@ def _new(like, shape=None):
     return torch.empty(like.shape if shape is None else shape, dtype=like.dtype, device=like.device)
 
 
+class _ValuesOnly(torch.autograd.Function):
+    """The result of a call that has no gradient: asking for one is an error, not a zero."""
+
+    @staticmethod
+    def forward(ctx, name, call, *inputs):
+        ctx.name = name
+        return call()
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("%s is not differentiable: train on whole rows, and call it under torch.no_grad()" % ctx.name)
+
+
+def _values_only(name, call, *inputs):
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in inputs):
+        return _ValuesOnly.apply(name, call, *inputs)
+    return call()
+
+
+def _moved_on(t):
+    """`t` changed behind autograd's back: a backward pass that has kept it must not take it for what it was."""
+    torch.autograd.graph.increment_version(t)
+
+
 _plans = B_.ArgPlans()
 _lay = _plans.layout
 
@@ -166,7 +191,12 @@ def causal_conv_bwd(gy, x, weight, bias=None, state=None, silu=True, gstate=None
 
 
 def causal_conv_step(x, window, weight, bias=None, silu=True):
-    """One node per row: x (batch, channels) -> y; `window` (batch, width - 1, channels) is moved on in place."""
+    """One node per row: x (batch, channels) -> y; `window` (batch, width - 1, channels) is moved on in place.
+    Not differentiable."""
+    return _values_only("causal_conv_step", lambda: _conv_step(x, window, weight, bias, silu), x, window, weight, bias)
+
+
+def _conv_step(x, window, weight, bias, silu):
     key = ("conv step", bool(silu), _lay(x), _lay(window), _lay(weight), _lay(bias))
     a = _plans.get(key)
     if a is None:
@@ -178,6 +208,7 @@ def causal_conv_step(x, window, weight, bias=None, silu=True):
     a.x, a.weight, a.bias, a.y = x.data_ptr(), weight.data_ptr(), _ptr(bias), y.data_ptr()
     a.state = a.state_out = window.data_ptr()
     B_.call_with("fpde_causal_conv_step", a, x.device.index)
+    _moved_on(window)
     return y
 
 
@@ -317,8 +348,13 @@ def selective_scan_bwd(gout, u, delta, A, B, C, D=None, z=None, delta_bias=None,
 
 def selective_scan_step(state, u, delta, A, B, C, D=None, z=None, delta_bias=None, delta_softplus=True):
     """One node per row: u, delta, z (batch, channels), B, C (batch, states) -> out (batch, channels); `state`
-    (batch, channels, states) is moved on in place."""
+    (batch, channels, states) is moved on in place.  Not differentiable."""
     t = (u, delta, A, B, C, D, z, delta_bias, state)
+    return _values_only("selective_scan_step", lambda: _scan_step(t, delta_softplus), *t)
+
+
+def _scan_step(t, delta_softplus):
+    u, delta, A, B, C, D, z, delta_bias, state = t
     key = ("scan step", bool(delta_softplus), _lay(u), _lay(delta), _lay(A), _lay(B), _lay(C), _lay(D), _lay(z), _lay(delta_bias), _lay(state))
     a = _plans.get(key)
     if a is None:
@@ -330,6 +366,7 @@ def selective_scan_step(state, u, delta, A, B, C, D=None, z=None, delta_bias=Non
     _scan_pointers(a, *t)
     a.state_out, a.out = state.data_ptr(), out.data_ptr()
     B_.call_with("fpde_selective_scan_step", a, u.device.index)
+    _moved_on(state)
     return out
 
 
