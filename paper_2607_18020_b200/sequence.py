@@ -104,8 +104,12 @@ class _ValuesOnly(torch.autograd.Function):
         raise RuntimeError("%s is not differentiable: train on whole rows, and call it under torch.no_grad()" % ctx.name)
 
 
+def _wants_grad(*inputs):
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in inputs)
+
+
 def _values_only(name, call, *inputs):
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in inputs):
+    if _wants_grad(*inputs):
         return _ValuesOnly.apply(name, call, *inputs)
     return call()
 
@@ -372,9 +376,8 @@ def _scan_step(t, delta_softplus):
 
 class _SelectiveScan(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, u, delta, A, B, C, D, z, delta_bias, delta_softplus, state):
-        out, last, kept = selective_scan_fwd(u, delta, A, B, C, D, z, delta_bias, delta_softplus, state,
-                                             keep=any(ctx.needs_input_grad))
+    def forward(ctx, u, delta, A, B, C, D, z, delta_bias, delta_softplus, state, keep):
+        out, last, kept = selective_scan_fwd(u, delta, A, B, C, D, z, delta_bias, delta_softplus, state, keep)
         ctx.save_for_backward(u, delta, A, B, C, D, z, delta_bias, state, kept)
         ctx.delta_softplus = delta_softplus
         ctx.set_materialize_grads(False)
@@ -387,10 +390,12 @@ class _SelectiveScan(torch.autograd.Function):
         if gout is None:
             gout = torch.zeros_like(u)
         g = selective_scan_bwd(gout, u, delta, A, B, C, D, z, delta_bias, ctx.delta_softplus, state, kept, glast)
-        return g.u, g.delta, g.A, g.B, g.C, g.D, g.z, g.delta_bias, None, g.state
+        return g.u, g.delta, g.A, g.B, g.C, g.D, g.z, g.delta_bias, None, g.state, None
 
 
 def selective_scan(u, delta, A, B, C, D=None, z=None, delta_bias=None, delta_softplus=True, state=None, return_state=False):
     """selective_scan_fwd, differentiable in every tensor."""
-    out, last = _SelectiveScan.apply(u, delta, A, B, C, D, z, delta_bias, delta_softplus, state)
+    # decided here: inside forward() grad mode is always off, and parameters ask for gradients in any mode
+    keep = _wants_grad(u, delta, A, B, C, D, z, delta_bias, state)
+    out, last = _SelectiveScan.apply(u, delta, A, B, C, D, z, delta_bias, delta_softplus, state, keep)
     return (out, last) if return_state else out

@@ -1,5 +1,5 @@
 """How the sequence operators behave towards autograd beyond their gradients: tensors that single-node calls move
-on in place, and results that have no gradient."""
+on in place, results that have no gradient, and what is stored for a backward pass that cannot follow."""
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -92,3 +92,25 @@ def test_steps_without_grad_mode_carry_no_graph():
     with torch.no_grad():
         assert not Q.causal_conv_step(x, window, w, b).requires_grad
         assert not Q.selective_scan_step(state, u, delta, A, B, C).requires_grad
+
+
+def test_nothing_is_stored_where_no_backward_pass_can_follow():
+    """A, D and the bias of a network in use are parameters: they ask for gradients in every mode."""
+    from paper_2607_18020_b200 import sequence as Q
+    batch, length, c, n = 2, 2048, 256, 16
+    stored = batch * (length // 8) * c * n * 4
+    u, delta, z = randn(batch, length, c), randn(batch, length, c), randn(batch, length, c)
+    B, C = randn(batch, length, n), randn(batch, length, n)
+    A, D, bias = (torch.nn.Parameter(t) for t in (-torch.rand(c, n, device="cuda"), randn(c), randn(c)))
+    for needs, mode in ((False, torch.no_grad()), (False, torch.inference_mode()), (True, torch.enable_grad())):
+        with mode:
+            Q.selective_scan(u, delta, A, B, C, D=D, z=z, delta_bias=bias)
+            torch.cuda.synchronize()
+            held = torch.cuda.memory_allocated()
+            torch.cuda.reset_peak_memory_stats()
+            Q.selective_scan(u, delta, A, B, C, D=D, z=z, delta_bias=bias)
+            rose = torch.cuda.max_memory_allocated() - held
+        assert (rose >= u.numel() * 4 + stored) == needs, (rose, needs)
+    with torch.no_grad():
+        out = Q.selective_scan(u, delta, A, B, C, D=D, z=z, delta_bias=bias)
+    assert not out.requires_grad and torch.equal(out, Q.selective_scan_fwd(u, delta, A, B, C, D, z, bias)[0])
