@@ -10,4 +10,5 @@ gather-form discrete adjoint, boundary-gradient correction) behind a C ABI.
 
 Nothing is loaded at import time; the binding raises if the shared library is missing.
 """
-__all__ = ["binding", "workloads", "build", "sequence", "optim"]
+# autograd, sequence, optim and slabs need torch: `import *` leaves them to whoever names them.
+__all__ = ["binding", "workloads", "build"]
