@@ -254,13 +254,29 @@ __device__ __forceinline__ void store_states(float* p, int n, int states, bool p
         if (n + i < states) p[n + i] = v[i];
 }
 
+// States that do not exist have zero A, B and C and stay zero while everything is finite; an infinite dt, dt u or gy
+// makes NaN of them (0 times infinity), which the sums over states must not see.  Lanes that hold no state at all
+// read dt, dt u and gy from a column of zeros behind the channels: full lanes (8, 16, 32, 64 states) lose nothing, others
+// an access to shared memory (8 x 1024 x 2048 x 12 fp32 236 -> 247 us, 4 x 2048 x 2048 x 4 bf16 training 805 -> 827).  Where
+// a lane's four states exist in part (PARTIAL: the number of states is no multiple of four), the others are cleared at
+// every node (4 x 2048 x 1024 x 5 bf16 training 442 -> 456).  Looking for infinities first, and clearing only in the
+// tiles that have them, took a second loop in the kernel and made the first one 3 to 12 % slower for every size.
+constexpr int ZEROS = 2;          // columns
+__device__ __forceinline__ Quad existing(const Quad& q, int n, int states) {
+    float v[NS];
+    quad_to(v, q);
+#pragma unroll
+    for (int i = 0; i < NS; ++i) v[i] = n + i < states ? v[i] : 0.f;
+    return quad_of(v);
+}
+
 // ------------------------------------------------------------------------------------------ forward
 template <typename T, int S, int NC, int VEC, bool ENDS>
 struct FwdSpace {
     static constexpr int THREADS = fwd_threads(NC), CT = THREADS / S * NC, NP = S * NS;
     static constexpr int RP = THREADS / (CT / VEC), RN = THREADS / NP;      // rows at a time
     using Act = Feed<T, VEC, TILE, RP, ENDS ? 2 : 3, THREADS>;
-    __align__(16) float2 sdt[TILE][CT], sdu[TILE][CT];      // dt, dt;  dt u, dt u: pairs as the arithmetic wants them
+    __align__(16) float2 sdt[TILE][CT + ZEROS], sdu[TILE][CT + ZEROS];      // dt, dt;  dt u, dt u: pairs as the arithmetic wants them
     __align__(16) float sb[TILE][NP], sc[ENDS ? 1 : TILE][NP];
     __align__(8) float sy[ENDS ? 1 : TILE][CT];
     typename Act::Space room;
@@ -269,7 +285,7 @@ struct FwdSpace {
 // ENDS = false: the march.  ENDS = true, for rows cut into chunks: only what the join needs,
 // local[b][chunk][channel][state] = state at the chunk's end when it starts from zero and
 // sums[b][chunk][channel] = sum of dt.
-template <typename T, int S, int NC, int VEC, bool ENDS>
+template <typename T, int S, int NC, int VEC, bool ENDS, bool PARTIAL>
 __global__ void __launch_bounds__(fwd_threads(NC), fwd_blocks(NC)) scan_fwd_kernel(ScanIn<T> in, const float* __restrict__ state, const float* __restrict__ enter,
                                                            T* __restrict__ out, float* __restrict__ state_out, float* __restrict__ kept,
                                                            float* __restrict__ local, float* __restrict__ sums, ScanShape s) {
@@ -283,7 +299,7 @@ __global__ void __launch_bounds__(fwd_threads(NC), fwd_blocks(NC)) scan_fwd_kern
     Space& m = *reinterpret_cast<Space*>(raw_space);
     const Where w = where(s);
     const int tid = threadIdx.x, q = tid % S, cl = tid / S * NC;
-    const int c0 = w.tile * CT, c = c0 + cl;
+    const int c0 = w.tile * CT, c = c0 + cl, from = ENDS || q * NS < s.states ? cl : CT;      // where it reads dt and dt u
     const int64_t first = (int64_t)w.chunk * s.chunk;
     const int64_t end = first + s.chunk < s.length ? first + s.chunk : s.length;
     const int64_t per = (int64_t)s.channels * s.states;
@@ -321,6 +337,7 @@ __global__ void __launch_bounds__(fwd_threads(NC), fwd_blocks(NC)) scan_fwd_kern
             ct.load(s.C_node, rn, here, row_n, TILE);
         }
     };
+    if (!ENDS && tid < TILE * ZEROS) m.sdt[tid / ZEROS][CT + tid % ZEROS] = m.sdu[tid / ZEROS][CT + tid % ZEROS] = make_float2(0.f, 0.f);
     float total[NC] = {};
     int left = (int)(end - first);               // nodes of the chunk from this tile on
     fetch(left);
@@ -368,12 +385,13 @@ __global__ void __launch_bounds__(fwd_threads(NC), fwd_blocks(NC)) scan_fwd_kern
                 Quad c4;
                 if constexpr (!ENDS) c4 = quad_at(&m.sc[k0 + r][q * NS]);
                 uint64_t dt2[NC], du2[NC];
-                get_channels(dt2, &m.sdt[k0 + r][cl]);
-                get_channels(du2, &m.sdu[k0 + r][cl]);
+                get_channels(dt2, &m.sdt[k0 + r][from]);
+                get_channels(du2, &m.sdu[k0 + r][from]);
 #pragma unroll
                 for (int k = 0; k < NC; ++k) {
                     h[k].lo = fma2(exp2_pair(mul2(dt2[k], a2[k].lo)), h[k].lo, mul2(du2[k], b4.lo));
                     h[k].hi = fma2(exp2_pair(mul2(dt2[k], a2[k].hi)), h[k].hi, mul2(du2[k], b4.hi));
+                    if constexpr (PARTIAL) h[k] = existing(h[k], q * NS, s.states);
                     if constexpr (ENDS) {
                         float dt, same;
                         unpair(dt2[k], dt, same);
@@ -465,7 +483,7 @@ __global__ void __launch_bounds__(256) scan_join_kernel(float* __restrict__ loca
 template <typename T, int S, int NC, int VEC>
 struct BackSpace {
     static constexpr int THREADS = back_threads(NC), CT = THREADS / S * NC, NP = S * NS, WARPS = THREADS / 32;
-    __align__(16) float2 sdt[TILE][CT], sdu[TILE][CT], sg[TILE][CT];     // dt, dt;  dt u, dt u;  gy, gy
+    __align__(16) float2 sdt[TILE][CT + ZEROS], sdu[TILE][CT + ZEROS], sg[TILE][CT + ZEROS];     // dt, dt;  dt u, dt u;  gy, gy
     __align__(16) float sb[TILE][NP], sc[TILE][NP];
     __align__(8) float sy[TILE][CT], st[TILE][CT], sq[TILE][CT];         // C.h, p.B, sum p a h A
     float red[WARPS][TILE][2 * NP];                         // the warps' sums over channels: gB, gC
@@ -479,7 +497,7 @@ struct BackSpace {
 // this chunk's share of gA, gD and gdelta_bias.
 // ENDS = true, for rows cut into chunks: only local = what the adjoint state hands to the node before the
 // chunk when nothing comes from behind it, and the sums of dt.
-template <typename T, int S, int NC, int VEC, bool ENDS>
+template <typename T, int S, int NC, int VEC, bool ENDS, bool PARTIAL>
 __global__ void __launch_bounds__(back_threads(NC), back_blocks(NC)) scan_bwd_kernel(ScanIn<T> in, const float* __restrict__ kept, const float* __restrict__ enter,
                                                                 const float* __restrict__ gstate_out, T* __restrict__ gu,
                                                                 T* __restrict__ gdelta, T* __restrict__ gz, float* __restrict__ gstate,
@@ -495,7 +513,7 @@ __global__ void __launch_bounds__(back_threads(NC), back_blocks(NC)) scan_bwd_ke
     Space& m = *reinterpret_cast<Space*>(raw_space);
     const Where w = where(s);
     const int tid = threadIdx.x, q = tid % S, cl = tid / S * NC, warp = tid / 32, lane = tid % 32;
-    const int c0 = w.tile * CT, c = c0 + cl;
+    const int c0 = w.tile * CT, c = c0 + cl, from = ENDS || q * NS < s.states ? cl : CT;      // where it reads dt, dt u and gy
     const int64_t first = (int64_t)w.chunk * s.chunk;
     const int64_t end = first + s.chunk < s.length ? first + s.chunk : s.length;
     const int64_t per = (int64_t)s.channels * s.states;
@@ -560,6 +578,8 @@ __global__ void __launch_bounds__(back_threads(NC), back_blocks(NC)) scan_bwd_ke
 #pragma unroll
             for (int k = 0; k < NC; ++k) m.hold[piece][k][tid] = {0, 0};
         if (ntiles > 0) fetch_states(last);
+        if (tid < TILE * ZEROS)
+            m.sdt[tid / ZEROS][CT + tid % ZEROS] = m.sdu[tid / ZEROS][CT + tid % ZEROS] = m.sg[tid / ZEROS][CT + tid % ZEROS] = make_float2(0.f, 0.f);
     }
     float total[NC] = {};
     if (ntiles > 0) fetch((int)(end - last));
@@ -635,12 +655,13 @@ __global__ void __launch_bounds__(back_threads(NC), back_blocks(NC)) scan_bwd_ke
                         const int r = k0 + j;
                         const Quad b4 = quad_at(&m.sb[base + r][q * NS]), c4 = quad_at(&m.sc[base + r][q * NS]);
                         uint64_t dt2[NC], du2[NC];
-                        get_channels(dt2, &m.sdt[base + r][cl]);
-                        get_channels(du2, &m.sdu[base + r][cl]);
+                        get_channels(dt2, &m.sdt[base + r][from]);
+                        get_channels(du2, &m.sdu[base + r][from]);
 #pragma unroll
                         for (int k = 0; k < NC; ++k) {
                             hs[r + 1][k].lo = fma2(exp2_pair(mul2(dt2[k], a2[k].lo)), hs[r][k].lo, mul2(du2[k], b4.lo));
                             hs[r + 1][k].hi = fma2(exp2_pair(mul2(dt2[k], a2[k].hi)), hs[r][k].hi, mul2(du2[k], b4.hi));
+                            if constexpr (PARTIAL) hs[r + 1][k] = existing(hs[r + 1][k], q * NS, s.states);
                             y[NC * j + k] = sum2(fma2(c4.lo, hs[r + 1][k].lo, mul2(c4.hi, hs[r + 1][k].hi)));
                         }
                     }
@@ -656,15 +677,16 @@ __global__ void __launch_bounds__(back_threads(NC), back_blocks(NC)) scan_bwd_ke
                         asm volatile("" ::: "memory");
                         const Quad b4 = quad_at(&m.sb[base + r][q * NS]), c4 = quad_at(&m.sc[base + r][q * NS]);
                         uint64_t dt2[NC], du2[NC], g2[NC];
-                        get_channels(dt2, &m.sdt[base + r][cl]);
-                        get_channels(du2, &m.sdu[base + r][cl]);
-                        get_channels(g2, &m.sg[base + r][cl]);
+                        get_channels(dt2, &m.sdt[base + r][from]);
+                        get_channels(du2, &m.sdu[base + r][from]);
+                        get_channels(g2, &m.sg[base + r][from]);
                         Quad vb, vc;                   // shares of gB and gC of this node, summed over the thread's channels
 #pragma unroll
                         for (int k = 0; k < NC; ++k) {
                             const uint64_t g = g2[k], dt = dt2[k], du = du2[k];
                             p[k].lo = fma2(c4.lo, g, p[k].lo);
                             p[k].hi = fma2(c4.hi, g, p[k].hi);
+                            if constexpr (PARTIAL) p[k] = existing(p[k], q * NS, s.states);
                             vb.lo = k == 0 ? mul2(p[k].lo, du) : fma2(p[k].lo, du, vb.lo);
                             vb.hi = k == 0 ? mul2(p[k].hi, du) : fma2(p[k].hi, du, vb.hi);
                             vc.lo = k == 0 ? mul2(hs[r + 1][k].lo, g) : fma2(hs[r + 1][k].lo, g, vc.lo);
@@ -672,6 +694,7 @@ __global__ void __launch_bounds__(back_threads(NC), back_blocks(NC)) scan_bwd_ke
                             tb[NC * j + k] = sum2(fma2(p[k].lo, b4.lo, mul2(p[k].hi, b4.hi)));
                             p[k].lo = mul2(p[k].lo, exp2_pair(mul2(dt, a2[k].lo)));
                             p[k].hi = mul2(p[k].hi, exp2_pair(mul2(dt, a2[k].hi)));
+                            if constexpr (PARTIAL) p[k] = existing(p[k], q * NS, s.states);
                             const uint64_t ph_lo = mul2(p[k].lo, hs[r][k].lo), ph_hi = mul2(p[k].hi, hs[r][k].hi);
                             ta[NC * j + k] = sum2(fma2(ph_lo, a2[k].lo, mul2(ph_hi, a2[k].hi)));
                             ga[k].lo = fma2(ph_lo, dt, ga[k].lo);
@@ -682,10 +705,10 @@ __global__ void __launch_bounds__(back_threads(NC), back_blocks(NC)) scan_bwd_ke
                         unpair(vb.hi, v[2], v[3]);
                         unpair(vc.lo, v[4], v[5]);
                         unpair(vc.hi, v[6], v[7]);
-                        const int from = sum_lanes<2 * NS, 16, S>(v, lane);
+                        const int share = sum_lanes<2 * NS, 16, S>(v, lane);
 #pragma unroll
                         for (int i = 0; i < sums_left<2 * NS, 16, S>(); ++i)
-                            m.red[warp][base + r][((from + i) / NS) * NP + q * NS + (from + i) % NS] = v[i];
+                            m.red[warp][base + r][((share + i) / NS) * NP + q * NS + (share + i) % NS] = v[i];
                     }
                     put_sums<S, NC, CT>(m.st, tb, base + k0, cl, q);
                     put_sums<S, NC, CT>(m.sq, ta, base + k0, cl, q);
@@ -712,10 +735,10 @@ __global__ void __launch_bounds__(back_threads(NC), back_blocks(NC)) scan_bwd_ke
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
                     const float dt = m.sdt[r][col + i].x, gy = m.sg[r][col + i].x, through = m.st[r][col + i];
-                    ou[i] = fmaf(dt, through, dd[i] * gy);
+                    ou[i] = fmaf(dt, through, in.D ? dd[i] * gy : 0.f);      // without D there is no term, not 0 gy
                     od[i] = fmaf(u[i], through, m.sq[r][col + i] * (1.f / LOG2_E));
                     if (s.softplus) od[i] *= slope[i];
-                    if (in.z) oz[i] = go[i] * fmaf(dd[i], u[i], m.sy[r][col + i]) * (gate[i] * fmaf(z[i], 1.f - gate[i], 1.f));
+                    if (in.z) oz[i] = go[i] * (in.D ? fmaf(dd[i], u[i], m.sy[r][col + i]) : m.sy[r][col + i]) * (gate[i] * fmaf(z[i], 1.f - gate[i], 1.f));
                     gd[i] = fmaf(gy, u[i], gd[i]);
                     gbias[i] += od[i];
                 }
@@ -821,9 +844,9 @@ __global__ void __launch_bounds__(256) scan_sum_a_kernel(const float* __restrict
 // Bound by the states' traffic, 8 bytes each.  S lanes share a channel, four states each, and take four
 // channels of one row at once, so that their loads are on their way together.  What is per channel (dt,
 // the gate) is computed by one lane for each: the lane to which the sum over the states comes.  B and C
-// of the row are loaded once per thread.  state_out may be state: a thread reads what it writes.
-template <typename T, int S>
-__global__ void __launch_bounds__(STEP_THREADS) scan_step_kernel(ScanIn<T> in, const float* state, T* __restrict__ out, float* state_out,
+// of the row are loaded once per thread.  PADDED: there are fewer states than lanes hold.  state_out may be state: a thread reads what it writes.
+template <typename T, int S, bool PADDED>
+__global__ void __launch_bounds__(STEP_THREADS, PADDED && S > 2 ? 8 : 1) scan_step_kernel(ScanIn<T> in, const float* state, T* __restrict__ out, float* state_out,
                                                                  int across, bool packed, ScanShape s) {
     pdl_wait_then_trigger();
     constexpr int CT = STEP_THREADS / S, K = STEP_CHANNELS;           // channels next to one another
@@ -875,6 +898,7 @@ __global__ void __launch_bounds__(STEP_THREADS) scan_step_kernel(ScanIn<T> in, c
         const uint64_t d = both(step * LOG2_E), w = both(du);
         h[k].lo = fma2(exp2_pair(mul2(d, a2[k].lo)), h[k].lo, mul2(w, b4.lo));
         h[k].hi = fma2(exp2_pair(mul2(d, a2[k].hi)), h[k].hi, mul2(w, b4.hi));
+        if constexpr (PADDED) h[k] = existing(h[k], n0, s.states);
         y[k] = sum2(fma2(c4.lo, h[k].lo, mul2(c4.hi, h[k].hi)));
         if (c < s.channels && state_out != nullptr) store_states(state_out + (b * s.channels + c) * s.states, n0, s.states, packed, h[k]);
     }
@@ -1023,17 +1047,20 @@ cudaError_t run_fwd(const fpde_scan_args* a, const ScanShape& s, cudaStream_t st
         float* sums = (float*)((char*)a->workspace + w.sums);
         constexpr size_t bytes = sizeof(FwdSpace<T, S, 1, VEC, true>);
         static std::atomic<uint64_t> allowed{0};
-        FPDE_TRY(allow_smem(scan_fwd_kernel<T, S, 1, VEC, true>, bytes, allowed));
-        FPDE_TRY(launch_kernel_smem(scan_fwd_kernel<T, S, 1, VEC, true>, grid, dim3(fwd_threads(1)), bytes, st, in, (const float*)nullptr, (const float*)nullptr,
+        FPDE_TRY(allow_smem(scan_fwd_kernel<T, S, 1, VEC, true, false>, bytes, allowed));
+        FPDE_TRY(launch_kernel_smem(scan_fwd_kernel<T, S, 1, VEC, true, false>, grid, dim3(fwd_threads(1)), bytes, st, in, (const float*)nullptr, (const float*)nullptr,
                                (T*)nullptr, (float*)nullptr, (float*)nullptr, local, sums, s));
         FPDE_TRY(launch_kernel(scan_join_kernel<false>, dim3((unsigned)ceil_div(a->batch * s.channels * s.states, 256)), dim3(256), st,
                                local, (const float*)sums, a->A, a->state, a->batch, s));
     }
     constexpr size_t bytes = sizeof(FwdSpace<T, S, NC, VEC, false>);
-    static std::atomic<uint64_t> allowed{0};
-    FPDE_TRY(allow_smem(scan_fwd_kernel<T, S, NC, VEC, false>, bytes, allowed));
-    return launch_kernel_smem(scan_fwd_kernel<T, S, NC, VEC, false>, grid, dim3(fwd_threads(NC)), bytes, st, in, a->state, (const float*)local, (T*)a->out,
-                         a->state_out, (float*)a->kept, (float*)nullptr, (float*)nullptr, s);
+    auto march = [&](auto* kernel, std::atomic<uint64_t>& allowed) {
+        FPDE_TRY(allow_smem(kernel, bytes, allowed));
+        return launch_kernel_smem(kernel, grid, dim3(fwd_threads(NC)), bytes, st, in, a->state, (const float*)local, (T*)a->out, a->state_out,
+                                  (float*)a->kept, (float*)nullptr, (float*)nullptr, s);
+    };
+    static std::atomic<uint64_t> whole{0}, partial{0};
+    return s.states % NS == 0 ? march(scan_fwd_kernel<T, S, NC, VEC, false, false>, whole) : march(scan_fwd_kernel<T, S, NC, VEC, false, true>, partial);
 }
 
 template <typename T, int S, int NC, int VEC>
@@ -1051,18 +1078,20 @@ cudaError_t run_bwd(const fpde_scan_args* a, const ScanShape& s, cudaStream_t st
         local = (float*)(ws + w.local);
         float* sums = (float*)(ws + w.sums);
         static std::atomic<uint64_t> allowed{0};
-        FPDE_TRY(allow_smem(scan_bwd_kernel<T, S, 1, VEC, true>, ends, allowed));
-        FPDE_TRY(launch_kernel_smem(scan_bwd_kernel<T, S, 1, VEC, true>, grid, dim3(back_threads(1)), ends, st, in, (const float*)nullptr,
+        FPDE_TRY(allow_smem(scan_bwd_kernel<T, S, 1, VEC, true, false>, ends, allowed));
+        FPDE_TRY(launch_kernel_smem(scan_bwd_kernel<T, S, 1, VEC, true, false>, grid, dim3(back_threads(1)), ends, st, in, (const float*)nullptr,
                                     (const float*)nullptr, (const float*)nullptr, (T*)nullptr, (T*)nullptr, (T*)nullptr, (float*)nullptr,
                                     (float*)nullptr, (float*)nullptr, local, sums, a->batch, s));
         FPDE_TRY(launch_kernel(scan_join_kernel<true>, dim3((unsigned)ceil_div(a->batch * s.channels * s.states, 256)), dim3(256), st,
                                local, (const float*)sums, a->A, a->gstate_out, a->batch, s));
     }
-    static std::atomic<uint64_t> allowed{0};
-    FPDE_TRY(allow_smem(scan_bwd_kernel<T, S, NC, VEC, false>, bytes, allowed));
-    FPDE_TRY(launch_kernel_smem(scan_bwd_kernel<T, S, NC, VEC, false>, grid, dim3(back_threads(NC)), bytes, st, in, (const float*)a->kept,
-                                (const float*)local, a->gstate_out, (T*)a->gu, (T*)a->gdelta, (T*)a->gz, a->gstate, part_bc, part_a,
-                                (float*)nullptr, (float*)nullptr, a->batch, s));
+    auto march = [&](auto* kernel, std::atomic<uint64_t>& allowed) {
+        FPDE_TRY(allow_smem(kernel, bytes, allowed));
+        return launch_kernel_smem(kernel, grid, dim3(back_threads(NC)), bytes, st, in, (const float*)a->kept, (const float*)local, a->gstate_out,
+                                  (T*)a->gu, (T*)a->gdelta, (T*)a->gz, a->gstate, part_bc, part_a, (float*)nullptr, (float*)nullptr, a->batch, s);
+    };
+    static std::atomic<uint64_t> whole{0}, partial{0};
+    FPDE_TRY(s.states % NS == 0 ? march(scan_bwd_kernel<T, S, NC, VEC, false, false>, whole) : march(scan_bwd_kernel<T, S, NC, VEC, false, true>, partial));
     if (a->batch * a->length > 0)
         FPDE_TRY(launch_kernel(scan_sum_bc_kernel<T>, dim3((unsigned)ceil_div(a->batch * a->length * 2 * S * NS, 256)), dim3(256), st,
                                (const float*)part_bc, s.tiles, a->batch * a->length, S * NS, s.states, (T*)a->gB, (T*)a->gC));
@@ -1076,7 +1105,8 @@ cudaError_t run_step(const fpde_scan_args* a, cudaStream_t st) {
     const int64_t across = ceil_div(s.channels, STEP_THREADS / S * STEP_CHANNELS), blocks = a->batch * across;
     if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
     const bool packed = s.states % NS == 0 && aligned(a->state, 16) && aligned(a->state_out, 16) && aligned(a->A, 16);
-    return launch_kernel(scan_step_kernel<T, S>, dim3((unsigned)blocks), dim3(STEP_THREADS), st, inputs<T>(a), a->state, (T*)a->out, a->state_out,
+    auto kernel = s.states == S * NS ? scan_step_kernel<T, S, false> : scan_step_kernel<T, S, true>;
+    return launch_kernel(kernel, dim3((unsigned)blocks), dim3(STEP_THREADS), st, inputs<T>(a), a->state, (T*)a->out, a->state_out,
                          (int)across, packed, s);
 }
 
