@@ -95,9 +95,9 @@ class _ValuesOnly(torch.autograd.Function):
     """The result of a call that has no gradient: asking for one is an error, not a zero."""
 
     @staticmethod
-    def forward(ctx, name, call, *inputs):
-        ctx.name = name
-        return call()
+    def forward(ctx, call, *args):
+        ctx.name = call.__name__
+        return call(*args)                  # grad mode is off in here: the call does its work
 
     @staticmethod
     def backward(ctx, *grads):
@@ -105,13 +105,11 @@ class _ValuesOnly(torch.autograd.Function):
 
 
 def _wants_grad(*inputs):
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in inputs)
-
-
-def _values_only(name, call, *inputs):
-    if _wants_grad(*inputs):
-        return _ValuesOnly.apply(name, call, *inputs)
-    return call()
+    if torch.is_grad_enabled():
+        for t in inputs:
+            if t is not None and t.requires_grad:
+                return True
+    return False
 
 
 def _moved_on(t):
@@ -197,10 +195,8 @@ def causal_conv_bwd(gy, x, weight, bias=None, state=None, silu=True, gstate=None
 def causal_conv_step(x, window, weight, bias=None, silu=True):
     """One node per row: x (batch, channels) -> y; `window` (batch, width - 1, channels) is moved on in place.
     Not differentiable."""
-    return _values_only("causal_conv_step", lambda: _conv_step(x, window, weight, bias, silu), x, window, weight, bias)
-
-
-def _conv_step(x, window, weight, bias, silu):
+    if _wants_grad(x, window, weight, bias):
+        return _ValuesOnly.apply(causal_conv_step, x, window, weight, bias, silu)
     key = ("conv step", bool(silu), _lay(x), _lay(window), _lay(weight), _lay(bias))
     a = _plans.get(key)
     if a is None:
@@ -354,11 +350,8 @@ def selective_scan_step(state, u, delta, A, B, C, D=None, z=None, delta_bias=Non
     """One node per row: u, delta, z (batch, channels), B, C (batch, states) -> out (batch, channels); `state`
     (batch, channels, states) is moved on in place.  Not differentiable."""
     t = (u, delta, A, B, C, D, z, delta_bias, state)
-    return _values_only("selective_scan_step", lambda: _scan_step(t, delta_softplus), *t)
-
-
-def _scan_step(t, delta_softplus):
-    u, delta, A, B, C, D, z, delta_bias, state = t
+    if _wants_grad(*t):
+        return _ValuesOnly.apply(selective_scan_step, state, u, delta, A, B, C, D, z, delta_bias, delta_softplus)
     key = ("scan step", bool(delta_softplus), _lay(u), _lay(delta), _lay(A), _lay(B), _lay(C), _lay(D), _lay(z), _lay(delta_bias), _lay(state))
     a = _plans.get(key)
     if a is None:
