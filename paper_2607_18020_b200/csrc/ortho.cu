@@ -128,8 +128,23 @@ __global__ void __launch_bounds__(256) ortho_square_kernel(OrthoIo io, double* _
     }
 }
 
-// 1 / (|U| + eps) from the blocks' sums (at most 256), added in the same order by every block that asks.
-__device__ __forceinline__ float inverse_norm(const double* sums, int blocks, double eps, double (&part)[8]) {
+// What makes the first X of U: 2^14 / (|U| + eps), in two factors.  The first is a power of two, and 1 unless the whole
+// nears the ends of fp32's range (norms below 1.3e-26 or above 2.1e34, which fp32 and bf16 gradients can have: with eps = 0
+// the single factor overflowed below 5e-35, and lost digits above 1.4e42).
+struct Fit {
+    float first, second;
+    Fit() = default;
+    __device__ __forceinline__ Fit(double norm, double eps) {
+        const double whole = (double)SCALE / (norm + eps);
+        const int side = whole > 0x1p100 ? 1 : whole < 0x1p-100 ? -1 : 0;
+        first = side > 0 ? 0x1p100f : side < 0 ? 0x1p-100f : 1.f;
+        second = (float)(side > 0 ? whole * 0x1p-100 : side < 0 ? whole * 0x1p100 : whole);
+    }
+    __device__ __forceinline__ float operator()(float v) const { return v * first * second; }
+};
+
+// The same from the blocks' sums of squares (at most 256), added in the same order by every block that asks.
+__device__ __forceinline__ Fit fit_of(const double* sums, int blocks, double eps, double (&part)[8]) {
     double v = threadIdx.x < blocks ? sums[threadIdx.x] : 0.0;
 #pragma unroll
     for (int m = 16; m > 0; m /= 2) v += __shfl_xor_sync(~0u, v, m);
@@ -138,7 +153,7 @@ __device__ __forceinline__ float inverse_norm(const double* sums, int blocks, do
     v = 0.0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) v += part[i];
-    return (float)(1.0 / (sqrt(v) + eps));
+    return Fit(sqrt(v), eps);
 }
 
 // Eight values of a row, already scaled, as hi and lo halves.
@@ -161,7 +176,7 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(OrthoIo io, const doub
     const int k = blockIdx.x / (across * down), t = blockIdx.x % (across * down), i0 = t / across * 64, j0 = t % across * 64;
     const int r0 = io.turned ? j0 : i0, c0 = io.turned ? i0 : j0;
     // the elements are on their way while the norm is added up
-    float scale;
+    Fit fit;
     if (io.wide) {
         float in[2][8];
 #pragma unroll
@@ -171,7 +186,7 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(OrthoIo io, const doub
             for (int i = 0; i < 8; ++i) in[q][i] = 0.f;
             if (r0 + r < io.rows && c0 + c < io.cols) update8<T>(in[q], io, k, r0 + r, c0 + c);
         }
-        scale = inverse_norm(sums + (int64_t)k * blocks, blocks, io.eps, part) * SCALE;
+        fit = fit_of(sums + (int64_t)k * blocks, blocks, io.eps, part);
 #pragma unroll
         for (int q = 0; q < 2; ++q)
 #pragma unroll
@@ -183,7 +198,7 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(OrthoIo io, const doub
             const int r = threadIdx.x / 64 + q * 4, c = threadIdx.x % 64;
             in[q] = r0 + r < io.rows && c0 + c < io.cols ? update_at<T>(io, k, r0 + r, c0 + c) : 0.f;
         }
-        scale = inverse_norm(sums + (int64_t)k * blocks, blocks, io.eps, part) * SCALE;
+        fit = fit_of(sums + (int64_t)k * blocks, blocks, io.eps, part);
 #pragma unroll
         for (int q = 0; q < 16; ++q) tile[threadIdx.x / 64 + q * 4][threadIdx.x % 64] = in[q];
     }
@@ -196,7 +211,7 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(OrthoIo io, const doub
 #pragma unroll
         for (int q = 0; q < 8; ++q) {       // padding stays zero, whatever the norm is
             const bool there = i0 + i < io.m && j0 + j + q < io.n;
-            v[q] = there ? (io.turned ? tile[j + q][i] : tile[i][j + q]) * scale : 0.f;
+            v[q] = there ? fit(io.turned ? tile[j + q][i] : tile[i][j + q]) : 0.f;
         }
         Pack<__half, 8> hi, lo;
         split8(v, hi, lo);
@@ -873,7 +888,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
     sum = 0.f;
 #pragma unroll
     for (int i = 0; i < WARPS; ++i) sum += part[i];
-    const float scale = (float)(1.0 / (ldexp((double)sqrtf(sum), e2) + io.eps)) * SCALE;
+    const Fit to_x(ldexp((double)sqrtf(sum), e2), io.eps);
     auto place = [&](auto segments) {                      // the first X
         constexpr int SEG = decltype(segments)::value, ROWS = 16 * SEG <= MOST ? 16 : MOST / SEG;
 #pragma unroll
@@ -884,7 +899,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
             for (int q = 0; q < SEG; ++q) {
                 const int c = lane + 32 * q, i = io.turned ? c : r, j = io.turned ? r : c;
                 if (c >= io.cols) continue;
-                const float v = u[n * SEG + q] * scale;
+                const float v = to_x(u[n * SEG + q]);
                 const __half h = __float2half_rn(v);
                 const uint32_t at = (uint32_t)(chunk_at(xh, i, j & ~7) - xh) + 2 * (j & 7);
                 *reinterpret_cast<__half*>(xh + at) = h;
