@@ -105,16 +105,11 @@ class _ValuesOnly(torch.autograd.Function):
 
 
 def _wants_grad(*inputs):
-    if torch.is_grad_enabled():
-        for t in inputs:
-            if t is not None and t.requires_grad:
-                return True
-    return False
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in inputs)
 
 
-def _moved_on(t):
-    """`t` changed behind autograd's back: a backward pass that has kept it must not take it for what it was."""
-    torch.autograd.graph.increment_version(t)
+# For a tensor changed behind autograd's back: a backward pass that has kept it must not take it for what it was.
+_moved_on = torch.autograd.graph.increment_version
 
 
 _plans = B_.ArgPlans()
@@ -195,7 +190,7 @@ def causal_conv_bwd(gy, x, weight, bias=None, state=None, silu=True, gstate=None
 def causal_conv_step(x, window, weight, bias=None, silu=True):
     """One node per row: x (batch, channels) -> y; `window` (batch, width - 1, channels) is moved on in place.
     Not differentiable."""
-    if _wants_grad(x, window, weight, bias):
+    if torch.is_grad_enabled() and _wants_grad(x, window, weight, bias):
         return _ValuesOnly.apply(causal_conv_step, x, window, weight, bias, silu)
     key = ("conv step", bool(silu), _lay(x), _lay(window), _lay(weight), _lay(bias))
     a = _plans.get(key)
@@ -350,7 +345,7 @@ def selective_scan_step(state, u, delta, A, B, C, D=None, z=None, delta_bias=Non
     """One node per row: u, delta, z (batch, channels), B, C (batch, states) -> out (batch, channels); `state`
     (batch, channels, states) is moved on in place.  Not differentiable."""
     t = (u, delta, A, B, C, D, z, delta_bias, state)
-    if _wants_grad(*t):
+    if torch.is_grad_enabled() and _wants_grad(*t):
         return _ValuesOnly.apply(selective_scan_step, state, u, delta, A, B, C, D, z, delta_bias, delta_softplus)
     key = ("scan step", bool(delta_softplus), _lay(u), _lay(delta), _lay(A), _lay(B), _lay(C), _lay(D), _lay(z), _lay(delta_bias), _lay(state))
     a = _plans.get(key)
