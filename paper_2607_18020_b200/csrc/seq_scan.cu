@@ -460,20 +460,44 @@ __global__ void __launch_bounds__(256) scan_join_kernel(float* __restrict__ loca
     float carry = start ? start[e] : 0.f;
     constexpr int AHEAD = 8;      // chunks whose values are loaded together: the chain itself is one fused add each
     for (int k0 = 0; k0 < s.chunks; k0 += AHEAD) {
-        float own[AHEAD], keep[AHEAD];
+        float own[AHEAD], keep[AHEAD], decay[AHEAD];
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
             const bool there = k0 + k < s.chunks;
             const int64_t at = b * s.chunks + (BACK ? s.chunks - 1 - (k0 + k) : k0 + k);
             own[k] = there ? local[at * per + cn] : 0.f;
-            keep[k] = there ? exp2_f32(a2 * sums[at * s.channels + c]) : 0.f;
+            decay[k] = there ? a2 * sums[at * s.channels + c] : 0.f;
+            keep[k] = exp2_f32(decay[k]);
+        }
+        const float start_of_group = carry;
+        float enters[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            enters[k] = carry;
+            carry = fmaf(keep[k], carry, own[k]);         // chunks that do not exist: own and keep are 0 and 1
+        }
+        // What is not finite stays so, so one look at the end of a group is enough.  A chunk's decay may leave fp32's range
+        // where those of its nodes do not: then it is applied in halves, and what was zero or infinite stays so, as it
+        // would node by node.
+        if (!(fabsf(carry) < INFINITY)) {
+            carry = start_of_group;
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                enters[k] = carry;
+                if (keep[k] == 0.f || keep[k] == INFINITY) {
+                    const float half = exp2_f32(0.5f * decay[k]);
+                    const bool stays = (carry == 0.f || fabsf(carry) == INFINITY) && fabsf(decay[k]) < INFINITY;
+                    carry = (stays ? carry : carry * half * half) + own[k];
+                } else {
+                    carry = fmaf(keep[k], carry, own[k]);
+                }
+            }
         }
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
             if (k0 + k >= s.chunks) break;
             const int64_t at = b * s.chunks + (BACK ? s.chunks - 1 - (k0 + k) : k0 + k);
-            local[at * per + cn] = carry;
-            carry = fmaf(keep[k], carry, own[k]);
+            local[at * per + cn] = enters[k];
         }
     }
 }
@@ -895,10 +919,11 @@ __global__ void __launch_bounds__(STEP_THREADS, PADDED && S > 2 ? 8 : 1) scan_st
     for (int k = 0; k < K; ++k) {
         const int c = c0 + k * CT, owner = (lane & ~(S - 1)) + (S >= K ? k * (S / K) : k / OWN);
         const float step = __shfl_sync(~0u, dt[k % OWN], owner), du = __shfl_sync(~0u, dt[k % OWN] * u[k % OWN], owner);
-        const uint64_t d = both(step * LOG2_E), w = both(du);
+        const bool live = !PADDED || mine;                            // infinities stop at lanes without a state
+        const uint64_t d = both(live ? step * LOG2_E : 0.f), w = both(live ? du : 0.f);
         h[k].lo = fma2(exp2_pair(mul2(d, a2[k].lo)), h[k].lo, mul2(w, b4.lo));
         h[k].hi = fma2(exp2_pair(mul2(d, a2[k].hi)), h[k].hi, mul2(w, b4.hi));
-        if constexpr (PADDED) h[k] = existing(h[k], n0, s.states);
+        if (PADDED && s.states % NS != 0) h[k] = existing(h[k], n0, s.states);
         y[k] = sum2(fma2(c4.lo, h[k].lo, mul2(c4.hi, h[k].hi)));
         if (c < s.channels && state_out != nullptr) store_states(state_out + (b * s.channels + c) * s.states, n0, s.states, packed, h[k]);
     }
