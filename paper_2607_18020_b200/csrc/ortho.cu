@@ -1112,7 +1112,9 @@ int check(const fpde_ortho_args* a) {
     if (a == nullptr) return FPDE_ERR_NULL;
     if (!dtype_ok(a->dtype)) return FPDE_ERR_DTYPE;
     if (a->steps < 0 || a->steps > 100 || !(a->eps >= 0)) return FPDE_ERR_PARAM;
-    if (a->count < 0 || a->rows < 0 || a->cols < 0 || a->rows > (1 << 20) || a->cols > (1 << 20) || a->count > (1 << 20)) return FPDE_ERR_SHAPE;
+    if (a->count < 0 || a->rows < 0 || a->cols < 0 || a->rows > (1 << 20) || a->cols > (1 << 20) || a->count > (1 << 20) ||
+        !product_fits(a->count, padded(a->rows), padded(a->cols)))
+        return FPDE_ERR_SHAPE;
     return FPDE_OK;
 }
 

@@ -188,6 +188,13 @@ __device__ __forceinline__ void store_v(T* p, typename Lanes<N>::V a) {
 }
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// Sizes whose product is at most 2^48: strides can be zero, so an input of any extents can be handed in, and workspaces,
+// grids and offsets of at most 2^12 times the product still fit 64 bits.
+inline bool product_fits(int64_t a, int64_t b, int64_t c) {
+    const auto at_least_1 = [](int64_t v) { return (unsigned __int128)(v > 0 ? v : 1); };
+    const unsigned __int128 most = (unsigned __int128)1 << 48, ab = at_least_1(a) * at_least_1(b);
+    return ab <= most && ab * at_least_1(c) <= most;
+}
 inline bool aligned(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 inline size_t dtype_bytes(int dtype) { return dtype == FPDE_F32 ? 4 : 2; }
 inline bool dtype_ok(int dtype) { return dtype == FPDE_F32 || dtype == FPDE_BF16 || dtype == FPDE_F16; }

@@ -391,17 +391,18 @@ __global__ void __launch_bounds__(128) conv_step_kernel(const T* __restrict__ x,
     }
 }
 
-int check_conv_sizes(const fpde_conv_args* a) {
+int check_conv_sizes(const fpde_conv_args* a, bool step = false) {
     if (a == nullptr) return FPDE_ERR_NULL;
     if (!dtype_ok(a->dtype)) return FPDE_ERR_DTYPE;
     if (a->width < 1 || a->width > FPDE_CONV_MAX_WIDTH) return FPDE_ERR_PARAM;
-    if (a->batch < 0 || a->channels < 0 || a->length < 0 || a->channels > (1 << 24) || a->length > (1ll << 40) || a->batch > (1ll << 40))
+    if (a->batch < 0 || a->channels < 0 || a->length < 0 || a->channels > (1 << 24) || a->length > (1ll << 40) || a->batch > (1ll << 40) ||
+        !product_fits(a->batch, step ? a->width : a->length + a->width, a->channels))
         return FPDE_ERR_SHAPE;
     return FPDE_OK;
 }
 
 int check_conv(const fpde_conv_args* a, bool step) {
-    const int st = check_conv_sizes(a);
+    const int st = check_conv_sizes(a, step);
     if (st != FPDE_OK) return st;
     if (a->batch * a->channels > 0) {
         const size_t e = dtype_bytes(a->dtype);

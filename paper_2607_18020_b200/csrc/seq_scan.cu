@@ -990,17 +990,18 @@ ScanShape plan(const fpde_scan_args* a, bool backward) {
     return s;
 }
 
-int check_scan_sizes(const fpde_scan_args* a) {
+int check_scan_sizes(const fpde_scan_args* a, bool step = false) {
     if (a == nullptr) return FPDE_ERR_NULL;
     if (!dtype_ok(a->dtype)) return FPDE_ERR_DTYPE;
     if (a->states < 1 || a->states > FPDE_SCAN_MAX_STATES) return FPDE_ERR_PARAM;
-    if (a->batch < 0 || a->channels < 0 || a->length < 0 || a->channels > (1 << 24) || a->length > (1ll << 36) || a->batch > (1ll << 36))
+    if (a->batch < 0 || a->channels < 0 || a->length < 0 || a->channels > (1 << 24) || a->length > (1ll << 36) || a->batch > (1ll << 36) ||
+        !product_fits(a->batch, step ? 1 : a->length, a->channels))
         return FPDE_ERR_SHAPE;
     return FPDE_OK;
 }
 
 int check_scan(const fpde_scan_args* a, bool step) {
-    const int st = check_scan_sizes(a);
+    const int st = check_scan_sizes(a, step);
     if (st != FPDE_OK) return st;
     if (a->batch * a->channels > 0) {
         if (a->A == nullptr) return FPDE_ERR_NULL;
