@@ -575,6 +575,9 @@ int fpde_selective_scan_step(const fpde_scan_args* args, void* stream);
  * Precision: with fp32 arrays the products are formed from fp16 pairs that hold 22 bits of each
  * factor and summed in fp32; with 16-bit arrays from single fp16 factors (11 bits), while the
  * running X keeps 22 bits.
+ *
+ * The products wait for one another inside the kernels, each wait for two seconds at most.  A call in
+ * which one gave up writes NaN (fpde_muon_step: over the weight) and counts in fpde_diag_ortho_timeouts.
  */
 typedef struct {
     int32_t dtype, steps, nesterov, reserved;
@@ -595,6 +598,9 @@ int fpde_muon_step(const fpde_ortho_args* args, void* stream);
 /* Bounded waits inside the orthogonalisation's products that gave up since the library was loaded
  * (0 in a healthy run; see fpde_diag_tma_timeouts). */
 unsigned int fpde_diag_ortho_timeouts(void);
+/* fpde_orthogonalize with one wait of a millisecond that nothing ends (and that is not counted): what a call does
+ * when it loses one. */
+int fpde_diag_orthogonalize_lost(const fpde_ortho_args* args, void* stream);
 
 #ifdef __cplusplus
 }

@@ -158,7 +158,8 @@ def lib():
             getattr(L, name).argtypes = [ctypes.POINTER(args)] + extra
         for name, args in (("fpde_causal_conv_fwd", ConvArgs), ("fpde_causal_conv_bwd", ConvArgs), ("fpde_causal_conv_step", ConvArgs),
                            ("fpde_selective_scan_fwd", ScanArgs), ("fpde_selective_scan_bwd", ScanArgs),
-                           ("fpde_selective_scan_step", ScanArgs), ("fpde_orthogonalize", OrthoArgs), ("fpde_muon_step", OrthoArgs)):
+                           ("fpde_selective_scan_step", ScanArgs), ("fpde_orthogonalize", OrthoArgs), ("fpde_muon_step", OrthoArgs),
+                           ("fpde_diag_orthogonalize_lost", OrthoArgs)):
             getattr(L, name).restype = ctypes.c_int
             getattr(L, name).argtypes = [ctypes.POINTER(args), ctypes.c_void_p]
         L.fpde_diag_ortho_timeouts.restype = ctypes.c_uint

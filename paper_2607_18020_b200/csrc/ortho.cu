@@ -77,8 +77,9 @@ __device__ __forceinline__ void update8(float (&v)[8], const OrthoIo& io, int64_
 // Moves the momentum on (muon) and leaves each block's sum of squares of the update, in 64 bits: the
 // squares of gradients of any scale fit.  A warp takes whole rows, `blocks` blocks share a matrix.
 template <typename T>
-__global__ void __launch_bounds__(256) ortho_square_kernel(OrthoIo io, double* __restrict__ sums, int blocks) {
+__global__ void __launch_bounds__(256) ortho_square_kernel(OrthoIo io, double* __restrict__ sums, int blocks, unsigned int* lost) {
     pdl_wait_then_trigger();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *lost = 0;
     __shared__ double part[8];
     const int k = blockIdx.x / blocks, lane = threadIdx.x % 32;
     const float decay = io.decay;
@@ -252,9 +253,13 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(OrthoIo io, const doub
 // from L2; 128 x 256 tiles need 96).
 enum Kind { GRAM, SQUARE, APPLY };
 
-// Tries of a wait before it gives up.  An epilogue waits for all the products of its tile: 2^20 columns are
-// 16384 slices, some 9 ms; a try takes 20 ns at the very least.
-constexpr int WAIT_TRIES = 1 << 20;
+// Every wait is bounded: it gives up after WAIT_NS, or WAIT_TRIES tries (of 20 ns at the very least).  The longest that is
+// due, an epilogue's for all the products of a tile 2^20 deep, takes some 9 ms when nothing else uses the GPU.  A
+// thread that gives up tells the others of its block, which then stop too, and the call (`lost`): its result is NaN.
+constexpr uint64_t WAIT_NS = 2000000000, LANDING_NS = 20000000, LOSE_NS = 1000000;
+constexpr int WAIT_TRIES = 1 << 28;
+// On one SM a wait is for one product, a microsecond: tries alone (20 ms at the very least) do, and cost less code.
+constexpr int SMALL_TRIES = 1 << 20;
 constexpr double PAIRS_START = 2e-6;        // seconds that a pair of blocks takes longer to start (four 333 x 1000: 14.4 us, 13.1 without pairs)
 constexpr int SEGMENT = 16;                 // slices of 64: 1024 of depth
 
@@ -375,6 +380,31 @@ __device__ __forceinline__ void load_sums(float (&v)[32], uint32_t addr, int apa
 
 __device__ unsigned int g_ortho_timeouts;
 
+__device__ __forceinline__ uint64_t now_ns() {
+    uint64_t t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
+}
+// Waits for the phase of `bar`, or gives up: `gave_up` then, and from then on.  `broken`: a word of shared memory, not 0
+// once a thread of the block has given up (none: nobody else waits for this one, and it is not counted).
+__device__ __forceinline__ void wait_for(uint32_t bar, uint32_t parity, bool& gave_up, volatile uint32_t* broken, unsigned int* lost, uint64_t limit = WAIT_NS) {
+    if (gave_up) return;
+    uint64_t start = 0;                   // the clock is slow to read: only once a wait has become a long one
+    for (int i = 0; i < WAIT_TRIES; ++i) {
+        if (mbar_try(bar, parity)) return;
+        if (i % 64 != 63) continue;
+        if (broken != nullptr && *broken != 0) break;
+        const uint64_t t = now_ns();
+        if (start == 0) start = t;
+        if (t - start > limit) break;
+    }
+    gave_up = true;
+    if (lost != nullptr) atomicExch(lost, 1u);
+    if (broken == nullptr) return;
+    *broken = 1;
+    atomicAdd(&g_ortho_timeouts, 1u);
+}
+
 // Tile number t of one matrix -> first row and column of the tile (CG * 128 rows, BN columns).
 template <bool LOWER, int CG, int BN>
 __device__ __forceinline__ void tile_at(int t, int across, int& i0, int& j0) {
@@ -396,21 +426,24 @@ __device__ __forceinline__ void tile_at(int t, int across, int& i0, int& j0) {
 // right: map of X in 64 x 64 boxes (APPLY).  added: planes of the term in the epilogue (S or X).
 template <bool PAIR, int CG, int BN, int KIND, bool LOWER, int KS>
 __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __grid_constant__ CUtensorMap left, const __grid_constant__ CUtensorMap right,
-                                                                      const __half* __restrict__ added, __half* __restrict__ out, ProductShape s) {
+                                                                      const __half* __restrict__ added, __half* __restrict__ out, unsigned int* lost, ProductShape s) {
     using R = Ring<PAIR, CG, BN>;
     static_assert(!LOWER || CG * BM % BN == 0, "columns of tiles end where rows do");
     static_assert(KS == 1 || (CG == 1 && BN == 64 && !LOWER), "the depth is split where tiles are few and narrow");
     extern __shared__ uint8_t raw[];
     uint8_t* ring = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
     uint64_t* bars = reinterpret_cast<uint64_t*>(ring + R::STAGES * R::STAGE);
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * R::STAGES + 4);
-    const uint32_t full = smem_u32(bars), empty = full + 8 * R::STAGES, done = empty + 8 * R::STAGES, freed = done + 16;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * R::STAGES + 5);
+    volatile uint32_t* broken = tmem_slot + 1;
+    const uint32_t full = smem_u32(bars), empty = full + 8 * R::STAGES, done = empty + 8 * R::STAGES, freed = done + 16, ended = freed + 16;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int rank = CG == 2 ? (int)(blockIdx.x & 1) : 0, workers = gridDim.x / (CG * KS), worker = blockIdx.x / (CG * KS);
     const int slice = KS > 1 ? (int)(blockIdx.x % KS) : 0;      // which part of the depth
     if (threadIdx.x == 0) {
         for (int i = 0; i < R::STAGES; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(done + 8 * i, 1); mbar_init(freed + 8 * i, CG * EPILOGUE_WARPS); }
+        mbar_init(ended, 1);
+        *broken = 0;
         mbar_fence_init();
         asm volatile("prefetch.tensormap [%0];" ::"l"(&left) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&right) : "memory");
@@ -438,14 +471,15 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
         if (lane == 0) {
             const uint32_t full_first = CG == 2 ? in_first_block(full) : full;
             int stage = 0, phase = 0;
-            for (int tile = worker; tile < s.tiles; tile += workers) {
+            for (int tile = worker; tile < s.tiles && !gave_up; tile += workers) {
                 const int k = tile / s.per_matrix;
                 int i0, j0;
                 tile_at<LOWER, CG, BN>(tile % s.per_matrix, s.across, i0, j0);
                 i0 += rank * BM;
                 j0 += rank * R::B_COLS;
                 for (int step = step0; step < step1; ++step) {
-                    mbar_wait<WAIT_TRIES>(empty + 8 * stage, phase ^ 1, gave_up, &g_ortho_timeouts);
+                    wait_for(empty + 8 * stage, phase ^ 1, gave_up, broken, lost);
+                    if (gave_up) break;
                     if (rank == 0) mbar_expect_tx(full + 8 * stage, CG * R::STAGE);
                     const uint32_t base = smem_u32(ring + stage * R::STAGE);
                     const uint32_t bar = full_first + 8 * stage;
@@ -464,10 +498,17 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
                 }
             }
             // the last copies have to land before the block may end: wait until they have been used
-            for (int i = 0; i < R::STAGES; ++i) {
-                mbar_wait<WAIT_TRIES>(empty + 8 * stage, phase ^ 1, gave_up, &g_ortho_timeouts);
+            const int issued = stage, pass = phase;
+            for (int i = 0; i < R::STAGES && !gave_up; ++i) {
+                wait_for(empty + 8 * stage, phase ^ 1, gave_up, broken, lost);
                 if (++stage == R::STAGES) { stage = 0; phase ^= 1; }
             }
+            if (gave_up)      // nobody uses them any more: until they have landed (the second block of a pair, whose bytes
+                              // count on the first one's barriers: until they must have)
+                for (int i = 0; i < R::STAGES; ++i) {
+                    bool late = false;
+                    wait_for(full + 8 * i, i < issued ? pass : pass ^ 1, late, nullptr, nullptr, LANDING_NS);
+                }
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
@@ -476,14 +517,16 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
             // one thread issues everything: what it computes per product has to stay short
             const uint64_t a0 = slice_desc(smem_u32(ring), false), b0 = slice_desc(smem_u32(ring) + R::PLANES * R::A_BYTES, KIND == APPLY);
             int stage = 0, phase = 0, acc = 0, acc_phase = 0;
-            for (int tile = worker; tile < s.tiles; tile += workers) {
-                for (int begin = step0; begin < step1;) {
+            for (int tile = worker; tile < s.tiles && !gave_up; tile += workers) {
+                for (int begin = step0; begin < step1 && !gave_up;) {
                     const int stop = PAIR && begin + SEGMENT < step1 ? begin + SEGMENT : step1;
-                    mbar_wait<WAIT_TRIES>(freed + 8 * acc, acc_phase ^ 1, gave_up, &g_ortho_timeouts);
+                    wait_for(freed + 8 * acc, acc_phase ^ 1, gave_up, broken, lost);
+                    if (gave_up) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint32_t d = tmem + acc * R::SET;
                     for (int step = begin; step < stop; ++step) {
-                        mbar_wait<WAIT_TRIES>(full + 8 * stage, phase, gave_up, &g_ortho_timeouts);
+                        wait_for(full + 8 * stage, phase, gave_up, broken, lost);
+                        if (gave_up) break;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                         const uint64_t a = desc_at(a0, stage * R::STAGE), b = desc_at(b0, stage * R::STAGE);
 #pragma unroll
@@ -499,11 +542,17 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
                         mma_commit<CG>(empty + 8 * stage);
                         if (++stage == R::STAGES) { stage = 0; phase ^= 1; }
                     }
+                    if (gave_up) break;
                     mma_commit<CG>(done + 8 * acc);
                     if (acc == 1) acc_phase ^= 1;
                     acc ^= 1;
                     begin = stop;
                 }
+            }
+            if (gave_up) {       // the products issued so far have to end before their accumulators are given back
+                bool late = false;
+                mma_commit<CG>(ended);
+                wait_for(ended, 0, late, nullptr, nullptr);
             }
         }
     } else if constexpr (KS == 1) {
@@ -511,7 +560,7 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
         const uint32_t freed_first = CG == 2 ? in_first_block(freed) : freed;
         int acc = 0, acc_phase = 0;
         const int64_t out_plane = (int64_t)s.mp * s.cols;
-        for (int tile = worker; tile < s.tiles; tile += workers) {
+        for (int tile = worker; tile < s.tiles && !gave_up; tile += workers) {
             const int k = tile / s.per_matrix;
             int i0, j0;
             tile_at<LOWER, CG, BN>(tile % s.per_matrix, s.across, i0, j0);
@@ -534,8 +583,8 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
             };
             fetch(half * 32);
             auto wait_done = [&]() {
-                mbar_wait<WAIT_TRIES>(done + 8 * acc, acc_phase, gave_up, &g_ortho_timeouts);
-                __syncwarp();                              // the reads of TMEM are the whole warp's
+                wait_for(done + 8 * acc, acc_phase, gave_up, broken, lost);
+                gave_up = __any_sync(~0u, gave_up);        // the reads of TMEM are the whole warp's
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             };
             auto release = [&]() {
@@ -556,6 +605,7 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
                     for (int i = 0; i < 32; ++i) run[g][i] = 0.f;
                 for (int begin = step0 + SEGMENT; begin < step1; begin += SEGMENT) {
                     wait_done();
+                    if (gave_up) break;
 #pragma unroll
                     for (int g = 0; g < BN / 64; ++g) {
                         float v[32];
@@ -567,6 +617,7 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
                 }
             }
             wait_done();
+            if (gave_up) break;
 #pragma unroll(PAIR ? BN / 64 : 1)
             for (int part = 0; part < BN / 64; ++part) {
                 const int c = half * 32 + 64 * part, col = j0 + c;
@@ -612,8 +663,9 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) product_kernel(const __gri
             float run[32] = {};
             int acc = 0, acc_phase = 0;
             for (int begin = step0; begin < step1; begin = PAIR ? begin + SEGMENT : step1) {
-                mbar_wait<WAIT_TRIES>(done + 8 * acc, acc_phase, gave_up, &g_ortho_timeouts);
-                __syncwarp();
+                wait_for(done + 8 * acc, acc_phase, gave_up, broken, lost);
+                gave_up = __any_sync(~0u, gave_up);
+                if (gave_up) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 float v[32];
                 load_sums<R::MAINS + R::PLANES - 1>(v, tmem + acc * R::SET + half * 32 + ((uint32_t)(quarter * 32) << 16), BN);
@@ -702,8 +754,8 @@ struct Maps {
 };
 
 template <bool PAIR, int CG, int BN, int KIND, bool LOWER, int KS = 1>
-cudaError_t launch_product(const Maps& left, const Maps& right, const __half* added, __half* out, ProductShape s, int64_t count, int sms,
-                           cudaStream_t st) {
+cudaError_t launch_product(const Maps& left, const Maps& right, const __half* added, __half* out, unsigned int* lost, ProductShape s,
+                           int64_t count, int sms, cudaStream_t st) {
     using R = Ring<PAIR, CG, BN>;
     const int64_t down = ceil_div(s.mp, CG * BM);
     s.across = (int)ceil_div(s.cols, BN);
@@ -738,7 +790,7 @@ cudaError_t launch_product(const Maps& left, const Maps& right, const __half* ad
     cfg.attrs = attr;
     cfg.numAttrs = n;
     const bool boxes64 = KIND == APPLY || R::B_COLS == 64;
-    return cudaLaunchKernelEx(&cfg, kernel, left.tall, boxes64 ? right.low : right.tall, added, out, s);
+    return cudaLaunchKernelEx(&cfg, kernel, left.tall, boxes64 ? right.low : right.tall, added, out, lost, s);
 }
 
 // Seconds that a form of a product takes, for comparing the forms.  A block brings `STAGE` bytes per 64 of
@@ -760,7 +812,8 @@ double product_seconds(const ProductShape& s, int64_t count, int sms) {
 // Pairs of SMs, or single blocks with tiles of 128 or 64 columns, the latter with the depth split over 2 or 4
 // blocks where there are few: whichever is reckoned fastest.
 template <bool PAIR, int KIND>
-cudaError_t run_product(const Maps& left, const Maps& right, const __half* added, __half* out, ProductShape s, int64_t count, int sms, cudaStream_t st) {
+cudaError_t run_product(const Maps& left, const Maps& right, const __half* added, __half* out, unsigned int* lost, ProductShape s, int64_t count,
+                        int sms, cudaStream_t st) {
     constexpr int WIDE = PAIR ? 128 : 256;      // PAIR: two accumulators a set
     constexpr bool LOWER = KIND != APPLY;
     const double t[5] = {product_seconds<PAIR, 2, WIDE, KIND, LOWER>(s, count, sms), product_seconds<PAIR, 1, 128, KIND, LOWER>(s, count, sms),
@@ -770,11 +823,11 @@ cudaError_t run_product(const Maps& left, const Maps& right, const __half* added
     for (int i = 1; i < 5; ++i)
         if (t[i] < t[best]) best = i;
     switch (best) {
-    case 0: return launch_product<PAIR, 2, WIDE, KIND, LOWER>(left, right, added, out, s, count, sms, st);
-    case 1: return launch_product<PAIR, 1, 128, KIND, LOWER>(left, right, added, out, s, count, sms, st);
-    case 2: return launch_product<PAIR, 1, 64, KIND, false>(left, right, added, out, s, count, sms, st);
-    case 3: return launch_product<PAIR, 1, 64, KIND, false, 2>(left, right, added, out, s, count, sms, st);
-    default: return launch_product<PAIR, 1, 64, KIND, false, 4>(left, right, added, out, s, count, sms, st);
+    case 0: return launch_product<PAIR, 2, WIDE, KIND, LOWER>(left, right, added, out, lost, s, count, sms, st);
+    case 1: return launch_product<PAIR, 1, 128, KIND, LOWER>(left, right, added, out, lost, s, count, sms, st);
+    case 2: return launch_product<PAIR, 1, 64, KIND, false>(left, right, added, out, lost, s, count, sms, st);
+    case 3: return launch_product<PAIR, 1, 64, KIND, false, 2>(left, right, added, out, lost, s, count, sms, st);
+    default: return launch_product<PAIR, 1, 64, KIND, false, 4>(left, right, added, out, lost, s, count, sms, st);
     }
 }
 
@@ -807,10 +860,10 @@ __device__ __forceinline__ float value_at(uint8_t* hi_plane, uint8_t* lo_plane, 
 }
 
 template <typename T>
-__global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo io, int steps) {
+__global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo io, int steps, bool lose) {
     constexpr bool PAIR = sizeof(T) == 4;
     extern __shared__ uint8_t raw[];
-    __shared__ __align__(8) uint64_t bar;
+    __shared__ __align__(8) uint64_t bar, ended;
     __shared__ uint32_t tmem_slot;
     __shared__ float part[SMALL_THREADS / 32];
     uint8_t* base = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
@@ -819,6 +872,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     if (tid == 0) {
         mbar_init(smem_u32(&bar), 1);
+        mbar_init(smem_u32(&ended), 1);
         mbar_fence_init();
     }
     if (warp == 0) {
@@ -925,7 +979,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
     const uint64_t dxh = slice_desc(axh, false), dxl = slice_desc(axl, false), dsh = slice_desc(ash, false), dsl = slice_desc(asl, false);
     const uint64_t rxh = slice_desc(axh, true, SMALL_BLOCK), rxl = slice_desc(axl, true, SMALL_BLOCK);
     auto finish = [&]() {               // the products are done, and every thread may read their sums
-        mbar_wait<WAIT_TRIES>(smem_u32(&bar), phase, gave_up, &g_ortho_timeouts);
+        mbar_wait<SMALL_TRIES>(smem_u32(&bar), phase, gave_up, &g_ortho_timeouts);
         phase ^= 1;
         __syncwarp();                   // the reads of TMEM are the whole warp's
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -1022,13 +1076,22 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
         }
         written();
     }
+    if (lose) wait_for(smem_u32(&bar), phase, gave_up, nullptr, nullptr, LOSE_NS);      // nothing arrives any more
+    const bool lost = __syncthreads_or(gave_up);
+    if (lost) {                         // what has been issued has to end before the accumulators are given back
+        bool late = false;
+        if (tid == 0) mma_commit(smem_u32(&ended));
+        wait_for(smem_u32(&ended), 0, late, nullptr, nullptr);
+        __syncthreads();
+    }
+    const float unit = lost ? NAN : 1.f / SCALE;     // as in ortho_finish_kernel
     // out, along the matrix's rows
     T* out = (T*)io.out + k * io.rows * io.cols;
 #pragma unroll 2
     for (int r = warp; r < io.rows; r += SMALL_THREADS / 32)
 #pragma unroll 4
         for (int c = lane; c < io.cols; c += 32) {
-            const float v = (io.turned ? value_at(xh, xl, c, r) : value_at(xh, xl, r, c)) * (1.f / SCALE);
+            const float v = (io.turned ? value_at(xh, xl, c, r) : value_at(xh, xl, r, c)) * unit;
             T* o = out + r * io.cols + c;
             *o = from_f32<T>(mom == nullptr ? v : fmaf(-io.rate, v, io.keep * to_f32<T>(*o)));
         }
@@ -1039,9 +1102,10 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
 // read in 16-byte packs along X's rows, written along the matrix's rows, through shared memory where those
 // are not the same.
 template <typename T>
-__global__ void __launch_bounds__(256) ortho_finish_kernel(OrthoIo io, const __half* __restrict__ x) {
+__global__ void __launch_bounds__(256) ortho_finish_kernel(OrthoIo io, const __half* __restrict__ x, const unsigned int* __restrict__ lost) {
     pdl_wait_then_trigger();
     __shared__ float tile[64][65];
+    const float unit = *lost != 0 ? NAN : 1.f / SCALE;      // products that were not waited for: nobody may take X for a result
     const int across = io.np / 64, down = io.mp / 64;
     const int k = blockIdx.x / (across * down), t = blockIdx.x % (across * down), i0 = t / across * 64, j0 = t % across * 64;
     const int64_t plane = (int64_t)io.mp * io.np;
@@ -1059,7 +1123,7 @@ __global__ void __launch_bounds__(256) ortho_finish_kernel(OrthoIo io, const __h
         const Pack<__half, 8>* p = reinterpret_cast<const Pack<__half, 8>*>(x + 2 * k * plane + (int64_t)(i0 + i) * io.np + j0 + j);
         const Pack<__half, 8> hi = p[0], lo = p[plane / 8];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) tile[i][j + q] = (__half2float(hi.v[q]) + __half2float(lo.v[q])) * (1.f / SCALE);
+        for (int q = 0; q < 8; ++q) tile[i][j + q] = (__half2float(hi.v[q]) + __half2float(lo.v[q])) * unit;
     }
     __syncthreads();
     if (io.wide) {
@@ -1088,8 +1152,18 @@ __global__ void __launch_bounds__(256) ortho_finish_kernel(OrthoIo io, const __h
     }
 }
 
+// For tests: a wait that nothing ends.
+__global__ void ortho_lose_kernel(unsigned int* lost) {
+    pdl_wait_then_trigger();
+    __shared__ __align__(8) uint64_t bar;
+    bool gave_up = false;
+    mbar_init(smem_u32(&bar), 1);
+    mbar_fence_init();
+    wait_for(smem_u32(&bar), 0, gave_up, nullptr, lost, LOSE_NS);
+}
+
 struct OrthoSpace {
-    size_t sums, x[2], s, p, total;
+    size_t sums, lost, x[2], s, p, total;
 };
 int64_t padded(int64_t n) { return ceil_div(n, 64) * 64; }
 bool is_small(int64_t m, int64_t n) { return m <= SMALL_M && n <= SMALL_N; }
@@ -1100,6 +1174,7 @@ OrthoSpace space(int64_t count, int64_t m, int64_t n) {
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
     w.sums = take(count * MOST_SUMS * 8);
+    w.lost = take(4);
     w.x[0] = take(count * mp * np * 4);
     w.x[1] = take(count * mp * np * 4);
     w.s = take(count * mp * mp * 4);
@@ -1125,7 +1200,7 @@ int check(const fpde_ortho_args* a) {
     } while (0)
 
 template <typename T>
-cudaError_t run(const fpde_ortho_args* a, bool muon, cudaStream_t st) {
+cudaError_t run(const fpde_ortho_args* a, bool muon, bool lose, cudaStream_t st) {
     OrthoIo io = {};
     io.grad = a->grad; io.grad_matrix = a->grad_matrix; io.grad_row = a->grad_row;
     io.out = muon ? a->weight : a->out;
@@ -1143,13 +1218,14 @@ cudaError_t run(const fpde_ortho_args* a, bool muon, cudaStream_t st) {
     if (is_small(io.m, io.n)) {
         static std::atomic<uint64_t> allowed{0};
         FPDE_TRY(allow_smem(ortho_small_kernel<T>, small_bytes(SMALL_N), allowed));
-        return launch_kernel_smem(ortho_small_kernel<T>, dim3((unsigned)a->count), dim3(SMALL_THREADS), small_bytes(io.np), st, io, a->steps);
+        return launch_kernel_smem(ortho_small_kernel<T>, dim3((unsigned)a->count), dim3(SMALL_THREADS), small_bytes(io.np), st, io, a->steps, lose);
     }
     const OrthoSpace w = space(a->count, io.m, io.n);
     char* ws = (char*)a->workspace;
     double* sums = (double*)(ws + w.sums);
     __half* x[2] = {(__half*)(ws + w.x[0]), (__half*)(ws + w.x[1])};
     __half *s = (__half*)(ws + w.s), *p = (__half*)(ws + w.p);
+    unsigned int* lost = (unsigned int*)(ws + w.lost);
     // enough blocks for two per SM over the stack, at least 8 rows (one per warp) each
     const int sms = sm_count_or_default();
     int64_t blocks = ceil_div(io.rows, 8);
@@ -1161,25 +1237,26 @@ cudaError_t run(const fpde_ortho_args* a, bool muon, cudaStream_t st) {
     if (a->steps > 0 && !(sm.encode(s, a->count, io.mp, io.mp) && pm.encode(p, a->count, io.mp, io.mp) && xm[0].encode(x[0], a->count, io.mp, io.np) &&
                           xm[1].encode(x[1], a->count, io.mp, io.np)))
         return cudaErrorNotSupported;
-    FPDE_TRY(launch_kernel(ortho_square_kernel<T>, dim3((unsigned)(a->count * blocks)), dim3(256), st, io, sums, (int)blocks));
+    FPDE_TRY(launch_kernel(ortho_square_kernel<T>, dim3((unsigned)(a->count * blocks)), dim3(256), st, io, sums, (int)blocks, lost));
     FPDE_TRY(launch_kernel(ortho_start_kernel<T>, dim3((unsigned)pieces), dim3(256), st, io, (const double*)sums, (int)blocks, x[0]));
+    if (lose) FPDE_TRY(launch_kernel(ortho_lose_kernel, dim3(1), dim3(1), st, lost));
     int at = 0;
     for (int i = 0; i < a->steps; ++i, at ^= 1) {
         constexpr bool PAIR = sizeof(T) == 4;
         ProductShape gram{io.mp, io.np, 0, 0, 0, 0, io.mp, 1.f / SCALE, 0.f};
         ProductShape square{io.mp, io.np, 0, 0, 0, 0, io.mp, NS_C / SCALE, NS_B};
         ProductShape apply{io.mp, io.np, 0, 0, 0, 0, io.np, 1.f / SCALE, NS_A};
-        FPDE_TRY((run_product<PAIR, GRAM>(xm[at], xm[at], s, s, gram, a->count, sms, st)));
+        FPDE_TRY((run_product<PAIR, GRAM>(xm[at], xm[at], s, s, lost, gram, a->count, sms, st)));
         // while S is small its square is bound by latency: pairs cost nothing, and its factors' rounding is the
         // largest part of the 16-bit types' error on matrices much wider than tall (40 x 900: 2.2e-3 of it)
-        if (PAIR || io.mp <= 512) FPDE_TRY((run_product<true, SQUARE>(sm, sm, s, p, square, a->count, sms, st)));
-        else FPDE_TRY((run_product<false, SQUARE>(sm, sm, s, p, square, a->count, sms, st)));
-        FPDE_TRY((run_product<PAIR, APPLY>(pm, xm[at], x[at], x[at ^ 1], apply, a->count, sms, st)));
+        if (PAIR || io.mp <= 512) FPDE_TRY((run_product<true, SQUARE>(sm, sm, s, p, lost, square, a->count, sms, st)));
+        else FPDE_TRY((run_product<false, SQUARE>(sm, sm, s, p, lost, square, a->count, sms, st)));
+        FPDE_TRY((run_product<PAIR, APPLY>(pm, xm[at], x[at], x[at ^ 1], lost, apply, a->count, sms, st)));
     }
-    return launch_kernel(ortho_finish_kernel<T>, dim3((unsigned)pieces), dim3(256), st, io, (const __half*)x[at]);
+    return launch_kernel(ortho_finish_kernel<T>, dim3((unsigned)pieces), dim3(256), st, io, (const __half*)x[at], (const unsigned int*)lost);
 }
 
-int call(const fpde_ortho_args* a, bool muon, void* stream) {
+int call(const fpde_ortho_args* a, bool muon, void* stream, bool lose = false) {
     const int st = check(a);
     if (st != FPDE_OK) return st;
     if (a->count * a->rows * a->cols == 0) return FPDE_OK;
@@ -1190,7 +1267,7 @@ int call(const fpde_ortho_args* a, bool muon, void* stream) {
     if (need > 0 && (a->workspace == nullptr || !aligned(a->workspace, 256) || a->workspace_bytes < need))
         return FPDE_ERR_WORKSPACE;
     const cudaStream_t s = (cudaStream_t)stream;
-    const cudaError_t err = a->dtype == FPDE_F32 ? run<float>(a, muon, s) : a->dtype == FPDE_BF16 ? run<__nv_bfloat16>(a, muon, s) : run<__half>(a, muon, s);
+    const cudaError_t err = a->dtype == FPDE_F32 ? run<float>(a, muon, lose, s) : a->dtype == FPDE_BF16 ? run<__nv_bfloat16>(a, muon, lose, s) : run<__half>(a, muon, lose, s);
     return err == cudaSuccess ? FPDE_OK : FPDE_ERR_CUDA;
 }
 
@@ -1209,6 +1286,7 @@ size_t fpde_orthogonalize_workspace_bytes(const fpde_ortho_args* a) {
 
 int fpde_orthogonalize(const fpde_ortho_args* a, void* stream) { return call(a, false, stream); }
 int fpde_muon_step(const fpde_ortho_args* a, void* stream) { return call(a, true, stream); }
+int fpde_diag_orthogonalize_lost(const fpde_ortho_args* a, void* stream) { return call(a, false, stream, true); }
 unsigned int fpde_diag_ortho_timeouts(void) {
     unsigned int n = 0;
     if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpyFromSymbol(&n, g_ortho_timeouts, sizeof n) != cudaSuccess) {

@@ -32,21 +32,24 @@ __device__ __forceinline__ void mbar_fence_init() {
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
+// One try, which the hardware may hold for some time: has the phase with the given parity completed?
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done != 0;
+}
 // Bounded wait for the phase with the given parity to complete.  A thread that has given up once
 // (`gave_up`) does not wait again, so a broken pipeline costs one bounded wait per thread, not one
 // per step.  `timeouts` is the translation unit's counter.
 template <int LIMIT = (1 << 16)>
 __device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, bool& gave_up, unsigned int* timeouts) {
     if (gave_up) return;
-    for (int it = 0; it < LIMIT; ++it) {
-        uint32_t done;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-        if (done) return;
-    }
+    for (int it = 0; it < LIMIT; ++it)
+        if (mbar_try(bar, parity)) return;
     gave_up = true;
     atomicAdd(timeouts, 1u);
 }
