@@ -602,6 +602,21 @@ unsigned int fpde_diag_ortho_timeouts(void);
  * when it loses one. */
 int fpde_diag_orthogonalize_lost(const fpde_ortho_args* args, void* stream);
 
+/*
+ * Which form of its kernels a call takes, from its sizes (for tests that have to reach each of them; 0, or -1 for the
+ * last, if the sizes are refused):
+ *   scan: channels of a thread in the march (1 or 2), and the pieces that a row is cut into;
+ *   convolution: nodes of a thread's piece of a row; rows of a thread in the single-node form, which depends on
+ *   the pointers' alignment too;
+ *   orthogonalisation: product 0 is X X^T, 1 b S + c S S, 2 a X + P X, on 0 pairs of SMs, single ones with 1 128 or 2 64
+ *   columns a tile, 3 or 4 those with the depth over 2 or 4 blocks; -1 also for matrices that stay on one SM.
+ */
+int fpde_diag_scan_channels(const fpde_scan_args* args, int backward);
+int fpde_diag_scan_chunks(const fpde_scan_args* args, int backward);
+int fpde_diag_conv_nodes(const fpde_conv_args* args, int backward);
+int fpde_diag_conv_step_rows(const fpde_conv_args* args);
+int fpde_diag_ortho_form(const fpde_ortho_args* args, int product);
+
 #ifdef __cplusplus
 }
 #endif

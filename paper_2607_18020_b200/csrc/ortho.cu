@@ -812,22 +812,32 @@ double product_seconds(const ProductShape& s, int64_t count, int sms) {
 // Pairs of SMs, or single blocks with tiles of 128 or 64 columns, the latter with the depth split over 2 or 4
 // blocks where there are few: whichever is reckoned fastest.
 template <bool PAIR, int KIND>
-cudaError_t run_product(const Maps& left, const Maps& right, const __half* added, __half* out, unsigned int* lost, ProductShape s, int64_t count,
-                        int sms, cudaStream_t st) {
+int best_form(const ProductShape& s, int64_t count, int sms) {
     constexpr int WIDE = PAIR ? 128 : 256;      // PAIR: two accumulators a set
     constexpr bool LOWER = KIND != APPLY;
     const double t[5] = {product_seconds<PAIR, 2, WIDE, KIND, LOWER>(s, count, sms), product_seconds<PAIR, 1, 128, KIND, LOWER>(s, count, sms),
                          product_seconds<PAIR, 1, 64, KIND, false>(s, count, sms), product_seconds<PAIR, 1, 64, KIND, false, 2>(s, count, sms),
-                         product_seconds<PAIR, 1, 64, KIND, false, 4>(s, count, sms)};
+                         // S S of single factors is formed from 576 rows on: 45 tiles or more, too many for clusters of 4
+                         KIND == SQUARE && !PAIR ? 1e9 : product_seconds<PAIR, 1, 64, KIND, false, 4>(s, count, sms)};
     int best = 0;
     for (int i = 1; i < 5; ++i)
         if (t[i] < t[best]) best = i;
-    switch (best) {
+    return best;
+}
+
+template <bool PAIR, int KIND>
+cudaError_t run_product(const Maps& left, const Maps& right, const __half* added, __half* out, unsigned int* lost, ProductShape s, int64_t count,
+                        int sms, cudaStream_t st) {
+    constexpr int WIDE = PAIR ? 128 : 256;
+    constexpr bool LOWER = KIND != APPLY;
+    switch (best_form<PAIR, KIND>(s, count, sms)) {
     case 0: return launch_product<PAIR, 2, WIDE, KIND, LOWER>(left, right, added, out, lost, s, count, sms, st);
     case 1: return launch_product<PAIR, 1, 128, KIND, LOWER>(left, right, added, out, lost, s, count, sms, st);
     case 2: return launch_product<PAIR, 1, 64, KIND, false>(left, right, added, out, lost, s, count, sms, st);
     case 3: return launch_product<PAIR, 1, 64, KIND, false, 2>(left, right, added, out, lost, s, count, sms, st);
-    default: return launch_product<PAIR, 1, 64, KIND, false, 4>(left, right, added, out, lost, s, count, sms, st);
+    default:
+        if constexpr (KIND == SQUARE && !PAIR) return cudaErrorNotSupported;
+        else return launch_product<PAIR, 1, 64, KIND, false, 4>(left, right, added, out, lost, s, count, sms, st);
     }
 }
 
@@ -1199,6 +1209,15 @@ int check(const fpde_ortho_args* a) {
         if (e_ != cudaSuccess) return e_;     \
     } while (0)
 
+ProductShape shape_of(int kind, int mp, int np) {
+    if (kind == GRAM) return {mp, np, 0, 0, 0, 0, mp, 1.f / SCALE, 0.f};
+    if (kind == SQUARE) return {mp, np, 0, 0, 0, 0, mp, NS_C / SCALE, NS_B};
+    return {mp, np, 0, 0, 0, 0, np, 1.f / SCALE, NS_A};
+}
+// While S is small its square is bound by latency: pairs cost nothing, and its factors' rounding is the largest part of
+// the 16-bit types' error on matrices much wider than tall (40 x 900: 2.2e-3 of it).
+bool square_of_pairs(int mp) { return mp <= 512; }
+
 template <typename T>
 cudaError_t run(const fpde_ortho_args* a, bool muon, bool lose, cudaStream_t st) {
     OrthoIo io = {};
@@ -1243,13 +1262,9 @@ cudaError_t run(const fpde_ortho_args* a, bool muon, bool lose, cudaStream_t st)
     int at = 0;
     for (int i = 0; i < a->steps; ++i, at ^= 1) {
         constexpr bool PAIR = sizeof(T) == 4;
-        ProductShape gram{io.mp, io.np, 0, 0, 0, 0, io.mp, 1.f / SCALE, 0.f};
-        ProductShape square{io.mp, io.np, 0, 0, 0, 0, io.mp, NS_C / SCALE, NS_B};
-        ProductShape apply{io.mp, io.np, 0, 0, 0, 0, io.np, 1.f / SCALE, NS_A};
+        const ProductShape gram = shape_of(GRAM, io.mp, io.np), square = shape_of(SQUARE, io.mp, io.np), apply = shape_of(APPLY, io.mp, io.np);
         FPDE_TRY((run_product<PAIR, GRAM>(xm[at], xm[at], s, s, lost, gram, a->count, sms, st)));
-        // while S is small its square is bound by latency: pairs cost nothing, and its factors' rounding is the
-        // largest part of the 16-bit types' error on matrices much wider than tall (40 x 900: 2.2e-3 of it)
-        if (PAIR || io.mp <= 512) FPDE_TRY((run_product<true, SQUARE>(sm, sm, s, p, lost, square, a->count, sms, st)));
+        if (PAIR || square_of_pairs(io.mp)) FPDE_TRY((run_product<true, SQUARE>(sm, sm, s, p, lost, square, a->count, sms, st)));
         else FPDE_TRY((run_product<false, SQUARE>(sm, sm, s, p, lost, square, a->count, sms, st)));
         FPDE_TRY((run_product<PAIR, APPLY>(pm, xm[at], x[at], x[at ^ 1], lost, apply, a->count, sms, st)));
     }
@@ -1282,6 +1297,18 @@ size_t fpde_orthogonalize_workspace_bytes(const fpde_ortho_args* a) {
     if (check(a) != FPDE_OK) return 0;
     const int64_t m = a->rows < a->cols ? a->rows : a->cols, n = a->rows < a->cols ? a->cols : a->rows;
     return space(a->count, m, n).total;
+}
+
+int fpde_diag_ortho_form(const fpde_ortho_args* a, int product) {
+    if (check(a) != FPDE_OK || product < GRAM || product > APPLY) return -1;
+    const int64_t m = a->rows < a->cols ? a->rows : a->cols, n = a->rows < a->cols ? a->cols : a->rows;
+    if (m == 0 || a->count == 0 || is_small(m, n)) return -1;
+    const int mp = (int)padded(m), np = (int)padded(n), sms = sm_count_or_default();
+    const ProductShape s = shape_of(product, mp, np);
+    const bool pair = a->dtype == FPDE_F32 || (product == SQUARE && square_of_pairs(mp));
+    if (product == GRAM) return pair ? best_form<true, GRAM>(s, a->count, sms) : best_form<false, GRAM>(s, a->count, sms);
+    if (product == SQUARE) return pair ? best_form<true, SQUARE>(s, a->count, sms) : best_form<false, SQUARE>(s, a->count, sms);
+    return pair ? best_form<true, APPLY>(s, a->count, sms) : best_form<false, APPLY>(s, a->count, sms);
 }
 
 int fpde_orthogonalize(const fpde_ortho_args* a, void* stream) { return call(a, false, stream); }

@@ -480,21 +480,27 @@ cudaError_t conv_by_type(const fpde_conv_args* a, bool backward, cudaStream_t st
     return conv_by_width<__half>(a, backward, st);
 }
 
+// One row a thread while the GPU is not full: latency.
+int step_rows(const fpde_conv_args* a, int64_t across) { return a->batch * across >= 148 * 16 ? 4 : 1; }
+
 template <typename T, int W, int VEC>
 cudaError_t conv_step_run(const fpde_conv_args* a, cudaStream_t st) {
     const int64_t across = ceil_div(a->channels, 128 * VEC);
-    const int rows = a->batch * across >= 148 * 16 ? 4 : 1;      // one row a thread while the GPU is not full: latency
+    const int rows = step_rows(a, across);
     const int64_t blocks = ceil_div(a->batch, rows) * across;
     if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
     return launch_kernel(conv_step_kernel<T, W, VEC>, dim3((unsigned)blocks), dim3(128), st, (const T*)a->x, a->x_batch, a->weight, a->bias,
                          (const T*)a->state, (T*)a->y, (T*)a->state_out, a->batch, (int)across, rows, (int)a->channels, a->silu);
 }
 
+bool step_pairs(const fpde_conv_args* a) {
+    const size_t e = dtype_bytes(a->dtype);
+    return a->channels % 2 == 0 && packs(a->x, a->x_batch, 0, e, 2) && aligned(a->y, 2 * e) && aligned(a->state, 2 * e) && aligned(a->state_out, 2 * e);
+}
+
 template <typename T, int W>
 cudaError_t conv_step_launch(const fpde_conv_args* a, cudaStream_t st) {
-    const bool pairs = a->channels % 2 == 0 && packs(a->x, a->x_batch, 0, sizeof(T), 2) && aligned(a->y, 2 * sizeof(T)) &&
-                       aligned(a->state, 2 * sizeof(T)) && aligned(a->state_out, 2 * sizeof(T));
-    return pairs ? conv_step_run<T, W, 2>(a, st) : conv_step_run<T, W, 1>(a, st);
+    return step_pairs(a) ? conv_step_run<T, W, 2>(a, st) : conv_step_run<T, W, 1>(a, st);
 }
 
 template <typename T>
@@ -520,6 +526,14 @@ size_t fpde_causal_conv_workspace_bytes(const fpde_conv_args* a) {
     if (check_conv_sizes(a) != FPDE_OK) return 0;
     const int64_t parts = a->batch * conv_spans(a, a->length + a->width - 1);
     return (size_t)(parts * a->channels * (a->width + 1)) * sizeof(float);
+}
+
+int fpde_diag_conv_nodes(const fpde_conv_args* a, int backward) {
+    return check_conv_sizes(a) != FPDE_OK ? 0 : conv_nodes(a, a->length + (backward ? a->width - 1 : 0));
+}
+
+int fpde_diag_conv_step_rows(const fpde_conv_args* a) {
+    return check_conv_sizes(a, true) != FPDE_OK ? 0 : step_rows(a, ceil_div(a->channels, step_pairs(a) ? 256 : 128));
 }
 
 int fpde_causal_conv_fwd(const fpde_conv_args* a, void* stream) {

@@ -1142,6 +1142,10 @@ cudaError_t run_step(const fpde_scan_args* a, cudaStream_t st) {
 // 384 blocks 961 / 855).  The pass that only forms the chunks' ends always does (169 / 189, 216 / 213).
 constexpr int64_t FWD_ONE = 148 * 4, BACK_ONE = 148 * 2;
 
+int channels_a_thread(const fpde_scan_args* a, const ScanShape& s, bool backward) {
+    return a->batch * s.tiles * s.chunks <= (backward ? BACK_ONE : FWD_ONE) ? 1 : 2;
+}
+
 enum Call { CALL_FWD, CALL_BWD, CALL_STEP };
 
 template <typename T, int S>
@@ -1149,13 +1153,13 @@ cudaError_t run(const fpde_scan_args* a, Call call, cudaStream_t st) {
     if (call == CALL_FWD) {
         const ScanShape s = plan(a, false);
         const bool pairs = scan_pairs<T>(a, false);
-        if (a->batch * s.tiles * s.chunks <= FWD_ONE) return pairs ? run_fwd<T, S, 1, 2>(a, s, st) : run_fwd<T, S, 1, 1>(a, s, st);
+        if (channels_a_thread(a, s, false) == 1) return pairs ? run_fwd<T, S, 1, 2>(a, s, st) : run_fwd<T, S, 1, 1>(a, s, st);
         return pairs ? run_fwd<T, S, 2, 2>(a, s, st) : run_fwd<T, S, 2, 1>(a, s, st);
     }
     if (call == CALL_BWD) {
         const ScanShape s = plan(a, true);
         const bool pairs = scan_pairs<T>(a, true);
-        if (a->batch * s.tiles * s.chunks <= BACK_ONE) return pairs ? run_bwd<T, S, 1, 2>(a, s, st) : run_bwd<T, S, 1, 1>(a, s, st);
+        if (channels_a_thread(a, s, true) == 1) return pairs ? run_bwd<T, S, 1, 2>(a, s, st) : run_bwd<T, S, 1, 1>(a, s, st);
         return pairs ? run_bwd<T, S, 2, 2>(a, s, st) : run_bwd<T, S, 2, 1>(a, s, st);
     }
     return run_step<T, S>(a, st);
@@ -1200,6 +1204,12 @@ size_t fpde_selective_scan_workspace_bytes(const fpde_scan_args* a, int backward
     if (check_scan_sizes(a) != FPDE_OK) return 0;
     return space(a, plan(a, backward != 0), backward != 0).total;
 }
+
+int fpde_diag_scan_channels(const fpde_scan_args* a, int backward) {
+    return check_scan_sizes(a) != FPDE_OK ? 0 : channels_a_thread(a, plan(a, backward != 0), backward != 0);
+}
+
+int fpde_diag_scan_chunks(const fpde_scan_args* a, int backward) { return check_scan_sizes(a) != FPDE_OK ? 0 : plan(a, backward != 0).chunks; }
 
 int fpde_selective_scan_fwd(const fpde_scan_args* a, void* stream) {
     int st = check_scan(a, false);

@@ -3,6 +3,7 @@ must not turn an infinite result into NaN, and must not reach anything else."""
 import pytest
 
 torch = pytest.importorskip("torch")
+from forms_util import SCAN_TWO
 from seq_util import check, d64, scan_ref
 
 pytestmark = pytest.mark.gpu
@@ -60,6 +61,26 @@ def test_infinite_input(n, channels, dtype):
     nodes[:] = False
     nodes[1, 20] = True
     split(g2.B, g.B, nodes)
+    assert torch.equal(g2.u, g.u)
+
+
+@pytest.mark.parametrize("size", SCAN_TWO)
+def test_infinite_input_where_threads_have_two_channels(size):
+    batch, length, channels, n = size
+    t = inputs(batch, length, channels, n, torch.float32)
+    out, last, g = run(t)
+    t[0][batch - 1, 10, channels - 1] = INF
+    out2, last2, g2 = run(t)
+    hit = torch.zeros_like(out, dtype=torch.bool)
+    hit[-1, 10:, -1] = True
+    split(out2, out, hit)
+    split(g2.z, g.z, hit)
+    rows = torch.zeros_like(last, dtype=torch.bool)
+    rows[-1, -1] = True
+    split(last2, last, rows)
+    nodes = torch.zeros_like(g.C, dtype=torch.bool)
+    nodes[-1, 10:] = True
+    split(g2.C, g.C, nodes)
     assert torch.equal(g2.u, g.u)
 
 
