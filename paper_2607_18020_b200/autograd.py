@@ -121,3 +121,21 @@ def fused_residual(op, fields: Sequence[torch.Tensor], sources: Sequence[torch.T
 def fused_residual_loss(op, fields: Sequence[torch.Tensor], sources: Sequence[torch.Tensor], spacing, coeffs, bc):
     """Sum over residual fields of the mean-square residual (fp64, 0-dim), differentiable w.r.t. the fields."""
     return _FusedResidualLoss.apply(op, tuple(sources), tuple(spacing), tuple(coeffs), tuple(bc), *fields)
+
+
+class ValuesOnly(torch.autograd.Function):
+    """The result of a call that has no gradient: asking for one is an error, not a zero."""
+
+    @staticmethod
+    def forward(ctx, call, *args):
+        ctx.name = call.__name__
+        return call(*args)                  # grad mode is off in here: the call does its work
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("%s is not differentiable" % ctx.name)
+
+
+def wants_grad(*inputs):
+    """Would torch record a graph for a result of these tensors (None among them)?"""
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in inputs)

@@ -13,15 +13,14 @@ import ctypes
 import torch
 
 from . import binding as B_
-
-_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+from .autograd import ValuesOnly, wants_grad
 
 
 def _matrices(name, t):
     """`t` as (count, rows, cols)."""
     if t.device.type != "cuda":
         raise ValueError("%s is on %s, expected a CUDA tensor" % (name, t.device))
-    if t.dtype not in _TYPES:
+    if str(t.dtype) not in B_.DTYPE_IDS:
         raise ValueError("%s is %s, expected fp32, bf16 or fp16" % (name, t.dtype))
     if t.dim() not in (2, 3):
         raise ValueError("%s has %d axes, expected a matrix or a stack of matrices" % (name, t.dim()))
@@ -37,7 +36,7 @@ def _args(grad, steps, eps):
     g = _matrices("grad", grad)
     if g.stride(2) != 1 and g.shape[2] > 1:
         g = g.contiguous()
-    a = B_.OrthoArgs(dtype=_TYPES[g.dtype], steps=steps, count=g.shape[0], rows=g.shape[1], cols=g.shape[2], grad_matrix=g.stride(0),
+    a = B_.OrthoArgs(dtype=B_.DTYPE_IDS[str(g.dtype)], steps=steps, count=g.shape[0], rows=g.shape[1], cols=g.shape[2], grad_matrix=g.stride(0),
                      grad_row=g.stride(1), eps=eps)
     a.workspace_bytes = B_.lib().fpde_orthogonalize_workspace_bytes(ctypes.byref(a))
     return a, g
@@ -56,7 +55,10 @@ def _plan(key, grad, steps, eps):
 def orthogonalize(grad, steps=5, eps=1e-7):
     """grad (rows, cols), or a stack (count, rows, cols) treated matrix by matrix, with its singular values driven
     towards one: X = grad / (|grad| + eps), then `steps` times X <- a X + (b S + c S S) X with S = X X^T and
-    (a, b, c) = (3.4445, -4.775, 2.0315), on the shorter side.  Returns a dense tensor of grad's type."""
+    (a, b, c) = (3.4445, -4.775, 2.0315), on the shorter side.  Returns a dense tensor of grad's type.  Not
+    differentiable: a backward pass that reaches the result raises."""
+    if wants_grad(grad):
+        return ValuesOnly.apply(orthogonalize, grad, steps, eps)
     a, g = _plan(("ortho", steps, eps, _lay(grad)), grad, steps, eps)
     dev = grad.device
     out = torch.empty_like(grad) if grad.is_contiguous() else torch.empty(grad.shape, dtype=grad.dtype, device=dev)

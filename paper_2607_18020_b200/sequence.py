@@ -24,8 +24,7 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from . import binding as B_
-
-_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+from .autograd import ValuesOnly, wants_grad
 
 
 class ConvGrads(NamedTuple):
@@ -72,7 +71,7 @@ def _same(given, taken):
 def _first(name, t, dims):
     if t.device.type != "cuda":
         raise ValueError("%s is on %s, expected a CUDA tensor" % (name, t.device))
-    if t.dtype not in _TYPES:
+    if str(t.dtype) not in B_.DTYPE_IDS:
         raise ValueError("%s is %s, expected fp32, bf16 or fp16" % (name, t.dtype))
     if t.dim() != dims:
         raise ValueError("%s has %d axes, expected %d" % (name, t.dim(), dims))
@@ -89,23 +88,6 @@ def _new(like, shape=None):
     if shape is None and like.is_contiguous():
         return torch.empty_like(like)            # a third of empty()'s host time
     return torch.empty(like.shape if shape is None else shape, dtype=like.dtype, device=like.device)
-
-
-class _ValuesOnly(torch.autograd.Function):
-    """The result of a call that has no gradient: asking for one is an error, not a zero."""
-
-    @staticmethod
-    def forward(ctx, call, *args):
-        ctx.name = call.__name__
-        return call(*args)                  # grad mode is off in here: the call does its work
-
-    @staticmethod
-    def backward(ctx, *grads):
-        raise RuntimeError("%s is not differentiable: train on whole rows, and call it under torch.no_grad()" % ctx.name)
-
-
-def _wants_grad(*inputs):
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in inputs)
 
 
 # For a tensor changed behind autograd's back: a backward pass that has kept it must not take it for what it was.
@@ -136,7 +118,7 @@ def _conv_args(x, weight, bias, state, silu, step, gy=None, gstate=None, workspa
             raise ValueError("window is updated in place and must be contiguous")
     else:
         state = _dense("state", state, window, dt, dev)
-    a = B_.ConvArgs(dtype=_TYPES[dt], width=width, silu=int(silu), batch=batch, length=1 if step else x.shape[1], channels=channels,
+    a = B_.ConvArgs(dtype=B_.DTYPE_IDS[str(dt)], width=width, silu=int(silu), batch=batch, length=1 if step else x.shape[1], channels=channels,
                     x_batch=x.stride(0), x_node=0 if step else x.stride(1))
     if gy is not None:
         gy = _activation("gy", gy, x.shape, dt, dev)
@@ -190,8 +172,8 @@ def causal_conv_bwd(gy, x, weight, bias=None, state=None, silu=True, gstate=None
 def causal_conv_step(x, window, weight, bias=None, silu=True):
     """One node per row: x (batch, channels) -> y; `window` (batch, width - 1, channels) is moved on in place.
     Not differentiable."""
-    if torch.is_grad_enabled() and _wants_grad(x, window, weight, bias):
-        return _ValuesOnly.apply(causal_conv_step, x, window, weight, bias, silu)
+    if torch.is_grad_enabled() and wants_grad(x, window, weight, bias):
+        return ValuesOnly.apply(causal_conv_step, x, window, weight, bias, silu)
     key = ("conv step", bool(silu), _lay(x), _lay(window), _lay(weight), _lay(bias))
     a = _plans.get(key)
     if a is None:
@@ -255,7 +237,7 @@ def _scan_args(u, delta, A, B, C, D, z, delta_bias, delta_softplus, state, step,
             raise ValueError("state is updated in place and must be contiguous")
     else:
         state = _dense("state", state, rest, torch.float32, dev)
-    a = B_.ScanArgs(dtype=_TYPES[dt], states=states, softplus=int(delta_softplus), batch=u.shape[0], length=1 if step else u.shape[1],
+    a = B_.ScanArgs(dtype=B_.DTYPE_IDS[str(dt)], states=states, softplus=int(delta_softplus), batch=u.shape[0], length=1 if step else u.shape[1],
                     channels=channels, u_batch=u.stride(0), delta_batch=delta.stride(0), B_batch=B.stride(0), C_batch=C.stride(0))
     if z is not None:
         a.z_batch = z.stride(0)
@@ -345,8 +327,8 @@ def selective_scan_step(state, u, delta, A, B, C, D=None, z=None, delta_bias=Non
     """One node per row: u, delta, z (batch, channels), B, C (batch, states) -> out (batch, channels); `state`
     (batch, channels, states) is moved on in place.  Not differentiable."""
     t = (u, delta, A, B, C, D, z, delta_bias, state)
-    if torch.is_grad_enabled() and _wants_grad(*t):
-        return _ValuesOnly.apply(selective_scan_step, state, u, delta, A, B, C, D, z, delta_bias, delta_softplus)
+    if torch.is_grad_enabled() and wants_grad(*t):
+        return ValuesOnly.apply(selective_scan_step, state, u, delta, A, B, C, D, z, delta_bias, delta_softplus)
     key = ("scan step", bool(delta_softplus), _lay(u), _lay(delta), _lay(A), _lay(B), _lay(C), _lay(D), _lay(z), _lay(delta_bias), _lay(state))
     a = _plans.get(key)
     if a is None:
@@ -384,6 +366,6 @@ class _SelectiveScan(torch.autograd.Function):
 def selective_scan(u, delta, A, B, C, D=None, z=None, delta_bias=None, delta_softplus=True, state=None, return_state=False):
     """selective_scan_fwd, differentiable in every tensor."""
     # decided here: inside forward() grad mode is always off, and parameters ask for gradients in any mode
-    keep = _wants_grad(u, delta, A, B, C, D, z, delta_bias, state)
+    keep = wants_grad(u, delta, A, B, C, D, z, delta_bias, state)
     out, last = _SelectiveScan.apply(u, delta, A, B, C, D, z, delta_bias, delta_softplus, state, keep)
     return (out, last) if return_state else out

@@ -21,6 +21,18 @@ def test_any_scale(size, scale, dtype):
     assert rel(x, ortho_ref(d64(g), 5, 0.0)) <= limit(dtype)
 
 
+def test_values_but_no_gradient():
+    from paper_2607_18020_b200 import optim
+    g = matrices(1, 40, 60, torch.float32)[0]
+    want = optim.orthogonalize(g)
+    x = optim.orthogonalize(g.requires_grad_(True))
+    assert torch.equal(x, want)
+    with pytest.raises(RuntimeError, match="orthogonalize is not differentiable"):
+        x.sum().backward()
+    with torch.no_grad():
+        assert not optim.orthogonalize(g).requires_grad
+
+
 @pytest.mark.parametrize("shape", [(48, 80), (300, 264)])
 def test_muon_step_of_tiny_gradients(shape):
     from paper_2607_18020_b200 import optim
