@@ -459,11 +459,16 @@ int fpde_diag_ns_tma_geometry(const int64_t* shape, int tile_rows, int narrays, 
  *
  * Rules on top of the general ones above
  *   - Activations are fp32, bf16 or fp16 (fpde_dtype); everything is computed in fp32 and rounded
- *     once, when it is stored.  Parameters, states and their gradients are fp32.
+ *     once, when it is stored (but see "Precision" at the orthogonalised update).  Exponentials and
+ *     reciprocals are the hardware's 2^x and 1/x, good to some 2^-22.  Parameters, states and their
+ *     gradients are fp32.
  *   - Activation inputs are (batch, length, channels) views: the channel axis is contiguous, the
  *     batch and node strides are given in elements (any value, zero included).  Outputs, parameters
- *     and states are dense.  Pointers need the alignment of their element type only; 16-byte
- *     aligned rows are read in wide loads.
+ *     and states are dense.  Pointers need the alignment of their element type only; where every row
+ *     starts on two elements, channels are read in pairs.
+ *   - Extents whose product passes 2^48 are refused.
+ *   - Infinities and NaN go where the formulas take them, with one exception: an infinite entry of B or
+ *     C can make NaN, in place of an infinity, of the gradients gC and gB of its own state.
  *   - Extents may be zero: an empty row leaves the state as it was.
  *   - The *_bytes queries look at the type, the settings and the sizes only (0 if they are refused).
  *   - The results of a call do not depend on what else runs: no atomics, sums in a fixed order.
@@ -520,6 +525,9 @@ int fpde_causal_conv_step(const fpde_conv_args* args, void* stream);
  * states that fpde_selective_scan_bwd starts from; both calls take the same sizes.
  * Rows are split along their length where batch and channels do not fill the GPU; the partial
  * states are joined in a fixed order.
+ * Memory: `kept` takes states / 2 bytes for each element of u; the workspace of the backward call, for its
+ * shares of gB and gC, about 2 bytes for 16 states, 8 for 32 and 32 for 64, and 4 bytes times the states for
+ * each row's piece and channel.  8 x 4096 x 4096 with 64 states: 4.3 GB each.
  */
 typedef struct {
     int32_t dtype, states, softplus, reserved;

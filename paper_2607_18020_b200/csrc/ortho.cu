@@ -4,11 +4,11 @@
 //   X = U / (|U| + eps);  `steps` times:  S = X X^T,  P = b S + c S S,  X <- a X + P X
 // on the shorter side (taller matrices are turned on the way in and back on the way out).
 //
-// Per step 2 m^2 (m + n) multiplications and additions are needed with the symmetry of S and S S, m <= n.
-// 4096^2 bf16, 5 steps: 1.37e12, 831 us at the measured bf16 rate, measured 1.35 ms (products 69, 69 and
-// 124 us a step, 80 % of the library product's rate for the one that has no symmetry; the passes around
-// them 64 us).  Four fp32 1000 x 333 steps of the optimiser: 183 us, small products that are bound by
-// latency.  Eight fp32 128 x 128 matrices: 36 us, 9 around the steps and 5.5 a step.
+// Per step m^2 (m + 3 n) multiplications and additions are needed with the symmetry of S and S S, m <= n.
+// 4096^2 bf16, 5 steps: 1.37e12, 831 us at the measured bf16 rate, measured 1.22 ms in short runs and 1.44 at the clock of
+// a loaded GPU (a step 231 us; its products 66, 65 and 113 under a profiler, the last, which has no symmetry, at 1216
+// TFLOP/s; the passes around them 68 us).  Four fp32 1000 x 333 steps of the optimiser: 172 us, small products that are
+// bound by latency.  Eight fp32 128 x 128 matrices: 37 us, 9 around the steps and 5.5 a step.
 #include <type_traits>
 
 #include "seq_common.cuh"
@@ -227,7 +227,8 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(OrthoIo io, const doub
 //   GRAM    S  = X X^T              SQUARE  P = b S + c S S             APPLY  X' = a X + P X
 //
 // Every matrix is held as two fp16 planes, hi and lo, of the value times 2^14: hi is the value rounded to
-// 11 bits, lo the next 11 bits of what is left.  The entries are at most 1.25 (X, S) or 2.81 (P) in size,
+// 11 bits, lo the next 11 bits of what is left.  The entries are at most 1.21 (X), 1.45 (S) or 2.81 (P) in size
+// (the quintic takes no singular value past 1.2025),
 // so the scaled hi stays below 65504, and 2^14 keeps lo above fp16's smallest numbers for entries down to
 // 2^-16.  With PAIR three products (hi hi, hi lo, lo hi) go into one fp32 accumulator: 22-bit factors.
 // Without it only hi hi is formed, and lo serves the terms a X and b S that are added in the epilogue.
@@ -250,7 +251,8 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(OrthoIo io, const doub
 // Large products run on pairs of SMs (CG = 2, cta_group::2): a tile has 256 rows, each block of the pair
 // loads its 128 rows of the left factor and half of the right one, and the first block issues for both.
 // What a block has to load per product is what bounds the one-block form (an SM takes 64 bytes a clock
-// from L2; 128 x 256 tiles need 96).
+// from L2; 128 x 256 tiles need 96).  Pairs bring 8.6, 9.3 and 10.1e12 bytes a second out of L2 in the three products of
+// 4096 x 4096, with the tensor pipe 68, 69 and 79 % busy.
 enum Kind { GRAM, SQUARE, APPLY };
 
 // Every wait is bounded: it gives up after WAIT_NS, or WAIT_TRIES tries (of 20 ns at the very least).  The longest that is
@@ -260,7 +262,10 @@ constexpr uint64_t WAIT_NS = 2000000000, LANDING_NS = 20000000, LOSE_NS = 100000
 constexpr int WAIT_TRIES = 1 << 28;
 // On one SM a wait is for one product, a microsecond: tries alone (20 ms at the very least) do, and cost less code.
 constexpr int SMALL_TRIES = 1 << 20;
-constexpr double PAIRS_START = 2e-6;        // seconds that a pair of blocks takes longer to start (four 333 x 1000: 14.4 us, 13.1 without pairs)
+// Seconds that a pair of blocks takes longer to start (four fp32 333 x 1000: 14.4 us a product, 13.1 without pairs).  Other sizes at
+// which the two meet, us a call with pairs against single blocks: 1024 x 1024 fp32 +23 (X X^T), 4 x 512 x 1024 +5 (P X), 2 x 1024 x 2048 +4
+// (X X^T, taken), 1536 x 1536 +7 (X X^T, taken), 2048 x 2048 +9 (X X^T, taken): more would do no harm.
+constexpr double PAIRS_START = 2e-6;
 constexpr int SEGMENT = 16;                 // slices of 64: 1024 of depth
 
 constexpr int BM = 128, BK = 64;
@@ -794,9 +799,12 @@ cudaError_t launch_product(const Maps& left, const Maps& right, const __half* ad
 }
 
 // Seconds that a form of a product takes, for comparing the forms.  A block brings `STAGE` bytes per 64 of
-// depth; all of them together get some 9e12 bytes a second out of L2 (8.4 to 8.7e12 in products of
-// 4096 x 4096 and 2048 x 8192), one alone some 76e9 (0.63 us for 48 KB), and its tensor core needs its time;
+// depth; all of them together are reckoned to get 9e12 bytes a second out of L2 (8.6 to 10.1e12 in
+// products of 4096 x 4096), one alone some 76e9 (0.63 us for 48 KB), and its tensor core needs its time;
 // the last tile's epilogue is not hidden, and joining a split depth takes two barriers of the cluster.
+// Each product was forced through every other form it could take, for 14 sizes from 40 x 900 to 2048 x 2048, stacks of up
+// to 16, fp32 and bf16: what is chosen is within 3 % of the best call, but for sixteen 300 x 300 (the square 8 and 6 %
+// slower in 128 columns a tile than in 64).
 template <bool PAIR, int CG, int BN, int KIND, bool LOWER, int KS = 1>
 double product_seconds(const ProductShape& s, int64_t count, int sms) {
     using R = Ring<PAIR, CG, BN>;

@@ -6,9 +6,10 @@
 // A thread owns a pair of neighbouring channels (one where rows start on odd elements) and marches along
 // its piece of a row with the last W-1 nodes in registers, so every value is loaded once per piece plus
 // a halo of W-1 nodes; the nodes ahead are on their way to shared memory meanwhile.  A block has 4 pieces
-// of 32 channel packs.  8 x 8192 x 2048 bf16, W = 4: forward 115 us (floor 82), gradients 208 us (floor 123,
-// issue slots 74 % busy: some 40 instructions an element for the filter, its gate, their gradients and the
-// weights').  Registers one group ahead instead of shared memory left too few bytes on their way: 328 and
+// of 32 channel packs.  8 x 8192 x 2048 bf16, W = 4: forward 115 us (floor 82, 0.66 instructions a
+// clock and scheduler, 45 % of the warps active), gradients 208 us (floor 123; 0.63 instructions, 28 % of the warps at 93
+// registers; some 40 instructions an element for the filter, its gate, their gradients and the weights'): neither bytes nor
+// issue slots are used up, both wait for latency.  Registers one group ahead instead of shared memory left too few bytes on their way: 328 and
 // 587 us.
 //
 // Gradients.  With g = gy * silu'(pre) the gradient of node t is sum_j w[j] g[t+W-1-j]: the march
@@ -424,15 +425,14 @@ int64_t conv_spans(const fpde_conv_args* a, int64_t positions) {
     return ceil_div(positions > 0 ? positions : 1, (int64_t)CONV_ROWS * conv_nodes(a, positions));
 }
 
-// Channels of one thread: 16 bytes of them where every row of every array starts on 16 bytes.
+// Two channels a thread where every row of every array starts on two elements.
 template <typename T>
-bool conv_wide(const fpde_conv_args* a, int vec, bool backward) {
+bool conv_pairs(const fpde_conv_args* a, bool backward) {
     const size_t e = sizeof(T);
-    bool ok = a->channels % vec == 0 && packs(a->x, a->x_batch, a->x_node, e, vec) && aligned(a->state, e * vec);
+    const bool ok = a->channels % 2 == 0 && packs(a->x, a->x_batch, a->x_node, e, 2) && aligned(a->state, 2 * e);
     if (backward)
-        return ok && packs(a->gy, a->gy_batch, a->gy_node, e, vec) && aligned(a->gx, e * vec) && aligned(a->gstate, e * vec) &&
-               aligned(a->gstate_out, e * vec);
-    return ok && aligned(a->y, e * vec) && aligned(a->state_out, e * vec);
+        return ok && packs(a->gy, a->gy_batch, a->gy_node, e, 2) && aligned(a->gx, 2 * e) && aligned(a->gstate, 2 * e) && aligned(a->gstate_out, 2 * e);
+    return ok && aligned(a->y, 2 * e) && aligned(a->state_out, 2 * e);
 }
 
 template <typename T, int VEC, int W, bool backward>
@@ -460,8 +460,8 @@ cudaError_t conv_launch(const fpde_conv_args* a, cudaStream_t st) {
 
 template <typename T, int W>
 cudaError_t conv_by_pack(const fpde_conv_args* a, bool backward, cudaStream_t st) {
-    if (backward) return conv_wide<T>(a, 2, true) ? conv_launch<T, 2, W, true>(a, st) : conv_launch<T, 1, W, true>(a, st);
-    return conv_wide<T>(a, 2, false) ? conv_launch<T, 2, W, false>(a, st) : conv_launch<T, 1, W, false>(a, st);
+    if (backward) return conv_pairs<T>(a, true) ? conv_launch<T, 2, W, true>(a, st) : conv_launch<T, 1, W, true>(a, st);
+    return conv_pairs<T>(a, false) ? conv_launch<T, 2, W, false>(a, st) : conv_launch<T, 1, W, false>(a, st);
 }
 
 template <typename T>

@@ -969,7 +969,9 @@ ScanShape plan(const fpde_scan_args* a, bool backward) {
     // Chunks.  The blocks run in waves of `resident` per SM, and a wave takes as long as its nodes: the marches
     // are bound by latency, so fewer blocks on an SM are hardly faster.  Splitting adds the pass that forms
     // the chunks' ends, a share `ends_cost` of the march, and two launches, worth about 80 nodes.  The
-    // cheapest number of chunks wins, the fewest of equals.
+    // cheapest number of chunks wins, the fewest of equals.  Measured against seven other numbers for each of 13 shapes, both
+    // directions: within 5 % of the best of them but for the forward pass of 32 x 300 x 333 (5 chunks 65 us, none 46), 8 x 512 x 1024 (4
+    // chunks 65, none 58), 2 x 8192 x 2048 (8 chunks 439, 32 400), 1 x 4096 x 256 and 1 x 65536 x 64 (10 %), and the gradients of 16 x 256 x 256 (57, 53).
     const int64_t length = a->length > 0 ? a->length : 1, blocks = a->batch * s.tiles;
     const int64_t resident = 148 * (backward ? back_blocks(2) : fwd_blocks(2));
     const double ends_cost = backward ? BACK_ENDS : FWD_ENDS;
@@ -1137,9 +1139,12 @@ cudaError_t run_step(const fpde_scan_args* a, cudaStream_t st) {
 }
 
 // Up to so many blocks a march gives its threads one channel instead of two: a block then has twice the
-// threads with half the work, which pays while SMs have warps to spare (us, one channel against two:
-// forward 4 blocks 11.6 / 16.3, 512 blocks 25.8 / 29.8, 1024 blocks 313 / 287; backward 256 blocks 70 / 75,
-// 384 blocks 961 / 855).  The pass that only forms the chunks' ends always does (169 / 189, 216 / 213).
+// threads with half the work, which pays while SMs have warps to spare.  Rows of 256 nodes, bf16, us with one channel and with
+// two.  16 states forward: 128 blocks 27 / 38, 256 31 / 39, 384 51 / 46, 592 51 / 47, 640 52 / 69, 896 76 / 71, 1280 91 / 99, 1792
+// 130 / 122; gradients: 128 127 / 141, 256 134 / 179, 296 136 / 181, 320 211 / 184, 448 259 / 297, 640 335 / 328.  32 states
+// alike.  8 states: one channel is as good or better nearly everywhere (592 51 / 59, 768 81 / 74, 1024 88 / 115; gradients 296 202 / 281,
+// 640 489 / 671).  Whole waves decide, and no one number is best at every size; these are the last ones at which one
+// channel wins in both types.  The pass that only forms the chunks' ends always has one (169 / 189, 216 / 213).
 constexpr int64_t FWD_ONE = 148 * 4, BACK_ONE = 148 * 2;
 
 int channels_a_thread(const fpde_scan_args* a, const ScanShape& s, bool backward) {
