@@ -803,8 +803,8 @@ cudaError_t launch_product(const Maps& left, const Maps& right, const __half* ad
 // products of 4096 x 4096), one alone some 76e9 (0.63 us for 48 KB), and its tensor core needs its time;
 // the last tile's epilogue is not hidden, and joining a split depth takes two barriers of the cluster.
 // Each product was forced through every other form it could take, for 14 sizes from 40 x 900 to 2048 x 2048, stacks of up
-// to 16, fp32 and bf16: what is chosen is within 3 % of the best call, but for sixteen 300 x 300 (the square 8 and 6 %
-// slower in 128 columns a tile than in 64).
+// to 16, fp32 and bf16: what is chosen is within 5 % of the best call, but for sixteen 300 x 300 (8 and 6 %
+// slower with the square in 128 columns a tile than in 64).
 template <bool PAIR, int CG, int BN, int KIND, bool LOWER, int KS = 1>
 double product_seconds(const ProductShape& s, int64_t count, int sms) {
     using R = Ring<PAIR, CG, BN>;

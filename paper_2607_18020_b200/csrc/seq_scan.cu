@@ -971,7 +971,8 @@ ScanShape plan(const fpde_scan_args* a, bool backward) {
     // the chunks' ends, a share `ends_cost` of the march, and two launches, worth about 80 nodes.  The
     // cheapest number of chunks wins, the fewest of equals.  Measured against seven other numbers for each of 13 shapes, both
     // directions: within 5 % of the best of them but for the forward pass of 32 x 300 x 333 (5 chunks 65 us, none 46), 8 x 512 x 1024 (4
-    // chunks 65, none 58), 2 x 8192 x 2048 (8 chunks 439, 32 400), 1 x 4096 x 256 and 1 x 65536 x 64 (10 %), and the gradients of 16 x 256 x 256 (57, 53).
+    // chunks 65, none 58), 2 x 8192 x 2048 (8 chunks 439, 32 400), 1 x 4096 x 256 and 1 x 65536 x 64 (10 %), and the gradients
+    // of 16 x 256 x 256 (57, 53) and 1 x 512 x 2048 (62, 59).
     const int64_t length = a->length > 0 ? a->length : 1, blocks = a->batch * s.tiles;
     const int64_t resident = 148 * (backward ? back_blocks(2) : fwd_blocks(2));
     const double ends_cost = backward ? BACK_ENDS : FWD_ENDS;
