@@ -582,7 +582,7 @@ int fpde_selective_scan_step(const fpde_scan_args* args, void* stream);
  *
  * Precision: with fp32 arrays the products are formed from fp16 pairs that hold 22 bits of each
  * factor and summed in fp32; with 16-bit arrays from single fp16 factors (11 bits), while the
- * running X keeps 22 bits.
+ * running X keeps 22 bits.  Matrices of at most 8 x 256 or 256 x 8 are multiplied as pairs in every type.
  *
  * The products wait for one another inside the kernels, each wait for two seconds at most.  A call in
  * which one gave up writes NaN (fpde_muon_step: over the weight) and counts in fpde_diag_ortho_timeouts.

@@ -857,6 +857,14 @@ cudaError_t run_product(const Maps& left, const Maps& right, const __half* added
 // next to 1.7e-3 from rounding the result to bf16).  One launch instead of three per step and three
 // around them; what bounds it is the chain of 3 x steps products, each of which waits for the one before.
 // The planes of X, rows of 64-column blocks, serve as K-major factor of S and as MN-major factor of P X.
+//
+// 16-bit matrices of up to SMALL_PAIRS on their shorter side are multiplied as pairs too.  A direction in which such a matrix
+// is almost singular is a large part of it, and single factors' rounding grows in it at every step.  The worst of 4096 to 16384
+// matrices, single factors, against 3e-3 (bf16) or 4e-4 (fp16) of the result's own rounding, which is all that pairs leave: 2 x 2
+// 1.5e-2, 3 x 5 1.2e-2, 3 x 20 1.1e-2, 6 x 6 9.9e-3, 8 x 8 5.8e-3, 16 x 16 3.6e-3, 24 x 24 3.3e-3, 128 x 128 2.4e-3: from 8 on the
+// rest dilutes it below the 8.3e-3 that single factors are allowed, and they are faster (eight 16 x 256 27 against 35 us, 64 x 256
+// 34 against 45, 128 x 128 32 against 39).
+constexpr int SMALL_PAIRS = 8;
 constexpr int SMALL_M = 128, SMALL_N = 256, SMALL_THREADS = 512;
 constexpr int SMALL_BLOCK = SMALL_M * 128;              // bytes of a 64-column block of a plane
 constexpr int SMALL_S = 4 * SMALL_BLOCK;                // S: two blocks, hi and lo
@@ -877,9 +885,8 @@ __device__ __forceinline__ float value_at(uint8_t* hi_plane, uint8_t* lo_plane, 
            __half2float(*reinterpret_cast<const __half*>(chunk_at(lo_plane, r, c & ~7) + 2 * (c & 7)));
 }
 
-template <typename T>
+template <typename T, bool PAIR>
 __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo io, int steps, bool lose) {
-    constexpr bool PAIR = sizeof(T) == 4;
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bar, ended;
     __shared__ uint32_t tmem_slot;
@@ -1243,9 +1250,13 @@ cudaError_t run(const fpde_ortho_args* a, bool muon, bool lose, cudaStream_t st)
     io.mp = (int)padded(io.m); io.np = (int)padded(io.n);
     io.wide = io.cols % 8 == 0 && packs(io.grad, io.grad_matrix, io.grad_row, sizeof(T), 16 / sizeof(T)) && aligned(io.out, 16) && aligned(io.momentum, 16);
     if (is_small(io.m, io.n)) {
-        static std::atomic<uint64_t> allowed{0};
-        FPDE_TRY(allow_smem(ortho_small_kernel<T>, small_bytes(SMALL_N), allowed));
-        return launch_kernel_smem(ortho_small_kernel<T>, dim3((unsigned)a->count), dim3(SMALL_THREADS), small_bytes(io.np), st, io, a->steps, lose);
+        auto launch = [&](auto* kernel, std::atomic<uint64_t>& allowed) {
+            FPDE_TRY(allow_smem(kernel, small_bytes(SMALL_N), allowed));
+            return launch_kernel_smem(kernel, dim3((unsigned)a->count), dim3(SMALL_THREADS), small_bytes(io.np), st, io, a->steps, lose);
+        };
+        static std::atomic<uint64_t> pairs{0}, single{0};
+        if (sizeof(T) == 4 || io.m <= SMALL_PAIRS) return launch(ortho_small_kernel<T, true>, pairs);
+        if constexpr (sizeof(T) == 2) return launch(ortho_small_kernel<T, false>, single);
     }
     const OrthoSpace w = space(a->count, io.m, io.n);
     char* ws = (char*)a->workspace;
