@@ -581,8 +581,10 @@ int fpde_selective_scan_step(const fpde_scan_args* args, void* stream);
  * in place on weight (dtype) and momentum (fp32).
  *
  * Precision: with fp32 arrays the products are formed from fp16 pairs that hold 22 bits of each
- * factor and summed in fp32; with 16-bit arrays from single fp16 factors (11 bits), while the
- * running X keeps 22 bits.  Matrices of at most 8 x 256 or 256 x 8 are multiplied as pairs in every type.
+ * factor and summed in fp32.  With 16-bit arrays the running X keeps 22 bits, and products are formed from
+ * single fp16 factors (11 bits) but for: S S up to 1024 on the shorter side; P X, P = b S + c S S, up to 128, where
+ * P alone is a pair if the longer side is at most 256; everything of at most 8 x 256 or 256 x 8.  What that
+ * leaves beside the result's own rounding is about as much again in bf16, and up to 2e-3 in fp16 (own 2.1e-4).
  *
  * The products wait for one another inside the kernels, each wait for two seconds at most.  A call in
  * which one gave up writes NaN (fpde_muon_step: over the weight) and counts in fpde_diag_ortho_timeouts.

@@ -819,16 +819,20 @@ double product_seconds(const ProductShape& s, int64_t count, int sms) {
 
 // Pairs of SMs, or single blocks with tiles of 128 or 64 columns, the latter with the depth split over 2 or 4
 // blocks where there are few: whichever is reckoned fastest.
+// The forms with 64 columns a tile are for few tiles.  S S of single factors is formed from 1088 rows on and has 153 of
+// them, against 45 of 128 columns.
+template <bool PAIR, int KIND>
+constexpr bool has_narrow() { return PAIR || KIND != SQUARE; }
+
 template <bool PAIR, int KIND>
 int best_form(const ProductShape& s, int64_t count, int sms) {
     constexpr int WIDE = PAIR ? 128 : 256;      // PAIR: two accumulators a set
     constexpr bool LOWER = KIND != APPLY;
     const double t[5] = {product_seconds<PAIR, 2, WIDE, KIND, LOWER>(s, count, sms), product_seconds<PAIR, 1, 128, KIND, LOWER>(s, count, sms),
                          product_seconds<PAIR, 1, 64, KIND, false>(s, count, sms), product_seconds<PAIR, 1, 64, KIND, false, 2>(s, count, sms),
-                         // S S of single factors is formed from 576 rows on: 45 tiles or more, too many for clusters of 4
-                         KIND == SQUARE && !PAIR ? 1e9 : product_seconds<PAIR, 1, 64, KIND, false, 4>(s, count, sms)};
+                         product_seconds<PAIR, 1, 64, KIND, false, 4>(s, count, sms)};
     int best = 0;
-    for (int i = 1; i < 5; ++i)
+    for (int i = 1; i < (has_narrow<PAIR, KIND>() ? 5 : 2); ++i)
         if (t[i] < t[best]) best = i;
     return best;
 }
@@ -838,32 +842,34 @@ cudaError_t run_product(const Maps& left, const Maps& right, const __half* added
                         int sms, cudaStream_t st) {
     constexpr int WIDE = PAIR ? 128 : 256;
     constexpr bool LOWER = KIND != APPLY;
-    switch (best_form<PAIR, KIND>(s, count, sms)) {
-    case 0: return launch_product<PAIR, 2, WIDE, KIND, LOWER>(left, right, added, out, lost, s, count, sms, st);
-    case 1: return launch_product<PAIR, 1, 128, KIND, LOWER>(left, right, added, out, lost, s, count, sms, st);
-    case 2: return launch_product<PAIR, 1, 64, KIND, false>(left, right, added, out, lost, s, count, sms, st);
-    case 3: return launch_product<PAIR, 1, 64, KIND, false, 2>(left, right, added, out, lost, s, count, sms, st);
-    default:
-        if constexpr (KIND == SQUARE && !PAIR) return cudaErrorNotSupported;
-        else return launch_product<PAIR, 1, 64, KIND, false, 4>(left, right, added, out, lost, s, count, sms, st);
+    const int form = best_form<PAIR, KIND>(s, count, sms);
+    if constexpr (has_narrow<PAIR, KIND>()) {
+        if (form == 2) return launch_product<PAIR, 1, 64, KIND, false>(left, right, added, out, lost, s, count, sms, st);
+        if (form == 3) return launch_product<PAIR, 1, 64, KIND, false, 2>(left, right, added, out, lost, s, count, sms, st);
+        if (form == 4) return launch_product<PAIR, 1, 64, KIND, false, 4>(left, right, added, out, lost, s, count, sms, st);
     }
+    if (form == 1) return launch_product<PAIR, 1, 128, KIND, LOWER>(left, right, added, out, lost, s, count, sms, st);
+    return launch_product<PAIR, 2, WIDE, KIND, LOWER>(left, right, added, out, lost, s, count, sms, st);
 }
 
 // --------------------------------------------------------------------------------- small matrices
 // A matrix whose shorter side is at most 128 and whose longer side is at most 256 stays on one SM for the
 // whole call: X and S (then P) as swizzled hi and lo planes in shared memory, the products' sums in TMEM,
-// cross products apart.  S S is formed from pairs whatever the type: in matrices this small its factors'
-// rounding is the largest part of the 16-bit types' error (64 x 200: 2.1e-3 of 2.1e-3, 1.2e-3 without it,
-// next to 1.7e-3 from rounding the result to bf16).  One launch instead of three per step and three
+// cross products apart.  One launch instead of three per step and three
 // around them; what bounds it is the chain of 3 x steps products, each of which waits for the one before.
 // The planes of X, rows of 64-column blocks, serve as K-major factor of S and as MN-major factor of P X.
+//
+// With 16-bit types X enters X X^T and P X as a single factor; S S and P are pairs whatever the type, which costs a product
+// each where three wait for one another anyway.  Error of bf16 results, of which 1.66e-3 is their own rounding: 64 x 200 3.8e-3 with
+// single factors throughout, 2.5e-3 with S as a pair, 2.1e-3 with P as one too (fp16: 3.5e-3, 1.9e-3, 1.3e-3, own 2.1e-4); P
+// takes eight 128 x 128 from 32 to 34 us, 400 128 x 256 from 150 to 165.
 //
 // 16-bit matrices of up to SMALL_PAIRS on their shorter side are multiplied as pairs too.  A direction in which such a matrix
 // is almost singular is a large part of it, and single factors' rounding grows in it at every step.  The worst of 4096 to 16384
 // matrices, single factors, against 3e-3 (bf16) or 4e-4 (fp16) of the result's own rounding, which is all that pairs leave: 2 x 2
 // 1.5e-2, 3 x 5 1.2e-2, 3 x 20 1.1e-2, 6 x 6 9.9e-3, 8 x 8 5.8e-3, 16 x 16 3.6e-3, 24 x 24 3.3e-3, 128 x 128 2.4e-3: from 8 on the
 // rest dilutes it below the 8.3e-3 that single factors are allowed, and they are faster (eight 16 x 256 27 against 35 us, 64 x 256
-// 34 against 45, 128 x 128 32 against 39).
+// 37 against 45, 128 x 128 34 against 39).
 constexpr int SMALL_PAIRS = 8;
 constexpr int SMALL_M = 128, SMALL_N = 256, SMALL_THREADS = 512;
 constexpr int SMALL_BLOCK = SMALL_M * 128;              // bytes of a 64-column block of a plane
@@ -1077,10 +1083,8 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
                 if (p >= deep_m) break;
                 const uint64_t h = k_major(dsh, p), r = desc_at(rxh, p * 2048);
                 mma_f16(tmem, h, r, idesc, p > 0);
-                if (PAIR) {
-                    mma_f16(tmem + 256, h, desc_at(rxl, p * 2048), idesc, p > 0);
-                    mma_f16(tmem + 256, k_major(dsl, p), r, idesc, true);
-                }
+                mma_f16(tmem + 256, k_major(dsl, p), r, idesc, p > 0);
+                if (PAIR) mma_f16(tmem + 256, h, desc_at(rxl, p * 2048), idesc, true);
             }
             mma_commit(smem_u32(&bar));
         }
@@ -1088,7 +1092,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(OrthoIo i
 #pragma unroll 1
         for (int c = part_of * 32; c < io.np; c += 128) {
             float v[32];
-            load_sums<PAIR ? 2 : 1>(v, tmem + lanes + c, 256);
+            load_sums<2>(v, tmem + lanes + c, 256);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const Pack<__half, 8> h = *reinterpret_cast<const Pack<__half, 8>*>(chunk_at(xh, row, c + 8 * q));
@@ -1229,9 +1233,13 @@ ProductShape shape_of(int kind, int mp, int np) {
     if (kind == SQUARE) return {mp, np, 0, 0, 0, 0, mp, NS_C / SCALE, NS_B};
     return {mp, np, 0, 0, 0, 0, np, 1.f / SCALE, NS_A};
 }
-// While S is small its square is bound by latency: pairs cost nothing, and its factors' rounding is the largest part of
-// the 16-bit types' error on matrices much wider than tall (40 x 900: 2.2e-3 of it).
-bool square_of_pairs(int mp) { return mp <= 512; }
+// 16-bit matrices: up to which padded shorter side S S and P X are formed from pairs.  While S is small its square is a small
+// part of the time and its factors' rounding a large part of the error (bf16, own rounding 1.66e-3): 40 x 900 5.1e-3 without and
+// 2.9e-3 with pairs there, 576 x 576 2.48e-3 and 2.19e-3, 1000 x 1000 2.35e-3 and 2.08e-3; at 1100 it is 2.33e-3 without.  Time: 640 x 640 and
+// 1024 x 1024 alike to 3 %, four 768 x 1536 279 -> 301 us.  P X of up to 128 rows: 32 x 300 2.9e-3 and 1.76e-3, 64 x 900 2.5e-3 and 1.67e-3;
+// two 40 x 900 85 -> 87 us.
+bool square_of_pairs(int mp) { return mp <= 1024; }
+bool apply_of_pairs(int mp) { return mp <= 128; }
 
 template <typename T>
 cudaError_t run(const fpde_ortho_args* a, bool muon, bool lose, cudaStream_t st) {
@@ -1285,7 +1293,8 @@ cudaError_t run(const fpde_ortho_args* a, bool muon, bool lose, cudaStream_t st)
         FPDE_TRY((run_product<PAIR, GRAM>(xm[at], xm[at], s, s, lost, gram, a->count, sms, st)));
         if (PAIR || square_of_pairs(io.mp)) FPDE_TRY((run_product<true, SQUARE>(sm, sm, s, p, lost, square, a->count, sms, st)));
         else FPDE_TRY((run_product<false, SQUARE>(sm, sm, s, p, lost, square, a->count, sms, st)));
-        FPDE_TRY((run_product<PAIR, APPLY>(pm, xm[at], x[at], x[at ^ 1], lost, apply, a->count, sms, st)));
+        if (PAIR || apply_of_pairs(io.mp)) FPDE_TRY((run_product<true, APPLY>(pm, xm[at], x[at], x[at ^ 1], lost, apply, a->count, sms, st)));
+        else FPDE_TRY((run_product<PAIR, APPLY>(pm, xm[at], x[at], x[at ^ 1], lost, apply, a->count, sms, st)));
     }
     return launch_kernel(ortho_finish_kernel<T>, dim3((unsigned)pieces), dim3(256), st, io, (const __half*)x[at], (const unsigned int*)lost);
 }
@@ -1324,7 +1333,7 @@ int fpde_diag_ortho_form(const fpde_ortho_args* a, int product) {
     if (m == 0 || a->count == 0 || is_small(m, n)) return -1;
     const int mp = (int)padded(m), np = (int)padded(n), sms = sm_count_or_default();
     const ProductShape s = shape_of(product, mp, np);
-    const bool pair = a->dtype == FPDE_F32 || (product == SQUARE && square_of_pairs(mp));
+    const bool pair = a->dtype == FPDE_F32 || (product == SQUARE && square_of_pairs(mp)) || (product == APPLY && apply_of_pairs(mp));
     if (product == GRAM) return pair ? best_form<true, GRAM>(s, a->count, sms) : best_form<false, GRAM>(s, a->count, sms);
     if (product == SQUARE) return pair ? best_form<true, SQUARE>(s, a->count, sms) : best_form<false, SQUARE>(s, a->count, sms);
     return pair ? best_form<true, APPLY>(s, a->count, sms) : best_form<false, APPLY>(s, a->count, sms);

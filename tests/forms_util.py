@@ -15,7 +15,7 @@ CONV_STEP_ROWS = [(250, 4096), (77, 4095), (1301, 512)]
 # count, rows, cols: together every form of every product that 32- and 16-bit matrices take
 ORTHO = [(1, 520, 264), (2, 264, 520), (1, 300, 301), (1, 40, 900), (40, 40, 900), (1, 33, 5000), (12, 200, 3000), (1, 1000, 1030),
          (4, 1000, 333), (1, 1500, 700), (24, 300, 300), (1, 2300, 2100), (64, 150, 260), (6, 640, 1280), (1, 700, 4000), (1, 640, 640),
-         (1, 448, 512), (1, 384, 1000)]
+         (1, 448, 512), (1, 384, 1000), (1, 1100, 1200)]
 
 
 def scan_forms(batch, length, channels, states, backward):

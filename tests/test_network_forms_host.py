@@ -28,10 +28,11 @@ def test_rows_a_thread():
 
 
 def test_every_form_of_every_product():
-    """Five forms of three products, of pairs (fp32, and the square of small S) and of single factors; single factors' square has four."""
+    """Five forms of three products, of pairs (fp32, the square of smaller S and the last product of small P) and of single
+    factors; single factors' square has two."""
     seen = set()
     for dtype in (0, 1):
         for size in ORTHO:
             short = (min(size[1:]) + 63) // 64 * 64
-            seen |= {(dtype == 0 or (p == 1 and short <= 512), p, f) for p, f in enumerate(ortho_forms(dtype, *size)) if f >= 0}
-    assert seen == {(pair, p, f) for pair in (True, False) for p in range(3) for f in range(5)} - {(False, 1, 4)}
+            seen |= {(dtype == 0 or short <= (0, 1024, 128)[p], p, f) for p, f in enumerate(ortho_forms(dtype, *size)) if f >= 0}
+    assert seen == {(pair, p, f) for pair in (True, False) for p in range(3) for f in range(5)} - {(False, 1, f) for f in (2, 3, 4)}
