@@ -5,7 +5,7 @@
 // on the shorter side (taller matrices are turned on the way in and back on the way out).
 //
 // Per step m^2 (m + 3 n) multiplications and additions are needed with the symmetry of S and S S, m <= n.
-// 4096^2 bf16, 5 steps: 1.37e12, 831 us at the measured bf16 rate, measured 1.22 ms in short runs and 1.44 at the clock of
+// 4096^2 bf16, 5 steps: 1.37e12, 831 us at the measured bf16 rate, measured 1.22 ms in short runs and 1.44 to 1.48 at the clock of
 // a loaded GPU (a step 231 us; its products 66, 65 and 113 under a profiler, the last, which has no symmetry, at 1216
 // TFLOP/s; the passes around them 68 us).  Four fp32 1000 x 333 steps of the optimiser: 172 us, small products that are
 // bound by latency.  Eight fp32 128 x 128 matrices: 37 us, 9 around the steps and 5.5 a step.
