@@ -569,6 +569,93 @@ int fpde_selective_scan_bwd(const fpde_scan_args* args, void* stream);
 int fpde_selective_scan_step(const fpde_scan_args* args, void* stream);
 
 /*
+ * Rotation of each head's queries and keys by their position, with or without a norm of the head before it:
+ *     u = norm ? x / sqrt(mean(x^2) + eps) * weight : x                       (over the `dim` features of a head)
+ *     y = u with its first 2 * pairs features turned: pair i by the angle position * inv_freq[i]
+ * Pair i is (u[i], u[i + pairs]), interleaved: (u[2i], u[2i+1]); it becomes (a cos - b sin, b cos + a sin).  The
+ * features behind 2 * pairs are not turned; pairs = 0 turns nothing.  position = offset + positions[b, t], or
+ * offset + t.  The angle is formed and reduced in 64 bits, so far positions keep their digits.
+ *
+ * q is (batch, length, q_heads, dim), k (batch, length, k_heads, dim), both views with contiguous features; k may be
+ * NULL (k_heads 0).  Results and gradients are dense.
+ *
+ * Gradients (fpde_head_rotary_bwd): from gq and gk, of q_out and k_out, to gx_q and gx_k; with norm from q and k too, and to
+ * the weights' gradients where those are not NULL.  Without norm q, k, weights and eps are not looked at.
+ */
+#define FPDE_HEAD_MAX_DIM 256
+
+typedef struct {
+    int32_t dtype, norm, interleaved, pairs;
+    int64_t batch, length, q_heads, k_heads, dim;
+    const void* q; int64_t q_batch, q_node, q_head;      /* (batch, length, q_heads, dim) */
+    const void* k; int64_t k_batch, k_node, k_head;      /* (batch, length, k_heads, dim), or NULL */
+    const float* q_weight;    /* (dim), or NULL */
+    const float* k_weight;    /* (dim), or NULL */
+    const float* inv_freq;    /* (pairs) */
+    const int64_t* positions; int64_t pos_batch, pos_node;   /* (batch, length), or NULL */
+    int64_t offset;
+    double eps;
+    void* q_out;              /* fwd: (batch, length, q_heads, dim) */
+    void* k_out;              /* fwd: (batch, length, k_heads, dim) */
+    /* gradients (fpde_head_rotary_bwd) */
+    const void* gq; int64_t gq_batch, gq_node, gq_head;
+    const void* gk; int64_t gk_batch, gk_node, gk_head;
+    void* gx_q;               /* (batch, length, q_heads, dim) */
+    void* gx_k;               /* (batch, length, k_heads, dim) */
+    float* gq_weight;         /* (dim), or NULL */
+    float* gk_weight;         /* (dim), or NULL */
+    void* workspace;          /* bwd with norm: at least fpde_head_rotary_workspace_bytes(), 16-byte aligned */
+    size_t workspace_bytes;
+} fpde_head_args;
+
+size_t fpde_head_rotary_workspace_bytes(const fpde_head_args* args);
+int fpde_head_rotary_fwd(const fpde_head_args* args, void* stream);
+int fpde_head_rotary_bwd(const fpde_head_args* args, void* stream);
+
+/*
+ * Linear attention that forgets: for every row and head, with the decay g = exp(log_decay[head]),
+ *     S[t] = g S[t-1] + k[t] v[t]^T              (dk x dv; S[-1] = state, zeros if NULL)
+ *     o[t] = scale * q[t] S[t]
+ * q and k are (batch, length, heads, dk) views, v (batch, length, heads, dv): contiguous features, any strides of the other
+ * axes, zero included (one key head for all queries).  The decay is a constant of the layer: it has no gradient.
+ *
+ * Gradients (fpde_linear_attention_bwd): from go, of o, and gstate_out, of state_out (zeros if NULL), to gq, gk, gv
+ * and gstate (NULL: not wanted).  Nothing is kept between the passes.
+ * Rows are split along their length where batch and heads do not fill the GPU; the workspace then holds a state for
+ * each piece.  Infinities and NaN of a node reach no earlier node and no other head; from that node on the sums that they enter
+ * are infinite or NaN, not always the one of the two that a march through the nodes would give.
+ */
+#define FPDE_LINEAR_MAX_DIM 128
+
+typedef struct {
+    int32_t dtype, reserved;
+    int64_t batch, length, heads, dk, dv;
+    const void* q; int64_t q_batch, q_node, q_head;      /* (batch, length, heads, dk) */
+    const void* k; int64_t k_batch, k_node, k_head;      /* (batch, length, heads, dk) */
+    const void* v; int64_t v_batch, v_node, v_head;      /* (batch, length, heads, dv) */
+    const float* log_decay;   /* (heads) */
+    double scale;
+    const float* state;       /* (batch, heads, dk, dv), or NULL */
+    void* o;                  /* fwd, step: (batch, length, heads, dv) */
+    float* state_out;         /* (batch, heads, dk, dv), or NULL.  fwd: must not be `state`. */
+    /* gradients (fpde_linear_attention_bwd) */
+    const void* go; int64_t go_batch, go_node, go_head;  /* (batch, length, heads, dv) */
+    const float* gstate_out;  /* gradient of state_out, or NULL */
+    void* gq;                 /* (batch, length, heads, dk) */
+    void* gk;                 /* (batch, length, heads, dk) */
+    void* gv;                 /* (batch, length, heads, dv) */
+    float* gstate;            /* (batch, heads, dk, dv), or NULL.  Must not be `gstate_out`. */
+    void* workspace;          /* at least fpde_linear_attention_workspace_bytes(), 16-byte aligned; NULL if that is 0 */
+    size_t workspace_bytes;
+} fpde_linear_args;
+
+size_t fpde_linear_attention_workspace_bytes(const fpde_linear_args* args, int backward);
+int fpde_linear_attention_fwd(const fpde_linear_args* args, void* stream);
+int fpde_linear_attention_bwd(const fpde_linear_args* args, void* stream);
+/* One node per row (length is taken as 1): `state_out` may be (and usually is) `state` itself. */
+int fpde_linear_attention_step(const fpde_linear_args* args, void* stream);
+
+/*
  * Orthogonalised update of a stack of `count` matrices (count, rows, cols):
  *     X = G / (|G|_F + eps);  `steps` times:  X <- a X + (b S + c S S) X,  S = X X^T
  * with (a, b, c) = (3.4445, -4.775, 2.0315), on the shorter side: it drives the singular values of

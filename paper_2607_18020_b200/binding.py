@@ -56,6 +56,29 @@ class ScanArgs(ctypes.Structure):
                 ("gdelta_bias", _vp), ("gstate", _vp), ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t)]
 
 
+def _view(*names, axes=("batch", "node", "head")):
+    return [(n + k, t) for n in names for k, t in [("", _vp)] + [("_" + a, _i64c) for a in axes]]
+
+
+class HeadArgs(ctypes.Structure):
+    """fpde_head_args of include/fpde.h."""
+    _fields_ = [("dtype", _i32c), ("norm", _i32c), ("interleaved", _i32c), ("pairs", _i32c),
+                ("batch", _i64c), ("length", _i64c), ("q_heads", _i64c), ("k_heads", _i64c), ("dim", _i64c)] + _view("q", "k") + \
+               [("q_weight", _vp), ("k_weight", _vp), ("inv_freq", _vp), ("positions", _vp), ("pos_batch", _i64c), ("pos_node", _i64c),
+                ("offset", _i64c), ("eps", ctypes.c_double), ("q_out", _vp), ("k_out", _vp)] + _view("gq", "gk") + \
+               [("gx_q", _vp), ("gx_k", _vp), ("gq_weight", _vp), ("gk_weight", _vp), ("workspace", _vp),
+                ("workspace_bytes", ctypes.c_size_t)]
+
+
+class LinearArgs(ctypes.Structure):
+    """fpde_linear_args of include/fpde.h."""
+    _fields_ = [("dtype", _i32c), ("reserved", _i32c),
+                ("batch", _i64c), ("length", _i64c), ("heads", _i64c), ("dk", _i64c), ("dv", _i64c)] + _view("q", "k", "v") + \
+               [("log_decay", _vp), ("scale", ctypes.c_double), ("state", _vp), ("o", _vp), ("state_out", _vp)] + _view("go") + \
+               [("gstate_out", _vp), ("gq", _vp), ("gk", _vp), ("gv", _vp), ("gstate", _vp), ("workspace", _vp),
+                ("workspace_bytes", ctypes.c_size_t)]
+
+
 class OrthoArgs(ctypes.Structure):
     """fpde_ortho_args of include/fpde.h."""
     _fields_ = [("dtype", _i32c), ("steps", _i32c), ("nesterov", _i32c), ("reserved", _i32c),
@@ -153,12 +176,16 @@ def lib():
         for name, args, extra in (("fpde_causal_conv_workspace_bytes", ConvArgs, []),
                                   ("fpde_selective_scan_kept_bytes", ScanArgs, []),
                                   ("fpde_selective_scan_workspace_bytes", ScanArgs, [ctypes.c_int]),
+                                  ("fpde_head_rotary_workspace_bytes", HeadArgs, []),
+                                  ("fpde_linear_attention_workspace_bytes", LinearArgs, [ctypes.c_int]),
                                   ("fpde_orthogonalize_workspace_bytes", OrthoArgs, [])):
             getattr(L, name).restype = ctypes.c_size_t
             getattr(L, name).argtypes = [ctypes.POINTER(args)] + extra
         for name, args in (("fpde_causal_conv_fwd", ConvArgs), ("fpde_causal_conv_bwd", ConvArgs), ("fpde_causal_conv_step", ConvArgs),
                            ("fpde_selective_scan_fwd", ScanArgs), ("fpde_selective_scan_bwd", ScanArgs),
-                           ("fpde_selective_scan_step", ScanArgs), ("fpde_orthogonalize", OrthoArgs), ("fpde_muon_step", OrthoArgs),
+                           ("fpde_selective_scan_step", ScanArgs), ("fpde_head_rotary_fwd", HeadArgs), ("fpde_head_rotary_bwd", HeadArgs),
+                           ("fpde_linear_attention_fwd", LinearArgs), ("fpde_linear_attention_bwd", LinearArgs),
+                           ("fpde_linear_attention_step", LinearArgs), ("fpde_orthogonalize", OrthoArgs), ("fpde_muon_step", OrthoArgs),
                            ("fpde_diag_orthogonalize_lost", OrthoArgs)):
             getattr(L, name).restype = ctypes.c_int
             getattr(L, name).argtypes = [ctypes.POINTER(args), ctypes.c_void_p]

@@ -1,23 +1,32 @@
 """Sequence operators of a network that marches fields along one axis of the grid: a short causal
-convolution and a selective state space scan over rows of (batch, length, channels) tensors.
+convolution and a selective state space scan over rows of (batch, length, channels) tensors, and linear
+attention with a decay for each head over (batch, length, heads, features), with the position rotation
+and the norm of its queries and keys.
 
     y = causal_conv(x, weight, bias)                              differentiable
     y = selective_scan(u, delta, A, B, C, D, z, delta_bias)       differentiable
+    q, k = rotary(q, k, inv_freq)                                 differentiable
+    q, k = norm_rotary(q, k, q_weight, k_weight, inv_freq)        differentiable
+    o = linear_attention(q, k, v, log_decay, scale)               differentiable but in log_decay
 
 with `state=` / `return_state=True` for a row that continues an earlier one, and for one node at a time
 
     y = causal_conv_step(x, window, weight, bias)                 window moved on in place
     y = selective_scan_step(state, u, delta, A, B, C, D, z, ...)  state moved on in place
+    o = linear_attention_step(state, q, k, v, log_decay, scale)   state moved on in place
+
+A row that continues gives the rotation its first node's position: `offset=`, or `positions=` for each row its own.
 
 `*_fwd` / `*_bwd` are the same calls without autograd.  The single-node forms are not differentiable either:
 they compute values, and a backward pass that reaches their result raises.  Activations are fp32, bf16 or fp16 CUDA tensors
-of one type whose channel axis is contiguous (slices of a wider projection are read in place);
-parameters and scan states are fp32.  Everything runs in libfpde.so on torch's current stream; torch
+of one type whose channel or feature axis is contiguous (slices of a wider projection are read in place);
+parameters, frequencies and states are fp32.  Everything runs in libfpde.so on torch's current stream; torch
 allocates the outputs and the scratch memory.  There is no CPU path.
 """
 from __future__ import annotations
 
 import ctypes
+import math
 from typing import NamedTuple, Optional
 
 import torch
@@ -31,6 +40,20 @@ class ConvGrads(NamedTuple):
     x: torch.Tensor
     weight: torch.Tensor
     bias: Optional[torch.Tensor]
+    state: Optional[torch.Tensor]
+
+
+class HeadGrads(NamedTuple):
+    q: torch.Tensor
+    k: Optional[torch.Tensor]
+    q_weight: Optional[torch.Tensor]
+    k_weight: Optional[torch.Tensor]
+
+
+class LinearGrads(NamedTuple):
+    q: torch.Tensor
+    k: torch.Tensor
+    v: torch.Tensor
     state: Optional[torch.Tensor]
 
 
@@ -369,3 +392,290 @@ def selective_scan(u, delta, A, B, C, D=None, z=None, delta_bias=None, delta_sof
     keep = wants_grad(u, delta, A, B, C, D, z, delta_bias, state)
     out, last = _SelectiveScan.apply(u, delta, A, B, C, D, z, delta_bias, delta_softplus, state, keep)
     return (out, last) if return_state else out
+
+
+# ---------------------------------------------------------------------------------- heads and positions
+def rotary_frequencies(pairs, base=10000.0, stretch=1.0, length=None, fast=32.0, slow=1.0, device="cuda"):
+    """inv_freq (pairs) fp32: pair i turns by base^(-i / pairs) a node, for rows `stretch` times as long as those that a
+    network was trained on divided by `stretch`.  With `length`, the nodes of a row in training, pairs that turn more
+    than `fast` times over such a row keep their frequency, those under `slow` times are divided, and those between
+    are blended."""
+    if pairs < 1 or not base > 0 or not stretch > 0 or not 0 < slow < fast:
+        raise ValueError("expected pairs >= 1, base > 0, stretch > 0 and 0 < slow < fast")
+    freq = base ** (-torch.arange(pairs, dtype=torch.float64) / pairs)
+    keep = torch.zeros_like(freq)
+    if length is not None:
+        keep = ((length * freq / (2 * math.pi) - slow) / (fast - slow)).clamp(0, 1)
+    return (freq * (keep + (1 - keep) / stretch)).to(device=device, dtype=torch.float32)
+
+
+def _heads(a, name, t, dim, dt, dev):
+    """A (batch, length, heads, dim) view as the call takes it; its strides go into the argument block."""
+    if t.dim() != 4:
+        raise ValueError("%s has %d axes, expected 4 (batch, length, heads, features)" % (name, t.dim()))
+    t = _activation(name, t, (a.batch, a.length, t.shape[2], dim), dt, dev)
+    setattr(a, name + "_batch", t.stride(0))
+    setattr(a, name + "_node", t.stride(1))
+    setattr(a, name + "_head", t.stride(2))
+    return t
+
+
+def _head_args(norm, q, k, q_weight, k_weight, inv_freq, positions, offset, interleaved, eps, gq=None, gk=None):
+    """As _conv_args, for a rotation or norm; without norm the gradients come with gq and gk in the place of q and k."""
+    _first("q", q, 4)
+    dev, dt, dim = q.device, q.dtype, q.shape[3]
+    a = B_.HeadArgs(dtype=B_.DTYPE_IDS[str(dt)], norm=int(norm), interleaved=int(interleaved), batch=q.shape[0], length=q.shape[1], q_heads=q.shape[2],
+                    k_heads=0 if k is None else k.shape[2], dim=dim, offset=offset, eps=eps)
+    if inv_freq is not None:
+        if inv_freq.dim() != 1:
+            raise ValueError("inv_freq has %d axes, expected 1 (pairs)" % inv_freq.dim())
+        inv_freq = _dense("inv_freq", inv_freq, inv_freq.shape, torch.float32, dev)
+        a.pairs = inv_freq.shape[0]
+        if 2 * a.pairs > dim:
+            raise ValueError("%d pairs do not fit %d features" % (a.pairs, dim))
+    if positions is not None:
+        if positions.shape != q.shape[:2] or positions.dtype != torch.int64 or positions.device != dev:
+            raise ValueError("positions are %s %s on %s, expected int64 %s on %s" % (positions.dtype, tuple(positions.shape), positions.device,
+                                                                                    tuple(q.shape[:2]), dev))
+        a.pos_batch, a.pos_node = positions.stride()
+    q_weight = _dense("q_weight", q_weight, (dim,), torch.float32, dev)
+    k_weight = _dense("k_weight", k_weight, (dim,), torch.float32, dev)
+    q = _heads(a, "q", q, dim, dt, dev)
+    k = None if k is None else _heads(a, "k", k, dim, dt, dev)
+    if gq is not None:
+        if gq.shape != q.shape or (gk is None) != (k is None) or (gk is not None and gk.shape != k.shape):
+            raise ValueError("gq and gk need the shapes of q and k")
+        gq = _heads(a, "gq", gq, dim, dt, dev)
+        gk = None if gk is None else _heads(a, "gk", gk, dim, dt, dev)
+        a.workspace_bytes = B_.lib().fpde_head_rotary_workspace_bytes(ctypes.byref(a))
+    return a, (q, k, q_weight, k_weight, inv_freq, positions, gq, gk)
+
+
+def _head_plan(kind, norm, q, k, q_weight, k_weight, inv_freq, positions, offset, interleaved, eps, gq=None, gk=None):
+    key = (kind, offset, bool(interleaved), eps, _lay(q), _lay(k), _lay(q_weight), _lay(k_weight), _lay(inv_freq), _lay(positions), _lay(gq), _lay(gk))
+    t = (q, k, q_weight, k_weight, inv_freq, positions, gq, gk)
+    a = _plans.get(key)
+    if a is None:
+        a, taken = _head_args(norm, *t[:6], offset, interleaved, eps, gq, gk)
+        if _same(t, taken):
+            _plans.keep(key, a)
+        t = taken
+    a.inv_freq, a.positions = _ptr(t[4]), _ptr(t[5])
+    return a, t
+
+
+def _head_fwd(kind, norm, q, k, q_weight, k_weight, inv_freq, positions, offset, interleaved, eps):
+    a, t = _head_plan(kind, norm, q, k, q_weight, k_weight, inv_freq, positions, offset, interleaved, eps)
+    out_q, out_k = _new(q), _new(k)
+    a.q, a.k, a.q_weight, a.k_weight = t[0].data_ptr(), _ptr(t[1]), _ptr(t[2]), _ptr(t[3])
+    a.q_out, a.k_out = out_q.data_ptr(), _ptr(out_k)
+    B_.call_with("fpde_head_rotary_fwd", a, q.device.index)
+    return out_q, out_k
+
+
+def rotary_fwd(q, k, inv_freq, positions=None, offset=0, interleaved=False):
+    """q (batch, length, heads, dim) and k (batch, length, k_heads, dim), or None, with the first 2 * len(inv_freq) features
+    of each head turned: pair i, which is (x[i], x[i + pairs]), or interleaved (x[2i], x[2i + 1]), by the angle
+    position * inv_freq[i].  The position is offset + t, or offset + positions[b, t] (int64)."""
+    return _head_fwd("rotary fwd", False, q, k, None, None, inv_freq, positions, offset, interleaved, 0.0)
+
+
+def rotary_bwd(gq, gk, inv_freq, positions=None, offset=0, interleaved=False):
+    """Gradients of rotary_fwd in q and k, for upstream gradients gq and gk (or None): turned back."""
+    a, t = _head_plan("rotary bwd", False, gq, gk, None, None, inv_freq, positions, offset, interleaved, 0.0)
+    out_q, out_k = _new(gq), _new(gk)
+    a.gq, a.gq_batch, a.gq_node, a.gq_head = t[0].data_ptr(), a.q_batch, a.q_node, a.q_head
+    a.gk, a.gk_batch, a.gk_node, a.gk_head = _ptr(t[1]), a.k_batch, a.k_node, a.k_head
+    a.gx_q, a.gx_k = out_q.data_ptr(), _ptr(out_k)
+    B_.call_with("fpde_head_rotary_bwd", a, gq.device.index)
+    return out_q, out_k
+
+
+def norm_rotary_fwd(q, k, q_weight=None, k_weight=None, inv_freq=None, positions=None, offset=0, interleaved=False, eps=1e-6):
+    """rotary_fwd of x / sqrt(mean(x^2) + eps) * weight, the mean over each head's features; without inv_freq the norm
+    alone.  q_weight, k_weight: (dim), or None for ones."""
+    return _head_fwd("norm fwd", True, q, k, q_weight, k_weight, inv_freq, positions, offset, interleaved, eps)
+
+
+def norm_rotary_bwd(gq, gk, q, k, q_weight=None, k_weight=None, inv_freq=None, positions=None, offset=0, interleaved=False, eps=1e-6) -> HeadGrads:
+    """Gradients of norm_rotary_fwd for upstream gradients gq and gk."""
+    a, t = _head_plan("norm bwd", True, q, k, q_weight, k_weight, inv_freq, positions, offset, interleaved, eps, gq, gk)
+    g = HeadGrads(_new(q), _new(k), _new(q_weight), _new(k_weight))
+    ws = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=q.device)
+    a.q, a.k, a.q_weight, a.k_weight = t[0].data_ptr(), _ptr(t[1]), _ptr(t[2]), _ptr(t[3])
+    a.gq, a.gk, a.gx_q, a.gx_k = t[6].data_ptr(), _ptr(t[7]), g.q.data_ptr(), _ptr(g.k)
+    a.gq_weight, a.gk_weight, a.workspace = _ptr(g.q_weight), _ptr(g.k_weight), ws.data_ptr()
+    B_.call_with("fpde_head_rotary_bwd", a, q.device.index)
+    return g
+
+
+class _Rotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, inv_freq, positions, offset, interleaved):
+        ctx.save_for_backward(inv_freq, positions)
+        ctx.how = (offset, interleaved)
+        ctx.like = (q.shape, None if k is None else k.shape, q.dtype, q.device)
+        ctx.set_materialize_grads(False)
+        return rotary_fwd(q, k, inv_freq, positions, offset, interleaved)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, gq, gk):
+        inv_freq, positions = ctx.saved_tensors
+        q_shape, k_shape, dt, dev = ctx.like
+        if gq is None:
+            gq = torch.zeros(q_shape, dtype=dt, device=dev)
+        if gk is None and k_shape is not None:
+            gk = torch.zeros(k_shape, dtype=dt, device=dev)
+        return rotary_bwd(gq, gk, inv_freq, positions, *ctx.how) + (None, None, None, None)
+
+
+class _NormRotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, inv_freq, positions, offset, interleaved, eps):
+        ctx.save_for_backward(q, k, q_weight, k_weight, inv_freq, positions)
+        ctx.how = (offset, interleaved, eps)
+        ctx.set_materialize_grads(False)
+        return norm_rotary_fwd(q, k, q_weight, k_weight, inv_freq, positions, offset, interleaved, eps)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, gq, gk):
+        q, k = ctx.saved_tensors[:2]
+        gq = torch.zeros_like(q) if gq is None else gq
+        gk = torch.zeros_like(k) if gk is None and k is not None else gk
+        return tuple(norm_rotary_bwd(gq, gk, *ctx.saved_tensors, *ctx.how)) + (None,) * 5
+
+
+def _no_gradient(name, t):
+    if wants_grad(t):
+        raise ValueError("%s has no gradient: detach it" % name)
+
+
+def rotary(q, k, inv_freq, positions=None, offset=0, interleaved=False):
+    """rotary_fwd, differentiable in q and k."""
+    _no_gradient("inv_freq", inv_freq)
+    return _Rotary.apply(q, k, inv_freq, positions, offset, interleaved)
+
+
+def norm_rotary(q, k, q_weight=None, k_weight=None, inv_freq=None, positions=None, offset=0, interleaved=False, eps=1e-6):
+    """norm_rotary_fwd, differentiable in q, k and the weights."""
+    _no_gradient("inv_freq", inv_freq)
+    return _NormRotary.apply(q, k, q_weight, k_weight, inv_freq, positions, offset, interleaved, eps)
+
+
+# --------------------------------------------------------------------------------- linear attention
+def _linear_args(q, k, v, log_decay, scale, state, step, go=None, gstate=None, backward=False):
+    """As _conv_args, for linear attention."""
+    _first("q", q, 3 if step else 4)
+    dev, dt, batch, heads, dk = q.device, q.dtype, q.shape[0], q.shape[-2], q.shape[-1]
+    if v.dim() != q.dim():
+        raise ValueError("v has %d axes, expected %d" % (v.dim(), q.dim()))
+    dv = v.shape[-1]
+    a = B_.LinearArgs(dtype=B_.DTYPE_IDS[str(dt)], batch=batch, length=1 if step else q.shape[1], heads=heads, dk=dk, dv=dv, scale=scale)
+
+    def view(name, t, like, width):
+        t = _activation(name, t, like.shape[:-1] + (width,), dt, dev)
+        setattr(a, name + "_batch", t.stride(0))
+        setattr(a, name + "_node", 0 if step else t.stride(1))
+        setattr(a, name + "_head", t.stride(-2))
+        return t
+    q, k, v = view("q", q, q, dk), view("k", k, q, dk), view("v", v, q, dv)
+    log_decay = _dense("log_decay", log_decay, (heads,), torch.float32, dev)
+    rest = (batch, heads, dk, dv)
+    if step:
+        _activation("state", state, rest, torch.float32, dev)
+        if not state.is_contiguous():
+            raise ValueError("state is updated in place and must be contiguous")
+    else:
+        state = _dense("state", state, rest, torch.float32, dev)
+        if backward:
+            go = view("go", go, q, dv)
+            gstate = _dense("gstate", gstate, rest, torch.float32, dev)
+        a.workspace_bytes = B_.lib().fpde_linear_attention_workspace_bytes(ctypes.byref(a), int(backward))
+    return a, (q, k, v, log_decay, state, go, gstate)
+
+
+def _linear_plan(kind, q, k, v, log_decay, scale, state, go=None, gstate=None):
+    key = (kind, scale, _lay(q), _lay(k), _lay(v), _lay(log_decay), _lay(state), _lay(go), _lay(gstate))
+    t = (q, k, v, log_decay, state, go, gstate)
+    a = _plans.get(key)
+    if a is None:
+        a, taken = _linear_args(q, k, v, log_decay, scale, state, kind == "linear step", go, gstate, kind == "linear bwd")
+        if _same(t, taken):
+            _plans.keep(key, a)
+        t = taken
+    a.q, a.k, a.v, a.log_decay, a.state = t[0].data_ptr(), t[1].data_ptr(), t[2].data_ptr(), t[3].data_ptr(), _ptr(t[4])
+    return a, t
+
+
+def linear_attention_fwd(q, k, v, log_decay, scale=1.0, state=None):
+    """For every row and head, with g = exp(log_decay[head]):
+
+        S[t] = g S[t-1] + k[t] v[t]^T,  o[t] = scale * q[t] S[t],  S[-1] = state (batch, heads, dk, dv) or zeros
+
+    q and k: (batch, length, heads, dk), v: (batch, length, heads, dv), up to 128 features each; log_decay: (heads).
+    Returns (o (batch, length, heads, dv), the last state)."""
+    a, t = _linear_plan("linear fwd", q, k, v, log_decay, scale, state)
+    dev = q.device
+    o = _new(v)
+    last = torch.empty((a.batch, a.heads, a.dk, a.dv), dtype=torch.float32, device=dev) if state is None else _new(state)
+    a.o, a.state_out = o.data_ptr(), last.data_ptr()
+    if a.workspace_bytes:
+        ws = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=dev)
+        a.workspace = ws.data_ptr()
+    B_.call_with("fpde_linear_attention_fwd", a, dev.index)
+    return o, last
+
+
+def linear_attention_bwd(go, q, k, v, log_decay, scale=1.0, state=None, gstate=None) -> LinearGrads:
+    """Gradients of linear_attention_fwd for upstream gradients go of `o` and `gstate` of the last state."""
+    a, t = _linear_plan("linear bwd", q, k, v, log_decay, scale, state, go, gstate)
+    dev = q.device
+    g = LinearGrads(_new(q), _new(k), _new(v), _new(state))
+    a.go, a.gstate_out = t[5].data_ptr(), _ptr(t[6])
+    a.gq, a.gk, a.gv, a.gstate = g.q.data_ptr(), g.k.data_ptr(), g.v.data_ptr(), _ptr(g.state)
+    if a.workspace_bytes:
+        ws = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=dev)
+        a.workspace = ws.data_ptr()
+    B_.call_with("fpde_linear_attention_bwd", a, dev.index)
+    return g
+
+
+def linear_attention_step(state, q, k, v, log_decay, scale=1.0):
+    """One node per row: q, k (batch, heads, dk), v (batch, heads, dv) -> o (batch, heads, dv); `state`
+    (batch, heads, dk, dv) is moved on in place.  Not differentiable."""
+    if torch.is_grad_enabled() and wants_grad(state, q, k, v, log_decay):
+        return ValuesOnly.apply(linear_attention_step, state, q, k, v, log_decay, scale)
+    a, t = _linear_plan("linear step", q, k, v, log_decay, scale, state)
+    o = _new(v)
+    a.state_out, a.o = state.data_ptr(), o.data_ptr()
+    B_.call_with("fpde_linear_attention_step", a, q.device.index)
+    _moved_on(state)
+    return o
+
+
+class _LinearAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, log_decay, scale, state):
+        o, last = linear_attention_fwd(q, k, v, log_decay, scale, state)
+        ctx.save_for_backward(q, k, v, log_decay, state)
+        ctx.scale = scale
+        ctx.set_materialize_grads(False)
+        return o, last
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, go, glast):
+        q, k, v, log_decay, state = ctx.saved_tensors
+        if go is None:
+            go = torch.zeros_like(v)
+        g = linear_attention_bwd(go, q, k, v, log_decay, ctx.scale, state, glast)
+        return g.q, g.k, g.v, None, None, g.state
+
+
+def linear_attention(q, k, v, log_decay, scale=1.0, state=None, return_state=False):
+    """linear_attention_fwd, differentiable in q, k, v and state; log_decay is a constant of the layer."""
+    _no_gradient("log_decay", log_decay)
+    o, last = _LinearAttention.apply(q, k, v, log_decay, scale, state)
+    return (o, last) if return_state else o
