@@ -654,6 +654,9 @@ int fpde_linear_attention_fwd(const fpde_linear_args* args, void* stream);
 int fpde_linear_attention_bwd(const fpde_linear_args* args, void* stream);
 /* One node per row (length is taken as 1): `state_out` may be (and usually is) `state` itself. */
 int fpde_linear_attention_step(const fpde_linear_args* args, void* stream);
+/* Bounded waits inside linear attention's products that gave up since the library was loaded (0 in a healthy run; see
+ * fpde_diag_tma_timeouts).  The results of a piece of a row that lost one are NaN. */
+unsigned int fpde_diag_linear_timeouts(void);
 
 /*
  * Orthogonalised update of a stack of `count` matrices (count, rows, cols):

@@ -631,6 +631,11 @@ def diag_ortho_timeouts() -> int:
     return int(lib().fpde_diag_ortho_timeouts())
 
 
+def diag_linear_timeouts() -> int:
+    """Bounded waits of linear attention's products that gave up (0 in a healthy run)."""
+    return int(lib().fpde_diag_linear_timeouts())
+
+
 @functools.lru_cache(maxsize=None)
 def _entry(name: str):
     import torch

@@ -11,39 +11,12 @@
 //   gq: (go, v, k) from state^T, the same
 //   gk: (v, go, q) from the last node to the first, from gstate^T, near = gain = scale, far = 1, shift = 1
 //   gv: (k, q, go) likewise from gstate; its last state is the gradient of the first one
-#include "seq_common.cuh"
+#include "seq_linear.cuh"
 
 namespace fpde {
 namespace {
 
-struct LinearView {
-    const void* p;
-    int64_t batch, node, head;
-};
-
-// A march over all rows and heads.
-struct March {
-    LinearView a, b, c;
-    int64_t batch, length, heads;
-    int da, dc;                    // features of a and b, and of c
-    int reversed;                  // from the last node to the first
-    int shift;
-    float near, far, gain;
-    const float* log_decay;
-    const float* start;            // (batch, heads, da, dc), or turned: (batch, heads, dc, da); NULL: zeros
-    int start_turned;
-    void* out;                     // (batch, length, heads, dc) dense
-    float* end;                    // (batch, heads, da, dc), or NULL
-    // pieces of a row: states at their starts in `local` (batch, heads, pieces, da, dc)
-    int pieces;
-    int64_t piece;                 // nodes of a piece
-    float* local;
-};
-
 constexpr int C = 32, THREADS = 128;
-
-// g^n for n >= 0, from 64 bits: rounded once, so that it stays exact enough when it is applied chunk after chunk.
-__device__ __forceinline__ double power(float log_decay, double n) { return n == 0. ? 1. : exp((double)log_decay * n); }
 
 template <int DA, int DC>
 struct Sizes {
@@ -210,7 +183,7 @@ __global__ void __launch_bounds__(THREADS) march_kernel(March m) {
     }
 }
 
-// What each piece leaves becomes the state that each starts from.
+// Eight pieces at a time, so that their loads are on their way together.
 __global__ void __launch_bounds__(256) join_kernel(March m) {
     pdl_wait_then_trigger();
     const int64_t size = (int64_t)m.da * m.dc, across = (size + 255) / 256;
@@ -219,12 +192,19 @@ __global__ void __launch_bounds__(256) join_kernel(March m) {
     const double g = power(m.log_decay[row % m.heads], (double)m.piece);
     const float hi = (float)g, lo = (float)(g - hi);
     float s = 0.f;
-    if (m.start != nullptr) s = m.start_turned ? m.start[row * size + i % m.dc * m.da + i / m.dc] : m.start[row * size + i];
+    // element (d, c) of the state
+    const int64_t d = m.local_turned ? i % m.da : i / m.dc, c = m.local_turned ? i / m.da : i % m.dc;
+    if (m.start != nullptr) s = m.start[row * size + (m.start_turned ? c * m.da + d : d * m.dc + c)];
     float* at = m.local + row * m.pieces * size + i;
-    for (int p = 0; p < m.pieces; ++p, at += size) {
-        const float u = *at;
-        *at = s;
-        s = fmaf(hi, s, fmaf(lo, s, u));
+    for (int p = 0; p < m.pieces; p += 8, at += 8 * size) {
+        float u[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[e] = p + e < m.pieces ? at[e * size] : 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (p + e < m.pieces) at[e * size] = s;
+            s = fmaf(hi, s, fmaf(lo, s, u[e]));
+        }
     }
 }
 
@@ -306,15 +286,30 @@ int check_linear(const fpde_linear_args* a, bool step) {
     return FPDE_OK;
 }
 
-// Pieces of a row: enough blocks to fill the GPU, none shorter than 4 chunks.
-void cut(March& m) {
-    const int64_t rows = m.batch * m.heads * ceil_div(m.dc, 64), chunks = ceil_div(m.length, C);
-    int64_t pieces = rows >= 148 * 2 ? 1 : ceil_div(148 * 4, rows > 0 ? rows : 1);
-    if (pieces > chunks / 4) pieces = chunks / 4;
-    if (pieces < 1) pieces = 1;
-    const int64_t each = ceil_div(chunks, pieces);
-    m.piece = (each > 0 ? each : 1) * C;
-    m.pieces = (int)ceil_div(chunks > 0 ? chunks : 1, each > 0 ? each : 1);
+// Rows of up to 64 nodes fill less than half of a chunk there.
+bool on_tensor_cores(const fpde_linear_args* a) { return a->dtype == FPDE_BF16 && a->length > 64; }
+
+// Pieces of a row.  With more than one every piece is marched through twice, the first time for its end alone (ENDS of the
+// time); a block's start costs as much as START chunks.  The number that takes the fewest waves of chunks is taken.
+void cut(const fpde_linear_args* a, March& m) {
+    const bool mma = on_tensor_cores(a);
+    const int chunk = mma ? MMA_CHUNK : C;
+    const double ends = 0.5, start = 1.;
+    const int64_t rows = m.batch * m.heads * (mma ? 1 : ceil_div(m.dc, 64)), slots = mma ? march_mma_blocks(m) : 148 * 4, chunks = ceil_div(m.length, chunk);
+    int64_t best = 1;
+    double least = 1e300;
+    for (int64_t p = 1; p <= chunks && p <= 1024 && rows * (p - 1) < 8 * slots; ++p) {
+        const int64_t each = ceil_div(chunks, p);
+        if (ceil_div(chunks, each) != p) continue;
+        const double waves = (double)ceil_div(rows * p, slots), time = waves * (p > 1 ? (start + each) * (1. + ends) + 2. : start + each);
+        if (time < least) {
+            least = time;
+            best = p;
+        }
+    }
+    const int64_t each = chunks > 0 ? ceil_div(chunks, best) : 1;
+    m.piece = each * chunk;
+    m.pieces = (int)best;
 }
 
 size_t local_bytes(const March& m) { return m.pieces > 1 ? (size_t)m.batch * m.heads * m.pieces * m.da * m.dc * sizeof(float) : 0; }
@@ -340,7 +335,7 @@ March march_o(const fpde_linear_args* a) {
     m.start = a->state;
     m.out = a->o;
     m.end = a->state_out;
-    cut(m);
+    cut(a, m);
     return m;
 }
 March march_gq(const fpde_linear_args* a) {
@@ -355,7 +350,7 @@ March march_gq(const fpde_linear_args* a) {
     m.start = a->state;
     m.start_turned = 1;
     m.out = a->gq;
-    cut(m);
+    cut(a, m);
     return m;
 }
 March march_gk(const fpde_linear_args* a) {
@@ -371,7 +366,7 @@ March march_gk(const fpde_linear_args* a) {
     m.start = a->gstate_out;
     m.start_turned = 1;
     m.out = a->gk;
-    cut(m);
+    cut(a, m);
     return m;
 }
 March march_gv(const fpde_linear_args* a) {
@@ -387,7 +382,7 @@ March march_gv(const fpde_linear_args* a) {
     m.start = a->gstate_out;
     m.out = a->gv;
     m.end = a->gstate;
-    cut(m);
+    cut(a, m);
     return m;
 }
 
@@ -406,9 +401,7 @@ cudaError_t march_launch(const March& m, cudaStream_t st) {
         static std::atomic<uint64_t> done{0};
         FPDE_TRY(allow_smem(march_kernel<T, DA, DC, true>, bytes, done));
         FPDE_TRY(launch_kernel_smem(march_kernel<T, DA, DC, true>, dim3((unsigned)blocks), dim3(THREADS), bytes, st, m));
-        const int64_t joins = m.batch * m.heads * ceil_div((int64_t)m.da * m.dc, 256);
-        if (joins > 0x7fffffff) return cudaErrorInvalidConfiguration;
-        FPDE_TRY(launch_kernel(join_kernel, dim3((unsigned)joins), dim3(256), st, m));
+        FPDE_TRY(march_join(m, st));
     }
     static std::atomic<uint64_t> done{0};
     FPDE_TRY(allow_smem(march_kernel<T, DA, DC, false>, bytes, done));
@@ -422,6 +415,8 @@ cudaError_t march_run(const March& m, cudaStream_t st) {
 }
 
 cudaError_t march_by_type(const fpde_linear_args* a, const March& m, cudaStream_t st) {
+    cudaError_t e;
+    if (on_tensor_cores(a) && march_mma(m, st, &e)) return e;
     if (a->dtype == FPDE_F32) return march_run<float>(m, st);
     if (a->dtype == FPDE_BF16) return march_run<__nv_bfloat16>(m, st);
     return march_run<__half>(m, st);
@@ -445,6 +440,13 @@ cudaError_t step_run(const fpde_linear_args* a, cudaStream_t st) {
 int as_status(cudaError_t e) { return e == cudaSuccess ? FPDE_OK : FPDE_ERR_CUDA; }
 
 }  // namespace
+
+cudaError_t march_join(const March& m, cudaStream_t st) {
+    const int64_t blocks = m.batch * m.heads * ceil_div((int64_t)m.da * m.dc, 256);
+    if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    return launch_kernel(join_kernel, dim3((unsigned)blocks), dim3(256), st, m);
+}
+
 }  // namespace fpde
 
 using namespace fpde;
@@ -497,5 +499,7 @@ int fpde_linear_attention_step(const fpde_linear_args* a, void* stream) {
     if (a->dtype == FPDE_BF16) return as_status(step_run<__nv_bfloat16>(a, s));
     return as_status(step_run<__half>(a, s));
 }
+
+unsigned int fpde_diag_linear_timeouts(void) { return march_mma_timeouts(); }
 
 }  // extern "C"

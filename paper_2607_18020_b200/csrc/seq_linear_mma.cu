@@ -1,0 +1,521 @@
+// Linear attention's march on the tensor cores, for bf16 arrays with up to 128 features.
+//
+// A block marches one row and head, or a piece of it, in chunks of 128 nodes.  The chunk's a, b and c lie in shared memory as
+// they come (rows of nodes, 64-feature blocks, 128-byte swizzle), zeros where there is no node or feature.  Products of a chunk:
+//   G = a b^T        128 x 128, both factors K-major
+//   far = a S        S, the state before the chunk, in shared memory, MN-major
+//   U = bw^T c       what the chunk adds to the state; bw = b with the decays to the chunk's end, MN-major
+//   near = P c       P = G with the decays between the nodes, as left factor in TMEM; c MN-major
+// Sums are fp32 in TMEM.  out = near + g^(i+1-shift) far, S <- g^128 S + U in fp32 registers.  A march from the last node to the
+// first takes the same tiles with their rows in the arrays' order: the masks and the decays are turned round instead.
+//
+// Roundings to fewer bits.  P and the S that `far` reads are single bf16 factors: each moves a bf16 result by about as much as
+// its own rounding, and nothing else.  The state itself stays fp32: bw is three bf16 parts that hold all 24 bits of b times its
+// decay, c is exact, U is formed of three products and the state is added up with ordinary rounding.
+//
+// Threads.  Eight warps, two threads for each of the 128 lanes of TMEM with half of the columns each, and one thread that loads (TMA)
+// and issues the products.  G and far run while all turn b into bw, U while G becomes P, and a tile's place takes the next chunk's
+// as soon as the products that read it are done: a and b after far, c after near.
+#include "mma_common.cuh"
+#include "seq_linear.cuh"
+
+namespace fpde {
+namespace {
+
+constexpr int N = MMA_CHUNK, WARPS = 8, THREADS = 32 * (WARPS + 1);
+constexpr int BLOCK = N * 128;                 // bytes of 64 features of a chunk
+constexpr int PARTS = 3;
+constexpr int TRIES = 1 << 20;                 // of a wait (for microseconds, in a healthy run); 20 ms at the very least
+
+__device__ unsigned int g_linear_timeouts;
+
+template <int DA, int DC>
+struct Room {
+    static constexpr int A = 0, B = A + DA / 64 * BLOCK, V = B + DA / 64 * BLOCK, BW = V + DC / 64 * BLOCK, S = BW + PARTS * (DA / 64) * BLOCK;
+    static constexpr int BYTES = S + DC / 64 * DA * 128 + 1024;      // slack to start on 1024 bytes
+    // columns of TMEM.  P takes the first and the last 32 of G, which their own readers have read before; with 64 columns of c near
+    // lies between them, so that two blocks fit an SM
+    static constexpr int G = 0, NEAR = DC == 64 ? 32 : 128, FAR = DC == 64 ? 128 : 256, U = DC == 64 ? 192 : 384, COLUMNS = DC == 64 ? 256 : 512;
+};
+__host__ __device__ constexpr int p_column(int k) { return k < 4 ? 8 * k : 96 + 8 * (k - 4); }      // of 16 nodes' products
+
+// Barriers.  FULL: the tiles have arrived; DONE: products are; READY: the compute warps have written what the next products read.
+enum Bar { FULL_AB, FULL_C, DONE_G, DONE_U, DONE_OUT, READY_BW, READY_P, READY, ENDED, BARS };
+
+__device__ __forceinline__ void sts16(uint32_t to, uint4 v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ uint4 lds16(uint32_t from) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(from) : "memory");
+    return v;
+}
+// Where row r's 8 features from 8 * q on lie in an array of `rows` rows.
+__device__ __forceinline__ uint32_t chunk_at(uint32_t base, int r, int q, int rows = N) { return base + (q / 8) * rows * 128 + r * 128 + ((q % 8) ^ (r & 7)) * 16; }
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// D += A B with A in TMEM: 16 bf16 of each row, two a column.
+__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(r[0]), "r"(r[1]),
+        "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
+        "r"(r[15]), "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t tmem_load1(uint32_t addr) {
+    uint32_t r;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+    return r;
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// 64 features of a tile's 128 nodes; what the map does not hold becomes zeros.
+__device__ __forceinline__ void load_tile(uint32_t to, const CUtensorMap* map, int feature, int head, int node, int batch, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(to), "l"(map),
+                 "r"(feature), "r"(head), "r"(node), "r"(batch), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void store32(void* to, const uint32_t (&v)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]),
+                 "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
+
+__device__ __forceinline__ float top_part(float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); }
+__device__ __forceinline__ uint32_t tops(float lo, float hi) { return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632); }
+
+struct Tiles {
+    CUtensorMap a, b, c;                       // (features, heads, nodes, batch)
+    int head_a, head_b, head_c, batch_a, batch_b, batch_c;      // 0: one for all
+};
+
+// ENDS: only the state that each piece leaves, from zero.
+template <int DA, int DC, bool ENDS>
+__global__ void __launch_bounds__(THREADS, DC == 64 && DA == 64 ? 2 : 1) march_mma_kernel(const __grid_constant__ March m, const __grid_constant__ Tiles tiles) {
+    using R = Room<DA, DC>;
+    extern __shared__ uint8_t raw[];
+    __shared__ __align__(8) uint64_t bars[BARS];
+    __shared__ uint32_t tmem_slot;
+    __shared__ __align__(16) float powers[N + 2];
+    __shared__ __align__(16) float near_end[32];                 // g^(31 - k)
+    __shared__ float whole[4];                                   // g^128 and that of the last chunk, each in two parts
+    const uint32_t base = (smem_u32(raw) + 1023) & ~1023u;
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, half = warp / 4, quarter = warp % 4;
+    auto bar = [&](int i) { return smem_u32(&bars[i]); };
+    if (tid == 0) {
+        for (int i = 0; i < BARS; ++i) mbar_init(bar(i), i == READY_BW || i == READY_P || i == READY ? WARPS : 1);
+        mbar_fence_init();
+    }
+    if (warp == WARPS) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "n"(R::COLUMNS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    pdl_wait_then_trigger();
+
+    int64_t id = blockIdx.x;
+    const int p = (int)(id % m.pieces);
+    id /= m.pieces;
+    const int64_t h = id % m.heads, bt = id / m.heads;
+    const float ld = m.log_decay[h];
+    const int64_t first = p * m.piece, last = min(m.length, first + m.piece);
+    const int tail = last > first ? (int)((last - first - 1) % N) + 1 : 0;
+    if (tid < N + 2) {
+        const float g = (float)power(ld, tid);
+        powers[tid] = g;
+        if (tid < 32) near_end[31 - tid] = g;
+    }
+    if (tid >= 192 && tid < 194) {
+        const double g = power(ld, tid == 192 ? N : tail);
+        whole[2 * (tid - 192)] = (float)g;
+        whole[2 * (tid - 192) + 1] = (float)(g - (float)g);
+    }
+
+    // The state: row d, columns half * DC / 2 and on.  With 64 rows the products use 16 lanes of each quarter.
+    constexpr int COLS = DC / 2;
+    const bool holds = warp < WARPS && (DA == 128 || lane < 16);
+    const int d = DA == 128 ? quarter * 32 + lane : quarter * 16 + lane, col0 = half * COLS;
+    const int64_t st = (bt * m.heads + h) * m.da * m.dc;
+    float* local = m.local + ((bt * m.heads + h) * m.pieces + p) * m.da * m.dc;      // by columns: neighbouring lanes are neighbours there
+    float S[COLS];
+#pragma unroll
+    for (int c = 0; c < COLS; ++c) S[c] = 0.f;
+    if (!ENDS && holds && d < m.da) {
+        if (m.pieces > 1 || (m.start != nullptr && m.start_turned)) {
+            const float* from = m.pieces > 1 ? local : m.start + st;
+#pragma unroll
+            for (int c = 0; c < COLS; ++c)
+                if (col0 + c < m.dc) S[c] = from[(int64_t)(col0 + c) * m.da + d];
+        } else if (m.start != nullptr) {
+            const float* from = m.start + st + (int64_t)d * m.dc + col0;
+            if (m.dc % 4 == 0 && m.start_packed) {
+#pragma unroll
+                for (int c = 0; c < COLS; c += 4)
+                    if (col0 + c < m.dc) {
+                        const Pack<float, 4> v = load_pack<float, 4>(from + c);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) S[c + e] = v.v[e];
+                    }
+            } else {
+#pragma unroll
+                for (int c = 0; c < COLS; ++c)
+                    if (col0 + c < m.dc) S[c] = from[c];
+            }
+        }
+    }
+    auto put_state = [&]() {                   // the factor of `far`
+        if (ENDS || !holds) return;
+#pragma unroll
+        for (int q = 0; q < COLS / 8; ++q)
+            sts16(chunk_at(base + R::S, d, half * (COLS / 8) + q, DA),
+                  make_uint4(pack_bf16(S[8 * q], S[8 * q + 1]), pack_bf16(S[8 * q + 2], S[8 * q + 3]), pack_bf16(S[8 * q + 4], S[8 * q + 5]),
+                             pack_bf16(S[8 * q + 6], S[8 * q + 7])));
+    };
+    put_state();
+    fence_async();
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = tmem_slot;
+    uint32_t phase = 0;
+    bool gave_up = false;
+    auto wait = [&](int i) { mbar_wait<TRIES>(bar(i), phase, gave_up, &g_linear_timeouts); };
+    int loads_ab = 0, loads_c = 0;             // of the loading thread
+    if (warp == WARPS) {
+        if (lane == 0 && first < last) {
+            auto node_at = [&](int64_t t) { return (int)(m.reversed ? m.length - t - N : t); };
+            auto load_ab = [&](int64_t t) {
+                mbar_expect_tx(bar(FULL_AB), (ENDS ? 1 : 2) * (DA / 64) * BLOCK);
+#pragma unroll
+                for (int f = 0; f < DA / 64; ++f) {
+                    load_tile(base + R::B + f * BLOCK, &tiles.b, 64 * f, tiles.head_b * (int)h, node_at(t), tiles.batch_b * (int)bt, bar(FULL_AB));
+                    if (!ENDS) load_tile(base + R::A + f * BLOCK, &tiles.a, 64 * f, tiles.head_a * (int)h, node_at(t), tiles.batch_a * (int)bt, bar(FULL_AB));
+                }
+                ++loads_ab;
+            };
+            auto load_c = [&](int64_t t) {
+                mbar_expect_tx(bar(FULL_C), (DC / 64) * BLOCK);
+#pragma unroll
+                for (int f = 0; f < DC / 64; ++f)
+                    load_tile(base + R::V + f * BLOCK, &tiles.c, 64 * f, tiles.head_c * (int)h, node_at(t), tiles.batch_c * (int)bt, bar(FULL_C));
+                ++loads_c;
+            };
+            constexpr uint32_t IDESC = 1u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(128 / 16) << 24;      // fp32 sums of bf16 factors, 128 rows
+            constexpr uint32_t IDESC_G = IDESC | (uint32_t)(N / 8) << 17, IDESC_OUT = IDESC | 1u << 16 | (uint32_t)(DC / 8) << 17;
+            constexpr uint32_t IDESC_U = 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | (uint32_t)(DC / 8) << 17 | (uint32_t)(DA / 16) << 24;
+            const uint64_t da = slice_desc(base + R::A, false), db = slice_desc(base + R::B, false), dc = slice_desc(base + R::V, true, BLOCK),
+                           ds = slice_desc(base + R::S, true, DA * 128);
+            load_ab(first);
+            load_c(first);
+            for (int64_t t = first; t < last; t += N, phase ^= 1) {
+                const bool more = t + N < last;
+                if (!ENDS) {
+                    if (t > first) mbar_wait<TRIES>(bar(READY), phase ^ 1, gave_up, &g_linear_timeouts);
+                    wait(FULL_AB);
+                    if (gave_up) break;
+                    fence_after();
+#pragma unroll
+                    for (int k = 0; k < DA / 16; ++k)
+                        mma_f16(tmem + R::G, desc_at(da, k / 4 * BLOCK + k % 4 * 32), desc_at(db, k / 4 * BLOCK + k % 4 * 32), IDESC_G, k > 0);
+#pragma unroll
+                    for (int k = 0; k < DA / 16; ++k) mma_f16(tmem + R::FAR, desc_at(da, k / 4 * BLOCK + k % 4 * 32), desc_at(ds, k * 2048), IDESC_OUT, k > 0);
+                    mma_commit(bar(DONE_G));
+                }
+                wait(READY_BW);
+                wait(FULL_C);
+                if (gave_up) break;
+                fence_after();
+#pragma unroll
+                for (int s = PARTS - 1; s >= 0; --s) {         // the small parts first: the sum is rounded towards zero at every product
+                    const uint64_t dw = slice_desc(base + R::BW + s * (DA / 64) * BLOCK, true, BLOCK);
+#pragma unroll
+                    for (int k = 0; k < N / 16; ++k) mma_f16(tmem + R::U, desc_at(dw, k * 2048), desc_at(dc, k * 2048), IDESC_U, s < PARTS - 1 || k > 0);
+                }
+                mma_commit(bar(DONE_U));
+                if (!ENDS) wait(DONE_G);
+                if (gave_up) break;
+                if (more) load_ab(t + N);
+                if (!ENDS) {
+                    wait(READY_P);
+                    if (gave_up) break;
+                    fence_after();
+#pragma unroll
+                    for (int k = 0; k < N / 16; ++k) mma_tmem(tmem + R::NEAR, tmem + R::G + p_column(k), desc_at(dc, k * 2048), IDESC_OUT, k > 0);
+                    mma_commit(bar(DONE_OUT));
+                    if (more) wait(DONE_OUT);
+                } else if (more) {
+                    wait(DONE_U);
+                }
+                if (gave_up) break;
+                if (more) load_c(t + N);
+            }
+        }
+    } else {
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        const int row = quarter * 32 + lane, r = m.reversed ? N - 1 - row : row;      // of the tile, and in the march's order
+        const int64_t dir = m.reversed ? -1 : 1, origin = m.reversed ? m.length - 1 : 0;
+        auto signal = [&](int i) {
+            fence_async();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(i));
+        };
+        auto wait_warp = [&](int i) {
+            wait(i);
+            gave_up = __any_sync(~0u, gave_up);
+            fence_after();
+        };
+        for (int64_t t = first; t < last; t += N, phase ^= 1) {
+            const int n = (int)min((int64_t)N, last - t);
+            wait_warp(FULL_AB);
+            if (gave_up) break;
+            {                                      // bw: a row, half of its features
+                const float w = r < n ? m.gain * powers[n - 1 - r + m.shift] : 0.f;
+#pragma unroll
+                for (int q = half * (DA / 16), e = 0; e < DA / 16; ++e, ++q) {
+                    const uint4 v = lds16(chunk_at(base + R::B, row, q));
+                    const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+                    uint32_t out[PARTS][4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        float lo = __uint_as_float(in[k] << 16) * w, hi = __uint_as_float(in[k] & 0xffff0000u) * w;
+#pragma unroll
+                        for (int s = 0; s < PARTS; ++s) {      // the top 8 bits of what is left, exactly
+                            out[s][k] = tops(lo, hi);
+                            lo -= top_part(lo);
+                            hi -= top_part(hi);
+                        }
+                    }
+#pragma unroll
+                    for (int s = 0; s < PARTS; ++s)
+                        sts16(chunk_at(base + R::BW + s * (DA / 64) * BLOCK, row, q), make_uint4(out[s][0], out[s][1], out[s][2], out[s][3]));
+                }
+            }
+            signal(READY_BW);
+            if (!ENDS) {
+                wait_warp(DONE_G);
+                if (gave_up) break;
+                // P, 32 columns at a time: those of this quarter's own nodes are cut along the diagonal, those of the nodes before them
+                // are whole, the others zeros.  In the last half the last columns come first: P lies over G.
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int part = half == 0 ? e : 3 - e, before = m.reversed ? part - quarter : quarter - part;
+                    uint32_t packed[16] = {};
+                    if (before >= 0) {
+                        float v[32];
+                        tmem_load32(tmem + R::G + lanes + part * 32, v);
+                        if (before == 0) {
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) {
+                                const int back = m.reversed ? k - lane : lane - k;
+                                v[k] = back < 0 ? 0.f : v[k] * (m.near * powers[max(back, 0)]);
+                            }
+                        } else if (m.reversed) {             // column k: back = 32 before + k - lane = (32 before - 31 + 31 - lane) + k
+                            const float w = m.near * powers[32 * before - lane];
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) v[k] *= w * near_end[31 - k];
+                        } else {                             // back = 32 before + lane - k
+                            const float w = m.near * powers[32 * before + lane - 31];
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) v[k] *= w * near_end[k];
+                        }
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) packed[k] = pack_bf16(v[2 * k], v[2 * k + 1]);
+                    }
+                    tmem_store16(tmem + R::G + p_column(2 * part) + lanes, packed);
+                }
+                tmem_stored();
+                signal(READY_P);
+            }
+            wait_warp(DONE_U);
+            if (gave_up) break;
+            const float hi = whole[n == N ? 0 : 2], lo = whole[n == N ? 1 : 3];
+#pragma unroll
+            for (int c = 0; c < COLS; c += 32) {
+                float u[32];
+                tmem_load32(tmem + R::U + lanes + col0 + c, u);
+#pragma unroll
+                for (int k = 0; k < 32; ++k) S[c + k] = fmaf(hi, S[c + k], fmaf(lo, S[c + k], u[k]));
+            }
+            put_state();                           // far has been read: DONE_G
+            if (ENDS) continue;
+            wait_warp(DONE_OUT);
+            if (gave_up) break;
+            const float w = m.far * powers[r + 1 - m.shift];
+            __nv_bfloat16* to = (__nv_bfloat16*)m.out + ((bt * m.length + origin + dir * (t + r)) * m.heads + h) * m.dc + col0;
+#pragma unroll 1
+            for (int c = 0; c < COLS; c += 32) {
+                const int left = m.dc - col0 - c;
+                if (left <= 0) break;
+                float o[32];
+                tmem_load32(tmem + R::NEAR + lanes + col0 + c, o);
+                float odd = 0.f;
+#pragma unroll
+                for (int k = 0; k < 32; ++k) odd = fmaf(o[k], 0.f, odd);
+                if (__any_sync(~0u, odd != 0.f)) {
+                    // a product with a node behind is 0 times what c holds there: an infinity or NaN is none of this row's
+                    float again[32] = {};
+                    const __nv_bfloat16* cs = (const __nv_bfloat16*)m.c.p + bt * m.c.batch + h * m.c.head + col0 + c;
+                    for (int j = 0; j < N; ++j) {
+                        const int rj = m.reversed ? N - 1 - j : j;
+                        const uint32_t two = tmem_load1(tmem + R::G + lanes + p_column(j / 16) + j % 16 / 2);
+                        const float x = j % 2 ? __uint_as_float(two & 0xffff0000u) : __uint_as_float(two << 16);
+                        if (rj <= r && r < n)
+#pragma unroll
+                            for (int k = 0; k < 32; ++k)
+                                if (k < left) again[k] = fmaf(x, __bfloat162float(cs[(origin + dir * (t + rj)) * m.c.node + k]), again[k]);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 32; ++k)
+                        if (o[k] - o[k] != 0.f) o[k] = again[k];
+                }
+                float f[32];
+                tmem_load32(tmem + R::FAR + lanes + col0 + c, f);
+#pragma unroll
+                for (int k = 0; k < 32; ++k) o[k] = fmaf(w, f[k], o[k]);
+                if (r < n) {
+                    if (left >= 32 && m.out_packed) {
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            uint32_t v[8];
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) v[k] = pack_bf16(o[16 * q + 2 * k], o[16 * q + 2 * k + 1]);
+                            store32(to + c + 16 * q, v);
+                        }
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            if (k < left) to[c + k] = __float2bfloat16_rn(o[k]);
+                    }
+                }
+            }
+            signal(READY);
+        }
+    }
+    const bool lost = __syncthreads_or(gave_up);
+    if (lost) {                 // what has been issued has to end before the block does; the results are NaN
+        if (warp == WARPS && lane == 0) {
+            bool late = false;
+            mma_commit(bar(ENDED));
+            mbar_wait<TRIES>(bar(ENDED), 0, late, &g_linear_timeouts);
+            if (loads_ab > 0) mbar_wait<TRIES>(bar(FULL_AB), (loads_ab - 1) & 1, late, &g_linear_timeouts);
+            if (loads_c > 0) mbar_wait<TRIES>(bar(FULL_C), (loads_c - 1) & 1, late, &g_linear_timeouts);
+        }
+        if (!ENDS)
+            for (int64_t i = first * m.dc + tid; i < last * m.dc; i += THREADS) {
+                const int64_t node = m.reversed ? m.length - 1 - i / m.dc : i / m.dc;
+                ((__nv_bfloat16*)m.out)[((bt * m.length + node) * m.heads + h) * m.dc + i % m.dc] = __float2bfloat16_rn(NAN);
+            }
+#pragma unroll
+        for (int c = 0; c < COLS; ++c) S[c] = NAN;
+        __syncthreads();
+    }
+    if (holds && d < m.da) {
+        if (ENDS) {
+#pragma unroll
+            for (int c = 0; c < COLS; ++c)
+                if (col0 + c < m.dc) local[(int64_t)(col0 + c) * m.da + d] = S[c];
+        } else if (p == m.pieces - 1 && m.end != nullptr) {
+            float* to = m.end + st + (int64_t)d * m.dc + col0;
+            if (m.dc % 4 == 0 && m.end_packed) {
+#pragma unroll
+                for (int c = 0; c < COLS; c += 4)
+                    if (col0 + c < m.dc) {
+                        const float v[4] = {S[c], S[c + 1], S[c + 2], S[c + 3]};
+                        store_pack<float, 4>(to + c, v);
+                    }
+            } else {
+#pragma unroll
+                for (int c = 0; c < COLS; ++c)
+                    if (col0 + c < m.dc) to[c] = S[c];
+            }
+        }
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    if (warp == WARPS) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(R::COLUMNS) : "memory");
+}
+
+// ------------------------------------------------------------------------------------------- host
+// The map of one array, (features, heads, nodes, batch).  An axis of stride zero has one entry for all.
+bool tile_map(const LinearView& x, int width, int64_t heads, int64_t length, int64_t batch, CUtensorMap* map, int* head, int* row) {
+    const EncodeTiledFn fn = tma_encode_fn();
+    const int64_t strides[3] = {x.head, x.node, x.batch}, extents[3] = {heads, length, batch};
+    if (fn == nullptr || !aligned(x.p, 16)) return false;
+    cuuint64_t dims[4] = {(cuuint64_t)width}, bytes[3];
+    for (int i = 0; i < 3; ++i) {
+        const bool one = extents[i] == 1 || strides[i] == 0;
+        if (i == 1 && strides[i] == 0 && extents[i] > 1) return false;       // all nodes the same: the tile needs them one by one
+        if (!one && (strides[i] < 0 || strides[i] % 8 != 0 || strides[i] >= (1ll << 38))) return false;
+        if (extents[i] > 0x7fffffff - 2 * N) return false;
+        dims[i + 1] = one ? 1 : (cuuint64_t)extents[i];
+        bytes[i] = one ? 16 : (cuuint64_t)strides[i] * 2;
+    }
+    *head = dims[1] > 1;
+    *row = dims[3] > 1;
+    const cuuint32_t box[4] = {64, 1, N, 1}, step[4] = {1, 1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(x.p), dims, bytes, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int DA, int DC, bool ENDS>
+cudaError_t launch(const March& m, const Tiles& tiles, cudaStream_t st) {
+    static std::atomic<uint64_t> done{0};
+    const size_t bytes = Room<DA, DC>::BYTES;
+    const cudaError_t e = allow_smem(march_mma_kernel<DA, DC, ENDS>, bytes, done);
+    if (e != cudaSuccess) return e;
+    const int64_t blocks = m.batch * m.heads * m.pieces;
+    if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    return launch_kernel_smem(march_mma_kernel<DA, DC, ENDS>, dim3((unsigned)blocks), dim3(THREADS), bytes, st, m, tiles);
+}
+
+template <int DA, int DC>
+cudaError_t run(const March& m, const Tiles& tiles, cudaStream_t st) {
+    if (m.pieces > 1) {
+        cudaError_t e = launch<DA, DC, true>(m, tiles, st);
+        if (e == cudaSuccess) e = march_join(m, st);
+        if (e != cudaSuccess) return e;
+    }
+    return launch<DA, DC, false>(m, tiles, st);
+}
+
+}  // namespace
+
+int march_mma_blocks(const March& m) { return m.da <= 64 && m.dc <= 64 ? 2 * 148 : 148; }
+
+bool march_mma(const March& given, cudaStream_t st, cudaError_t* e) {
+    March m = given;
+    Tiles tiles;
+    if (!tile_map(m.a, m.da, m.heads, m.length, m.batch, &tiles.a, &tiles.head_a, &tiles.batch_a) ||
+        !tile_map(m.b, m.da, m.heads, m.length, m.batch, &tiles.b, &tiles.head_b, &tiles.batch_b) ||
+        !tile_map(m.c, m.dc, m.heads, m.length, m.batch, &tiles.c, &tiles.head_c, &tiles.batch_c))
+        return false;
+    m.local_turned = 1;
+    m.start_packed = aligned(m.start, 16);
+    m.end_packed = aligned(m.end, 16);
+    m.out_packed = m.dc % 16 == 0 && aligned(m.out, 32);
+    if (m.dc <= 64) *e = m.da <= 64 ? run<64, 64>(m, tiles, st) : run<128, 64>(m, tiles, st);
+    else *e = m.da <= 64 ? run<64, 128>(m, tiles, st) : run<128, 128>(m, tiles, st);
+    return true;
+}
+
+unsigned int march_mma_timeouts() {
+    unsigned int n = 0;
+    return cudaMemcpyFromSymbol(&n, g_linear_timeouts, sizeof n) == cudaSuccess ? n : 0xffffffffu;
+}
+
+}  // namespace fpde
