@@ -295,7 +295,7 @@ void cut(const fpde_linear_args* a, March& m) {
     const bool mma = on_tensor_cores(a);
     const int chunk = mma ? MMA_CHUNK : C;
     const double ends = 0.5, start = 1.;
-    const int64_t rows = m.batch * m.heads * (mma ? 1 : ceil_div(m.dc, 64)), slots = mma ? march_mma_blocks(m) : 148 * 4, chunks = ceil_div(m.length, chunk);
+    const int64_t rows = m.batch * m.heads * (mma ? 1 : ceil_div(m.dc, 64)), slots = mma ? march_mma_blocks() : 148 * 4, chunks = ceil_div(m.length, chunk);
     int64_t best = 1;
     double least = 1e300;
     for (int64_t p = 1; p <= chunks && p <= 1024 && rows * (p - 1) < 8 * slots; ++p) {

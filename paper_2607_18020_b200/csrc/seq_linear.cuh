@@ -39,7 +39,7 @@ cudaError_t march_join(const March& m, cudaStream_t st);
 // The march of bf16 arrays on the tensor cores (seq_linear_mma.cu).  Its pieces are multiples of MMA_CHUNK nodes.  False, with
 // nothing launched: the copy engine cannot read one of the arrays (a start or stride that is no multiple of 16 bytes).
 constexpr int MMA_CHUNK = 128;
-int march_mma_blocks(const March& m);                // resident blocks of the GPU
+int march_mma_blocks();                // resident blocks of the GPU
 bool march_mma(const March& m, cudaStream_t st, cudaError_t* e);
 unsigned int march_mma_timeouts();
 

@@ -13,16 +13,18 @@
 // its own rounding, and nothing else.  The state itself stays fp32: bw is three bf16 parts that hold all 24 bits of b times its
 // decay, c is exact, U is formed of three products and the state is added up with ordinary rounding.
 //
-// Threads.  Eight warps, two threads for each of the 128 lanes of TMEM with half of the columns each, and one thread that loads (TMA)
-// and issues the products.  G and far run while all turn b into bw, U while G becomes P, and a tile's place takes the next chunk's
-// as soon as the products that read it are done: a and b after far, c after near.
+// Threads.  One block an SM; its warps have tasks of their own, so that a chunk's steps run beside one another and beside those of
+// the chunks before and after: four turn G into P, four turn b into bw, eight write the output and move the state on (two threads
+// for each lane of TMEM, half of the columns each), one issues the products and one loads (TMA).  A tile's place takes the next
+// chunk's as soon as the products that read it are done.  (With all warps at the same step, one after the other: 16 warps
+// that wait for one another's latencies, 11 800 cycles a chunk of 128 x 128 features at a quarter of the issue slots.)
 #include "mma_common.cuh"
 #include "seq_linear.cuh"
 
 namespace fpde {
 namespace {
 
-constexpr int N = MMA_CHUNK, WARPS = 8, THREADS = 32 * (WARPS + 1);
+constexpr int N = MMA_CHUNK;
 constexpr int BLOCK = N * 128;                 // bytes of 64 features of a chunk
 constexpr int PARTS = 3;
 constexpr int TRIES = 1 << 20;                 // of a wait (for microseconds, in a healthy run); 20 ms at the very least
@@ -33,14 +35,16 @@ template <int DA, int DC>
 struct Room {
     static constexpr int A = 0, B = A + DA / 64 * BLOCK, V = B + DA / 64 * BLOCK, BW = V + DC / 64 * BLOCK, S = BW + PARTS * (DA / 64) * BLOCK;
     static constexpr int BYTES = S + DC / 64 * DA * 128 + 1024;      // slack to start on 1024 bytes
-    // columns of TMEM.  P takes the first and the last 32 of G, which their own readers have read before; with 64 columns of c near
-    // lies between them, so that two blocks fit an SM
-    static constexpr int G = 0, NEAR = DC == 64 ? 32 : 128, FAR = DC == 64 ? 128 : 256, U = DC == 64 ? 192 : 384, COLUMNS = DC == 64 ? 256 : 512;
+    static constexpr int G = 0, NEAR = 128, FAR = NEAR + DC, U = FAR + DC;      // columns of TMEM; P lies over G
 };
-__host__ __device__ constexpr int p_column(int k) { return k < 4 ? 8 * k : 96 + 8 * (k - 4); }      // of 16 nodes' products
+// Warps, in groups of four, and their registers: 640 threads start with 96 each.
+constexpr int GROUP_P = 0, GROUP_BW = 1, GROUP_OUT = 2, GROUP_CONTROL = 4, THREADS = 5 * 128;
+constexpr int OUT_WARPS = 8, OUT_REGS = 144, OTHER_REGS = 64;
+static_assert(2 * OUT_REGS + 3 * OTHER_REGS <= 5 * 96, "the groups share what the block starts with");
 
-// Barriers.  FULL: the tiles have arrived; DONE: products are; READY: the compute warps have written what the next products read.
-enum Bar { FULL_AB, FULL_C, DONE_G, DONE_U, DONE_OUT, READY_BW, READY_P, READY, ENDED, BARS };
+// Barriers.  FULL: a tile has arrived; DONE: the products up to these are done; READY: warps have written what products read;
+// FREE: warps have read what products write.
+enum Bar { FULL_A, FULL_B, FULL_C, DONE_G, DONE_FAR, DONE_NEAR, DONE_U, READY_P, READY_BW, READY_S, FREE_OUT, ENDED, BARS };
 
 __device__ __forceinline__ void sts16(uint32_t to, uint4 v) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
@@ -71,6 +75,18 @@ __device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t (&r)[
         "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
         "r"(r[15]), "r"(addr)
         : "memory");
+}
+__device__ __forceinline__ void tmem_load(uint32_t addr, float (&v)[32]) { tmem_load32(addr, v); }
+__device__ __forceinline__ void tmem_load(uint32_t addr, float (&v)[16]) {
+    uint32_t r[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint32_t tmem_load1(uint32_t addr) {
@@ -105,23 +121,24 @@ struct Tiles {
 
 // ENDS: only the state that each piece leaves, from zero.
 template <int DA, int DC, bool ENDS>
-__global__ void __launch_bounds__(THREADS, DC == 64 && DA == 64 ? 2 : 1) march_mma_kernel(const __grid_constant__ March m, const __grid_constant__ Tiles tiles) {
+__global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_constant__ March m, const __grid_constant__ Tiles tiles) {
     using R = Room<DA, DC>;
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[BARS];
     __shared__ uint32_t tmem_slot;
     __shared__ __align__(16) float powers[N + 2];
-    __shared__ __align__(16) float near_end[32];                 // g^(31 - k)
+    __shared__ float falling[64], rising[64];                    // g^(31 - i) and g^(i - 31), 0 where that is no power
     __shared__ float whole[4];                                   // g^128 and that of the last chunk, each in two parts
     const uint32_t base = (smem_u32(raw) + 1023) & ~1023u;
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, half = warp / 4, quarter = warp % 4;
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, group = warp / 4, quarter = warp % 4;
+    const int BW_WARPS = ENDS ? 8 : 4;                           // without P its warps help with bw
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     if (tid == 0) {
-        for (int i = 0; i < BARS; ++i) mbar_init(bar(i), i == READY_BW || i == READY_P || i == READY ? WARPS : 1);
+        for (int i = 0; i < BARS; ++i) mbar_init(bar(i), i == READY_P ? 4 : i == READY_BW ? BW_WARPS : i == READY_S || i == FREE_OUT ? OUT_WARPS : 1);
         mbar_fence_init();
     }
-    if (warp == WARPS) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "n"(R::COLUMNS) : "memory");
+    if (warp == 4 * GROUP_CONTROL) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_slot)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     pdl_wait_then_trigger();
@@ -130,112 +147,85 @@ __global__ void __launch_bounds__(THREADS, DC == 64 && DA == 64 ? 2 : 1) march_m
     const int p = (int)(id % m.pieces);
     id /= m.pieces;
     const int64_t h = id % m.heads, bt = id / m.heads;
-    const float ld = m.log_decay[h];
     const int64_t first = p * m.piece, last = min(m.length, first + m.piece);
-    const int tail = last > first ? (int)((last - first - 1) % N) + 1 : 0;
-    if (tid < N + 2) {
-        const float g = (float)power(ld, tid);
-        powers[tid] = g;
-        if (tid < 32) near_end[31 - tid] = g;
-    }
-    if (tid >= 192 && tid < 194) {
-        const double g = power(ld, tid == 192 ? N : tail);
-        whole[2 * (tid - 192)] = (float)g;
-        whole[2 * (tid - 192) + 1] = (float)(g - (float)g);
-    }
-
-    // The state: row d, columns half * DC / 2 and on.  With 64 rows the products use 16 lanes of each quarter.
-    constexpr int COLS = DC / 2;
-    const bool holds = warp < WARPS && (DA == 128 || lane < 16);
-    const int d = DA == 128 ? quarter * 32 + lane : quarter * 16 + lane, col0 = half * COLS;
-    const int64_t st = (bt * m.heads + h) * m.da * m.dc;
-    float* local = m.local + ((bt * m.heads + h) * m.pieces + p) * m.da * m.dc;      // by columns: neighbouring lanes are neighbours there
-    float S[COLS];
-#pragma unroll
-    for (int c = 0; c < COLS; ++c) S[c] = 0.f;
-    if (!ENDS && holds && d < m.da) {
-        if (m.pieces > 1 || (m.start != nullptr && m.start_turned)) {
-            const float* from = m.pieces > 1 ? local : m.start + st;
-#pragma unroll
-            for (int c = 0; c < COLS; ++c)
-                if (col0 + c < m.dc) S[c] = from[(int64_t)(col0 + c) * m.da + d];
-        } else if (m.start != nullptr) {
-            const float* from = m.start + st + (int64_t)d * m.dc + col0;
-            if (m.dc % 4 == 0 && m.start_packed) {
-#pragma unroll
-                for (int c = 0; c < COLS; c += 4)
-                    if (col0 + c < m.dc) {
-                        const Pack<float, 4> v = load_pack<float, 4>(from + c);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) S[c + e] = v.v[e];
-                    }
-            } else {
-#pragma unroll
-                for (int c = 0; c < COLS; ++c)
-                    if (col0 + c < m.dc) S[c] = from[c];
+    {
+        const float ld = m.log_decay[h];
+        if (tid < N + 2) {
+            const float g = (float)power(ld, tid);
+            powers[tid] = g;
+            if (tid < 32) {
+                falling[31 - tid] = rising[31 + tid] = g;
+                falling[32 + tid] = 0.f;
+                if (tid < 31) rising[tid] = 0.f;
+                if (tid == 31) rising[63] = 0.f;
             }
         }
+        if (tid >= 192 && tid < 194) {
+            const double g = power(ld, tid == 192 ? N : last > first ? (int)((last - first - 1) % N) + 1 : 0);
+            whole[2 * (tid - 192)] = (float)g;
+            whole[2 * (tid - 192) + 1] = (float)(g - (float)g);
+        }
     }
-    auto put_state = [&]() {                   // the factor of `far`
-        if (ENDS || !holds) return;
-#pragma unroll
-        for (int q = 0; q < COLS / 8; ++q)
-            sts16(chunk_at(base + R::S, d, half * (COLS / 8) + q, DA),
-                  make_uint4(pack_bf16(S[8 * q], S[8 * q + 1]), pack_bf16(S[8 * q + 2], S[8 * q + 3]), pack_bf16(S[8 * q + 4], S[8 * q + 5]),
-                             pack_bf16(S[8 * q + 6], S[8 * q + 7])));
-    };
-    put_state();
-    fence_async();
     fence_before();
     __syncthreads();
     fence_after();
     const uint32_t tmem = tmem_slot;
     uint32_t phase = 0;
     bool gave_up = false;
+    int asked_a = 0, asked_b = 0, asked_c = 0; // tiles that this thread has asked for
     auto wait = [&](int i) { mbar_wait<TRIES>(bar(i), phase, gave_up, &g_linear_timeouts); };
-    int loads_ab = 0, loads_c = 0;             // of the loading thread
-    if (warp == WARPS) {
-        if (lane == 0 && first < last) {
-            auto node_at = [&](int64_t t) { return (int)(m.reversed ? m.length - t - N : t); };
-            auto load_ab = [&](int64_t t) {
-                mbar_expect_tx(bar(FULL_AB), (ENDS ? 1 : 2) * (DA / 64) * BLOCK);
-#pragma unroll
-                for (int f = 0; f < DA / 64; ++f) {
-                    load_tile(base + R::B + f * BLOCK, &tiles.b, 64 * f, tiles.head_b * (int)h, node_at(t), tiles.batch_b * (int)bt, bar(FULL_AB));
-                    if (!ENDS) load_tile(base + R::A + f * BLOCK, &tiles.a, 64 * f, tiles.head_a * (int)h, node_at(t), tiles.batch_a * (int)bt, bar(FULL_AB));
-                }
-                ++loads_ab;
-            };
-            auto load_c = [&](int64_t t) {
-                mbar_expect_tx(bar(FULL_C), (DC / 64) * BLOCK);
-#pragma unroll
-                for (int f = 0; f < DC / 64; ++f)
-                    load_tile(base + R::V + f * BLOCK, &tiles.c, 64 * f, tiles.head_c * (int)h, node_at(t), tiles.batch_c * (int)bt, bar(FULL_C));
-                ++loads_c;
-            };
-            constexpr uint32_t IDESC = 1u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(128 / 16) << 24;      // fp32 sums of bf16 factors, 128 rows
-            constexpr uint32_t IDESC_G = IDESC | (uint32_t)(N / 8) << 17, IDESC_OUT = IDESC | 1u << 16 | (uint32_t)(DC / 8) << 17;
-            constexpr uint32_t IDESC_U = 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | (uint32_t)(DC / 8) << 17 | (uint32_t)(DA / 16) << 24;
+    auto wait_last = [&](int i) { mbar_wait<TRIES>(bar(i), phase ^ 1, gave_up, &g_linear_timeouts); };      // of the chunk before
+    auto wait_warp = [&](int i) {
+        wait(i);
+        gave_up = __any_sync(~0u, gave_up);
+        fence_after();
+    };
+    auto signal = [&](int i) {
+        fence_async();
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(i));
+    };
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    const int row = quarter * 32 + lane, r = m.reversed ? N - 1 - row : row;      // of the tile, and in the march's order
+
+    if (group == GROUP_CONTROL) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
+        constexpr uint32_t IDESC = 1u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(128 / 16) << 24;      // fp32 sums of bf16 factors, 128 rows
+        constexpr uint32_t IDESC_G = IDESC | (uint32_t)(N / 8) << 17, IDESC_OUT = IDESC | 1u << 16 | (uint32_t)(DC / 8) << 17;
+        constexpr uint32_t IDESC_U = 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | (uint32_t)(DC / 8) << 17 | (uint32_t)(DA / 16) << 24;
+        if (quarter == 0 && lane == 0) {       // products
             const uint64_t da = slice_desc(base + R::A, false), db = slice_desc(base + R::B, false), dc = slice_desc(base + R::V, true, BLOCK),
                            ds = slice_desc(base + R::S, true, DA * 128);
-            load_ab(first);
-            load_c(first);
             for (int64_t t = first; t < last; t += N, phase ^= 1) {
-                const bool more = t + N < last;
                 if (!ENDS) {
-                    if (t > first) mbar_wait<TRIES>(bar(READY), phase ^ 1, gave_up, &g_linear_timeouts);
-                    wait(FULL_AB);
+                    wait(FULL_A);
+                    wait(FULL_B);
+                    if (t > first) wait_last(FREE_OUT);
                     if (gave_up) break;
                     fence_after();
 #pragma unroll
                     for (int k = 0; k < DA / 16; ++k)
                         mma_f16(tmem + R::G, desc_at(da, k / 4 * BLOCK + k % 4 * 32), desc_at(db, k / 4 * BLOCK + k % 4 * 32), IDESC_G, k > 0);
+                    mma_commit(bar(DONE_G));
+                    wait(READY_S);             // of the state before this chunk
+                    if (gave_up) break;
+                    fence_after();
 #pragma unroll
                     for (int k = 0; k < DA / 16; ++k) mma_f16(tmem + R::FAR, desc_at(da, k / 4 * BLOCK + k % 4 * 32), desc_at(ds, k * 2048), IDESC_OUT, k > 0);
-                    mma_commit(bar(DONE_G));
+                    mma_commit(bar(DONE_FAR));
+                    wait(READY_P);
+                    wait(FULL_C);
+                    if (gave_up) break;
+                    fence_after();
+#pragma unroll
+                    for (int k = 0; k < N / 16; ++k) mma_tmem(tmem + R::NEAR, tmem + R::G + 8 * k, desc_at(dc, k * 2048), IDESC_OUT, k > 0);
+                    mma_commit(bar(DONE_NEAR));
+                } else {
+                    wait(READY_S);
+                    wait(FULL_C);
                 }
                 wait(READY_BW);
-                wait(FULL_C);
                 if (gave_up) break;
                 fence_after();
 #pragma unroll
@@ -245,209 +235,250 @@ __global__ void __launch_bounds__(THREADS, DC == 64 && DA == 64 ? 2 : 1) march_m
                     for (int k = 0; k < N / 16; ++k) mma_f16(tmem + R::U, desc_at(dw, k * 2048), desc_at(dc, k * 2048), IDESC_U, s < PARTS - 1 || k > 0);
                 }
                 mma_commit(bar(DONE_U));
-                if (!ENDS) wait(DONE_G);
-                if (gave_up) break;
-                if (more) load_ab(t + N);
+            }
+        } else if (quarter == 1 && lane == 0) {                // tiles
+            auto load = [&](int full, int at, int blocks, const CUtensorMap* map, int head, int batch, int64_t t) {
+                mbar_expect_tx(bar(full), blocks * BLOCK);
+                const int node = (int)(m.reversed ? m.length - t - N : t);
+                for (int f = 0; f < blocks; ++f) load_tile(base + at + f * BLOCK, map, 64 * f, head * (int)h, node, batch * (int)bt, bar(full));
+            };
+            // the places are the last chunk's: a is read by G and far, b by G and bw, c by near and U
+            for (int64_t t = first; t < last; t += N) {
                 if (!ENDS) {
-                    wait(READY_P);
+                    if (t > first) wait(DONE_FAR);
                     if (gave_up) break;
-                    fence_after();
-#pragma unroll
-                    for (int k = 0; k < N / 16; ++k) mma_tmem(tmem + R::NEAR, tmem + R::G + p_column(k), desc_at(dc, k * 2048), IDESC_OUT, k > 0);
-                    mma_commit(bar(DONE_OUT));
-                    if (more) wait(DONE_OUT);
-                } else if (more) {
-                    wait(DONE_U);
+                    load(FULL_A, R::A, DA / 64, &tiles.a, tiles.head_a, tiles.batch_a, t);
+                    ++asked_a;
                 }
+                if (t > first) wait(READY_BW);
                 if (gave_up) break;
-                if (more) load_c(t + N);
+                load(FULL_B, R::B, DA / 64, &tiles.b, tiles.head_b, tiles.batch_b, t);
+                ++asked_b;
+                if (t > first) wait(DONE_U);
+                if (gave_up) break;
+                load(FULL_C, R::V, DC / 64, &tiles.c, tiles.head_c, tiles.batch_c, t);
+                ++asked_c;
+                if (t > first) phase ^= 1;
             }
         }
-    } else {
-        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-        const int row = quarter * 32 + lane, r = m.reversed ? N - 1 - row : row;      // of the tile, and in the march's order
-        const int64_t dir = m.reversed ? -1 : 1, origin = m.reversed ? m.length - 1 : 0;
-        auto signal = [&](int i) {
-            fence_async();
-            fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(i));
-        };
-        auto wait_warp = [&](int i) {
-            wait(i);
-            gave_up = __any_sync(~0u, gave_up);
-            fence_after();
-        };
+    } else if (group == GROUP_BW || (ENDS && group == GROUP_P)) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
         for (int64_t t = first; t < last; t += N, phase ^= 1) {
             const int n = (int)min((int64_t)N, last - t);
-            wait_warp(FULL_AB);
+            wait_warp(FULL_B);
+            if (t > first) {                   // bw's place is the last chunk's until U is done
+                wait_last(DONE_U);
+                gave_up = __any_sync(~0u, gave_up);
+            }
             if (gave_up) break;
-            {                                      // bw: a row, half of its features
-                const float w = r < n ? m.gain * powers[n - 1 - r + m.shift] : 0.f;
+            const float w = r < n ? m.gain * powers[n - 1 - r + m.shift] : 0.f;
+            constexpr int EACH = ENDS ? DA / 16 : DA / 8;
+#pragma unroll 4
+            for (int e = 0; e < EACH; ++e) {
+                const int q = (ENDS ? group * EACH : 0) + e;
+                const uint4 v = lds16(chunk_at(base + R::B, row, q));
+                const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+                uint32_t out[PARTS][4];
 #pragma unroll
-                for (int q = half * (DA / 16), e = 0; e < DA / 16; ++e, ++q) {
-                    const uint4 v = lds16(chunk_at(base + R::B, row, q));
-                    const uint32_t in[4] = {v.x, v.y, v.z, v.w};
-                    uint32_t out[PARTS][4];
+                for (int k = 0; k < 4; ++k) {
+                    float lo = __uint_as_float(in[k] << 16) * w, hi = __uint_as_float(in[k] & 0xffff0000u) * w;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        float lo = __uint_as_float(in[k] << 16) * w, hi = __uint_as_float(in[k] & 0xffff0000u) * w;
-#pragma unroll
-                        for (int s = 0; s < PARTS; ++s) {      // the top 8 bits of what is left, exactly
-                            out[s][k] = tops(lo, hi);
-                            lo -= top_part(lo);
-                            hi -= top_part(hi);
-                        }
+                    for (int s = 0; s < PARTS; ++s) {          // the top 8 bits of what is left, exactly
+                        out[s][k] = tops(lo, hi);
+                        lo -= top_part(lo);
+                        hi -= top_part(hi);
                     }
-#pragma unroll
-                    for (int s = 0; s < PARTS; ++s)
-                        sts16(chunk_at(base + R::BW + s * (DA / 64) * BLOCK, row, q), make_uint4(out[s][0], out[s][1], out[s][2], out[s][3]));
                 }
+#pragma unroll
+                for (int s = 0; s < PARTS; ++s)
+                    sts16(chunk_at(base + R::BW + s * (DA / 64) * BLOCK, row, q), make_uint4(out[s][0], out[s][1], out[s][2], out[s][3]));
             }
             signal(READY_BW);
+        }
+    } else if (group == GROUP_P) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
+        for (int64_t t = first; t < last; t += N, phase ^= 1) {
+            wait_warp(DONE_G);
+            if (gave_up) break;
+            // 32 columns at a time: those of this quarter's own nodes are cut along the diagonal, those of the nodes before them
+            // are whole, the others zeros.  Column k of the 32 is g^(32 before + lane - k), or + k - lane, times the product.  A thread
+            // has a lane of G for itself, and P's columns are behind those that it still has to read.
+#pragma unroll 1
+            for (int part = 0; part < 4; ++part) {
+                const int before = m.reversed ? part - quarter : quarter - part;
+                const float* table = before == 0 ? (m.reversed ? rising + 31 - lane : falling + 31 - lane) : (m.reversed ? rising + 31 : falling);
+                const float w = before > 0 ? m.near * powers[32 * before + (m.reversed ? -lane : lane - 31)] : m.near;
+                const uint32_t there = before > 0 ? ~0u : m.reversed ? ~0u << lane : (2u << lane) - 1u;
+                uint32_t packed[16];
+                if (before >= 0) {
+                    float v[32];
+                    tmem_load32(tmem + R::G + lanes + part * 32, v);
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) v[k] = (there >> k & 1u) != 0 ? v[k] * (w * table[k]) : 0.f;
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) packed[k] = pack_bf16(v[2 * k], v[2 * k + 1]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) packed[k] = 0;
+                }
+                tmem_store16(tmem + R::G + part * 16 + lanes, packed);
+            }
+            tmem_stored();
+            signal(READY_P);
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(OUT_REGS));
+        // The state: row d, half of the columns.  With 64 rows the products use 16 lanes of each quarter.
+        constexpr int COLS = DC / 2;
+        const bool holds = DA == 128 || lane < 16;
+        const int d = DA == 128 ? quarter * 32 + lane : quarter * 16 + lane, col0 = (group - GROUP_OUT) * COLS;
+        const int64_t st = (bt * m.heads + h) * m.da * m.dc;
+        float* local = m.local + ((bt * m.heads + h) * m.pieces + p) * m.da * m.dc;      // by columns: neighbouring lanes are neighbours there
+        float S[COLS];
+#pragma unroll
+        for (int c = 0; c < COLS; ++c) S[c] = 0.f;
+        if (!ENDS && holds && d < m.da) {
+            if (m.pieces > 1 || (m.start != nullptr && m.start_turned)) {
+                const float* from = m.pieces > 1 ? local : m.start + st;
+#pragma unroll
+                for (int c = 0; c < COLS; ++c)
+                    if (col0 + c < m.dc) S[c] = from[(col0 + c) * m.da + d];
+            } else if (m.start != nullptr) {
+                const float* from = m.start + st + d * m.dc + col0;
+                if (m.dc % 4 == 0 && m.start_packed) {
+#pragma unroll
+                    for (int c = 0; c < COLS; c += 4)
+                        if (col0 + c < m.dc) {
+                            const Pack<float, 4> v = load_pack<float, 4>(from + c);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) S[c + e] = v.v[e];
+                        }
+                } else {
+#pragma unroll
+                    for (int c = 0; c < COLS; ++c)
+                        if (col0 + c < m.dc) S[c] = from[c];
+                }
+            }
+        }
+        auto put_state = [&]() {               // the factor of `far`
+            if (!ENDS && holds) {
+#pragma unroll
+                for (int q = 0; q < COLS / 8; ++q)
+                    sts16(chunk_at(base + R::S, d, col0 / 8 + q, DA),
+                          make_uint4(pack_bf16(S[8 * q], S[8 * q + 1]), pack_bf16(S[8 * q + 2], S[8 * q + 3]), pack_bf16(S[8 * q + 4], S[8 * q + 5]),
+                                     pack_bf16(S[8 * q + 6], S[8 * q + 7])));
+            }
+            signal(READY_S);
+        };
+        put_state();
+        const int64_t dir = m.reversed ? -1 : 1, origin = m.reversed ? m.length - 1 : 0;
+        for (int64_t t = first; t < last; t += N, phase ^= 1) {
+            const int n = (int)min((int64_t)N, last - t);
             if (!ENDS) {
-                wait_warp(DONE_G);
+                wait_warp(DONE_NEAR);
                 if (gave_up) break;
-                // P, 32 columns at a time: those of this quarter's own nodes are cut along the diagonal, those of the nodes before them
-                // are whole, the others zeros.  In the last half the last columns come first: P lies over G.
+                const float w = m.far * powers[r + 1 - m.shift];
+                __nv_bfloat16* to = (__nv_bfloat16*)m.out + ((bt * m.length + origin + dir * (t + r)) * m.heads + h) * m.dc + col0;
+#pragma unroll 1
+                for (int c = 0; c < COLS; c += 16) {
+                    const int left = m.dc - col0 - c;
+                    if (left <= 0) break;
+                    float o[16], f[16];
+                    tmem_load(tmem + R::NEAR + lanes + col0 + c, o);
+                    tmem_load(tmem + R::FAR + lanes + col0 + c, f);
+                    float odd = 0.f;
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int part = half == 0 ? e : 3 - e, before = m.reversed ? part - quarter : quarter - part;
-                    uint32_t packed[16] = {};
-                    if (before >= 0) {
-                        float v[32];
-                        tmem_load32(tmem + R::G + lanes + part * 32, v);
-                        if (before == 0) {
+                    for (int k = 0; k < 16; ++k) odd = fmaf(o[k], 0.f, odd);
+                    if (__any_sync(~0u, odd != 0.f)) {
+                        // a product with a node behind is 0 times what c holds there: an infinity or NaN is none of this row's
+                        float again[16] = {};
+                        const __nv_bfloat16* cs = (const __nv_bfloat16*)m.c.p + bt * m.c.batch + h * m.c.head + col0 + c;
+#pragma unroll 1
+                        for (int j = 0; j < N; ++j) {
+                            const int rj = m.reversed ? N - 1 - j : j;
+                            const uint32_t two = tmem_load1(tmem + R::G + lanes + j / 2);
+                            const float x = j % 2 ? __uint_as_float(two & 0xffff0000u) : __uint_as_float(two << 16);
+                            if (rj <= r && r < n)
 #pragma unroll
-                            for (int k = 0; k < 32; ++k) {
-                                const int back = m.reversed ? k - lane : lane - k;
-                                v[k] = back < 0 ? 0.f : v[k] * (m.near * powers[max(back, 0)]);
-                            }
-                        } else if (m.reversed) {             // column k: back = 32 before + k - lane = (32 before - 31 + 31 - lane) + k
-                            const float w = m.near * powers[32 * before - lane];
-#pragma unroll
-                            for (int k = 0; k < 32; ++k) v[k] *= w * near_end[31 - k];
-                        } else {                             // back = 32 before + lane - k
-                            const float w = m.near * powers[32 * before + lane - 31];
-#pragma unroll
-                            for (int k = 0; k < 32; ++k) v[k] *= w * near_end[k];
+                                for (int k = 0; k < 16; ++k)
+                                    if (k < left) again[k] = fmaf(x, __bfloat162float(cs[(origin + dir * (t + rj)) * m.c.node + k]), again[k]);
                         }
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) packed[k] = pack_bf16(v[2 * k], v[2 * k + 1]);
+                        for (int k = 0; k < 16; ++k)
+                            if (o[k] - o[k] != 0.f) o[k] = again[k];
                     }
-                    tmem_store16(tmem + R::G + p_column(2 * part) + lanes, packed);
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) o[k] = fmaf(w, f[k], o[k]);
+                    if (r < n) {
+                        if (left >= 16 && m.out_packed) {
+                            uint32_t v[8];
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) v[k] = pack_bf16(o[2 * k], o[2 * k + 1]);
+                            store32(to + c, v);
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < 16; ++k)
+                                if (k < left) to[c + k] = __float2bfloat16_rn(o[k]);
+                        }
+                    }
                 }
-                tmem_stored();
-                signal(READY_P);
+                signal(FREE_OUT);
             }
             wait_warp(DONE_U);
             if (gave_up) break;
             const float hi = whole[n == N ? 0 : 2], lo = whole[n == N ? 1 : 3];
 #pragma unroll
-            for (int c = 0; c < COLS; c += 32) {
-                float u[32];
-                tmem_load32(tmem + R::U + lanes + col0 + c, u);
+            for (int c = 0; c < COLS; c += 16) {
+                float u[16];
+                tmem_load(tmem + R::U + lanes + col0 + c, u);
 #pragma unroll
-                for (int k = 0; k < 32; ++k) S[c + k] = fmaf(hi, S[c + k], fmaf(lo, S[c + k], u[k]));
+                for (int k = 0; k < 16; ++k) S[c + k] = fmaf(hi, S[c + k], fmaf(lo, S[c + k], u[k]));
             }
-            put_state();                           // far has been read: DONE_G
-            if (ENDS) continue;
-            wait_warp(DONE_OUT);
-            if (gave_up) break;
-            const float w = m.far * powers[r + 1 - m.shift];
-            __nv_bfloat16* to = (__nv_bfloat16*)m.out + ((bt * m.length + origin + dir * (t + r)) * m.heads + h) * m.dc + col0;
-#pragma unroll 1
-            for (int c = 0; c < COLS; c += 32) {
-                const int left = m.dc - col0 - c;
-                if (left <= 0) break;
-                float o[32];
-                tmem_load32(tmem + R::NEAR + lanes + col0 + c, o);
-                float odd = 0.f;
+            put_state();                       // far has been read
+        }
+        float* to = ENDS ? local : p == m.pieces - 1 && m.end != nullptr ? m.end + st : nullptr;
+        if (to != nullptr && holds && d < m.da) {
+            if (ENDS) {
 #pragma unroll
-                for (int k = 0; k < 32; ++k) odd = fmaf(o[k], 0.f, odd);
-                if (__any_sync(~0u, odd != 0.f)) {
-                    // a product with a node behind is 0 times what c holds there: an infinity or NaN is none of this row's
-                    float again[32] = {};
-                    const __nv_bfloat16* cs = (const __nv_bfloat16*)m.c.p + bt * m.c.batch + h * m.c.head + col0 + c;
-                    for (int j = 0; j < N; ++j) {
-                        const int rj = m.reversed ? N - 1 - j : j;
-                        const uint32_t two = tmem_load1(tmem + R::G + lanes + p_column(j / 16) + j % 16 / 2);
-                        const float x = j % 2 ? __uint_as_float(two & 0xffff0000u) : __uint_as_float(two << 16);
-                        if (rj <= r && r < n)
+                for (int c = 0; c < COLS; ++c)
+                    if (col0 + c < m.dc) to[(col0 + c) * m.da + d] = S[c];
+            } else if (m.dc % 4 == 0 && m.end_packed) {
 #pragma unroll
-                            for (int k = 0; k < 32; ++k)
-                                if (k < left) again[k] = fmaf(x, __bfloat162float(cs[(origin + dir * (t + rj)) * m.c.node + k]), again[k]);
+                for (int c = 0; c < COLS; c += 4)
+                    if (col0 + c < m.dc) {
+                        const float v[4] = {S[c], S[c + 1], S[c + 2], S[c + 3]};
+                        store_pack<float, 4>(to + d * m.dc + col0 + c, v);
                     }
+            } else {
 #pragma unroll
-                    for (int k = 0; k < 32; ++k)
-                        if (o[k] - o[k] != 0.f) o[k] = again[k];
-                }
-                float f[32];
-                tmem_load32(tmem + R::FAR + lanes + col0 + c, f);
-#pragma unroll
-                for (int k = 0; k < 32; ++k) o[k] = fmaf(w, f[k], o[k]);
-                if (r < n) {
-                    if (left >= 32 && m.out_packed) {
-#pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-                            uint32_t v[8];
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) v[k] = pack_bf16(o[16 * q + 2 * k], o[16 * q + 2 * k + 1]);
-                            store32(to + c + 16 * q, v);
-                        }
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 32; ++k)
-                            if (k < left) to[c + k] = __float2bfloat16_rn(o[k]);
-                    }
-                }
+                for (int c = 0; c < COLS; ++c)
+                    if (col0 + c < m.dc) to[d * m.dc + col0 + c] = S[c];
             }
-            signal(READY);
         }
     }
     const bool lost = __syncthreads_or(gave_up);
     if (lost) {                 // what has been issued has to end before the block does; the results are NaN
-        if (warp == WARPS && lane == 0) {
-            bool late = false;
+        bool late = false;
+        if (warp == 4 * GROUP_CONTROL && lane == 0) {
             mma_commit(bar(ENDED));
             mbar_wait<TRIES>(bar(ENDED), 0, late, &g_linear_timeouts);
-            if (loads_ab > 0) mbar_wait<TRIES>(bar(FULL_AB), (loads_ab - 1) & 1, late, &g_linear_timeouts);
-            if (loads_c > 0) mbar_wait<TRIES>(bar(FULL_C), (loads_c - 1) & 1, late, &g_linear_timeouts);
         }
+        if (asked_a > 0) mbar_wait<TRIES>(bar(FULL_A), (asked_a - 1) & 1, late, &g_linear_timeouts);
+        if (asked_b > 0) mbar_wait<TRIES>(bar(FULL_B), (asked_b - 1) & 1, late, &g_linear_timeouts);
+        if (asked_c > 0) mbar_wait<TRIES>(bar(FULL_C), (asked_c - 1) & 1, late, &g_linear_timeouts);
         if (!ENDS)
             for (int64_t i = first * m.dc + tid; i < last * m.dc; i += THREADS) {
                 const int64_t node = m.reversed ? m.length - 1 - i / m.dc : i / m.dc;
                 ((__nv_bfloat16*)m.out)[((bt * m.length + node) * m.heads + h) * m.dc + i % m.dc] = __float2bfloat16_rn(NAN);
             }
-#pragma unroll
-        for (int c = 0; c < COLS; ++c) S[c] = NAN;
-        __syncthreads();
-    }
-    if (holds && d < m.da) {
-        if (ENDS) {
-#pragma unroll
-            for (int c = 0; c < COLS; ++c)
-                if (col0 + c < m.dc) local[(int64_t)(col0 + c) * m.da + d] = S[c];
-        } else if (p == m.pieces - 1 && m.end != nullptr) {
-            float* to = m.end + st + (int64_t)d * m.dc + col0;
-            if (m.dc % 4 == 0 && m.end_packed) {
-#pragma unroll
-                for (int c = 0; c < COLS; c += 4)
-                    if (col0 + c < m.dc) {
-                        const float v[4] = {S[c], S[c + 1], S[c + 2], S[c + 3]};
-                        store_pack<float, 4>(to + c, v);
-                    }
-            } else {
-#pragma unroll
-                for (int c = 0; c < COLS; ++c)
-                    if (col0 + c < m.dc) to[c] = S[c];
-            }
-        }
+        float* to = ENDS ? m.local + ((bt * m.heads + h) * m.pieces + p) * m.da * m.dc
+                         : p == m.pieces - 1 && m.end != nullptr ? m.end + (bt * m.heads + h) * m.da * m.dc : nullptr;
+        for (int i = tid; to != nullptr && i < m.da * m.dc; i += THREADS) to[i] = NAN;
     }
     fence_before();
     __syncthreads();
     fence_after();
-    if (warp == WARPS) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(R::COLUMNS) : "memory");
+    if (warp == 4 * GROUP_CONTROL) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
 // ------------------------------------------------------------------------------------------- host
@@ -495,7 +526,7 @@ cudaError_t run(const March& m, const Tiles& tiles, cudaStream_t st) {
 
 }  // namespace
 
-int march_mma_blocks(const March& m) { return m.da <= 64 && m.dc <= 64 ? 2 * 148 : 148; }
+int march_mma_blocks() { return 148; }
 
 bool march_mma(const March& given, cudaStream_t st, cudaError_t* e) {
     March m = given;
