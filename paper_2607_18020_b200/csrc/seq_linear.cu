@@ -192,9 +192,7 @@ __global__ void __launch_bounds__(256) join_kernel(March m) {
     const double g = power(m.log_decay[row % m.heads], (double)m.piece);
     const float hi = (float)g, lo = (float)(g - hi);
     float s = 0.f;
-    // element (d, c) of the state
-    const int64_t d = m.local_turned ? i % m.da : i / m.dc, c = m.local_turned ? i / m.da : i % m.dc;
-    if (m.start != nullptr) s = m.start[row * size + (m.start_turned ? c * m.da + d : d * m.dc + c)];
+    if (m.start != nullptr) s = m.start[row * size + (m.start_turned ? i % m.dc * m.da + i / m.dc : i)];
     float* at = m.local + row * m.pieces * size + i;
     for (int p = 0; p < m.pieces; p += 8, at += 8 * size) {
         float u[8];

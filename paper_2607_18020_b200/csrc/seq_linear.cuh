@@ -26,8 +26,7 @@ struct March {
     int pieces;
     int64_t piece;                 // nodes of a piece
     float* local;
-    int local_turned;              // (batch, heads, pieces, dc, da) instead
-    bool start_packed, end_packed, out_packed;     // start on 16 bytes; rows of out on 32
+    bool out_packed;               // rows of out start on 32 bytes
 };
 
 // g^n for n >= 0, from 64 bits: rounded once, so that it stays exact enough when it is applied chunk after chunk.

@@ -14,10 +14,10 @@
 // decay, c is exact, U is formed of three products and the state is added up with ordinary rounding.
 //
 // Threads.  One block an SM; its warps have tasks of their own, so that a chunk's steps run beside one another and beside those of
-// the chunks before and after: four turn G into P, four turn b into bw, eight write the output and move the state on (two threads
-// for each lane of TMEM, half of the columns each), one issues the products and one loads (TMA).  A tile's place takes the next
-// chunk's as soon as the products that read it are done.  (With all warps at the same step, one after the other: 16 warps
-// that wait for one another's latencies, 11 800 cycles a chunk of 128 x 128 features at a quarter of the issue slots.)
+// the chunks before and after: eight turn G into P, eight turn b into bw, eight write the output and move the state on (two
+// threads for each lane of TMEM), one issues the products and one loads (TMA).  A tile's place takes the next chunk's as soon as
+// the products that read it are done.  (With all warps at the same step, one after the other, they wait for one another's
+// latencies: 11 800 cycles a chunk of 128 x 128 features at a quarter of the issue slots.)
 #include "mma_common.cuh"
 #include "seq_linear.cuh"
 
@@ -27,9 +27,26 @@ namespace {
 constexpr int N = MMA_CHUNK;
 constexpr int BLOCK = N * 128;                 // bytes of 64 features of a chunk
 constexpr int PARTS = 3;
-constexpr int TRIES = 1 << 20;                 // of a wait (for microseconds, in a healthy run); 20 ms at the very least
+// A wait (for microseconds, in a healthy run) gives up after TRIES tries of a microsecond each, or less where the hardware holds a
+// try for less: 0.26 s at most, 5 ms at the very least.
+constexpr int TRIES = 1 << 18, TRY_NS = 1000;
 
 __device__ unsigned int g_linear_timeouts;
+
+__device__ __forceinline__ void wait_for(uint32_t bar, uint32_t parity, bool& gave_up) {
+    if (gave_up) return;
+    for (int i = 0; i < TRIES; ++i) {
+        uint32_t done;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(done) : "r"(bar), "r"(parity), "r"(TRY_NS) : "memory");
+        if (done) return;
+    }
+    gave_up = true;
+    atomicAdd(&g_linear_timeouts, 1u);
+}
 
 template <int DA, int DC>
 struct Room {
@@ -37,10 +54,12 @@ struct Room {
     static constexpr int BYTES = S + DC / 64 * DA * 128 + 1024;      // slack to start on 1024 bytes
     static constexpr int G = 0, NEAR = 128, FAR = NEAR + DC, U = FAR + DC;      // columns of TMEM; P lies over G
 };
-// Warps, in groups of four, and their registers: 640 threads start with 96 each.
-constexpr int GROUP_P = 0, GROUP_BW = 1, GROUP_OUT = 2, GROUP_CONTROL = 4, THREADS = 5 * 128;
-constexpr int OUT_WARPS = 8, OUT_REGS = 144, OTHER_REGS = 64;
-static_assert(2 * OUT_REGS + 3 * OTHER_REGS <= 5 * 96, "the groups share what the block starts with");
+// Groups of eight warps, the last of four, and their registers: 896 threads start with 72 each.
+constexpr int GROUP_P = 0, GROUP_BW = 1, GROUP_OUT = 2, GROUP_CONTROL = 3, CONTROL = 24, THREADS = 28 * 32;
+constexpr int OUT_REGS = 128, OTHER_REGS = 48;
+static_assert(256 * OUT_REGS + 640 * OTHER_REGS <= THREADS * 72, "the groups share what the block starts with");
+// P lies over G, each 32 columns' 16 over their own: the column of 16 nodes' products.
+__host__ __device__ constexpr int p_column(int k) { return 32 * (k / 2) + 8 * (k % 2); }
 
 // Barriers.  FULL: a tile has arrived; DONE: the products up to these are done; READY: warps have written what products read;
 // FREE: warps have read what products write.
@@ -69,24 +88,36 @@ __device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uin
         "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
         : "memory");
 }
-__device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(r[0]), "r"(r[1]),
-        "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
-        "r"(r[15]), "r"(addr)
-        : "memory");
+__device__ __forceinline__ void tmem_store8(uint32_t addr, const uint32_t (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]),
+                 "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(addr)
+                 : "memory");
 }
-__device__ __forceinline__ void tmem_load(uint32_t addr, float (&v)[32]) { tmem_load32(addr, v); }
-__device__ __forceinline__ void tmem_load(uint32_t addr, float (&v)[16]) {
-    uint32_t r[16];
+__device__ __forceinline__ void tmem_ask16(uint32_t addr, uint32_t (&r)[16]) {          // there after tmem_asked()
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
           "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(addr));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_asked() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_load(uint32_t addr, float (&v)[16]) {
+    uint32_t r[16];
+    tmem_ask16(addr, r);
+    tmem_asked();
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_load_both(uint32_t addr, float (&v)[16], uint32_t other, float (&w)[16]) {
+    uint32_t r[16], q[16];
+    tmem_ask16(addr, r);
+    tmem_ask16(other, q);
+    tmem_asked();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        v[i] = __uint_as_float(r[i]);
+        w[i] = __uint_as_float(q[i]);
+    }
 }
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint32_t tmem_load1(uint32_t addr) {
@@ -127,17 +158,15 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
     __shared__ __align__(8) uint64_t bars[BARS];
     __shared__ uint32_t tmem_slot;
     __shared__ __align__(16) float powers[N + 2];
-    __shared__ float falling[64], rising[64];                    // g^(31 - i) and g^(i - 31), 0 where that is no power
     __shared__ float whole[4];                                   // g^128 and that of the last chunk, each in two parts
     const uint32_t base = (smem_u32(raw) + 1023) & ~1023u;
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, group = warp / 4, quarter = warp % 4;
-    const int BW_WARPS = ENDS ? 8 : 4;                           // without P its warps help with bw
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, group = warp / 8, half = warp / 4 % 2, quarter = warp % 4;
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     if (tid == 0) {
-        for (int i = 0; i < BARS; ++i) mbar_init(bar(i), i == READY_P ? 4 : i == READY_BW ? BW_WARPS : i == READY_S || i == FREE_OUT ? OUT_WARPS : 1);
+        for (int i = 0; i < BARS; ++i) mbar_init(bar(i), i == READY_P || i == READY_BW || i == READY_S || i == FREE_OUT ? 8 : 1);
         mbar_fence_init();
     }
-    if (warp == 4 * GROUP_CONTROL) {
+    if (warp == CONTROL) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_slot)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -148,23 +177,35 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
     id /= m.pieces;
     const int64_t h = id % m.heads, bt = id / m.heads;
     const int64_t first = p * m.piece, last = min(m.length, first + m.piece);
+    const float ld = m.log_decay[h];
     {
-        const float ld = m.log_decay[h];
-        if (tid < N + 2) {
-            const float g = (float)power(ld, tid);
-            powers[tid] = g;
-            if (tid < 32) {
-                falling[31 - tid] = rising[31 + tid] = g;
-                falling[32 + tid] = 0.f;
-                if (tid < 31) rising[tid] = 0.f;
-                if (tid == 31) rising[63] = 0.f;
-            }
-        }
+        if (tid < N + 2) powers[tid] = (float)power(ld, tid);
         if (tid >= 192 && tid < 194) {
             const double g = power(ld, tid == 192 ? N : last > first ? (int)((last - first - 1) % N) + 1 : 0);
             whole[2 * (tid - 192)] = (float)g;
             whole[2 * (tid - 192) + 1] = (float)(g - (float)g);
         }
+    }
+    // The state comes and goes through bw's place, along its rows or, turned, its columns.
+    constexpr int PITCH = DC + 1;
+    static_assert(DA * PITCH * 4 <= PARTS * (DA / 64) * BLOCK, "the state fits bw's place");
+    float* stage = reinterpret_cast<float*>(raw + (base - smem_u32(raw)) + R::BW);
+    const int64_t st = (bt * m.heads + h) * m.da * m.dc;
+    float* local = m.local + ((bt * m.heads + h) * m.pieces + p) * m.da * m.dc;
+    if (!ENDS) {
+        const float* from = m.pieces > 1 ? local : m.start != nullptr ? m.start + st : nullptr;
+        const bool turned = m.pieces == 1 && m.start_turned;
+        const int across = turned ? m.da : m.dc;
+        if (from == nullptr || m.da < DA || m.dc < DC) {
+            for (int i = tid; i < DA * PITCH; i += THREADS) stage[i] = 0.f;
+            __syncthreads();
+        }
+        if (from != nullptr)
+#pragma unroll 4
+            for (int i = tid; i < m.da * m.dc; i += THREADS) {
+                const int a = i / across, b = i - a * across;
+                stage[turned ? b * PITCH + a : a * PITCH + b] = from[i];
+            }
     }
     fence_before();
     __syncthreads();
@@ -173,8 +214,8 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
     uint32_t phase = 0;
     bool gave_up = false;
     int asked_a = 0, asked_b = 0, asked_c = 0; // tiles that this thread has asked for
-    auto wait = [&](int i) { mbar_wait<TRIES>(bar(i), phase, gave_up, &g_linear_timeouts); };
-    auto wait_last = [&](int i) { mbar_wait<TRIES>(bar(i), phase ^ 1, gave_up, &g_linear_timeouts); };      // of the chunk before
+    auto wait = [&](int i) { wait_for(bar(i), phase, gave_up); };
+    auto wait_last = [&](int i) { wait_for(bar(i), phase ^ 1, gave_up); };      // of the chunk before
     auto wait_warp = [&](int i) {
         wait(i);
         gave_up = __any_sync(~0u, gave_up);
@@ -219,7 +260,7 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                     if (gave_up) break;
                     fence_after();
 #pragma unroll
-                    for (int k = 0; k < N / 16; ++k) mma_tmem(tmem + R::NEAR, tmem + R::G + 8 * k, desc_at(dc, k * 2048), IDESC_OUT, k > 0);
+                    for (int k = 0; k < N / 16; ++k) mma_tmem(tmem + R::NEAR, tmem + R::G + p_column(k), desc_at(dc, k * 2048), IDESC_OUT, k > 0);
                     mma_commit(bar(DONE_NEAR));
                 } else {
                     wait(READY_S);
@@ -261,32 +302,31 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                 if (t > first) phase ^= 1;
             }
         }
-    } else if (group == GROUP_BW || (ENDS && group == GROUP_P)) {
+    } else if (group == GROUP_BW) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
         for (int64_t t = first; t < last; t += N, phase ^= 1) {
             const int n = (int)min((int64_t)N, last - t);
             wait_warp(FULL_B);
-            if (t > first) {                   // bw's place is the last chunk's until U is done
-                wait_last(DONE_U);
-                gave_up = __any_sync(~0u, gave_up);
-            }
+            // bw's place is the last chunk's until U is done, the state's before that
+            if (t > first) wait_last(DONE_U);
+            else wait(READY_S);
+            gave_up = __any_sync(~0u, gave_up);
             if (gave_up) break;
             const float w = r < n ? m.gain * powers[n - 1 - r + m.shift] : 0.f;
-            constexpr int EACH = ENDS ? DA / 16 : DA / 8;
-#pragma unroll 4
-            for (int e = 0; e < EACH; ++e) {
-                const int q = (ENDS ? group * EACH : 0) + e;
+#pragma unroll 1
+            for (int q = half * (DA / 16); q < (half + 1) * (DA / 16); ++q) {
                 const uint4 v = lds16(chunk_at(base + R::B, row, q));
                 const uint32_t in[4] = {v.x, v.y, v.z, v.w};
                 uint32_t out[PARTS][4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    float lo = __uint_as_float(in[k] << 16) * w, hi = __uint_as_float(in[k] & 0xffff0000u) * w;
+                    uint64_t x = mul2(pair(__uint_as_float(in[k] << 16), __uint_as_float(in[k] & 0xffff0000u)), both(w));
 #pragma unroll
                     for (int s = 0; s < PARTS; ++s) {          // the top 8 bits of what is left, exactly
+                        float lo, hi;
+                        unpair(x, lo, hi);
                         out[s][k] = tops(lo, hi);
-                        lo -= top_part(lo);
-                        hi -= top_part(hi);
+                        if (s < PARTS - 1) x = add2(x, pair(-top_part(lo), -top_part(hi)));
                     }
                 }
 #pragma unroll
@@ -297,31 +337,29 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
         }
     } else if (group == GROUP_P) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
-        for (int64_t t = first; t < last; t += N, phase ^= 1) {
+        // g^n as 2^(n log2 g), good to 2^-22 or, far back, to n log2 g 2^-24 of itself; the least finite number stands for log 0,
+        // of which 2^(0 x) has to be 1
+        const float l2 = fmaxf(ld * LOG2_E, -3e38f);
+        for (int64_t t = first; !ENDS && t < last; t += N, phase ^= 1) {
             wait_warp(DONE_G);
             if (gave_up) break;
-            // 32 columns at a time: those of this quarter's own nodes are cut along the diagonal, those of the nodes before them
-            // are whole, the others zeros.  Column k of the 32 is g^(32 before + lane - k), or + k - lane, times the product.  A thread
-            // has a lane of G for itself, and P's columns are behind those that it still has to read.
+            // 32 columns at a time, a thread every other: those of this quarter's own nodes are cut along the diagonal, those of the
+            // nodes before them are whole, the others zeros.  Column k of the 32 is the product times g^(32 before + lane - k), or + k - lane.
 #pragma unroll 1
-            for (int part = 0; part < 4; ++part) {
-                const int before = m.reversed ? part - quarter : quarter - part;
-                const float* table = before == 0 ? (m.reversed ? rising + 31 - lane : falling + 31 - lane) : (m.reversed ? rising + 31 : falling);
-                const float w = before > 0 ? m.near * powers[32 * before + (m.reversed ? -lane : lane - 31)] : m.near;
-                const uint32_t there = before > 0 ? ~0u : m.reversed ? ~0u << lane : (2u << lane) - 1u;
-                uint32_t packed[16];
+            for (int e = 0; e < 4; ++e) {
+                const int part = e / 2 * 2 + half, c = e % 2 * 16, before = m.reversed ? part - quarter : quarter - part;
+                uint32_t packed[8] = {};
                 if (before >= 0) {
-                    float v[32];
-                    tmem_load32(tmem + R::G + lanes + part * 32, v);
+                    const uint32_t there = (before > 0 ? ~0u : m.reversed ? ~0u << lane : (2u << lane) - 1u) >> c;
+                    const float from = 32 * before + (m.reversed ? c - lane : lane - c), step = m.reversed ? 1.f : -1.f;
+                    float v[16];
+                    tmem_load(tmem + R::G + lanes + part * 32 + c, v);
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) v[k] = (there >> k & 1u) != 0 ? v[k] * (w * table[k]) : 0.f;
+                    for (int k = 0; k < 16; ++k) v[k] = (there >> k & 1u) != 0 ? v[k] * exp2_f32(fmaf(k, step, from) * l2) : 0.f;
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) packed[k] = pack_bf16(v[2 * k], v[2 * k + 1]);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) packed[k] = 0;
+                    for (int k = 0; k < 8; ++k) packed[k] = pack_bf16(v[2 * k], v[2 * k + 1]);
                 }
-                tmem_store16(tmem + R::G + part * 16 + lanes, packed);
+                tmem_store8(tmem + R::G + p_column(2 * part) + c / 2 + lanes, packed);
             }
             tmem_stored();
             signal(READY_P);
@@ -331,35 +369,10 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
         // The state: row d, half of the columns.  With 64 rows the products use 16 lanes of each quarter.
         constexpr int COLS = DC / 2;
         const bool holds = DA == 128 || lane < 16;
-        const int d = DA == 128 ? quarter * 32 + lane : quarter * 16 + lane, col0 = (group - GROUP_OUT) * COLS;
-        const int64_t st = (bt * m.heads + h) * m.da * m.dc;
-        float* local = m.local + ((bt * m.heads + h) * m.pieces + p) * m.da * m.dc;      // by columns: neighbouring lanes are neighbours there
+        const int d = DA == 128 ? quarter * 32 + lane : quarter * 16 + lane, col0 = half * COLS;
         float S[COLS];
 #pragma unroll
-        for (int c = 0; c < COLS; ++c) S[c] = 0.f;
-        if (!ENDS && holds && d < m.da) {
-            if (m.pieces > 1 || (m.start != nullptr && m.start_turned)) {
-                const float* from = m.pieces > 1 ? local : m.start + st;
-#pragma unroll
-                for (int c = 0; c < COLS; ++c)
-                    if (col0 + c < m.dc) S[c] = from[(col0 + c) * m.da + d];
-            } else if (m.start != nullptr) {
-                const float* from = m.start + st + d * m.dc + col0;
-                if (m.dc % 4 == 0 && m.start_packed) {
-#pragma unroll
-                    for (int c = 0; c < COLS; c += 4)
-                        if (col0 + c < m.dc) {
-                            const Pack<float, 4> v = load_pack<float, 4>(from + c);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) S[c + e] = v.v[e];
-                        }
-                } else {
-#pragma unroll
-                    for (int c = 0; c < COLS; ++c)
-                        if (col0 + c < m.dc) S[c] = from[c];
-                }
-            }
-        }
+        for (int c = 0; c < COLS; ++c) S[c] = ENDS ? 0.f : stage[min(d, DA - 1) * PITCH + col0 + c];
         auto put_state = [&]() {               // the factor of `far`
             if (!ENDS && holds) {
 #pragma unroll
@@ -384,31 +397,41 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                     const int left = m.dc - col0 - c;
                     if (left <= 0) break;
                     float o[16], f[16];
-                    tmem_load(tmem + R::NEAR + lanes + col0 + c, o);
-                    tmem_load(tmem + R::FAR + lanes + col0 + c, f);
-                    float odd = 0.f;
+                    tmem_load_both(tmem + R::NEAR + lanes + col0 + c, o, tmem + R::FAR + lanes + col0 + c, f);
+                    uint64_t odd = both(0.f), more = both(0.f);
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) odd = fmaf(o[k], 0.f, odd);
-                    if (__any_sync(~0u, odd != 0.f)) {
+                    for (int k = 0; k < 16; k += 4) {
+                        odd = fma2(pair(o[k], o[k + 1]), both(0.f), odd);
+                        more = fma2(pair(o[k + 2], o[k + 3]), both(0.f), more);
+                    }
+                    if (__any_sync(~0u, sum2(add2(odd, more)) != 0.f)) {
                         // a product with a node behind is 0 times what c holds there: an infinity or NaN is none of this row's
                         float again[16] = {};
                         const __nv_bfloat16* cs = (const __nv_bfloat16*)m.c.p + bt * m.c.batch + h * m.c.head + col0 + c;
-#pragma unroll 1
-                        for (int j = 0; j < N; ++j) {
-                            const int rj = m.reversed ? N - 1 - j : j;
-                            const uint32_t two = tmem_load1(tmem + R::G + lanes + j / 2);
-                            const float x = j % 2 ? __uint_as_float(two & 0xffff0000u) : __uint_as_float(two << 16);
-                            if (rj <= r && r < n)
+                        uint32_t bad = 0;      // features that are none in a row, and those that a node up to j has made so
 #pragma unroll
-                                for (int k = 0; k < 16; ++k)
-                                    if (k < left) again[k] = fmaf(x, __bfloat162float(cs[(origin + dir * (t + rj)) * m.c.node + k]), again[k]);
+                        for (int k = 0; k < 16; ++k) bad |= (o[k] - o[k] != 0.f) << k;
+                        bad = __reduce_or_sync(~0u, bad);
+#pragma unroll 1
+                        for (int j = 0; j < N && bad != 0; ++j) {
+                            const int at = m.reversed ? N - 1 - j : j;
+                            const uint32_t two = tmem_load1(tmem + R::G + lanes + p_column(at / 16) + at % 16 / 2);
+                            const float x = at % 2 ? __uint_as_float(two & 0xffff0000u) : __uint_as_float(two << 16);
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) {
+                                const float y = j < n && k < left ? __bfloat162float(cs[(origin + dir * (t + j)) * m.c.node + k]) : 0.f;
+                                if (j <= r) again[k] = fmaf(x, y, again[k]);
+                                if (y - y != 0.f) bad &= ~(1u << k);
+                            }
                         }
+                        // a row that comes before j has its sum; in the others an infinity or NaN is their own
 #pragma unroll
                         for (int k = 0; k < 16; ++k)
                             if (o[k] - o[k] != 0.f) o[k] = again[k];
+                        tmem_load(tmem + R::FAR + lanes + col0 + c, f);      // once more, rather than kept meanwhile
                     }
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) o[k] = fmaf(w, f[k], o[k]);
+                    for (int k = 0; k < 16; ++k) o[k] = fmaf(m.near, o[k], w * f[k]);
                     if (r < n) {
                         if (left >= 16 && m.out_packed) {
                             uint32_t v[8];
@@ -428,57 +451,42 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
             if (gave_up) break;
             const float hi = whole[n == N ? 0 : 2], lo = whole[n == N ? 1 : 3];
 #pragma unroll
-            for (int c = 0; c < COLS; c += 16) {
-                float u[16];
-                tmem_load(tmem + R::U + lanes + col0 + c, u);
+            for (int c = 0; c < COLS; c += 32) {
+                float u[32];
+                tmem_load32(tmem + R::U + lanes + col0 + c, u);
 #pragma unroll
-                for (int k = 0; k < 16; ++k) S[c + k] = fmaf(hi, S[c + k], fmaf(lo, S[c + k], u[k]));
+                for (int k = 0; k < 32; ++k) S[c + k] = fmaf(hi, S[c + k], fmaf(lo, S[c + k], u[k]));
             }
             put_state();                       // far has been read
         }
-        float* to = ENDS ? local : p == m.pieces - 1 && m.end != nullptr ? m.end + st : nullptr;
-        if (to != nullptr && holds && d < m.da) {
-            if (ENDS) {
+        if (holds)
 #pragma unroll
-                for (int c = 0; c < COLS; ++c)
-                    if (col0 + c < m.dc) to[(col0 + c) * m.da + d] = S[c];
-            } else if (m.dc % 4 == 0 && m.end_packed) {
-#pragma unroll
-                for (int c = 0; c < COLS; c += 4)
-                    if (col0 + c < m.dc) {
-                        const float v[4] = {S[c], S[c + 1], S[c + 2], S[c + 3]};
-                        store_pack<float, 4>(to + d * m.dc + col0 + c, v);
-                    }
-            } else {
-#pragma unroll
-                for (int c = 0; c < COLS; ++c)
-                    if (col0 + c < m.dc) to[d * m.dc + col0 + c] = S[c];
-            }
-        }
+            for (int c = 0; c < COLS; ++c) stage[d * PITCH + col0 + c] = S[c];      // U is done, and with it all that read bw
     }
     const bool lost = __syncthreads_or(gave_up);
     if (lost) {                 // what has been issued has to end before the block does; the results are NaN
         bool late = false;
-        if (warp == 4 * GROUP_CONTROL && lane == 0) {
+        if (warp == CONTROL && lane == 0) {
             mma_commit(bar(ENDED));
-            mbar_wait<TRIES>(bar(ENDED), 0, late, &g_linear_timeouts);
+            wait_for(bar(ENDED), 0, late);
         }
-        if (asked_a > 0) mbar_wait<TRIES>(bar(FULL_A), (asked_a - 1) & 1, late, &g_linear_timeouts);
-        if (asked_b > 0) mbar_wait<TRIES>(bar(FULL_B), (asked_b - 1) & 1, late, &g_linear_timeouts);
-        if (asked_c > 0) mbar_wait<TRIES>(bar(FULL_C), (asked_c - 1) & 1, late, &g_linear_timeouts);
+        if (asked_a > 0) wait_for(bar(FULL_A), (asked_a - 1) & 1, late);
+        if (asked_b > 0) wait_for(bar(FULL_B), (asked_b - 1) & 1, late);
+        if (asked_c > 0) wait_for(bar(FULL_C), (asked_c - 1) & 1, late);
         if (!ENDS)
             for (int64_t i = first * m.dc + tid; i < last * m.dc; i += THREADS) {
                 const int64_t node = m.reversed ? m.length - 1 - i / m.dc : i / m.dc;
                 ((__nv_bfloat16*)m.out)[((bt * m.length + node) * m.heads + h) * m.dc + i % m.dc] = __float2bfloat16_rn(NAN);
             }
-        float* to = ENDS ? m.local + ((bt * m.heads + h) * m.pieces + p) * m.da * m.dc
-                         : p == m.pieces - 1 && m.end != nullptr ? m.end + (bt * m.heads + h) * m.da * m.dc : nullptr;
-        for (int i = tid; to != nullptr && i < m.da * m.dc; i += THREADS) to[i] = NAN;
     }
+    float* to = ENDS ? local : p == m.pieces - 1 && m.end != nullptr ? m.end + st : nullptr;
+    if (to != nullptr)
+#pragma unroll 4
+        for (int i = tid; i < m.da * m.dc; i += THREADS) to[i] = lost ? NAN : stage[i / m.dc * PITCH + i % m.dc];
     fence_before();
     __syncthreads();
     fence_after();
-    if (warp == 4 * GROUP_CONTROL) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    if (warp == CONTROL) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
 // ------------------------------------------------------------------------------------------- host
@@ -535,9 +543,6 @@ bool march_mma(const March& given, cudaStream_t st, cudaError_t* e) {
         !tile_map(m.b, m.da, m.heads, m.length, m.batch, &tiles.b, &tiles.head_b, &tiles.batch_b) ||
         !tile_map(m.c, m.dc, m.heads, m.length, m.batch, &tiles.c, &tiles.head_c, &tiles.batch_c))
         return false;
-    m.local_turned = 1;
-    m.start_packed = aligned(m.start, 16);
-    m.end_packed = aligned(m.end, 16);
     m.out_packed = m.dc % 16 == 0 && aligned(m.out, 32);
     if (m.dc <= 64) *e = m.da <= 64 ? run<64, 64>(m, tiles, st) : run<128, 64>(m, tiles, st);
     else *e = m.da <= 64 ? run<64, 128>(m, tiles, st) : run<128, 128>(m, tiles, st);
