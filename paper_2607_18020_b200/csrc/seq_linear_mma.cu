@@ -35,6 +35,7 @@ __device__ unsigned int g_linear_timeouts;
 
 __device__ __forceinline__ void wait_for(uint32_t bar, uint32_t parity, bool& gave_up) {
     if (gave_up) return;
+#pragma unroll 1
     for (int i = 0; i < TRIES; ++i) {
         uint32_t done;
         asm volatile(
@@ -81,12 +82,26 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-// D += A B with A in TMEM: 16 bf16 of each row, two a column.
-__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+// D += A B, by the one lane of a warp that asks for it; all come here, so that operands are the warp's.  An instruction's operands
+// are moved one by one otherwise: 100 clocks a product in a loop of one thread, against the 64 that it takes.
+__device__ __forceinline__ void product(bool leader, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add), "r"((uint32_t)leader)
         : "memory");
+}
+// The same with A in TMEM: 16 bf16 of each row, two a column.
+__device__ __forceinline__ void product_tmem(bool leader, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add),
+        "r"((uint32_t)leader)
+        : "memory");
+}
+__device__ __forceinline__ bool elected() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
 }
 __device__ __forceinline__ void tmem_store8(uint32_t addr, const uint32_t (&r)[8]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]),
@@ -158,11 +173,13 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
     __shared__ __align__(8) uint64_t bars[BARS];
     __shared__ uint32_t tmem_slot;
     __shared__ __align__(16) float powers[N + 2];
+    __shared__ int odd_chunk[2];                                 // the last chunk of either parity with an infinity or NaN in c, counted from 1
     __shared__ float whole[4];                                   // g^128 and that of the last chunk, each in two parts
     const uint32_t base = (smem_u32(raw) + 1023) & ~1023u;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, group = warp / 8, half = warp / 4 % 2, quarter = warp % 4;
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     if (tid == 0) {
+        odd_chunk[0] = odd_chunk[1] = 0;
         for (int i = 0; i < BARS; ++i) mbar_init(bar(i), i == READY_P || i == READY_BW || i == READY_S || i == FREE_OUT ? 8 : 1);
         mbar_fence_init();
     }
@@ -172,18 +189,21 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
     }
     pdl_wait_then_trigger();
 
-    int64_t id = blockIdx.x;
-    const int p = (int)(id % m.pieces);
-    id /= m.pieces;
-    const int64_t h = id % m.heads, bt = id / m.heads;
+    const unsigned rest = blockIdx.x / (unsigned)m.pieces;
+    const int p = (int)(blockIdx.x - rest * m.pieces);
+    const int64_t bt = rest / (unsigned)m.heads, h = rest - (unsigned)bt * (unsigned)m.heads;
     const int64_t first = p * m.piece, last = min(m.length, first + m.piece);
     const float ld = m.log_decay[h];
     {
-        if (tid < N + 2) powers[tid] = (float)power(ld, tid);
-        if (tid >= 192 && tid < 194) {
-            const double g = power(ld, tid == 192 ? N : last > first ? (int)((last - first - 1) % N) + 1 : 0);
-            whole[2 * (tid - 192)] = (float)g;
-            whole[2 * (tid - 192) + 1] = (float)(g - (float)g);
+        const int tail = last > first ? (int)((last - first - 1) % N) + 1 : 0;
+        if (tid < N + 4) {
+            const double g = power(ld, tid < N + 2 ? tid : tid == N + 2 ? N : tail);
+            if (tid < N + 2) {
+                powers[tid] = (float)g;
+            } else {
+                whole[2 * (tid - N - 2)] = (float)g;
+                whole[2 * (tid - N - 2) + 1] = (float)(g - (float)g);
+            }
         }
     }
     // The state comes and goes through bw's place, along its rows or, turned, its columns.
@@ -210,7 +230,7 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
     fence_before();
     __syncthreads();
     fence_after();
-    const uint32_t tmem = tmem_slot;
+    constexpr uint32_t tmem = 0;               // all 512 columns: they start there
     uint32_t phase = 0;
     bool gave_up = false;
     int asked_a = 0, asked_b = 0, asked_c = 0; // tiles that this thread has asked for
@@ -235,47 +255,57 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
         constexpr uint32_t IDESC = 1u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(128 / 16) << 24;      // fp32 sums of bf16 factors, 128 rows
         constexpr uint32_t IDESC_G = IDESC | (uint32_t)(N / 8) << 17, IDESC_OUT = IDESC | 1u << 16 | (uint32_t)(DC / 8) << 17;
         constexpr uint32_t IDESC_U = 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | (uint32_t)(DC / 8) << 17 | (uint32_t)(DA / 16) << 24;
-        if (quarter == 0 && lane == 0) {       // products
+        if (__shfl_sync(~0u, quarter, 0) == 0) {               // products
             const uint64_t da = slice_desc(base + R::A, false), db = slice_desc(base + R::B, false), dc = slice_desc(base + R::V, true, BLOCK),
-                           ds = slice_desc(base + R::S, true, DA * 128);
+                           ds = slice_desc(base + R::S, true, DA * 128), dw = slice_desc(base + R::BW, true, BLOCK);
+            const bool leader = elected();
+            auto commit = [&](int i) {
+                if (leader) mma_commit(bar(i));
+            };
+            auto all_wait = [&]() {
+                __syncwarp();
+                gave_up = __any_sync(~0u, gave_up);
+                fence_after();
+            };
             for (int64_t t = first; t < last; t += N, phase ^= 1) {
                 if (!ENDS) {
                     wait(FULL_A);
                     wait(FULL_B);
-                    if (t > first) wait_last(FREE_OUT);
+                    if (t > first && *(volatile int*)&odd_chunk[phase ^ 1] == (int)((t - first) / N)) wait_last(FREE_OUT);      // P is still read
+                    all_wait();
                     if (gave_up) break;
-                    fence_after();
 #pragma unroll
                     for (int k = 0; k < DA / 16; ++k)
-                        mma_f16(tmem + R::G, desc_at(da, k / 4 * BLOCK + k % 4 * 32), desc_at(db, k / 4 * BLOCK + k % 4 * 32), IDESC_G, k > 0);
-                    mma_commit(bar(DONE_G));
+                        product(leader, tmem + R::G, desc_at(da, k / 4 * BLOCK + k % 4 * 32), desc_at(db, k / 4 * BLOCK + k % 4 * 32), IDESC_G, k > 0);
+                    commit(DONE_G);
                     wait(READY_S);             // of the state before this chunk
+                    if (t > first) wait_last(FREE_OUT);
+                    all_wait();
                     if (gave_up) break;
-                    fence_after();
 #pragma unroll
-                    for (int k = 0; k < DA / 16; ++k) mma_f16(tmem + R::FAR, desc_at(da, k / 4 * BLOCK + k % 4 * 32), desc_at(ds, k * 2048), IDESC_OUT, k > 0);
-                    mma_commit(bar(DONE_FAR));
+                    for (int k = 0; k < DA / 16; ++k)
+                        product(leader, tmem + R::FAR, desc_at(da, k / 4 * BLOCK + k % 4 * 32), desc_at(ds, k * 2048), IDESC_OUT, k > 0);
+                    commit(DONE_FAR);
                     wait(READY_P);
                     wait(FULL_C);
+                    all_wait();
                     if (gave_up) break;
-                    fence_after();
 #pragma unroll
-                    for (int k = 0; k < N / 16; ++k) mma_tmem(tmem + R::NEAR, tmem + R::G + p_column(k), desc_at(dc, k * 2048), IDESC_OUT, k > 0);
-                    mma_commit(bar(DONE_NEAR));
+                    for (int k = 0; k < N / 16; ++k) product_tmem(leader, tmem + R::NEAR, tmem + R::G + p_column(k), desc_at(dc, k * 2048), IDESC_OUT, k > 0);
+                    commit(DONE_NEAR);
                 } else {
                     wait(READY_S);
                     wait(FULL_C);
                 }
                 wait(READY_BW);
+                all_wait();
                 if (gave_up) break;
-                fence_after();
 #pragma unroll
-                for (int s = PARTS - 1; s >= 0; --s) {         // the small parts first: the sum is rounded towards zero at every product
-                    const uint64_t dw = slice_desc(base + R::BW + s * (DA / 64) * BLOCK, true, BLOCK);
+                for (int s = PARTS - 1; s >= 0; --s)           // the small parts first: the sum is rounded towards zero at every product
 #pragma unroll
-                    for (int k = 0; k < N / 16; ++k) mma_f16(tmem + R::U, desc_at(dw, k * 2048), desc_at(dc, k * 2048), IDESC_U, s < PARTS - 1 || k > 0);
-                }
-                mma_commit(bar(DONE_U));
+                    for (int k = 0; k < N / 16; ++k)
+                        product(leader, tmem + R::U, desc_at(dw, s * (DA / 64) * BLOCK + k * 2048), desc_at(dc, k * 2048), IDESC_U, s < PARTS - 1 || k > 0);
+                commit(DONE_U);
             }
         } else if (quarter == 1 && lane == 0) {                // tiles
             auto load = [&](int full, int at, int blocks, const CUtensorMap* map, int head, int batch, int64_t t) {
@@ -350,17 +380,32 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                 const int part = e / 2 * 2 + half, c = e % 2 * 16, before = m.reversed ? part - quarter : quarter - part;
                 uint32_t packed[8] = {};
                 if (before >= 0) {
-                    const uint32_t there = (before > 0 ? ~0u : m.reversed ? ~0u << lane : (2u << lane) - 1u) >> c;
-                    const float from = 32 * before + (m.reversed ? c - lane : lane - c), step = m.reversed ? 1.f : -1.f;
                     float v[16];
                     tmem_load(tmem + R::G + lanes + part * 32 + c, v);
+                    const float from = 32 * before + (m.reversed ? c - lane : lane - c), step = m.reversed ? 1.f : -1.f;
+                    if (before > 0) {
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) v[k] = (there >> k & 1u) != 0 ? v[k] * exp2_f32(fmaf(k, step, from) * l2) : 0.f;
+                        for (int k = 0; k < 16; ++k) v[k] *= exp2_f32(fmaf(k, step, from) * l2);
+                    } else {
+                        const uint32_t there = (m.reversed ? ~0u << lane : (2u << lane) - 1u) >> c;
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) v[k] = (there >> k & 1u) != 0 ? v[k] * exp2_f32(fmaf(k, step, from) * l2) : 0.f;
+                    }
 #pragma unroll
                     for (int k = 0; k < 8; ++k) packed[k] = pack_bf16(v[2 * k], v[2 * k + 1]);
                 }
                 tmem_store8(tmem + R::G + p_column(2 * part) + c / 2 + lanes, packed);
             }
+            // an infinity or NaN in c makes NaN of P's zeros for the nodes before it: their rows are summed again
+            wait_warp(FULL_C);
+            if (gave_up) break;
+            uint32_t most = 0;
+#pragma unroll 2
+            for (int q = half * (DC / 16); q < (half + 1) * (DC / 16); ++q) {
+                const uint4 v = lds16(chunk_at(base + R::V, row, q));
+                most = __vmaxu2(most, __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu)));
+            }
+            if ((most >> 16) >= 0x7f80u || (most & 0xffffu) >= 0x7f80u) odd_chunk[phase] = (int)((t - first) / N) + 1;
             tmem_stored();
             signal(READY_P);
         }
@@ -388,8 +433,10 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
         for (int64_t t = first; t < last; t += N, phase ^= 1) {
             const int n = (int)min((int64_t)N, last - t);
             if (!ENDS) {
+                wait(READY_P);                 // for odd_chunk
                 wait_warp(DONE_NEAR);
                 if (gave_up) break;
+                const bool odd = *(volatile int*)&odd_chunk[phase] == (int)((t - first) / N) + 1;
                 const float w = m.far * powers[r + 1 - m.shift];
                 __nv_bfloat16* to = (__nv_bfloat16*)m.out + ((bt * m.length + origin + dir * (t + r)) * m.heads + h) * m.dc + col0;
 #pragma unroll 1
@@ -398,13 +445,7 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                     if (left <= 0) break;
                     float o[16], f[16];
                     tmem_load_both(tmem + R::NEAR + lanes + col0 + c, o, tmem + R::FAR + lanes + col0 + c, f);
-                    uint64_t odd = both(0.f), more = both(0.f);
-#pragma unroll
-                    for (int k = 0; k < 16; k += 4) {
-                        odd = fma2(pair(o[k], o[k + 1]), both(0.f), odd);
-                        more = fma2(pair(o[k + 2], o[k + 3]), both(0.f), more);
-                    }
-                    if (__any_sync(~0u, sum2(add2(odd, more)) != 0.f)) {
+                    if (odd) {
                         // a product with a node behind is 0 times what c holds there: an infinity or NaN is none of this row's
                         float again[16] = {};
                         const __nv_bfloat16* cs = (const __nv_bfloat16*)m.c.p + bt * m.c.batch + h * m.c.head + col0 + c;
@@ -431,7 +472,7 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                         tmem_load(tmem + R::FAR + lanes + col0 + c, f);      // once more, rather than kept meanwhile
                     }
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) o[k] = fmaf(m.near, o[k], w * f[k]);
+                    for (int k = 0; k < 16; k += 2) unpair(fma2(pair(o[k], o[k + 1]), both(m.near), mul2(pair(f[k], f[k + 1]), both(w))), o[k], o[k + 1]);
                     if (r < n) {
                         if (left >= 16 && m.out_packed) {
                             uint32_t v[8];
@@ -455,7 +496,10 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                 float u[32];
                 tmem_load32(tmem + R::U + lanes + col0 + c, u);
 #pragma unroll
-                for (int k = 0; k < 32; ++k) S[c + k] = fmaf(hi, S[c + k], fmaf(lo, S[c + k], u[k]));
+                for (int k = 0; k < 32; k += 2) {
+                    const uint64_t x = pair(S[c + k], S[c + k + 1]);
+                    unpair(fma2(both(hi), x, fma2(both(lo), x, pair(u[k], u[k + 1]))), S[c + k], S[c + k + 1]);
+                }
             }
             put_state();                       // far has been read
         }
