@@ -11,7 +11,8 @@
 //
 // Roundings to fewer bits.  P and the S that `far` reads are single bf16 factors: each moves a bf16 result by about as much as
 // its own rounding, and nothing else.  The state itself stays fp32: bw is three bf16 parts that hold all 24 bits of b times its
-// decay, c is exact, U is formed of three products and the state is added up with ordinary rounding.
+// decay, c is exact, U is formed of three products and the state is added up with ordinary rounding.  In a march whose last
+// state nobody takes (gq and gk) bw is two parts of 8 bits, a hundredth of the rounding that the state sees in `far`.
 //
 // Threads.  One block an SM; its warps have tasks of their own, so that a chunk's steps run beside one another and beside those of
 // the chunks before and after: eight turn G into P, eight turn b into bw, eight write the output and move the state on (two
@@ -26,7 +27,6 @@ namespace {
 
 constexpr int N = MMA_CHUNK;
 constexpr int BLOCK = N * 128;                 // bytes of 64 features of a chunk
-constexpr int PARTS = 3;
 // A wait (for microseconds, in a healthy run) gives up after TRIES tries of a microsecond each, or less where the hardware holds a
 // try for less: 0.26 s at most, 5 ms at the very least.
 constexpr int TRIES = 1 << 18, TRY_NS = 1000;
@@ -49,9 +49,11 @@ __device__ __forceinline__ void wait_for(uint32_t bar, uint32_t parity, bool& ga
     atomicAdd(&g_linear_timeouts, 1u);
 }
 
-template <int DA, int DC>
+template <int DA, int DC, int PARTS>
 struct Room {
-    static constexpr int A = 0, B = A + DA / 64 * BLOCK, V = B + DA / 64 * BLOCK, BW = V + DC / 64 * BLOCK, S = BW + PARTS * (DA / 64) * BLOCK;
+    static constexpr int A = 0, B = A + DA / 64 * BLOCK, V = B + DA / 64 * BLOCK, BW = V + DC / 64 * BLOCK;
+    static constexpr int STATE = (DA * (DC + 1) * 4 + 1023) / 1024 * 1024, PLANES = PARTS * (DA / 64) * BLOCK;      // fp32 state and bw share a place
+    static constexpr int S = BW + (PLANES > STATE ? PLANES : STATE);
     static constexpr int BYTES = S + DC / 64 * DA * 128 + 1024;      // slack to start on 1024 bytes
     static constexpr int G = 0, NEAR = 128, FAR = NEAR + DC, U = FAR + DC;      // columns of TMEM; P lies over G
 };
@@ -64,7 +66,7 @@ __host__ __device__ constexpr int p_column(int k) { return 32 * (k / 2) + 8 * (k
 
 // Barriers.  FULL: a tile has arrived; DONE: the products up to these are done; READY: warps have written what products read;
 // FREE: warps have read what products write.
-enum Bar { FULL_A, FULL_B, FULL_C, DONE_G, DONE_FAR, DONE_NEAR, DONE_U, READY_P, READY_BW, READY_S, FREE_OUT, ENDED, BARS };
+enum Bar { FULL_A, FULL_B, FULL_C, DONE_G, DONE_FAR, DONE_NEAR, DONE_U, READY_P, READY_BW, READY_S, SCANNED, FREE_OUT, ENDED, BARS };
 
 __device__ __forceinline__ void sts16(uint32_t to, uint4 v) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
@@ -166,9 +168,9 @@ struct Tiles {
 };
 
 // ENDS: only the state that each piece leaves, from zero.
-template <int DA, int DC, bool ENDS>
+template <int DA, int DC, int PARTS, bool ENDS>
 __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_constant__ March m, const __grid_constant__ Tiles tiles) {
-    using R = Room<DA, DC>;
+    using R = Room<DA, DC, PARTS>;
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[BARS];
     __shared__ uint32_t tmem_slot;
@@ -180,7 +182,7 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     if (tid == 0) {
         odd_chunk[0] = odd_chunk[1] = 0;
-        for (int i = 0; i < BARS; ++i) mbar_init(bar(i), i == READY_P || i == READY_BW || i == READY_S || i == FREE_OUT ? 8 : 1);
+        for (int i = 0; i < BARS; ++i) mbar_init(bar(i), i >= READY_P && i <= FREE_OUT ? 8 : 1);
         mbar_fence_init();
     }
     if (warp == CONTROL) {
@@ -208,7 +210,6 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
     }
     // The state comes and goes through bw's place, along its rows or, turned, its columns.
     constexpr int PITCH = DC + 1;
-    static_assert(DA * PITCH * 4 <= PARTS * (DA / 64) * BLOCK, "the state fits bw's place");
     float* stage = reinterpret_cast<float*>(raw + (base - smem_u32(raw)) + R::BW);
     const int64_t st = (bt * m.heads + h) * m.da * m.dc;
     float* local = m.local + ((bt * m.heads + h) * m.pieces + p) * m.da * m.dc;
@@ -278,26 +279,10 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                     for (int k = 0; k < DA / 16; ++k)
                         product(leader, tmem + R::G, desc_at(da, k / 4 * BLOCK + k % 4 * 32), desc_at(db, k / 4 * BLOCK + k % 4 * 32), IDESC_G, k > 0);
                     commit(DONE_G);
-                    wait(READY_S);             // of the state before this chunk
-                    if (t > first) wait_last(FREE_OUT);
-                    all_wait();
-                    if (gave_up) break;
-#pragma unroll
-                    for (int k = 0; k < DA / 16; ++k)
-                        product(leader, tmem + R::FAR, desc_at(da, k / 4 * BLOCK + k % 4 * 32), desc_at(ds, k * 2048), IDESC_OUT, k > 0);
-                    commit(DONE_FAR);
-                    wait(READY_P);
-                    wait(FULL_C);
-                    all_wait();
-                    if (gave_up) break;
-#pragma unroll
-                    for (int k = 0; k < N / 16; ++k) product_tmem(leader, tmem + R::NEAR, tmem + R::G + p_column(k), desc_at(dc, k * 2048), IDESC_OUT, k > 0);
-                    commit(DONE_NEAR);
-                } else {
-                    wait(READY_S);
-                    wait(FULL_C);
                 }
                 wait(READY_BW);
+                wait(READY_S);                 // U before this one has been added, and S is the state before this chunk
+                wait(FULL_C);
                 all_wait();
                 if (gave_up) break;
 #pragma unroll
@@ -306,6 +291,21 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                     for (int k = 0; k < N / 16; ++k)
                         product(leader, tmem + R::U, desc_at(dw, s * (DA / 64) * BLOCK + k * 2048), desc_at(dc, k * 2048), IDESC_U, s < PARTS - 1 || k > 0);
                 commit(DONE_U);
+                if (ENDS) continue;
+                if (t > first) wait_last(FREE_OUT);
+                all_wait();
+                if (gave_up) break;
+#pragma unroll
+                for (int k = 0; k < DA / 16; ++k)
+                    product(leader, tmem + R::FAR, desc_at(da, k / 4 * BLOCK + k % 4 * 32), desc_at(ds, k * 2048), IDESC_OUT, k > 0);
+                commit(DONE_FAR);
+                wait(READY_P);
+                wait(SCANNED);
+                all_wait();
+                if (gave_up) break;
+#pragma unroll
+                for (int k = 0; k < N / 16; ++k) product_tmem(leader, tmem + R::NEAR, tmem + R::G + p_column(k), desc_at(dc, k * 2048), IDESC_OUT, k > 0);
+                commit(DONE_NEAR);
             }
         } else if (quarter == 1 && lane == 0) {                // tiles
             auto load = [&](int full, int at, int blocks, const CUtensorMap* map, int head, int batch, int64_t t) {
@@ -313,19 +313,25 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                 const int node = (int)(m.reversed ? m.length - t - N : t);
                 for (int f = 0; f < blocks; ++f) load_tile(base + at + f * BLOCK, map, 64 * f, head * (int)h, node, batch * (int)bt, bar(full));
             };
-            // the places are the last chunk's: a is read by G and far, b by G and bw, c by near and U
+            // the places are the last chunk's: b is read by G and for bw, a by G and far, c by U, near and the scan
             for (int64_t t = first; t < last; t += N) {
+                if (t > first) {
+                    wait(READY_BW);
+                    if (!ENDS) wait(DONE_G);
+                }
+                if (gave_up) break;
+                load(FULL_B, R::B, DA / 64, &tiles.b, tiles.head_b, tiles.batch_b, t);
+                ++asked_b;
                 if (!ENDS) {
                     if (t > first) wait(DONE_FAR);
                     if (gave_up) break;
                     load(FULL_A, R::A, DA / 64, &tiles.a, tiles.head_a, tiles.batch_a, t);
                     ++asked_a;
                 }
-                if (t > first) wait(READY_BW);
-                if (gave_up) break;
-                load(FULL_B, R::B, DA / 64, &tiles.b, tiles.head_b, tiles.batch_b, t);
-                ++asked_b;
-                if (t > first) wait(DONE_U);
+                if (t > first) {
+                    wait(ENDS ? DONE_U : DONE_NEAR);
+                    if (!ENDS) wait(SCANNED);
+                }
                 if (gave_up) break;
                 load(FULL_C, R::V, DC / 64, &tiles.c, tiles.head_c, tiles.batch_c, t);
                 ++asked_c;
@@ -343,6 +349,7 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
             gave_up = __any_sync(~0u, gave_up);
             if (gave_up) break;
             const float w = r < n ? m.gain * powers[n - 1 - r + m.shift] : 0.f;
+            const __nv_bfloat162 w1 = __float2bfloat162_rn(w), w2 = __float2bfloat162_rn(w - __low2float(w1));
 #pragma unroll 1
             for (int q = half * (DA / 16); q < (half + 1) * (DA / 16); ++q) {
                 const uint4 v = lds16(chunk_at(base + R::B, row, q));
@@ -350,13 +357,20 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                 uint32_t out[PARTS][4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    uint64_t x = mul2(pair(__uint_as_float(in[k] << 16), __uint_as_float(in[k] & 0xffff0000u)), both(w));
+                    if constexpr (PARTS == 3) {                // 8 bits at a time, exactly
+                        uint64_t x = mul2(pair(__uint_as_float(in[k] << 16), __uint_as_float(in[k] & 0xffff0000u)), both(w));
 #pragma unroll
-                    for (int s = 0; s < PARTS; ++s) {          // the top 8 bits of what is left, exactly
-                        float lo, hi;
-                        unpair(x, lo, hi);
-                        out[s][k] = tops(lo, hi);
-                        if (s < PARTS - 1) x = add2(x, pair(-top_part(lo), -top_part(hi)));
+                        for (int s = 0; s < PARTS; ++s) {
+                            float lo, hi;
+                            unpair(x, lo, hi);
+                            out[s][k] = tops(lo, hi);
+                            if (s < PARTS - 1) x = add2(x, pair(-top_part(lo), -top_part(hi)));
+                        }
+                    } else {                                   // b w1 and what its rounding left, exactly, plus b w2
+                        const __nv_bfloat162 y = reinterpret_cast<const __nv_bfloat162&>(in[k]), first_part = __hmul2(y, w1);
+                        const __nv_bfloat162 second = __hfma2(y, w2, __hfma2(y, w1, __hneg2(first_part)));
+                        out[0][k] = reinterpret_cast<const uint32_t&>(first_part);
+                        out[1][k] = reinterpret_cast<const uint32_t&>(second);
                     }
                 }
 #pragma unroll
@@ -370,6 +384,10 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
         // g^n as 2^(n log2 g), good to 2^-22 or, far back, to n log2 g 2^-24 of itself; the least finite number stands for log 0,
         // of which 2^(0 x) has to be 1
         const float l2 = fmaxf(ld * LOG2_E, -3e38f);
+        uint64_t steps[8];                     // of 16 columns, from the last or the first on: whole blocks take them times one power
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            steps[k] = m.reversed ? pair(exp2_f32(2 * k * l2), exp2_f32((2 * k + 1) * l2)) : pair(exp2_f32((15 - 2 * k) * l2), exp2_f32((14 - 2 * k) * l2));
         for (int64_t t = first; !ENDS && t < last; t += N, phase ^= 1) {
             wait_warp(DONE_G);
             if (gave_up) break;
@@ -384,8 +402,9 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                     tmem_load(tmem + R::G + lanes + part * 32 + c, v);
                     const float from = 32 * before + (m.reversed ? c - lane : lane - c), step = m.reversed ? 1.f : -1.f;
                     if (before > 0) {
+                        const uint64_t w = both(exp2_f32((m.reversed ? from : from - 15.f) * l2));
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) v[k] *= exp2_f32(fmaf(k, step, from) * l2);
+                        for (int k = 0; k < 16; k += 2) unpair(mul2(pair(v[k], v[k + 1]), mul2(w, steps[k / 2])), v[k], v[k + 1]);
                     } else {
                         const uint32_t there = (m.reversed ? ~0u << lane : (2u << lane) - 1u) >> c;
 #pragma unroll
@@ -396,16 +415,6 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                 }
                 tmem_store8(tmem + R::G + p_column(2 * part) + c / 2 + lanes, packed);
             }
-            // an infinity or NaN in c makes NaN of P's zeros for the nodes before it: their rows are summed again
-            wait_warp(FULL_C);
-            if (gave_up) break;
-            uint32_t most = 0;
-#pragma unroll 2
-            for (int q = half * (DC / 16); q < (half + 1) * (DC / 16); ++q) {
-                const uint4 v = lds16(chunk_at(base + R::V, row, q));
-                most = __vmaxu2(most, __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu)));
-            }
-            if ((most >> 16) >= 0x7f80u || (most & 0xffffu) >= 0x7f80u) odd_chunk[phase] = (int)((t - first) / N) + 1;
             tmem_stored();
             signal(READY_P);
         }
@@ -433,62 +442,23 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
         for (int64_t t = first; t < last; t += N, phase ^= 1) {
             const int n = (int)min((int64_t)N, last - t);
             if (!ENDS) {
-                wait(READY_P);                 // for odd_chunk
-                wait_warp(DONE_NEAR);
+                // an infinity or NaN in c makes NaN of P's zeros for the nodes before it: their rows are summed again
+                wait_warp(FULL_C);
                 if (gave_up) break;
-                const bool odd = *(volatile int*)&odd_chunk[phase] == (int)((t - first) / N) + 1;
-                const float w = m.far * powers[r + 1 - m.shift];
-                __nv_bfloat16* to = (__nv_bfloat16*)m.out + ((bt * m.length + origin + dir * (t + r)) * m.heads + h) * m.dc + col0;
-#pragma unroll 1
-                for (int c = 0; c < COLS; c += 16) {
-                    const int left = m.dc - col0 - c;
-                    if (left <= 0) break;
-                    float o[16], f[16];
-                    tmem_load_both(tmem + R::NEAR + lanes + col0 + c, o, tmem + R::FAR + lanes + col0 + c, f);
-                    if (odd) {
-                        // a product with a node behind is 0 times what c holds there: an infinity or NaN is none of this row's
-                        float again[16] = {};
-                        const __nv_bfloat16* cs = (const __nv_bfloat16*)m.c.p + bt * m.c.batch + h * m.c.head + col0 + c;
-                        uint32_t bad = 0;      // features that are none in a row, and those that a node up to j has made so
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) bad |= (o[k] - o[k] != 0.f) << k;
-                        bad = __reduce_or_sync(~0u, bad);
-#pragma unroll 1
-                        for (int j = 0; j < N && bad != 0; ++j) {
-                            const int at = m.reversed ? N - 1 - j : j;
-                            const uint32_t two = tmem_load1(tmem + R::G + lanes + p_column(at / 16) + at % 16 / 2);
-                            const float x = at % 2 ? __uint_as_float(two & 0xffff0000u) : __uint_as_float(two << 16);
-#pragma unroll
-                            for (int k = 0; k < 16; ++k) {
-                                const float y = j < n && k < left ? __bfloat162float(cs[(origin + dir * (t + j)) * m.c.node + k]) : 0.f;
-                                if (j <= r) again[k] = fmaf(x, y, again[k]);
-                                if (y - y != 0.f) bad &= ~(1u << k);
-                            }
-                        }
-                        // a row that comes before j has its sum; in the others an infinity or NaN is their own
-#pragma unroll
-                        for (int k = 0; k < 16; ++k)
-                            if (o[k] - o[k] != 0.f) o[k] = again[k];
-                        tmem_load(tmem + R::FAR + lanes + col0 + c, f);      // once more, rather than kept meanwhile
-                    }
-#pragma unroll
-                    for (int k = 0; k < 16; k += 2) unpair(fma2(pair(o[k], o[k + 1]), both(m.near), mul2(pair(f[k], f[k + 1]), both(w))), o[k], o[k + 1]);
-                    if (r < n) {
-                        if (left >= 16 && m.out_packed) {
-                            uint32_t v[8];
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) v[k] = pack_bf16(o[2 * k], o[2 * k + 1]);
-                            store32(to + c, v);
-                        } else {
-#pragma unroll
-                            for (int k = 0; k < 16; ++k)
-                                if (k < left) to[c + k] = __float2bfloat16_rn(o[k]);
-                        }
-                    }
+                __nv_bfloat162 sum = {}, zero = {};
+#pragma unroll 2
+                for (int q = half * (DC / 16); q < (half + 1) * (DC / 16); ++q) {
+                    const uint4 v = lds16(chunk_at(base + R::V, row, q));
+                    sum = __hfma2(reinterpret_cast<const __nv_bfloat162&>(v.x), zero, sum);
+                    sum = __hfma2(reinterpret_cast<const __nv_bfloat162&>(v.y), zero, sum);
+                    sum = __hfma2(reinterpret_cast<const __nv_bfloat162&>(v.z), zero, sum);
+                    sum = __hfma2(reinterpret_cast<const __nv_bfloat162&>(v.w), zero, sum);
                 }
-                signal(FREE_OUT);
+                if ((reinterpret_cast<const uint32_t&>(sum) & 0x7fff7fffu) != 0) odd_chunk[phase] = (int)((t - first) / N) + 1;
+                signal(SCANNED);
             }
             wait_warp(DONE_U);
+            if (!ENDS) wait_warp(DONE_FAR);        // S is written over
             if (gave_up) break;
             const float hi = whole[n == N ? 0 : 2], lo = whole[n == N ? 1 : 3];
 #pragma unroll
@@ -501,7 +471,62 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                     unpair(fma2(both(hi), x, fma2(both(lo), x, pair(u[k], u[k + 1]))), S[c + k], S[c + k + 1]);
                 }
             }
-            put_state();                       // far has been read
+            put_state();
+            if (ENDS) continue;
+            wait(SCANNED);
+            wait_warp(DONE_NEAR);
+            if (gave_up) break;
+            const bool odd = *(volatile int*)&odd_chunk[phase] == (int)((t - first) / N) + 1;
+            const float w = m.far * powers[r + 1 - m.shift];
+            __nv_bfloat16* to = (__nv_bfloat16*)m.out + ((bt * m.length + origin + dir * (t + r)) * m.heads + h) * m.dc + col0;
+#pragma unroll 1
+            for (int c = 0; c < COLS; c += 16) {
+                const int left = m.dc - col0 - c;
+                if (left <= 0) break;
+                float o[16], f[16];
+                tmem_load_both(tmem + R::NEAR + lanes + col0 + c, o, tmem + R::FAR + lanes + col0 + c, f);
+                if (odd) {
+                    // a product with a node behind is 0 times what c holds there: an infinity or NaN is none of this row's
+                    float again[16] = {};
+                    const __nv_bfloat16* cs = (const __nv_bfloat16*)m.c.p + bt * m.c.batch + h * m.c.head + col0 + c;
+                    uint32_t bad = 0;      // features that are none in a row, and those that a node up to j has made so
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) bad |= (o[k] - o[k] != 0.f) << k;
+                    bad = __reduce_or_sync(~0u, bad);
+#pragma unroll 1
+                    for (int j = 0; j < N && bad != 0; ++j) {
+                        const int at = m.reversed ? N - 1 - j : j;
+                        const uint32_t two = tmem_load1(tmem + R::G + lanes + p_column(at / 16) + at % 16 / 2);
+                        const float x = at % 2 ? __uint_as_float(two & 0xffff0000u) : __uint_as_float(two << 16);
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            const float y = j < n && k < left ? __bfloat162float(cs[(origin + dir * (t + j)) * m.c.node + k]) : 0.f;
+                            if (j <= r) again[k] = fmaf(x, y, again[k]);
+                            if (y - y != 0.f) bad &= ~(1u << k);
+                        }
+                    }
+                    // a row that comes before j has its sum; in the others an infinity or NaN is their own
+#pragma unroll
+                    for (int k = 0; k < 16; ++k)
+                        if (o[k] - o[k] != 0.f) o[k] = again[k];
+                    tmem_load(tmem + R::FAR + lanes + col0 + c, f);      // once more, rather than kept meanwhile
+                }
+#pragma unroll
+                for (int k = 0; k < 16; k += 2) unpair(fma2(pair(o[k], o[k + 1]), both(m.near), mul2(pair(f[k], f[k + 1]), both(w))), o[k], o[k + 1]);
+                if (r < n) {
+                    if (left >= 16 && m.out_packed) {
+                        uint32_t v[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) v[k] = pack_bf16(o[2 * k], o[2 * k + 1]);
+                        store32(to + c, v);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 16; ++k)
+                            if (k < left) to[c + k] = __float2bfloat16_rn(o[k]);
+                    }
+                }
+            }
+            signal(FREE_OUT);
         }
         if (holds)
 #pragma unroll
@@ -555,25 +580,30 @@ bool tile_map(const LinearView& x, int width, int64_t heads, int64_t length, int
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int DA, int DC, bool ENDS>
+template <int DA, int DC, int PARTS, bool ENDS>
 cudaError_t launch(const March& m, const Tiles& tiles, cudaStream_t st) {
     static std::atomic<uint64_t> done{0};
-    const size_t bytes = Room<DA, DC>::BYTES;
-    const cudaError_t e = allow_smem(march_mma_kernel<DA, DC, ENDS>, bytes, done);
+    const size_t bytes = Room<DA, DC, PARTS>::BYTES;
+    const cudaError_t e = allow_smem(march_mma_kernel<DA, DC, PARTS, ENDS>, bytes, done);
     if (e != cudaSuccess) return e;
     const int64_t blocks = m.batch * m.heads * m.pieces;
     if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
-    return launch_kernel_smem(march_mma_kernel<DA, DC, ENDS>, dim3((unsigned)blocks), dim3(THREADS), bytes, st, m, tiles);
+    return launch_kernel_smem(march_mma_kernel<DA, DC, PARTS, ENDS>, dim3((unsigned)blocks), dim3(THREADS), bytes, st, m, tiles);
 }
 
-template <int DA, int DC>
-cudaError_t run(const March& m, const Tiles& tiles, cudaStream_t st) {
+template <int DA, int DC, int PARTS>
+cudaError_t run_parts(const March& m, const Tiles& tiles, cudaStream_t st) {
     if (m.pieces > 1) {
-        cudaError_t e = launch<DA, DC, true>(m, tiles, st);
+        cudaError_t e = launch<DA, DC, PARTS, true>(m, tiles, st);
         if (e == cudaSuccess) e = march_join(m, st);
         if (e != cudaSuccess) return e;
     }
-    return launch<DA, DC, false>(m, tiles, st);
+    return launch<DA, DC, PARTS, false>(m, tiles, st);
+}
+// A state that leaves the march is fp32's; one that only `far` reads is rounded to bf16 there, and two parts of bw are enough.
+template <int DA, int DC>
+cudaError_t run(const March& m, const Tiles& tiles, cudaStream_t st) {
+    return m.end != nullptr ? run_parts<DA, DC, 3>(m, tiles, st) : run_parts<DA, DC, 2>(m, tiles, st);
 }
 
 }  // namespace
