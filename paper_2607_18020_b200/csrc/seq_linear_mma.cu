@@ -33,20 +33,23 @@ constexpr int TRIES = 1 << 18, TRY_NS = 1000;
 
 __device__ unsigned int g_linear_timeouts;
 
+// A loop of its own in a few instructions: a block's tasks share an instruction cache, and there are some thirty waits.
 __device__ __forceinline__ void wait_for(uint32_t bar, uint32_t parity, bool& gave_up) {
     if (gave_up) return;
-#pragma unroll 1
-    for (int i = 0; i < TRIES; ++i) {
-        uint32_t done;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(done) : "r"(bar), "r"(parity), "r"(TRY_NS) : "memory");
-        if (done) return;
-    }
-    gave_up = true;
-    atomicAdd(&g_linear_timeouts, 1u);
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .u32 n;\n\t"
+        "mov.u32 n, %4;\n\t"
+        "AGAIN:\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "@p bra DONE;\n\t"
+        "sub.u32 n, n, 1;\n\t"
+        "setp.ne.u32 p, n, 0;\n\t"
+        "@p bra AGAIN;\n\t"
+        "DONE:\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done) : "r"(bar), "r"(parity), "r"(TRY_NS), "n"(TRIES) : "memory");
+    gave_up = done == 0;
 }
 
 template <int DA, int DC, int PARTS>
@@ -59,14 +62,15 @@ struct Room {
 };
 // Groups of eight warps, the last of four, and their registers: 896 threads start with 72 each.
 constexpr int GROUP_P = 0, GROUP_BW = 1, GROUP_OUT = 2, GROUP_CONTROL = 3, CONTROL = 24, THREADS = 28 * 32;
-constexpr int OUT_REGS = 128, OTHER_REGS = 48;
-static_assert(256 * OUT_REGS + 640 * OTHER_REGS <= THREADS * 72, "the groups share what the block starts with");
+constexpr int OUT_REGS = 128, P_REGS = 64, OTHER_REGS = 40;
+static_assert(256 * (OUT_REGS + P_REGS) + 384 * OTHER_REGS <= THREADS * 72, "the groups share what the block starts with");
 // P lies over G, each 32 columns' 16 over their own: the column of 16 nodes' products.
 __host__ __device__ constexpr int p_column(int k) { return 32 * (k / 2) + 8 * (k % 2); }
 
 // Barriers.  FULL: a tile has arrived; DONE: the products up to these are done; READY: warps have written what products read;
-// FREE: warps have read what products write.
-enum Bar { FULL_A, FULL_B, FULL_C, DONE_G, DONE_FAR, DONE_NEAR, DONE_U, READY_P, READY_BW, READY_S, SCANNED, FREE_OUT, ENDED, BARS };
+// FREE: warps have read what products write.  AGAIN: rows with an infinity or NaN behind them have been summed again; its phases are those
+// of such chunks.
+enum Bar { FULL_A, FULL_B, FULL_C, DONE_G, DONE_FAR, DONE_NEAR, DONE_U, READY_P, READY_BW, READY_S, SCANNED, FREE_OUT, AGAIN, ENDED, BARS };
 
 __device__ __forceinline__ void sts16(uint32_t to, uint4 v) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
@@ -167,6 +171,39 @@ struct Tiles {
     int head_a, head_b, head_c, batch_a, batch_b, batch_c;      // 0: one for all
 };
 
+// A row's output where c holds an infinity or NaN.  The product with a node behind is 0 times what c holds there, which is none of
+// this row's: those sums are formed once more, over the nodes up to the row's own, from the same P.
+template <int DC>
+__device__ __forceinline__ void sum_again(const March& m, const __nv_bfloat16* c, int64_t node, __nv_bfloat16* to, int n, int r, uint32_t lanes, int col0, float w) {
+    using R = Room<64, DC, 2>;                 // the columns of TMEM are those of every DA
+    for (int e = 0; e < DC / 2 && col0 + e < m.dc; e += 16) {
+        const int left = m.dc - col0 - e;
+        float o[16], f[16], again[16] = {};
+        tmem_load_both(R::NEAR + lanes + col0 + e, o, R::FAR + lanes + col0 + e, f);
+        uint32_t bad = 0;                      // features of which a row is none, until a node up to j has made them so
+#pragma unroll
+        for (int k = 0; k < 16; ++k) bad |= (o[k] - o[k] != 0.f) << k;
+        bad = __reduce_or_sync(~0u, bad);
+#pragma unroll 1
+        for (int j = 0; j < n && bad != 0; ++j) {
+            const int at = m.reversed ? N - 1 - j : j;
+            const uint32_t two = tmem_load1(R::G + lanes + p_column(at / 16) + at % 16 / 2);
+            const float x = at % 2 ? __uint_as_float(two & 0xffff0000u) : __uint_as_float(two << 16);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const float y = k < left ? __bfloat162float(c[j * node + col0 + e + k]) : 0.f;
+                if (j <= r) again[k] = fmaf(x, y, again[k]);
+                if (y - y != 0.f) bad &= ~(1u << k);
+            }
+        }
+        // a row before j has its sum; in the others an infinity or NaN is their own
+        if (r < n)
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+                if (k < left && o[k] - o[k] != 0.f) to[col0 + e + k] = __float2bfloat16_rn(fmaf(again[k], m.near, w * f[k]));
+    }
+}
+
 // ENDS: only the state that each piece leaves, from zero.
 template <int DA, int DC, int PARTS, bool ENDS>
 __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_constant__ March m, const __grid_constant__ Tiles tiles) {
@@ -182,7 +219,7 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     if (tid == 0) {
         odd_chunk[0] = odd_chunk[1] = 0;
-        for (int i = 0; i < BARS; ++i) mbar_init(bar(i), i >= READY_P && i <= FREE_OUT ? 8 : 1);
+        for (int i = 0; i < BARS; ++i) mbar_init(bar(i), i >= READY_P && i <= AGAIN ? 8 : 1);
         mbar_fence_init();
     }
     if (warp == CONTROL) {
@@ -195,11 +232,11 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
     const int p = (int)(blockIdx.x - rest * m.pieces);
     const int64_t bt = rest / (unsigned)m.heads, h = rest - (unsigned)bt * (unsigned)m.heads;
     const int64_t first = p * m.piece, last = min(m.length, first + m.piece);
+    const int chunks = (int)((last - first + N - 1) / N), tail = (int)(last - first) - (chunks - 1) * N;
     const float ld = m.log_decay[h];
     {
-        const int tail = last > first ? (int)((last - first - 1) % N) + 1 : 0;
         if (tid < N + 4) {
-            const double g = power(ld, tid < N + 2 ? tid : tid == N + 2 ? N : tail);
+            const double g = power(ld, tid < N + 2 ? tid : tid == N + 2 ? N : max(tail, 0));
             if (tid < N + 2) {
                 powers[tid] = (float)g;
             } else {
@@ -232,7 +269,7 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
     __syncthreads();
     fence_after();
     constexpr uint32_t tmem = 0;               // all 512 columns: they start there
-    uint32_t phase = 0;
+    uint32_t phase = 0, odd_phase = 0;
     bool gave_up = false;
     int asked_a = 0, asked_b = 0, asked_c = 0; // tiles that this thread has asked for
     auto wait = [&](int i) { wait_for(bar(i), phase, gave_up); };
@@ -268,11 +305,14 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                 gave_up = __any_sync(~0u, gave_up);
                 fence_after();
             };
-            for (int64_t t = first; t < last; t += N, phase ^= 1) {
+            for (int c = 0; c < chunks; ++c, phase ^= 1) {
                 if (!ENDS) {
                     wait(FULL_A);
                     wait(FULL_B);
-                    if (t > first && *(volatile int*)&odd_chunk[phase ^ 1] == (int)((t - first) / N)) wait_last(FREE_OUT);      // P is still read
+                    if (c > 0 && *(volatile int*)&odd_chunk[phase ^ 1] == c) {         // P, near and far are still read
+                        wait_for(bar(AGAIN), odd_phase, gave_up);
+                        odd_phase ^= 1;
+                    }
                     all_wait();
                     if (gave_up) break;
 #pragma unroll
@@ -292,7 +332,7 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                         product(leader, tmem + R::U, desc_at(dw, s * (DA / 64) * BLOCK + k * 2048), desc_at(dc, k * 2048), IDESC_U, s < PARTS - 1 || k > 0);
                 commit(DONE_U);
                 if (ENDS) continue;
-                if (t > first) wait_last(FREE_OUT);
+                if (c > 0) wait_last(FREE_OUT);
                 all_wait();
                 if (gave_up) break;
 #pragma unroll
@@ -308,43 +348,43 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                 commit(DONE_NEAR);
             }
         } else if (quarter == 1 && lane == 0) {                // tiles
-            auto load = [&](int full, int at, int blocks, const CUtensorMap* map, int head, int batch, int64_t t) {
+            auto load = [&](int full, int at, int blocks, const CUtensorMap* map, int head, int batch, int c) {
                 mbar_expect_tx(bar(full), blocks * BLOCK);
-                const int node = (int)(m.reversed ? m.length - t - N : t);
+                const int node = (int)(m.reversed ? m.length - first - N : first) + (m.reversed ? -N : N) * c;
                 for (int f = 0; f < blocks; ++f) load_tile(base + at + f * BLOCK, map, 64 * f, head * (int)h, node, batch * (int)bt, bar(full));
             };
             // the places are the last chunk's: b is read by G and for bw, a by G and far, c by U, near and the scan
-            for (int64_t t = first; t < last; t += N) {
-                if (t > first) {
+            for (int c = 0; c < chunks; ++c) {
+                if (c > 0) {
                     wait(READY_BW);
                     if (!ENDS) wait(DONE_G);
                 }
                 if (gave_up) break;
-                load(FULL_B, R::B, DA / 64, &tiles.b, tiles.head_b, tiles.batch_b, t);
+                load(FULL_B, R::B, DA / 64, &tiles.b, tiles.head_b, tiles.batch_b, c);
                 ++asked_b;
                 if (!ENDS) {
-                    if (t > first) wait(DONE_FAR);
+                    if (c > 0) wait(DONE_FAR);
                     if (gave_up) break;
-                    load(FULL_A, R::A, DA / 64, &tiles.a, tiles.head_a, tiles.batch_a, t);
+                    load(FULL_A, R::A, DA / 64, &tiles.a, tiles.head_a, tiles.batch_a, c);
                     ++asked_a;
                 }
-                if (t > first) {
+                if (c > 0) {
                     wait(ENDS ? DONE_U : DONE_NEAR);
                     if (!ENDS) wait(SCANNED);
                 }
                 if (gave_up) break;
-                load(FULL_C, R::V, DC / 64, &tiles.c, tiles.head_c, tiles.batch_c, t);
+                load(FULL_C, R::V, DC / 64, &tiles.c, tiles.head_c, tiles.batch_c, c);
                 ++asked_c;
-                if (t > first) phase ^= 1;
+                if (c > 0) phase ^= 1;
             }
         }
     } else if (group == GROUP_BW) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
-        for (int64_t t = first; t < last; t += N, phase ^= 1) {
-            const int n = (int)min((int64_t)N, last - t);
+        for (int c = 0; c < chunks; ++c, phase ^= 1) {
+            const int n = c < chunks - 1 ? N : tail;
             wait_warp(FULL_B);
             // bw's place is the last chunk's until U is done, the state's before that
-            if (t > first) wait_last(DONE_U);
+            if (c > 0) wait_last(DONE_U);
             else wait(READY_S);
             gave_up = __any_sync(~0u, gave_up);
             if (gave_up) break;
@@ -380,43 +420,59 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
             signal(READY_BW);
         }
     } else if (group == GROUP_P) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(P_REGS));
         // g^n as 2^(n log2 g), good to 2^-22 or, far back, to n log2 g 2^-24 of itself; the least finite number stands for log 0,
         // of which 2^(0 x) has to be 1
         const float l2 = fmaxf(ld * LOG2_E, -3e38f);
-        uint64_t steps[8];                     // of 16 columns, from the last or the first on: whole blocks take them times one power
+        uint64_t steps[8];                     // of 16 columns: whole blocks take these times the power of their nearest column
+        auto make_steps = [&]() {
+            float l = l2;
+            asm volatile("" : "+f"(l));        // made anew each time
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            steps[k] = m.reversed ? pair(exp2_f32(2 * k * l2), exp2_f32((2 * k + 1) * l2)) : pair(exp2_f32((15 - 2 * k) * l2), exp2_f32((14 - 2 * k) * l2));
-        for (int64_t t = first; !ENDS && t < last; t += N, phase ^= 1) {
+            for (int k = 0; k < 8; ++k)
+                steps[k] = m.reversed ? pair(exp2_f32(2 * k * l), exp2_f32((2 * k + 1) * l)) : pair(exp2_f32((15 - 2 * k) * l), exp2_f32((14 - 2 * k) * l));
+        };
+        make_steps();
+        for (int c = 0; !ENDS && c < chunks; ++c, phase ^= 1) {
             wait_warp(DONE_G);
             if (gave_up) break;
             // 32 columns at a time, a thread every other: those of this quarter's own nodes are cut along the diagonal, those of the
             // nodes before them are whole, the others zeros.  Column k of the 32 is the product times g^(32 before + lane - k), or + k - lane.
 #pragma unroll 1
             for (int e = 0; e < 4; ++e) {
-                const int part = e / 2 * 2 + half, c = e % 2 * 16, before = m.reversed ? part - quarter : quarter - part;
+                const int part = e / 2 * 2 + half, col = e % 2 * 16, before = m.reversed ? part - quarter : quarter - part;
                 uint32_t packed[8] = {};
                 if (before >= 0) {
                     float v[16];
-                    tmem_load(tmem + R::G + lanes + part * 32 + c, v);
-                    const float from = 32 * before + (m.reversed ? c - lane : lane - c), step = m.reversed ? 1.f : -1.f;
+                    tmem_load(tmem + R::G + lanes + part * 32 + col, v);
+                    const float from = 32 * before + (m.reversed ? col - lane : lane - col), step = m.reversed ? 1.f : -1.f;
                     if (before > 0) {
                         const uint64_t w = both(exp2_f32((m.reversed ? from : from - 15.f) * l2));
 #pragma unroll
                         for (int k = 0; k < 16; k += 2) unpair(mul2(pair(v[k], v[k + 1]), mul2(w, steps[k / 2])), v[k], v[k + 1]);
                     } else {
-                        const uint32_t there = (m.reversed ? ~0u << lane : (2u << lane) - 1u) >> c;
+                        const uint32_t there = (m.reversed ? ~0u << lane : (2u << lane) - 1u) >> col;
 #pragma unroll
                         for (int k = 0; k < 16; ++k) v[k] = (there >> k & 1u) != 0 ? v[k] * exp2_f32(fmaf(k, step, from) * l2) : 0.f;
                     }
 #pragma unroll
                     for (int k = 0; k < 8; ++k) packed[k] = pack_bf16(v[2 * k], v[2 * k + 1]);
                 }
-                tmem_store8(tmem + R::G + p_column(2 * part) + c / 2 + lanes, packed);
+                tmem_store8(tmem + R::G + p_column(2 * part) + col / 2 + lanes, packed);
             }
             tmem_stored();
             signal(READY_P);
+            wait(SCANNED);
+            if (*(volatile int*)&odd_chunk[phase] == c + 1) {
+                wait_warp(FREE_OUT);           // and the rows are stored
+                if (gave_up) break;
+                const int64_t dir = m.reversed ? -1 : 1, node = (m.reversed ? m.length - 1 - first : first) + dir * (c * N);
+                sum_again<DC>(m, (const __nv_bfloat16*)m.c.p + bt * m.c.batch + h * m.c.head + node * m.c.node, dir * m.c.node,
+                              (__nv_bfloat16*)m.out + ((bt * m.length + node + dir * r) * m.heads + h) * m.dc, c < chunks - 1 ? N : tail, r, lanes, half * (DC / 2),
+                              m.far * powers[r + 1 - m.shift]);
+                signal(AGAIN);
+                make_steps();                  // rather than kept meanwhile
+            }
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(OUT_REGS));
@@ -438,9 +494,10 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
             signal(READY_S);
         };
         put_state();
-        const int64_t dir = m.reversed ? -1 : 1, origin = m.reversed ? m.length - 1 : 0;
-        for (int64_t t = first; t < last; t += N, phase ^= 1) {
-            const int n = (int)min((int64_t)N, last - t);
+        const int64_t dir = m.reversed ? -1 : 1, origin = m.reversed ? m.length - 1 - first : first;
+        __nv_bfloat16* out = (__nv_bfloat16*)m.out + (bt * m.length * m.heads + h) * m.dc + col0;
+        for (int c = 0; c < chunks; ++c, phase ^= 1) {
+            const int n = c < chunks - 1 ? N : tail;
             if (!ENDS) {
                 // an infinity or NaN in c makes NaN of P's zeros for the nodes before it: their rows are summed again
                 wait_warp(FULL_C);
@@ -454,7 +511,7 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                     sum = __hfma2(reinterpret_cast<const __nv_bfloat162&>(v.z), zero, sum);
                     sum = __hfma2(reinterpret_cast<const __nv_bfloat162&>(v.w), zero, sum);
                 }
-                if ((reinterpret_cast<const uint32_t&>(sum) & 0x7fff7fffu) != 0) odd_chunk[phase] = (int)((t - first) / N) + 1;
+                if ((reinterpret_cast<const uint32_t&>(sum) & 0x7fff7fffu) != 0) odd_chunk[phase] = c + 1;
                 signal(SCANNED);
             }
             wait_warp(DONE_U);
@@ -462,55 +519,27 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
             if (gave_up) break;
             const float hi = whole[n == N ? 0 : 2], lo = whole[n == N ? 1 : 3];
 #pragma unroll
-            for (int c = 0; c < COLS; c += 32) {
+            for (int e = 0; e < COLS; e += 32) {
                 float u[32];
-                tmem_load32(tmem + R::U + lanes + col0 + c, u);
+                tmem_load32(tmem + R::U + lanes + col0 + e, u);
 #pragma unroll
                 for (int k = 0; k < 32; k += 2) {
-                    const uint64_t x = pair(S[c + k], S[c + k + 1]);
-                    unpair(fma2(both(hi), x, fma2(both(lo), x, pair(u[k], u[k + 1]))), S[c + k], S[c + k + 1]);
+                    const uint64_t x = pair(S[e + k], S[e + k + 1]);
+                    unpair(fma2(both(hi), x, fma2(both(lo), x, pair(u[k], u[k + 1]))), S[e + k], S[e + k + 1]);
                 }
             }
             put_state();
             if (ENDS) continue;
-            wait(SCANNED);
             wait_warp(DONE_NEAR);
             if (gave_up) break;
-            const bool odd = *(volatile int*)&odd_chunk[phase] == (int)((t - first) / N) + 1;
             const float w = m.far * powers[r + 1 - m.shift];
-            __nv_bfloat16* to = (__nv_bfloat16*)m.out + ((bt * m.length + origin + dir * (t + r)) * m.heads + h) * m.dc + col0;
+            __nv_bfloat16* to = out + (origin + dir * (c * N + r)) * m.heads * m.dc;
 #pragma unroll 1
-            for (int c = 0; c < COLS; c += 16) {
-                const int left = m.dc - col0 - c;
+            for (int e = 0; e < COLS; e += 16) {
+                const int left = m.dc - col0 - e;
                 if (left <= 0) break;
                 float o[16], f[16];
-                tmem_load_both(tmem + R::NEAR + lanes + col0 + c, o, tmem + R::FAR + lanes + col0 + c, f);
-                if (odd) {
-                    // a product with a node behind is 0 times what c holds there: an infinity or NaN is none of this row's
-                    float again[16] = {};
-                    const __nv_bfloat16* cs = (const __nv_bfloat16*)m.c.p + bt * m.c.batch + h * m.c.head + col0 + c;
-                    uint32_t bad = 0;      // features that are none in a row, and those that a node up to j has made so
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) bad |= (o[k] - o[k] != 0.f) << k;
-                    bad = __reduce_or_sync(~0u, bad);
-#pragma unroll 1
-                    for (int j = 0; j < N && bad != 0; ++j) {
-                        const int at = m.reversed ? N - 1 - j : j;
-                        const uint32_t two = tmem_load1(tmem + R::G + lanes + p_column(at / 16) + at % 16 / 2);
-                        const float x = at % 2 ? __uint_as_float(two & 0xffff0000u) : __uint_as_float(two << 16);
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) {
-                            const float y = j < n && k < left ? __bfloat162float(cs[(origin + dir * (t + j)) * m.c.node + k]) : 0.f;
-                            if (j <= r) again[k] = fmaf(x, y, again[k]);
-                            if (y - y != 0.f) bad &= ~(1u << k);
-                        }
-                    }
-                    // a row that comes before j has its sum; in the others an infinity or NaN is their own
-#pragma unroll
-                    for (int k = 0; k < 16; ++k)
-                        if (o[k] - o[k] != 0.f) o[k] = again[k];
-                    tmem_load(tmem + R::FAR + lanes + col0 + c, f);      // once more, rather than kept meanwhile
-                }
+                tmem_load_both(tmem + R::NEAR + lanes + col0 + e, o, tmem + R::FAR + lanes + col0 + e, f);
 #pragma unroll
                 for (int k = 0; k < 16; k += 2) unpair(fma2(pair(o[k], o[k + 1]), both(m.near), mul2(pair(f[k], f[k + 1]), both(w))), o[k], o[k + 1]);
                 if (r < n) {
@@ -518,11 +547,11 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                         uint32_t v[8];
 #pragma unroll
                         for (int k = 0; k < 8; ++k) v[k] = pack_bf16(o[2 * k], o[2 * k + 1]);
-                        store32(to + c, v);
+                        store32(to + e, v);
                     } else {
 #pragma unroll
                         for (int k = 0; k < 16; ++k)
-                            if (k < left) to[c + k] = __float2bfloat16_rn(o[k]);
+                            if (k < left) to[e + k] = __float2bfloat16_rn(o[k]);
                     }
                 }
             }
@@ -534,6 +563,7 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
     }
     const bool lost = __syncthreads_or(gave_up);
     if (lost) {                 // what has been issued has to end before the block does; the results are NaN
+        if (tid == 0) atomicAdd(&g_linear_timeouts, 1u);
         bool late = false;
         if (warp == CONTROL && lane == 0) {
             mma_commit(bar(ENDED));
