@@ -18,161 +18,269 @@ namespace {
 
 constexpr int C = 32, THREADS = 128;
 
-template <int DA, int DC>
+// The march of 32- and 16-bit arrays in 32 bits.  A block takes a row and head, or a piece, and up to 64 features of c, in
+// chunks of 32 nodes: a, b and c in shared memory as fp32, the next chunk's on their way there (fp32 arrays: copied; 16-bit ones are
+// widened when their turn comes), the state there too.  The four products run in packed
+// arithmetic.
+template <typename T, int DA, int DC>
 struct Sizes {
-    static constexpr int PA = DA + 4, PC = DC + 4, PP = C + 4;
-    static constexpr size_t BYTES = sizeof(float) * (2 * C * PA + C * PC + DA * PC + C * PP);
+    static constexpr int PA = DA + 4, PC = DC + 4, PP = C + 4, STAGES = sizeof(T) == 4 && DA <= 64 ? 2 : 1;
+    static constexpr int TILE = 2 * C * PA + C * PC;
+    static constexpr size_t BYTES = sizeof(float) * (STAGES * TILE + DA * PC + C * PP);
 };
 
+// Rows of a chunk to shared memory, W features of pitch P, zeros where there is no node or feature.
 template <typename T, int W, int P>
-__device__ __forceinline__ void load_rows(float* to, const T* from, int64_t stride, int rows, int cols) {
-    for (int i = threadIdx.x; i < C * W; i += THREADS) {
-        const int r = i / W, c = i % W;
-        to[r * P + c] = r < rows && c < cols ? to_f32<T>(from[r * stride + c]) : 0.f;
+__device__ __forceinline__ void load_rows(float* to, const T* from, int64_t stride, int rows, int cols, bool packed) {
+    if constexpr (sizeof(T) == 4) {
+        const uint32_t base = (uint32_t)__cvta_generic_to_shared(to);
+        if (packed) {
+#pragma unroll
+            for (int i = threadIdx.x; i < C * W / 4; i += THREADS) {
+                const int r = i / (W / 4), c = i % (W / 4) * 4, have = r < rows ? min(max(cols - c, 0), 4) : 0;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(base + (r * P + c) * 4), "l"(have ? from + r * stride + c : from), "r"(4 * have)
+                             : "memory");
+            }
+        } else {
+            for (int i = threadIdx.x; i < C * W; i += THREADS) {
+                const int r = i / W, c = i % W;
+                const bool have = r < rows && c < cols;
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(base + (r * P + c) * 4), "l"(have ? from + r * stride + c : from), "r"(have ? 4 : 0)
+                             : "memory");
+            }
+        }
+    } else {
+        for (int i = threadIdx.x; i < C * W / 4; i += THREADS) {
+            const int r = i / (W / 4), c = i % (W / 4) * 4;
+            float v[4] = {};
+            if (r < rows && packed && c + 4 <= cols) widen<T, 4>(v, load_pack<T, 4>(from + r * stride + c));
+            else if (r < rows)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (c + e < cols) v[e] = to_f32<T>(from[r * stride + c + e]);
+            *reinterpret_cast<float4*>(to + r * P + c) = make_float4(v[0], v[1], v[2], v[3]);
+        }
     }
 }
 
-// One piece of a row and head and DC features of c.  ENDS: only the state that the piece leaves, from zero.
+// The sums of two lanes that took a half of the terms each: the lower one gets the first N / 2 rows, the upper one the others.
+template <int N>
+__device__ __forceinline__ void halves(uint64_t (&v)[N][2], int half) {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint64_t mine = half ? v[N / 2 + i][e] : v[i][e], other = half ? v[i][e] : v[N / 2 + i][e];
+            v[i][e] = add2(mine, __shfl_xor_sync(~0u, other, 16));
+        }
+}
+
+__device__ __forceinline__ void lds_pairs(uint64_t (&p)[2], const float* from) {
+    const float4 v = *reinterpret_cast<const float4*>(from);
+    p[0] = pair(v.x, v.y);
+    p[1] = pair(v.z, v.w);
+}
+
+// ENDS: only the state that a piece leaves, from zero.
 template <typename T, int DA, int DC, bool ENDS>
-__global__ void __launch_bounds__(THREADS) march_kernel(March m) {
-    using Z = Sizes<DA, DC>;
+__global__ void __launch_bounds__(THREADS) march_kernel(March m, bool a_packed, bool b_packed, bool c_packed, bool out_packed) {
+    using Z = Sizes<T, DA, DC>;
     extern __shared__ __align__(16) float smem[];
-    float *sa = smem, *sb = sa + C * Z::PA, *sc = sb + C * Z::PA, *ss = sc + C * Z::PC, *sp = ss + DA * Z::PC;
+    float *ss = smem + Z::STAGES * Z::TILE, *sp = ss + DA * Z::PC;
     __shared__ float powers[C + 2];
-    __shared__ float whole[2];
+    __shared__ float whole[4];                             // g^32 and that of the last chunk, each in two parts
     pdl_wait_then_trigger();
     const int tid = threadIdx.x;
-    const int across = (m.dc + DC - 1) / DC;
-    int64_t id = blockIdx.x;
+    const int across = (m.dc + DC - 1) / DC, pieces = ENDS ? m.pieces - 1 : m.pieces;      // nobody starts from the last one's end
+    unsigned id = blockIdx.x;
     const int c0 = (int)(id % across) * DC;
     id /= across;
-    const int p = (int)(id % m.pieces);
-    id /= m.pieces;
-    const int64_t h = id % m.heads, bt = id / m.heads;
+    const int p = (int)(id % pieces);
+    id /= pieces;
+    const int64_t bt = id / (unsigned)m.heads, h = id - (unsigned)bt * (unsigned)m.heads;
     const int cols = min(DC, m.dc - c0);
-    const float ld = m.log_decay[h];
-    if (tid < C + 2) powers[tid] = (float)power(ld, tid);
     const int64_t first = p * m.piece, last = min(m.length, first + m.piece);
+    const int chunks = (int)((last - first + C - 1) / C), tail = (int)(last - first) - (chunks - 1) * C;
+    const int64_t dir = m.reversed ? -1 : 1, origin = m.reversed ? m.length - 1 - first : first;
+    const T* a = (const T*)m.a.p + bt * m.a.batch + h * m.a.head + origin * m.a.node;
+    const T* b = (const T*)m.b.p + bt * m.b.batch + h * m.b.head + origin * m.b.node;
+    const T* cc = (const T*)m.c.p + bt * m.c.batch + h * m.c.head + origin * m.c.node + c0;
+    auto load = [&](int c, int stage) {
+        const int n = c < chunks - 1 ? C : tail;
+        const int64_t at = dir * c * C;
+        float* to = smem + stage * Z::TILE;
+        if (!ENDS) load_rows<T, DA, Z::PA>(to, a + at * m.a.node, dir * m.a.node, n, m.da, a_packed);
+        load_rows<T, DA, Z::PA>(to + C * Z::PA, b + at * m.b.node, dir * m.b.node, n, m.da, b_packed);
+        load_rows<T, DC, Z::PC>(to + 2 * C * Z::PA, cc + at * m.c.node, dir * m.c.node, n, cols, c_packed);
+        if constexpr (sizeof(T) == 4) asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    if (chunks > 0) load(0, 0);
+    if (tid < C + 4) {
+        const double g = power(m.log_decay[h], tid < C + 2 ? tid : tid == C + 2 ? C : max(tail, 0));
+        if (tid < C + 2) {
+            powers[tid] = (float)g;
+        } else {
+            whole[2 * (tid - C - 2)] = (float)g;
+            whole[2 * (tid - C - 2) + 1] = (float)(g - (float)g);
+        }
+    }
     const int64_t st = (bt * m.heads + h) * m.da * m.dc;
     float* local = m.local + ((bt * m.heads + h) * m.pieces + p) * m.da * m.dc;
-    for (int i = tid; i < DA * DC; i += THREADS) {
-        const int r = i / DC, c = i % DC;
+    const float* from = ENDS ? nullptr : m.pieces > 1 ? local : m.start != nullptr ? m.start + st : nullptr;
+    const bool turned = m.pieces > 1 ? m.local_turned : m.start_turned;
+    for (int i = tid; i < DA * DC; i += THREADS) {         // along the rows of what is read
+        const int r = turned ? i % DA : i / DC, c = turned ? i / DA : i % DC;
         float v = 0.f;
-        if (!ENDS && r < m.da && c < cols) {
-            if (m.pieces > 1) v = local[r * m.dc + c0 + c];
-            else if (m.start != nullptr) v = m.start_turned ? m.start[st + (int64_t)(c0 + c) * m.da + r] : m.start[st + r * m.dc + c0 + c];
-        }
+        if (from != nullptr && r < m.da && c < cols) v = from[turned ? (c0 + c) * m.da + r : r * m.dc + c0 + c];
         ss[r * Z::PC + c] = v;
     }
-    const T* a = (const T*)m.a.p + bt * m.a.batch + h * m.a.head;
-    const T* b = (const T*)m.b.p + bt * m.b.batch + h * m.b.head;
-    const T* cc = (const T*)m.c.p + bt * m.c.batch + h * m.c.head + c0;
-    constexpr int GC = DC / 4, GR = THREADS / GC;          // threads along the columns and the rows of a result
-    constexpr int RO = C / GR, RS = DA / GR;               // rows of a thread
-    const int tc = tid % GC * 4, tr = tid / GC;
-    for (int64_t t = first; t < last; t += C) {
-        const int n = (int)min((int64_t)C, last - t);
-        const int64_t node = m.reversed ? m.length - 1 - t : t;
-        const int64_t dir = m.reversed ? -1 : 1;
+    // A result is tiles of 4 x 4 to 16 x 4 a thread.  Where that leaves threads over, two lanes share a tile, each with half of the
+    // terms: half the registers filled from shared memory, which is what binds this, for the tiles of 2 x 4 that would take all.
+    constexpr int GC = DC / 4, HALVES = DC == 32 ? 2 : 1, GR = THREADS / GC / HALVES;
+    constexpr int RO = C / GR, RS = DA / GR, MO = RO / HALVES, MS = RS / HALVES;
+    static_assert(RO == 4 && THREADS == 128, "");
+    const int half = HALVES == 2 ? tid >> 4 & 1 : 0, t = HALVES == 2 ? (tid & 15) | (tid >> 5) << 4 : tid;
+    const int tc = t % GC * 4, tr = t / GC;
+#pragma unroll 1
+    for (int c = 0; c < chunks; ++c) {
+        const int n = c < chunks - 1 ? C : tail, stage = Z::STAGES == 2 ? c & 1 : 0;
+        const float *sa = smem + stage * Z::TILE, *sb = sa + C * Z::PA, *sc = sb + C * Z::PA;
+        if (Z::STAGES == 1 && c > 0) load(c, 0);
+        if constexpr (sizeof(T) == 4) asm volatile("cp.async.wait_group 0;" ::: "memory");
         __syncthreads();
-        if (!ENDS) load_rows<T, DA, Z::PA>(sa, a + node * m.a.node, dir * m.a.node, n, m.da);
-        load_rows<T, DA, Z::PA>(sb, b + node * m.b.node, dir * m.b.node, n, m.da);
-        load_rows<T, DC, Z::PC>(sc, cc + node * m.c.node, dir * m.c.node, n, cols);
-        if (tid == 0) {
-            const double g = power(ld, n);
-            whole[0] = (float)g;
-            whole[1] = (float)(g - (float)g);
-        }
-        __syncthreads();
+        if (Z::STAGES == 2 && c + 1 < chunks) load(c + 1, stage ^ 1);
         if (!ENDS) {
-            // (a_i . b_j), 2 x 4 a thread, with the decay between the nodes
-            const int j0 = tid % 8, i0 = tid / 8 * 2;
-            float s[2][4] = {};
-            for (int d = 0; d < DA; d += 4) {
-                float4 x[2], y[4];
+            // (a_i . b_j), 4 x 4 and half of the features a thread, with the decay between the nodes
+            const int hd = tid >> 4 & 1, td = (tid & 15) | (tid >> 5) << 4, j0 = td % 8, i0 = td / 8 * 4;
+            uint64_t s[4][4];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) x[i] = *reinterpret_cast<const float4*>(sa + (i0 + i) * Z::PA + d);
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const float4*>(sb + (j0 + 8 * j) * Z::PA + d);
+                for (int j = 0; j < 4; ++j) s[i][j] = both(0.f);
+#pragma unroll 4
+            for (int d = hd * (DA / 2); d < (hd + 1) * (DA / 2); d += 4) {
+                uint64_t x[4][2], y[4][2];
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+                for (int i = 0; i < 4; ++i) lds_pairs(x[i], sa + (i0 + i) * Z::PA + d);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        s[i][j] = fmaf(x[i].w, y[j].w, fmaf(x[i].z, y[j].z, fmaf(x[i].y, y[j].y, fmaf(x[i].x, y[j].x, s[i][j]))));
+                for (int j = 0; j < 4; ++j) lds_pairs(y[j], sb + (j0 + 8 * j) * Z::PA + d);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[i][j] = fma2(x[i][1], y[j][1], fma2(x[i][0], y[j][0], s[i][j]));
             }
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const int back = i0 + i - (j0 + 8 * j);
-                    sp[(i0 + i) * Z::PP + j0 + 8 * j] = back < 0 ? 0.f : m.near * powers[back] * s[i][j];
+                    const float lo = sum2(s[i][j]), hi = sum2(s[2 + i][j]);
+                    const float sum = (hd ? hi : lo) + __shfl_xor_sync(~0u, hd ? lo : hi, 16);
+                    const int row = i0 + 2 * hd + i, back = row - (j0 + 8 * j);
+                    sp[row * Z::PP + j0 + 8 * j] = back < 0 ? 0.f : m.near * powers[max(back, 0)] * sum;
                 }
-            __syncthreads();
-            float o[RO][4] = {};
-            for (int d = 0; d < DA; d += 4) {
-                float4 y[4];
+            uint64_t o[RO][2];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] = *reinterpret_cast<const float4*>(ss + (d + e) * Z::PC + tc);
+            for (int i = 0; i < RO; ++i) o[i][0] = o[i][1] = both(0.f);
+#pragma unroll 2
+            for (int d = half * (DA / HALVES); d < (half + 1) * (DA / HALVES); d += 4) {
+                uint64_t y[4][2];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) lds_pairs(y[e], ss + (d + e) * Z::PC + tc);
 #pragma unroll
                 for (int i = 0; i < RO; ++i) {
                     const float4 x = *reinterpret_cast<const float4*>(sa + (tr * RO + i) * Z::PA + d);
                     const float xs[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        o[i][0] = fmaf(xs[e], y[e].x, o[i][0]);
-                        o[i][1] = fmaf(xs[e], y[e].y, o[i][1]);
-                        o[i][2] = fmaf(xs[e], y[e].z, o[i][2]);
-                        o[i][3] = fmaf(xs[e], y[e].w, o[i][3]);
+                        o[i][0] = fma2(both(xs[e]), y[e][0], o[i][0]);
+                        o[i][1] = fma2(both(xs[e]), y[e][1], o[i][1]);
                     }
                 }
             }
 #pragma unroll
-            for (int i = 0; i < RO; ++i)
+            for (int i = 0; i < RO; ++i) {
+                const uint64_t w = both(m.far * powers[tr * RO + i + 1 - m.shift]);
+                o[i][0] = mul2(o[i][0], w);
+                o[i][1] = mul2(o[i][1], w);
+            }
+            __syncthreads();
+            // rows behind a node are not looked at: they may hold anything
+#pragma unroll 1
+            for (int j = 4 * half; j < tr * RO; j += 4 * HALVES) {
+                uint64_t y[4][2];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[i][e] *= m.far * powers[tr * RO + i + 1 - m.shift];
-            for (int j = 0; j < (tr + 1) * RO; ++j) {      // rows behind a node are not looked at: they may hold anything
-                const float4 y = *reinterpret_cast<const float4*>(sc + j * Z::PC + tc);
+                for (int e = 0; e < 4; ++e) lds_pairs(y[e], sc + (j + e) * Z::PC + tc);
+#pragma unroll
+                for (int i = 0; i < RO; ++i) {
+                    const float4 x = *reinterpret_cast<const float4*>(sp + (tr * RO + i) * Z::PP + j);
+                    const float xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        o[i][0] = fma2(both(xs[e]), y[e][0], o[i][0]);
+                        o[i][1] = fma2(both(xs[e]), y[e][1], o[i][1]);
+                    }
+                }
+            }
+#pragma unroll 1
+            for (int j = tr * RO + half; j < (tr + 1) * RO; j += HALVES) {
+                uint64_t y[2];
+                lds_pairs(y, sc + j * Z::PC + tc);
 #pragma unroll
                 for (int i = 0; i < RO; ++i) {
                     if (j > tr * RO + i) continue;
-                    const float x = sp[(tr * RO + i) * Z::PP + j];
-                    o[i][0] = fmaf(x, y.x, o[i][0]);
-                    o[i][1] = fmaf(x, y.y, o[i][1]);
-                    o[i][2] = fmaf(x, y.z, o[i][2]);
-                    o[i][3] = fmaf(x, y.w, o[i][3]);
+                    const uint64_t x = both(sp[(tr * RO + i) * Z::PP + j]);
+                    o[i][0] = fma2(x, y[0], o[i][0]);
+                    o[i][1] = fma2(x, y[1], o[i][1]);
                 }
             }
+            if constexpr (HALVES == 2) halves(o, half);
+            const int row = tr * RO + half * MO;
+            T* out = (T*)m.out + ((bt * m.length + origin + dir * (c * C + row)) * m.heads + h) * m.dc + c0 + tc;
 #pragma unroll
-            for (int i = 0; i < RO; ++i) {
-                const int r = tr * RO + i;
-                if (r >= n) continue;
-                T* to = (T*)m.out + ((bt * m.length + node + dir * r) * m.heads + h) * m.dc + c0;
+            for (int i = 0; i < MO; ++i, out += dir * m.heads * m.dc) {
+                if (row + i >= n) continue;
+                float v[4];
+                unpair(o[i][0], v[0], v[1]);
+                unpair(o[i][1], v[2], v[3]);
+                if (out_packed && tc + 4 <= cols) store_pack<T, 4>(out, v);
+                else
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (tc + e < cols) to[tc + e] = from_f32<T>(o[i][e]);
+                    for (int e = 0; e < 4; ++e)
+                        if (tc + e < cols) out[e] = from_f32<T>(v[e]);
             }
-            __syncthreads();
         }
-        float u[RS][4] = {};
-        for (int j = 0; j < n; ++j) {
-            const float w = m.gain * powers[n - 1 - j + m.shift];
-            float4 y = *reinterpret_cast<const float4*>(sc + j * Z::PC + tc);
+        uint64_t u[RS][2];
+#pragma unroll
+        for (int i = 0; i < RS; ++i) u[i][0] = u[i][1] = both(0.f);
+#pragma unroll 2
+        for (int j = half; j < n; j += HALVES) {
+            uint64_t y[2];
+            const uint64_t w = both(m.gain * powers[n - 1 - j + m.shift]);
+            lds_pairs(y, sc + j * Z::PC + tc);
+            y[0] = mul2(y[0], w);
+            y[1] = mul2(y[1], w);
+            float x[RS];
+#pragma unroll
+            for (int i = 0; i < RS; i += 4) *reinterpret_cast<float4*>(x + i) = *reinterpret_cast<const float4*>(sb + j * Z::PA + tr * RS + i);
 #pragma unroll
             for (int i = 0; i < RS; ++i) {
-                const float x = sb[j * Z::PA + tr * RS + i] * w;
-                u[i][0] = fmaf(x, y.x, u[i][0]);
-                u[i][1] = fmaf(x, y.y, u[i][1]);
-                u[i][2] = fmaf(x, y.z, u[i][2]);
-                u[i][3] = fmaf(x, y.w, u[i][3]);
+                u[i][0] = fma2(both(x[i]), y[0], u[i][0]);
+                u[i][1] = fma2(both(x[i]), y[1], u[i][1]);
             }
         }
+        if constexpr (HALVES == 2) halves(u, half);
+        const uint64_t hi = both(whole[n == C ? 0 : 2]), lo = both(whole[n == C ? 1 : 3]);
+        __syncthreads();                                   // everyone has read the state
 #pragma unroll
-        for (int i = 0; i < RS; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float& v = ss[(tr * RS + i) * Z::PC + tc + e];
-                v = fmaf(whole[0], v, fmaf(whole[1], v, u[i][e]));
-            }
+        for (int i = 0; i < MS; ++i) {
+            float* at = ss + (tr * RS + half * MS + i) * Z::PC + tc;
+            uint64_t v[2];
+            lds_pairs(v, at);
+            float4 w;
+            unpair(fma2(hi, v[0], fma2(lo, v[0], u[i][0])), w.x, w.y);
+            unpair(fma2(hi, v[1], fma2(lo, v[1], u[i][1])), w.z, w.w);
+            *reinterpret_cast<float4*>(at) = w;
+        }
     }
     __syncthreads();
     float* to = ENDS ? local : p == m.pieces - 1 && m.end != nullptr ? m.end + st : nullptr;
@@ -197,7 +305,7 @@ __global__ void __launch_bounds__(256) join_kernel(March m) {
     for (int p = 0; p < m.pieces; p += 8, at += 8 * size) {
         float u[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) u[e] = p + e < m.pieces ? at[e * size] : 0.f;
+        for (int e = 0; e < 8; ++e) u[e] = p + e < m.pieces - 1 ? at[e * size] : 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             if (p + e < m.pieces) at[e * size] = s;
@@ -287,19 +395,24 @@ int check_linear(const fpde_linear_args* a, bool step) {
 // Rows of up to 64 nodes fill less than half of a chunk there.
 bool on_tensor_cores(const fpde_linear_args* a) { return a->dtype == FPDE_BF16 && a->length > 64; }
 
-// Pieces of a row.  With more than one every piece is marched through twice, the first time for its end alone (ENDS of the
-// time); a block's start costs as much as START chunks.  The number that takes the fewest waves of chunks is taken.
+// Pieces of a row.  With more than one, all but the last are marched through twice, the first time for their ends alone, and the
+// states are joined in between.  The number with the least time of waves of blocks is taken; the figures are measured
+// microseconds of a chunk and of a block's start, and of the join, which reads and writes a state for each piece.
 void cut(const fpde_linear_args* a, March& m) {
-    const bool mma = on_tensor_cores(a);
+    const bool mma = on_tensor_cores(a), wide = m.da > 64 || m.dc > 64;
     const int chunk = mma ? MMA_CHUNK : C;
-    const double ends = 0.5, start = 1.;
-    const int64_t rows = m.batch * m.heads * (mma ? 1 : ceil_div(m.dc, 64)), slots = mma ? march_mma_blocks() : 148 * 4, chunks = ceil_div(m.length, chunk);
+    const double main = mma ? (wide ? 4.3 : 2.5) : 4.0, ends = mma ? (wide ? 2.8 : 1.6) : 2.0, start = mma ? 6. : 4.;
+    const int64_t rows = m.batch * m.heads * (mma ? 1 : ceil_div(m.dc, 64)), slots = mma ? MMA_BLOCKS : 148 * 4, chunks = ceil_div(m.length, chunk);
+    const double join = (double)m.batch * m.heads * m.da * m.dc * 8 / 5e6;
     int64_t best = 1;
     double least = 1e300;
     for (int64_t p = 1; p <= chunks && p <= 1024 && rows * (p - 1) < 8 * slots; ++p) {
         const int64_t each = ceil_div(chunks, p);
         if (ceil_div(chunks, each) != p) continue;
-        const double waves = (double)ceil_div(rows * p, slots), time = waves * (p > 1 ? (start + each) * (1. + ends) + 2. : start + each);
+        // a chunk takes longer the more blocks read memory with it: 4.3 us of 128 x 128 features on 64 SMs, 5.5 on all
+        const auto load = [&](int64_t blocks) { return 0.8 + 0.45 * (blocks < slots ? (double)blocks / slots : 1.); };
+        double time = (double)ceil_div(rows * p, slots) * (start + each * main * load(rows * p));
+        if (p > 1) time += (double)ceil_div(rows * (p - 1), slots) * (start + each * ends * load(rows * (p - 1))) + 3. + p * join;
         if (time < least) {
             least = time;
             best = p;
@@ -351,22 +464,6 @@ March march_gq(const fpde_linear_args* a) {
     cut(a, m);
     return m;
 }
-March march_gk(const fpde_linear_args* a) {
-    March m = march_of(a);
-    m.a = {a->v, a->v_batch, a->v_node, a->v_head};
-    m.b = {a->go, a->go_batch, a->go_node, a->go_head};
-    m.c = {a->q, a->q_batch, a->q_node, a->q_head};
-    m.da = (int)a->dv;
-    m.dc = (int)a->dk;
-    m.reversed = m.shift = 1;
-    m.near = m.gain = (float)a->scale;
-    m.far = 1.f;
-    m.start = a->gstate_out;
-    m.start_turned = 1;
-    m.out = a->gk;
-    cut(a, m);
-    return m;
-}
 March march_gv(const fpde_linear_args* a) {
     March m = march_of(a);
     m.a = {a->k, a->k_batch, a->k_node, a->k_head};
@@ -383,6 +480,25 @@ March march_gv(const fpde_linear_args* a) {
     cut(a, m);
     return m;
 }
+// Starts from the states that gv's march has joined, turned.
+March march_gk(const fpde_linear_args* a, const March& gv) {
+    March m = march_of(a);
+    m.a = {a->v, a->v_batch, a->v_node, a->v_head};
+    m.b = {a->go, a->go_batch, a->go_node, a->go_head};
+    m.c = {a->q, a->q_batch, a->q_node, a->q_head};
+    m.da = (int)a->dv;
+    m.dc = (int)a->dk;
+    m.reversed = m.shift = 1;
+    m.near = m.gain = (float)a->scale;
+    m.far = 1.f;
+    m.start = a->gstate_out;
+    m.start_turned = m.local_turned = 1;
+    m.out = a->gk;
+    m.pieces = gv.pieces;
+    m.piece = gv.piece;
+    m.local_there = true;
+    return m;
+}
 
 #define FPDE_TRY(x)                           \
     do {                                      \
@@ -392,18 +508,20 @@ March march_gv(const fpde_linear_args* a) {
 
 template <typename T, int DA, int DC>
 cudaError_t march_launch(const March& m, cudaStream_t st) {
-    const size_t bytes = Sizes<DA, DC>::BYTES;
-    const int64_t blocks = m.batch * m.heads * m.pieces * ceil_div(m.dc, DC);
+    const size_t bytes = Sizes<T, DA, DC>::BYTES;
+    const bool pa = packs(m.a.p, m.a.batch, m.a.node, sizeof(T), 4) && m.a.head % 4 == 0, pb = packs(m.b.p, m.b.batch, m.b.node, sizeof(T), 4) && m.b.head % 4 == 0,
+               pc = packs(m.c.p, m.c.batch, m.c.node, sizeof(T), 4) && m.c.head % 4 == 0, po = m.dc % 4 == 0 && aligned(m.out, 4 * sizeof(T));
+    const int64_t rows = m.batch * m.heads * ceil_div(m.dc, DC), blocks = rows * m.pieces;
     if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
-    if (m.pieces > 1) {
+    if (m.pieces > 1 && !m.local_there) {
         static std::atomic<uint64_t> done{0};
         FPDE_TRY(allow_smem(march_kernel<T, DA, DC, true>, bytes, done));
-        FPDE_TRY(launch_kernel_smem(march_kernel<T, DA, DC, true>, dim3((unsigned)blocks), dim3(THREADS), bytes, st, m));
+        FPDE_TRY(launch_kernel_smem(march_kernel<T, DA, DC, true>, dim3((unsigned)(rows * (m.pieces - 1))), dim3(THREADS), bytes, st, m, pa, pb, pc, po));
         FPDE_TRY(march_join(m, st));
     }
     static std::atomic<uint64_t> done{0};
     FPDE_TRY(allow_smem(march_kernel<T, DA, DC, false>, bytes, done));
-    return launch_kernel_smem(march_kernel<T, DA, DC, false>, dim3((unsigned)blocks), dim3(THREADS), bytes, st, m);
+    return launch_kernel_smem(march_kernel<T, DA, DC, false>, dim3((unsigned)blocks), dim3(THREADS), bytes, st, m, pa, pb, pc, po);
 }
 
 template <typename T>
@@ -454,8 +572,8 @@ extern "C" {
 size_t fpde_linear_attention_workspace_bytes(const fpde_linear_args* a, int backward) {
     if (check_linear_sizes(a) != FPDE_OK) return 0;
     if (!backward) return local_bytes(march_o(a));
-    const size_t q = local_bytes(march_gq(a)), k = local_bytes(march_gk(a)), v = local_bytes(march_gv(a));
-    return q > k ? (q > v ? q : v) : (k > v ? k : v);
+    const size_t q = local_bytes(march_gq(a)), v = local_bytes(march_gv(a));
+    return q > v ? q : v;
 }
 
 static int check_workspace(const fpde_linear_args* a, int backward) {
@@ -482,8 +600,9 @@ int fpde_linear_attention_bwd(const fpde_linear_args* a, void* stream) {
     if ((st = check_workspace(a, 1)) != FPDE_OK) return st;
     const cudaStream_t s = (cudaStream_t)stream;
     cudaError_t e = march_by_type(a, march_gq(a), s);
-    if (e == cudaSuccess) e = march_by_type(a, march_gk(a), s);
-    if (e == cudaSuccess) e = march_by_type(a, march_gv(a), s);
+    const March gv = march_gv(a);
+    if (e == cudaSuccess) e = march_by_type(a, gv, s);
+    if (e == cudaSuccess) e = march_by_type(a, march_gk(a, gv), s);
     return as_status(e);
 }
 

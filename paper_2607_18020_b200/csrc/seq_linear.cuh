@@ -22,10 +22,12 @@ struct March {
     int start_turned;
     void* out;                     // (batch, length, heads, dc) dense
     float* end;                    // (batch, heads, da, dc), or NULL
-    // pieces of a row: states at their starts in `local` (batch, heads, pieces, da, dc)
+    // pieces of a row: states at their starts in `local` (batch, heads, pieces, da, dc), or turned
     int pieces;
     int64_t piece;                 // nodes of a piece
     float* local;
+    int local_turned;
+    bool local_there;              // another march's, which has been joined
     bool out_packed;               // rows of out start on 32 bytes
 };
 
@@ -38,7 +40,7 @@ cudaError_t march_join(const March& m, cudaStream_t st);
 // The march of bf16 arrays on the tensor cores (seq_linear_mma.cu).  Its pieces are multiples of MMA_CHUNK nodes.  False, with
 // nothing launched: the copy engine cannot read one of the arrays (a start or stride that is no multiple of 16 bytes).
 constexpr int MMA_CHUNK = 128;
-int march_mma_blocks();                // resident blocks of the GPU
+constexpr int MMA_BLOCKS = 148;                      // resident on the GPU
 bool march_mma(const March& m, cudaStream_t st, cudaError_t* e);
 unsigned int march_mma_timeouts();
 

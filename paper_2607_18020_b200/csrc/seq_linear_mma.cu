@@ -228,8 +228,8 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
     }
     pdl_wait_then_trigger();
 
-    const unsigned rest = blockIdx.x / (unsigned)m.pieces;
-    const int p = (int)(blockIdx.x - rest * m.pieces);
+    const unsigned pieces = ENDS ? m.pieces - 1 : m.pieces, rest = blockIdx.x / pieces;      // nobody starts from the last one's end
+    const int p = (int)(blockIdx.x - rest * pieces);
     const int64_t bt = rest / (unsigned)m.heads, h = rest - (unsigned)bt * (unsigned)m.heads;
     const int64_t first = p * m.piece, last = min(m.length, first + m.piece);
     const int chunks = (int)((last - first + N - 1) / N), tail = (int)(last - first) - (chunks - 1) * N;
@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
     float* local = m.local + ((bt * m.heads + h) * m.pieces + p) * m.da * m.dc;
     if (!ENDS) {
         const float* from = m.pieces > 1 ? local : m.start != nullptr ? m.start + st : nullptr;
-        const bool turned = m.pieces == 1 && m.start_turned;
+        const bool turned = m.pieces > 1 ? m.local_turned : m.start_turned;
         const int across = turned ? m.da : m.dc;
         if (from == nullptr || m.da < DA || m.dc < DC) {
             for (int i = tid; i < DA * PITCH; i += THREADS) stage[i] = 0.f;
@@ -616,14 +616,14 @@ cudaError_t launch(const March& m, const Tiles& tiles, cudaStream_t st) {
     const size_t bytes = Room<DA, DC, PARTS>::BYTES;
     const cudaError_t e = allow_smem(march_mma_kernel<DA, DC, PARTS, ENDS>, bytes, done);
     if (e != cudaSuccess) return e;
-    const int64_t blocks = m.batch * m.heads * m.pieces;
+    const int64_t blocks = m.batch * m.heads * (ENDS ? m.pieces - 1 : m.pieces);
     if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
     return launch_kernel_smem(march_mma_kernel<DA, DC, PARTS, ENDS>, dim3((unsigned)blocks), dim3(THREADS), bytes, st, m, tiles);
 }
 
 template <int DA, int DC, int PARTS>
 cudaError_t run_parts(const March& m, const Tiles& tiles, cudaStream_t st) {
-    if (m.pieces > 1) {
+    if (m.pieces > 1 && !m.local_there) {
         cudaError_t e = launch<DA, DC, PARTS, true>(m, tiles, st);
         if (e == cudaSuccess) e = march_join(m, st);
         if (e != cudaSuccess) return e;
@@ -637,8 +637,6 @@ cudaError_t run(const March& m, const Tiles& tiles, cudaStream_t st) {
 }
 
 }  // namespace
-
-int march_mma_blocks() { return 148; }
 
 bool march_mma(const March& given, cudaStream_t st, cudaError_t* e) {
     March m = given;
