@@ -624,6 +624,11 @@ int fpde_head_rotary_bwd(const fpde_head_args* args, void* stream);
  * Rows are split along their length where batch and heads do not fill the GPU; the workspace then holds a state for
  * each piece.  Infinities and NaN of a node reach no earlier node and no other head; from that node on the sums that they enter
  * are infinite or NaN, not always the one of the two that a march through the nodes would give.
+ *
+ * Precision: states are fp32's, and products and sums are formed in 32 bits.  bf16 rows of more than 64 nodes, where TMA can
+ * read them (16-byte aligned base, strides of whole 16 bytes), take the tensor cores: there the factor between two nodes of
+ * 128, scale * g^n * (q . k), and the state that an output reads are rounded to bf16 once, which leaves about as much as the
+ * output's own rounding; the states handed on are sums of products whose factors keep 22 bits and more.
  */
 #define FPDE_LINEAR_MAX_DIM 128
 
@@ -709,13 +714,16 @@ int fpde_diag_orthogonalize_lost(const fpde_ortho_args* args, void* stream);
  *   convolution: nodes of a thread's piece of a row; rows of a thread in the single-node form, which depends on
  *   the pointers' alignment too;
  *   orthogonalisation: product 0 is X X^T, 1 b S + c S S, 2 a X + P X, on 0 pairs of SMs, single ones with 1 128 or 2 64
- *   columns a tile, 3 or 4 those with the depth over 2 or 4 blocks; -1 also for matrices that stay on one SM.
+ *   columns a tile, 3 or 4 those with the depth over 2 or 4 blocks; -1 also for matrices that stay on one SM;
+ *   linear attention: the pieces that a row is cut into in the march 0 of o, 1 of gq, 2 of gv and gk; with a minus where the
+ *   tensor cores take the products, if TMA can read the arrays.
  */
 int fpde_diag_scan_channels(const fpde_scan_args* args, int backward);
 int fpde_diag_scan_chunks(const fpde_scan_args* args, int backward);
 int fpde_diag_conv_nodes(const fpde_conv_args* args, int backward);
 int fpde_diag_conv_step_rows(const fpde_conv_args* args);
 int fpde_diag_ortho_form(const fpde_ortho_args* args, int product);
+int fpde_diag_linear_form(const fpde_linear_args* args, int march);
 
 #ifdef __cplusplus
 }

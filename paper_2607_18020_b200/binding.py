@@ -191,11 +191,13 @@ def lib():
             getattr(L, name).argtypes = [ctypes.POINTER(args), ctypes.c_void_p]
         for name, args, extra in (("fpde_diag_scan_channels", ScanArgs, [ctypes.c_int]), ("fpde_diag_scan_chunks", ScanArgs, [ctypes.c_int]),
                                   ("fpde_diag_conv_nodes", ConvArgs, [ctypes.c_int]), ("fpde_diag_conv_step_rows", ConvArgs, []),
-                                  ("fpde_diag_ortho_form", OrthoArgs, [ctypes.c_int])):
+                                  ("fpde_diag_ortho_form", OrthoArgs, [ctypes.c_int]), ("fpde_diag_linear_form", LinearArgs, [ctypes.c_int])):
             getattr(L, name).restype = ctypes.c_int
             getattr(L, name).argtypes = [ctypes.POINTER(args)] + extra
         L.fpde_diag_ortho_timeouts.restype = ctypes.c_uint
         L.fpde_diag_ortho_timeouts.argtypes = []
+        L.fpde_diag_linear_timeouts.restype = ctypes.c_uint
+        L.fpde_diag_linear_timeouts.argtypes = []
         _lib = L
     return _lib
 

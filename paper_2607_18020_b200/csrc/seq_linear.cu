@@ -83,7 +83,7 @@ __device__ __forceinline__ void lds_pairs(uint64_t (&p)[2], const float* from) {
 
 // ENDS: only the state that a piece leaves, from zero.
 template <typename T, int DA, int DC, bool ENDS>
-__global__ void __launch_bounds__(THREADS) march_kernel(March m, bool a_packed, bool b_packed, bool c_packed, bool out_packed) {
+__global__ void __launch_bounds__(THREADS, DA == 32 ? 5 : DA == 64 ? 3 : 2) march_kernel(March m, bool a_packed, bool b_packed, bool c_packed, bool out_packed) {
     using Z = Sizes<T, DA, DC>;
     extern __shared__ __align__(16) float smem[];
     float *ss = smem + Z::STAGES * Z::TILE, *sp = ss + DA * Z::PC;
@@ -618,5 +618,11 @@ int fpde_linear_attention_step(const fpde_linear_args* a, void* stream) {
 }
 
 unsigned int fpde_diag_linear_timeouts(void) { return march_mma_timeouts(); }
+
+int fpde_diag_linear_form(const fpde_linear_args* a, int march) {
+    if (check_linear_sizes(a) != FPDE_OK || march < 0 || march > 2) return 0;
+    const int pieces = (march == 0 ? march_o(a) : march == 1 ? march_gq(a) : march_gv(a)).pieces;
+    return on_tensor_cores(a) ? -pieces : pieces;
+}
 
 }  // extern "C"
