@@ -60,8 +60,8 @@ struct Room {
     static constexpr int BYTES = S + DC / 64 * DA * 128 + 1024;      // slack to start on 1024 bytes
     static constexpr int G = 0, NEAR = 128, FAR = NEAR + DC, U = FAR + DC;      // columns of TMEM; P lies over G
 };
-// Groups of eight warps, the last of four, and their registers: 896 threads start with 72 each.
-constexpr int GROUP_P = 0, GROUP_BW = 1, GROUP_OUT = 2, GROUP_CONTROL = 3, CONTROL = 24, THREADS = 28 * 32;
+// Groups of eight warps (2 is OUT), the last of four, and their registers: 896 threads start with 72 each.
+constexpr int GROUP_P = 0, GROUP_BW = 1, GROUP_CONTROL = 3, CONTROL = 24, THREADS = 28 * 32;
 constexpr int OUT_REGS = 128, P_REGS = 64, OTHER_REGS = 40;
 static_assert(256 * (OUT_REGS + P_REGS) + 384 * OTHER_REGS <= THREADS * 72, "the groups share what the block starts with");
 // P lies over G, each 32 columns' 16 over their own: the column of 16 nodes' products.
