@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(THREADS, DA == 32 ? 5 : DA == 64 ? 3 : 2) marc
     constexpr int RO = C / GR, RS = DA / GR, MO = RO / HALVES, MS = RS / HALVES;
     static_assert(RO == 4 && THREADS == 128, "");
     const int half = HALVES == 2 ? tid >> 4 & 1 : 0, t = HALVES == 2 ? (tid & 15) | (tid >> 5) << 4 : tid;
-    const int tc = t % GC * 4, tr = t / GC;
+    const int tc = t % GC * 4, tr = GR - 1 - t / GC;        // the warps with the most pairs of nodes to multiply have the fewest to sum
 #pragma unroll 1
     for (int c = 0; c < chunks; ++c) {
         const int n = c < chunks - 1 ? C : tail, stage = Z::STAGES == 2 ? c & 1 : 0;
@@ -151,24 +151,29 @@ __global__ void __launch_bounds__(THREADS, DA == 32 ? 5 : DA == 64 ? 3 : 2) marc
         if (Z::STAGES == 2 && c + 1 < chunks) load(c + 1, stage ^ 1);
         if (!ENDS) {
             // (a_i . b_j), 4 x 4 and half of the features a thread, with the decay between the nodes
-            const int hd = tid >> 4 & 1, td = (tid & 15) | (tid >> 5) << 4, j0 = td % 8, i0 = td / 8 * 4;
+            const int hd = tid >> 4 & 1, warp = tid / 32, td = (tid & 15) | warp << 4, j0 = td % 8, i0 = td / 8 * 4;
             uint64_t s[4][4];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) s[i][j] = both(0.f);
+            auto dots = [&](auto count) {
+                constexpr int J = decltype(count)::value;
 #pragma unroll 4
-            for (int d = hd * (DA / 2); d < (hd + 1) * (DA / 2); d += 4) {
-                uint64_t x[4][2], y[4][2];
+                for (int d = hd * (DA / 2); d < (hd + 1) * (DA / 2); d += 4) {
+                    uint64_t x[4][2], y[J][2];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) lds_pairs(x[i], sa + (i0 + i) * Z::PA + d);
+                    for (int i = 0; i < 4; ++i) lds_pairs(x[i], sa + (i0 + i) * Z::PA + d);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) lds_pairs(y[j], sb + (j0 + 8 * j) * Z::PA + d);
+                    for (int j = 0; j < J; ++j) lds_pairs(y[j], sb + (j0 + 8 * j) * Z::PA + d);
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                    for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) s[i][j] = fma2(x[i][1], y[j][1], fma2(x[i][0], y[j][0], s[i][j]));
-            }
+                        for (int j = 0; j < J; ++j) s[i][j] = fma2(x[i][1], y[j][1], fma2(x[i][0], y[j][0], s[i][j]));
+                }
+            };
+            if (warp < 2) dots(std::integral_constant<int, 2>());      // the rest lies behind all of the warp's nodes
+            else dots(std::integral_constant<int, 4>());
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
