@@ -340,7 +340,6 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                     product(leader, tmem + R::FAR, desc_at(da, k / 4 * BLOCK + k % 4 * 32), desc_at(ds, k * 2048), IDESC_OUT, k > 0);
                 commit(DONE_FAR);
                 wait(READY_P);
-                wait(SCANNED);
                 all_wait();
                 if (gave_up) break;
 #pragma unroll
@@ -368,10 +367,7 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                     load(FULL_A, R::A, DA / 64, &tiles.a, tiles.head_a, tiles.batch_a, c);
                     ++asked_a;
                 }
-                if (c > 0) {
-                    wait(ENDS ? DONE_U : DONE_NEAR);
-                    if (!ENDS) wait(SCANNED);
-                }
+                if (c > 0) wait(ENDS ? DONE_U : DONE_NEAR);
                 if (gave_up) break;
                 load(FULL_C, R::V, DC / 64, &tiles.c, tiles.head_c, tiles.batch_c, c);
                 ++asked_c;
@@ -461,8 +457,9 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                 tmem_store8(tmem + R::G + p_column(2 * part) + col / 2 + lanes, packed);
             }
             tmem_stored();
+            wait_warp(SCANNED);                // before READY_P: the next chunk's cannot be over yet
+            if (gave_up) break;
             signal(READY_P);
-            wait(SCANNED);
             if (*(volatile int*)&odd_chunk[phase] == c + 1) {
                 wait_warp(FREE_OUT);           // and the rows are stored
                 if (gave_up) break;
