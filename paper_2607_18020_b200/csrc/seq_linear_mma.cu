@@ -166,6 +166,30 @@ __device__ __forceinline__ void store32(void* to, const uint32_t (&v)[8]) {
 __device__ __forceinline__ float top_part(float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); }
 __device__ __forceinline__ uint32_t tops(float lo, float hi) { return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632); }
 
+// Eight features of b times their node's weight, as PARTS bf16 each.
+template <int PARTS>
+__device__ __forceinline__ void weigh(uint32_t (&out)[PARTS][4], uint4 v, float w, __nv_bfloat162 w1, __nv_bfloat162 w2) {
+    const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if constexpr (PARTS == 3) {                            // 8 bits at a time, exactly
+            uint64_t x = mul2(pair(__uint_as_float(in[k] << 16), __uint_as_float(in[k] & 0xffff0000u)), both(w));
+#pragma unroll
+            for (int s = 0; s < PARTS; ++s) {
+                float lo, hi;
+                unpair(x, lo, hi);
+                out[s][k] = tops(lo, hi);
+                if (s < PARTS - 1) x = add2(x, pair(-top_part(lo), -top_part(hi)));
+            }
+        } else {                                               // b w1 and what its rounding left, exactly, plus b w2
+            const __nv_bfloat162 y = reinterpret_cast<const __nv_bfloat162&>(in[k]), first_part = __hmul2(y, w1);
+            const __nv_bfloat162 second = __hfma2(y, w2, __hfma2(y, w1, __hneg2(first_part)));
+            out[0][k] = reinterpret_cast<const uint32_t&>(first_part);
+            out[1][k] = reinterpret_cast<const uint32_t&>(second);
+        }
+    }
+}
+
 struct Tiles {
     CUtensorMap a, b, c;                       // (features, heads, nodes, batch)
     int head_a, head_b, head_c, batch_a, batch_b, batch_c;      // 0: one for all
@@ -204,8 +228,7 @@ __device__ __forceinline__ void sum_again(const March& m, const __nv_bfloat16* c
     }
 }
 
-// ENDS: only the state that each piece leaves, from zero.
-template <int DA, int DC, int PARTS, bool ENDS>
+template <int DA, int DC, int PARTS>
 __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_constant__ March m, const __grid_constant__ Tiles tiles) {
     using R = Room<DA, DC, PARTS>;
     extern __shared__ uint8_t raw[];
@@ -228,8 +251,8 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
     }
     pdl_wait_then_trigger();
 
-    const unsigned pieces = ENDS ? m.pieces - 1 : m.pieces, rest = blockIdx.x / pieces;      // nobody starts from the last one's end
-    const int p = (int)(blockIdx.x - rest * pieces);
+    const unsigned rest = blockIdx.x / (unsigned)m.pieces;
+    const int p = (int)(blockIdx.x - rest * (unsigned)m.pieces);
     const int64_t bt = rest / (unsigned)m.heads, h = rest - (unsigned)bt * (unsigned)m.heads;
     const int64_t first = p * m.piece, last = min(m.length, first + m.piece);
     const int chunks = (int)((last - first + N - 1) / N), tail = (int)(last - first) - (chunks - 1) * N;
@@ -249,8 +272,8 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
     constexpr int PITCH = DC + 1;
     float* stage = reinterpret_cast<float*>(raw + (base - smem_u32(raw)) + R::BW);
     const int64_t st = (bt * m.heads + h) * m.da * m.dc;
-    float* local = m.local + ((bt * m.heads + h) * m.pieces + p) * m.da * m.dc;
-    if (!ENDS) {
+    {
+        const float* local = m.local + ((bt * m.heads + h) * m.pieces + p) * m.da * m.dc;
         const float* from = m.pieces > 1 ? local : m.start != nullptr ? m.start + st : nullptr;
         const bool turned = m.pieces > 1 ? m.local_turned : m.start_turned;
         const int across = turned ? m.da : m.dc;
@@ -306,20 +329,18 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                 fence_after();
             };
             for (int c = 0; c < chunks; ++c, phase ^= 1) {
-                if (!ENDS) {
-                    wait(FULL_A);
-                    wait(FULL_B);
-                    if (c > 0 && *(volatile int*)&odd_chunk[phase ^ 1] == c) {         // P, near and far are still read
-                        wait_for(bar(AGAIN), odd_phase, gave_up);
-                        odd_phase ^= 1;
-                    }
-                    all_wait();
-                    if (gave_up) break;
-#pragma unroll
-                    for (int k = 0; k < DA / 16; ++k)
-                        product(leader, tmem + R::G, desc_at(da, k / 4 * BLOCK + k % 4 * 32), desc_at(db, k / 4 * BLOCK + k % 4 * 32), IDESC_G, k > 0);
-                    commit(DONE_G);
+                wait(FULL_A);
+                wait(FULL_B);
+                if (c > 0 && *(volatile int*)&odd_chunk[phase ^ 1] == c) {         // P, near and far are still read
+                    wait_for(bar(AGAIN), odd_phase, gave_up);
+                    odd_phase ^= 1;
                 }
+                all_wait();
+                if (gave_up) break;
+#pragma unroll
+                for (int k = 0; k < DA / 16; ++k)
+                    product(leader, tmem + R::G, desc_at(da, k / 4 * BLOCK + k % 4 * 32), desc_at(db, k / 4 * BLOCK + k % 4 * 32), IDESC_G, k > 0);
+                commit(DONE_G);
                 wait(READY_BW);
                 wait(READY_S);                 // U before this one has been added, and S is the state before this chunk
                 wait(FULL_C);
@@ -331,7 +352,6 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                     for (int k = 0; k < N / 16; ++k)
                         product(leader, tmem + R::U, desc_at(dw, s * (DA / 64) * BLOCK + k * 2048), desc_at(dc, k * 2048), IDESC_U, s < PARTS - 1 || k > 0);
                 commit(DONE_U);
-                if (ENDS) continue;
                 if (c > 0) wait_last(FREE_OUT);
                 all_wait();
                 if (gave_up) break;
@@ -356,18 +376,16 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
             for (int c = 0; c < chunks; ++c) {
                 if (c > 0) {
                     wait(READY_BW);
-                    if (!ENDS) wait(DONE_G);
+                    wait(DONE_G);
                 }
                 if (gave_up) break;
                 load(FULL_B, R::B, DA / 64, &tiles.b, tiles.head_b, tiles.batch_b, c);
                 ++asked_b;
-                if (!ENDS) {
-                    if (c > 0) wait(DONE_FAR);
-                    if (gave_up) break;
-                    load(FULL_A, R::A, DA / 64, &tiles.a, tiles.head_a, tiles.batch_a, c);
-                    ++asked_a;
-                }
-                if (c > 0) wait(ENDS ? DONE_U : DONE_NEAR);
+                if (c > 0) wait(DONE_FAR);
+                if (gave_up) break;
+                load(FULL_A, R::A, DA / 64, &tiles.a, tiles.head_a, tiles.batch_a, c);
+                ++asked_a;
+                if (c > 0) wait(DONE_NEAR);
                 if (gave_up) break;
                 load(FULL_C, R::V, DC / 64, &tiles.c, tiles.head_c, tiles.batch_c, c);
                 ++asked_c;
@@ -388,27 +406,8 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
             const __nv_bfloat162 w1 = __float2bfloat162_rn(w), w2 = __float2bfloat162_rn(w - __low2float(w1));
 #pragma unroll 1
             for (int q = half * (DA / 16); q < (half + 1) * (DA / 16); ++q) {
-                const uint4 v = lds16(chunk_at(base + R::B, row, q));
-                const uint32_t in[4] = {v.x, v.y, v.z, v.w};
                 uint32_t out[PARTS][4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if constexpr (PARTS == 3) {                // 8 bits at a time, exactly
-                        uint64_t x = mul2(pair(__uint_as_float(in[k] << 16), __uint_as_float(in[k] & 0xffff0000u)), both(w));
-#pragma unroll
-                        for (int s = 0; s < PARTS; ++s) {
-                            float lo, hi;
-                            unpair(x, lo, hi);
-                            out[s][k] = tops(lo, hi);
-                            if (s < PARTS - 1) x = add2(x, pair(-top_part(lo), -top_part(hi)));
-                        }
-                    } else {                                   // b w1 and what its rounding left, exactly, plus b w2
-                        const __nv_bfloat162 y = reinterpret_cast<const __nv_bfloat162&>(in[k]), first_part = __hmul2(y, w1);
-                        const __nv_bfloat162 second = __hfma2(y, w2, __hfma2(y, w1, __hneg2(first_part)));
-                        out[0][k] = reinterpret_cast<const uint32_t&>(first_part);
-                        out[1][k] = reinterpret_cast<const uint32_t&>(second);
-                    }
-                }
+                weigh<PARTS>(out, lds16(chunk_at(base + R::B, row, q)), w, w1, w2);
 #pragma unroll
                 for (int s = 0; s < PARTS; ++s)
                     sts16(chunk_at(base + R::BW + s * (DA / 64) * BLOCK, row, q), make_uint4(out[s][0], out[s][1], out[s][2], out[s][3]));
@@ -429,7 +428,7 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                 steps[k] = m.reversed ? pair(exp2_f32(2 * k * l), exp2_f32((2 * k + 1) * l)) : pair(exp2_f32((15 - 2 * k) * l), exp2_f32((14 - 2 * k) * l));
         };
         make_steps();
-        for (int c = 0; !ENDS && c < chunks; ++c, phase ^= 1) {
+        for (int c = 0; c < chunks; ++c, phase ^= 1) {
             wait_warp(DONE_G);
             if (gave_up) break;
             // 32 columns at a time, a thread every other: those of this quarter's own nodes are cut along the diagonal, those of the
@@ -479,9 +478,9 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
         const int d = DA == 128 ? quarter * 32 + lane : quarter * 16 + lane, col0 = half * COLS;
         float S[COLS];
 #pragma unroll
-        for (int c = 0; c < COLS; ++c) S[c] = ENDS ? 0.f : stage[min(d, DA - 1) * PITCH + col0 + c];
+        for (int c = 0; c < COLS; ++c) S[c] = stage[min(d, DA - 1) * PITCH + col0 + c];
         auto put_state = [&]() {               // the factor of `far`
-            if (!ENDS && holds) {
+            if (holds) {
 #pragma unroll
                 for (int q = 0; q < COLS / 8; ++q)
                     sts16(chunk_at(base + R::S, d, col0 / 8 + q, DA),
@@ -495,24 +494,22 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
         __nv_bfloat16* out = (__nv_bfloat16*)m.out + (bt * m.length * m.heads + h) * m.dc + col0;
         for (int c = 0; c < chunks; ++c, phase ^= 1) {
             const int n = c < chunks - 1 ? N : tail;
-            if (!ENDS) {
-                // an infinity or NaN in c makes NaN of P's zeros for the nodes before it: their rows are summed again
-                wait_warp(FULL_C);
-                if (gave_up) break;
-                __nv_bfloat162 sum = {}, zero = {};
+            // an infinity or NaN in c makes NaN of P's zeros for the nodes before it: their rows are summed again
+            wait_warp(FULL_C);
+            if (gave_up) break;
+            __nv_bfloat162 sum = {}, zero = {};
 #pragma unroll 2
-                for (int q = half * (DC / 16); q < (half + 1) * (DC / 16); ++q) {
-                    const uint4 v = lds16(chunk_at(base + R::V, row, q));
-                    sum = __hfma2(reinterpret_cast<const __nv_bfloat162&>(v.x), zero, sum);
-                    sum = __hfma2(reinterpret_cast<const __nv_bfloat162&>(v.y), zero, sum);
-                    sum = __hfma2(reinterpret_cast<const __nv_bfloat162&>(v.z), zero, sum);
-                    sum = __hfma2(reinterpret_cast<const __nv_bfloat162&>(v.w), zero, sum);
-                }
-                if ((reinterpret_cast<const uint32_t&>(sum) & 0x7fff7fffu) != 0) odd_chunk[phase] = c + 1;
-                signal(SCANNED);
+            for (int q = half * (DC / 16); q < (half + 1) * (DC / 16); ++q) {
+                const uint4 v = lds16(chunk_at(base + R::V, row, q));
+                sum = __hfma2(reinterpret_cast<const __nv_bfloat162&>(v.x), zero, sum);
+                sum = __hfma2(reinterpret_cast<const __nv_bfloat162&>(v.y), zero, sum);
+                sum = __hfma2(reinterpret_cast<const __nv_bfloat162&>(v.z), zero, sum);
+                sum = __hfma2(reinterpret_cast<const __nv_bfloat162&>(v.w), zero, sum);
             }
+            if ((reinterpret_cast<const uint32_t&>(sum) & 0x7fff7fffu) != 0) odd_chunk[phase] = c + 1;
+            signal(SCANNED);
             wait_warp(DONE_U);
-            if (!ENDS) wait_warp(DONE_FAR);        // S is written over
+            wait_warp(DONE_FAR);                   // S is written over
             if (gave_up) break;
             const float hi = whole[n == N ? 0 : 2], lo = whole[n == N ? 1 : 3];
 #pragma unroll
@@ -526,7 +523,6 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                 }
             }
             put_state();
-            if (ENDS) continue;
             wait_warp(DONE_NEAR);
             if (gave_up) break;
             const float w = m.far * powers[r + 1 - m.shift];
@@ -569,13 +565,12 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
         if (asked_a > 0) wait_for(bar(FULL_A), (asked_a - 1) & 1, late);
         if (asked_b > 0) wait_for(bar(FULL_B), (asked_b - 1) & 1, late);
         if (asked_c > 0) wait_for(bar(FULL_C), (asked_c - 1) & 1, late);
-        if (!ENDS)
-            for (int64_t i = first * m.dc + tid; i < last * m.dc; i += THREADS) {
-                const int64_t node = m.reversed ? m.length - 1 - i / m.dc : i / m.dc;
-                ((__nv_bfloat16*)m.out)[((bt * m.length + node) * m.heads + h) * m.dc + i % m.dc] = __float2bfloat16_rn(NAN);
-            }
+        for (int64_t i = first * m.dc + tid; i < last * m.dc; i += THREADS) {
+            const int64_t node = m.reversed ? m.length - 1 - i / m.dc : i / m.dc;
+            ((__nv_bfloat16*)m.out)[((bt * m.length + node) * m.heads + h) * m.dc + i % m.dc] = __float2bfloat16_rn(NAN);
+        }
     }
-    float* to = ENDS ? local : p == m.pieces - 1 && m.end != nullptr ? m.end + st : nullptr;
+    float* to = p == m.pieces - 1 && m.end != nullptr ? m.end + st : nullptr;
     if (to != nullptr)
 #pragma unroll 4
         for (int i = tid; i < m.da * m.dc; i += THREADS) to[i] = lost ? NAN : stage[i / m.dc * PITCH + i % m.dc];
@@ -583,6 +578,177 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
     __syncthreads();
     fence_after();
     if (warp == CONTROL) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+
+// The state that each piece but the last leaves, from zero: U alone.  Nothing but bw's products is there to wait for, so tiles and U have
+// two places each, and bw too where it fits: the tiles' way from memory, bw, its products and the sum of their results overlap.
+template <int DA, int DC, int PARTS>
+struct EndsRoom {
+    static constexpr int TILE_B = DA / 64 * BLOCK, TILE_C = DC / 64 * BLOCK, FACTORS = PARTS * TILE_B, ROUNDS = DA == 64 ? 2 : 1;
+    static constexpr int B = 0, V = B + 2 * TILE_B, BW = V + 2 * TILE_C, BYTES = BW + ROUNDS * FACTORS + 1024;
+    static_assert(DA * (DC + 1) * 4 <= BW, "the state leaves through the tiles' places");
+};
+enum EndsBar { E_FULL_B, E_FULL_C = E_FULL_B + 2, E_READY_BW = E_FULL_C + 2, E_DONE_U = E_READY_BW + 2, E_READ_U = E_DONE_U + 2, E_ENDED = E_READ_U + 2, E_BARS };
+constexpr int E_BW_WARPS = 16, E_SUM = 16, E_CONTROL = 24, E_BW_REGS = 48, E_SUM_REGS = 128, E_CONTROL_REGS = 40;
+static_assert(512 * E_BW_REGS + 256 * E_SUM_REGS + 128 * E_CONTROL_REGS <= THREADS * 72, "the groups share what the block starts with");
+
+template <int DA, int DC, int PARTS>
+__global__ void __launch_bounds__(THREADS, 1) march_mma_ends_kernel(const __grid_constant__ March m, const __grid_constant__ Tiles tiles) {
+    using R = EndsRoom<DA, DC, PARTS>;
+    extern __shared__ uint8_t raw[];
+    __shared__ __align__(8) uint64_t bars[E_BARS];
+    __shared__ uint32_t tmem_slot;
+    __shared__ float powers[N + 1];
+    const uint32_t base = (smem_u32(raw) + 1023) & ~1023u;
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, quarter = warp % 4;
+    auto bar = [&](int i) { return smem_u32(&bars[i]); };
+    if (tid == 0) {
+        for (int i = 0; i < E_BARS; ++i)
+            mbar_init(bar(i), i >= E_READY_BW && i < E_DONE_U ? E_BW_WARPS : i >= E_READ_U && i < E_ENDED ? E_CONTROL - E_SUM : 1);
+        mbar_fence_init();
+    }
+    if (warp == E_CONTROL) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_slot)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    pdl_wait_then_trigger();
+
+    const unsigned pieces = m.pieces - 1, rest = blockIdx.x / pieces;      // nobody starts from the last one's end
+    const int p = (int)(blockIdx.x - rest * pieces);
+    const int64_t bt = rest / (unsigned)m.heads, h = rest - (unsigned)bt * (unsigned)m.heads, first = p * m.piece;
+    const int chunks = (int)(m.piece / N);     // all of them whole
+    if (tid < N + 1) powers[tid] = (float)power(m.log_decay[h], tid);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    constexpr uint32_t tmem = 0;               // all 512 columns: they start there
+    bool gave_up = false;
+    int asked_b = 0, asked_c = 0;              // tiles that this thread has asked for
+    // for chunk c's phase of the one of two barriers that even or odd chunks use
+    auto wait = [&](int i, int c) { wait_for(bar(i + (c & 1)), (c >> 1) & 1, gave_up); };
+    auto wait_warp = [&](int i, int c) {
+        wait(i, c);
+        gave_up = __any_sync(~0u, gave_up);
+        fence_after();
+    };
+    auto signal = [&](int i, int c) {
+        fence_async();
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(i + (c & 1)));
+    };
+    constexpr int PITCH = DC + 1;
+    float* stage = reinterpret_cast<float*>(raw + (base - smem_u32(raw)));
+
+    float S[DC / 2];
+    const bool holds = DA == 128 || lane < 16;               // with 64 rows the products use 16 lanes of each quarter
+    const int d = DA == 128 ? quarter * 32 + lane : quarter * 16 + lane, col0 = warp / 4 % 2 * (DC / 2);
+    if (warp >= E_CONTROL) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(E_CONTROL_REGS));
+        constexpr uint32_t IDESC_U = 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | (uint32_t)(DC / 8) << 17 | (uint32_t)(DA / 16) << 24;
+        if (__shfl_sync(~0u, quarter, 0) == 0) {
+            const bool leader = elected();
+            for (int c = 0; c < chunks; ++c) {
+                wait(E_READY_BW, c);
+                wait(E_FULL_C, c);
+                if (c >= 2) wait(E_READ_U, c - 2);
+                __syncwarp();
+                gave_up = __any_sync(~0u, gave_up);
+                fence_after();
+                if (gave_up) break;
+                const uint64_t dc = slice_desc(base + R::V + (c & 1) * R::TILE_C, true, BLOCK),
+                               dw = slice_desc(base + R::BW + (R::ROUNDS == 2 ? c & 1 : 0) * R::FACTORS, true, BLOCK);
+#pragma unroll
+                for (int s = PARTS - 1; s >= 0; --s)           // the small parts first: the sum is rounded towards zero at every product
+#pragma unroll
+                    for (int k = 0; k < N / 16; ++k)
+                        product(leader, tmem + (c & 1) * DC, desc_at(dw, s * R::TILE_B + k * 2048), desc_at(dc, k * 2048), IDESC_U, s < PARTS - 1 || k > 0);
+                if (leader) mma_commit(bar(E_DONE_U + (c & 1)));
+            }
+        } else if (quarter == 1 && lane == 0) {
+            for (int c = 0; c < chunks; ++c) {
+                const int node = (int)(m.reversed ? m.length - first - N : first) + (m.reversed ? -N : N) * c;
+                if (c >= 2) wait(E_READY_BW, c - 2);
+                if (gave_up) break;
+                mbar_expect_tx(bar(E_FULL_B + (c & 1)), R::TILE_B);
+                for (int f = 0; f < DA / 64; ++f)
+                    load_tile(base + R::B + (c & 1) * R::TILE_B + f * BLOCK, &tiles.b, 64 * f, tiles.head_b * (int)h, node, tiles.batch_b * (int)bt, bar(E_FULL_B + (c & 1)));
+                ++asked_b;
+                if (c >= 2) wait(E_DONE_U, c - 2);
+                if (gave_up) break;
+                mbar_expect_tx(bar(E_FULL_C + (c & 1)), R::TILE_C);
+                for (int f = 0; f < DC / 64; ++f)
+                    load_tile(base + R::V + (c & 1) * R::TILE_C + f * BLOCK, &tiles.c, 64 * f, tiles.head_c * (int)h, node, tiles.batch_c * (int)bt, bar(E_FULL_C + (c & 1)));
+                ++asked_c;
+            }
+        }
+    } else if (warp < E_SUM) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(E_BW_REGS));
+        const int row = quarter * 32 + lane, r = m.reversed ? N - 1 - row : row, share = warp / 4;
+        const float w = m.gain * powers[N - 1 - r + m.shift];
+        const __nv_bfloat162 w1 = __float2bfloat162_rn(w), w2 = __float2bfloat162_rn(w - __low2float(w1));
+        for (int c = 0; c < chunks; ++c) {
+            wait(E_FULL_B, c);
+            if (c >= R::ROUNDS) wait(E_DONE_U, c - R::ROUNDS);             // its place is free
+            gave_up = __any_sync(~0u, gave_up);
+            if (gave_up) break;
+            fence_after();
+            const uint32_t from = base + R::B + (c & 1) * R::TILE_B, to = base + R::BW + (R::ROUNDS == 2 ? c & 1 : 0) * R::FACTORS;
+#pragma unroll 1
+            for (int q = share * (DA / 32); q < (share + 1) * (DA / 32); ++q) {
+                uint32_t out[PARTS][4];
+                weigh<PARTS>(out, lds16(chunk_at(from, row, q)), w, w1, w2);
+#pragma unroll
+                for (int s = 0; s < PARTS; ++s) sts16(chunk_at(to + s * R::TILE_B, row, q), make_uint4(out[s][0], out[s][1], out[s][2], out[s][3]));
+            }
+            signal(E_READY_BW, c);
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(E_SUM_REGS));
+        const double g = power(m.log_decay[h], N);
+        const float hi = (float)g, lo = (float)(g - hi);
+#pragma unroll
+        for (int c = 0; c < DC / 2; ++c) S[c] = 0.f;
+        for (int c = 0; c < chunks; ++c) {
+            wait_warp(E_DONE_U, c);
+            if (gave_up) break;
+#pragma unroll
+            for (int e = 0; e < DC / 2; e += 32) {
+                float u[32];
+                tmem_load32(tmem + (c & 1) * DC + ((uint32_t)(quarter * 32) << 16) + col0 + e, u);
+#pragma unroll
+                for (int k = 0; k < 32; k += 2) {
+                    const uint64_t x = pair(S[e + k], S[e + k + 1]);
+                    unpair(fma2(both(hi), x, fma2(both(lo), x, pair(u[k], u[k + 1]))), S[e + k], S[e + k + 1]);
+                }
+            }
+            signal(E_READ_U, c);
+        }
+        // U is done, and with it all that read the tiles
+        if (holds)
+#pragma unroll
+            for (int c = 0; c < DC / 2; ++c) stage[d * PITCH + col0 + c] = S[c];
+    }
+    const bool lost = __syncthreads_or(gave_up);
+    if (lost) {                 // as above
+        if (tid == 0) atomicAdd(&g_linear_timeouts, 1u);
+        bool late = false;
+        if (warp == E_CONTROL && lane == 0) {
+            mma_commit(bar(E_ENDED));
+            wait_for(bar(E_ENDED), 0, late);
+        }
+        for (int s = 0; s < 2; ++s) {
+            if (asked_b > s) wait_for(bar(E_FULL_B + s), ((asked_b - 1 - s) >> 1) & 1, late);
+            if (asked_c > s) wait_for(bar(E_FULL_C + s), ((asked_c - 1 - s) >> 1) & 1, late);
+        }
+    }
+    float* to = m.local + ((bt * m.heads + h) * m.pieces + p) * m.da * m.dc;
+#pragma unroll 4
+    for (int i = tid; i < m.da * m.dc; i += THREADS) to[i] = lost ? NAN : stage[i / m.dc * PITCH + i % m.dc];
+    fence_before();
+    __syncthreads();
+    fence_after();
+    if (warp == E_CONTROL) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
 // ------------------------------------------------------------------------------------------- host
@@ -607,25 +773,25 @@ bool tile_map(const LinearView& x, int width, int64_t heads, int64_t length, int
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int DA, int DC, int PARTS, bool ENDS>
-cudaError_t launch(const March& m, const Tiles& tiles, cudaStream_t st) {
-    static std::atomic<uint64_t> done{0};
-    const size_t bytes = Room<DA, DC, PARTS>::BYTES;
-    const cudaError_t e = allow_smem(march_mma_kernel<DA, DC, PARTS, ENDS>, bytes, done);
+template <typename Kernel>
+cudaError_t launch(Kernel kernel, size_t bytes, int pieces, std::atomic<uint64_t>& done, const March& m, const Tiles& tiles, cudaStream_t st) {
+    const cudaError_t e = allow_smem(kernel, bytes, done);
     if (e != cudaSuccess) return e;
-    const int64_t blocks = m.batch * m.heads * (ENDS ? m.pieces - 1 : m.pieces);
+    const int64_t blocks = m.batch * m.heads * pieces;
     if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
-    return launch_kernel_smem(march_mma_kernel<DA, DC, PARTS, ENDS>, dim3((unsigned)blocks), dim3(THREADS), bytes, st, m, tiles);
+    return launch_kernel_smem(kernel, dim3((unsigned)blocks), dim3(THREADS), bytes, st, m, tiles);
 }
 
 template <int DA, int DC, int PARTS>
 cudaError_t run_parts(const March& m, const Tiles& tiles, cudaStream_t st) {
     if (m.pieces > 1 && !m.local_there) {
-        cudaError_t e = launch<DA, DC, PARTS, true>(m, tiles, st);
+        static std::atomic<uint64_t> done{0};
+        cudaError_t e = launch(march_mma_ends_kernel<DA, DC, PARTS>, EndsRoom<DA, DC, PARTS>::BYTES, m.pieces - 1, done, m, tiles, st);
         if (e == cudaSuccess) e = march_join(m, st);
         if (e != cudaSuccess) return e;
     }
-    return launch<DA, DC, PARTS, false>(m, tiles, st);
+    static std::atomic<uint64_t> done{0};
+    return launch(march_mma_kernel<DA, DC, PARTS>, Room<DA, DC, PARTS>::BYTES, m.pieces, done, m, tiles, st);
 }
 // A state that leaves the march is fp32's; one that only `far` reads is rounded to bf16 there, and two parts of bw are enough.
 template <int DA, int DC>
