@@ -297,24 +297,32 @@ __global__ void __launch_bounds__(THREADS, DA == 32 ? 5 : DA == 64 ? 3 : 2) marc
 }
 
 // Eight pieces at a time, so that their loads are on their way together.
-__global__ void __launch_bounds__(256) join_kernel(March m) {
+constexpr int SQUARE = 16;                     // features of a block either way: a turned state is read by whole sectors too
+__global__ void __launch_bounds__(SQUARE * SQUARE) join_kernel(March m) {
+    __shared__ float parts[2];
     pdl_wait_then_trigger();
-    const int64_t size = (int64_t)m.da * m.dc, across = (size + 255) / 256;
-    const int64_t i = blockIdx.x % across * 256 + threadIdx.x, row = blockIdx.x / across;
-    if (i >= size) return;
-    const double g = power(m.log_decay[row % m.heads], (double)m.piece);
-    const float hi = (float)g, lo = (float)(g - hi);
+    const int across = (m.dc + SQUARE - 1) / SQUARE, squares = across * ((m.da + SQUARE - 1) / SQUARE);
+    const int64_t row = blockIdx.x / (unsigned)squares, size = (int64_t)m.da * m.dc;
+    const int square = (int)(blockIdx.x - row * squares), d = square / across * SQUARE + threadIdx.x / SQUARE, e = square % across * SQUARE + threadIdx.x % SQUARE;
+    if (threadIdx.x == 0) {
+        const double g = power(m.log_decay[row % m.heads], (double)m.piece);
+        parts[0] = (float)g;
+        parts[1] = (float)(g - (float)g);
+    }
+    __syncthreads();
+    if (d >= m.da || e >= m.dc) return;
+    const float hi = parts[0], lo = parts[1];
     float s = 0.f;
-    if (m.start != nullptr) s = m.start[row * size + (m.start_turned ? i % m.dc * m.da + i / m.dc : i)];
-    float* at = m.local + row * m.pieces * size + i;
+    if (m.start != nullptr) s = m.start[row * size + (m.start_turned ? e * m.da + d : d * m.dc + e)];
+    float* at = m.local + row * m.pieces * size + d * m.dc + e;
     for (int p = 0; p < m.pieces; p += 8, at += 8 * size) {
         float u[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) u[e] = p + e < m.pieces - 1 ? at[e * size] : 0.f;
+        for (int k = 0; k < 8; ++k) u[k] = p + k < m.pieces - 1 ? at[k * size] : 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (p + e < m.pieces) at[e * size] = s;
-            s = fmaf(hi, s, fmaf(lo, s, u[e]));
+        for (int k = 0; k < 8; ++k) {
+            if (p + k < m.pieces) at[k * size] = s;
+            s = fmaf(hi, s, fmaf(lo, s, u[k]));
         }
     }
 }
@@ -403,12 +411,13 @@ bool on_tensor_cores(const fpde_linear_args* a) { return a->dtype == FPDE_BF16 &
 // Pieces of a row.  With more than one, all but the last are marched through twice, the first time for their ends alone, and the
 // states are joined in between.  The number with the least time of waves of blocks is taken; the figures are measured
 // microseconds of a chunk and of a block's start, and of the join, which reads and writes a state for each piece.
-void cut(const fpde_linear_args* a, March& m) {
+void cut(const fpde_linear_args* a, March& m, bool gradient) {
     const bool mma = on_tensor_cores(a), wide = m.da > 64 || m.dc > 64;
     const int chunk = mma ? MMA_CHUNK : C;
-    const double main = mma ? (wide ? 4.3 : 2.5) : 4.0, ends = mma ? (wide ? 2.8 : 1.6) : 2.0, start = mma ? 6. : 4.;
+    const double main = mma ? (wide ? 4.3 : 2.5) : 4.0, ends = mma ? (wide ? 2.8 : 1.2) : 2.0, start = mma ? 6. : 4.;
     const int64_t rows = m.batch * m.heads * (mma ? 1 : ceil_div(m.dc, 64)), slots = mma ? MMA_BLOCKS : 148 * 4, chunks = ceil_div(m.length, chunk);
     const double join = (double)m.batch * m.heads * m.da * m.dc * 8 / 5e6;
+    const double first = gradient ? 2. / 3. : 1.;         // of three marches one uses another's states
     int64_t best = 1;
     double least = 1e300;
     for (int64_t p = 1; p <= chunks && p <= 1024 && rows * (p - 1) < 8 * slots; ++p) {
@@ -417,7 +426,7 @@ void cut(const fpde_linear_args* a, March& m) {
         // a chunk takes longer the more blocks read memory with it: 4.3 us of 128 x 128 features on 64 SMs, 5.5 on all
         const auto load = [&](int64_t blocks) { return 0.8 + 0.45 * (blocks < slots ? (double)blocks / slots : 1.); };
         double time = (double)ceil_div(rows * p, slots) * (start + each * main * load(rows * p));
-        if (p > 1) time += (double)ceil_div(rows * (p - 1), slots) * (start + each * ends * load(rows * (p - 1))) + 3. + p * join;
+        if (p > 1) time += first * ((double)ceil_div(rows * (p - 1), slots) * (start + each * ends * load(rows * (p - 1))) + 3. + p * join);
         if (time < least) {
             least = time;
             best = p;
@@ -451,7 +460,7 @@ March march_o(const fpde_linear_args* a) {
     m.start = a->state;
     m.out = a->o;
     m.end = a->state_out;
-    cut(a, m);
+    cut(a, m, false);
     return m;
 }
 March march_gq(const fpde_linear_args* a) {
@@ -466,7 +475,7 @@ March march_gq(const fpde_linear_args* a) {
     m.start = a->state;
     m.start_turned = 1;
     m.out = a->gq;
-    cut(a, m);
+    cut(a, m, true);
     return m;
 }
 March march_gv(const fpde_linear_args* a) {
@@ -482,7 +491,7 @@ March march_gv(const fpde_linear_args* a) {
     m.start = a->gstate_out;
     m.out = a->gv;
     m.end = a->gstate;
-    cut(a, m);
+    cut(a, m, true);
     return m;
 }
 // Starts from the states that gv's march has joined, turned.
@@ -563,9 +572,9 @@ int as_status(cudaError_t e) { return e == cudaSuccess ? FPDE_OK : FPDE_ERR_CUDA
 }  // namespace
 
 cudaError_t march_join(const March& m, cudaStream_t st) {
-    const int64_t blocks = m.batch * m.heads * ceil_div((int64_t)m.da * m.dc, 256);
+    const int64_t blocks = m.batch * m.heads * ceil_div(m.da, SQUARE) * ceil_div(m.dc, SQUARE);
     if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
-    return launch_kernel(join_kernel, dim3((unsigned)blocks), dim3(256), st, m);
+    return launch_kernel(join_kernel, dim3((unsigned)blocks), dim3(SQUARE * SQUARE), st, m);
 }
 
 }  // namespace fpde
