@@ -414,7 +414,7 @@ bool on_tensor_cores(const fpde_linear_args* a) { return a->dtype == FPDE_BF16 &
 void cut(const fpde_linear_args* a, March& m, bool gradient) {
     const bool mma = on_tensor_cores(a), wide = m.da > 64 || m.dc > 64;
     const int chunk = mma ? MMA_CHUNK : C;
-    const double main = mma ? (wide ? 4.3 : 2.5) : 4.0, ends = mma ? (wide ? 2.8 : 1.2) : 2.0, start = mma ? 6. : 4.;
+    const double main = mma ? (wide ? 4.3 : 2.2) : 4.0, ends = mma ? (wide ? 2.8 : 1.2) : 2.0, start = mma ? 6. : 4.;
     const int64_t rows = m.batch * m.heads * (mma ? 1 : ceil_div(m.dc, 64)), slots = mma ? MMA_BLOCKS : 148 * 4, chunks = ceil_div(m.length, chunk);
     const double join = (double)m.batch * m.heads * m.da * m.dc * 8 / 5e6;
     const double first = gradient ? 2. / 3. : 1.;         // of three marches one uses another's states

@@ -54,8 +54,10 @@ __device__ __forceinline__ void wait_for(uint32_t bar, uint32_t parity, bool& ga
 
 template <int DA, int DC, int PARTS>
 struct Room {
-    static constexpr int A = 0, B = A + DA / 64 * BLOCK, V = B + DA / 64 * BLOCK, BW = V + DC / 64 * BLOCK;
     static constexpr int STATE = (DA * (DC + 1) * 4 + 1023) / 1024 * 1024, PLANES = PARTS * (DA / 64) * BLOCK;      // fp32 state and bw share a place
+    static constexpr int TILES = (2 * DA + DC) / 64 * BLOCK, REST = (PLANES > STATE ? PLANES : STATE) + DC / 64 * DA * 128 + 1024;
+    static constexpr int STAGES = 2 * TILES + REST <= 226 * 1024 ? 2 : 1;       // places of each tile
+    static constexpr int A = 0, B = A + STAGES * (DA / 64) * BLOCK, V = B + STAGES * (DA / 64) * BLOCK, BW = V + STAGES * (DC / 64) * BLOCK;
     static constexpr int S = BW + (PLANES > STATE ? PLANES : STATE);
     static constexpr int BYTES = S + DC / 64 * DA * 128 + 1024;      // slack to start on 1024 bytes
     static constexpr int G = 0, NEAR = 128, FAR = NEAR + DC, U = FAR + DC;      // columns of TMEM; P lies over G
@@ -232,17 +234,17 @@ template <int DA, int DC, int PARTS>
 __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_constant__ March m, const __grid_constant__ Tiles tiles) {
     using R = Room<DA, DC, PARTS>;
     extern __shared__ uint8_t raw[];
-    __shared__ __align__(8) uint64_t bars[BARS];
+    __shared__ __align__(8) uint64_t bars[2 * BARS];
     __shared__ uint32_t tmem_slot;
     __shared__ __align__(16) float powers[N + 2];
     __shared__ int odd_chunk[2];                                 // the last chunk of either parity with an infinity or NaN in c, counted from 1
     __shared__ float whole[4];                                   // g^128 and that of the last chunk, each in two parts
     const uint32_t base = (smem_u32(raw) + 1023) & ~1023u;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, group = warp / 8, half = warp / 4 % 2, quarter = warp % 4;
-    auto bar = [&](int i) { return smem_u32(&bars[i]); };
+    auto bar = [&](int i, int c) { return smem_u32(&bars[2 * i + (c & 1)]); };
     if (tid == 0) {
         odd_chunk[0] = odd_chunk[1] = 0;
-        for (int i = 0; i < BARS; ++i) mbar_init(bar(i), i >= READY_P && i <= AGAIN ? 8 : 1);
+        for (int i = 0; i < 2 * BARS; ++i) mbar_init(bar(i / 2, i), i / 2 >= READY_P && i / 2 <= AGAIN ? 8 : 1);
         mbar_fence_init();
     }
     if (warp == CONTROL) {
@@ -292,21 +294,20 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
     __syncthreads();
     fence_after();
     constexpr uint32_t tmem = 0;               // all 512 columns: they start there
-    uint32_t phase = 0, odd_phase = 0;
+    uint32_t odd_phase = 0;
     bool gave_up = false;
     int asked_a = 0, asked_b = 0, asked_c = 0; // tiles that this thread has asked for
-    auto wait = [&](int i) { wait_for(bar(i), phase, gave_up); };
-    auto wait_last = [&](int i) { wait_for(bar(i), phase ^ 1, gave_up); };      // of the chunk before
-    auto wait_warp = [&](int i) {
-        wait(i);
+    auto wait = [&](int i, int c) { wait_for(bar(i, c), (c >> 1) & 1, gave_up); };
+    auto wait_warp = [&](int i, int c) {
+        wait(i, c);
         gave_up = __any_sync(~0u, gave_up);
         fence_after();
     };
-    auto signal = [&](int i) {
+    auto signal = [&](int i, int c) {
         fence_async();
         fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(i));
+        if (lane == 0) mbar_arrive(bar(i, c));
     };
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     const int row = quarter * 32 + lane, r = m.reversed ? N - 1 - row : row;      // of the tile, and in the march's order
@@ -320,86 +321,88 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
             const uint64_t da = slice_desc(base + R::A, false), db = slice_desc(base + R::B, false), dc = slice_desc(base + R::V, true, BLOCK),
                            ds = slice_desc(base + R::S, true, DA * 128), dw = slice_desc(base + R::BW, true, BLOCK);
             const bool leader = elected();
-            auto commit = [&](int i) {
-                if (leader) mma_commit(bar(i));
+            auto commit = [&](int i, int c) {
+                if (leader) mma_commit(bar(i, c));
             };
             auto all_wait = [&]() {
                 __syncwarp();
                 gave_up = __any_sync(~0u, gave_up);
                 fence_after();
             };
-            for (int c = 0; c < chunks; ++c, phase ^= 1) {
-                wait(FULL_A);
-                wait(FULL_B);
-                if (c > 0 && *(volatile int*)&odd_chunk[phase ^ 1] == c) {         // P, near and far are still read
-                    wait_for(bar(AGAIN), odd_phase, gave_up);
+            for (int c = 0; c < chunks; ++c) {
+                wait(FULL_A, c);
+                wait(FULL_B, c);
+                if (c > 0 && *(volatile int*)&odd_chunk[(c - 1) & 1] == c) {         // P, near and far are still read
+                    wait_for(bar(AGAIN, 0), odd_phase, gave_up);
                     odd_phase ^= 1;
                 }
                 all_wait();
                 if (gave_up) break;
+                const uint32_t at_a = c % R::STAGES * (DA / 64 * BLOCK), at_c = c % R::STAGES * (DC / 64 * BLOCK);
 #pragma unroll
                 for (int k = 0; k < DA / 16; ++k)
-                    product(leader, tmem + R::G, desc_at(da, k / 4 * BLOCK + k % 4 * 32), desc_at(db, k / 4 * BLOCK + k % 4 * 32), IDESC_G, k > 0);
-                commit(DONE_G);
-                wait(READY_BW);
-                wait(READY_S);                 // U before this one has been added, and S is the state before this chunk
-                wait(FULL_C);
+                    product(leader, tmem + R::G, desc_at(da, at_a + k / 4 * BLOCK + k % 4 * 32), desc_at(db, at_a + k / 4 * BLOCK + k % 4 * 32), IDESC_G, k > 0);
+                commit(DONE_G, c);
+                wait(READY_BW, c);
+                wait(READY_S, c);                 // U before this one has been added, and S is the state before this chunk
+                wait(FULL_C, c);
                 all_wait();
                 if (gave_up) break;
 #pragma unroll
                 for (int s = PARTS - 1; s >= 0; --s)           // the small parts first: the sum is rounded towards zero at every product
 #pragma unroll
                     for (int k = 0; k < N / 16; ++k)
-                        product(leader, tmem + R::U, desc_at(dw, s * (DA / 64) * BLOCK + k * 2048), desc_at(dc, k * 2048), IDESC_U, s < PARTS - 1 || k > 0);
-                commit(DONE_U);
-                if (c > 0) wait_last(FREE_OUT);
+                        product(leader, tmem + R::U, desc_at(dw, s * (DA / 64) * BLOCK + k * 2048), desc_at(dc, at_c + k * 2048), IDESC_U, s < PARTS - 1 || k > 0);
+                commit(DONE_U, c);
+                if (c > 0) wait(FREE_OUT, c - 1);
                 all_wait();
                 if (gave_up) break;
 #pragma unroll
                 for (int k = 0; k < DA / 16; ++k)
-                    product(leader, tmem + R::FAR, desc_at(da, k / 4 * BLOCK + k % 4 * 32), desc_at(ds, k * 2048), IDESC_OUT, k > 0);
-                commit(DONE_FAR);
-                wait(READY_P);
+                    product(leader, tmem + R::FAR, desc_at(da, at_a + k / 4 * BLOCK + k % 4 * 32), desc_at(ds, k * 2048), IDESC_OUT, k > 0);
+                commit(DONE_FAR, c);
+                wait(READY_P, c);
                 all_wait();
                 if (gave_up) break;
 #pragma unroll
-                for (int k = 0; k < N / 16; ++k) product_tmem(leader, tmem + R::NEAR, tmem + R::G + p_column(k), desc_at(dc, k * 2048), IDESC_OUT, k > 0);
-                commit(DONE_NEAR);
+                for (int k = 0; k < N / 16; ++k) product_tmem(leader, tmem + R::NEAR, tmem + R::G + p_column(k), desc_at(dc, at_c + k * 2048), IDESC_OUT, k > 0);
+                commit(DONE_NEAR, c);
             }
         } else if (quarter == 1 && lane == 0) {                // tiles
             auto load = [&](int full, int at, int blocks, const CUtensorMap* map, int head, int batch, int c) {
-                mbar_expect_tx(bar(full), blocks * BLOCK);
+                const uint32_t to = base + at + c % R::STAGES * (blocks * BLOCK);
+                mbar_expect_tx(bar(full, c), blocks * BLOCK);
                 const int node = (int)(m.reversed ? m.length - first - N : first) + (m.reversed ? -N : N) * c;
-                for (int f = 0; f < blocks; ++f) load_tile(base + at + f * BLOCK, map, 64 * f, head * (int)h, node, batch * (int)bt, bar(full));
+                for (int f = 0; f < blocks; ++f) load_tile(to + f * BLOCK, map, 64 * f, head * (int)h, node, batch * (int)bt, bar(full, c));
             };
-            // the places are the last chunk's: b is read by G and for bw, a by G and far, c by U, near and the scan
+            // the places are an earlier chunk's: b is read by G and for bw, a by G and far, c by U, near and the scan
             for (int c = 0; c < chunks; ++c) {
-                if (c > 0) {
-                    wait(READY_BW);
-                    wait(DONE_G);
+                const int before = c - R::STAGES;
+                if (before >= 0) {
+                    wait(READY_BW, before);
+                    wait(DONE_G, before);
                 }
                 if (gave_up) break;
                 load(FULL_B, R::B, DA / 64, &tiles.b, tiles.head_b, tiles.batch_b, c);
                 ++asked_b;
-                if (c > 0) wait(DONE_FAR);
+                if (before >= 0) wait(DONE_FAR, before);
                 if (gave_up) break;
                 load(FULL_A, R::A, DA / 64, &tiles.a, tiles.head_a, tiles.batch_a, c);
                 ++asked_a;
-                if (c > 0) wait(DONE_NEAR);
+                if (before >= 0) wait(DONE_NEAR, before);
                 if (gave_up) break;
                 load(FULL_C, R::V, DC / 64, &tiles.c, tiles.head_c, tiles.batch_c, c);
                 ++asked_c;
-                if (c > 0) phase ^= 1;
             }
         }
     } else if (group == GROUP_BW) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
-        for (int c = 0; c < chunks; ++c, phase ^= 1) {
+        for (int c = 0; c < chunks; ++c) {
             const int n = c < chunks - 1 ? N : tail;
-            wait_warp(FULL_B);
+            wait_warp(FULL_B, c);
             // bw's place is the last chunk's until U is done, the state's before that
-            if (c > 0) wait_last(DONE_U);
-            else wait(READY_S);
+            if (c > 0) wait(DONE_U, c - 1);
+            else wait(READY_S, 0);
             gave_up = __any_sync(~0u, gave_up);
             if (gave_up) break;
             const float w = r < n ? m.gain * powers[n - 1 - r + m.shift] : 0.f;
@@ -407,12 +410,12 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
 #pragma unroll 1
             for (int q = half * (DA / 16); q < (half + 1) * (DA / 16); ++q) {
                 uint32_t out[PARTS][4];
-                weigh<PARTS>(out, lds16(chunk_at(base + R::B, row, q)), w, w1, w2);
+                weigh<PARTS>(out, lds16(chunk_at(base + R::B + c % R::STAGES * (DA / 64 * BLOCK), row, q)), w, w1, w2);
 #pragma unroll
                 for (int s = 0; s < PARTS; ++s)
                     sts16(chunk_at(base + R::BW + s * (DA / 64) * BLOCK, row, q), make_uint4(out[s][0], out[s][1], out[s][2], out[s][3]));
             }
-            signal(READY_BW);
+            signal(READY_BW, c);
         }
     } else if (group == GROUP_P) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(P_REGS));
@@ -428,8 +431,8 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                 steps[k] = m.reversed ? pair(exp2_f32(2 * k * l), exp2_f32((2 * k + 1) * l)) : pair(exp2_f32((15 - 2 * k) * l), exp2_f32((14 - 2 * k) * l));
         };
         make_steps();
-        for (int c = 0; c < chunks; ++c, phase ^= 1) {
-            wait_warp(DONE_G);
+        for (int c = 0; c < chunks; ++c) {
+            wait_warp(DONE_G, c);
             if (gave_up) break;
             // 32 columns at a time, a thread every other: those of this quarter's own nodes are cut along the diagonal, those of the
             // nodes before them are whole, the others zeros.  Column k of the 32 is the product times g^(32 before + lane - k), or + k - lane.
@@ -456,17 +459,17 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                 tmem_store8(tmem + R::G + p_column(2 * part) + col / 2 + lanes, packed);
             }
             tmem_stored();
-            wait_warp(SCANNED);                // before READY_P: the next chunk's cannot be over yet
+            wait_warp(SCANNED, c);                // before READY_P: the next chunk's cannot be over yet
             if (gave_up) break;
-            signal(READY_P);
-            if (*(volatile int*)&odd_chunk[phase] == c + 1) {
-                wait_warp(FREE_OUT);           // and the rows are stored
+            signal(READY_P, c);
+            if (*(volatile int*)&odd_chunk[c & 1] == c + 1) {
+                wait_warp(FREE_OUT, c);           // and the rows are stored
                 if (gave_up) break;
                 const int64_t dir = m.reversed ? -1 : 1, node = (m.reversed ? m.length - 1 - first : first) + dir * (c * N);
                 sum_again<DC>(m, (const __nv_bfloat16*)m.c.p + bt * m.c.batch + h * m.c.head + node * m.c.node, dir * m.c.node,
                               (__nv_bfloat16*)m.out + ((bt * m.length + node + dir * r) * m.heads + h) * m.dc, c < chunks - 1 ? N : tail, r, lanes, half * (DC / 2),
                               m.far * powers[r + 1 - m.shift]);
-                signal(AGAIN);
+                signal(AGAIN, 0);
                 make_steps();                  // rather than kept meanwhile
             }
         }
@@ -487,29 +490,29 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                           make_uint4(pack_bf16(S[8 * q], S[8 * q + 1]), pack_bf16(S[8 * q + 2], S[8 * q + 3]), pack_bf16(S[8 * q + 4], S[8 * q + 5]),
                                      pack_bf16(S[8 * q + 6], S[8 * q + 7])));
             }
-            signal(READY_S);
         };
         put_state();
+        signal(READY_S, 0);
         const int64_t dir = m.reversed ? -1 : 1, origin = m.reversed ? m.length - 1 - first : first;
         __nv_bfloat16* out = (__nv_bfloat16*)m.out + (bt * m.length * m.heads + h) * m.dc + col0;
-        for (int c = 0; c < chunks; ++c, phase ^= 1) {
+        for (int c = 0; c < chunks; ++c) {
             const int n = c < chunks - 1 ? N : tail;
             // an infinity or NaN in c makes NaN of P's zeros for the nodes before it: their rows are summed again
-            wait_warp(FULL_C);
+            wait_warp(FULL_C, c);
             if (gave_up) break;
             __nv_bfloat162 sum = {}, zero = {};
 #pragma unroll 2
             for (int q = half * (DC / 16); q < (half + 1) * (DC / 16); ++q) {
-                const uint4 v = lds16(chunk_at(base + R::V, row, q));
+                const uint4 v = lds16(chunk_at(base + R::V + c % R::STAGES * (DC / 64 * BLOCK), row, q));
                 sum = __hfma2(reinterpret_cast<const __nv_bfloat162&>(v.x), zero, sum);
                 sum = __hfma2(reinterpret_cast<const __nv_bfloat162&>(v.y), zero, sum);
                 sum = __hfma2(reinterpret_cast<const __nv_bfloat162&>(v.z), zero, sum);
                 sum = __hfma2(reinterpret_cast<const __nv_bfloat162&>(v.w), zero, sum);
             }
-            if ((reinterpret_cast<const uint32_t&>(sum) & 0x7fff7fffu) != 0) odd_chunk[phase] = c + 1;
-            signal(SCANNED);
-            wait_warp(DONE_U);
-            wait_warp(DONE_FAR);                   // S is written over
+            if ((reinterpret_cast<const uint32_t&>(sum) & 0x7fff7fffu) != 0) odd_chunk[c & 1] = c + 1;
+            signal(SCANNED, c);
+            wait_warp(DONE_U, c);
+            wait_warp(DONE_FAR, c);                   // S is written over
             if (gave_up) break;
             const float hi = whole[n == N ? 0 : 2], lo = whole[n == N ? 1 : 3];
 #pragma unroll
@@ -523,7 +526,8 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                 }
             }
             put_state();
-            wait_warp(DONE_NEAR);
+            signal(READY_S, c + 1);
+            wait_warp(DONE_NEAR, c);
             if (gave_up) break;
             const float w = m.far * powers[r + 1 - m.shift];
             __nv_bfloat16* to = out + (origin + dir * (c * N + r)) * m.heads * m.dc;
@@ -548,7 +552,7 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                     }
                 }
             }
-            signal(FREE_OUT);
+            signal(FREE_OUT, c);
         }
         if (holds)
 #pragma unroll
@@ -559,12 +563,14 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
         if (tid == 0) atomicAdd(&g_linear_timeouts, 1u);
         bool late = false;
         if (warp == CONTROL && lane == 0) {
-            mma_commit(bar(ENDED));
-            wait_for(bar(ENDED), 0, late);
+            mma_commit(bar(ENDED, 0));
+            wait_for(bar(ENDED, 0), 0, late);
         }
-        if (asked_a > 0) wait_for(bar(FULL_A), (asked_a - 1) & 1, late);
-        if (asked_b > 0) wait_for(bar(FULL_B), (asked_b - 1) & 1, late);
-        if (asked_c > 0) wait_for(bar(FULL_C), (asked_c - 1) & 1, late);
+        for (int s = 0; s < 2; ++s) {
+            if (asked_a > s) wait_for(bar(FULL_A, s), ((asked_a - 1 - s) >> 1) & 1, late);
+            if (asked_b > s) wait_for(bar(FULL_B, s), ((asked_b - 1 - s) >> 1) & 1, late);
+            if (asked_c > s) wait_for(bar(FULL_C, s), ((asked_c - 1 - s) >> 1) & 1, late);
+        }
         for (int64_t i = first * m.dc + tid; i < last * m.dc; i += THREADS) {
             const int64_t node = m.reversed ? m.length - 1 - i / m.dc : i / m.dc;
             ((__nv_bfloat16*)m.out)[((bt * m.length + node) * m.heads + h) * m.dc + i % m.dc] = __float2bfloat16_rn(NAN);
