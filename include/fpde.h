@@ -625,10 +625,10 @@ int fpde_head_rotary_bwd(const fpde_head_args* args, void* stream);
  * each piece.  Infinities and NaN of a node reach no earlier node and no other head; from that node on the sums that they enter
  * are infinite or NaN, not always the one of the two that a march through the nodes would give.
  *
- * Precision: states are fp32's, and products and sums are formed in 32 bits.  bf16 rows of more than 64 nodes, where TMA can
- * read them (16-byte aligned base, strides of whole 16 bytes), take the tensor cores: there the factor between two nodes of
- * 128, scale * g^n * (q . k), and the state that an output reads are rounded to bf16 once, which leaves about as much as the
- * output's own rounding; the states handed on are sums of products whose factors keep 22 bits and more.
+ * Precision: states are fp32's, and products and sums are formed in 32 bits.  bf16 rows of some length (24 nodes of up to 128
+ * features, 40 of 64, 193 of 32) that TMA can read (bases and strides of whole 16 bytes) take the tensor cores: there
+ * g^n (q . k) of two nodes, and the state that an output reads, are rounded to bf16 once more, which leaves
+ * about as much as the output's own rounding; the states handed on are sums of products that keep fp32's bits.
  */
 #define FPDE_LINEAR_MAX_DIM 128
 

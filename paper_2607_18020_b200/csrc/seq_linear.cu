@@ -20,8 +20,10 @@ constexpr int C = 32, THREADS = 128;
 
 // The march of 32- and 16-bit arrays in 32 bits.  A block takes a row and head, or a piece, and up to 64 features of c, in
 // chunks of 32 nodes: a, b and c in shared memory as fp32, the next chunk's on their way there (fp32 arrays: copied; 16-bit ones are
-// widened when their turn comes), the state there too.  The four products run in packed
-// arithmetic.
+// widened when their turn comes), the state there too.  The four products run in packed arithmetic.  Registers filled from shared
+// memory bind it, then instructions: 256 x 128 nodes of 4 heads of 32 in fp32, 44 us a march (with tiles of 2 x 4 for all products and
+// without the skipped pairs 60; memory's floor is 10).  16 nodes a chunk would be fewer multiplications, but more barriers and half a tile
+// for each thread.
 template <typename T, int DA, int DC>
 struct Sizes {
     static constexpr int PA = DA + 4, PC = DC + 4, PP = C + 4, STAGES = sizeof(T) == 4 && DA <= 64 ? 2 : 1;
@@ -296,7 +298,7 @@ __global__ void __launch_bounds__(THREADS, DA == 32 ? 5 : DA == 64 ? 3 : 2) marc
     }
 }
 
-// Eight pieces at a time, so that their loads are on their way together.
+// What each piece leaves becomes the state that each starts from; eight pieces at a time, so that their loads are on their way together.
 constexpr int SQUARE = 16;                     // features of a block either way: a turned state is read by whole sectors too
 __global__ void __launch_bounds__(SQUARE * SQUARE) join_kernel(March m) {
     __shared__ float parts[2];
@@ -328,7 +330,8 @@ __global__ void __launch_bounds__(SQUARE * SQUARE) join_kernel(March m) {
 }
 
 // One node of every row and head.  A block takes one head's state: LX lanes of V columns each, the rows over the
-// rest of its threads, whose shares of the output are summed in shared memory.
+// rest of its threads, whose shares of the output are summed in shared memory.  Memory bounds it, the state's way there and back:
+// 256 rows of 32 heads of 128 x 128, 200 us of 165.
 constexpr int STEP_THREADS = 256;
 template <typename T, int V>
 __global__ void __launch_bounds__(STEP_THREADS) linear_step_kernel(LinearView q, LinearView k, LinearView v, const float* __restrict__ log_decay,
@@ -405,8 +408,14 @@ int check_linear(const fpde_linear_args* a, bool step) {
     return FPDE_OK;
 }
 
-// Rows of up to 64 nodes fill less than half of a chunk there.
-bool on_tensor_cores(const fpde_linear_args* a) { return a->dtype == FPDE_BF16 && a->length > 64; }
+// A chunk there takes as long however few of its 128 nodes and 64 or 128 features there are.  2048 rows and heads, 32-bit
+// arithmetic and tensor cores: 32 features, 192 nodes 143 and 155 us, 256 nodes 186 and 158; 64 features, 40 nodes 139 and 138, 96 nodes 231
+// and 144; 128 features, 24 nodes 400 and 261, 96 nodes 933 and 280.  fp16's range is too short for products of queries and
+// keys and for states, so its arrays are widened.
+bool on_tensor_cores(const fpde_linear_args* a) {
+    const int64_t widest = a->dk > a->dv ? a->dk : a->dv, enough = widest <= 32 ? 193 : widest <= 64 ? 40 : 24;
+    return a->dtype == FPDE_BF16 && a->length >= enough;
+}
 
 // Pieces of a row.  With more than one, all but the last are marched through twice, the first time for their ends alone, and the
 // states are joined in between.  The number with the least time of waves of blocks is taken; the figures are measured
