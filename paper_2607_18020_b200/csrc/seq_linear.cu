@@ -419,23 +419,22 @@ bool on_tensor_cores(const fpde_linear_args* a) {
 
 // Pieces of a row.  With more than one, all but the last are marched through twice, the first time for their ends alone, and the
 // states are joined in between.  The number with the least time of waves of blocks is taken; the figures are measured
-// microseconds of a chunk and of a block's start, and of the join, which reads and writes a state for each piece.
+// microseconds of a chunk and of a block's start, and of two more launches and the join, which reads and writes a state for each piece.
 void cut(const fpde_linear_args* a, March& m, bool gradient) {
     const bool mma = on_tensor_cores(a), wide = m.da > 64 || m.dc > 64;
     const int chunk = mma ? MMA_CHUNK : C;
-    const double main = mma ? (wide ? 4.3 : 2.2) : 4.0, ends = mma ? (wide ? 2.8 : 1.2) : 2.0, start = mma ? 6. : 4.;
+    const double main = mma ? (wide ? 4.3 : 2.5) : 4.0, ends = mma ? (wide ? 2.8 : 1.2) : 2.0, start = mma ? 6. : 4.;
     const int64_t rows = m.batch * m.heads * (mma ? 1 : ceil_div(m.dc, 64)), slots = mma ? MMA_BLOCKS : 148 * 4, chunks = ceil_div(m.length, chunk);
     const double join = (double)m.batch * m.heads * m.da * m.dc * 8 / 5e6;
     const double first = gradient ? 2. / 3. : 1.;         // of three marches one uses another's states
     int64_t best = 1;
     double least = 1e300;
-    for (int64_t p = 1; p <= chunks && p <= 1024 && rows * (p - 1) < 8 * slots; ++p) {
-        const int64_t each = ceil_div(chunks, p);
-        if (ceil_div(chunks, each) != p) continue;
+    for (int64_t p = 1, each; p <= chunks && p <= 1024 && rows * (p - 1) < 8 * slots; p = each > 1 ? ceil_div(chunks, each - 1) : chunks + 1) {
+        each = ceil_div(chunks, p);
         // a chunk takes longer the more blocks read memory with it: 4.3 us of 128 x 128 features on 64 SMs, 5.5 on all
         const auto load = [&](int64_t blocks) { return 0.8 + 0.45 * (blocks < slots ? (double)blocks / slots : 1.); };
         double time = (double)ceil_div(rows * p, slots) * (start + each * main * load(rows * p));
-        if (p > 1) time += first * ((double)ceil_div(rows * (p - 1), slots) * (start + each * ends * load(rows * (p - 1))) + 3. + p * join);
+        if (p > 1) time += first * ((double)ceil_div(rows * (p - 1), slots) * (start + each * ends * load(rows * (p - 1))) + 4.5 + p * join);
         if (time < least) {
             least = time;
             best = p;

@@ -3,7 +3,7 @@ import ctypes
 
 import pytest
 
-from attention_forms import ONE, PIECES, PLAIN, linear_forms
+from attention_forms import MIXED, ONE, PIECES, PLAIN, linear_forms
 from paper_2607_18020_b200 import binding as B
 
 
@@ -21,6 +21,12 @@ def test_rows_in_one_piece_on_tensor_cores(case):
 @pytest.mark.parametrize("case", PLAIN)
 def test_rows_in_pieces_of_32_bit_arithmetic(case, dtype):
     assert all(pieces > 1 and not mma for pieces, mma in linear_forms(dtype, *case))
+
+
+@pytest.mark.parametrize("case", MIXED)
+def test_rows_in_one_piece_forwards_and_several_backwards(case):
+    o, *rest = linear_forms("float32", *case)
+    assert o == (1, False) and all(pieces > 1 and not mma for pieces, mma in rest)
 
 
 def test_questions_refused():

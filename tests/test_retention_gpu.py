@@ -5,7 +5,7 @@ import random
 import pytest
 
 torch = pytest.importorskip("torch")
-from attention_forms import ONE, PIECES, PLAIN
+from attention_forms import MIXED, ONE, PIECES, PLAIN
 from attention_util import attention_bound, check_attention, linear_ref, norm_ref, rotary_ref
 from seq_util import GuardedTorch, d64, rel
 
@@ -70,7 +70,7 @@ def test_forms_on_tensor_cores(case, ends, guard):
 
 
 @pytest.mark.parametrize("dtype", [F32, F16])
-@pytest.mark.parametrize("case", PLAIN)
+@pytest.mark.parametrize("case", PLAIN + MIXED)
 def test_forms_of_32_bit_arithmetic(case, dtype, guard):
     batch, length, heads, dk, dv = case
     r = gen(42)
