@@ -21,7 +21,8 @@ A row that continues gives the rotation its first node's position: `offset=`, or
 they compute values, and a backward pass that reaches their result raises.  Activations are fp32, bf16 or fp16 CUDA tensors
 of one type whose channel or feature axis is contiguous (slices of a wider projection are read in place);
 parameters, frequencies and states are fp32.  Everything runs in libfpde.so on torch's current stream; torch
-allocates the outputs and the scratch memory.  There is no CPU path.
+allocates the outputs and the scratch memory.  There is no CPU path.  Calls can be captured into CUDA graphs, a
+backward pass as torch allows it: while no eager graph of the same leaves lives.
 """
 from __future__ import annotations
 
@@ -636,9 +637,13 @@ def _linear_fwd(q, k, v, log_decay, scale, state, ends):
 
 def linear_attention_bwd(go, q, k, v, log_decay, scale=1.0, state=None, gstate=None) -> LinearGrads:
     """Gradients of linear_attention_fwd for upstream gradients go of `o` and `gstate` of the last state."""
+    return _linear_bwd(go, q, k, v, log_decay, scale, state, gstate, state is not None)
+
+
+def _linear_bwd(go, q, k, v, log_decay, scale, state, gstate, of_state):
     a, t = _linear_plan("linear bwd", q, k, v, log_decay, scale, state, go, gstate)
     dev = q.device
-    g = LinearGrads(_new(q), _new(k), _new(v), _new(state))
+    g = LinearGrads(_new(q), _new(k), _new(v), _new(state) if of_state else None)
     a.go, a.gstate_out = t[5].data_ptr(), _ptr(t[6])
     a.gq, a.gk, a.gv, a.gstate = g.q.data_ptr(), g.k.data_ptr(), g.v.data_ptr(), _ptr(g.state)
     if a.workspace_bytes:
@@ -676,7 +681,7 @@ class _LinearAttention(torch.autograd.Function):
         q, k, v, log_decay, state = ctx.saved_tensors
         if go is None:
             go = torch.zeros_like(v)
-        g = linear_attention_bwd(go, q, k, v, log_decay, ctx.scale, state, glast)
+        g = _linear_bwd(go, q, k, v, log_decay, ctx.scale, state, glast, ctx.needs_input_grad[5])
         return g.q, g.k, g.v, None, None, g.state, None
 
 

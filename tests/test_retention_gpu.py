@@ -281,3 +281,27 @@ def test_two_streams_at_once():
     for i in range(2):
         for g in got[i]:
             assert all(torch.equal(a, e) for a, e in zip(g, want[i]))
+
+
+def test_only_the_gradients_that_are_asked_for():
+    """A state without a gradient, none wanted of the values, and a last state that nobody takes leave the others as they are."""
+    from paper_2607_18020_b200 import sequence as Q
+    r = gen(58)
+    ld = decays(2)
+    for dtype, length in ((F32, 70), (BF16, 700)):
+        q, k, v, go = (r(1, length, 2, 64).to(dtype) for _ in range(4))
+        s, gs = r(1, 2, 64, 64), r(1, 2, 64, 64)
+        want = Q.linear_attention_bwd(go, q, k, v, ld, 0.1, s, gs)
+        leaves = [q.clone().requires_grad_(True), k.clone().requires_grad_(True), v, s]
+        o, last = Q.linear_attention(leaves[0], leaves[1], v, ld, 0.1, s, return_state=True)
+        gq, gk = torch.autograd.grad([o, last], leaves[:2], [go, gs])
+        assert torch.equal(gq, want.q)
+        # gk starts from the joined states of gv's march, which keeps 16 bits of b's weights instead of 24 where no state leaves.  That
+        # moves a state by 2^-17 of itself at most, and so the bf16 factor made of it by one step of 2^-7 in no more than 2^-9 of its
+        # elements: 2^-11.5 in the 2-norm.  With the two results' own roundings, 2^-9 each way: within 2^-8 + 2^-11.5 < 2^-7.
+        assert rel(gk, want.k) <= (2.0 ** -7 if dtype == BF16 else 0.0)
+        o2 = Q.linear_attention(q.requires_grad_(True), k, v, ld, 0.1, s)
+        check_attention("o", o2.detach(), o.detach().double())
+        (gq,) = torch.autograd.grad(o2, [q], go)
+        assert torch.equal(gq, want.q)
+        q.requires_grad_(False)
