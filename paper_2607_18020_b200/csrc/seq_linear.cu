@@ -298,33 +298,44 @@ __global__ void __launch_bounds__(THREADS, DA == 32 ? 5 : DA == 64 ? 3 : 2) marc
     }
 }
 
-// What each piece leaves becomes the state that each starts from; eight pieces at a time, so that their loads are on their way together.
-constexpr int SQUARE = 16;                     // features of a block either way: a turned state is read by whole sectors too
+// What each piece leaves becomes the state that each starts from; four pieces at a time, so that their loads are on their way together.
+constexpr int SQUARE = 16, JOINED = 4;         // features of a block either way, so that a turned state is read by whole sectors too; squares of a block
 __global__ void __launch_bounds__(SQUARE * SQUARE) join_kernel(March m) {
     __shared__ float parts[2];
     pdl_wait_then_trigger();
-    const int across = (m.dc + SQUARE - 1) / SQUARE, squares = across * ((m.da + SQUARE - 1) / SQUARE);
+    const int across = (m.dc + SQUARE - 1) / SQUARE, squares = across * ((m.da + SQUARE * JOINED - 1) / (SQUARE * JOINED));
     const int64_t row = blockIdx.x / (unsigned)squares, size = (int64_t)m.da * m.dc;
-    const int square = (int)(blockIdx.x - row * squares), d = square / across * SQUARE + threadIdx.x / SQUARE, e = square % across * SQUARE + threadIdx.x % SQUARE;
+    const int square = (int)(blockIdx.x - row * squares), d0 = square / across * (SQUARE * JOINED) + threadIdx.x / SQUARE,
+              e = square % across * SQUARE + threadIdx.x % SQUARE;
     if (threadIdx.x == 0) {
         const double g = power(m.log_decay[row % m.heads], (double)m.piece);
         parts[0] = (float)g;
         parts[1] = (float)(g - (float)g);
     }
+    float s[JOINED];
+#pragma unroll
+    for (int j = 0; j < JOINED; ++j) {
+        const int d = d0 + j * SQUARE;
+        s[j] = m.start != nullptr && d < m.da && e < m.dc ? m.start[row * size + (m.start_turned ? e * m.da + d : d * m.dc + e)] : 0.f;
+    }
     __syncthreads();
-    if (d >= m.da || e >= m.dc) return;
+    if (e >= m.dc) return;
     const float hi = parts[0], lo = parts[1];
-    float s = 0.f;
-    if (m.start != nullptr) s = m.start[row * size + (m.start_turned ? e * m.da + d : d * m.dc + e)];
-    float* at = m.local + row * m.pieces * size + d * m.dc + e;
-    for (int p = 0; p < m.pieces; p += 8, at += 8 * size) {
-        float u[8];
+    float* at = m.local + row * m.pieces * size + d0 * m.dc + e;
+    for (int p = 0; p < m.pieces; p += 4, at += 4 * size) {
+        float u[4][JOINED];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) u[k] = p + k < m.pieces - 1 ? at[k * size] : 0.f;
+        for (int k = 0; k < 4; ++k)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            if (p + k < m.pieces) at[k * size] = s;
-            s = fmaf(hi, s, fmaf(lo, s, u[k]));
+            for (int j = 0; j < JOINED; ++j) u[k][j] = p + k < m.pieces - 1 && d0 + j * SQUARE < m.da ? at[k * size + j * SQUARE * m.dc] : 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (p + k >= m.pieces) break;
+#pragma unroll
+            for (int j = 0; j < JOINED; ++j) {
+                if (d0 + j * SQUARE < m.da) at[k * size + j * SQUARE * m.dc] = s[j];
+                s[j] = fmaf(hi, s[j], fmaf(lo, s[j], u[k][j]));
+            }
         }
     }
 }
@@ -580,7 +591,7 @@ int as_status(cudaError_t e) { return e == cudaSuccess ? FPDE_OK : FPDE_ERR_CUDA
 }  // namespace
 
 cudaError_t march_join(const March& m, cudaStream_t st) {
-    const int64_t blocks = m.batch * m.heads * ceil_div(m.da, SQUARE) * ceil_div(m.dc, SQUARE);
+    const int64_t blocks = m.batch * m.heads * ceil_div(m.da, SQUARE * JOINED) * ceil_div(m.dc, SQUARE);
     if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
     return launch_kernel(join_kernel, dim3((unsigned)blocks), dim3(SQUARE * SQUARE), st, m);
 }
