@@ -298,8 +298,10 @@ __global__ void __launch_bounds__(THREADS, DA == 32 ? 5 : DA == 64 ? 3 : 2) marc
     }
 }
 
-// What each piece leaves becomes the state that each starts from; four pieces at a time, so that their loads are on their way together.
+// What each piece leaves becomes the state that each starts from; PIECES pieces at a time, so that their loads are on their way
+// together: 4, or 8 where there are more (2 pieces of 64 rows and heads of 128 x 128: 7 and 14 us; 16 of 8, the whole call: 41 and 36).
 constexpr int SQUARE = 16, JOINED = 4;         // features of a block either way, so that a turned state is read by whole sectors too; squares of a block
+template <int PIECES>
 __global__ void __launch_bounds__(SQUARE * SQUARE) join_kernel(March m) {
     __shared__ float parts[2];
     pdl_wait_then_trigger();
@@ -322,14 +324,14 @@ __global__ void __launch_bounds__(SQUARE * SQUARE) join_kernel(March m) {
     if (e >= m.dc) return;
     const float hi = parts[0], lo = parts[1];
     float* at = m.local + row * m.pieces * size + d0 * m.dc + e;
-    for (int p = 0; p < m.pieces; p += 4, at += 4 * size) {
-        float u[4][JOINED];
+    for (int p = 0; p < m.pieces; p += PIECES, at += PIECES * size) {
+        float u[PIECES][JOINED];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < PIECES; ++k)
 #pragma unroll
             for (int j = 0; j < JOINED; ++j) u[k][j] = p + k < m.pieces - 1 && d0 + j * SQUARE < m.da ? at[k * size + j * SQUARE * m.dc] : 0.f;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < PIECES; ++k) {
             if (p + k >= m.pieces) break;
 #pragma unroll
             for (int j = 0; j < JOINED; ++j) {
@@ -434,7 +436,7 @@ bool on_tensor_cores(const fpde_linear_args* a) {
 void cut(const fpde_linear_args* a, March& m, bool gradient) {
     const bool mma = on_tensor_cores(a), wide = m.da > 64 || m.dc > 64;
     const int chunk = mma ? MMA_CHUNK : C;
-    const double main = mma ? (wide ? 4.3 : 2.5) : 4.0, ends = mma ? (wide ? 2.8 : 1.2) : 2.0, start = mma ? 6. : 4.;
+    const double main = mma ? (wide ? 4.3 : 2.5) : 4.0, ends = mma ? (wide ? 2.2 : 1.2) : 2.0, start = mma ? 6. : 4.;
     const int64_t rows = m.batch * m.heads * (mma ? 1 : ceil_div(m.dc, 64)), slots = mma ? MMA_BLOCKS : 148 * 4, chunks = ceil_div(m.length, chunk);
     const double join = (double)m.batch * m.heads * m.da * m.dc * 8 / 5e6;
     const double first = gradient ? 2. / 3. : 1.;         // of three marches one uses another's states
@@ -593,7 +595,7 @@ int as_status(cudaError_t e) { return e == cudaSuccess ? FPDE_OK : FPDE_ERR_CUDA
 cudaError_t march_join(const March& m, cudaStream_t st) {
     const int64_t blocks = m.batch * m.heads * ceil_div(m.da, SQUARE * JOINED) * ceil_div(m.dc, SQUARE);
     if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
-    return launch_kernel(join_kernel, dim3((unsigned)blocks), dim3(SQUARE * SQUARE), st, m);
+    return launch_kernel(m.pieces > 4 ? join_kernel<8> : join_kernel<4>, dim3((unsigned)blocks), dim3(SQUARE * SQUARE), st, m);
 }
 
 }  // namespace fpde

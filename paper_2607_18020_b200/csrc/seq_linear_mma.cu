@@ -589,14 +589,16 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
 }
 
 // The state that each piece but the last leaves, from zero: U alone.  Nothing but bw's products is there to wait for, so tiles and U have
-// two places each, and bw too where it fits: the tiles' way from memory, bw, its products and the sum of their results overlap.
+// two places each: the tiles' way from memory, bw, its products and the sum of their results overlap.  bw has two places too: of
+// a whole chunk with 64 features of b; of half a chunk's nodes with 128, where eight warps make the one half and eight the other
+// (one place of a whole chunk: half of the nodes of 4 x 4096 x 16 x 128 47 us, 38 so).
 template <int DA, int DC, int PARTS>
 struct EndsRoom {
-    static constexpr int TILE_B = DA / 64 * BLOCK, TILE_C = DC / 64 * BLOCK, FACTORS = PARTS * TILE_B, ROUNDS = DA == 64 ? 2 : 1;
+    static constexpr int TILE_B = DA / 64 * BLOCK, TILE_C = DC / 64 * BLOCK, FACTORS = PARTS * TILE_B, ROUNDS = DA == 64 ? 2 : 1;      // places of whole chunks
     static constexpr int B = 0, V = B + 2 * TILE_B, BW = V + 2 * TILE_C, BYTES = BW + ROUNDS * FACTORS + 1024;
     static_assert(DA * (DC + 1) * 4 <= BW, "the state leaves through the tiles' places");
 };
-enum EndsBar { E_FULL_B, E_FULL_C = E_FULL_B + 2, E_READY_BW = E_FULL_C + 2, E_DONE_U = E_READY_BW + 2, E_READ_U = E_DONE_U + 2, E_ENDED = E_READ_U + 2, E_BARS };
+enum EndsBar { E_FULL_B, E_FULL_C = E_FULL_B + 2, E_READY_BW = E_FULL_C + 2, E_DONE_U = E_READY_BW + 2, E_READ_U = E_DONE_U + 2, E_DONE_HALF = E_READ_U + 2, E_ENDED = E_DONE_HALF + 2, E_BARS };
 constexpr int E_BW_WARPS = 16, E_SUM = 16, E_CONTROL = 24, E_BW_REGS = 48, E_SUM_REGS = 128, E_CONTROL_REGS = 40;
 static_assert(512 * E_BW_REGS + 256 * E_SUM_REGS + 128 * E_CONTROL_REGS <= THREADS * 72, "the groups share what the block starts with");
 
@@ -612,7 +614,7 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_ends_kernel(const __grid
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     if (tid == 0) {
         for (int i = 0; i < E_BARS; ++i)
-            mbar_init(bar(i), i >= E_READY_BW && i < E_DONE_U ? E_BW_WARPS : i >= E_READ_U && i < E_ENDED ? E_CONTROL - E_SUM : 1);
+            mbar_init(bar(i), i >= E_READY_BW && i < E_DONE_U ? E_BW_WARPS * R::ROUNDS / 2 : i >= E_READ_U && i < E_DONE_HALF ? E_CONTROL - E_SUM : 1);
         mbar_fence_init();
     }
     if (warp == E_CONTROL) {
@@ -657,26 +659,34 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_ends_kernel(const __grid
         if (__shfl_sync(~0u, quarter, 0) == 0) {
             const bool leader = elected();
             for (int c = 0; c < chunks; ++c) {
-                wait(E_READY_BW, c);
                 wait(E_FULL_C, c);
                 if (c >= 2) wait(E_READ_U, c - 2);
-                __syncwarp();
-                gave_up = __any_sync(~0u, gave_up);
-                fence_after();
-                if (gave_up) break;
                 const uint64_t dc = slice_desc(base + R::V + (c & 1) * R::TILE_C, true, BLOCK),
                                dw = slice_desc(base + R::BW + (R::ROUNDS == 2 ? c & 1 : 0) * R::FACTORS, true, BLOCK);
+#pragma unroll 1
+                for (int half = 0; half < 3 - R::ROUNDS; ++half) {
+                    if (R::ROUNDS == 2) wait(E_READY_BW, c);
+                    else wait_for(bar(E_READY_BW + half), c & 1, gave_up);
+                    __syncwarp();
+                    gave_up = __any_sync(~0u, gave_up);
+                    fence_after();
+                    if (gave_up) break;
+                    constexpr int K = N / 16 * R::ROUNDS / 2;
 #pragma unroll
-                for (int s = PARTS - 1; s >= 0; --s)           // the small parts first: the sum is rounded towards zero at every product
+                    for (int s = PARTS - 1; s >= 0; --s)       // the small parts first: the sum is rounded towards zero at every product
 #pragma unroll
-                    for (int k = 0; k < N / 16; ++k)
-                        product(leader, tmem + (c & 1) * DC, desc_at(dw, s * R::TILE_B + k * 2048), desc_at(dc, k * 2048), IDESC_U, s < PARTS - 1 || k > 0);
+                        for (int k = 0; k < K; ++k)
+                            product(leader, tmem + (c & 1) * DC, desc_at(dw, s * R::TILE_B + (half * K + k) * 2048), desc_at(dc, (half * K + k) * 2048), IDESC_U,
+                                    half > 0 || s < PARTS - 1 || k > 0);
+                    if (R::ROUNDS == 1 && leader) mma_commit(bar(E_DONE_HALF + half));
+                }
+                if (gave_up) break;
                 if (leader) mma_commit(bar(E_DONE_U + (c & 1)));
             }
         } else if (quarter == 1 && lane == 0) {
             for (int c = 0; c < chunks; ++c) {
                 const int node = (int)(m.reversed ? m.length - first - N : first) + (m.reversed ? -N : N) * c;
-                if (c >= 2) wait(E_READY_BW, c - 2);
+                if (c >= 2) wait(R::ROUNDS == 2 ? E_READY_BW : E_DONE_U, c - 2);      // b has been read
                 if (gave_up) break;
                 mbar_expect_tx(bar(E_FULL_B + (c & 1)), R::TILE_B);
                 for (int f = 0; f < DA / 64; ++f)
@@ -697,7 +707,9 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_ends_kernel(const __grid
         const __nv_bfloat162 w1 = __float2bfloat162_rn(w), w2 = __float2bfloat162_rn(w - __low2float(w1));
         for (int c = 0; c < chunks; ++c) {
             wait(E_FULL_B, c);
-            if (c >= R::ROUNDS) wait(E_DONE_U, c - R::ROUNDS);             // its place is free
+            // its place is free
+            if (R::ROUNDS == 2 && c >= 2) wait(E_DONE_U, c - 2);
+            if (R::ROUNDS == 1 && c >= 1) wait_for(bar(E_DONE_HALF + quarter / 2), (c - 1) & 1, gave_up);
             gave_up = __any_sync(~0u, gave_up);
             if (gave_up) break;
             fence_after();
@@ -709,7 +721,7 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_ends_kernel(const __grid
 #pragma unroll
                 for (int s = 0; s < PARTS; ++s) sts16(chunk_at(to + s * R::TILE_B, row, q), make_uint4(out[s][0], out[s][1], out[s][2], out[s][3]));
             }
-            signal(E_READY_BW, c);
+            signal(E_READY_BW, R::ROUNDS == 2 ? c : quarter / 2);
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(E_SUM_REGS));
