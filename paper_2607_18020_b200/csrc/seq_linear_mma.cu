@@ -334,6 +334,7 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
             for (int c = 0; c < chunks; ++c) {
                 wait(FULL_A, c);
                 wait(FULL_B, c);
+                if (c > 0) wait(DONE_NEAR, c - 1);           // G is written over P: products run in the order of their issue only where they share a sum
                 if (c > 0 && *(volatile int*)&odd_chunk[(c - 1) & 1] == c) {         // P, near and far are still read
                     wait_for(bar(AGAIN, 0), odd_phase, gave_up);
                     odd_phase ^= 1;
