@@ -660,8 +660,12 @@ int fpde_linear_attention_bwd(const fpde_linear_args* args, void* stream);
 /* One node per row (length is taken as 1): `state_out` may be (and usually is) `state` itself. */
 int fpde_linear_attention_step(const fpde_linear_args* args, void* stream);
 /* Bounded waits inside linear attention's products that gave up since the library was loaded (0 in a healthy run; see
- * fpde_diag_tma_timeouts).  The results of a piece of a row that lost one are NaN. */
+ * fpde_diag_tma_timeouts).  The results of a piece of a row that lost one are NaN, and those of the pieces behind it that start from
+ * its state. */
 unsigned int fpde_diag_linear_timeouts(void);
+/* fpde_linear_attention_fwd with a wait that nothing ends in every block of the march on the tensor cores or, `ends`, of the pass for the
+ * pieces' ends: for tests of what such a wait leaves.  Each block counts in fpde_diag_linear_timeouts. */
+int fpde_diag_linear_lost(const fpde_linear_args* args, int ends, void* stream);
 
 /*
  * Orthogonalised update of a stack of `count` matrices (count, rows, cols):

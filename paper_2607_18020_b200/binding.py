@@ -196,6 +196,8 @@ def lib():
             getattr(L, name).argtypes = [ctypes.POINTER(args)] + extra
         L.fpde_diag_ortho_timeouts.restype = ctypes.c_uint
         L.fpde_diag_ortho_timeouts.argtypes = []
+        L.fpde_diag_linear_lost.restype = ctypes.c_int
+        L.fpde_diag_linear_lost.argtypes = [ctypes.POINTER(LinearArgs), ctypes.c_int, ctypes.c_void_p]
         L.fpde_diag_linear_timeouts.restype = ctypes.c_uint
         L.fpde_diag_linear_timeouts.argtypes = []
         _lib = L
@@ -634,7 +636,7 @@ def diag_ortho_timeouts() -> int:
 
 
 def diag_linear_timeouts() -> int:
-    """Bounded waits of linear attention's products that gave up (0 in a healthy run)."""
+    """Blocks of linear attention's products that lost a bounded wait (0 in a healthy run)."""
     return int(lib().fpde_diag_linear_timeouts())
 
 

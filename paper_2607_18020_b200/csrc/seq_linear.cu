@@ -616,15 +616,19 @@ static int check_workspace(const fpde_linear_args* a, int backward) {
     return need > 0 && (a->workspace == nullptr || !aligned(a->workspace, 16) || a->workspace_bytes < need) ? FPDE_ERR_WORKSPACE : FPDE_OK;
 }
 
-int fpde_linear_attention_fwd(const fpde_linear_args* a, void* stream) {
+static int forward(const fpde_linear_args* a, int lose, void* stream) {
     int st = check_linear(a, false);
     if (st != FPDE_OK) return st;
     if (a->batch * a->heads == 0) return FPDE_OK;
     if (a->o == nullptr && a->length > 0) return FPDE_ERR_NULL;
     if (a->state != nullptr && a->state == a->state_out) return FPDE_ERR_PARAM;      // blocks still read it
     if ((st = check_workspace(a, 0)) != FPDE_OK) return st;
-    return as_status(march_by_type(a, march_o(a), (cudaStream_t)stream));
+    March m = march_o(a);
+    m.lose = lose;
+    return as_status(march_by_type(a, m, (cudaStream_t)stream));
 }
+
+int fpde_linear_attention_fwd(const fpde_linear_args* a, void* stream) { return forward(a, 0, stream); }
 
 int fpde_linear_attention_bwd(const fpde_linear_args* a, void* stream) {
     int st = check_linear(a, false);
@@ -651,6 +655,8 @@ int fpde_linear_attention_step(const fpde_linear_args* a, void* stream) {
     if (a->dtype == FPDE_BF16) return as_status(step_run<__nv_bfloat16>(a, s));
     return as_status(step_run<__half>(a, s));
 }
+
+int fpde_diag_linear_lost(const fpde_linear_args* a, int ends, void* stream) { return forward(a, ends ? 2 : 1, stream); }
 
 unsigned int fpde_diag_linear_timeouts(void) { return march_mma_timeouts(); }
 

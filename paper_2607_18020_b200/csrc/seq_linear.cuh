@@ -29,6 +29,7 @@ struct March {
     int local_turned;
     bool local_there;              // another march's, which has been joined
     bool out_packed;               // rows of out start on 32 bytes
+    int lose;                      // a wait that nothing ends, in the march 1 or in the pass for the pieces' ends 2; 0 but in a test
 };
 
 // g^n for n >= 0, from 64 bits: rounded once, so that it stays exact enough when it is applied chunk after chunk.

@@ -434,6 +434,7 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
                 steps[k] = m.reversed ? pair(exp2_f32(2 * k * l), exp2_f32((2 * k + 1) * l)) : pair(exp2_f32((15 - 2 * k) * l), exp2_f32((14 - 2 * k) * l));
         };
         make_steps();
+        if (m.lose == 1) wait_for(bar(ENDED, 0), 0, gave_up);
         for (int c = 0; c < chunks; ++c) {
             wait_warp(DONE_G, c);
             if (gave_up) break;
@@ -565,7 +566,8 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_kernel(const __grid_cons
     if (lost) {                 // what has been issued has to end before the block does; the results are NaN
         if (tid == 0) atomicAdd(&g_linear_timeouts, 1u);
         bool late = false;
-        if (warp == CONTROL && lane == 0) {
+        // a commit stands for the products of its own thread: the one that issued them, as a whole warp always elects the same
+        if (warp == CONTROL && elected()) {
             mma_commit(bar(ENDED, 0));
             wait_for(bar(ENDED, 0), 0, late);
         }
@@ -706,6 +708,7 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_ends_kernel(const __grid
         const int row = quarter * 32 + lane, r = m.reversed ? N - 1 - row : row, share = warp / 4;
         const float w = m.gain * powers[N - 1 - r + m.shift];
         const __nv_bfloat162 w1 = __float2bfloat162_rn(w), w2 = __float2bfloat162_rn(w - __low2float(w1));
+        if (m.lose == 2) wait_for(bar(E_ENDED), 0, gave_up);
         for (int c = 0; c < chunks; ++c) {
             wait(E_FULL_B, c);
             // its place is free
@@ -754,7 +757,7 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_ends_kernel(const __grid
     if (lost) {                 // as above
         if (tid == 0) atomicAdd(&g_linear_timeouts, 1u);
         bool late = false;
-        if (warp == E_CONTROL && lane == 0) {
+        if (warp == E_CONTROL && elected()) {
             mma_commit(bar(E_ENDED));
             wait_for(bar(E_ENDED), 0, late);
         }
