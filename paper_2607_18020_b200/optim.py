@@ -42,7 +42,9 @@ def _args(grad, steps, eps):
     return a, g
 
 
-def _plan(key, grad, steps, eps):
+def _plan(name, grad, steps, eps):
+    eps = float(eps)                            # a tensor may hold another number in the next call
+    key = (name, steps, eps, _lay(grad))
     a = _plans.get(key)
     if a is None:
         a, g = _args(grad, steps, eps)
@@ -59,7 +61,7 @@ def orthogonalize(grad, steps=5, eps=1e-7):
     differentiable: a backward pass that reaches the result raises."""
     if wants_grad(grad):
         return ValuesOnly.apply(orthogonalize, grad, steps, eps)
-    a, g = _plan(("ortho", steps, eps, _lay(grad)), grad, steps, eps)
+    a, g = _plan("ortho", grad, steps, eps)
     dev = grad.device
     out = torch.empty_like(grad) if grad.is_contiguous() else torch.empty(grad.shape, dtype=grad.dtype, device=dev)
     a.grad, a.out = g.data_ptr(), out.data_ptr()
@@ -86,7 +88,7 @@ def muon_step(weight, grad, momentum, lr, momentum_decay=0.95, weight_decay=0.0,
         raise ValueError("weight, grad and momentum live on different devices")
     if not (weight.is_contiguous() and momentum.is_contiguous()):
         raise ValueError("weight and momentum are updated in place and must be contiguous")
-    a, g = _plan(("muon", steps, eps, _lay(grad)), grad, steps, eps)
+    a, g = _plan("muon", grad, steps, eps)
     dev = weight.device
     a.nesterov = int(nesterov)
     a.grad, a.weight, a.momentum = g.data_ptr(), weight.data_ptr(), momentum.data_ptr()

@@ -28,6 +28,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import numbers
 from typing import NamedTuple, Optional
 
 import torch
@@ -103,6 +104,15 @@ def _first(name, t, dims):
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
+
+
+def _number(name, x):
+    """A setting that a plan is kept by, and so a plain number: a tensor may hold another one in the next call."""
+    if type(x) is float:
+        return x
+    if not isinstance(x, numbers.Real):
+        raise ValueError("%s is of type %s, expected a number" % (name, type(x).__name__))
+    return float(x)
 
 
 def _new(like, shape=None):
@@ -453,6 +463,7 @@ def _head_args(norm, q, k, q_weight, k_weight, inv_freq, positions, offset, inte
 
 
 def _head_plan(kind, norm, q, k, q_weight, k_weight, inv_freq, positions, offset, interleaved, eps, gq=None, gk=None):
+    eps = _number("eps", eps)
     key = (kind, offset, bool(interleaved), eps, _lay(q), _lay(k), _lay(q_weight), _lay(k_weight), _lay(inv_freq), _lay(positions), _lay(gq), _lay(gk))
     t = (q, k, q_weight, k_weight, inv_freq, positions, gq, gk)
     a = _plans.get(key)
@@ -598,6 +609,7 @@ def _linear_args(q, k, v, log_decay, scale, state, step, go=None, gstate=None, b
 
 
 def _linear_plan(kind, q, k, v, log_decay, scale, state, go=None, gstate=None):
+    scale = _number("scale", scale)
     key = (kind, scale, _lay(q), _lay(k), _lay(v), _lay(log_decay), _lay(state), _lay(go), _lay(gstate))
     t = (q, k, v, log_decay, state, go, gstate)
     a = _plans.get(key)
