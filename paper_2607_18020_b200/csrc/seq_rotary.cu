@@ -51,6 +51,7 @@ struct HeadShape {
 struct Tile {
     int64_t batch[MOST_TILE], node[MOST_TILE];
     uint64_t position[MOST_TILE], turn[MOST_PAIRS];        // turn: 2^-64 turns a node
+    float sound[MOST_PAIRS];                               // 1, or NaN for a frequency that is infinite or NaN
     alignas(16) float cosine[MOST_ANGLES];
     alignas(16) float sine[MOST_ANGLES];
 };
@@ -62,6 +63,7 @@ __device__ __forceinline__ void open_turns(Tile& t, const HeadShape& s) {
         double turns = (double)s.inv_freq[i] * 0.15915494309189535;
         turns -= rint(turns);
         t.turn[i] = (uint64_t)__double2ll_rn(turns * 0x1p63) << 1;
+        t.sound[i] = turns - turns == 0. ? 1.f : NAN;          // a whole number cannot say it
     }
 }
 // The nodes of the tile that starts at node `first` of all rows.
@@ -78,11 +80,11 @@ __device__ __forceinline__ void open_nodes(Tile& t, const HeadShape& s, int64_t 
 // And the cosines and sines of their angles.
 __device__ __forceinline__ void open_angles(Tile& t, const HeadShape& s, int count) {
     for (int i = threadIdx.x; i < count * s.pairs; i += THREADS) {
-        const int n = i / s.pairs;
+        const int n = i / s.pairs, pair = i - n * s.pairs;
         float c, q;
-        sincospif((float)(int64_t)(t.position[n] * t.turn[i - n * s.pairs]) * 0x1p-63f, &q, &c);
-        t.cosine[i] = c;
-        t.sine[i] = q * s.sign;
+        sincospif((float)(int64_t)(t.position[n] * t.turn[pair]) * 0x1p-63f, &q, &c);
+        t.cosine[i] = c * t.sound[pair];
+        t.sine[i] = q * s.sign * t.sound[pair];
     }
     __syncthreads();
 }
