@@ -431,12 +431,12 @@ def _heads(a, name, t, dim, dt, dev):
     return t
 
 
-def _head_args(norm, q, k, q_weight, k_weight, inv_freq, positions, offset, interleaved, eps, gq=None, gk=None):
+def _head_args(norm, q, k, q_weight, k_weight, inv_freq, positions, interleaved, eps, gq=None, gk=None):
     """As _conv_args, for a rotation or norm; without norm the gradients come with gq and gk in the place of q and k."""
     _first("q", q, 4)
     dev, dt, dim = q.device, q.dtype, q.shape[3]
     a = B_.HeadArgs(dtype=B_.DTYPE_IDS[str(dt)], norm=int(norm), interleaved=int(interleaved), batch=q.shape[0], length=q.shape[1], q_heads=q.shape[2],
-                    k_heads=0 if k is None else k.shape[2], dim=dim, offset=offset, eps=eps)
+                    k_heads=0 if k is None else k.shape[2], dim=dim, eps=eps)
     if inv_freq is not None:
         if inv_freq.dim() != 1:
             raise ValueError("inv_freq has %d axes, expected 1 (pairs)" % inv_freq.dim())
@@ -464,15 +464,15 @@ def _head_args(norm, q, k, q_weight, k_weight, inv_freq, positions, offset, inte
 
 def _head_plan(kind, norm, q, k, q_weight, k_weight, inv_freq, positions, offset, interleaved, eps, gq=None, gk=None):
     eps = _number("eps", eps)
-    key = (kind, offset, bool(interleaved), eps, _lay(q), _lay(k), _lay(q_weight), _lay(k_weight), _lay(inv_freq), _lay(positions), _lay(gq), _lay(gk))
+    key = (kind, bool(interleaved), eps, _lay(q), _lay(k), _lay(q_weight), _lay(k_weight), _lay(inv_freq), _lay(positions), _lay(gq), _lay(gk))
     t = (q, k, q_weight, k_weight, inv_freq, positions, gq, gk)
     a = _plans.get(key)
     if a is None:
-        a, taken = _head_args(norm, *t[:6], offset, interleaved, eps, gq, gk)
+        a, taken = _head_args(norm, *t[:6], interleaved, eps, gq, gk)
         if _same(t, taken):
             _plans.keep(key, a)
         t = taken
-    a.inv_freq, a.positions = _ptr(t[4]), _ptr(t[5])
+    a.inv_freq, a.positions, a.offset = _ptr(t[4]), _ptr(t[5]), offset      # a march has another offset in every call
     return a, t
 
 

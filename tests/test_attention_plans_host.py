@@ -75,3 +75,16 @@ def test_the_optimiser_takes_the_eps_of_the_call(monkeypatch):
         optim.muon_step(w, g, m, 0.1, eps=eps)
         eps.mul_(0.5)
     assert queued == [0.5, 0.5, 0.25, 0.25]
+
+
+def test_a_march_by_offset_keeps_one_plan_a_call(calls):
+    """The position of a row that continues is another one in every call, and none of them drives out the plans of other operators."""
+    from paper_2607_18020_b200 import sequence as Q
+    x, taps = torch.zeros(1, 9, 16), torch.zeros(16, 4)
+    Q.causal_conv_fwd(x, taps)
+    conv = [k for k in Q._plans._plans]
+    assert len(conv) == 1
+    for t in range(600):
+        rotation(Q, t)
+    assert all(k in Q._plans._plans for k in conv) and len(Q._plans._plans) == 5
+    assert [a.offset for a in calls[1:]] == [t for t in range(600) for _ in range(4)]
