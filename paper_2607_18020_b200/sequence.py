@@ -115,6 +115,13 @@ def _number(name, x):
     return float(x)
 
 
+def _offset(x):
+    """A whole number that fits 64 bits: the argument block would take a larger one for what is left of it there."""
+    if not isinstance(x, numbers.Integral) or not -1 << 63 <= x < 1 << 63:
+        raise ValueError("offset is %r, expected a whole number of 64 bits" % (x,))
+    return int(x)
+
+
 def _new(like, shape=None):
     """A dense tensor of `like`'s type, shape (or `shape`) and device."""
     if like is None:
@@ -472,7 +479,7 @@ def _head_plan(kind, norm, q, k, q_weight, k_weight, inv_freq, positions, offset
         if _same(t, taken):
             _plans.keep(key, a)
         t = taken
-    a.inv_freq, a.positions, a.offset = _ptr(t[4]), _ptr(t[5]), offset      # a march has another offset in every call
+    a.inv_freq, a.positions, a.offset = _ptr(t[4]), _ptr(t[5]), _offset(offset)      # a march has another offset in every call
     return a, t
 
 

@@ -88,3 +88,19 @@ def test_a_march_by_offset_keeps_one_plan_a_call(calls):
         rotation(Q, t)
     assert all(k in Q._plans._plans for k in conv) and len(Q._plans._plans) == 5
     assert [a.offset for a in calls[1:]] == [t for t in range(600) for _ in range(4)]
+
+
+def test_offsets_are_whole_numbers_of_64_bits(calls):
+    from paper_2607_18020_b200 import sequence as Q
+    ends = (-2 ** 63, -1, 0, np.int64(7), 2 ** 63 - 1)
+    for x in ends:
+        rotation(Q, x)
+    assert [a.offset for a in calls] == [int(x) for x in ends for _ in range(4)]
+    calls.clear()
+    q, freq = torch.zeros(1, 9, 2, 16), torch.zeros(8)
+    for x in (2 ** 63, -2 ** 63 - 1, 2 ** 64, 1.0, "1", None, torch.tensor(3)):
+        for call in (lambda: Q.rotary_fwd(q, q, freq, offset=x), lambda: Q.rotary_bwd(q, q, freq, offset=x), lambda: Q.rotary(q, q, freq, offset=x),
+                     lambda: Q.norm_rotary_fwd(q, q, None, None, freq, offset=x), lambda: Q.norm_rotary_bwd(q, q, q, q, None, None, freq, offset=x)):
+            with pytest.raises(ValueError, match="offset"):
+                call()
+    assert not calls
