@@ -622,11 +622,12 @@ int fpde_head_rotary_bwd(const fpde_head_args* args, void* stream);
  * Gradients (fpde_linear_attention_bwd): from go, of o, and gstate_out, of state_out (zeros if NULL), to gq, gk, gv
  * and gstate (NULL: not wanted).  Nothing is kept between the passes.
  * Rows are split along their length where batch and heads do not fill the GPU; the workspace then holds a state for
- * each piece.  Infinities and NaN of a node reach no earlier node and no other head; from that node on the sums that they enter
+ * each piece.  Its size depends on the strides too: they have to be there when it is asked for, the pointers need not.
+ * Infinities and NaN of a node reach no earlier node and no other head; from that node on the sums that they enter
  * are infinite or NaN, not always the one of the two that a march through the nodes would give.
  *
  * Precision: states are fp32's, and products and sums are formed in 32 bits.  bf16 rows of some length (24 nodes of up to 128
- * features, 40 of 64, 193 of 32) that TMA can read (bases and strides of whole 16 bytes) take the tensor cores: there
+ * features, 40 of 64, 193 of 32) that TMA can read (bases and strides of whole 16 bytes, the nodes' not zero) take the tensor cores: there
  * g^n (q . k) of two nodes, and the state that an output reads, are rounded to bf16 once more, which leaves
  * about as much as the output's own rounding; the states handed on are sums of products that keep fp32's bits.
  */
@@ -720,7 +721,8 @@ int fpde_diag_orthogonalize_lost(const fpde_ortho_args* args, void* stream);
  *   orthogonalisation: product 0 is X X^T, 1 b S + c S S, 2 a X + P X, on 0 pairs of SMs, single ones with 1 128 or 2 64
  *   columns a tile, 3 or 4 those with the depth over 2 or 4 blocks; -1 also for matrices that stay on one SM;
  *   linear attention: the pieces that a row is cut into in the march 0 of o, 1 of gq, 2 of gv and gk; with a minus where the
- *   tensor cores take the products, if TMA can read the arrays.
+ *   tensor cores take the products (of both), if the arrays start on 16 bytes.  An array whose strides are all zero stands for dense rows
+ *   of whole 16 bytes.
  */
 int fpde_diag_scan_channels(const fpde_scan_args* args, int backward);
 int fpde_diag_scan_chunks(const fpde_scan_args* args, int backward);

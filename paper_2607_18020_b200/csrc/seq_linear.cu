@@ -432,18 +432,23 @@ int check_linear(const fpde_linear_args* a, bool step) {
 // arithmetic and tensor cores: 32 features, 192 nodes 143 and 155 us, 256 nodes 186 and 158; 64 features, 40 nodes 139 and 138, 96 nodes 231
 // and 144; 128 features, 24 nodes 400 and 261, 96 nodes 933 and 280.  fp16's range is too short for products of queries and
 // keys and for states, so its arrays are widened.
-bool on_tensor_cores(const fpde_linear_args* a) {
+bool on_tensor_cores(const fpde_linear_args* a, const March& m) {
     const int64_t widest = a->dk > a->dv ? a->dk : a->dv, enough = widest <= 32 ? 193 : widest <= 64 ? 40 : 24;
-    return a->dtype == FPDE_BF16 && a->length >= enough;
+    if (a->dtype != FPDE_BF16 || a->length < enough) return false;
+    for (const LinearView* x : {&m.a, &m.b, &m.c})
+        if (!aligned(x->p, 16) || !tile_steps(*x, a->heads, a->length, a->batch)) return false;
+    return true;
 }
 
 // Pieces of a row.  With more than one, all but the last are marched through twice, the first time for their ends alone, and the
 // states are joined in between.  The number with the least time of waves of blocks is taken; the figures are measured
 // microseconds of a chunk and of a block's start, and of two more launches and the join, which reads and writes a state for each piece.
-void cut(const fpde_linear_args* a, March& m, bool gradient) {
-    const bool mma = on_tensor_cores(a), wide = m.da > 64 || m.dc > 64;
-    const int chunk = mma ? MMA_CHUNK : C;
-    const double main = mma ? (wide ? 4.3 : 2.5) : 4.0, ends = mma ? (wide ? 2.2 : 1.2) : 2.0, start = mma ? 6. : 4.;
+// `other`: a march that shares the pieces is on the tensor cores.  If only one of the two is, the one in 32 bits, which takes longer,
+// decides, in whole chunks of the other.
+void cut(March& m, bool gradient, bool other) {
+    const bool mma = m.mma && other, wide = m.da > 64 || m.dc > 64;
+    const int chunk = m.mma || other ? MMA_CHUNK : C;
+    const double main = mma ? (wide ? 4.3 : 2.5) : 4.0 * (chunk / C), ends = mma ? (wide ? 2.2 : 1.2) : 2.0 * (chunk / C), start = mma ? 6. : 4.;
     const int64_t rows = m.batch * m.heads * (mma ? 1 : ceil_div(m.dc, 64)), slots = mma ? MMA_BLOCKS : 148 * 4, chunks = ceil_div(m.length, chunk);
     const double join = (double)m.batch * m.heads * m.da * m.dc * 8 / 5e6;
     const double first = gradient ? 2. / 3. : 1.;         // of three marches one uses another's states
@@ -466,6 +471,20 @@ void cut(const fpde_linear_args* a, March& m, bool gradient) {
 }
 
 size_t local_bytes(const March& m) { return m.pieces > 1 ? (size_t)m.batch * m.heads * m.pieces * m.da * m.dc * sizeof(float) : 0; }
+// For the march, and for what it becomes if arrays turn out to start on no multiple of 16 bytes.
+size_t most_bytes(const March& m, bool gradient, bool other) {
+    size_t most = 0;
+    for (const int mma : {0, 1})
+        for (const int shared : {0, 1}) {
+            if (mma > m.mma || shared > other) continue;
+            March as = m;
+            as.mma = mma;
+            cut(as, gradient, shared);
+            const size_t bytes = local_bytes(as);
+            if (bytes > most) most = bytes;
+        }
+    return most;
+}
 
 March march_of(const fpde_linear_args* a) {
     March m = {};
@@ -488,7 +507,8 @@ March march_o(const fpde_linear_args* a) {
     m.start = a->state;
     m.out = a->o;
     m.end = a->state_out;
-    cut(a, m, false);
+    m.mma = on_tensor_cores(a, m);
+    cut(m, false, m.mma);
     return m;
 }
 March march_gq(const fpde_linear_args* a) {
@@ -503,27 +523,12 @@ March march_gq(const fpde_linear_args* a) {
     m.start = a->state;
     m.start_turned = 1;
     m.out = a->gq;
-    cut(a, m, true);
+    m.mma = on_tensor_cores(a, m);
+    cut(m, true, m.mma);
     return m;
 }
-March march_gv(const fpde_linear_args* a) {
-    March m = march_of(a);
-    m.a = {a->k, a->k_batch, a->k_node, a->k_head};
-    m.b = {a->q, a->q_batch, a->q_node, a->q_head};
-    m.c = {a->go, a->go_batch, a->go_node, a->go_head};
-    m.da = (int)a->dk;
-    m.dc = (int)a->dv;
-    m.reversed = m.shift = 1;
-    m.near = m.gain = (float)a->scale;
-    m.far = 1.f;
-    m.start = a->gstate_out;
-    m.out = a->gv;
-    m.end = a->gstate;
-    cut(a, m, true);
-    return m;
-}
-// Starts from the states that gv's march has joined, turned.
-March march_gk(const fpde_linear_args* a, const March& gv) {
+// Starts from the states that gv's march has joined, turned; its pieces are that one's.
+March march_gk(const fpde_linear_args* a) {
     March m = march_of(a);
     m.a = {a->v, a->v_batch, a->v_node, a->v_head};
     m.b = {a->go, a->go_batch, a->go_node, a->go_head};
@@ -536,9 +541,25 @@ March march_gk(const fpde_linear_args* a, const March& gv) {
     m.start = a->gstate_out;
     m.start_turned = m.local_turned = 1;
     m.out = a->gk;
-    m.pieces = gv.pieces;
-    m.piece = gv.piece;
     m.local_there = true;
+    m.mma = on_tensor_cores(a, m);
+    return m;
+}
+March march_gv(const fpde_linear_args* a, const March& gk) {
+    March m = march_of(a);
+    m.a = {a->k, a->k_batch, a->k_node, a->k_head};
+    m.b = {a->q, a->q_batch, a->q_node, a->q_head};
+    m.c = {a->go, a->go_batch, a->go_node, a->go_head};
+    m.da = (int)a->dk;
+    m.dc = (int)a->dv;
+    m.reversed = m.shift = 1;
+    m.near = m.gain = (float)a->scale;
+    m.far = 1.f;
+    m.start = a->gstate_out;
+    m.out = a->gv;
+    m.end = a->gstate;
+    m.mma = on_tensor_cores(a, m);
+    cut(m, true, gk.mma);
     return m;
 }
 
@@ -574,7 +595,7 @@ cudaError_t march_run(const March& m, cudaStream_t st) {
 
 cudaError_t march_by_type(const fpde_linear_args* a, const March& m, cudaStream_t st) {
     cudaError_t e;
-    if (on_tensor_cores(a) && march_mma(m, st, &e)) return e;
+    if (m.mma && march_mma(m, st, &e)) return e;
     if (a->dtype == FPDE_F32) return march_run<float>(m, st);
     if (a->dtype == FPDE_BF16) return march_run<__nv_bfloat16>(m, st);
     return march_run<__half>(m, st);
@@ -613,8 +634,14 @@ extern "C" {
 
 size_t fpde_linear_attention_workspace_bytes(const fpde_linear_args* a, int backward) {
     if (check_linear_sizes(a) != FPDE_OK) return 0;
-    if (!backward) return local_bytes(march_o(a));
-    const size_t q = local_bytes(march_gq(a)), v = local_bytes(march_gv(a));
+    fpde_linear_args b = *a;
+    b.q = b.k = b.v = b.go = nullptr;              // the size is the same wherever the arrays start
+    if (!backward) {
+        const March m = march_o(&b);
+        return most_bytes(m, false, m.mma);
+    }
+    const March gq = march_gq(&b), gk = march_gk(&b);
+    const size_t q = most_bytes(gq, true, gq.mma), v = most_bytes(march_gv(&b, gk), true, gk.mma);
     return q > v ? q : v;
 }
 
@@ -646,9 +673,12 @@ int fpde_linear_attention_bwd(const fpde_linear_args* a, void* stream) {
     if ((st = check_workspace(a, 1)) != FPDE_OK) return st;
     const cudaStream_t s = (cudaStream_t)stream;
     cudaError_t e = march_by_type(a, march_gq(a), s);
-    const March gv = march_gv(a);
+    March gk = march_gk(a);
+    const March gv = march_gv(a, gk);
+    gk.pieces = gv.pieces;
+    gk.piece = gv.piece;
     if (e == cudaSuccess) e = march_by_type(a, gv, s);
-    if (e == cudaSuccess) e = march_by_type(a, march_gk(a, gv), s);
+    if (e == cudaSuccess) e = march_by_type(a, gk, s);
     return as_status(e);
 }
 
@@ -669,8 +699,21 @@ unsigned int fpde_diag_linear_timeouts(void) { return march_mma_timeouts(); }
 
 int fpde_diag_linear_form(const fpde_linear_args* a, int march) {
     if (check_linear_sizes(a) != FPDE_OK || march < 0 || march > 2) return 0;
-    const int pieces = (march == 0 ? march_o(a) : march == 1 ? march_gq(a) : march_gv(a)).pieces;
-    return on_tensor_cores(a) ? -pieces : pieces;
+    // an array without strides stands for dense rows of whole 16 bytes
+    fpde_linear_args b = *a;
+    b.q = b.k = b.v = b.go = nullptr;
+    const auto rows = [&](int64_t& batch, int64_t& node, int64_t& head, int64_t width) {
+        if (batch != 0 || node != 0 || head != 0) return;
+        head = ceil_div(width, 8) * 8;
+        node = head * b.heads;
+        batch = node * b.length;
+    };
+    rows(b.q_batch, b.q_node, b.q_head, b.dk);
+    rows(b.k_batch, b.k_node, b.k_head, b.dk);
+    rows(b.v_batch, b.v_node, b.v_head, b.dv);
+    rows(b.go_batch, b.go_node, b.go_head, b.dv);
+    const March gk = march_gk(&b), m = march == 0 ? march_o(&b) : march == 1 ? march_gq(&b) : march_gv(&b, gk);
+    return m.mma && (march < 2 || gk.mma) ? -m.pieces : m.pieces;
 }
 
 }  // extern "C"

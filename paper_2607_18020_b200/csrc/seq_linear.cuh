@@ -14,6 +14,7 @@ struct March {
     LinearView a, b, c;
     int64_t batch, length, heads;
     int da, dc;                    // features of a and b, and of c
+    bool mma;                      // on the tensor cores
     int reversed;                  // from the last node to the first
     int shift;
     float near, far, gain;
@@ -39,10 +40,12 @@ __device__ __forceinline__ double power(float log_decay, double n) { return n ==
 cudaError_t march_join(const March& m, cudaStream_t st);
 
 // The march of bf16 arrays on the tensor cores (seq_linear_mma.cu).  Its pieces are multiples of MMA_CHUNK nodes.  False, with
-// nothing launched: the copy engine cannot read one of the arrays (a start or stride that is no multiple of 16 bytes).
+// nothing launched: the copy engine cannot read one of the arrays (steps as below, or a start on no multiple of 16 bytes).
 constexpr int MMA_CHUNK = 128;
 constexpr int MMA_BLOCKS = 148;                      // resident on the GPU
 bool march_mma(const March& m, cudaStream_t st, cudaError_t* e);
+// Can the copy engine step through a bf16 array: strides of whole 16 bytes, or zero, but for the nodes', which a tile needs one by one.
+bool tile_steps(const LinearView& x, int64_t heads, int64_t length, int64_t batch);
 unsigned int march_mma_timeouts();
 
 }  // namespace fpde

@@ -780,13 +780,10 @@ __global__ void __launch_bounds__(THREADS, 1) march_mma_ends_kernel(const __grid
 bool tile_map(const LinearView& x, int width, int64_t heads, int64_t length, int64_t batch, CUtensorMap* map, int* head, int* row) {
     const EncodeTiledFn fn = tma_encode_fn();
     const int64_t strides[3] = {x.head, x.node, x.batch}, extents[3] = {heads, length, batch};
-    if (fn == nullptr || !aligned(x.p, 16)) return false;
+    if (fn == nullptr || !aligned(x.p, 16) || !tile_steps(x, heads, length, batch)) return false;
     cuuint64_t dims[4] = {(cuuint64_t)width}, bytes[3];
     for (int i = 0; i < 3; ++i) {
         const bool one = extents[i] == 1 || strides[i] == 0;
-        if (i == 1 && strides[i] == 0 && extents[i] > 1) return false;       // all nodes the same: the tile needs them one by one
-        if (!one && (strides[i] < 0 || strides[i] % 8 != 0 || strides[i] >= (1ll << 38))) return false;
-        if (extents[i] > 0x7fffffff - 2 * N) return false;
         dims[i + 1] = one ? 1 : (cuuint64_t)extents[i];
         bytes[i] = one ? 16 : (cuuint64_t)strides[i] * 2;
     }
@@ -824,6 +821,17 @@ cudaError_t run(const March& m, const Tiles& tiles, cudaStream_t st) {
 }
 
 }  // namespace
+
+bool tile_steps(const LinearView& x, int64_t heads, int64_t length, int64_t batch) {
+    const int64_t strides[3] = {x.head, x.node, x.batch}, extents[3] = {heads, length, batch};
+    for (int i = 0; i < 3; ++i) {
+        if (extents[i] > 0x7fffffff - 2 * N) return false;
+        if (extents[i] == 1) continue;
+        if (i == 1 && strides[i] == 0) return false;
+        if (strides[i] < 0 || strides[i] % 8 != 0 || strides[i] >= (1ll << 38)) return false;
+    }
+    return true;
+}
 
 bool march_mma(const March& given, cudaStream_t st, cudaError_t* e) {
     March m = given;
