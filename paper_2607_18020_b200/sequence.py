@@ -117,7 +117,7 @@ def _number(name, x):
 
 def _offset(x):
     """A whole number that fits 64 bits: the argument block would take a larger one for what is left of it there."""
-    if not isinstance(x, numbers.Integral) or not -1 << 63 <= x < 1 << 63:
+    if type(x) is not int and not isinstance(x, numbers.Integral) or not -1 << 63 <= x < 1 << 63:
         raise ValueError("offset is %r, expected a whole number of 64 bits" % (x,))
     return int(x)
 
