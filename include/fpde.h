@@ -574,7 +574,8 @@ int fpde_selective_scan_step(const fpde_scan_args* args, void* stream);
  *     y = u with its first 2 * pairs features turned: pair i by the angle position * inv_freq[i]
  * Pair i is (u[i], u[i + pairs]), interleaved: (u[2i], u[2i+1]); it becomes (a cos - b sin, b cos + a sin).  The
  * features behind 2 * pairs are not turned; pairs = 0 turns nothing.  position = offset + positions[b, t], or
- * offset + t.  The angle is formed and reduced in 64 bits, so far positions keep their digits.
+ * offset + t.  The angle is formed and reduced in 64 bits, so far positions keep their digits; a frequency that is infinite or
+ * NaN makes its pair NaN.  The mean is formed in fp32: heads whose squares leave its range have a norm of infinity or zero.
  *
  * q is (batch, length, q_heads, dim), k (batch, length, k_heads, dim), both views with contiguous features; k may be
  * NULL (k_heads 0).  Results and gradients are dense.
@@ -629,7 +630,9 @@ int fpde_head_rotary_bwd(const fpde_head_args* args, void* stream);
  * Precision: states are fp32's, and products and sums are formed in 32 bits.  bf16 rows of some length (24 nodes of up to 128
  * features, 40 of 64, 193 of 32) that TMA can read (bases and strides of whole 16 bytes, the nodes' not zero) take the tensor cores: there
  * g^n (q . k) of two nodes, and the state that an output reads, are rounded to bf16 once more, which leaves
- * about as much as the output's own rounding; the states handed on are sums of products that keep fp32's bits.
+ * about as much as the output's own rounding; the states handed on are sums of products that keep fp32's bits.  Where state_out or
+ * gstate is NULL the states of that march keep 16 bits instead, far below the rounding that they see as factors: other results
+ * may differ in their last bits from those of a call that wants it.
  */
 #define FPDE_LINEAR_MAX_DIM 128
 

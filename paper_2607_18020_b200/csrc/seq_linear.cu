@@ -430,8 +430,8 @@ int check_linear(const fpde_linear_args* a, bool step) {
 
 // A chunk there takes as long however few of its 128 nodes and 64 or 128 features there are.  2048 rows and heads, 32-bit
 // arithmetic and tensor cores: 32 features, 192 nodes 143 and 155 us, 256 nodes 186 and 158; 64 features, 40 nodes 139 and 138, 96 nodes 231
-// and 144; 128 features, 24 nodes 400 and 261, 96 nodes 933 and 280.  fp16's range is too short for products of queries and
-// keys and for states, so its arrays are widened.
+// and 144; 128 features, 24 nodes 400 and 261, 96 nodes 933 and 280.  fp16 arrays are widened to fp32: fp16 holds neither the products of
+// queries and keys nor the states, and as bf16 factors its values would be two parts each, which the march is not written for.
 bool on_tensor_cores(const fpde_linear_args* a, const March& m) {
     const int64_t widest = a->dk > a->dv ? a->dk : a->dv, enough = widest <= 32 ? 193 : widest <= 64 ? 40 : 24;
     if (a->dtype != FPDE_BF16 || a->length < enough) return false;
@@ -443,6 +443,7 @@ bool on_tensor_cores(const fpde_linear_args* a, const March& m) {
 // Pieces of a row.  With more than one, all but the last are marched through twice, the first time for their ends alone, and the
 // states are joined in between.  The number with the least time of waves of blocks is taken; the figures are measured
 // microseconds of a chunk and of a block's start, and of two more launches and the join, which reads and writes a state for each piece.
+// In 32 bits one figure stands for all widths: four blocks an SM, where 5, 3 or 2 are resident with up to 32, 64 and 128 features of a.
 // `other`: a march that shares the pieces is on the tensor cores.  If only one of the two is, the one in 32 bits, which takes longer,
 // decides, in whole chunks of the other.
 void cut(March& m, bool gradient, bool other) {

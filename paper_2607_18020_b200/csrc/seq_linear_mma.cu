@@ -19,8 +19,8 @@
 // threads for each lane of TMEM), one issues the products and one loads (TMA).  A tile's place takes the next chunk's as soon as
 // the products that read it are done.  (With all warps at the same step, one after the other, they wait for one another's
 // latencies: 11 800 cycles a chunk of 128 x 128 features at a quarter of the issue slots.)  A chunk of 128 x 128 features takes 7 700 to
-// 8 500 clocks, 3 072 of them products; no task bounds it alone.  8 x 2048 nodes of 32 heads of 128: 160 us, memory's floor 87;
-// 16384 nodes of 16 heads of 64: 74 us of 20.
+// 8 500 clocks, 3 072 of them products; no task bounds it alone.  A call of 8 x 2048 nodes of 32 heads of 128 takes 183 to 187 us, memory's
+// floor 87; 16384 nodes of 16 heads of 64, with their pieces' ends, 71 of 20.
 #include "mma_common.cuh"
 #include "seq_linear.cuh"
 

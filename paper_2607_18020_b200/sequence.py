@@ -495,7 +495,7 @@ def _head_fwd(kind, norm, q, k, q_weight, k_weight, inv_freq, positions, offset,
 def rotary_fwd(q, k, inv_freq, positions=None, offset=0, interleaved=False):
     """q (batch, length, heads, dim) and k (batch, length, k_heads, dim), or None, with the first 2 * len(inv_freq) features
     of each head turned: pair i, which is (x[i], x[i + pairs]), or interleaved (x[2i], x[2i + 1]), by the angle
-    position * inv_freq[i].  The position is offset + t, or offset + positions[b, t] (int64)."""
+    position * inv_freq[i].  The position is offset + t, or offset + positions[b, t] (int64); offset is a whole number of 64 bits."""
     return _head_fwd("rotary fwd", False, q, k, None, None, inv_freq, positions, offset, interleaved, 0.0)
 
 
@@ -512,7 +512,7 @@ def rotary_bwd(gq, gk, inv_freq, positions=None, offset=0, interleaved=False):
 
 def norm_rotary_fwd(q, k, q_weight=None, k_weight=None, inv_freq=None, positions=None, offset=0, interleaved=False, eps=1e-6):
     """rotary_fwd of x / sqrt(mean(x^2) + eps) * weight, the mean over each head's features; without inv_freq the norm
-    alone.  q_weight, k_weight: (dim), or None for ones."""
+    alone.  q_weight, k_weight: (dim), or None for ones; eps is a plain number."""
     return _head_fwd("norm fwd", True, q, k, q_weight, k_weight, inv_freq, positions, offset, interleaved, eps)
 
 
@@ -634,7 +634,8 @@ def linear_attention_fwd(q, k, v, log_decay, scale=1.0, state=None):
 
         S[t] = g S[t-1] + k[t] v[t]^T,  o[t] = scale * q[t] S[t],  S[-1] = state (batch, heads, dk, dv) or zeros
 
-    q and k: (batch, length, heads, dk), v: (batch, length, heads, dv), up to 128 features each; log_decay: (heads).
+    q and k: (batch, length, heads, dk), v: (batch, length, heads, dv), up to 128 features each; log_decay: (heads); scale: a plain
+    number.
     Returns (o (batch, length, heads, dv), the last state)."""
     return _linear_fwd(q, k, v, log_decay, scale, state, True)
 
